@@ -381,6 +381,68 @@ knn_status knn_mix_rrc(const int32_t *nbr_ids, const float *nbr_dists, const int
                        float *lambda_out, float *p_m, void *stream);
 
 /*
+ * The language model's own step around the mixture.  A step of nearest-
+ * neighbour speculation runs the language model over the next rows of each
+ * sequence: the token being decoded, or the draft tokens that knn_nest_step
+ * and knn_spec_verify then check (Section 3.4).  knn_kv_append puts the rows'
+ * keys and values into a paged cache, knn_tree_attention attends over it, and
+ * knn_sample draws a token from the model's logits or from the mixture's rows.
+ *
+ * Rows.  S sequences own the rows row_offsets[s] .. row_offsets[s+1]-1 (int64
+ * [S+1], device, monotone from 0); `rows` is the number the buffers hold, and
+ * rows from row_offsets[S] on (a batch padded to a fixed size) are neither
+ * read nor written.  A sequence may own no row.
+ *
+ * Cache.  k_cache and v_cache are [n_pages, kv_heads, page_size, head_dim];
+ * page_size is a power of two from 16 to 65536.  pages [S, table_width] int32
+ * (device) names each sequence's pages: its cache index c lies in page
+ * pages[s, c / page_size], slot c % page_size.  cache_lens [S] int32 (device)
+ * is the number of tokens of each sequence that are in the cache before the
+ * rows of this call, which take the indices cache_lens[s], cache_lens[s] + 1,
+ * ...  Entries of the table past a sequence's last page are not read by
+ * knn_kv_append and may hold anything; an entry outside [0, n_pages) is no
+ * page: nothing is written there and its keys are seen by no row.
+ *
+ * Element types are KNN_BF16 and KNN_F16; KNN_F32 is KNN_ERR_UNSUPPORTED
+ * except for knn_sample.  None of these calls copies to the host or depends on
+ * values that the host reads, so a captured graph replays on new lengths,
+ * tables and parameters.
+ */
+
+/* Largest number of query or key heads. */
+#define KNNLM_MAX_HEADS 1024
+
+/*
+ * knn_kv_append -- the rows' keys and values into the paged cache, with the
+ * position rotation of keys (and of queries, in the same pass).
+ *
+ *   q, k, v        dtype; element e of head h of row t lies at t * row_stride + h * head_stride + e (elements),
+ *                  so the parts of one projection's output are passed as they are.  q may be NULL, with
+ *                  q_heads 0 and q_out NULL.
+ *   positions      [rows] int32, the position of each row (a draft's depth in its tree, say), or NULL: its cache index.
+ *   inv_freq       [rot_dim / 2] fp32, or NULL with rot_dim 0: pair i of a head is turned by position * inv_freq[i]
+ *                  radians.  The product is formed in 64 bits, so far positions keep their angle.
+ *   source_rows    [rows] int32, or NULL: row t is read from row source_rows[t] of q, k and v (an accepted path
+ *                  appended once more over a tree's drafts); a row whose source lies outside [0, source_count) is
+ *                  left out: its slot of the cache and its row of q_out keep what they hold.
+ *   source_count   rows that q, k and v hold (>= rows without source_rows).
+ *   rot_dim        even, 0..head_dim: the first rot_dim elements of a head are rotated, in pairs (i, i + rot_dim / 2),
+ *                  or (2 i, 2 i + 1) with interleaved != 0; the others are copied.
+ *   q_out          [rows, q_heads, head_dim] dense; may be q itself where q is dense and source_rows NULL.
+ *   k_cache, v_cache   written at the rows' indices; nothing else of them is touched.  Where two rows name one slot
+ *                  (two sequences that share a page), its elements are of either.
+ * head_dim up to 1024 (KNN_ERR_UNSUPPORTED above).
+ */
+knn_status knn_kv_append(const void *q, const void *k, const void *v, const int64_t *row_offsets,
+                         const int32_t *cache_lens, const int32_t *pages, const int32_t *positions,
+                         const float *inv_freq, const int32_t *source_rows, int64_t rows, int64_t source_count,
+                         int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t rot_dim,
+                         int32_t interleaved, int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride,
+                         int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, int64_t n_pages,
+                         int64_t page_size, int64_t table_width, knn_dtype dtype, void *q_out, void *k_cache,
+                         void *v_cache, void *stream);
+
+/*
  * knn_stream_read -- a measurement aid, not a step of the method: one plain
  * read of `bytes` bytes of device memory at `buf` (16-byte aligned, a multiple
  * of 16 bytes) with the same 16-byte non-temporal loads the distance stage

@@ -1,0 +1,136 @@
+"""The language model's own step around the mixture: cache append, attention of drafts, sampling.
+
+Like the rest of the package this only marshals arguments; the HIP kernels
+behind include/knnlm.h do the work.  Each class keeps the buffers, the planning
+hints and the workspace of repeated calls; run() takes the tensors' contents as
+they are when the stream gets there, so it can be captured into a graph and
+replayed on new ones.  The function of each is a one-shot call.
+"""
+from __future__ import annotations
+
+import math
+from typing import Optional, Sequence, Tuple
+
+import torch
+
+from . import _lib
+from . import _dtype_code, _need, _ptr, _stream
+from ._lib import load
+
+
+def _on_device(first: torch.Tensor, **named: Optional[torch.Tensor]) -> int:
+    """Checks that the tensors given are on the current GPU (that of `first`) and returns its index."""
+    _need(first.is_cuda, "device tensors are needed")
+    for name, t in named.items():
+        if t is not None:
+            _need(t.is_cuda and t.device == first.device, f"{name} must be on {first.device}")
+    index = first.device.index
+    _need(index == torch.cuda.current_device(), f"the tensors are on {first.device}, which is not the current device")
+    return index
+
+
+def _flat(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...]):
+    if t is not None:
+        _need(t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous(),
+              f"{name}: contiguous {list(shape)} {dtype} tensor")
+
+
+class _Call:
+    """A call that is made again and again on one GPU; `_own`: the tensors that it allocated."""
+
+    def _keep(self, index: int, *own: torch.Tensor):
+        self._index = index
+        self._own = own
+        self._home = _stream(None)
+        self._known = {self._home}
+
+    def _handle(self, stream):
+        _need(torch.cuda.current_device() == self._index, f"made for cuda:{self._index}, which is not the current device")
+        h = _stream(stream)
+        if h not in self._known:  # the allocator has to know who else uses what this object allocated
+            if not torch.cuda.is_current_stream_capturing():
+                s = torch.cuda.ExternalStream(h) if h else torch.cuda.default_stream()
+                for t in self._own:
+                    t.record_stream(s)
+                self._known.add(h)
+        return h
+
+
+def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, row_offsets: torch.Tensor,
+           cache_lens: torch.Tensor) -> Tuple[int, int, int, int, int]:
+    """Checks the cache's tensors: (S, n_pages, kv_heads, page_size, head_dim)."""
+    _need(k_cache.dim() == 4 and k_cache.is_contiguous(), "k_cache: contiguous [n_pages, kv_heads, page_size, head_dim]")
+    _flat("v_cache", v_cache, k_cache.dtype, tuple(k_cache.shape))
+    _need(pages.dim() == 2, "pages: [S, table_width]")
+    _flat("pages", pages, torch.int32, tuple(pages.shape))
+    S = pages.shape[0]
+    _flat("row_offsets", row_offsets, torch.int64, (S + 1,))
+    _flat("cache_lens", cache_lens, torch.int32, (S,))
+    n_pages, kv_heads, page_size, d = k_cache.shape
+    return S, n_pages, kv_heads, page_size, d
+
+
+class KVAppend(_Call):
+    """knn_kv_append on these buffers: the rows' keys and values into the paged cache, keys and queries rotated.
+
+    k, v [source rows, kv_heads, d] and q [source rows, q_heads, d] (bf16 or f16) may be views with any row and head
+    stride, such as the parts of one projection's output; k_cache, v_cache [n_pages, kv_heads, page_size, d]; pages
+    [S, width] int32, row_offsets [S+1] int64, cache_lens [S] int32 as the header says.  positions [rows] int32
+    (default: the cache index); inv_freq [rotated elements / 2] fp32 (None: no rotation); interleaved: pairs
+    (2i, 2i+1); source_rows [rows] int32: the row that each row is read from.  q_out [rows, q_heads, d] is
+    allocated where it is not given (it may be q).
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                 pages: torch.Tensor, row_offsets: torch.Tensor, cache_lens: torch.Tensor,
+                 q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 positions: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                 interleaved: bool = False, source_rows: Optional[torch.Tensor] = None):
+        index = _on_device(k, v=v, k_cache=k_cache, v_cache=v_cache, pages=pages, row_offsets=row_offsets,
+                           cache_lens=cache_lens, q=q, q_out=q_out, positions=positions, inv_freq=inv_freq,
+                           source_rows=source_rows)
+        S, n_pages, kv_heads, page_size, d = _paged(k_cache, v_cache, pages, row_offsets, cache_lens)
+        source = k.shape[0]
+        for name, t in (("k", k), ("v", v)):
+            _need(t.dim() == 3 and t.dtype == k_cache.dtype and tuple(t.shape) == (source, kv_heads, d) and
+                  t.stride(2) == 1, f"{name}: [rows, {kv_heads}, {d}] {k_cache.dtype} with dense heads")
+        rows = source if source_rows is None else source_rows.numel()
+        _flat("source_rows", source_rows, torch.int32, (rows,))
+        _flat("positions", positions, torch.int32, (rows,))
+        q_heads, own = 0, ()
+        if q is not None:
+            _need(q.dim() == 3 and q.dtype == k.dtype and q.shape[0] == source and q.shape[2] == d and
+                  q.stride(2) == 1, f"q: [{source}, q_heads, {d}] {k.dtype} with dense heads")
+            q_heads = q.shape[1]
+            if q_out is None:
+                q_out = torch.empty((rows, q_heads, d), dtype=q.dtype, device=q.device)
+                own = (q_out,)
+            _flat("q_out", q_out, q.dtype, (rows, q_heads, d))
+        else:
+            _need(q_out is None, "q_out without q")
+        half = 0
+        if inv_freq is not None:
+            half = inv_freq.numel()
+            _flat("inv_freq", inv_freq, torch.float32, (half,))
+        self.q_out = q_out
+        self._tensors = (q, k, v, row_offsets, cache_lens, pages, positions, inv_freq, source_rows)
+        self._caches = (k_cache, v_cache)
+        strides = [t.stride(i) if t is not None else 0 for t in (q, k, v) for i in (0, 1)]
+        self._sizes = (rows, source, S, q_heads, kv_heads, d, 2 * half, int(bool(interleaved)), *strides, n_pages,
+                       page_size, pages.shape[1], _dtype_code(k))
+        self._keep(index, *own)
+
+    def run(self, stream=None) -> Optional[torch.Tensor]:
+        """One call; returns q_out (the rotated queries), valid after stream sync."""
+        h = self._handle(stream)
+        st = load().knn_kv_append(*map(_ptr, self._tensors), *self._sizes, _ptr(self.q_out),
+                                  *map(_ptr, self._caches), h)
+        _lib.check("knn_kv_append", st)
+        return self.q_out
+
+
+def kv_append(k, v, k_cache, v_cache, pages, row_offsets, cache_lens, q=None, q_out=None, positions=None,
+              inv_freq=None, interleaved=False, source_rows=None, stream=None):
+    """One-shot knn_kv_append: writes the caches and returns the rotated queries (None without q)."""
+    return KVAppend(k, v, k_cache, v_cache, pages, row_offsets, cache_lens, q, q_out, positions, inv_freq,
+                    interleaved, source_rows).run(stream)
