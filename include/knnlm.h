@@ -443,6 +443,50 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
                          void *v_cache, void *stream);
 
 /*
+ * knn_tree_attention -- the rows of drafts over the paged cache: row i of a
+ * sequence sees every key of the cached tokens, and of its sequence's rows the
+ * keys its mask names:
+ *
+ *   out = sum_j w_j v_j,   w = softmax over the keys seen of scale q.k_j.
+ *
+ * The rows' own keys and values are in the cache already (knn_kv_append with
+ * the same row_offsets and cache_lens).  One row a sequence is plain decoding,
+ * several without a mask are a chain (a span being verified, a piece of a
+ * prompt), several with one a tree of spans that share their beginnings.
+ *
+ *   q              dtype; element e of head h of row t at t * q_row_stride + h * q_head_stride + e.  Query head h
+ *                  reads key head h / (q_heads / kv_heads); q_heads is a multiple of kv_heads.
+ *   tree_mask      [rows, mask_words] uint32 or NULL: bit (j & 31) of word j >> 5 of row i set means that it sees its
+ *                  sequence's row j (itself only where its own bit is set); NULL: the rows up to itself.
+ *   max_rows       host hint: the most rows of a sequence (1 .. 65535, at most `rows`; 32 mask_words with a mask).
+ *   max_keys       host hint: at least cache_lens[s] + its rows, for every sequence; at most table_width * page_size.
+ *                  It decides how the work is split: a bound near the longest sequence is the fastest.
+ *   scale          finite; 1 / sqrt(head_dim) as a rule.
+ *   out            [rows, q_heads, head_dim] dtype, dense.  A row that sees no key gets 0.
+ *   lse            [rows, q_heads] fp32 or NULL: the natural logarithm of the weights' sum (-inf for such a row).
+ *   workspace      knn_tree_attention_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
+ *
+ * Sums, maxima and logarithms are in fp32; the weights are rounded to the
+ * element type for the product with v, and summed as rounded.  Results do not
+ * depend on the order in which workgroups run.  Keys and values that a row
+ * does not see may hold anything, infinities and NaN too; a value that is not
+ * finite makes NaN what sees it.  head_dim is 64, 128 or 256, q and the caches
+ * and out lie on 16 bytes and the strides are multiples of 8 elements
+ * (KNN_ERR_UNSUPPORTED otherwise).
+ */
+knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_cache, const int32_t *pages,
+                              const int64_t *row_offsets, const int32_t *cache_lens, const uint32_t *tree_mask,
+                              int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                              int64_t q_row_stride, int64_t q_head_stride, int64_t n_pages, int64_t page_size,
+                              int64_t table_width, int64_t mask_words, int64_t max_rows, int64_t max_keys,
+                              knn_dtype dtype, float scale, void *out, float *lse, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace knn_tree_attention needs for these sizes (0 if they are invalid). */
+size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                         int64_t max_rows, int64_t max_keys);
+
+/*
  * knn_stream_read -- a measurement aid, not a step of the method: one plain
  * read of `bytes` bytes of device memory at `buf` (16-byte aligned, a multiple
  * of 16 bytes) with the same 16-byte non-temporal loads the distance stage

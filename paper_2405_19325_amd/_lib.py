@@ -49,6 +49,8 @@ SIGNATURES: Dict[str, tuple] = {
     "knn_mix": (I, [P, P, P, P, P, P, I64, I64, I64, I32, F, F, P, P]),
     "knn_mix_rrc": (I, [P, P, P, P, P, P, I64, I64, I64, I32, F, F, F, P, P, P]),
     "knn_kv_append": (I, [P] * 9 + [I64] * 7 + [I32] + [I64] * 9 + [I, P, P, P, P]),
+    "knn_tree_attention": (I, [P] * 7 + [I64] * 13 + [I, F, P, P, P, SZ, P]),
+    "knn_tree_attention_workspace_size": (SZ, [I64] * 7),
     "knn_stream_read": (I, [P, SZ, P, P]),
     "knn_status_string": (ctypes.c_char_p, [I]),
     "knn_abi_version": (I, []),

@@ -1,0 +1,457 @@
+// Attention of the rows of drafts over a paged cache.
+//
+// Row i of a sequence with L cached tokens sees the keys j < L and, of the
+// drafts' keys L + j, those that its mask names (a chain: j <= i).  Per query
+// head, with x_j = scale q.k_j over the keys seen,
+//   out = sum_j exp(x_j - m) v_j / sum_j exp(x_j - m),   lse = m + log(sum).
+// One pass over the keys: a running reference m, and sums relative to it that
+// are scaled when it moves.  m need not be the maximum: it follows the maximum
+// only when that rises by more than 2^kSlack over it, so the weights stay
+// under 2^kSlack, far inside the range of either type, and most tiles neither
+// reduce a maximum over lanes nor scale anything.
+//
+// All query heads of a key head and all rows of a sequence read the same keys,
+// so they are the columns of one matrix product: S^T = K Q^T with 16 keys x 16
+// columns per matrix instruction.  A lane then holds 4 consecutive keys of one
+// column, which is what the second product O^T = V^T P^T wants of its right
+// operand, in an order of the keys that the left operand follows: the weights
+// never leave the registers.  V^T comes out of LDS by the transposing read.
+// The row of ones in front of V sums the weights as they were rounded for the
+// product, so that they sum to one.
+#include "lm_internal.h"
+#include "mfma_device.h"
+
+namespace knnlm {
+
+namespace {
+
+constexpr float kFloor = -1.0e30f;  // reference before the first key
+constexpr float kSlack = 8.0f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+// What a workgroup works on.
+struct Tile {
+    int64_t r0;      // first row of the sequence
+    int n;           // its rows
+    int64_t length;  // cached tokens
+    int64_t total;   // keys
+};
+
+__device__ __forceinline__ Tile tile_of(const AttendArgs &a, int64_t s) {
+    Tile t;
+    t.r0 = a.row_offsets[s];
+    int64_t r1 = a.row_offsets[s + 1];
+    if (r1 > a.rows) r1 = a.rows;
+    const int64_t n = r1 - t.r0;
+    t.n = static_cast<int>(n < 0 ? 0 : n > a.max_rows ? a.max_rows : n);
+    const int64_t len = a.cache_lens[s];
+    t.length = len < 0 ? 0 : len;
+    t.total = t.length + t.n;
+    if (t.total > a.max_keys) t.total = a.max_keys;
+    const int64_t room = a.cache.table_width << a.cache.page_log2;
+    if (t.total > room) t.total = room;
+    return t;
+}
+
+template <knn_dtype DT>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {  // to nearest, ties to even
+    if constexpr (DT == KNN_BF16) {
+        const bf16x2_t v = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+        return __builtin_bit_cast(uint32_t, v);
+    } else {
+        const f16x2_t v = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+}
+
+// 16-byte chunk c of row r of a tile in LDS lies at chunk c ^ spread(r): the 8
+// rows that a product's operand read takes at once, and the 4 rows x 2 chunks
+// of a transposing read, then fall on different banks.
+__device__ __forceinline__ int spread(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+// Four 16-bit elements of one column: lane l of each 16 gets column l of the 4
+// rows whose 8-byte pieces the 16 lanes point at.
+__device__ __forceinline__ u32x2_t read_transposed(uint32_t lds) {
+    const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        reinterpret_cast<__attribute__((address_space(3))) s16x4_t *>(static_cast<uintptr_t>(lds)));
+    return __builtin_bit_cast(u32x2_t, v);
+}
+
+// The 16-bit elements of w that are infinite or NaN: as a word with 0xffff there.
+template <knn_dtype DT>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    constexpr uint32_t kExp = DT == KNN_BF16 ? 0x7f80u : 0x7c00u;
+    return ((w & kExp) == kExp ? 0xffffu : 0u) | (((w >> 16) & kExp) == kExp ? 0xffff0000u : 0u);
+}
+
+template <int D>
+struct Shape {
+    static constexpr int W = D == 256 ? 2 : 4;         // waves of a workgroup, each on keys of its own
+    static constexpr int ROW = 2 * D;                  // bytes of a key
+    static constexpr int HALF = 32 * ROW;              // of 32 keys: one stage's K, then its V
+    static constexpr int STAGES = 2;
+    static constexpr int LOADS = HALF / 1024;          // wave loads of one half
+    static constexpr int LANES = ROW / 16;             // lanes of a load on one key
+    static constexpr int PER = 64 / LANES;             // keys of one load
+    static constexpr size_t LDS = static_cast<size_t>(W) * STAGES * 2 * HALF;
+};
+
+// W waves share NT x 16 columns; wave w takes the 32-key tiles w, w + W, ... of
+// the workgroup's range and keeps its own reference and sums, joined at the
+// end.  Each wave fills its own two stages by loads straight to LDS, one tile
+// ahead, and waits only for its own loads: no barrier in the loop.
+template <knn_dtype DT, int D, int NT>
+__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t splits, int64_t chunk,
+                                                           float *part, float *part_ml) {
+    using Sh = Shape<D>;
+    constexpr int W = Sh::W, KK = D / 32, DB = D / 16, COLS = 16 * NT;
+    extern __shared__ __align__(16) u32x4_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quad = lane >> 4;
+
+    int64_t b = blockIdx.x;
+    const int64_t split = b % splits;
+    b /= splits;
+    const int64_t ct = b % tiles;
+    b /= tiles;
+    const int h = static_cast<int>(b % a.kv_heads);
+    const int64_t s = b / a.kv_heads;
+    const int g = a.q_heads / a.kv_heads;
+    const Tile t = tile_of(a, s);
+    const int64_t c0 = ct * COLS, cols = static_cast<int64_t>(t.n) * g;
+    if (c0 >= cols) return;
+    // the keys of this range that any of the columns sees
+    int64_t end = t.total;
+    if (a.tree_mask == nullptr) {
+        const int64_t last = (c0 + COLS - 1 < cols ? c0 + COLS - 1 : cols - 1) / g;
+        if (t.length + last + 1 < end) end = t.length + last + 1;
+    }
+    const int64_t k0 = split * chunk;
+    if (splits > 1 && k0 >= t.total) return;
+    if (k0 + chunk < end) end = k0 + chunk;
+
+    // Columns: queries as the right operand, lane = (column, 8 elements a quad).
+    u32x4_t qr[NT][KK];
+    int row_of[NT];
+    bool live[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int64_t c = c0 + 16 * i + col;
+        live[i] = c < cols;
+        row_of[i] = live[i] ? static_cast<int>(c / g) : 0;
+        const uint16_t *q = static_cast<const uint16_t *>(a.q) + (t.r0 + row_of[i]) * a.q_row +
+                            (h * g + (live[i] ? static_cast<int>(c % g) : 0)) * a.q_head;
+#pragma unroll
+        for (int k = 0; k < KK; ++k) qr[i][k] = *reinterpret_cast<const u32x4_t *>(q + 32 * k + 8 * quad);
+    }
+
+    f32x4_t o[NT][DB], sum[NT];
+    float m[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        m[i] = kFloor;
+        sum[i] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[i][d] = f32x4_t{0, 0, 0, 0};
+    }
+
+    const float c2 = a.scale * kLog2e;
+    const uint32_t mine =
+        __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * static_cast<uint32_t>(Sh::STAGES * 2 * Sh::HALF);
+    const int64_t n_tiles = end > k0 ? (end - k0 + 31) / 32 : 0;
+    const int64_t own = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // this wave's tiles
+    const int32_t *table = a.cache.pages + s * a.cache.table_width;
+    const int page_log2 = a.cache.page_log2;
+    const int64_t last_key = end - 1;
+    const int64_t head_bytes = static_cast<int64_t>(h) * Sh::ROW << page_log2;
+    const int64_t page_bytes = static_cast<int64_t>(a.kv_heads) * Sh::ROW << page_log2;
+    // Lane l keeps the page of half l & 1 of this wave's tile l / 2 from tile `held` on.
+    int32_t page_reg = 0;
+    auto hold_pages = [&](int64_t held) {
+        int64_t key = k0 + 32 * (wave + W * (held + (lane >> 1))) + 16 * (lane & 1);
+        key = key < last_key ? key : last_key;
+        page_reg = table[key >> page_log2];
+    };
+    auto page_of = [&](int64_t tile, int half) {
+        return __builtin_amdgcn_readlane(page_reg, 2 * static_cast<int>(tile & 31) + half);
+    };
+    // Tile `i` of this wave into stage i & 1.  Keys past the last one are read as the last one.
+    auto fill = [&](int64_t i) {
+        const int64_t key = k0 + 32 * (wave + W * i);
+        const uint32_t to = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            int64_t kb = key + 16 * half;
+            int32_t page = page_of(i, half);
+            if (page < 0 || page >= a.cache.n_pages) page = 0;
+            if (kb > last_key) kb = last_key & ~int64_t{15};
+            const int rows = last_key - kb < 15 ? static_cast<int>(last_key - kb) : 15;  // the last row there is
+            const int64_t at = page * page_bytes + head_bytes + (kb & ((int64_t{1} << page_log2) - 1)) * Sh::ROW;
+            const char *kp = static_cast<const char *>(a.k_cache) + at;
+            const char *vp = static_cast<const char *>(a.v_cache) + at;
+#pragma unroll
+            for (int j = 0; j < Sh::LOADS / 2; ++j) {
+                const int r = j * Sh::PER + lane / Sh::LANES;
+                const int from = r < rows ? r : rows;
+                const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread(r));
+                load_to_lds_16(kp, off, to + half * (Sh::HALF / 2) + j * 1024);
+                load_to_lds_16(vp, off, to + Sh::HALF + half * (Sh::HALF / 2) + j * 1024);
+            }
+        }
+    };
+
+    if (own > 0) {
+        hold_pages(0);
+        fill(0);
+    }
+    for (int64_t i = 0; i < own; ++i) {
+        const int32_t page_a = page_of(i, 0), page_b = page_of(i, 1);
+        if (i + 1 < own) {
+            if (((i + 1) & 31) == 0) hold_pages(i + 1);
+            fill(i + 1);
+            __builtin_amdgcn_s_waitcnt(vmcnt_encoding<2 * Sh::LOADS>());
+        } else {
+            __builtin_amdgcn_s_waitcnt(kVmcntZero);
+        }
+        asm volatile("" ::: "memory");
+        const uint32_t kt = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF), vt = kt + Sh::HALF;
+        const int64_t key = k0 + 32 * (wave + W * i);
+
+        f32x4_t x[2][NT];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[half][n] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < KK; ++k) {
+                const u32x4_t kr = *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t *>(
+                    static_cast<uintptr_t>(kt + (16 * half + col) * Sh::ROW + 16 * ((4 * k + quad) ^ spread(col))));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[half][n] = mfma16<DT>(kr, qr[n][k], x[half][n]);
+            }
+        }
+        // Keys that not every column sees: drafts, keys past the end, keys without a page.
+        const bool real_a = page_a >= 0 && page_a < a.cache.n_pages, real_b = page_b >= 0 && page_b < a.cache.n_pages;
+        const bool all = key + 32 <= (t.length < end ? t.length : end) && real_a && real_b;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[half][n][j] *= c2;
+        if (!all) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int64_t at = key + 16 * half + 4 * quad + j;
+                        bool sees = at < end && (half == 0 ? real_a : real_b);
+                        if (sees && at >= t.length) {
+                            const int64_t draft = at - t.length;
+                            if (a.tree_mask == nullptr) {
+                                sees = draft <= row_of[n];
+                            } else {
+                                sees = (draft >> 5) < a.mask_words &&
+                                       ((a.tree_mask[(t.r0 + row_of[n]) * a.mask_words + (draft >> 5)] >> (draft & 31)) & 1u) != 0u;
+                            }
+                        }
+                        x[half][n][j] = sees ? x[half][n][j] : -INFINITY;
+                    }
+        }
+        u32x4_t p[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float top = fmaxf(fmaxf(fmaxf(x[0][n][0], x[0][n][1]), fmaxf(x[0][n][2], x[0][n][3])),
+                              fmaxf(fmaxf(x[1][n][0], x[1][n][1]), fmaxf(x[1][n][2], x[1][n][3])));
+            if (__any(top > m[n] + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float to = fmaxf(m[n], top);
+                const float by = exp2f(m[n] - to);
+                m[n] = to;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[n][j] *= by;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[n][d][j] *= by;
+            }
+            float e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(x[j >> 2][n][j & 3] - m[n]);
+            p[n] = u32x4_t{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7])};
+        }
+        constexpr uint32_t kOne = DT == KNN_BF16 ? 0x3f803f80u : 0x3c003c00u;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sum[n] = mfma16<DT>(u32x4_t{kOne, kOne, kOne, kOne}, p[n], sum[n]);
+        const int vrow = 4 * quad + (col >> 2);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            const uint32_t at = vt + vrow * Sh::ROW + 16 * ((2 * d + ((col >> 1) & 1)) ^ spread(vrow)) + 8 * (col & 1);
+            const u32x2_t va = read_transposed(at), vb = read_transposed(at + 16 * Sh::ROW);
+            u32x4_t v = {va.x, va.y, vb.x, vb.y};
+            if (!all) {
+                // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such
+                // elements are left out of the product, and make NaN what sees them.
+                const u32x4_t bad = {not_finite<DT>(v.x), not_finite<DT>(v.y), not_finite<DT>(v.z), not_finite<DT>(v.w)};
+                if (__any((bad.x | bad.y | bad.z | bad.w) != 0u)) {
+                    v &= ~bad;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const f32x4_t seen = mfma16<DT>(bad & kOne, p[n], f32x4_t{0, 0, 0, 0});
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[n][d][j] = seen[j] > 0.0f ? __builtin_nanf("") : o[n][d][j];
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[n], o[n][d]);
+        }
+        // the stage is read: the next round's loads may overwrite it
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+
+    // Join the waves: references first, then each one's sums relative to the common reference.
+    __syncthreads();  // every wave is done with its stages (its loads have landed)
+    constexpr int PITCH = D + 4;
+    float *stat = reinterpret_cast<float *>(lds);    // [2][W][COLS]: reference, sum
+    float *acc = stat + 2 * W * COLS;                // [W][COLS][PITCH]
+    static_assert((2 * W * COLS + W * COLS * PITCH) * sizeof(float) <= Sh::LDS, "the join fits the stages");
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (quad == 0) {
+            stat[wave * COLS + 16 * n + col] = m[n];
+            stat[W * COLS + wave * COLS + 16 * n + col] = sum[n][0];
+        }
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+            *reinterpret_cast<f32x4_t *>(acc + (wave * COLS + 16 * n + col) * PITCH + 16 * d + 4 * quad) = o[n][d];
+    }
+    __syncthreads();
+    const int64_t heads = a.q_heads;
+    for (int i = threadIdx.x; i < COLS * (D / 4); i += W * 64) {
+        const int c = i / (D / 4), d = i % (D / 4) * 4;
+        if (c0 + c >= cols) continue;
+        float top = kFloor;
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w * COLS + c]);
+        float l = 0.0f;
+        f32x4_t r{0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float by = exp2f(stat[w * COLS + c] - top);
+            const float lw = stat[W * COLS + w * COLS + c];
+            l += by * lw;
+            r += by * *reinterpret_cast<const f32x4_t *>(acc + (w * COLS + c) * PITCH + d);
+        }
+        const int64_t at = (t.r0 + (c0 + c) / g) * heads + h * g + (c0 + c) % g;  // (row, query head)
+        if (splits > 1) {
+            const int64_t to = split * a.rows * heads + at;
+            if (d == 0) {
+                part_ml[2 * to] = top;
+                part_ml[2 * to + 1] = l;
+            }
+            *reinterpret_cast<f32x4_t *>(part + to * D + d) = r;
+        } else {
+            const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // no key: 0; NaN stays
+            *reinterpret_cast<u32x2_t *>(static_cast<uint16_t *>(a.out) + at * D + d) =
+                u32x2_t{pack2<DT>(r[0] * by, r[1] * by), pack2<DT>(r[2] * by, r[3] * by)};
+            if (d == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+        }
+    }
+}
+
+// Joins the ranges of a (row, query head), one wave each.
+template <knn_dtype DT, int D>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t splits, int64_t chunk, const float *part,
+                                                     const float *part_ml) {
+    constexpr int PER = D / 64;  // elements of a lane
+    const int lane = threadIdx.x & 63;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // (row, query head)
+    const int64_t heads = a.q_heads, row = at / heads;
+    if (row >= a.rows || row >= a.row_offsets[a.S]) return;  // the whole wave
+    const int64_t s = set_of_query_wave(a.row_offsets, a.S, row);
+    const Tile t = tile_of(a, s);
+    if (row - t.r0 >= t.n) return;
+    const int64_t n = t.total > 0 ? (t.total + chunk - 1) / chunk : 1, plane = a.rows * heads;
+    float top = kFloor;
+    for (int64_t i = lane; i < n; i += 64) top = fmaxf(top, part_ml[2 * (i * plane + at)]);
+    top = wave_allmax(top);
+    float l = 0.0f, r[PER] = {};
+    for (int64_t i = 0; i < n; ++i) {
+        const float by = exp2f(part_ml[2 * (i * plane + at)] - top);
+        l += by * part_ml[2 * (i * plane + at) + 1];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) r[j] += by * part[(i * plane + at) * D + lane * PER + j];
+    }
+    const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    uint16_t *out = static_cast<uint16_t *>(a.out) + at * D + lane * PER;
+    if constexpr (PER == 1) {
+        out[0] = static_cast<uint16_t>(pack2<DT>(r[0] * by, 0.0f));
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER; j += 2) *reinterpret_cast<uint32_t *>(out + j) = pack2<DT>(r[j] * by, r[j + 1] * by);
+    }
+    if (lane == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+}
+
+template <knn_dtype DT, int D>
+hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *part_ml, hipStream_t stream) {
+    const int64_t blocks = a.S * a.kv_heads * p.tiles * p.splits;
+    const int64_t joins = (a.rows * a.q_heads + 3) / 4;
+    if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const dim3 grid(static_cast<unsigned>(blocks)), threads(Shape<D>::W * 64);
+    if (p.cols == 16)
+        k_attend<DT, D, 1><<<grid, threads, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+    else
+        k_attend<DT, D, 2><<<grid, threads, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+    if (p.splits > 1)
+        k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.splits, p.chunk, part, part_ml);
+    return hipGetLastError();
+}
+
+template <knn_dtype DT>
+hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *part_ml, hipStream_t stream) {
+    switch (a.head_dim) {
+    case 64: return launch<DT, 64>(a, p, part, part_ml, stream);
+    case 128: return launch<DT, 128>(a, p, part, part_ml, stream);
+    default: return launch<DT, 256>(a, p, part, part_ml, stream);
+    }
+}
+
+}  // namespace
+
+AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_rows,
+                       int64_t max_keys) {
+    AttendPlan p{};
+    const int64_t cols = max_rows * (q_heads / kv_heads);
+    p.cols = cols <= 16 ? 16 : 32;
+    p.tiles = (cols + p.cols - 1) / p.cols;
+    // Two workgroups a CU, each on 256 keys or more.
+    const int64_t base = S * kv_heads * p.tiles, most = (max_keys + 255) / 256;
+    p.splits = (512 + base - 1) / base;
+    if (p.splits > most) p.splits = most;
+    if (p.splits > 256) p.splits = 256;
+    p.chunk = ((max_keys + p.splits - 1) / p.splits + 127) / 128 * 128;
+    p.splits = (max_keys + p.chunk - 1) / p.chunk;
+    const size_t cells = p.splits > 1 ? static_cast<size_t>(p.splits) * static_cast<size_t>(rows * q_heads) : 0;
+    p.off_ml = cells * static_cast<size_t>(head_dim) * sizeof(float);
+    p.total = p.off_ml + cells * 2 * sizeof(float);
+    return p;
+}
+
+hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, knn_dtype dtype, void *workspace,
+                         hipStream_t stream) {
+    float *part = static_cast<float *>(workspace);
+    float *part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.off_ml);
+    return dtype == KNN_BF16 ? launch<KNN_BF16>(a, p, part, part_ml, stream)
+                             : launch<KNN_F16>(a, p, part, part_ml, stream);
+}
+
+}  // namespace knnlm

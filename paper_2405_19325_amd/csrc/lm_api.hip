@@ -35,9 +35,65 @@ PagedCache paged(const int32_t *pages, int64_t n_pages, int64_t page_size, int64
     return PagedCache{pages, n_pages, table_width, log2};
 }
 
+// Whether an attention call's sizes are served; KNN_OK or the error.
+knn_status check_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_rows,
+                        int64_t max_keys) {
+    if (rows < 1 || S < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads != 0) return KNN_ERR_INVALID_ARG;
+    if (max_rows < 1 || max_rows > rows || max_keys < 1) return KNN_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return KNN_ERR_UNSUPPORTED;
+    if (rows > 0x7fffffff || max_rows > 65535 || max_keys > 0x7fffffff || q_heads > KNNLM_MAX_HEADS || S > 0x7fffffff)
+        return KNN_ERR_UNSUPPORTED;
+    return KNN_OK;
+}
+
+bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
 }  // namespace
 
 extern "C" {
+
+size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                         int64_t max_rows, int64_t max_keys) {
+    if (check_attend(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys) != KNN_OK) return 0;
+    const size_t need = plan_attend(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys).total;
+    return need < 256 ? 256 : (need + 255) / 256 * 256;
+}
+
+knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_cache, const int32_t *pages,
+                              const int64_t *row_offsets, const int32_t *cache_lens, const uint32_t *tree_mask,
+                              int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                              int64_t q_row_stride, int64_t q_head_stride, int64_t n_pages, int64_t page_size,
+                              int64_t table_width, int64_t mask_words, int64_t max_rows, int64_t max_keys,
+                              knn_dtype dtype, float scale, void *out, float *lse, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    if (!q || !k_cache || !v_cache || !pages || !row_offsets || !cache_lens || !out) return KNN_ERR_INVALID_ARG;
+    knn_status st = check_cache(S, kv_heads, head_dim, n_pages, page_size, table_width, dtype);
+    if (st != KNN_OK) return st;
+    st = check_attend(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys);
+    if (st != KNN_OK) return st;
+    if (max_keys > table_width * page_size || !isfinite(scale) || q_row_stride < 0 || q_head_stride < 0)
+        return KNN_ERR_INVALID_ARG;
+    if (tree_mask != nullptr && mask_words * 32 < max_rows) return KNN_ERR_INVALID_ARG;
+    if ((q_row_stride | q_head_stride) % 8 != 0 || !aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
+        !aligned(out, 16))
+        return KNN_ERR_UNSUPPORTED;
+    if (!workspace || !aligned(workspace, 256) ||
+        workspace_bytes < knn_tree_attention_workspace_size(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys))
+        return KNN_ERR_WORKSPACE;
+    AttendArgs a{};
+    a.q = q, a.k_cache = k_cache, a.v_cache = v_cache;
+    a.row_offsets = row_offsets, a.cache_lens = cache_lens, a.tree_mask = tree_mask;
+    a.rows = rows, a.S = S;
+    a.q_heads = static_cast<int>(q_heads), a.kv_heads = static_cast<int>(kv_heads);
+    a.head_dim = static_cast<int>(head_dim);
+    a.q_row = q_row_stride, a.q_head = q_head_stride;
+    a.cache = paged(pages, n_pages, page_size, table_width);
+    a.mask_words = mask_words, a.max_rows = max_rows, a.max_keys = max_keys;
+    a.scale = scale;
+    a.out = out, a.lse = lse;
+    return status_of(launch_attend(a, plan_attend(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys), dtype,
+                                   workspace, static_cast<hipStream_t>(stream)));
+}
 
 knn_status knn_kv_append(const void *q, const void *k, const void *v, const int64_t *row_offsets,
                          const int32_t *cache_lens, const int32_t *pages, const int32_t *positions,

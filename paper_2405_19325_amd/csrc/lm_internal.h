@@ -33,6 +33,39 @@ struct AppendArgs {
     void *q_out, *k_cache, *v_cache;
 };
 
+struct AttendArgs {
+    const void *q;  // [rows, q_heads, head_dim], rows q_row elements apart, heads q_head
+    const void *k_cache, *v_cache;
+    const int64_t *row_offsets;
+    const int32_t *cache_lens;
+    const uint32_t *tree_mask;  // [rows, mask_words] or null: a chain
+    int64_t rows, S;
+    int q_heads, kv_heads, head_dim;
+    int64_t q_row, q_head;
+    PagedCache cache;
+    int64_t mask_words;
+    int64_t max_rows, max_keys;
+    float scale;
+    void *out;   // [rows, q_heads, head_dim]
+    float *lse;  // [rows, q_heads] or null
+};
+
+// How an attention call is cut: column tiles of `cols` (row, query head) pairs
+// of one key head, and `splits` ranges of `chunk` keys, joined by a second
+// launch where there are several.
+struct AttendPlan {
+    int cols;
+    int64_t tiles;
+    int64_t splits;
+    int64_t chunk;
+    size_t off_ml, total;  // workspace: the ranges' outputs, then (maximum, sum)
+};
+
+AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_rows,
+                       int64_t max_keys);
+hipError_t launch_attend(const AttendArgs &args, const AttendPlan &plan, knn_dtype dtype, void *workspace,
+                         hipStream_t stream);
+
 hipError_t launch_kv_append(const AppendArgs &args, knn_dtype dtype, hipStream_t stream);
 
 }  // namespace knnlm

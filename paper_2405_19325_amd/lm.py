@@ -134,3 +134,85 @@ def kv_append(k, v, k_cache, v_cache, pages, row_offsets, cache_lens, q=None, q_
     """One-shot knn_kv_append: writes the caches and returns the rotated queries (None without q)."""
     return KVAppend(k, v, k_cache, v_cache, pages, row_offsets, cache_lens, q, q_out, positions, inv_freq,
                     interleaved, source_rows).run(stream)
+
+
+def tree_words(parents: Sequence[int], device) -> torch.Tensor:
+    """The masks of one sequence's rows as knn_tree_attention reads them, [rows, words] int32: every row sees itself
+    and its ancestors, parents[i] < i being the row that row i hangs under (-1: none)."""
+    n = len(parents)
+    words = torch.zeros((n, (n + 31) // 32), dtype=torch.int64)
+    for i, p in enumerate(parents):
+        _need(-1 <= p < i, "parents: each row's parent comes before it")
+        if p >= 0:
+            words[i] = words[p]
+        words[i, i // 32] |= 1 << (i % 32)
+    return (words - ((words >> 31) << 32)).to(torch.int32).to(device)
+
+
+class TreeAttention(_Call):
+    """knn_tree_attention on these buffers: rows of drafts over the paged cache.
+
+    q [rows, q_heads, d] (bf16 or f16; any row and head stride that is a multiple of 8), the cache's tensors as in
+    KVAppend.  max_rows and max_keys bound the rows of a sequence and its tokens with them; where they are not given
+    they come from the tensors' present contents, copied to the host once.  tree_mask [rows, words] int32 (see
+    tree_words) or None for chains.  out and lse ([rows, q_heads] fp32; only with want_lse) are allocated where they
+    are not given.
+    """
+
+    def __init__(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor,
+                 row_offsets: torch.Tensor, cache_lens: torch.Tensor, max_rows: Optional[int] = None,
+                 max_keys: Optional[int] = None, tree_mask: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 want_lse: bool = False):
+        index = _on_device(q, k_cache=k_cache, v_cache=v_cache, pages=pages, row_offsets=row_offsets,
+                           cache_lens=cache_lens, tree_mask=tree_mask, out=out, lse=lse)
+        S, n_pages, kv_heads, page_size, d = _paged(k_cache, v_cache, pages, row_offsets, cache_lens)
+        _need(q.dim() == 3 and q.dtype == k_cache.dtype and q.shape[2] == d and q.stride(2) == 1,
+              f"q: [rows, q_heads, {d}] {k_cache.dtype} with dense heads")
+        rows, q_heads = q.shape[0], q.shape[1]
+        if max_rows is None or max_keys is None:
+            count = row_offsets.diff()
+            if max_rows is None:
+                max_rows = max(1, int(count.max()))
+            if max_keys is None:
+                max_keys = max(1, int((cache_lens + count).max()))
+        words = 0
+        if tree_mask is not None:
+            _need(tree_mask.dim() == 2, "tree_mask: [rows, words]")
+            words = tree_mask.shape[1]
+            _flat("tree_mask", tree_mask, torch.int32, (rows, words))
+        own = []
+        if out is None:
+            out = torch.empty((rows, q_heads, d), dtype=q.dtype, device=q.device)
+            own.append(out)
+        if lse is None and want_lse:
+            lse = torch.empty((rows, q_heads), dtype=torch.float32, device=q.device)
+            own.append(lse)
+        _flat("out", out, q.dtype, (rows, q_heads, d))
+        _flat("lse", lse, torch.float32, (rows, q_heads))
+        self.out, self.lse = out, lse
+        need = load().knn_tree_attention_workspace_size(rows, S, q_heads, kv_heads, d, int(max_rows), int(max_keys))
+        self.workspace = torch.empty(max(int(need), 256), dtype=torch.uint8, device=q.device)
+        own.append(self.workspace)
+        self._tensors = (q, k_cache, v_cache, pages, row_offsets, cache_lens, tree_mask)
+        self._sizes = (rows, S, q_heads, kv_heads, d, q.stride(0), q.stride(1), n_pages, page_size, pages.shape[1],
+                       words, int(max_rows), int(max_keys), _dtype_code(q),
+                       float(1.0 / math.sqrt(d) if scale is None else scale))
+        self._keep(index, *own)
+
+    def run(self, stream=None) -> torch.Tensor:
+        """One call; returns out (and fills lse, where there is one), valid after stream sync."""
+        h = self._handle(stream)
+        st = load().knn_tree_attention(*map(_ptr, self._tensors), *self._sizes, _ptr(self.out), _ptr(self.lse),
+                                       _ptr(self.workspace), self.workspace.numel(), h)
+        _lib.check("knn_tree_attention", st)
+        return self.out
+
+
+def tree_attention(q, k_cache, v_cache, pages, row_offsets, cache_lens, max_rows=None, max_keys=None, tree_mask=None,
+                   scale=None, out=None, lse=None, want_lse=False, stream=None):
+    """One-shot knn_tree_attention: out, or (out, lse) with an lse."""
+    call = TreeAttention(q, k_cache, v_cache, pages, row_offsets, cache_lens, max_rows, max_keys, tree_mask, scale, out,
+                         lse, want_lse)
+    call.run(stream)
+    return call.out if call.lse is None else (call.out, call.lse)
