@@ -487,6 +487,46 @@ size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_head
                                          int64_t max_rows, int64_t max_keys);
 
 /*
+ * knn_sample -- a token of each row, drawn by a uniform number that the caller
+ * gives, from the model's logits or from a distribution such as knn_nest_step's
+ * p_m (whose greedy token is the other choice).
+ *
+ *   scores         [rows, V] fp32, bf16 or f16, rows row_stride elements apart.  Logits (probabilities = 0): present
+ *                  unless NaN or -inf.  Probabilities (!= 0; they need not add up to 1): present where > 0.  If the
+ *                  largest one is +inf, only those that are +inf are present.
+ *   uniforms       [rows] fp32 in [0, 1) (NaN and less than 0 count as 0, 1 and more as just under 1).
+ *   temperature, top_k, top_p, min_p
+ *                  [rows] fp32 / int32 / fp32 / fp32, each or NULL (1, 0, 1, 0), all on the device.
+ *
+ * With T the row's temperature the weight of a present element is
+ * exp((x - max) / T) of logits, (x / max)^(1 / T) of probabilities.  They are
+ * ordered by x, the larger first, the lower token first among equals, and
+ *   1. top_k in [1, present): the first top_k stay;
+ *   2. top_p < 1: of these, those before which less than top_p of their weight lies (always the first);
+ *   3. min_p > 0: of these, those of weight min_p (of the largest's) and more (always the first).
+ * The token is the first one that stays, by token id, at which the running
+ * weight of those that stay exceeds uniform times their sum.  T <= 0 or NaN
+ * takes the first element of the order.  NaN filters are off.
+ *
+ *   token          [rows] int32 out; -1 where nothing is present.
+ *   prob           [rows] fp32 out or NULL: its share of the weight that stays (0 for token -1).
+ *   kept           [rows] int32 out or NULL: how many stay.
+ *   workspace      knn_sample_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
+ *
+ * Weights are in 64 bits and are summed as whole numbers of 2^-s of the
+ * largest, s = 62 - ceil(log2 V), so the outcome is the same bits every time
+ * and that of exact arithmetic but for borders that lie that near.
+ * V <= 2^24 (KNN_ERR_UNSUPPORTED above).
+ */
+knn_status knn_sample(const void *scores, const float *uniforms, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, int64_t rows, int64_t V, int64_t row_stride,
+                      int32_t probabilities, knn_dtype dtype, int32_t *token, float *prob, int32_t *kept,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace knn_sample needs for these sizes (0 if they are invalid). */
+size_t knn_sample_workspace_size(int64_t rows, int64_t V, knn_dtype dtype);
+
+/*
  * knn_stream_read -- a measurement aid, not a step of the method: one plain
  * read of `bytes` bytes of device memory at `buf` (16-byte aligned, a multiple
  * of 16 bytes) with the same 16-byte non-temporal loads the distance stage

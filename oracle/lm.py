@@ -127,7 +127,8 @@ def sample(scores, uniform: float, probabilities: bool, temperature=1.0, top_k=0
         with np.errstate(divide="ignore", invalid="ignore"):
             w = np.exp(np.log(x / first) / temperature) if temperature != 1.0 else x / first
     else:
-        w = np.exp((x - first) / temperature)
+        with np.errstate(invalid="ignore"):
+            w = np.exp((x - first) / temperature)
     n = len(order)
     if top_k > 0:
         n = min(n, int(top_k))

@@ -51,6 +51,8 @@ SIGNATURES: Dict[str, tuple] = {
     "knn_kv_append": (I, [P] * 9 + [I64] * 7 + [I32] + [I64] * 9 + [I, P, P, P, P]),
     "knn_tree_attention": (I, [P] * 7 + [I64] * 13 + [I, F, P, P, P, SZ, P]),
     "knn_tree_attention_workspace_size": (SZ, [I64] * 7),
+    "knn_sample": (I, [P] * 6 + [I64] * 3 + [I32, I, P, P, P, P, SZ, P]),
+    "knn_sample_workspace_size": (SZ, [I64, I64, I]),
     "knn_stream_read": (I, [P, SZ, P, P]),
     "knn_status_string": (ctypes.c_char_p, [I]),
     "knn_abi_version": (I, []),

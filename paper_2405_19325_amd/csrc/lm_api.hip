@@ -46,6 +46,11 @@ knn_status check_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_hea
     return KNN_OK;
 }
 
+knn_status check_sample(int64_t rows, int64_t V, knn_dtype dtype) {
+    if (rows < 1 || V < 1 || (dtype != KNN_F32 && dtype != KNN_BF16 && dtype != KNN_F16)) return KNN_ERR_INVALID_ARG;
+    return rows > 0x7fffffff || V > kSampleMaxV ? KNN_ERR_UNSUPPORTED : KNN_OK;
+}
+
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 }  // namespace
@@ -130,6 +135,29 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
     a.cache = paged(pages, n_pages, page_size, table_width);
     a.q_out = q_out, a.k_cache = k_cache, a.v_cache = v_cache;
     return status_of(launch_kv_append(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+size_t knn_sample_workspace_size(int64_t rows, int64_t V, knn_dtype dtype) {
+    return check_sample(rows, V, dtype) == KNN_OK ? 256 : 0;
+}
+
+knn_status knn_sample(const void *scores, const float *uniforms, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, int64_t rows, int64_t V, int64_t row_stride,
+                      int32_t probabilities, knn_dtype dtype, int32_t *token, float *prob, int32_t *kept,
+                      void *workspace, size_t workspace_bytes, void *stream) {
+    if (!scores || !uniforms || !token) return KNN_ERR_INVALID_ARG;
+    const knn_status st = check_sample(rows, V, dtype);
+    if (st != KNN_OK) return st;
+    if (row_stride < 0) return KNN_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < knn_sample_workspace_size(rows, V, dtype))
+        return KNN_ERR_WORKSPACE;
+    SampleArgs a{};
+    a.scores = scores, a.uniforms = uniforms;
+    a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p;
+    a.rows = rows, a.V = static_cast<int>(V), a.stride = row_stride;
+    a.probabilities = probabilities != 0;
+    a.token = token, a.prob = prob, a.kept = kept;
+    return status_of(launch_sample(a, dtype, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -66,6 +66,25 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
 hipError_t launch_attend(const AttendArgs &args, const AttendPlan &plan, knn_dtype dtype, void *workspace,
                          hipStream_t stream);
 
+struct SampleArgs {
+    const void *scores;  // [rows, V], rows `stride` elements apart
+    const float *uniforms;
+    const float *temperature;  // each [rows], or null: 1, 0, 1, 0
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    int64_t rows;
+    int V;
+    int64_t stride;
+    bool probabilities;
+    int32_t *token;
+    float *prob;    // or null
+    int32_t *kept;  // or null
+};
+
+constexpr int64_t kSampleMaxV = int64_t{1} << 24;
+
+hipError_t launch_sample(const SampleArgs &args, knn_dtype dtype, void *workspace, hipStream_t stream);
+
 hipError_t launch_kv_append(const AppendArgs &args, knn_dtype dtype, hipStream_t stream);
 
 }  // namespace knnlm

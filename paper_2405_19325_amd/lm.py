@@ -216,3 +216,45 @@ def tree_attention(q, k_cache, v_cache, pages, row_offsets, cache_lens, max_rows
                          lse, want_lse)
     call.run(stream)
     return call.out if call.lse is None else (call.out, call.lse)
+
+
+class Sampler(_Call):
+    """knn_sample on these buffers: a token of each row of scores [rows, V] (f32, bf16 or f16, dense rows).
+
+    scores are logits, or a distribution with probabilities=True (p_m of a MixtureProblem, say); uniforms [rows] fp32.
+    temperature, top_p, min_p [rows] fp32 and top_k [rows] int32, or None: 1, 1, 0 and 0 (off).
+    """
+
+    def __init__(self, scores: torch.Tensor, uniforms: torch.Tensor, probabilities: bool = False,
+                 temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                 top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None):
+        index = _on_device(scores, uniforms=uniforms, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+        _need(scores.dim() == 2 and (scores.stride(1) == 1 or scores.shape[1] == 1), "scores: [rows, V] with dense rows")
+        rows, V = scores.shape
+        for name, t, dtype in (("uniforms", uniforms, torch.float32), ("temperature", temperature, torch.float32),
+                               ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                               ("min_p", min_p, torch.float32)):
+            _flat(name, t, dtype, (rows,))
+        dev = scores.device
+        self.token = torch.empty(rows, dtype=torch.int32, device=dev)
+        self.prob = torch.empty(rows, dtype=torch.float32, device=dev)
+        self.kept = torch.empty(rows, dtype=torch.int32, device=dev)
+        code = _dtype_code(scores)
+        need = load().knn_sample_workspace_size(rows, V, code)
+        self.workspace = torch.empty(max(int(need), 256), dtype=torch.uint8, device=dev)
+        self._tensors = (scores, uniforms, temperature, top_k, top_p, min_p)
+        self._sizes = (rows, V, scores.stride(0), int(bool(probabilities)), code)
+        self._keep(index, self.token, self.prob, self.kept, self.workspace)
+
+    def run(self, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """One call; returns (token, its probability among those kept, how many were kept), valid after stream sync."""
+        h = self._handle(stream)
+        st = load().knn_sample(*map(_ptr, self._tensors), *self._sizes, _ptr(self.token), _ptr(self.prob),
+                               _ptr(self.kept), _ptr(self.workspace), self.workspace.numel(), h)
+        _lib.check("knn_sample", st)
+        return self.token, self.prob, self.kept
+
+
+def sample(scores, uniforms, probabilities=False, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """One-shot knn_sample: (token [rows], its probability among those kept, how many were kept)."""
+    return Sampler(scores, uniforms, probabilities, temperature, top_k, top_p, min_p).run(stream)

@@ -64,3 +64,41 @@ def test_attention_workspace_size(lib):
     assert size(0, 2, 8, 2, 128, 16, 640) == 0
     for keys in (1, 31, 4096, 131072, 0x7fffffff):  # every size gets a workspace that is a multiple of its alignment
         assert size(64, 64, 32, 8, 128, 1, keys) % 256 == 0 and size(64, 64, 32, 8, 128, 1, keys) > 0
+
+
+SAMPLE = dict(scores=FAKE, uniforms=FAKE, temperature=None, top_k=None, top_p=None, min_p=None, rows=4, V=1000,
+              row_stride=1000, probabilities=0, dtype=0, token=FAKE, prob=None, kept=None, workspace=FAKE,
+              workspace_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("over,expect", [
+    (dict(scores=None), INVALID), (dict(uniforms=None), INVALID), (dict(token=None), INVALID), (dict(rows=0), INVALID),
+    (dict(V=0), INVALID), (dict(row_stride=-1), INVALID), (dict(dtype=4), INVALID), (dict(dtype=0x101), INVALID),
+    (dict(V=(1 << 24) + 1), UNSUPPORTED), (dict(rows=1 << 31), UNSUPPORTED), (dict(workspace=None), WORKSPACE),
+    (dict(workspace=FAKE + 4), WORKSPACE), (dict(workspace_bytes=0), WORKSPACE)])
+def test_sample_refuses(lib, over, expect):
+    assert lib.knn_sample(*dict(SAMPLE, **over).values()) == expect
+
+
+def test_sample_workspace_size(lib):
+    assert lib.knn_sample_workspace_size(1, 1, 0) > 0 and lib.knn_sample_workspace_size(256, 131072, 2) > 0
+    assert lib.knn_sample_workspace_size(0, 1, 0) == 0 and lib.knn_sample_workspace_size(1, 1, 5) == 0
+
+
+def test_oracle_sample_by_hand():
+    """The oracle's draw on rows worked out by hand."""
+    import math
+
+    from oracle import lm
+
+    x = [math.log(0.1), math.log(0.4), math.log(0.2), math.log(0.3)]
+    assert [lm.sample(x, u, False)[0] for u in (0.0, 0.05, 0.15, 0.55, 0.65, 0.75, 0.99)] == [0, 0, 1, 2, 2, 3, 3]
+    assert lm.sample(x, 0.5, False, top_k=2)[::2] == (1, 2)          # 0.4 and 0.3 stay: 4/7 > 0.5
+    assert lm.sample(x, 0.6, False, top_k=2)[::2] == (3, 2)
+    assert lm.sample(x, 0.6, False, top_p=0.39)[::2] == (1, 1)
+    assert lm.sample(x, 0.99, False, top_p=0.75)[::2] == (3, 3)      # 0.4, 0.3, 0.2: 0.7 lies before the third
+    assert lm.sample(x, 0.99, False, min_p=0.6)[::2] == (3, 2)
+    assert abs(lm.sample(x, 0.0, False, temperature=0.5)[1] - 0.01 / 0.30) < 1e-12
+    assert lm.sample([0.25] * 4, 0.5, True, top_k=3)[::2] == (1, 3)  # running 1/3, 2/3: the first over a half
+    assert lm.sample([0.0, -1.0], 0.5, True) == (-1, 0.0, 0)
+    assert lm.sample(x, 0.9, False, temperature=0.0) == (1, 1.0, 1)
