@@ -10,10 +10,18 @@
 // row in 10^7.  (In 32 bits it would for one row in 50.)
 //
 // Every filter keeps a first part of one order: larger x first, the lower
-// index first among equals.  A cut in it is a value and how many of the
-// elements equal to it stay (the ones with the lowest indexes).  A cut is
-// found on the 32-bit keys that order like the values, eleven bits a pass,
-// from the largest down: a histogram of counts (top-k) or of weights (top-p).
+// index first among equals.  A cut in it is its last element.  To find one,
+// the elements go into 2048 bins that follow the order, of about a 64th of a
+// factor e (of an octave, for probabilities) each: counts for top-k, weights
+// for top-p.  A scan finds the bin of the cut; its elements, a few dozen as a
+// rule, are listed, and each one's place and what lies before it come from
+// comparing it with all others.  Where they are more than the list holds (a
+// value that hundreds of tokens share, a row far from any logarithmic
+// spread), the cut is found on the keys that order like the values, eleven
+// bits a pass.
+//
+// One workgroup takes a row.  A row of up to 128 KiB stays in LDS from the first
+// pass on; a longer one is read three times, from the caches after the first.
 #include "knnlm_device.h"
 #include "lm_internal.h"
 
@@ -25,6 +33,9 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
 
+constexpr size_t kHeldBytes = 128 * 1024;
+constexpr int kList = 512;  // elements of a cut's bin that are compared with each other
+
 template <knn_dtype DT>
 __device__ __forceinline__ float element(const void *row, int i) {
     if constexpr (DT == KNN_F32) return static_cast<const float *>(row)[i];
@@ -33,11 +44,15 @@ __device__ __forceinline__ float element(const void *row, int i) {
     return static_cast<float>(static_cast<const _Float16 *>(row)[i]);
 }
 
-// A key that orders like x; 0 where x is absent (NaN, -inf; of probabilities
-// also what is not above 0).
-__device__ __forceinline__ uint32_t key_of(float x, bool probabilities) {
-    if (!(x > (probabilities ? 0.0f : -INFINITY))) return 0;
-    const uint32_t b = __float_as_uint(x == 0.0f ? 0.0f : x);
+// -inf for what is absent (NaN; of probabilities also what is not above 0); one zero.
+__device__ __forceinline__ float present(float x, bool probabilities) {
+    return x > (probabilities ? 0.0f : -INFINITY) ? x + 0.0f : -INFINITY;
+}
+
+// A key that orders like a present x; 0 for an absent one.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    if (!(x > -INFINITY)) return 0;
+    const uint32_t b = __float_as_uint(x);
     return b ^ ((b >> 31) != 0 ? 0xffffffffu : 0x80000000u);
 }
 
@@ -45,141 +60,476 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key ^ ((key >> 31) != 0 ? 0x80000000u : 0xffffffffu));
 }
 
-// The weights of a row, as a function of the key.
-struct Weights {
-    double top;      // the largest value
-    double inv_t;
-    double scale;    // 2^s, or 2^s over the largest value's power of two where the values are the weights
-    double least;    // min-p
-    bool probabilities, plain, flat;  // plain: probabilities at T = 1; flat: the largest is infinite
+// 2^a to 2^-51 relative, a <= 0: the power series of exp(f ln 2), |f| <= 1/2,
+// whose 13th term is 2e-16.  What is under 2^-200 counts as that.
+__device__ __forceinline__ double power2(double a) {
+    a = fmax(a, -200.0);
+    const double n = rint(a), f = a - n;
+    double r = 2.5678435993488206e-11;  // ln(2)^12 / 12!
+    r = fma(r, f, 4.4455382718708116e-10);
+    r = fma(r, f, 7.0549116208011230e-09);
+    r = fma(r, f, 1.0178086009239700e-07);
+    r = fma(r, f, 1.3215486790144310e-06);
+    r = fma(r, f, 1.5252733804059840e-05);
+    r = fma(r, f, 1.5403530393381610e-04);
+    r = fma(r, f, 1.3333558146428443e-03);
+    r = fma(r, f, 9.6181291076284770e-03);
+    r = fma(r, f, 5.5504108664821580e-02);
+    r = fma(r, f, 2.4022650695910070e-01);
+    r = fma(r, f, 6.9314718055994530e-01);
+    r = fma(r, f, 1.0);
+    return ldexp(r, static_cast<int>(n));
+}
 
-    __device__ __forceinline__ double of(uint32_t key) const {  // the largest one's is 2^s (plain: at most)
-        const double x = value_of(key);
-        if (flat) return scale;
-        if (plain) return x * scale;
-        return exp((probabilities ? log(x / top) : x - top) * inv_t) * scale;
+enum Kind { kLogits, kPlain, kPower };  // kPlain: probabilities at T = 1, which are their own weights
+
+// The weights of a row, as a function of the value; the largest one's is 2^s
+// (kPlain: at most, with the values brought under 1 by a power of two).
+template <Kind KIND>
+struct Weights {
+    float top;     // the largest value
+    double rate;   // log2(e) / T, or 1 / T of probabilities
+    double unit;   // 2^s
+    double least;  // min-p, as a weight
+
+    __device__ __forceinline__ double of(float x) const {
+        if constexpr (KIND == kPlain) return static_cast<double>(x) * unit;
+        double far = static_cast<double>(x) - static_cast<double>(top);
+        if constexpr (KIND == kPower) far = log2(static_cast<double>(x) / static_cast<double>(top));
+        return power2(x == top ? 0.0 : far * rate) * unit;  // (an infinite one is as far as itself)
     }
-    __device__ __forceinline__ uint64_t whole(double w) const { return static_cast<uint64_t>(w + 0.5); }
-    __device__ __forceinline__ bool heavy(double w) const { return w >= least * (plain ? top * scale : scale); }
+    // To the nearest whole number: w < 2^52, so the sum's low bits are it.
+    __device__ __forceinline__ static uint64_t whole(double w) {
+        return static_cast<uint64_t>(__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ll);
+    }
 };
 
 struct Shared {
-    uint64_t mass[kBins];
-    uint32_t count[kBins];
+    uint64_t mass[kBins];  // bins, then the weights of the row's pieces
+    uint64_t list[kList];  // key << 32 | ~index: larger is earlier in the order
+    uint64_t weight[kList];
     uint64_t part[kWaves];
     uint32_t part32[kWaves];
-    uint64_t answer64;
-    uint32_t answer, answer2;
+    uint64_t before, cut;
+    uint32_t bin, listed, kept;
+    int index;
 };
 
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_u64(uint64_t v) {
+    return static_cast<uint64_t>(dpp_u32<CTRL>(0u, static_cast<uint32_t>(v >> 32))) << 32 |
+           dpp_u32<CTRL>(0u, static_cast<uint32_t>(v));
+}
+__device__ __forceinline__ uint64_t readlane_u64(uint64_t v, int lane) {
+    return static_cast<uint64_t>(readlane_u32(static_cast<uint32_t>(v >> 32), lane)) << 32 |
+           readlane_u32(static_cast<uint32_t>(v), lane);
+}
+// Sum over the wave, in scalar registers: exchanges within the 16 lanes of a row, then the four rows.
 __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    v += dpp_u64<0xB1>(v);   // quad_perm [1,0,3,2]
+    v += dpp_u64<0x4E>(v);   // quad_perm [2,3,0,1]
+    v += dpp_u64<0x141>(v);  // row_half_mirror
+    v += dpp_u64<0x140>(v);  // row_mirror
+    return (readlane_u64(v, 0) + readlane_u64(v, 16)) + (readlane_u64(v, 32) + readlane_u64(v, 48));
 }
 __device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
-
-__device__ __forceinline__ uint64_t block_sum64(uint64_t v, Shared &sh) {
-    v = wave_sum64(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    uint64_t r = 0;
+__device__ __forceinline__ uint64_t wave_scan64(uint64_t v, int lane) {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) r += sh.part[w];
-    return r;
-}
-
-// The key at which the running count (or weight) from the largest key down
-// first reaches `goal`, given that it does: {key, what lies above it}.  Keys
-// under `floor_key` do not count.
-template <bool MASS, typename Each>
-__device__ uint32_t descend(double goal, uint32_t floor_key, const Weights &w, Shared &sh, Each each, uint64_t &above) {
-    uint32_t prefix = 0;
-    above = 0;
-    for (int level = 0; level < 3; ++level) {
-        const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-        const uint32_t mask = (1u << bits) - 1;
-        __syncthreads();
-        for (int i = threadIdx.x; i < kBins; i += kThreads) {
-            if constexpr (MASS) sh.mass[i] = 0; else sh.count[i] = 0;
-        }
-        __syncthreads();
-        each([&](uint32_t key) {
-            if (key == 0 || key < floor_key) return;
-            if (level > 0 && (key >> (shift + bits)) != prefix) return;
-            const uint32_t bin = (key >> shift) & mask;
-            if constexpr (MASS)
-                atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[bin]), static_cast<unsigned long long>(w.whole(w.of(key))));
-            else
-                atomicAdd(&sh.count[bin], 1u);
-        });
-        __syncthreads();
-        // One wave walks the bins down, 64 at a time.
-        if (threadIdx.x < kWave) {
-            const int lane = threadIdx.x;
-            uint64_t run = above;
-            uint32_t found = 0;
-            uint64_t before = above;
-            bool done = false;
-            for (int b = static_cast<int>(mask); b >= 0 && !done; b -= kWave) {
-                const int bin = b - lane;
-                const uint64_t v = MASS ? sh.mass[bin] : static_cast<uint64_t>(sh.count[bin]);
-                uint64_t incl = v;
-#pragma unroll
-                for (int o = 1; o < kWave; o <<= 1) {
-                    const uint64_t up = __shfl_up(incl, o);
-                    if (lane >= o) incl += up;
-                }
-                const uint64_t hit = __ballot(v != 0 && static_cast<double>(run + incl) >= goal);
-                const uint64_t some = __ballot(v != 0);
-                if (some != 0) {  // where the goal is never reached (by a rounding), the last bin with anything
-                    const int lane_at = hit != 0 ? __ffsll(static_cast<unsigned long long>(hit)) - 1
-                                                 : 63 - __clzll(static_cast<long long>(some));
-                    found = static_cast<uint32_t>(b - lane_at);
-                    before = run + __shfl(incl - v, lane_at);
-                    done = hit != 0;
-                }
-                run += __shfl(incl, 63);
-            }
-            if (lane == 0) {
-                sh.answer = found;
-                sh.answer64 = before;
-            }
-        }
-        __syncthreads();
-        prefix = (prefix << bits) | sh.answer;
-        above = sh.answer64;
+    for (int o = 1; o < kWave; o <<= 1) {
+        const uint64_t up = __shfl_up(v, o);
+        if (lane >= o) v += up;
     }
-    return prefix;
+    return v;
 }
 
-template <knn_dtype DT>
-__global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_scale) {
-    __shared__ Shared sh;
-    const int64_t r = blockIdx.x;
+// The sum of sh.mass; with hit(before, own) true for one entry, its number and
+// what lies before it in sh.bin and sh.before.
+template <typename Goal, typename Hit>
+__device__ __forceinline__ uint64_t scan_bins(Shared &sh, Goal goal_of, Hit hit) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const char *row = static_cast<const char *>(a.scores) + r * a.stride * (DT == KNN_F32 ? 4 : 2);
-    const int V = a.V;
-    // The waves take consecutive pieces of the row, so that what lies before an element is known by wave.
-    const int piece = (V + kWaves - 1) / kWaves;
-    const int i0 = min(V, wave * piece), i1 = min(V, i0 + piece);
-    auto each = [&](auto f) {
-        for (int i = i0 + lane; i < i1; i += kWave) f(key_of(element<DT>(row, i), a.probabilities));
+    const uint64_t a = sh.mass[2 * threadIdx.x], b = sh.mass[2 * threadIdx.x + 1];
+    const uint64_t incl = wave_scan64(a + b, lane);
+    if (lane == 63) sh.part[wave] = incl;
+    __syncthreads();
+    uint64_t before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const uint64_t v = sh.part[w];
+        before += w < wave ? v : 0;
+        total += v;
+    }
+    before += incl - a - b;
+    const auto goal = goal_of(total);
+    if (hit(before, a, goal)) sh.bin = 2 * threadIdx.x, sh.before = before;
+    if (hit(before + a, b, goal)) sh.bin = 2 * threadIdx.x + 1, sh.before = before + a;
+    __syncthreads();
+    return total;
+}
+
+constexpr int kPieceLog2 = 9;  // elements of a row's pieces (more where a row would have over kBins of them)
+
+// A row of scores: in LDS from the first reading on (HELD), or in memory.  VEC:
+// four elements a load.
+template <knn_dtype DT, bool HELD, bool VEC, bool PROBS>
+struct Row {
+    const char *row;
+    char *held;
+    int V, pieces, piece_log2;
+
+    static constexpr int SIZE = DT == KNN_F32 ? 4 : 2;
+
+    __device__ __forceinline__ static void widen4(const void *p, float (&x)[4]) {
+        if constexpr (DT == KNN_F32) {
+            const float4 v = *static_cast<const float4 *>(p);
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        } else {
+            const uint2 v = *static_cast<const uint2 *>(p);
+            const uint16_t h[4] = {static_cast<uint16_t>(v.x), static_cast<uint16_t>(v.x >> 16),
+                                   static_cast<uint16_t>(v.y), static_cast<uint16_t>(v.y >> 16)};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = element<DT>(h, c);
+        }
+    }
+    // Elements i .. i + 3 (i a multiple of four) of the row in memory; absent past its end.
+    __device__ __forceinline__ void read4(int i, float (&x)[4]) const {
+        if (VEC && i + 3 < V) {
+            widen4(row + static_cast<int64_t>(i) * SIZE, x);
+        } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = i + c < V ? element<DT>(row, i + c) : -INFINITY;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = present(x[c], PROBS);
+    }
+    __device__ __forceinline__ void load4(int i, float (&x)[4]) const {
+        if constexpr (HELD) widen4(held + i * SIZE, x); else read4(i, x);
+    }
+    __device__ __forceinline__ float at(int i) const {
+        return i < V ? present(element<DT>(row, i), PROBS) : -INFINITY;
+    }
+    __device__ __forceinline__ void keep4(int i, const float (&x)[4]) const {
+        if constexpr (DT == KNN_F32) {
+            *reinterpret_cast<float4 *>(held + i * 4) = make_float4(x[0], x[1], x[2], x[3]);
+        } else {  // the values came from the type, so they go back exactly
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if constexpr (DT == KNN_BF16)
+                    reinterpret_cast<uint16_t *>(held)[i + c] = static_cast<uint16_t>(__float_as_uint(x[c]) >> 16);
+                else
+                    reinterpret_cast<_Float16 *>(held)[i + c] = static_cast<_Float16>(x[c]);
+            }
+        }
+    }
+    // f(index, value) over this wave's pieces, which are consecutive; done(piece) after each.
+    template <bool FIRST = false, typename F, typename Done>
+    __device__ __forceinline__ void pass(int wave, int lane, F f, Done done) const {
+        const int each = (pieces + kWaves - 1) / kWaves;
+        const int end = min(pieces, (wave + 1) * each);
+        for (int piece = wave * each; piece < end; ++piece) {
+            for (int i = piece << piece_log2; i < (piece + 1) << piece_log2; i += 512) {
+                float x[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int at = i + 256 * j + 4 * lane;
+                    if constexpr (FIRST) read4(at, x[j]); else load4(at, x[j]);
+                    if constexpr (FIRST && HELD) keep4(at, x[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) f(i + 256 * j + 4 * lane + c, x[j][c]);
+            }
+            done(piece);
+        }
+    }
+};
+
+// The filters and the draw of a row whose largest present value is `top` and
+// smallest `low`, at a temperature t > 0 and top-p p > 0.
+template <Kind KIND, typename R>
+__device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &sh, int64_t r, float top, float low, float t,
+                                     float p, int log2_unit) {
+    constexpr bool PROBS = KIND != kLogits;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int V = rw.V, pieces = rw.pieces, piece_log2 = rw.piece_log2;
+    auto pass = [&](auto f, auto done) { rw.pass(wave, lane, f, done); };
+    auto nothing = [](int) {};
+    Weights<KIND> w;
+    w.top = top;
+    w.rate = (PROBS ? 1.0 : 1.4426950408889634074) / static_cast<double>(t);
+    w.unit = ldexp(1.0, log2_unit - (KIND == kPlain ? ilogb(static_cast<double>(top)) + 1 : 0));
+    const float min_p = a.min_p != nullptr ? a.min_p[r] : 0.0f;
+    w.least = (min_p > 0.0f ? fmin(static_cast<double>(min_p), 1.0) : 0.0) *
+              (KIND == kPlain ? static_cast<double>(top) * w.unit : w.unit);
+
+    // Bins that follow the order; what is past the last one's start is in it.
+    // Logits: steps of the distance from the largest, over 32 T or the row's
+    // range.  Probabilities: steps of the bits, which grow like a logarithm.
+    const float span = fminf(top - low, 32.0f * t);
+    const float step = span > 0.0f ? kBins / span : 0.0f;
+    const uint32_t top_bits = __float_as_uint(top);
+    int shift = 0;
+    if (PROBS) {
+        const float octaves = fminf(46.0f * t, 255.0f);  // 2^-46 = e^-32
+        uint32_t bits = min(top_bits - __float_as_uint(fminf(low, top)), static_cast<uint32_t>(octaves * 8388608.0f));
+        while (bits >> shift >= kBins) ++shift;
+    }
+    auto bin_of = [&](float x) -> uint32_t {
+        if (PROBS) return min((top_bits - __float_as_uint(x)) >> shift, static_cast<uint32_t>(kBins - 1));
+        return static_cast<uint32_t>(fminf((top - x) * step, static_cast<float>(kBins - 1)));
     };
 
-    uint32_t top = 0;
-    each([&](uint32_t key) { top = max(top, key); });
-    top = wave_allmax_u32(top);
-    if (lane == 0) sh.part32[wave] = top;
+    // What stays: x above `cut_x`, or equal to it with an index up to `cut_i`.
+    float cut_x = top == INFINITY ? 3.402823466e38f : -INFINITY;
+    int cut_i = -1;
+    auto stays = [&](int i, float x) { return x > cut_x || (x == cut_x && i <= cut_i); };
+    auto clear = [&]() {
+        __syncthreads();
+        sh.mass[2 * threadIdx.x] = 0;
+        sh.mass[2 * threadIdx.x + 1] = 0;
+        if (threadIdx.x == 0) sh.listed = 0, sh.cut = ~0ull;
+        __syncthreads();
+    };
+    uint32_t kept = 0;
+    bool summed = false;
+    uint64_t run = 0;  // this wave's weights of the piece at hand
+    auto end_piece = [&](int piece) {
+        const uint64_t s = wave_sum64(run);
+        if (lane == 0) sh.mass[piece] = s;
+        run = 0;
+    };
+    auto add = [&](float x) {
+        const double v = w.of(x);
+        if (v >= w.least) {
+            run += Weights<KIND>::whole(v);
+            ++kept;
+        }
+    };
+    // The cut at `goal` (a count, or a weight) of the elements that stay, whose
+    // bins are in sh.mass, from sh.bin and sh.before on; with `last` the pieces' weights too.
+    auto cut_at = [&](bool by_weight, double goal, bool last) {
+        const uint32_t bin = sh.bin;
+        const uint64_t before = sh.before;
+        pass(
+            [&](int i, float x) {
+                const bool in = stays(i, x);
+                const uint32_t b = bin_of(x);
+                if (in && b == bin) {
+                    const uint32_t at = atomicAdd(&sh.listed, 1u);
+                    if (at < kList) sh.list[at] = static_cast<uint64_t>(key_of(x)) << 32 | ~static_cast<uint32_t>(i);
+                }
+                if (last && in && b < bin) add(x);
+            },
+            [&](int piece) {
+                if (last) end_piece(piece);
+            });
+        __syncthreads();
+        const int n = static_cast<int>(sh.listed);
+        if (n <= kList) {
+            const int me = threadIdx.x;
+            uint64_t mine = 0, own = 0;
+            if (me < n) {
+                mine = sh.list[me];
+                own = by_weight || last ? Weights<KIND>::whole(w.of(value_of(static_cast<uint32_t>(mine >> 32)))) : 0;
+                sh.weight[me] = by_weight ? own : 1;
+            }
+            __syncthreads();
+            bool in = false;
+            if (me < n) {
+                uint64_t ahead = before;
+                for (int j = 0; j < n; ++j) ahead += sh.list[j] > mine ? sh.weight[j] : 0;
+                in = static_cast<double>(ahead) < goal;
+                if (in) atomicMin(reinterpret_cast<unsigned long long *>(&sh.cut), static_cast<unsigned long long>(mine));
+            }
+            if (last && in) {
+                const double v = w.of(value_of(static_cast<uint32_t>(mine >> 32)));
+                if (v >= w.least) {
+                    const int i = static_cast<int>(~static_cast<uint32_t>(mine));
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[i >> piece_log2]),
+                              static_cast<unsigned long long>(own));
+                    ++kept;
+                }
+            }
+            __syncthreads();
+            cut_x = value_of(static_cast<uint32_t>(sh.cut >> 32));
+            cut_i = static_cast<int>(~static_cast<uint32_t>(sh.cut));
+            summed = last;
+            return;
+        }
+        kept = 0;
+        run = 0;
+        // By keys, eleven bits a pass: the key of the cut, and how much of the goal is left for the elements equal to it.
+        uint32_t prefix = 0;
+        uint64_t above = 0;
+        for (int level = 0; level < 3; ++level) {
+            const int low_bit = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+            clear();
+            pass(
+                [&](int i, float x) {
+                    const uint32_t key = key_of(x);
+                    if (!stays(i, x) || (level > 0 && key >> (low_bit + bits) != prefix)) return;
+                    const uint32_t b = kBins - 1 - ((key >> low_bit) & ((1u << bits) - 1));
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[b]),
+                              by_weight ? static_cast<unsigned long long>(Weights<KIND>::whole(w.of(x))) : 1ull);
+                },
+                nothing);
+            __syncthreads();
+            const uint64_t base = above;
+            scan_bins(sh, [&](uint64_t) { return goal; }, [&](uint64_t at, uint64_t v, double to) {
+                return static_cast<double>(base + at) < to && static_cast<double>(base + at + v) >= to;
+            });
+            prefix = prefix << bits | ((kBins - 1 - sh.bin) & ((1u << bits) - 1));
+            above = base + sh.before;
+        }
+        const float x_at = value_of(prefix);
+        const uint64_t one = by_weight ? Weights<KIND>::whole(w.of(x_at)) : 1;
+        // The n-th element equal to it is the last before which less than the goal lies.
+        uint64_t left = static_cast<uint64_t>((goal - static_cast<double>(above)) / static_cast<double>(one));
+        while (static_cast<double>(above + left * one) < goal) ++left;
+        while (left > 1 && static_cast<double>(above + (left - 1) * one) >= goal) --left;
+        clear();
+        uint32_t equal = 0;
+        pass([&](int i, float x) { equal += x == x_at && stays(i, x) ? 1u : 0u; },
+             [&](int piece) {
+                 const uint32_t s = wave_sum32(equal);
+                 if (lane == 0) sh.mass[piece] = s;
+                 equal = 0;
+             });
+        __syncthreads();
+        scan_bins(sh, [&](uint64_t) { return left; },
+                  [&](uint64_t at, uint64_t v, uint64_t to) { return at < to && at + v >= to; });
+        if (wave == 0) {
+            uint64_t seen = sh.before;
+            bool found = false;
+            for (int i = static_cast<int>(sh.bin) << piece_log2; !found; i += kWave) {
+                const int at = i + lane;
+                const float x = at < V ? rw.at(at) : -INFINITY;
+                const uint64_t eq = __ballot(x == x_at && stays(at, x));
+                const int here = __popcll(eq & ((2ull << lane) - 1));
+                if (x == x_at && ((eq >> lane) & 1) != 0 && seen + here == left) sh.index = at;
+                seen += __popcll(eq);
+                found = seen >= left || i + kWave >= V;
+            }
+        }
+        __syncthreads();
+        cut_i = sh.index;
+        cut_x = x_at;
+    };
+
+    const int k = a.top_k != nullptr ? a.top_k[r] : 0;
+    if (k > 0 && k < V) {
+        clear();
+        pass(
+            [&](int i, float x) {
+                if (stays(i, x)) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[bin_of(x)]), 1ull);
+            },
+            nothing);
+        __syncthreads();
+        const uint64_t n = scan_bins(sh, [&](uint64_t) { return static_cast<uint64_t>(k); },
+                                     [&](uint64_t at, uint64_t v, uint64_t to) { return at < to && at + v >= to; });
+        if (static_cast<uint64_t>(k) < n) cut_at(false, k, !(p < 1.0f));
+    }
+    if (p < 1.0f) {
+        clear();
+        pass(
+            [&](int i, float x) {
+                if (stays(i, x))
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[bin_of(x)]),
+                              static_cast<unsigned long long>(Weights<KIND>::whole(w.of(x))));
+            },
+            nothing);
+        __syncthreads();
+        const double share = p;
+        const uint64_t sum = scan_bins(sh, [&](uint64_t all) { return share * static_cast<double>(all); },
+                                       [&](uint64_t at, uint64_t v, double to) {
+                                           return static_cast<double>(at) < to && static_cast<double>(at + v) >= to;
+                                       });
+        cut_at(true, share * static_cast<double>(sum), true);
+    }
+    if (!summed) {
+        clear();
+        pass([&](int i, float x) { if (stays(i, x)) add(x); }, end_piece);
+    } else {
+        __syncthreads();
+    }
+    kept = wave_sum32(kept);
+    if (lane == 0) atomicAdd(&sh.kept, kept);
+    // Entries past the last piece hold no weight.
+    for (int i = pieces + threadIdx.x; i < kBins; i += kThreads) sh.mass[i] = 0;
+    __syncthreads();
+    const float u = a.uniforms[r];
+    const double at = u > 0.0f ? fmin(static_cast<double>(u), 1.0) : 0.0;
+    auto aim = [&](uint64_t all) {  // the token is the first whose running weight exceeds it
+        const uint64_t goal = static_cast<uint64_t>(at * static_cast<double>(all));
+        return goal < all ? goal : all - 1;
+    };
+    const uint64_t total =
+        scan_bins(sh, aim, [](uint64_t before, uint64_t v, uint64_t to) { return before <= to && to < before + v; });
+    if (wave != 0) return;
+    const uint64_t goal = aim(total);
+    uint64_t before = sh.before;
+    for (int i = static_cast<int>(sh.bin) << piece_log2;; i += 256) {
+        float x[4];
+        rw.load4(i + 4 * lane, x);
+        uint64_t q[4], sum = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const double v = stays(i + 4 * lane + c, x[c]) ? w.of(x[c]) : 0.0;
+            q[c] = v >= w.least ? Weights<KIND>::whole(v) : 0;
+            sum += q[c];
+        }
+        const uint64_t incl = wave_scan64(sum, lane);
+        const uint64_t hit = __ballot(before + incl > goal);
+        if (hit != 0) {
+            if (lane == __ffsll(static_cast<unsigned long long>(hit)) - 1) {
+                uint64_t here = before + incl - sum;
+                int c = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    here += q[j];
+                    c += here <= goal ? 1 : 0;
+                }
+                const float v = c == 0 ? x[0] : c == 1 ? x[1] : c == 2 ? x[2] : x[3];
+                a.token[r] = i + 4 * lane + c;
+                if (a.prob != nullptr) a.prob[r] = static_cast<float>(w.of(v) / static_cast<double>(total));
+                if (a.kept != nullptr) a.kept[r] = static_cast<int32_t>(sh.kept);
+            }
+            return;
+        }
+        before += __shfl(incl, 63);
+        if (i + 256 >= V) return;  // not reached: the piece holds the goal
+    }
+}
+
+template <knn_dtype DT, bool HELD, bool VEC, bool PROBS>
+__global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit, int piece_log2) {
+    __shared__ Shared sh;
+    extern __shared__ __align__(16) char held[];
+    const int64_t r = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    using R = Row<DT, HELD, VEC, PROBS>;
+    const R rw{static_cast<const char *>(a.scores) + r * a.stride * R::SIZE, held, a.V,
+               (a.V + (1 << piece_log2) - 1) >> piece_log2, piece_log2};
+    auto nothing = [](int) {};
+
+    float top = -INFINITY, low = INFINITY;  // the largest and the smallest present value
+    rw.template pass<true>(wave, lane, [&](int, float x) { top = fmaxf(top, x), low = fminf(low, x > -INFINITY ? x : INFINITY); },
+                           nothing);
+    top = wave_allmax(top);
+    low = wave_allmin(low);
+    if (lane == 0) sh.part32[wave] = __float_as_uint(top), sh.part[wave] = __float_as_uint(low);
+    if (threadIdx.x == 0) sh.kept = 0, sh.index = 0x7fffffff;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = max(top, sh.part32[w]);
-    if (top == 0) {
+    for (int w = 0; w < kWaves; ++w) {
+        top = fmaxf(top, __uint_as_float(sh.part32[w]));
+        low = fminf(low, __uint_as_float(static_cast<uint32_t>(sh.part[w])));
+    }
+    if (!(top > -INFINITY)) {
         if (threadIdx.x == 0) {
             a.token[r] = -1;
             if (a.prob != nullptr) a.prob[r] = 0.0f;
@@ -188,150 +538,63 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_scal
         return;
     }
     const float t = a.temperature != nullptr ? a.temperature[r] : 1.0f;
-    const bool greedy = !(t > 0.0f);
-    Weights w{};
-    w.top = value_of(top);
-    w.inv_t = 1.0 / static_cast<double>(t);
-    w.probabilities = a.probabilities;
-    w.flat = value_of(top) == INFINITY;
-    w.plain = !w.flat && a.probabilities && t == 1.0f;
-    w.scale = ldexp(1.0, log2_scale - (w.plain ? ilogb(w.top) + 1 : 0));
-    const float least = a.min_p != nullptr ? a.min_p[r] : 0.0f;
-    w.least = least > 0.0f ? fmin(static_cast<double>(least), 1.0) : 0.0;
-
-    // The cut: keys above `cut` stay, and the first `rest` of those equal to it.
-    uint32_t cut = w.flat ? top - 1 : 0;
-    uint64_t rest = 0;
-    if (greedy) {
-        cut = top;
-        rest = 1;
-    }
-    const uint32_t floor_key = cut + 1;  // what counts at all
-    const int k = a.top_k != nullptr ? a.top_k[r] : 0;
-    if (!greedy && k > 0 && k < V) {
-        uint32_t n = 0;
-        each([&](uint32_t key) { n += key >= floor_key ? 1u : 0u; });
-        if (static_cast<uint64_t>(k) < block_sum64(n, sh)) {
-            uint64_t above;
-            cut = descend<false>(static_cast<double>(k), floor_key, w, sh, each, above);
-            rest = static_cast<uint64_t>(k) - above;
-        }
-    }
     const float p = a.top_p != nullptr ? a.top_p[r] : 1.0f;
-    if (!greedy && p < 1.0f) {
-        if (!(p > 0.0f)) {
-            cut = top;
-            rest = 1;
-        } else {
-            uint64_t sum = 0;
-            each([&](uint32_t key) { sum += key > cut ? w.whole(w.of(key)) : 0; });
-            sum = block_sum64(sum, sh);
-            if (rest > 0) sum += rest * w.whole(w.of(cut));
-            const double goal = static_cast<double>(p) * static_cast<double>(sum);
-            uint64_t above;
-            const uint32_t at = descend<true>(goal, rest > 0 ? cut : cut + 1, w, sh, each, above);
-            const uint64_t one = w.whole(w.of(at));
-            uint64_t n = 1;
-            if (one > 0 && goal > static_cast<double>(above)) {
-                n = static_cast<uint64_t>((goal - static_cast<double>(above)) / static_cast<double>(one));
-                while (static_cast<double>(above + n * one) < goal) ++n;
-                while (n > 1 && static_cast<double>(above + (n - 1) * one) >= goal) --n;
-            }
-            rest = at == cut && n > rest ? rest : n;
-            cut = at;
+    if (!(t > 0.0f) || p <= 0.0f) {  // the first element of the order
+        int first = 0x7fffffff;
+        rw.pass(wave, lane, [&](int i, float x) { first = x == top && i < first ? i : first; }, nothing);
+        first = static_cast<int>(wave_allmin_u32(static_cast<uint32_t>(first)));
+        if (lane == 0) atomicMin(&sh.index, first);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            a.token[r] = sh.index;
+            if (a.prob != nullptr) a.prob[r] = 1.0f;
+            if (a.kept != nullptr) a.kept[r] = 1;
         }
+        return;
     }
+    if constexpr (!PROBS) {
+        draw<kLogits>(a, rw, sh, r, top, low, t, p, log2_unit);
+    } else {
+        if (t == 1.0f && top < INFINITY) draw<kPlain>(a, rw, sh, r, top, low, t, p, log2_unit);
+        else draw<kPower>(a, rw, sh, r, top, low, t, p, log2_unit);
+    }
+}
 
-    // Elements equal to the cut before each wave's piece, then in index order: what stays, and its weight.
-    uint32_t ties = 0;
-    if (rest > 0) {
-        each([&](uint32_t key) { ties += key == cut ? 1u : 0u; });
-        ties = wave_sum32(ties);
-        __syncthreads();
-        if (lane == 0) sh.part32[wave] = ties;
-        __syncthreads();
-        ties = 0;
-        for (int v = 0; v < wave; ++v) ties += sh.part32[v];
+template <knn_dtype DT, bool PROBS>
+void launch(const SampleArgs &a, int log2_unit, int piece_log2, hipStream_t stream) {
+    const dim3 grid(static_cast<unsigned>(a.rows));
+    constexpr size_t size = DT == KNN_F32 ? 4 : 2;
+    const bool vec = reinterpret_cast<uintptr_t>(a.scores) % (4 * size) == 0 && a.stride % 4 == 0;
+    // Whole pieces, so that every element of a piece has its place.
+    const size_t bytes = ((static_cast<size_t>(a.V) + 511) & ~size_t{511}) * size;
+    if (bytes <= kHeldBytes) {
+        if (vec) k_sample<DT, true, true, PROBS><<<grid, kThreads, bytes, stream>>>(a, log2_unit, piece_log2);
+        else k_sample<DT, true, false, PROBS><<<grid, kThreads, bytes, stream>>>(a, log2_unit, piece_log2);
+    } else {
+        if (vec) k_sample<DT, false, true, PROBS><<<grid, kThreads, 0, stream>>>(a, log2_unit, piece_log2);
+        else k_sample<DT, false, false, PROBS><<<grid, kThreads, 0, stream>>>(a, log2_unit, piece_log2);
     }
-    auto ordered = [&](auto f) {  // f(index, weight or 0) for the wave's piece, 64 consecutive elements at a time
-        uint64_t run = ties;
-        for (int base = i0; base < i1; base += kWave) {
-            const int i = base + lane;
-            const uint32_t key = i < i1 ? key_of(element<DT>(row, i), a.probabilities) : 0;
-            bool stays = key > cut;
-            if (rest > 0) {
-                const uint64_t eq = __ballot(i < i1 && key == cut);
-                stays |= i < i1 && key == cut && run + __popcll(eq & ((1ull << lane) - 1)) < rest;
-                run += __popcll(eq);
-            }
-            double x = 0.0;
-            if (stays) {
-                x = greedy ? w.scale : w.of(key);
-                stays = w.heavy(x) || greedy;
-            }
-            if (f(i, stays, stays ? w.whole(x) : 0, x)) break;
-        }
-    };
-    uint64_t sum = 0;
-    uint32_t n = 0;
-    ordered([&](int, bool stays, uint64_t q, double) {
-        sum += q;
-        n += stays ? 1u : 0u;
-        return false;
-    });
-    sum = wave_sum64(sum);
-    n = wave_sum32(n);
-    __syncthreads();
-    if (lane == 0) {
-        sh.part[wave] = sum;
-        sh.part32[wave] = n;
-    }
-    __syncthreads();
-    uint64_t total = 0, mine = 0;
-    uint32_t kept = 0;
-    for (int v = 0; v < kWaves; ++v) {
-        if (v == wave) mine = total;
-        total += sh.part[v];
-        kept += sh.part32[v];
-    }
-    if (threadIdx.x == 0 && a.kept != nullptr) a.kept[r] = static_cast<int32_t>(kept);
-    const float u = a.uniforms[r];
-    const double aim = (u > 0.0f ? fmin(static_cast<double>(u), 1.0) : 0.0) * static_cast<double>(total);
-    uint64_t goal = static_cast<uint64_t>(aim);  // the token is the first whose running weight exceeds it
-    if (goal >= total) goal = total - 1;
-    if (goal < mine || goal >= mine + sum) return;
-    ordered([&](int i, bool, uint64_t q, double x) {
-        uint64_t incl = q;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const uint64_t up = __shfl_up(incl, o);
-            if (lane >= o) incl += up;
-        }
-        const uint64_t hit = __ballot(mine + incl > goal);
-        if (hit != 0) {
-            if (lane == __ffsll(static_cast<unsigned long long>(hit)) - 1) {
-                a.token[r] = i;
-                if (a.prob != nullptr) a.prob[r] = static_cast<float>(x / static_cast<double>(total));
-            }
-            return true;
-        }
-        mine += __shfl(incl, 63);
-        return false;
-    });
+}
+
+template <knn_dtype DT>
+hipError_t launch(const SampleArgs &a, hipStream_t stream) {
+    int bits = 0;
+    while ((int64_t{1} << bits) < a.V) ++bits;
+    const int unit = bits < 11 ? 51 : 62 - bits;  // 2^51 is what a sum with 2^52 can round to a whole number
+    const int piece = bits - 11 > kPieceLog2 ? bits - 11 : kPieceLog2;  // at most kBins pieces
+    if (a.probabilities) launch<DT, true>(a, unit, piece, stream);
+    else launch<DT, false>(a, unit, piece, stream);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs &a, knn_dtype dtype, void *, hipStream_t stream) {
-    int bits = 0;
-    while ((int64_t{1} << bits) < a.V) ++bits;
-    const dim3 grid(static_cast<unsigned>(a.rows));
     switch (dtype) {
-    case KNN_F32: k_sample<KNN_F32><<<grid, kThreads, 0, stream>>>(a, 62 - bits); break;
-    case KNN_BF16: k_sample<KNN_BF16><<<grid, kThreads, 0, stream>>>(a, 62 - bits); break;
-    default: k_sample<KNN_F16><<<grid, kThreads, 0, stream>>>(a, 62 - bits); break;
+    case KNN_F32: return launch<KNN_F32>(a, stream);
+    case KNN_BF16: return launch<KNN_BF16>(a, stream);
+    default: return launch<KNN_F16>(a, stream);
     }
-    return hipGetLastError();
 }
 
 }  // namespace knnlm

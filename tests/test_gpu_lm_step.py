@@ -136,4 +136,8 @@ def test_a_tree_is_drafted_verified_kept_and_decoded_on():
     other = Sequence(layer)
     all_tokens = [torch.cat([tokens[:37], drafts[[0, 1, 3, 4]], last[:1]]), torch.cat([tokens[37:], drafts[6:8], last[1:]])]
     fed = other.step(torch.cat(all_tokens), [0, 42, 42 + 93])
-    assert (after - fed[[41, 134]]).abs().max() <= 2.0 ** -8 * 4 * fed[[41, 134]].abs().max()
+    # the caches hold the same bits, so either side is off by half a step of the result and of its weights, of which the
+    # mass is at most the largest value's, 1e-4 of it for the 32-bit scores
+    most = float(np.nan_to_num(np.abs(host(seq.v))).max())
+    want = host(fed[[41, 134]])
+    assert (np.abs(host(after) - want) <= 2 * (2.0 ** -8 * (2 * np.abs(want) + most) + 1e-4 * most) + 1e-6).all()
