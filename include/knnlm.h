@@ -514,7 +514,7 @@ size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_head
  *   workspace      knn_sample_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
  *
  * Weights are in 64 bits and are summed as whole numbers of 2^-s of the
- * largest, s = 62 - ceil(log2 V), so the outcome is the same bits every time
+ * largest, s = 62 - ceil(log2(V + 3)) and at most 51, so the outcome is the same bits every time
  * and that of exact arithmetic but for borders that lie that near.
  * V <= 2^24 (KNN_ERR_UNSUPPORTED above).
  */

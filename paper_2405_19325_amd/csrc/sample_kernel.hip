@@ -60,43 +60,75 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key ^ ((key >> 31) != 0 ? 0x80000000u : 0xffffffffu));
 }
 
-// 2^a to 2^-51 relative, a <= 0: the power series of exp(f ln 2), |f| <= 1/2,
-// whose 13th term is 2e-16.  What is under 2^-200 counts as that.
-__device__ __forceinline__ double power2(double a) {
-    a = fmax(a, -200.0);
-    const double n = rint(a), f = a - n;
-    double r = 2.5678435993488206e-11;  // ln(2)^12 / 12!
-    r = fma(r, f, 4.4455382718708116e-10);
-    r = fma(r, f, 7.0549116208011230e-09);
-    r = fma(r, f, 1.0178086009239700e-07);
-    r = fma(r, f, 1.3215486790144310e-06);
-    r = fma(r, f, 1.5252733804059840e-05);
-    r = fma(r, f, 1.5403530393381610e-04);
-    r = fma(r, f, 1.3333558146428443e-03);
-    r = fma(r, f, 9.6181291076284770e-03);
-    r = fma(r, f, 5.5504108664821580e-02);
-    r = fma(r, f, 2.4022650695910070e-01);
-    r = fma(r, f, 6.9314718055994530e-01);
-    r = fma(r, f, 1.0);
-    return ldexp(r, static_cast<int>(n));
+// 2^(y / 64) 2^e for y <= 0, to 2^-51 relative: a table of the 64th roots of
+// two, and the power series of exp(f ln(2) / 64), |f| <= 1/2, whose 6th term is
+// 4e-17.  What is under 2^-200 counts as that.
+__device__ __forceinline__ double power2(double y, int e, const double *roots) {
+    y = fmax(y, -12800.0);
+    const double moved = y + 6755399441055744.0;  // 1.5 2^52: the nearest whole number in the low bits
+    const double f = y - (moved - 6755399441055744.0);
+    const int n = static_cast<int>(__double_as_longlong(moved));
+    const double root = roots[n & 63];
+    double r = 1.2417843701716923e-12;           // c^5 / 5!, c = ln(2) / 64
+    r = fma(r, f, 5.732851688640402e-10);       // c^4 / 4!
+    r = fma(r, f, 2.1173137155464774e-07);       // c^3 / 3!
+    r = fma(r, f, 5.864904955056169e-05);       // c^2 / 2
+    r = fma(r, f, 0.010830424696249145);       // c
+    return ldexp(fma(root, r * f, root), (n >> 6) + e);
 }
 
-enum Kind { kLogits, kPlain, kPower };  // kPlain: probabilities at T = 1, which are their own weights
+// log2 of a positive finite x, to 2^-50: x = 2^e m, and with c one of 64 values
+// near 1 / m, log2 m = -log2 c + log2(1 + r), r = m c - 1, |r| < 2^-6.9, by
+// the series of the logarithm, whose 8th term is 2^-58.
+__device__ __forceinline__ double log2_of(float x, const double2 *logs) {
+    const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(static_cast<double>(x)));
+    const double m = __longlong_as_double(static_cast<long long>((bits & 0x000fffffffffffffull) | 0x3ff0000000000000ull));
+    const double2 at = logs[(bits >> 46) & 63];
+    const double r = fma(m, at.x, -1.0);
+    double q = 1.0 / 7.0;
+    q = fma(q, r, -1.0 / 6.0);
+    q = fma(q, r, 1.0 / 5.0);
+    q = fma(q, r, -1.0 / 4.0);
+    q = fma(q, r, 1.0 / 3.0);
+    q = fma(q, r, -1.0 / 2.0);
+    q = fma(q, r, 1.0);
+    return fma(r * q, 1.4426950408889634074, at.y) + static_cast<double>(static_cast<int>(bits >> 52) - 1023);
+}
 
-// The weights of a row, as a function of the value; the largest one's is 2^s
-// (kPlain: at most, with the values brought under 1 by a power of two).
-template <Kind KIND>
+// The weights of a row, as a function of the value; the largest one's is 2^s.
+// Probabilities at T = 1 are their own weights (`plain`), brought under 2^s by
+// a power of two.
+template <bool PROBS>
 struct Weights {
-    float top;     // the largest value
-    double rate;   // log2(e) / T, or 1 / T of probabilities
+    double top;    // the largest value, or its log2 where the values are probabilities
+    double rate;   // 64 log2(e) / T, or 64 / T of probabilities
     double unit;   // 2^s
     double least;  // min-p, as a weight
+    int log2_unit;
+    bool plain;
+    const double *roots;
+    const double2 *logs;
 
+    // An infinite value is as far from the largest as that from itself.
+    __device__ __forceinline__ static float finite(float x) { return fminf(x, 3.402823466e38f); }
+    template <int N>
+    __device__ __forceinline__ void of(const float (&x)[N], double (&v)[N]) const {
+        if (PROBS && plain) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) v[c] = static_cast<double>(x[c]) * unit;
+        } else {
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                const double far = (PROBS ? log2_of(finite(x[c]), logs) : static_cast<double>(finite(x[c]))) - top;
+                v[c] = power2(far * rate, log2_unit, roots);
+            }
+        }
+    }
     __device__ __forceinline__ double of(float x) const {
-        if constexpr (KIND == kPlain) return static_cast<double>(x) * unit;
-        double far = static_cast<double>(x) - static_cast<double>(top);
-        if constexpr (KIND == kPower) far = log2(static_cast<double>(x) / static_cast<double>(top));
-        return power2(x == top ? 0.0 : far * rate) * unit;  // (an infinite one is as far as itself)
+        const float y[1] = {x};
+        double v[1];
+        of(y, v);
+        return v[0];
     }
     // To the nearest whole number: w < 2^52, so the sum's low bits are it.
     __device__ __forceinline__ static uint64_t whole(double w) {
@@ -105,6 +137,8 @@ struct Weights {
 };
 
 struct Shared {
+    double roots[64];  // 2^(i / 64)
+    double2 logs[64];  // of the 64ths of [1, 2): c = 1 / its middle, -log2(c)
     uint64_t mass[kBins];  // bins, then the weights of the row's pieces
     uint64_t list[kList];  // key << 32 | ~index: larger is earlier in the order
     uint64_t weight[kList];
@@ -137,13 +171,15 @@ __device__ __forceinline__ uint32_t wave_sum32(uint32_t v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
+// What the lanes up to this one hold: shifts within the 16 lanes of a row, then the rows before.
 __device__ __forceinline__ uint64_t wave_scan64(uint64_t v, int lane) {
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const uint64_t up = __shfl_up(v, o);
-        if (lane >= o) v += up;
-    }
-    return v;
+    v += dpp_u64<0x111>(v);  // row_shr:1
+    v += dpp_u64<0x112>(v);  // row_shr:2
+    v += dpp_u64<0x114>(v);  // row_shr:4
+    v += dpp_u64<0x118>(v);  // row_shr:8
+    const uint64_t r0 = readlane_u64(v, 15), r1 = r0 + readlane_u64(v, 31), r2 = r1 + readlane_u64(v, 47);
+    const int row = lane >> 4;
+    return v + (row == 0 ? 0 : row == 1 ? r0 : row == 2 ? r1 : r2);
 }
 
 // The sum of sh.mass; with hit(before, own) true for one entry, its number and
@@ -172,15 +208,16 @@ __device__ __forceinline__ uint64_t scan_bins(Shared &sh, Goal goal_of, Hit hit)
 
 constexpr int kPieceLog2 = 9;  // elements of a row's pieces (more where a row would have over kBins of them)
 
-// A row of scores: in LDS from the first reading on (HELD), or in memory.  VEC:
-// four elements a load.
-template <knn_dtype DT, bool HELD, bool VEC, bool PROBS>
+// A row of scores: in LDS from the first reading on (HELD), or in memory.  Its
+// places start at the 4-element boundary in memory at or before the first
+// element: element i is at place i + lead, places outside the row are absent.
+template <knn_dtype DT, bool HELD, bool PROBS>
 struct Row {
-    const char *row;
-    char *held;
-    int V, pieces, piece_log2;
-
     static constexpr int SIZE = DT == KNN_F32 ? 4 : 2;
+    const char *row;  // place 0
+    char *held;
+    int lead, end;  // the elements' places
+    int pieces, piece_log2;
 
     __device__ __forceinline__ static void widen4(const void *p, float (&x)[4]) {
         if constexpr (DT == KNN_F32) {
@@ -194,77 +231,114 @@ struct Row {
             for (int c = 0; c < 4; ++c) x[c] = element<DT>(h, c);
         }
     }
-    // Elements i .. i + 3 (i a multiple of four) of the row in memory; absent past its end.
+    __device__ __forceinline__ float at(int i) const {
+        return i >= lead && i < end ? present(element<DT>(row, i), PROBS) : -INFINITY;
+    }
+    // Places i .. i + 3 (i a multiple of four).
     __device__ __forceinline__ void read4(int i, float (&x)[4]) const {
-        if (VEC && i + 3 < V) {
+        if (i >= lead && i + 3 < end) {
             widen4(row + static_cast<int64_t>(i) * SIZE, x);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = present(x[c], PROBS);
         } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = i + c < V ? element<DT>(row, i + c) : -INFINITY;
+            for (int c = 0; c < 4; ++c) x[c] = at(i + c);
         }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] = present(x[c], PROBS);
     }
     __device__ __forceinline__ void load4(int i, float (&x)[4]) const {
         if constexpr (HELD) widen4(held + i * SIZE, x); else read4(i, x);
     }
-    __device__ __forceinline__ float at(int i) const {
-        return i < V ? present(element<DT>(row, i), PROBS) : -INFINITY;
+    __device__ __forceinline__ void load8(int i, float (&x)[8]) const {
+        float u[4], v[4];
+        load4(i, u);
+        load4(i + 256, v);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[c] = u[c], x[c + 4] = v[c];
+    }
+    // f(place, value) over this wave's pieces, one place a lane: where there is little code to spare.
+    template <typename F, typename Done>
+    __device__ __forceinline__ void slow_pass(int wave, int lane, F f, Done done) const {
+        const int each = (pieces + kWaves - 1) / kWaves;
+        const int last = min(pieces, (wave + 1) * each);
+        for (int piece = wave * each; piece < last; ++piece) {
+#pragma unroll 1
+            for (int i = piece << piece_log2; i < (piece + 1) << piece_log2; i += kWave) f(i + lane, at(i + lane));
+            done(piece);
+        }
     }
     __device__ __forceinline__ void keep4(int i, const float (&x)[4]) const {
         if constexpr (DT == KNN_F32) {
             *reinterpret_cast<float4 *>(held + i * 4) = make_float4(x[0], x[1], x[2], x[3]);
         } else {  // the values came from the type, so they go back exactly
+            uint32_t h[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                if constexpr (DT == KNN_BF16)
-                    reinterpret_cast<uint16_t *>(held)[i + c] = static_cast<uint16_t>(__float_as_uint(x[c]) >> 16);
-                else
-                    reinterpret_cast<_Float16 *>(held)[i + c] = static_cast<_Float16>(x[c]);
-            }
+            for (int c = 0; c < 4; ++c)
+                h[c] = DT == KNN_BF16 ? __float_as_uint(x[c]) >> 16
+                                      : __builtin_bit_cast(uint16_t, static_cast<_Float16>(x[c]));
+            *reinterpret_cast<uint2 *>(held + i * 2) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
         }
     }
-    // f(index, value) over this wave's pieces, which are consecutive; done(piece) after each.
+    // f(place of x[0], x) for this wave's pieces, which are consecutive, four
+    // places a lane; done(piece) after each piece.  FIRST: the first reading.
     template <bool FIRST = false, typename F, typename Done>
     __device__ __forceinline__ void pass(int wave, int lane, F f, Done done) const {
         const int each = (pieces + kWaves - 1) / kWaves;
-        const int end = min(pieces, (wave + 1) * each);
-        for (int piece = wave * each; piece < end; ++piece) {
-            for (int i = piece << piece_log2; i < (piece + 1) << piece_log2; i += 512) {
-                float x[2][4];
+        const int last = min(pieces, (wave + 1) * each);
+        if constexpr (FIRST) {  // eight loads a lane in flight
+            const int stop = last << piece_log2;
+            for (int i = (wave * each) << piece_log2; i < stop; i += 2048) {
+                float x[8][4];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int at = i + 256 * j + 4 * lane;
-                    if constexpr (FIRST) read4(at, x[j]); else load4(at, x[j]);
-                    if constexpr (FIRST && HELD) keep4(at, x[j]);
+                for (int j = 0; j < 8; ++j)
+                    if (i + 256 * j < stop) read4(i + 256 * j + 4 * lane, x[j]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (i + 256 * j < stop) {
+                        if constexpr (HELD) keep4(i + 256 * j + 4 * lane, x[j]);
+                        f(i + 256 * j + 4 * lane, x[j]);
+                    }
                 }
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) f(i + 256 * j + 4 * lane + c, x[j][c]);
             }
-            done(piece);
+        } else {
+            // x[c] is at place i + 4 lane + c + (c < 4 ? 0 : 252); the next eight are on their way meanwhile
+            const int stop = last << piece_log2, mask = (1 << piece_log2) - 1;
+            int i = (wave * each) << piece_log2;
+            if (i >= stop) return;
+            float x[8], next[8];
+            load8(i + 4 * lane, x);
+            for (; i < stop; i += 512) {
+                if (i + 512 < stop) load8(i + 512 + 4 * lane, next);
+                f(i + 4 * lane, x);
+                if (((i + 512) & mask) == 0) done(i >> piece_log2);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) x[c] = next[c];
+            }
         }
     }
 };
 
+__device__ __forceinline__ int place(int i, int c) { return i + c + (c < 4 ? 0 : 252); }
+
 // The filters and the draw of a row whose largest present value is `top` and
 // smallest `low`, at a temperature t > 0 and top-p p > 0.
-template <Kind KIND, typename R>
+template <bool PROBS, typename R>
 __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &sh, int64_t r, float top, float low, float t,
                                      float p, int log2_unit) {
-    constexpr bool PROBS = KIND != kLogits;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int V = rw.V, pieces = rw.pieces, piece_log2 = rw.piece_log2;
+    const int V = rw.end - rw.lead, pieces = rw.pieces, piece_log2 = rw.piece_log2;
     auto pass = [&](auto f, auto done) { rw.pass(wave, lane, f, done); };
     auto nothing = [](int) {};
-    Weights<KIND> w;
-    w.top = top;
-    w.rate = (PROBS ? 1.0 : 1.4426950408889634074) / static_cast<double>(t);
-    w.unit = ldexp(1.0, log2_unit - (KIND == kPlain ? ilogb(static_cast<double>(top)) + 1 : 0));
+    Weights<PROBS> w;
+    w.plain = PROBS && t == 1.0f && top < INFINITY;
+    w.roots = sh.roots;
+    w.logs = sh.logs;
+    w.top = PROBS ? log2_of(w.finite(top), sh.logs) : static_cast<double>(w.finite(top));
+    w.rate = (PROBS ? 64.0 : 92.332482616893656874) / static_cast<double>(t);
+    w.log2_unit = log2_unit - (w.plain ? ilogb(static_cast<double>(top)) + 1 : 0);
+    w.unit = ldexp(1.0, w.log2_unit);
     const float min_p = a.min_p != nullptr ? a.min_p[r] : 0.0f;
     w.least = (min_p > 0.0f ? fmin(static_cast<double>(min_p), 1.0) : 0.0) *
-              (KIND == kPlain ? static_cast<double>(top) * w.unit : w.unit);
+              (w.plain ? static_cast<double>(top) * w.unit : w.unit);
 
     // Bins that follow the order; what is past the last one's start is in it.
     // Logits: steps of the distance from the largest, over 32 T or the row's
@@ -302,27 +376,77 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
         if (lane == 0) sh.mass[piece] = s;
         run = 0;
     };
-    auto add = [&](float x) {
-        const double v = w.of(x);
-        if (v >= w.least) {
-            run += Weights<KIND>::whole(v);
-            ++kept;
-        }
+    // The weights of eight places at once, where any lane needs one.
+    auto weigh = [&](const float (&x)[8], const bool (&in)[8], auto f) {
+        bool any = false;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) any |= in[c];
+        if (!__any(any)) return;
+        double v[8];
+        w.of(x, v);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) f(c, v[c]);
     };
-    // The cut at `goal` (a count, or a weight) of the elements that stay, whose
-    // bins are in sh.mass, from sh.bin and sh.before on; with `last` the pieces' weights too.
-    auto cut_at = [&](bool by_weight, double goal, bool last) {
+    auto add = [&](const float (&x)[8], const bool (&in)[8]) {
+        weigh(x, in, [&](int c, double v) {
+            const bool keep = in[c] && v >= w.least;
+            run += keep ? Weights<PROBS>::whole(v) : 0;
+            kept += keep ? 1u : 0u;
+        });
+    };
+    auto count = [&](uint64_t v, uint32_t bin) {
+        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[bin]), static_cast<unsigned long long>(v));
+    };
+    // The cuts: by count (top-k), then by weight (top-p).
+    const int k = a.top_k != nullptr ? a.top_k[r] : 0;
+    const bool stages[2] = {k > 0 && k < V, p < 1.0f};
+#pragma unroll 1
+    for (int stage = 0; stage < 2; ++stage) {
+        if (stage == 0 ? !stages[0] : !stages[1]) continue;
+        const bool by_weight = stage == 1, last = by_weight || !stages[1];  // last: sums the row's pieces too
+        clear();
+        pass(
+            [&](int i, const float (&x)[8]) {
+                bool in[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) in[c] = stays(place(i, c), x[c]);
+                if (by_weight) {
+                    weigh(x, in, [&](int c, double v) {
+                        if (in[c]) count(Weights<PROBS>::whole(v), bin_of(x[c]));
+                    });
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        if (in[c]) count(1, bin_of(x[c]));
+                }
+            },
+            nothing);
+        __syncthreads();
+        const double share = p;
+        auto goal_of = [&](uint64_t all) { return by_weight ? share * static_cast<double>(all) : static_cast<double>(k); };
+        auto crosses = [](uint64_t at, uint64_t v, double to) {
+            return static_cast<double>(at) < to && static_cast<double>(at + v) >= to;
+        };
+        const uint64_t all = scan_bins(sh, goal_of, crosses);
+        if (!by_weight && static_cast<uint64_t>(k) >= all) continue;  // all that is present stays
+        const double goal = goal_of(all);
         const uint32_t bin = sh.bin;
         const uint64_t before = sh.before;
         pass(
-            [&](int i, float x) {
-                const bool in = stays(i, x);
-                const uint32_t b = bin_of(x);
-                if (in && b == bin) {
-                    const uint32_t at = atomicAdd(&sh.listed, 1u);
-                    if (at < kList) sh.list[at] = static_cast<uint64_t>(key_of(x)) << 32 | ~static_cast<uint32_t>(i);
+            [&](int i, const float (&x)[8]) {
+                bool under[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const bool in = stays(place(i, c), x[c]);
+                    const uint32_t b = bin_of(x[c]);
+                    if (in && b == bin) {
+                        const uint32_t at = atomicAdd(&sh.listed, 1u);
+                        if (at < kList)
+                            sh.list[at] = static_cast<uint64_t>(key_of(x[c])) << 32 | ~static_cast<uint32_t>(place(i, c));
+                    }
+                    under[c] = in && b < bin;
                 }
-                if (last && in && b < bin) add(x);
+                if (last) add(x, under);
             },
             [&](int piece) {
                 if (last) end_piece(piece);
@@ -330,129 +454,105 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
         __syncthreads();
         const int n = static_cast<int>(sh.listed);
         if (n <= kList) {
-            const int me = threadIdx.x;
-            uint64_t mine = 0, own = 0;
-            if (me < n) {
-                mine = sh.list[me];
-                own = by_weight || last ? Weights<KIND>::whole(w.of(value_of(static_cast<uint32_t>(mine >> 32)))) : 0;
-                sh.weight[me] = by_weight ? own : 1;
+            if (static_cast<int>(threadIdx.x) < n) {
+                const double v = w.of(value_of(static_cast<uint32_t>(sh.list[threadIdx.x] >> 32)));
+                sh.weight[threadIdx.x] = Weights<PROBS>::whole(v);
             }
             __syncthreads();
-            bool in = false;
-            if (me < n) {
-                uint64_t ahead = before;
-                for (int j = 0; j < n; ++j) ahead += sh.list[j] > mine ? sh.weight[j] : 0;
-                in = static_cast<double>(ahead) < goal;
-                if (in) atomicMin(reinterpret_cast<unsigned long long *>(&sh.cut), static_cast<unsigned long long>(mine));
-            }
-            if (last && in) {
-                const double v = w.of(value_of(static_cast<uint32_t>(mine >> 32)));
-                if (v >= w.least) {
-                    const int i = static_cast<int>(~static_cast<uint32_t>(mine));
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[i >> piece_log2]),
-                              static_cast<unsigned long long>(own));
-                    ++kept;
+            // What lies before each entry: eight lanes an entry, each over an eighth of the others.
+            for (int first = 0; first < n; first += kThreads / 8) {
+                const int me = first + static_cast<int>(threadIdx.x >> 3);
+                const uint64_t mine = me < n ? sh.list[me] : ~0ull;
+                uint64_t ahead = 0;
+                for (int j = threadIdx.x & 7; j < n; j += 8)
+                    ahead += sh.list[j] > mine ? (by_weight ? sh.weight[j] : 1) : 0;
+                ahead += dpp_u64<0xB1>(ahead);
+                ahead += dpp_u64<0x4E>(ahead);
+                ahead += dpp_u64<0x141>(ahead);
+                if (me < n && (threadIdx.x & 7) == 0 && static_cast<double>(before + ahead) < goal) {
+                    atomicMin(reinterpret_cast<unsigned long long *>(&sh.cut), static_cast<unsigned long long>(mine));
+                    const double v = w.of(value_of(static_cast<uint32_t>(mine >> 32)));
+                    if (last && v >= w.least) {
+                        count(sh.weight[me], ~static_cast<uint32_t>(mine) >> piece_log2);
+                        ++kept;
+                    }
                 }
             }
             __syncthreads();
             cut_x = value_of(static_cast<uint32_t>(sh.cut >> 32));
             cut_i = static_cast<int>(~static_cast<uint32_t>(sh.cut));
             summed = last;
-            return;
+            continue;
         }
         kept = 0;
         run = 0;
         // By keys, eleven bits a pass: the key of the cut, and how much of the goal is left for the elements equal to it.
         uint32_t prefix = 0;
         uint64_t above = 0;
+#pragma unroll 1
         for (int level = 0; level < 3; ++level) {
             const int low_bit = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
             clear();
-            pass(
+            rw.slow_pass(
+                wave, lane,
                 [&](int i, float x) {
                     const uint32_t key = key_of(x);
                     if (!stays(i, x) || (level > 0 && key >> (low_bit + bits) != prefix)) return;
-                    const uint32_t b = kBins - 1 - ((key >> low_bit) & ((1u << bits) - 1));
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[b]),
-                              by_weight ? static_cast<unsigned long long>(Weights<KIND>::whole(w.of(x))) : 1ull);
+                    count(by_weight ? Weights<PROBS>::whole(w.of(x)) : 1,
+                          kBins - 1 - ((key >> low_bit) & ((1u << bits) - 1)));
                 },
                 nothing);
             __syncthreads();
             const uint64_t base = above;
-            scan_bins(sh, [&](uint64_t) { return goal; }, [&](uint64_t at, uint64_t v, double to) {
-                return static_cast<double>(base + at) < to && static_cast<double>(base + at + v) >= to;
-            });
+            scan_bins(sh, [&](uint64_t) { return goal; },
+                      [&](uint64_t at, uint64_t v, double to) { return crosses(base + at, v, to); });
             prefix = prefix << bits | ((kBins - 1 - sh.bin) & ((1u << bits) - 1));
             above = base + sh.before;
         }
         const float x_at = value_of(prefix);
-        const uint64_t one = by_weight ? Weights<KIND>::whole(w.of(x_at)) : 1;
+        const uint64_t one = by_weight ? Weights<PROBS>::whole(w.of(x_at)) : 1;
         // The n-th element equal to it is the last before which less than the goal lies.
         uint64_t left = static_cast<uint64_t>((goal - static_cast<double>(above)) / static_cast<double>(one));
         while (static_cast<double>(above + left * one) < goal) ++left;
         while (left > 1 && static_cast<double>(above + (left - 1) * one) >= goal) --left;
         clear();
         uint32_t equal = 0;
-        pass([&](int i, float x) { equal += x == x_at && stays(i, x) ? 1u : 0u; },
-             [&](int piece) {
-                 const uint32_t s = wave_sum32(equal);
-                 if (lane == 0) sh.mass[piece] = s;
-                 equal = 0;
-             });
+        rw.slow_pass(
+            wave, lane, [&](int i, float x) { equal += x == x_at && stays(i, x) ? 1u : 0u; },
+            [&](int piece) {
+                const uint32_t s = wave_sum32(equal);
+                if (lane == 0) sh.mass[piece] = s;
+                equal = 0;
+            });
         __syncthreads();
-        scan_bins(sh, [&](uint64_t) { return left; },
-                  [&](uint64_t at, uint64_t v, uint64_t to) { return at < to && at + v >= to; });
+        scan_bins(sh, [&](uint64_t) { return static_cast<double>(left); }, crosses);
         if (wave == 0) {
             uint64_t seen = sh.before;
             bool found = false;
             for (int i = static_cast<int>(sh.bin) << piece_log2; !found; i += kWave) {
                 const int at = i + lane;
-                const float x = at < V ? rw.at(at) : -INFINITY;
+                const float x = rw.at(at);
                 const uint64_t eq = __ballot(x == x_at && stays(at, x));
                 const int here = __popcll(eq & ((2ull << lane) - 1));
-                if (x == x_at && ((eq >> lane) & 1) != 0 && seen + here == left) sh.index = at;
+                if (((eq >> lane) & 1) != 0 && seen + here == left) sh.index = at;
                 seen += __popcll(eq);
-                found = seen >= left || i + kWave >= V;
+                found = seen >= left || i + kWave >= rw.end;
             }
         }
         __syncthreads();
         cut_i = sh.index;
         cut_x = x_at;
-    };
-
-    const int k = a.top_k != nullptr ? a.top_k[r] : 0;
-    if (k > 0 && k < V) {
-        clear();
-        pass(
-            [&](int i, float x) {
-                if (stays(i, x)) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[bin_of(x)]), 1ull);
-            },
-            nothing);
-        __syncthreads();
-        const uint64_t n = scan_bins(sh, [&](uint64_t) { return static_cast<uint64_t>(k); },
-                                     [&](uint64_t at, uint64_t v, uint64_t to) { return at < to && at + v >= to; });
-        if (static_cast<uint64_t>(k) < n) cut_at(false, k, !(p < 1.0f));
-    }
-    if (p < 1.0f) {
-        clear();
-        pass(
-            [&](int i, float x) {
-                if (stays(i, x))
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[bin_of(x)]),
-                              static_cast<unsigned long long>(Weights<KIND>::whole(w.of(x))));
-            },
-            nothing);
-        __syncthreads();
-        const double share = p;
-        const uint64_t sum = scan_bins(sh, [&](uint64_t all) { return share * static_cast<double>(all); },
-                                       [&](uint64_t at, uint64_t v, double to) {
-                                           return static_cast<double>(at) < to && static_cast<double>(at + v) >= to;
-                                       });
-        cut_at(true, share * static_cast<double>(sum), true);
     }
     if (!summed) {
         clear();
-        pass([&](int i, float x) { if (stays(i, x)) add(x); }, end_piece);
+        pass(
+            [&](int i, const float (&x)[8]) {
+                bool in[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) in[c] = stays(place(i, c), x[c]);
+                add(x, in);
+            },
+            end_piece);
     } else {
         __syncthreads();
     }
@@ -479,7 +579,7 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const double v = stays(i + 4 * lane + c, x[c]) ? w.of(x[c]) : 0.0;
-            q[c] = v >= w.least ? Weights<KIND>::whole(v) : 0;
+            q[c] = v >= w.least ? Weights<PROBS>::whole(v) : 0;
             sum += q[c];
         }
         const uint64_t incl = wave_scan64(sum, lane);
@@ -494,31 +594,44 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
                     c += here <= goal ? 1 : 0;
                 }
                 const float v = c == 0 ? x[0] : c == 1 ? x[1] : c == 2 ? x[2] : x[3];
-                a.token[r] = i + 4 * lane + c;
+                a.token[r] = i + 4 * lane + c - rw.lead;
                 if (a.prob != nullptr) a.prob[r] = static_cast<float>(w.of(v) / static_cast<double>(total));
                 if (a.kept != nullptr) a.kept[r] = static_cast<int32_t>(sh.kept);
             }
             return;
         }
         before += __shfl(incl, 63);
-        if (i + 256 >= V) return;  // not reached: the piece holds the goal
+        if (i + 256 >= rw.end) return;  // not reached: the piece holds the goal
     }
 }
 
-template <knn_dtype DT, bool HELD, bool VEC, bool PROBS>
+template <knn_dtype DT, bool HELD, bool PROBS>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit, int piece_log2) {
     __shared__ Shared sh;
     extern __shared__ __align__(16) char held[];
     const int64_t r = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    using R = Row<DT, HELD, VEC, PROBS>;
-    const R rw{static_cast<const char *>(a.scores) + r * a.stride * R::SIZE, held, a.V,
-               (a.V + (1 << piece_log2) - 1) >> piece_log2, piece_log2};
-    auto nothing = [](int) {};
+    using R = Row<DT, HELD, PROBS>;
+    const char *first_of_row = static_cast<const char *>(a.scores) + r * a.stride * R::SIZE;
+    const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(first_of_row) % (4 * R::SIZE)) / R::SIZE;
+    const R rw{first_of_row - lead * R::SIZE, held, lead, lead + a.V, (lead + a.V + (1 << piece_log2) - 1) >> piece_log2,
+               piece_log2};
 
+    if (threadIdx.x < 64) {
+        sh.roots[threadIdx.x] = exp2(threadIdx.x * (1.0 / 64.0));
+        if constexpr (PROBS) {
+            const double c = 1.0 / (1.0 + (threadIdx.x + 0.5) * (1.0 / 64.0));
+            sh.logs[threadIdx.x] = make_double2(c, -log2(c));
+        }
+    }
     float top = -INFINITY, low = INFINITY;  // the largest and the smallest present value
-    rw.template pass<true>(wave, lane, [&](int, float x) { top = fmaxf(top, x), low = fminf(low, x > -INFINITY ? x : INFINITY); },
-                           nothing);
+    rw.template pass<true>(
+        wave, lane,
+        [&](int, const float (&x)[4]) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) top = fmaxf(top, x[c]), low = fminf(low, x[c] > -INFINITY ? x[c] : INFINITY);
+        },
+        [](int) {});
     top = wave_allmax(top);
     low = wave_allmin(low);
     if (lane == 0) sh.part32[wave] = __float_as_uint(top), sh.part[wave] = __float_as_uint(low);
@@ -541,45 +654,39 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit
     const float p = a.top_p != nullptr ? a.top_p[r] : 1.0f;
     if (!(t > 0.0f) || p <= 0.0f) {  // the first element of the order
         int first = 0x7fffffff;
-        rw.pass(wave, lane, [&](int i, float x) { first = x == top && i < first ? i : first; }, nothing);
+        rw.pass(
+            wave, lane,
+            [&](int i, const float (&x)[8]) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) first = x[c] == top && place(i, c) < first ? place(i, c) : first;
+            },
+            [](int) {});
         first = static_cast<int>(wave_allmin_u32(static_cast<uint32_t>(first)));
         if (lane == 0) atomicMin(&sh.index, first);
         __syncthreads();
         if (threadIdx.x == 0) {
-            a.token[r] = sh.index;
+            a.token[r] = sh.index - lead;
             if (a.prob != nullptr) a.prob[r] = 1.0f;
             if (a.kept != nullptr) a.kept[r] = 1;
         }
         return;
     }
-    if constexpr (!PROBS) {
-        draw<kLogits>(a, rw, sh, r, top, low, t, p, log2_unit);
-    } else {
-        if (t == 1.0f && top < INFINITY) draw<kPlain>(a, rw, sh, r, top, low, t, p, log2_unit);
-        else draw<kPower>(a, rw, sh, r, top, low, t, p, log2_unit);
-    }
+    draw<PROBS>(a, rw, sh, r, top, low, t, p, log2_unit);
 }
 
 template <knn_dtype DT, bool PROBS>
 void launch(const SampleArgs &a, int log2_unit, int piece_log2, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.rows));
-    constexpr size_t size = DT == KNN_F32 ? 4 : 2;
-    const bool vec = reinterpret_cast<uintptr_t>(a.scores) % (4 * size) == 0 && a.stride % 4 == 0;
-    // Whole pieces, so that every element of a piece has its place.
-    const size_t bytes = ((static_cast<size_t>(a.V) + 511) & ~size_t{511}) * size;
-    if (bytes <= kHeldBytes) {
-        if (vec) k_sample<DT, true, true, PROBS><<<grid, kThreads, bytes, stream>>>(a, log2_unit, piece_log2);
-        else k_sample<DT, true, false, PROBS><<<grid, kThreads, bytes, stream>>>(a, log2_unit, piece_log2);
-    } else {
-        if (vec) k_sample<DT, false, true, PROBS><<<grid, kThreads, 0, stream>>>(a, log2_unit, piece_log2);
-        else k_sample<DT, false, false, PROBS><<<grid, kThreads, 0, stream>>>(a, log2_unit, piece_log2);
-    }
+    // Whole pieces, with up to three places before the first element.
+    const size_t bytes = ((static_cast<size_t>(a.V) + 3 + 511) & ~size_t{511}) * (DT == KNN_F32 ? 4 : 2);
+    if (bytes <= kHeldBytes) k_sample<DT, true, PROBS><<<grid, kThreads, bytes, stream>>>(a, log2_unit, piece_log2);
+    else k_sample<DT, false, PROBS><<<grid, kThreads, 0, stream>>>(a, log2_unit, piece_log2);
 }
 
 template <knn_dtype DT>
 hipError_t launch(const SampleArgs &a, hipStream_t stream) {
     int bits = 0;
-    while ((int64_t{1} << bits) < a.V) ++bits;
+    while ((int64_t{1} << bits) < a.V + 3) ++bits;
     const int unit = bits < 11 ? 51 : 62 - bits;  // 2^51 is what a sum with 2^52 can round to a whole number
     const int piece = bits - 11 > kPieceLog2 ? bits - 11 : kPieceLog2;  // at most kBins pieces
     if (a.probabilities) launch<DT, true>(a, unit, piece, stream);
