@@ -29,7 +29,7 @@ def check(scores, uniforms, probabilities=False, **filters):
         where = (r, {n: v[r] for n, v in given.items()}, want, token[r], prob[r], kept[r])
         assert (token[r], kept[r]) == (want[0], want[2]), where
         # half a step of fp32, and the weights' sum in units of 2^-46 of the largest at worst (V <= 2^17)
-        assert abs(prob[r] - want[1]) <= 2.0 ** -24 * want[1] + 1e-9 * want[1] + 2.0 ** -149, where
+        assert abs(float(prob[r]) - want[1]) <= 2.0 ** -24 * want[1] + 1e-9 * want[1] + 2.0 ** -149, where
     return token, prob, kept
 
 
