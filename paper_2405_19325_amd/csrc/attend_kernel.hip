@@ -88,139 +88,65 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     return ((w & kExp) == kExp ? 0xffffu : 0u) | (((w >> 16) & kExp) == kExp ? 0xffff0000u : 0u);
 }
 
-template <int D>
-struct Shape {
-    static constexpr int W = D == 256 ? 2 : 4;         // waves of a workgroup, each on keys of its own
-    static constexpr int ROW = 2 * D;                  // bytes of a key
-    static constexpr int HALF = 32 * ROW;              // of 32 keys: one stage's K, then its V
-    static constexpr int STAGES = 2;
-    static constexpr int LOADS = HALF / 1024;          // wave loads of one half
-    static constexpr int LANES = ROW / 16;             // lanes of a load on one key
-    static constexpr int PER = 64 / LANES;             // keys of one load
-    static constexpr size_t LDS = static_cast<size_t>(W) * STAGES * 2 * HALF;
-};
-
-// W waves share NT x 16 columns; wave w takes the 32-key tiles w, w + W, ... of
-// the workgroup's range and keeps its own reference and sums, joined at the
-// end.  Each wave fills its own two stages by loads straight to LDS, one tile
-// ahead, and waits only for its own loads: no barrier in the loop.
-template <knn_dtype DT, int D, int NT>
-__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t splits, int64_t chunk,
-                                                           float *part, float *part_ml) {
-    using Sh = Shape<D>;
-    constexpr int W = Sh::W, KK = D / 32, DB = D / 16, COLS = 16 * NT;
-    extern __shared__ __align__(16) u32x4_t lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, quad = lane >> 4;
-
-    int64_t b = blockIdx.x;
-    const int64_t split = b % splits;
-    b /= splits;
-    const int64_t ct = b % tiles;
-    b /= tiles;
-    const int h = static_cast<int>(b % a.kv_heads);
-    const int64_t s = b / a.kv_heads;
-    const int g = a.q_heads / a.kv_heads;
-    const Tile t = tile_of(a, s);
-    const int64_t c0 = ct * COLS, cols = static_cast<int64_t>(t.n) * g;
-    if (c0 >= cols) return;
-    // the keys of this range that any of the columns sees
-    int64_t end = t.total;
+// Which of the four keys from `at` on a row sees, as bits, whether or not they
+// have pages: those before `limit`, of these the cached ones and the drafts.
+__device__ __forceinline__ uint32_t first_bits(int64_t n) { return n <= 0 ? 0u : n >= 4 ? 15u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t seen(const AttendArgs &a, const Tile &t, int row, int64_t at, int64_t limit) {
+    const int64_t draft = at - t.length;  // of the first key
     if (a.tree_mask == nullptr) {
-        const int64_t last = (c0 + COLS - 1 < cols ? c0 + COLS - 1 : cols - 1) / g;
-        if (t.length + last + 1 < end) end = t.length + last + 1;
+        const int64_t own = t.length + row + 1;
+        return first_bits((own < limit ? own : limit) - at);
     }
-    const int64_t k0 = split * chunk;
-    if (splits > 1 && k0 >= t.total) return;
-    if (k0 + chunk < end) end = k0 + chunk;
+    // Four bits of the row's mask from `draft` on (or from draft 0 on, moved up by the cached keys before it); they may
+    // lie in two words.  Words past the last are read as the last and count as none.
+    const uint32_t *words = a.tree_mask + (t.r0 + row) * a.mask_words;
+    const int64_t from = draft < 0 ? 0 : draft, w0 = from >> 5, w1 = (from + 3) >> 5, last = a.mask_words - 1;
+    const uint32_t lo = words[w0 < last ? w0 : last], hi = words[w1 < last ? w1 : last];
+    const uint64_t both = (w0 <= last ? lo : 0u) | static_cast<uint64_t>(w1 <= last ? hi : 0u) << 32;
+    uint32_t bits = w0 == w1 ? static_cast<uint32_t>(both) >> (from & 31) : static_cast<uint32_t>(both >> (from & 31));
+    bits = draft <= -4 ? 0u : bits << (from - draft);
+    return (first_bits(-draft) | bits) & first_bits(limit - at);
+}
 
-    // Columns: queries as the right operand, lane = (column, 8 elements a quad).
-    u32x4_t qr[NT][KK];
-    int row_of[NT];
-    bool live[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        const int64_t c = c0 + 16 * i + col;
-        live[i] = c < cols;
-        row_of[i] = live[i] ? static_cast<int>(c / g) : 0;
-        const uint16_t *q = static_cast<const uint16_t *>(a.q) + (t.r0 + row_of[i]) * a.q_row +
-                            (h * g + (live[i] ? static_cast<int>(c % g) : 0)) * a.q_head;
-#pragma unroll
-        for (int k = 0; k < KK; ++k) qr[i][k] = *reinterpret_cast<const u32x4_t *>(q + 32 * k + 8 * quad);
-    }
+// The columns of a wave: NT x 16 (row, query head) pairs of one key head.
+template <knn_dtype DT, int D, int NT>
+struct Columns {
+    static constexpr int KK = D / 32, DB = D / 16, ROW = 2 * D;
+    u32x4_t q[NT][KK];  // right operand of the scores: lane = (column, 8 elements a quad)
+    f32x4_t o[NT][DB];  // lane = (column, 4 elements a quad)
+    f32x4_t sum[NT];    // the same sum four times
+    float m[NT];        // reference, of the scores times log2(e)
+    int row_of[NT];     // row within the sequence
+    float c2;           // scale log2(e), not negative: its sign is in q
 
-    f32x4_t o[NT][DB], sum[NT];
-    float m[NT];
+    __device__ __forceinline__ void load(const AttendArgs &a, const Tile &t, int h, int g, int64_t c0, int64_t cols, int col,
+                                         int quad) {
+        c2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        m[i] = kFloor;
-        sum[i] = f32x4_t{0, 0, 0, 0};
+        for (int n = 0; n < NT; ++n) {
+            const int64_t c = c0 + 16 * n + col;
+            const bool live = c < cols;
+            row_of[n] = live ? static_cast<int>(c / g) : 0;
+            const uint16_t *at = static_cast<const uint16_t *>(a.q) + (t.r0 + row_of[n]) * a.q_row +
+                                 (h * g + (live ? static_cast<int>(c % g) : 0)) * a.q_head;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[i][d] = f32x4_t{0, 0, 0, 0};
-    }
-
-    const float c2 = a.scale * kLog2e;
-    const uint32_t mine =
-        __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * static_cast<uint32_t>(Sh::STAGES * 2 * Sh::HALF);
-    const int64_t n_tiles = end > k0 ? (end - k0 + 31) / 32 : 0;
-    const int64_t own = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // this wave's tiles
-    const int32_t *table = a.cache.pages + s * a.cache.table_width;
-    const int page_log2 = a.cache.page_log2;
-    const int64_t last_key = end - 1;
-    const int64_t head_bytes = static_cast<int64_t>(h) * Sh::ROW << page_log2;
-    const int64_t page_bytes = static_cast<int64_t>(a.kv_heads) * Sh::ROW << page_log2;
-    // Lane l keeps the page of half l & 1 of this wave's tile l / 2 from tile `held` on.
-    int32_t page_reg = 0;
-    auto hold_pages = [&](int64_t held) {
-        int64_t key = k0 + 32 * (wave + W * (held + (lane >> 1))) + 16 * (lane & 1);
-        key = key < last_key ? key : last_key;
-        page_reg = table[key >> page_log2];
-    };
-    auto page_of = [&](int64_t tile, int half) {
-        return __builtin_amdgcn_readlane(page_reg, 2 * static_cast<int>(tile & 31) + half);
-    };
-    // Tile `i` of this wave into stage i & 1.  Keys past the last one are read as the last one.
-    auto fill = [&](int64_t i) {
-        const int64_t key = k0 + 32 * (wave + W * i);
-        const uint32_t to = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            int64_t kb = key + 16 * half;
-            int32_t page = page_of(i, half);
-            if (page < 0 || page >= a.cache.n_pages) page = 0;
-            if (kb > last_key) kb = last_key & ~int64_t{15};
-            const int rows = last_key - kb < 15 ? static_cast<int>(last_key - kb) : 15;  // the last row there is
-            const int64_t at = page * page_bytes + head_bytes + (kb & ((int64_t{1} << page_log2) - 1)) * Sh::ROW;
-            const char *kp = static_cast<const char *>(a.k_cache) + at;
-            const char *vp = static_cast<const char *>(a.v_cache) + at;
-#pragma unroll
-            for (int j = 0; j < Sh::LOADS / 2; ++j) {
-                const int r = j * Sh::PER + lane / Sh::LANES;
-                const int from = r < rows ? r : rows;
-                const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread(r));
-                load_to_lds_16(kp, off, to + half * (Sh::HALF / 2) + j * 1024);
-                load_to_lds_16(vp, off, to + Sh::HALF + half * (Sh::HALF / 2) + j * 1024);
+            for (int k = 0; k < KK; ++k) {
+                u32x4_t v = *reinterpret_cast<const u32x4_t *>(at + 32 * k + 8 * quad);
+                if (a.scale == 0.0f) v = u32x4_t{0, 0, 0, 0};
+                if (a.scale < 0.0f) v ^= u32x4_t{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+                q[n][k] = v;
             }
+            m[n] = kFloor;
+            sum[n] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[n][d] = f32x4_t{0, 0, 0, 0};
         }
-    };
-
-    if (own > 0) {
-        hold_pages(0);
-        fill(0);
     }
-    for (int64_t i = 0; i < own; ++i) {
-        const int32_t page_a = page_of(i, 0), page_b = page_of(i, 1);
-        if (i + 1 < own) {
-            if (((i + 1) & 31) == 0) hold_pages(i + 1);
-            fill(i + 1);
-            __builtin_amdgcn_s_waitcnt(vmcnt_encoding<2 * Sh::LOADS>());
-        } else {
-            __builtin_amdgcn_s_waitcnt(kVmcntZero);
-        }
-        asm volatile("" ::: "memory");
-        const uint32_t kt = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF), vt = kt + Sh::HALF;
-        const int64_t key = k0 + 32 * (wave + W * i);
 
+    // 32 keys from `key` on, in LDS at kt and vt.  `all`: every column sees every one of them; else a key is seen if it
+    // is before `end`, its half's page is one, and it is cached or named by the row's mask.
+    __device__ __forceinline__ void tile(const AttendArgs &a, const Tile &t, uint32_t kt, uint32_t vt, int64_t key, bool all,
+                                         int64_t end, bool real_a, bool real_b, int col, int quad) {
         f32x4_t x[2][NT];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -229,46 +155,26 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
 #pragma unroll
             for (int k = 0; k < KK; ++k) {
                 const u32x4_t kr = *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t *>(
-                    static_cast<uintptr_t>(kt + (16 * half + col) * Sh::ROW + 16 * ((4 * k + quad) ^ spread(col))));
+                    static_cast<uintptr_t>(kt + (16 * half + col) * ROW + 16 * ((4 * k + quad) ^ spread(col))));
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[half][n] = mfma16<DT>(kr, qr[n][k], x[half][n]);
+                for (int n = 0; n < NT; ++n) x[half][n] = mfma16<DT>(kr, q[n][k], x[half][n]);
             }
         }
-        // Keys that not every column sees: drafts, keys past the end, keys without a page.
-        const bool real_a = page_a >= 0 && page_a < a.cache.n_pages, real_b = page_b >= 0 && page_b < a.cache.n_pages;
-        const bool all = key + 32 <= (t.length < end ? t.length : end) && real_a && real_b;
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[half][n][j] *= c2;
         if (!all) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t bits = (half == 0 ? real_a : real_b) ? seen(a, t, row_of[n], key + 16 * half + 4 * quad, end) : 0u;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int64_t at = key + 16 * half + 4 * quad + j;
-                        bool sees = at < end && (half == 0 ? real_a : real_b);
-                        if (sees && at >= t.length) {
-                            const int64_t draft = at - t.length;
-                            if (a.tree_mask == nullptr) {
-                                sees = draft <= row_of[n];
-                            } else {
-                                sees = (draft >> 5) < a.mask_words &&
-                                       ((a.tree_mask[(t.r0 + row_of[n]) * a.mask_words + (draft >> 5)] >> (draft & 31)) & 1u) != 0u;
-                            }
-                        }
-                        x[half][n][j] = sees ? x[half][n][j] : -INFINITY;
-                    }
+                    for (int j = 0; j < 4; ++j) x[half][n][j] = (bits >> j & 1u) != 0u ? x[half][n][j] : -INFINITY;
+                }
         }
         u32x4_t p[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float top = fmaxf(fmaxf(fmaxf(x[0][n][0], x[0][n][1]), fmaxf(x[0][n][2], x[0][n][3])),
-                              fmaxf(fmaxf(x[1][n][0], x[1][n][1]), fmaxf(x[1][n][2], x[1][n][3])));
+                              fmaxf(fmaxf(x[1][n][0], x[1][n][1]), fmaxf(x[1][n][2], x[1][n][3]))) * c2;
             if (__any(top > m[n] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -284,7 +190,7 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
             }
             float e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(x[j >> 2][n][j & 3] - m[n]);
+            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(x[j >> 2][n][j & 3], c2, -m[n]));
             p[n] = u32x4_t{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7])};
         }
         constexpr uint32_t kOne = DT == KNN_BF16 ? 0x3f803f80u : 0x3c003c00u;
@@ -293,8 +199,8 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
         const int vrow = 4 * quad + (col >> 2);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-            const uint32_t at = vt + vrow * Sh::ROW + 16 * ((2 * d + ((col >> 1) & 1)) ^ spread(vrow)) + 8 * (col & 1);
-            const u32x2_t va = read_transposed(at), vb = read_transposed(at + 16 * Sh::ROW);
+            const uint32_t at = vt + vrow * ROW + 16 * ((2 * d + ((col >> 1) & 1)) ^ spread(vrow)) + 8 * (col & 1);
+            const u32x2_t va = read_transposed(at), vb = read_transposed(at + 16 * ROW);
             u32x4_t v = {va.x, va.y, vb.x, vb.y};
             if (!all) {
                 // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such
@@ -313,6 +219,171 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
 #pragma unroll
             for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[n], o[n][d]);
         }
+    }
+};
+
+// Four elements of a finished column, or of a range's part of one, and with
+// d == 0 its reference and sum.
+template <knn_dtype DT, int D>
+__device__ __forceinline__ void store(const AttendArgs &a, int64_t splits, int64_t split, int64_t at, int d, f32x4_t r,
+                                      float top, float l, float *part, float *part_ml) {
+    if (splits > 1) {
+        const int64_t to = split * a.rows * a.q_heads + at;
+        if (d == 0) {
+            part_ml[2 * to] = top;
+            part_ml[2 * to + 1] = l;
+        }
+        *reinterpret_cast<f32x4_t *>(part + to * D + d) = r;
+    } else {
+        const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // no key: 0; NaN stays
+        *reinterpret_cast<u32x2_t *>(static_cast<uint16_t *>(a.out) + at * D + d) =
+            u32x2_t{pack2<DT>(r[0] * by, r[1] * by), pack2<DT>(r[2] * by, r[3] * by)};
+        if (d == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+    }
+}
+
+template <int D>
+struct Shape {
+    static constexpr int ROW = 2 * D;           // bytes of a key
+    static constexpr int HALF = 32 * ROW;       // of 32 keys: one stage's K, then its V
+    static constexpr int LOADS = HALF / 1024;   // wave loads of one half
+    static constexpr int LANES = ROW / 16;      // lanes of a load on one key
+    static constexpr int PER = 64 / LANES;      // keys of one load
+    // Few columns: each wave on keys of its own.
+    static constexpr int W = D == 256 ? 2 : 4;
+    static constexpr int STAGES = 2;
+    static constexpr size_t LDS = static_cast<size_t>(W) * STAGES * 2 * HALF;
+    // Many columns: four waves on the same keys.
+    static constexpr int RING = D == 256 ? 3 : 4;
+    static constexpr size_t RING_LDS = static_cast<size_t>(RING) * 2 * HALF;
+};
+
+// A workgroup's part of the work: column tile `ct` of key head h of sequence s,
+// range `split` of the keys.  Its neighbours in the grid go to the 8 XCDs in
+// turn, and those that read the same keys (column tiles of one range) to one.
+struct Work {
+    int64_t s, ct, split;
+    int h;
+    bool any;
+};
+
+__device__ __forceinline__ Work work_of(const AttendArgs &a, int64_t tiles, int64_t splits) {
+    const int64_t id = blockIdx.x, group = id / (8 * tiles), in = id % (8 * tiles);
+    int64_t unit = group * 8 + in % 8;
+    Work w;
+    w.ct = in / 8;
+    w.any = unit < a.S * a.kv_heads * splits;
+    w.split = unit % splits;
+    unit /= splits;
+    w.h = static_cast<int>(unit % a.kv_heads);
+    w.s = unit / a.kv_heads;
+    return w;
+}
+
+// One half tile's keys: where they lie, and how many rows there are to read.
+template <int D>
+struct Keys {
+    const int32_t *table;
+    int page_log2;
+    int64_t n_pages, head_bytes, page_bytes, last_key;
+
+    __device__ __forceinline__ Keys(const AttendArgs &a, int64_t s, int h, int64_t end)
+        : table(a.cache.pages + s * a.cache.table_width), page_log2(a.cache.page_log2), n_pages(a.cache.n_pages),
+          head_bytes(static_cast<int64_t>(h) * 2 * D << a.cache.page_log2),
+          page_bytes(static_cast<int64_t>(a.kv_heads) * 2 * D << a.cache.page_log2), last_key(end - 1) {}
+    // The page of a key (keys past the last one are read as the last one).
+    __device__ __forceinline__ int32_t entry(int64_t key) const { return table[(key < last_key ? key : last_key) >> page_log2]; }
+    __device__ __forceinline__ bool real(int32_t page) const { return page >= 0 && page < n_pages; }
+    // Byte offset of 16 keys from kb on in either cache; `rows`: the last of them that there is.
+    __device__ __forceinline__ int64_t at(int64_t kb, int32_t page, int &rows) const {
+        if (!real(page)) page = 0;
+        if (kb > last_key) kb = last_key & ~int64_t{15};
+        rows = last_key - kb < 15 ? static_cast<int>(last_key - kb) : 15;
+        return page * page_bytes + head_bytes + (kb & ((int64_t{1} << page_log2) - 1)) * (2 * D);
+    }
+};
+
+// Few columns (NT x 16): the W waves share them and wave w takes the 32-key
+// tiles w, w + W, ... of the workgroup's range with a reference and sums of its
+// own, joined at the end.  Each wave fills its own two stages by loads straight
+// to LDS, one tile ahead, and waits only for its own loads: no barrier in the
+// loop.
+template <knn_dtype DT, int D, int NT>
+__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t splits, int64_t chunk,
+                                                           float *part, float *part_ml) {
+    using Sh = Shape<D>;
+    constexpr int W = Sh::W, DB = D / 16, COLS = 16 * NT;
+    extern __shared__ __align__(16) u32x4_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quad = lane >> 4;
+    const Work wk = work_of(a, tiles, splits);
+    if (!wk.any) return;
+    const int h = wk.h, g = a.q_heads / a.kv_heads;
+    const Tile t = tile_of(a, wk.s);
+    const int64_t c0 = wk.ct * COLS, cols = static_cast<int64_t>(t.n) * g;
+    if (c0 >= cols) return;
+    // the keys of this range that any of the columns sees
+    int64_t end = t.total;
+    if (a.tree_mask == nullptr) {
+        const int64_t last = (c0 + COLS - 1 < cols ? c0 + COLS - 1 : cols - 1) / g;
+        if (t.length + last + 1 < end) end = t.length + last + 1;
+    }
+    const int64_t k0 = wk.split * chunk;
+    if (splits > 1 && k0 >= t.total) return;
+    if (k0 + chunk < end) end = k0 + chunk;
+
+    Columns<DT, D, NT> c;
+    c.load(a, t, h, g, c0, cols, col, quad);
+    const uint32_t mine =
+        __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * static_cast<uint32_t>(Sh::STAGES * 2 * Sh::HALF);
+    const int64_t n_tiles = end > k0 ? (end - k0 + 31) / 32 : 0;
+    const int64_t own = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // this wave's tiles
+    const Keys<D> keys(a, wk.s, h, end);
+    // Lane l keeps the page of half l & 1 of this wave's tile l / 2 from tile `held` on.
+    int32_t page_reg = 0;
+    auto hold_pages = [&](int64_t held) {
+        page_reg = keys.entry(k0 + 32 * (wave + W * (held + (lane >> 1))) + 16 * (lane & 1));
+    };
+    auto page_of = [&](int64_t tile, int half) {
+        return __builtin_amdgcn_readlane(page_reg, 2 * static_cast<int>(tile & 31) + half);
+    };
+    auto fill = [&](int64_t i) {  // tile i of this wave into stage i & 1
+        const uint32_t to = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            int rows;
+            const int64_t at = keys.at(k0 + 32 * (wave + W * i) + 16 * half, page_of(i, half), rows);
+            const char *kp = static_cast<const char *>(a.k_cache) + at;
+            const char *vp = static_cast<const char *>(a.v_cache) + at;
+#pragma unroll
+            for (int j = 0; j < Sh::LOADS / 2; ++j) {
+                const int r = j * Sh::PER + lane / Sh::LANES;
+                const int from = r < rows ? r : rows;
+                const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread(r));
+                load_to_lds_16(kp, off, to + half * (Sh::HALF / 2) + j * 1024);
+                load_to_lds_16(vp, off, to + Sh::HALF + half * (Sh::HALF / 2) + j * 1024);
+            }
+        }
+    };
+
+    if (own > 0) {
+        hold_pages(0);
+        fill(0);
+    }
+    for (int64_t i = 0; i < own; ++i) {
+        const bool real_a = keys.real(page_of(i, 0)), real_b = keys.real(page_of(i, 1));
+        if (i + 1 < own) {
+            if (((i + 1) & 31) == 0) hold_pages(i + 1);
+            fill(i + 1);
+            __builtin_amdgcn_s_waitcnt(vmcnt_encoding<2 * Sh::LOADS>());
+        } else {
+            __builtin_amdgcn_s_waitcnt(kVmcntZero);
+        }
+        asm volatile("" ::: "memory");
+        const uint32_t kt = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF), vt = kt + Sh::HALF;
+        const int64_t key = k0 + 32 * (wave + W * i);
+        const bool all = key + 32 <= (t.length < end ? t.length : end) && real_a && real_b;
+        c.tile(a, t, kt, vt, key, all, end, real_a, real_b, col, quad);
         // the stage is read: the next round's loads may overwrite it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -326,44 +397,118 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (quad == 0) {
-            stat[wave * COLS + 16 * n + col] = m[n];
-            stat[W * COLS + wave * COLS + 16 * n + col] = sum[n][0];
+            stat[wave * COLS + 16 * n + col] = c.m[n];
+            stat[W * COLS + wave * COLS + 16 * n + col] = c.sum[n][0];
         }
 #pragma unroll
         for (int d = 0; d < DB; ++d)
-            *reinterpret_cast<f32x4_t *>(acc + (wave * COLS + 16 * n + col) * PITCH + 16 * d + 4 * quad) = o[n][d];
+            *reinterpret_cast<f32x4_t *>(acc + (wave * COLS + 16 * n + col) * PITCH + 16 * d + 4 * quad) = c.o[n][d];
     }
     __syncthreads();
-    const int64_t heads = a.q_heads;
     for (int i = threadIdx.x; i < COLS * (D / 4); i += W * 64) {
-        const int c = i / (D / 4), d = i % (D / 4) * 4;
-        if (c0 + c >= cols) continue;
+        const int cc = i / (D / 4), d = i % (D / 4) * 4;
+        if (c0 + cc >= cols) continue;
         float top = kFloor;
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w * COLS + c]);
+        for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w * COLS + cc]);
         float l = 0.0f;
         f32x4_t r{0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float by = exp2f(stat[w * COLS + c] - top);
-            const float lw = stat[W * COLS + w * COLS + c];
-            l += by * lw;
-            r += by * *reinterpret_cast<const f32x4_t *>(acc + (w * COLS + c) * PITCH + d);
+            const float by = exp2f(stat[w * COLS + cc] - top);
+            l += by * stat[W * COLS + w * COLS + cc];
+            r += by * *reinterpret_cast<const f32x4_t *>(acc + (w * COLS + cc) * PITCH + d);
         }
-        const int64_t at = (t.r0 + (c0 + c) / g) * heads + h * g + (c0 + c) % g;  // (row, query head)
-        if (splits > 1) {
-            const int64_t to = split * a.rows * heads + at;
-            if (d == 0) {
-                part_ml[2 * to] = top;
-                part_ml[2 * to + 1] = l;
-            }
-            *reinterpret_cast<f32x4_t *>(part + to * D + d) = r;
-        } else {
-            const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // no key: 0; NaN stays
-            *reinterpret_cast<u32x2_t *>(static_cast<uint16_t *>(a.out) + at * D + d) =
-                u32x2_t{pack2<DT>(r[0] * by, r[1] * by), pack2<DT>(r[2] * by, r[3] * by)};
-            if (d == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+        const int64_t at = (t.r0 + (c0 + cc) / g) * a.q_heads + h * g + (c0 + cc) % g;  // (row, query head)
+        store<DT, D>(a, splits, wk.split, at, d, r, top, l, part, part_ml);
+    }
+}
+
+// Many columns: four waves of NT x 16 each on the same keys, which all of them
+// read out of a ring of stages.  Each wave fetches a quarter of a tile, RING - 1
+// tiles ahead.  One barrier a tile: behind it every wave's loads of the tile
+// have landed and every wave has read the tile before, whose stage is filled
+// next.
+template <knn_dtype DT, int D, int NT>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t splits, int64_t chunk,
+                                                     float *part, float *part_ml) {
+    using Sh = Shape<D>;
+    constexpr int DB = D / 16, COLS = 64 * NT, RING = Sh::RING, MINE = Sh::LOADS / 2;  // loads of a wave and tile
+    extern __shared__ __align__(16) u32x4_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quad = lane >> 4;
+    const Work wk = work_of(a, tiles, splits);
+    if (!wk.any) return;
+    const int h = wk.h, g = a.q_heads / a.kv_heads;
+    const Tile t = tile_of(a, wk.s);
+    const int64_t c0 = wk.ct * COLS, cols = static_cast<int64_t>(t.n) * g;
+    if (c0 >= cols) return;
+    int64_t end = t.total;
+    if (a.tree_mask == nullptr) {
+        const int64_t last = (c0 + COLS - 1 < cols ? c0 + COLS - 1 : cols - 1) / g;
+        if (t.length + last + 1 < end) end = t.length + last + 1;
+    }
+    const int64_t k0 = wk.split * chunk;
+    if (splits > 1 && k0 >= t.total) return;
+    if (k0 + chunk < end) end = k0 + chunk;
+
+    Columns<DT, D, NT> c;
+    c.load(a, t, h, g, c0 + 16 * NT * wave, cols, col, quad);
+    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_offset(lds));
+    const int n = end > k0 ? static_cast<int>((end - k0 + 31) / 32) : 0;
+    const Keys<D> keys(a, wk.s, h, end);
+    // Lane l keeps the page of half l & 1 of tile l / 2 from tile `held` on, and of the 32 tiles before.
+    int32_t page_reg = 0, page_old = 0;
+    auto hold_pages = [&](int held) {
+        page_old = page_reg;
+        page_reg = keys.entry(k0 + 32 * static_cast<int64_t>(held + (lane >> 1)) + 16 * (lane & 1));
+    };
+    auto fill = [&](int i) {  // this wave's quarter of tile i into its stage
+        if ((i & 31) == 0) hold_pages(i);
+        const uint32_t to = base + static_cast<uint32_t>(i % RING) * (2 * Sh::HALF);
+#pragma unroll
+        for (int j = 0; j < MINE / 2; ++j) {  // load `at` of a half's LOADS: its 16 keys are half at / (LOADS / 2)
+            const int load = wave * (MINE / 2) + j, half = load / (Sh::LOADS / 2), in = load % (Sh::LOADS / 2);
+            int rows;
+            const int64_t at = keys.at(k0 + 32 * static_cast<int64_t>(i) + 16 * half,
+                                       __builtin_amdgcn_readlane(page_reg, 2 * (i & 31) + half), rows);
+            const int r = in * Sh::PER + lane / Sh::LANES;
+            const int from = r < rows ? r : rows;
+            const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread(r));
+            load_to_lds_16(static_cast<const char *>(a.k_cache) + at, off, to + load * 1024);
+            load_to_lds_16(static_cast<const char *>(a.v_cache) + at, off, to + Sh::HALF + load * 1024);
         }
+    };
+
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i)
+        if (i < n) fill(i);
+    for (int i = 0; i < n; ++i) {
+        // this wave's loads of tile i have landed when only the later tiles' are on their way
+        if (i + RING - 2 < n) __builtin_amdgcn_s_waitcnt(vmcnt_encoding<(RING - 2) * MINE>());
+        else __builtin_amdgcn_s_waitcnt(kVmcntZero);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (i + RING - 1 < n) fill(i + RING - 1);
+        // the pages of tile i: held since it was filled
+        const bool old = (i & 31) + RING - 1 >= 32 && ((i + RING - 1 < n ? i + RING - 1 : n - 1) >> 5) != (i >> 5);
+        const int32_t pages = old ? page_old : page_reg;
+        const bool real_a = keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31)));
+        const bool real_b = keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31) + 1));
+        const uint32_t kt = base + static_cast<uint32_t>(i % RING) * (2 * Sh::HALF);
+        const int64_t key = k0 + 32 * static_cast<int64_t>(i);
+        const bool all = key + 32 <= (t.length < end ? t.length : end) && real_a && real_b;
+        c.tile(a, t, kt, kt + Sh::HALF, key, all, end, real_a, real_b, col, quad);
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int64_t cc = c0 + 16 * NT * wave + 16 * i + col;
+        if (cc >= cols) continue;
+        const int64_t at = (t.r0 + cc / g) * a.q_heads + h * g + cc % g;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+            store<DT, D>(a, splits, wk.split, at, 16 * d + 4 * quad, c.o[i][d], c.m[i], c.sum[i][0], part, part_ml);
     }
 }
 
@@ -403,14 +548,18 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t split
 
 template <knn_dtype DT, int D>
 hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *part_ml, hipStream_t stream) {
-    const int64_t blocks = a.S * a.kv_heads * p.tiles * p.splits;
+    const int64_t units = a.S * a.kv_heads * p.splits, blocks = (units + 7) / 8 * 8 * p.tiles;
     const int64_t joins = (a.rows * a.q_heads + 3) / 4;
     if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<unsigned>(blocks)), threads(Shape<D>::W * 64);
+    const dim3 grid(static_cast<unsigned>(blocks)), few(Shape<D>::W * 64);
     if (p.cols == 16)
-        k_attend<DT, D, 1><<<grid, threads, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+        k_attend<DT, D, 1><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+    else if (p.cols == 32)
+        k_attend<DT, D, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+    else if (p.cols == 64)
+        k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
     else
-        k_attend<DT, D, 2><<<grid, threads, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+        k_attend_many<DT, D, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
     if (p.splits > 1)
         k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.splits, p.chunk, part, part_ml);
     return hipGetLastError();
@@ -431,11 +580,13 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
                        int64_t max_keys) {
     AttendPlan p{};
     const int64_t cols = max_rows * (q_heads / kv_heads);
-    p.cols = cols <= 16 ? 16 : 32;
+    p.cols = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
     p.tiles = (cols + p.cols - 1) / p.cols;
-    // Two workgroups a CU, each on 256 keys or more.
-    const int64_t base = S * kv_heads * p.tiles, most = (max_keys + 255) / 256;
-    p.splits = (512 + base - 1) / base;
+    // Few columns: two workgroups a CU, each on 256 keys or more.  Many: the CUs hold two at a time, eight of them or
+    // more for every CU even out sequences of different lengths, each on 1024 keys or more.
+    const bool many = p.cols > 32;
+    const int64_t base = S * kv_heads * p.tiles, least = many ? 1024 : 256, most = (max_keys + least - 1) / least;
+    p.splits = ((many ? 2048 : 512) + base - 1) / base;
     if (p.splits > most) p.splits = most;
     if (p.splits > 256) p.splits = 256;
     p.chunk = ((max_keys + p.splits - 1) / p.splits + 127) / 128 * 128;
