@@ -68,10 +68,16 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {  // to nearest, ti
     }
 }
 
-// 16-byte chunk c of row r of a tile in LDS lies at chunk c ^ spread(r): the 8
-// rows that a product's operand read takes at once, and the 4 rows x 2 chunks
-// of a transposing read, then fall on different banks.
-__device__ __forceinline__ int spread(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+// 16-byte chunk c of row r of a tile in LDS lies at chunk c ^ spread(r).  LDS
+// has 64 banks, 16 chunks wide: the 16 rows x 1 chunk that 16 lanes of a
+// product's operand read take at once, and the 8 rows x 2 neighbouring chunks
+// of 32 lanes of a transposing read, then fall on 16 different ones.  (Rows of
+// 8 chunks lie two in 16.)
+template <int D>
+__device__ __forceinline__ int spread(int r) {
+    if constexpr (D == 64) return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
+    return ((r & 7) << 1) | ((r >> 3) & 1);
+}
 
 // Four 16-bit elements of one column: lane l of each 16 gets column l of the 4
 // rows whose 8-byte pieces the 16 lanes point at.
@@ -143,38 +149,43 @@ struct Columns {
         }
     }
 
-    // 32 keys from `key` on, in LDS at kt and vt.  `all`: every column sees every one of them; else a key is seen if it
-    // is before `end`, its half's page is one, and it is cached or named by the row's mask.
-    __device__ __forceinline__ void tile(const AttendArgs &a, const Tile &t, uint32_t kt, uint32_t vt, int64_t key, bool all,
-                                         int64_t end, bool real_a, bool real_b, int col, int quad) {
-        f32x4_t x[2][NT];
+    // U x 32 keys from `key` on, 32 each in LDS at kt[u] and their values behind them.  `all`: every column sees every
+    // one of them; else a key is seen if it is before `end`, its half's page is one (bit 2 u + half of `real`), and it
+    // is cached or named by the row's mask.
+    template <int U>
+    __device__ __forceinline__ void tile(const AttendArgs &a, const Tile &t, const uint32_t (&kt)[U], int64_t key, bool all,
+                                         int64_t end, uint32_t real, int col, int quad) {
+        f32x4_t x[2 * U][NT];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int u = 0; u < 2 * U; ++u) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[half][n] = f32x4_t{0, 0, 0, 0};
+            for (int n = 0; n < NT; ++n) x[u][n] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < KK; ++k) {
                 const u32x4_t kr = *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t *>(
-                    static_cast<uintptr_t>(kt + (16 * half + col) * ROW + 16 * ((4 * k + quad) ^ spread(col))));
+                    static_cast<uintptr_t>(kt[u / 2] + (16 * (u & 1) + col) * ROW + 16 * ((4 * k + quad) ^ spread<D>(col))));
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[half][n] = mfma16<DT>(kr, q[n][k], x[half][n]);
+                for (int n = 0; n < NT; ++n) x[u][n] = mfma16<DT>(kr, q[n][k], x[u][n]);
             }
         }
         if (!all) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t bits = (half == 0 ? real_a : real_b) ? seen(a, t, row_of[n], key + 16 * half + 4 * quad, end) : 0u;
+                for (int u = 0; u < 2 * U; ++u) {
+                    const uint32_t bits = (real >> u & 1u) != 0u ? seen(a, t, row_of[n], key + 16 * u + 4 * quad, end) : 0u;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[half][n][j] = (bits >> j & 1u) != 0u ? x[half][n][j] : -INFINITY;
+                    for (int j = 0; j < 4; ++j) x[u][n][j] = (bits >> j & 1u) != 0u ? x[u][n][j] : -INFINITY;
                 }
         }
-        u32x4_t p[NT];
+        u32x4_t p[U][NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float top = fmaxf(fmaxf(fmaxf(x[0][n][0], x[0][n][1]), fmaxf(x[0][n][2], x[0][n][3])),
-                              fmaxf(fmaxf(x[1][n][0], x[1][n][1]), fmaxf(x[1][n][2], x[1][n][3]))) * c2;
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 2 * U; ++u)
+                top = fmaxf(fmaxf(top, fmaxf(x[u][n][0], x[u][n][1])), fmaxf(x[u][n][2], x[u][n][3]));
+            top *= c2;
             if (__any(top > m[n] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -188,36 +199,45 @@ struct Columns {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[n][d][j] *= by;
             }
-            float e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(x[j >> 2][n][j & 3], c2, -m[n]));
-            p[n] = u32x4_t{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7])};
+            for (int u = 0; u < U; ++u) {
+                float e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(x[2 * u + (j >> 2)][n][j & 3], c2, -m[n]));
+                p[u][n] = u32x4_t{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7])};
+            }
         }
         constexpr uint32_t kOne = DT == KNN_BF16 ? 0x3f803f80u : 0x3c003c00u;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) sum[n] = mfma16<DT>(u32x4_t{kOne, kOne, kOne, kOne}, p[n], sum[n]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sum[n] = mfma16<DT>(u32x4_t{kOne, kOne, kOne, kOne}, p[u][n], sum[n]);
         const int vrow = 4 * quad + (col >> 2);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            const uint32_t at = vt + vrow * ROW + 16 * ((2 * d + ((col >> 1) & 1)) ^ spread(vrow)) + 8 * (col & 1);
-            const u32x2_t va = read_transposed(at), vb = read_transposed(at + 16 * ROW);
-            u32x4_t v = {va.x, va.y, vb.x, vb.y};
-            if (!all) {
-                // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such
-                // elements are left out of the product, and make NaN what sees them.
-                const u32x4_t bad = {not_finite<DT>(v.x), not_finite<DT>(v.y), not_finite<DT>(v.z), not_finite<DT>(v.w)};
-                if (__any((bad.x | bad.y | bad.z | bad.w) != 0u)) {
-                    v &= ~bad;
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const f32x4_t seen = mfma16<DT>(bad & kOne, p[n], f32x4_t{0, 0, 0, 0});
+            for (int d = 0; d < DB; ++d) {
+                const uint32_t at = kt[u] + 32 * ROW + vrow * ROW +
+                                    16 * ((2 * d + ((col >> 1) & 1)) ^ spread<D>(vrow)) + 8 * (col & 1);
+                const u32x2_t va = read_transposed(at), vb = read_transposed(at + 16 * ROW);
+                u32x4_t v = {va.x, va.y, vb.x, vb.y};
+                if (!all) {
+                    // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such
+                    // elements are left out of the product, and make NaN what sees them.
+                    const u32x4_t bad = {not_finite<DT>(v.x), not_finite<DT>(v.y), not_finite<DT>(v.z), not_finite<DT>(v.w)};
+                    if (__any((bad.x | bad.y | bad.z | bad.w) != 0u)) {
+                        v &= ~bad;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) o[n][d][j] = seen[j] > 0.0f ? __builtin_nanf("") : o[n][d][j];
+                        for (int n = 0; n < NT; ++n) {
+                            const f32x4_t sees = mfma16<DT>(bad & kOne, p[u][n], f32x4_t{0, 0, 0, 0});
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[n][d][j] = sees[j] > 0.0f ? __builtin_nanf("") : o[n][d][j];
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[n], o[n][d]);
+                for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[u][n], o[n][d]);
+            }
         }
     }
 };
@@ -254,7 +274,7 @@ struct Shape {
     static constexpr int STAGES = 2;
     static constexpr size_t LDS = static_cast<size_t>(W) * STAGES * 2 * HALF;
     // Many columns: four waves on the same keys.
-    static constexpr int RING = D == 256 ? 3 : 4;
+    static constexpr int RING = D == 64 ? 8 : D == 128 ? 5 : 4;
     static constexpr size_t RING_LDS = static_cast<size_t>(RING) * 2 * HALF;
 };
 
@@ -359,7 +379,7 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
             for (int j = 0; j < Sh::LOADS / 2; ++j) {
                 const int r = j * Sh::PER + lane / Sh::LANES;
                 const int from = r < rows ? r : rows;
-                const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread(r));
+                const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread<D>(r));
                 load_to_lds_16(kp, off, to + half * (Sh::HALF / 2) + j * 1024);
                 load_to_lds_16(vp, off, to + Sh::HALF + half * (Sh::HALF / 2) + j * 1024);
             }
@@ -380,10 +400,10 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
             __builtin_amdgcn_s_waitcnt(kVmcntZero);
         }
         asm volatile("" ::: "memory");
-        const uint32_t kt = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF), vt = kt + Sh::HALF;
+        const uint32_t kt[1] = {mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF)};
         const int64_t key = k0 + 32 * (wave + W * i);
         const bool all = key + 32 <= (t.length < end ? t.length : end) && real_a && real_b;
-        c.tile(a, t, kt, vt, key, all, end, real_a, real_b, col, quad);
+        c.template tile<1>(a, t, kt, key, all, end, (real_a ? 1u : 0u) | (real_b ? 2u : 0u), col, quad);
         // the stage is read: the next round's loads may overwrite it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -424,10 +444,10 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
     }
 }
 
-// Many columns: four waves of NT x 16 each on the same keys, which all of them
-// read out of a ring of stages.  Each wave fetches a quarter of a tile, RING - 1
-// tiles ahead.  One barrier a tile: behind it every wave's loads of the tile
-// have landed and every wave has read the tile before, whose stage is filled
+// Many columns: four waves of NT x 16 each on the same keys, 64 at a time, which
+// all of them read out of a ring of 32-key stages.  Each wave fetches a quarter
+// of a tile.  One barrier every two tiles: behind it every wave's loads of them
+// have landed and every wave has read the two before, whose stages are filled
 // next.
 template <knn_dtype DT, int D, int NT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t splits, int64_t chunk,
@@ -474,32 +494,38 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
                                        __builtin_amdgcn_readlane(page_reg, 2 * (i & 31) + half), rows);
             const int r = in * Sh::PER + lane / Sh::LANES;
             const int from = r < rows ? r : rows;
-            const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread(r));
+            const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread<D>(r));
             load_to_lds_16(static_cast<const char *>(a.k_cache) + at, off, to + load * 1024);
             load_to_lds_16(static_cast<const char *>(a.v_cache) + at, off, to + Sh::HALF + load * 1024);
         }
     };
 
 #pragma unroll
-    for (int i = 0; i < RING - 1; ++i)
+    for (int i = 0; i < RING - 2; ++i)
         if (i < n) fill(i);
-    for (int i = 0; i < n; ++i) {
-        // this wave's loads of tile i have landed when only the later tiles' are on their way
-        if (i + RING - 2 < n) __builtin_amdgcn_s_waitcnt(vmcnt_encoding<(RING - 2) * MINE>());
+    uint32_t stage = base;
+    for (int i = 0; i < n; i += 2) {
+        // This wave's loads of tiles i and i + 1 have landed when only the later tiles' are on their way.
+        if (i + RING - 3 < n) __builtin_amdgcn_s_waitcnt(vmcnt_encoding<(RING - 4) * MINE>());
         else __builtin_amdgcn_s_waitcnt(kVmcntZero);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        if (i + RING - 2 < n) fill(i + RING - 2);
         if (i + RING - 1 < n) fill(i + RING - 1);
-        // the pages of tile i: held since it was filled
-        const bool old = (i & 31) + RING - 1 >= 32 && ((i + RING - 1 < n ? i + RING - 1 : n - 1) >> 5) != (i >> 5);
-        const int32_t pages = old ? page_old : page_reg;
-        const bool real_a = keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31)));
-        const bool real_b = keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31) + 1));
-        const uint32_t kt = base + static_cast<uint32_t>(i % RING) * (2 * Sh::HALF);
+        // the pages of tiles i and i + 1 (i is even): held since they were filled
+        const int filled = i + RING - 1 < n ? i + RING - 1 : n - 1;
+        const int32_t pages = (filled >> 5) != (i >> 5) ? page_old : page_reg;
+        uint32_t real = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) real |= keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31) + u)) ? 1u << u : 0u;
+        uint32_t kt[2] = {stage, stage + 2 * Sh::HALF};
+        if (kt[1] == base + RING * 2 * Sh::HALF) kt[1] = base;
+        stage = kt[1] + 2 * Sh::HALF;
+        if (stage == base + RING * 2 * Sh::HALF) stage = base;
         const int64_t key = k0 + 32 * static_cast<int64_t>(i);
-        const bool all = key + 32 <= (t.length < end ? t.length : end) && real_a && real_b;
-        c.tile(a, t, kt, kt + Sh::HALF, key, all, end, real_a, real_b, col, quad);
+        const bool all = key + 64 <= (t.length < end ? t.length : end) && real == 15u;
+        c.template tile<2>(a, t, kt, key, all, end, real, col, quad);
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -554,12 +580,12 @@ hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *
     const dim3 grid(static_cast<unsigned>(blocks)), few(Shape<D>::W * 64);
     if (p.cols == 16)
         k_attend<DT, D, 1><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
-    else if (p.cols == 32)
-        k_attend<DT, D, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+    else if (D < 256 && p.cols == 32)
+        k_attend<DT, D < 256 ? D : 64, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
     else if (p.cols == 64)
         k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
     else
-        k_attend_many<DT, D, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
+        k_attend_many<DT, D < 256 ? D : 64, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
     if (p.splits > 1)
         k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.splits, p.chunk, part, part_ml);
     return hipGetLastError();
@@ -580,7 +606,8 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
                        int64_t max_keys) {
     AttendPlan p{};
     const int64_t cols = max_rows * (q_heads / kv_heads);
-    p.cols = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+    // (At head_dim 256 the wider kind of either kernel does not fit the registers.)
+    p.cols = cols <= 16 ? 16 : cols <= 32 && head_dim < 256 ? 32 : cols <= 64 || head_dim == 256 ? 64 : 128;
     p.tiles = (cols + p.cols - 1) / p.cols;
     // Few columns: two workgroups a CU, each on 256 keys or more.  Many: the CUs hold two at a time, eight of them or
     // more for every CU even out sequences of different lengths, each on 1024 keys or more.
