@@ -181,10 +181,11 @@ struct Columns {
         u32x4_t p[U][NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float top = -INFINITY;
+            float top = -INFINITY;  // (the median with +inf is the larger one, in one instruction; fmaxf takes two)
 #pragma unroll
             for (int u = 0; u < 2 * U; ++u)
-                top = fmaxf(fmaxf(top, fmaxf(x[u][n][0], x[u][n][1])), fmaxf(x[u][n][2], x[u][n][3]));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top = __builtin_amdgcn_fmed3f(top, x[u][n][j], INFINITY);
             top *= c2;
             if (__any(top > m[n] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
@@ -213,32 +214,43 @@ struct Columns {
 #pragma unroll
             for (int n = 0; n < NT; ++n) sum[n] = mfma16<DT>(u32x4_t{kOne, kOne, kOne, kOne}, p[u][n], sum[n]);
         const int vrow = 4 * quad + (col >> 2);
+        auto values = [&](int u, int d) {
+            const uint32_t at =
+                kt[u] + 32 * ROW + vrow * ROW + 16 * ((2 * d + ((col >> 1) & 1)) ^ spread<D>(vrow)) + 8 * (col & 1);
+            const u32x2_t va = read_transposed(at), vb = read_transposed(at + 16 * ROW);
+            return u32x4_t{va.x, va.y, vb.x, vb.y};
+        };
+        if (all) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const u32x4_t v = values(u, d);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[u][n], o[n][d]);
+                }
+            return;
+        }
+        // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such elements are
+        // left out of the product, and make NaN what sees them.
+#pragma unroll
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const uint32_t at = kt[u] + 32 * ROW + vrow * ROW +
-                                    16 * ((2 * d + ((col >> 1) & 1)) ^ spread<D>(vrow)) + 8 * (col & 1);
-                const u32x2_t va = read_transposed(at), vb = read_transposed(at + 16 * ROW);
-                u32x4_t v = {va.x, va.y, vb.x, vb.y};
-                if (!all) {
-                    // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such
-                    // elements are left out of the product, and make NaN what sees them.
-                    const u32x4_t bad = {not_finite<DT>(v.x), not_finite<DT>(v.y), not_finite<DT>(v.z), not_finite<DT>(v.w)};
-                    if (__any((bad.x | bad.y | bad.z | bad.w) != 0u)) {
-                        v &= ~bad;
+                u32x4_t v = values(u, d);
+                const u32x4_t bad = {not_finite<DT>(v.x), not_finite<DT>(v.y), not_finite<DT>(v.z), not_finite<DT>(v.w)};
+                if (__any((bad.x | bad.y | bad.z | bad.w) != 0u)) {
+                    v &= ~bad;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const f32x4_t sees = mfma16<DT>(bad & kOne, p[u][n], f32x4_t{0, 0, 0, 0});
+                    for (int n = 0; n < NT; ++n) {
+                        const f32x4_t sees = mfma16<DT>(bad & kOne, p[u][n], f32x4_t{0, 0, 0, 0});
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) o[n][d][j] = sees[j] > 0.0f ? __builtin_nanf("") : o[n][d][j];
-                        }
+                        for (int j = 0; j < 4; ++j) o[n][d][j] = sees[j] > 0.0f ? __builtin_nanf("") : o[n][d][j];
                     }
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[u][n], o[n][d]);
             }
-        }
     }
 };
 
@@ -300,26 +312,29 @@ __device__ __forceinline__ Work work_of(const AttendArgs &a, int64_t tiles, int6
     return w;
 }
 
-// One half tile's keys: where they lie, and how many rows there are to read.
+// The keys of a workgroup's range, counted from its first one, k0 (a multiple
+// of 128): where they lie, and how many rows there are to read.
 template <int D>
 struct Keys {
-    const int32_t *table;
-    int page_log2;
-    int64_t n_pages, head_bytes, page_bytes, last_key;
+    const int32_t *table;  // of k0's page
+    int page_log2, slot0;  // slot0: k0's in its page
+    int64_t n_pages, head_bytes, page_bytes;
+    int last;  // the last key
 
-    __device__ __forceinline__ Keys(const AttendArgs &a, int64_t s, int h, int64_t end)
-        : table(a.cache.pages + s * a.cache.table_width), page_log2(a.cache.page_log2), n_pages(a.cache.n_pages),
+    __device__ __forceinline__ Keys(const AttendArgs &a, int64_t s, int h, int64_t k0, int64_t end)
+        : table(a.cache.pages + s * a.cache.table_width + (k0 >> a.cache.page_log2)), page_log2(a.cache.page_log2),
+          slot0(static_cast<int>(k0 & ((int64_t{1} << a.cache.page_log2) - 1))), n_pages(a.cache.n_pages),
           head_bytes(static_cast<int64_t>(h) * 2 * D << a.cache.page_log2),
-          page_bytes(static_cast<int64_t>(a.kv_heads) * 2 * D << a.cache.page_log2), last_key(end - 1) {}
+          page_bytes(static_cast<int64_t>(a.kv_heads) * 2 * D << a.cache.page_log2), last(static_cast<int>(end - 1 - k0)) {}
     // The page of a key (keys past the last one are read as the last one).
-    __device__ __forceinline__ int32_t entry(int64_t key) const { return table[(key < last_key ? key : last_key) >> page_log2]; }
+    __device__ __forceinline__ int32_t entry(int key) const { return table[(slot0 + min(key, last)) >> page_log2]; }
     __device__ __forceinline__ bool real(int32_t page) const { return page >= 0 && page < n_pages; }
-    // Byte offset of 16 keys from kb on in either cache; `rows`: the last of them that there is.
-    __device__ __forceinline__ int64_t at(int64_t kb, int32_t page, int &rows) const {
+    // Byte offset of 16 keys from `key` on in either cache; `rows`: the last of them that there is.
+    __device__ __forceinline__ int64_t at(int key, int32_t page, int &rows) const {
         if (!real(page)) page = 0;
-        if (kb > last_key) kb = last_key & ~int64_t{15};
-        rows = last_key - kb < 15 ? static_cast<int>(last_key - kb) : 15;
-        return page * page_bytes + head_bytes + (kb & ((int64_t{1} << page_log2) - 1)) * (2 * D);
+        key = key > last ? last & ~15 : key;
+        rows = min(last - key, 15);
+        return page * page_bytes + head_bytes + ((slot0 + key) & ((1 << page_log2) - 1)) * (2 * D);
     }
 };
 
@@ -356,23 +371,22 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
     c.load(a, t, h, g, c0, cols, col, quad);
     const uint32_t mine =
         __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * static_cast<uint32_t>(Sh::STAGES * 2 * Sh::HALF);
-    const int64_t n_tiles = end > k0 ? (end - k0 + 31) / 32 : 0;
-    const int64_t own = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // this wave's tiles
-    const Keys<D> keys(a, wk.s, h, end);
+    const int n_tiles = end > k0 ? static_cast<int>((end - k0 + 31) / 32) : 0;
+    const int own = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // this wave's tiles
+    const int64_t whole = (t.length < end ? t.length : end) - k0;       // keys that every column sees
+    const Keys<D> keys(a, wk.s, h, k0, end);
     // Lane l keeps the page of half l & 1 of this wave's tile l / 2 from tile `held` on.
     int32_t page_reg = 0;
-    auto hold_pages = [&](int64_t held) {
-        page_reg = keys.entry(k0 + 32 * (wave + W * (held + (lane >> 1))) + 16 * (lane & 1));
+    auto hold_pages = [&](int held) {
+        page_reg = keys.entry(32 * (wave + W * (held + (lane >> 1))) + 16 * (lane & 1));
     };
-    auto page_of = [&](int64_t tile, int half) {
-        return __builtin_amdgcn_readlane(page_reg, 2 * static_cast<int>(tile & 31) + half);
-    };
-    auto fill = [&](int64_t i) {  // tile i of this wave into stage i & 1
+    auto page_of = [&](int tile, int half) { return __builtin_amdgcn_readlane(page_reg, 2 * (tile & 31) + half); };
+    auto fill = [&](int i) {  // tile i of this wave into stage i & 1
         const uint32_t to = mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             int rows;
-            const int64_t at = keys.at(k0 + 32 * (wave + W * i) + 16 * half, page_of(i, half), rows);
+            const int64_t at = keys.at(32 * (wave + W * i) + 16 * half, page_of(i, half), rows);
             const char *kp = static_cast<const char *>(a.k_cache) + at;
             const char *vp = static_cast<const char *>(a.v_cache) + at;
 #pragma unroll
@@ -390,7 +404,7 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
         hold_pages(0);
         fill(0);
     }
-    for (int64_t i = 0; i < own; ++i) {
+    for (int i = 0; i < own; ++i) {
         const bool real_a = keys.real(page_of(i, 0)), real_b = keys.real(page_of(i, 1));
         if (i + 1 < own) {
             if (((i + 1) & 31) == 0) hold_pages(i + 1);
@@ -401,9 +415,9 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
         }
         asm volatile("" ::: "memory");
         const uint32_t kt[1] = {mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF)};
-        const int64_t key = k0 + 32 * (wave + W * i);
-        const bool all = key + 32 <= (t.length < end ? t.length : end) && real_a && real_b;
-        c.template tile<1>(a, t, kt, key, all, end, (real_a ? 1u : 0u) | (real_b ? 2u : 0u), col, quad);
+        const int key = 32 * (wave + W * i);
+        const bool all = key + 32 <= whole && real_a && real_b;
+        c.template tile<1>(a, t, kt, k0 + key, all, end, (real_a ? 1u : 0u) | (real_b ? 2u : 0u), col, quad);
         // the stage is read: the next round's loads may overwrite it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -476,27 +490,27 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
     c.load(a, t, h, g, c0 + 16 * NT * wave, cols, col, quad);
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_offset(lds));
     const int n = end > k0 ? static_cast<int>((end - k0 + 31) / 32) : 0;
-    const Keys<D> keys(a, wk.s, h, end);
+    const int64_t whole = (t.length < end ? t.length : end) - k0;  // keys that every column sees
+    const Keys<D> keys(a, wk.s, h, k0, end);
     // Lane l keeps the page of half l & 1 of tile l / 2 from tile `held` on, and of the 32 tiles before.
     int32_t page_reg = 0, page_old = 0;
     auto hold_pages = [&](int held) {
         page_old = page_reg;
-        page_reg = keys.entry(k0 + 32 * static_cast<int64_t>(held + (lane >> 1)) + 16 * (lane & 1));
+        page_reg = keys.entry(32 * (held + (lane >> 1)) + 16 * (lane & 1));
     };
-    auto fill = [&](int i) {  // this wave's quarter of tile i into its stage
+    const int half = wave >> 1;  // of a tile's 32 keys: which 16 this wave fetches half of
+    auto fill = [&](int i) {     // this wave's quarter of tile i into its stage
         if ((i & 31) == 0) hold_pages(i);
         const uint32_t to = base + static_cast<uint32_t>(i % RING) * (2 * Sh::HALF);
+        int rows;
+        const int64_t at = keys.at(32 * i + 16 * half, __builtin_amdgcn_readlane(page_reg, 2 * (i & 31) + half), rows);
+        const char *kp = static_cast<const char *>(a.k_cache) + at, *vp = static_cast<const char *>(a.v_cache) + at;
 #pragma unroll
-        for (int j = 0; j < MINE / 2; ++j) {  // load `at` of a half's LOADS: its 16 keys are half at / (LOADS / 2)
-            const int load = wave * (MINE / 2) + j, half = load / (Sh::LOADS / 2), in = load % (Sh::LOADS / 2);
-            int rows;
-            const int64_t at = keys.at(k0 + 32 * static_cast<int64_t>(i) + 16 * half,
-                                       __builtin_amdgcn_readlane(page_reg, 2 * (i & 31) + half), rows);
-            const int r = in * Sh::PER + lane / Sh::LANES;
-            const int from = r < rows ? r : rows;
-            const uint32_t off = from * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread<D>(r));
-            load_to_lds_16(static_cast<const char *>(a.k_cache) + at, off, to + load * 1024);
-            load_to_lds_16(static_cast<const char *>(a.v_cache) + at, off, to + Sh::HALF + load * 1024);
+        for (int j = 0; j < MINE / 2; ++j) {
+            const int r = ((wave & 1) * (MINE / 2) + j) * Sh::PER + lane / Sh::LANES;  // row of the half
+            const uint32_t off = min(r, rows) * Sh::ROW + 16 * ((lane % Sh::LANES) ^ spread<D>(r));
+            load_to_lds_16(kp, off, to + (wave * (MINE / 2) + j) * 1024);
+            load_to_lds_16(vp, off, to + Sh::HALF + (wave * (MINE / 2) + j) * 1024);
         }
     };
 
@@ -523,9 +537,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
         if (kt[1] == base + RING * 2 * Sh::HALF) kt[1] = base;
         stage = kt[1] + 2 * Sh::HALF;
         if (stage == base + RING * 2 * Sh::HALF) stage = base;
-        const int64_t key = k0 + 32 * static_cast<int64_t>(i);
-        const bool all = key + 64 <= (t.length < end ? t.length : end) && real == 15u;
-        c.template tile<2>(a, t, kt, key, all, end, real, col, quad);
+        const bool all = 32 * i + 64 <= whole && real == 15u;
+        c.template tile<2>(a, t, kt, k0 + 32 * i, all, end, real, col, quad);
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
