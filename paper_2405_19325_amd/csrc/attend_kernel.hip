@@ -254,18 +254,14 @@ struct Columns {
     }
 };
 
-// Four elements of a finished column, or of a range's part of one, and with
-// d == 0 its reference and sum.
+// Four elements of a finished column, or of a part of one (`part` not null: its
+// columns [cols][D]), and with d == 0 its reference and sum.
 template <knn_dtype DT, int D>
-__device__ __forceinline__ void store(const AttendArgs &a, int64_t splits, int64_t split, int64_t at, int d, f32x4_t r,
-                                      float top, float l, float *part, float *part_ml) {
-    if (splits > 1) {
-        const int64_t to = split * a.rows * a.q_heads + at;
-        if (d == 0) {
-            part_ml[2 * to] = top;
-            part_ml[2 * to + 1] = l;
-        }
-        *reinterpret_cast<f32x4_t *>(part + to * D + d) = r;
+__device__ __forceinline__ void store(const AttendArgs &a, int64_t at, int col, int d, f32x4_t r, float top, float l,
+                                      float *part, float *part_ml) {
+    if (part != nullptr) {
+        if (d == 0) *reinterpret_cast<float2 *>(part_ml + 2 * col) = make_float2(top, l);
+        *reinterpret_cast<f32x4_t *>(part + static_cast<int64_t>(col) * D + d) = r;
     } else {
         const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // no key: 0; NaN stays
         *reinterpret_cast<u32x2_t *>(static_cast<uint16_t *>(a.out) + at * D + d) =
@@ -290,30 +286,119 @@ struct Shape {
     static constexpr size_t RING_LDS = static_cast<size_t>(RING) * 2 * HALF;
 };
 
-// A workgroup's part of the work: column tile `ct` of key head h of sequence s,
-// range `split` of the keys.  Its neighbours in the grid go to the 8 XCDs in
-// turn, and those that read the same keys (column tiles of one range) to one.
-struct Work {
-    int64_t s, ct, split;
-    int h;
-    bool any;
-};
+constexpr int kStep = 64;  // keys of a step: what runs of keys are counted in
 
-__device__ __forceinline__ Work work_of(const AttendArgs &a, int64_t tiles, int64_t splits) {
-    const int64_t id = blockIdx.x, group = id / (8 * tiles), in = id % (8 * tiles);
-    int64_t unit = group * 8 + in % 8;
-    Work w;
-    w.ct = in / 8;
-    w.any = unit < a.S * a.kv_heads * splits;
-    w.split = unit % splits;
-    unit /= splits;
-    w.h = static_cast<int>(unit % a.kv_heads);
-    w.s = unit / a.kv_heads;
-    return w;
+__device__ __forceinline__ int steps_of(const Tile &t) {
+    return t.n > 0 ? static_cast<int>((t.total + kStep - 1) / kStep) : 0;
 }
 
-// The keys of a workgroup's range, counted from its first one, k0 (a multiple
-// of 128): where they lie, and how many rows there are to read.
+// The steps of all sequences and key heads one behind the other (sequences in
+// order, each one's heads in order), cut into one run a team; they differ by one
+// step at most, and with fewer steps than teams only as many teams have one.
+// Found by a wave, 64 sequences at a time.
+struct Runs {
+    int64_t total, teams;  // steps, and the teams that have any
+
+    __device__ __forceinline__ Runs(const AttendArgs &a, int64_t most) : total(0) {
+        const int lane = threadIdx.x & 63;
+        for (int64_t s = 0; s < a.S; s += 64) {
+            const uint32_t v = s + lane < a.S ? static_cast<uint32_t>(steps_of(tile_of(a, s + lane))) : 0u;
+            total += readlane_u32(wave_incl_scan_u32(v, lane), 63);
+        }
+        total *= a.kv_heads;
+        teams = total < most ? total : most;
+    }
+    __device__ __forceinline__ int64_t begin(int64_t team) const { return team * total / teams; }
+    // The team whose run holds step `at`.
+    __device__ __forceinline__ int64_t team_of(int64_t at) const {
+        int64_t w = at * teams / total;
+        while (w + 1 < teams && begin(w + 1) <= at) ++w;
+        while (w > 0 && begin(w) > at) --w;
+        return w;
+    }
+    // The first step of sequence s (s < 0: of the sequence that holds step `at`, which s then is).
+    __device__ __forceinline__ int64_t first(const AttendArgs &a, int64_t &s, int64_t at) const {
+        const int lane = threadIdx.x & 63;
+        int64_t run = 0;
+        for (int64_t base = 0; base < a.S; base += 64) {
+            const uint32_t v = base + lane < a.S ? static_cast<uint32_t>(steps_of(tile_of(a, base + lane))) : 0u;
+            const uint32_t incl = wave_incl_scan_u32(v, lane);
+            if (s < 0) {
+                const uint64_t hit = __ballot((run + incl) * a.kv_heads > at);
+                if (hit != 0) {
+                    const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+                    s = base + l;
+                    return (run + readlane_u32(incl, l) - readlane_u32(v, l)) * a.kv_heads;
+                }
+            } else if (s < base + 64) {
+                const int l = static_cast<int>(s - base);
+                return (run + readlane_u32(incl, l) - readlane_u32(v, l)) * a.kv_heads;
+            }
+            run += readlane_u32(incl, 63);
+        }
+        return run * a.kv_heads;
+    }
+};
+
+// A workgroup is column tile `ct` of a team.  Neighbours in the grid go to the 8
+// XCDs in turn: a team's workgroups, which read the same keys, go to one.
+struct Place {
+    int64_t team, ct;
+};
+__device__ __forceinline__ Place place_of(int64_t tiles) {
+    const int64_t id = blockIdx.x, in = id % (8 * tiles);
+    return Place{id / (8 * tiles) * 8 + in % 8, in / 8};
+}
+
+// The keys k0 .. end - 1 of head h of sequence s, as far as column tile `ct`
+// sees them, into the output or, where the head has keys in other runs too,
+// into a part: f(tile, s, h, k0, end, part, part_ml) for one after the other of a
+// team's run.  `cols` columns a tile.
+template <int D, typename F>
+__device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, int64_t teams, int cols, float *part,
+                                          float *part_ml, F f) {
+    const Place at = place_of(tiles);
+    const Runs runs(a, teams);
+    if (at.team >= runs.teams) return;
+    int64_t pos = runs.begin(at.team);
+    const int64_t stop = runs.begin(at.team + 1);
+    int64_t s = -1;
+    const int64_t off = pos - runs.first(a, s, pos);
+    Tile t = tile_of(a, s);
+    int steps = steps_of(t);
+    int h = static_cast<int>(off / steps), step = static_cast<int>(off % steps);
+    const int g = a.q_heads / a.kv_heads;
+    while (true) {
+        const int n = static_cast<int>(steps - step < stop - pos ? steps - step : stop - pos);
+        const int64_t c0 = at.ct * cols, all = static_cast<int64_t>(t.n) * g;
+        if (c0 < all) {
+            int64_t end = static_cast<int64_t>(step + n) * kStep;
+            if (end > t.total) end = t.total;
+            if (a.tree_mask == nullptr) {  // a chain: nothing sees what lies behind the tile's last row
+                const int64_t last = (c0 + cols < all ? c0 + cols - 1 : all - 1) / g;
+                if (t.length + last + 1 < end) end = t.length + last + 1;
+            }
+            const bool whole = n == steps;
+            const int64_t slot = (at.team * tiles + at.ct) * 2 + (step == 0 ? 1 : 0);
+            f(t, s, h, static_cast<int64_t>(step) * kStep, end, whole ? nullptr : part + slot * cols * D,
+              whole ? nullptr : part_ml + slot * cols * 2);
+        }
+        pos += n;
+        if (pos >= stop) return;
+        step = 0;
+        if (++h == a.kv_heads) {
+            h = 0;
+            do {
+                t = tile_of(a, ++s);
+                steps = steps_of(t);
+            } while (steps == 0);
+        }
+        __syncthreads();  // the stages are read: the next keys may overwrite them
+    }
+}
+
+// The keys of a span, counted from its first one, k0 (a multiple
+// of kStep): where they lie, and how many rows there are to read.
 template <int D>
 struct Keys {
     const int32_t *table;  // of k0's page
@@ -339,34 +424,18 @@ struct Keys {
 };
 
 // Few columns (NT x 16): the W waves share them and wave w takes the 32-key
-// tiles w, w + W, ... of the workgroup's range with a reference and sums of its
-// own, joined at the end.  Each wave fills its own two stages by loads straight
-// to LDS, one tile ahead, and waits only for its own loads: no barrier in the
-// loop.
+// tiles w, w + W, ... of a span with a reference and sums of its own, joined at
+// the end.  Each wave fills its own two stages by loads straight to LDS, one
+// tile ahead, and waits only for its own loads: no barrier in the loop.
 template <knn_dtype DT, int D, int NT>
-__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t splits, int64_t chunk,
-                                                           float *part, float *part_ml) {
+__device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int64_t s, int h, int64_t c0, int64_t k0,
+                                         int64_t end, u32x4_t *lds, float *part, float *part_ml) {
     using Sh = Shape<D>;
     constexpr int W = Sh::W, DB = D / 16, COLS = 16 * NT;
-    extern __shared__ __align__(16) u32x4_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
-    const Work wk = work_of(a, tiles, splits);
-    if (!wk.any) return;
-    const int h = wk.h, g = a.q_heads / a.kv_heads;
-    const Tile t = tile_of(a, wk.s);
-    const int64_t c0 = wk.ct * COLS, cols = static_cast<int64_t>(t.n) * g;
-    if (c0 >= cols) return;
-    // the keys of this range that any of the columns sees
-    int64_t end = t.total;
-    if (a.tree_mask == nullptr) {
-        const int64_t last = (c0 + COLS - 1 < cols ? c0 + COLS - 1 : cols - 1) / g;
-        if (t.length + last + 1 < end) end = t.length + last + 1;
-    }
-    const int64_t k0 = wk.split * chunk;
-    if (splits > 1 && k0 >= t.total) return;
-    if (k0 + chunk < end) end = k0 + chunk;
-
+    const int g = a.q_heads / a.kv_heads;
+    const int64_t cols = static_cast<int64_t>(t.n) * g;
     Columns<DT, D, NT> c;
     c.load(a, t, h, g, c0, cols, col, quad);
     const uint32_t mine =
@@ -374,7 +443,7 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
     const int n_tiles = end > k0 ? static_cast<int>((end - k0 + 31) / 32) : 0;
     const int own = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // this wave's tiles
     const int64_t whole = (t.length < end ? t.length : end) - k0;       // keys that every column sees
-    const Keys<D> keys(a, wk.s, h, k0, end);
+    const Keys<D> keys(a, s, h, k0, end);
     // Lane l keeps the page of half l & 1 of this wave's tile l / 2 from tile `held` on.
     int32_t page_reg = 0;
     auto hold_pages = [&](int held) {
@@ -454,8 +523,19 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
             r += by * *reinterpret_cast<const f32x4_t *>(acc + (w * COLS + cc) * PITCH + d);
         }
         const int64_t at = (t.r0 + (c0 + cc) / g) * a.q_heads + h * g + (c0 + cc) % g;  // (row, query head)
-        store<DT, D>(a, splits, wk.split, at, d, r, top, l, part, part_ml);
+        store<DT, D>(a, at, cc, d, r, top, l, part, part_ml);
     }
+}
+
+template <knn_dtype DT, int D, int NT>
+__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t teams, float *part,
+                                                           float *part_ml) {
+    extern __shared__ __align__(16) u32x4_t lds[];
+    const int64_t c0 = place_of(tiles).ct * (16 * NT);
+    each_span<D>(a, tiles, teams, 16 * NT, part, part_ml,
+                 [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
+                     span_few<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
+                 });
 }
 
 // Many columns: four waves of NT x 16 each on the same keys, 64 at a time, which
@@ -464,34 +544,20 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
 // have landed and every wave has read the two before, whose stages are filled
 // next.
 template <knn_dtype DT, int D, int NT>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t splits, int64_t chunk,
-                                                     float *part, float *part_ml) {
+__device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, int64_t s, int h, int64_t c0, int64_t k0,
+                                          int64_t end, u32x4_t *lds, float *part, float *part_ml) {
     using Sh = Shape<D>;
-    constexpr int DB = D / 16, COLS = 64 * NT, RING = Sh::RING, MINE = Sh::LOADS / 2;  // loads of a wave and tile
-    extern __shared__ __align__(16) u32x4_t lds[];
+    constexpr int DB = D / 16, RING = Sh::RING, MINE = Sh::LOADS / 2;  // loads of a wave and tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
-    const Work wk = work_of(a, tiles, splits);
-    if (!wk.any) return;
-    const int h = wk.h, g = a.q_heads / a.kv_heads;
-    const Tile t = tile_of(a, wk.s);
-    const int64_t c0 = wk.ct * COLS, cols = static_cast<int64_t>(t.n) * g;
-    if (c0 >= cols) return;
-    int64_t end = t.total;
-    if (a.tree_mask == nullptr) {
-        const int64_t last = (c0 + COLS - 1 < cols ? c0 + COLS - 1 : cols - 1) / g;
-        if (t.length + last + 1 < end) end = t.length + last + 1;
-    }
-    const int64_t k0 = wk.split * chunk;
-    if (splits > 1 && k0 >= t.total) return;
-    if (k0 + chunk < end) end = k0 + chunk;
-
+    const int g = a.q_heads / a.kv_heads;
+    const int64_t cols = static_cast<int64_t>(t.n) * g;
     Columns<DT, D, NT> c;
     c.load(a, t, h, g, c0 + 16 * NT * wave, cols, col, quad);
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_offset(lds));
     const int n = end > k0 ? static_cast<int>((end - k0 + 31) / 32) : 0;
     const int64_t whole = (t.length < end ? t.length : end) - k0;  // keys that every column sees
-    const Keys<D> keys(a, wk.s, h, k0, end);
+    const Keys<D> keys(a, s, h, k0, end);
     // Lane l keeps the page of half l & 1 of tile l / 2 from tile `held` on, and of the 32 tiles before.
     int32_t page_reg = 0, page_old = 0;
     auto hold_pages = [&](int held) {
@@ -542,37 +608,74 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        const int64_t cc = c0 + 16 * NT * wave + 16 * i + col;
-        if (cc >= cols) continue;
-        const int64_t at = (t.r0 + cc / g) * a.q_heads + h * g + cc % g;
+        const int cc = 16 * NT * wave + 16 * i + col;
+        if (c0 + cc >= cols) continue;
+        const int64_t at = (t.r0 + (c0 + cc) / g) * a.q_heads + h * g + (c0 + cc) % g;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
-            store<DT, D>(a, splits, wk.split, at, 16 * d + 4 * quad, c.o[i][d], c.m[i], c.sum[i][0], part, part_ml);
+            store<DT, D>(a, at, cc, 16 * d + 4 * quad, c.o[i][d], c.m[i], c.sum[i][0], part, part_ml);
     }
 }
 
-// Joins the ranges of a (row, query head), one wave each.
+template <knn_dtype DT, int D, int NT>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t teams,
+                                                                      float *part, float *part_ml) {
+    extern __shared__ __align__(16) u32x4_t lds[];
+    const int64_t c0 = place_of(tiles).ct * (64 * NT);
+    each_span<D>(a, tiles, teams, 64 * NT, part, part_ml,
+                 [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
+                     span_many<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
+                 });
+}
+
+// Joins the parts of a (row, query head) whose keys lie in several runs, one
+// wave each: the references of up to 64 parts at once, a lane each, then the
+// parts' outputs.
 template <knn_dtype DT, int D>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t splits, int64_t chunk, const float *part,
-                                                     const float *part_ml) {
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles, int64_t teams, int cols,
+                                                     const float *part, const float *part_ml) {
     constexpr int PER = D / 64;  // elements of a lane
     const int lane = threadIdx.x & 63;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // (row, query head)
     const int64_t heads = a.q_heads, row = at / heads;
     if (row >= a.rows || row >= a.row_offsets[a.S]) return;  // the whole wave
-    const int64_t s = set_of_query_wave(a.row_offsets, a.S, row);
+    int64_t s = set_of_query_wave(a.row_offsets, a.S, row);
     const Tile t = tile_of(a, s);
     if (row - t.r0 >= t.n) return;
-    const int64_t n = t.total > 0 ? (t.total + chunk - 1) / chunk : 1, plane = a.rows * heads;
-    float top = kFloor;
-    for (int64_t i = lane; i < n; i += 64) top = fmaxf(top, part_ml[2 * (i * plane + at)]);
-    top = wave_allmax(top);
-    float l = 0.0f, r[PER] = {};
-    for (int64_t i = 0; i < n; ++i) {
-        const float by = exp2f(part_ml[2 * (i * plane + at)] - top);
-        l += by * part_ml[2 * (i * plane + at) + 1];
+    const int g = a.q_heads / a.kv_heads, head = static_cast<int>(at % heads), h = head / g;
+    const int64_t col = (row - t.r0) * g + head % g, ct = col / cols, c = col % cols;
+    const Runs runs(a, teams);
+    const int64_t steps = steps_of(t), first = runs.first(a, s, 0) + h * steps;
+    const int64_t w0 = runs.team_of(first), w1 = runs.team_of(first + steps - 1);
+    if (w0 == w1) return;  // one team had all of it
+    auto slot = [&](int64_t w) { return ((w * tiles + ct) * 2 + (w == w0 ? 1 : 0)) * cols + c; };
+    float top = kFloor, l = 0.0f, r[PER] = {};
+    for (int64_t base = w0; base <= w1; base += 64) {
+        const int n = static_cast<int>(w1 - base + 1 < 64 ? w1 - base + 1 : 64);
+        const float2 ml = lane < n ? *reinterpret_cast<const float2 *>(part_ml + 2 * slot(base + lane)) : make_float2(kFloor, 0.0f);
+        const float to = fmaxf(top, wave_allmax(ml.x));
+        const float old = exp2f(top - to), mine = exp2f(ml.x - to);
+        top = to;
+        l *= old;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) r[j] += by * part[(i * plane + at) * D + lane * PER + j];
+        for (int j = 0; j < PER; ++j) r[j] *= old;
+        l += wave_allsum(mine * ml.y);
+        for (int i = 0; i < n; i += 4) {  // four parts on their way at once
+            float v[4][PER];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float *from = part + slot(base + min(i + u, n - 1)) * D + lane * PER;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) v[u][j] = from[j];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (i + u >= n) break;
+                const float by = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), i + u));
+#pragma unroll
+                for (int j = 0; j < PER; ++j) r[j] += by * v[u][j];
+            }
+        }
     }
     const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
     uint16_t *out = static_cast<uint16_t *>(a.out) + at * D + lane * PER;
@@ -587,20 +690,16 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t split
 
 template <knn_dtype DT, int D>
 hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *part_ml, hipStream_t stream) {
-    const int64_t units = a.S * a.kv_heads * p.splits, blocks = (units + 7) / 8 * 8 * p.tiles;
-    const int64_t joins = (a.rows * a.q_heads + 3) / 4;
+    const int64_t blocks = p.teams * p.tiles, joins = (a.rows * a.q_heads + 3) / 4;
     if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(blocks)), few(Shape<D>::W * 64);
-    if (p.cols == 16)
-        k_attend<DT, D, 1><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
-    else if (D < 256 && p.cols == 32)
-        k_attend<DT, D < 256 ? D : 64, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
-    else if (p.cols == 64)
-        k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
-    else
-        k_attend_many<DT, D < 256 ? D : 64, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.splits, p.chunk, part, part_ml);
-    if (p.splits > 1)
-        k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.splits, p.chunk, part, part_ml);
+    constexpr int N = D < 256 ? D : 64;  // (the wider kinds are not taken at 256)
+    if (p.cols == 16) k_attend<DT, D, 1><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
+    else if (p.cols == 32) k_attend<DT, N, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
+    else if (p.cols == 64) k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
+    else k_attend_many<DT, N, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
+    if (p.total > 0)
+        k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.tiles, p.teams, p.cols, part, part_ml);
     return hipGetLastError();
 }
 
@@ -622,16 +721,13 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
     // (At head_dim 256 the wider kind of either kernel does not fit the registers.)
     p.cols = cols <= 16 ? 16 : cols <= 32 && head_dim < 256 ? 32 : cols <= 64 || head_dim == 256 ? 64 : 128;
     p.tiles = (cols + p.cols - 1) / p.cols;
-    // Few columns: two workgroups a CU, each on 256 keys or more.  Many: the CUs hold two at a time, eight of them or
-    // more for every CU even out sequences of different lengths, each on 1024 keys or more.
-    const bool many = p.cols > 32;
-    const int64_t base = S * kv_heads * p.tiles, least = many ? 1024 : 256, most = (max_keys + least - 1) / least;
-    p.splits = ((many ? 2048 : 512) + base - 1) / base;
-    if (p.splits > most) p.splits = most;
-    if (p.splits > 256) p.splits = 256;
-    p.chunk = ((max_keys + p.splits - 1) / p.splits + 127) / 128 * 128;
-    p.splits = (max_keys + p.chunk - 1) / p.chunk;
-    const size_t cells = p.splits > 1 ? static_cast<size_t>(p.splits) * static_cast<size_t>(rows * q_heads) : 0;
+    // As many workgroups as the CUs hold at once, each with 256 keys or more; a multiple of 8 teams (the XCDs). 
+    const int64_t slots = head_dim == 256 || (p.cols <= 32 && head_dim == 128) ? 256 : 512;
+    const int64_t units = S * kv_heads, steps = (max_keys + kStep - 1) / kStep;
+    int64_t teams = slots / p.tiles, most = units * ((steps + 3) / 4);
+    if (teams > most) teams = most;
+    p.teams = (teams + 7) / 8 * 8;
+    const size_t cells = static_cast<size_t>(p.teams * p.tiles) * 2 * static_cast<size_t>(p.cols);
     p.off_ml = cells * static_cast<size_t>(head_dim) * sizeof(float);
     p.total = p.off_ml + cells * 2 * sizeof(float);
     return p;

@@ -51,14 +51,15 @@ struct AttendArgs {
 };
 
 // How an attention call is cut: column tiles of `cols` (row, query head) pairs
-// of one key head, and `splits` ranges of `chunk` keys, joined by a second
-// launch where there are several.
+// of one key head, and one run of keys for each of `teams` teams of workgroups,
+// a workgroup a column tile.  The keys of all sequences and heads lie one
+// behind the other for that, so that every team gets as many, whatever the
+// sequences' lengths; what a team has of a head that others have parts of is
+// joined by a second launch.
 struct AttendPlan {
     int cols;
-    int64_t tiles;
-    int64_t splits;
-    int64_t chunk;
-    size_t off_ml, total;  // workspace: the ranges' outputs, then (maximum, sum)
+    int64_t tiles, teams;
+    size_t off_ml, total;  // workspace: the parts, then (maximum, sum); two parts a workgroup
 };
 
 AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_rows,
