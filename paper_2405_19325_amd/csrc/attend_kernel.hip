@@ -125,16 +125,16 @@ struct Columns {
     int row_of[NT];     // row within the sequence
     float c2;           // scale log2(e), not negative: its sign is in q
 
-    __device__ __forceinline__ void load(const AttendArgs &a, const Tile &t, int h, int g, int64_t c0, int64_t cols, int col,
+    __device__ __forceinline__ void load(const AttendArgs &a, const Tile &t, int h, int g, int c0, int cols, int col,
                                          int quad) {
         c2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int64_t c = c0 + 16 * n + col;
+            const int c = c0 + 16 * n + col;
             const bool live = c < cols;
-            row_of[n] = live ? static_cast<int>(c / g) : 0;
+            row_of[n] = live ? c / g : 0;
             const uint16_t *at = static_cast<const uint16_t *>(a.q) + (t.r0 + row_of[n]) * a.q_row +
-                                 (h * g + (live ? static_cast<int>(c % g) : 0)) * a.q_head;
+                                 (h * g + (live ? c - row_of[n] * g : 0)) * a.q_head;
 #pragma unroll
             for (int k = 0; k < KK; ++k) {
                 u32x4_t v = *reinterpret_cast<const u32x4_t *>(at + 32 * k + 8 * quad);
@@ -292,51 +292,82 @@ __device__ __forceinline__ int steps_of(const Tile &t) {
     return t.n > 0 ? static_cast<int>((t.total + kStep - 1) / kStep) : 0;
 }
 
+// Unsigned quotient, in 32 bits where that is enough (a fifth of the instructions).
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(
+                                    static_cast<int>(static_cast<uint64_t>(v) >> 32)))) << 32 |
+                                static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))));
+}
+__device__ __forceinline__ int64_t readlane64(int64_t v, int lane) {
+    return static_cast<int64_t>(static_cast<uint64_t>(readlane_u32(static_cast<uint32_t>(static_cast<uint64_t>(v) >> 32), lane)) << 32 |
+                                readlane_u32(static_cast<uint32_t>(v), lane));
+}
+
 // The steps of all sequences and key heads one behind the other (sequences in
 // order, each one's heads in order), cut into one run a team; they differ by one
 // step at most, and with fewer steps than teams only as many teams have one.
-// Found by a wave, 64 sequences at a time.
+// Found by a wave, 64 sequences at a time, which its lanes keep.
 struct Runs {
-    int64_t total, teams;  // steps, and the teams that have any
+    uint64_t total, teams, each, more;  // steps; the teams that have any; the first `more` runs have each + 1 steps
+    int64_t base;                       // first sequence of those the lanes hold
+    int64_t behind;                     // steps of a head of the sequences before them
+    Tile mine;
+    uint32_t incl, own;  // steps of a head up to this lane's sequence, and its own
 
-    __device__ __forceinline__ Runs(const AttendArgs &a, int64_t most) : total(0) {
+    __device__ __forceinline__ void hold(const AttendArgs &a, int64_t s) {
         const int lane = threadIdx.x & 63;
-        for (int64_t s = 0; s < a.S; s += 64) {
-            const uint32_t v = s + lane < a.S ? static_cast<uint32_t>(steps_of(tile_of(a, s + lane))) : 0u;
-            total += readlane_u32(wave_incl_scan_u32(v, lane), 63);
-        }
-        total *= a.kv_heads;
-        teams = total < most ? total : most;
+        base = s;
+        mine = tile_of(a, s + lane < a.S ? s + lane : a.S - 1);
+        own = s + lane < a.S ? static_cast<uint32_t>(steps_of(mine)) : 0u;
+        incl = wave_incl_scan_u32(own, lane);
     }
-    __device__ __forceinline__ int64_t begin(int64_t team) const { return team * total / teams; }
+    __device__ __forceinline__ Runs(const AttendArgs &a, int64_t most) {
+        behind = 0;
+        hold(a, 0);
+        uint64_t sum = readlane_u32(incl, 63);
+        for (int64_t s = 64; s < a.S; s += 64) {
+            behind = static_cast<int64_t>(sum);
+            hold(a, s);
+            sum += readlane_u32(incl, 63);
+        }
+        total = sum * static_cast<uint64_t>(a.kv_heads);
+        teams = total < static_cast<uint64_t>(most) ? total : static_cast<uint64_t>(most);
+        each = teams > 0 ? quotient(total, teams) : 0;
+        more = total - each * teams;
+    }
+    __device__ __forceinline__ uint64_t begin(uint64_t team) const { return team * each + (team < more ? team : more); }
     // The team whose run holds step `at`.
-    __device__ __forceinline__ int64_t team_of(int64_t at) const {
-        int64_t w = at * teams / total;
-        while (w + 1 < teams && begin(w + 1) <= at) ++w;
-        while (w > 0 && begin(w) > at) --w;
-        return w;
+    __device__ __forceinline__ int64_t team_of(uint64_t at) const {
+        const uint64_t longer = more * (each + 1);
+        return static_cast<int64_t>(at < longer ? quotient(at, each + 1) : more + quotient(at - longer, each));
     }
-    // The first step of sequence s (s < 0: of the sequence that holds step `at`, which s then is).
-    __device__ __forceinline__ int64_t first(const AttendArgs &a, int64_t &s, int64_t at) const {
-        const int lane = threadIdx.x & 63;
-        int64_t run = 0;
-        for (int64_t base = 0; base < a.S; base += 64) {
-            const uint32_t v = base + lane < a.S ? static_cast<uint32_t>(steps_of(tile_of(a, base + lane))) : 0u;
-            const uint32_t incl = wave_incl_scan_u32(v, lane);
-            if (s < 0) {
-                const uint64_t hit = __ballot((run + incl) * a.kv_heads > at);
-                if (hit != 0) {
-                    const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
-                    s = base + l;
-                    return (run + readlane_u32(incl, l) - readlane_u32(v, l)) * a.kv_heads;
-                }
-            } else if (s < base + 64) {
-                const int l = static_cast<int>(s - base);
-                return (run + readlane_u32(incl, l) - readlane_u32(v, l)) * a.kv_heads;
-            }
-            run += readlane_u32(incl, 63);
+    // The sequence for which of(lane's steps before it, its steps) is true first, held and its lane returned.
+    template <typename F>
+    __device__ __forceinline__ int find(const AttendArgs &a, F of) {
+        if (a.S > 64) {
+            behind = 0;
+            hold(a, 0);
         }
-        return run * a.kv_heads;
+        while (true) {
+            const uint64_t hit = __ballot(of(static_cast<uint64_t>(behind) + incl - own, static_cast<uint64_t>(own)));
+            if (hit != 0) return __ffsll(static_cast<unsigned long long>(hit)) - 1;
+            if (base + 64 >= a.S) return 0;  // not reached
+            behind += readlane_u32(incl, 63);
+            hold(a, base + 64);
+        }
+    }
+    __device__ __forceinline__ Tile tile(int lane) const {
+        return Tile{readlane64(mine.r0, lane), __builtin_amdgcn_readlane(mine.n, lane), readlane64(mine.length, lane),
+                    readlane64(mine.total, lane)};
+    }
+    // Steps of a head before the sequence of a lane.
+    __device__ __forceinline__ uint64_t before(int lane) const {
+        return static_cast<uint64_t>(behind) + readlane_u32(incl, lane) - readlane_u32(own, lane);
     }
 };
 
@@ -358,24 +389,27 @@ template <int D, typename F>
 __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, int64_t teams, int cols, float *part,
                                           float *part_ml, F f) {
     const Place at = place_of(tiles);
-    const Runs runs(a, teams);
-    if (at.team >= runs.teams) return;
-    int64_t pos = runs.begin(at.team);
-    const int64_t stop = runs.begin(at.team + 1);
-    int64_t s = -1;
-    const int64_t off = pos - runs.first(a, s, pos);
-    Tile t = tile_of(a, s);
+    Runs runs(a, teams);
+    if (static_cast<uint64_t>(at.team) >= runs.teams) return;
+    int64_t pos = static_cast<int64_t>(runs.begin(at.team));
+    const int64_t stop = static_cast<int64_t>(runs.begin(at.team + 1));
+    const uint64_t heads = static_cast<uint64_t>(a.kv_heads);
+    const int l = runs.find(a, [&](uint64_t before, uint64_t own) { return (before + own) * heads > static_cast<uint64_t>(pos); });
+    int64_t s = runs.base + l;
+    const uint64_t off = static_cast<uint64_t>(pos) - runs.before(l) * heads;
+    Tile t = runs.tile(l);
     int steps = steps_of(t);
-    int h = static_cast<int>(off / steps), step = static_cast<int>(off % steps);
+    int h = static_cast<int>(quotient(off, static_cast<uint64_t>(steps)));
+    int step = static_cast<int>(off - static_cast<uint64_t>(h) * static_cast<uint64_t>(steps));
     const int g = a.q_heads / a.kv_heads;
     while (true) {
         const int n = static_cast<int>(steps - step < stop - pos ? steps - step : stop - pos);
-        const int64_t c0 = at.ct * cols, all = static_cast<int64_t>(t.n) * g;
+        const int c0 = static_cast<int>(at.ct) * cols, all = t.n * g;
         if (c0 < all) {
             int64_t end = static_cast<int64_t>(step + n) * kStep;
             if (end > t.total) end = t.total;
             if (a.tree_mask == nullptr) {  // a chain: nothing sees what lies behind the tile's last row
-                const int64_t last = (c0 + cols < all ? c0 + cols - 1 : all - 1) / g;
+                const int last = (c0 + cols < all ? c0 + cols - 1 : all - 1) / g;
                 if (t.length + last + 1 < end) end = t.length + last + 1;
             }
             const bool whole = n == steps;
@@ -390,6 +424,8 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
             h = 0;
             do {
                 t = tile_of(a, ++s);
+                t.r0 = uniform(t.r0), t.length = uniform(t.length), t.total = uniform(t.total);
+                t.n = __builtin_amdgcn_readfirstlane(t.n);
                 steps = steps_of(t);
             } while (steps == 0);
         }
@@ -428,14 +464,14 @@ struct Keys {
 // the end.  Each wave fills its own two stages by loads straight to LDS, one
 // tile ahead, and waits only for its own loads: no barrier in the loop.
 template <knn_dtype DT, int D, int NT>
-__device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int64_t s, int h, int64_t c0, int64_t k0,
+__device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int64_t s, int h, int c0, int64_t k0,
                                          int64_t end, u32x4_t *lds, float *part, float *part_ml) {
     using Sh = Shape<D>;
     constexpr int W = Sh::W, DB = D / 16, COLS = 16 * NT;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
     const int g = a.q_heads / a.kv_heads;
-    const int64_t cols = static_cast<int64_t>(t.n) * g;
+    const int cols = t.n * g;
     Columns<DT, D, NT> c;
     c.load(a, t, h, g, c0, cols, col, quad);
     const uint32_t mine =
@@ -522,7 +558,8 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
             l += by * stat[W * COLS + w * COLS + cc];
             r += by * *reinterpret_cast<const f32x4_t *>(acc + (w * COLS + cc) * PITCH + d);
         }
-        const int64_t at = (t.r0 + (c0 + cc) / g) * a.q_heads + h * g + (c0 + cc) % g;  // (row, query head)
+        const int row = (c0 + cc) / g;
+        const int64_t at = (t.r0 + row) * a.q_heads + h * g + (c0 + cc - row * g);  // (row, query head)
         store<DT, D>(a, at, cc, d, r, top, l, part, part_ml);
     }
 }
@@ -531,7 +568,7 @@ template <knn_dtype DT, int D, int NT>
 __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t teams, float *part,
                                                            float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
-    const int64_t c0 = place_of(tiles).ct * (16 * NT);
+    const int c0 = static_cast<int>(place_of(tiles).ct) * (16 * NT);
     each_span<D>(a, tiles, teams, 16 * NT, part, part_ml,
                  [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
                      span_few<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
@@ -544,14 +581,14 @@ __global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64
 // have landed and every wave has read the two before, whose stages are filled
 // next.
 template <knn_dtype DT, int D, int NT>
-__device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, int64_t s, int h, int64_t c0, int64_t k0,
+__device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, int64_t s, int h, int c0, int64_t k0,
                                           int64_t end, u32x4_t *lds, float *part, float *part_ml) {
     using Sh = Shape<D>;
     constexpr int DB = D / 16, RING = Sh::RING, MINE = Sh::LOADS / 2;  // loads of a wave and tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
     const int g = a.q_heads / a.kv_heads;
-    const int64_t cols = static_cast<int64_t>(t.n) * g;
+    const int cols = t.n * g;
     Columns<DT, D, NT> c;
     c.load(a, t, h, g, c0 + 16 * NT * wave, cols, col, quad);
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_offset(lds));
@@ -610,7 +647,8 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
     for (int i = 0; i < NT; ++i) {
         const int cc = 16 * NT * wave + 16 * i + col;
         if (c0 + cc >= cols) continue;
-        const int64_t at = (t.r0 + (c0 + cc) / g) * a.q_heads + h * g + (c0 + cc) % g;
+        const int row = (c0 + cc) / g;
+        const int64_t at = (t.r0 + row) * a.q_heads + h * g + (c0 + cc - row * g);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
             store<DT, D>(a, at, cc, 16 * d + 4 * quad, c.o[i][d], c.m[i], c.sum[i][0], part, part_ml);
@@ -621,7 +659,7 @@ template <knn_dtype DT, int D, int NT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t teams,
                                                                       float *part, float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
-    const int64_t c0 = place_of(tiles).ct * (64 * NT);
+    const int c0 = static_cast<int>(place_of(tiles).ct) * (64 * NT);
     each_span<D>(a, tiles, teams, 64 * NT, part, part_ml,
                  [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
                      span_many<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
@@ -637,15 +675,21 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles
     constexpr int PER = D / 64;  // elements of a lane
     const int lane = threadIdx.x & 63;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // (row, query head)
-    const int64_t heads = a.q_heads, row = at / heads;
+    const int64_t heads = a.q_heads, row = static_cast<int64_t>(quotient(static_cast<uint64_t>(at), static_cast<uint64_t>(heads)));
     if (row >= a.rows || row >= a.row_offsets[a.S]) return;  // the whole wave
-    int64_t s = set_of_query_wave(a.row_offsets, a.S, row);
-    const Tile t = tile_of(a, s);
+    Runs runs(a, teams);
+    int64_t s = 0;
+    if (a.S > 64) s = set_of_query_wave(a.row_offsets, a.S, row);
+    const int lane_of = a.S > 64 ? runs.find(a, [&](uint64_t, uint64_t) { return runs.base + lane == s; })
+                                 : __ffsll(static_cast<unsigned long long>(__ballot(
+                                       lane < a.S && runs.mine.r0 <= row && row < runs.mine.r0 + runs.mine.n))) - 1;
+    if (lane_of < 0) return;  // a row past the most that the caller said
+    const Tile t = runs.tile(lane_of);
     if (row - t.r0 >= t.n) return;
-    const int g = a.q_heads / a.kv_heads, head = static_cast<int>(at % heads), h = head / g;
-    const int64_t col = (row - t.r0) * g + head % g, ct = col / cols, c = col % cols;
-    const Runs runs(a, teams);
-    const int64_t steps = steps_of(t), first = runs.first(a, s, 0) + h * steps;
+    const int g = a.q_heads / a.kv_heads, head = static_cast<int>(at - row * heads), h = head / g;
+    const int col = static_cast<int>(row - t.r0) * g + head - h * g, ct = col / cols, c = col - ct * cols;
+    const uint64_t steps = static_cast<uint64_t>(steps_of(t));
+    const uint64_t first = runs.before(lane_of) * static_cast<uint64_t>(a.kv_heads) + static_cast<uint64_t>(h) * steps;
     const int64_t w0 = runs.team_of(first), w1 = runs.team_of(first + steps - 1);
     if (w0 == w1) return;  // one team had all of it
     auto slot = [&](int64_t w) { return ((w * tiles + ct) * 2 + (w == w0 ? 1 : 0)) * cols + c; };
