@@ -29,6 +29,7 @@ constexpr float kFloor = -1.0e30f;  // reference before the first key
 constexpr float kSlack = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int64_t kWhole = 256;  // keys of a head that is not parted
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -286,16 +287,15 @@ struct Shape {
     static constexpr size_t RING_LDS = static_cast<size_t>(RING) * 2 * HALF;
 };
 
-constexpr int kStep = 64;  // keys of a step: what runs of keys are counted in
-
-__device__ __forceinline__ int steps_of(const Tile &t) {
-    return t.n > 0 ? static_cast<int>((t.total + kStep - 1) / kStep) : 0;
-}
-
 // Unsigned quotient, in 32 bits where that is enough (a fifth of the instructions).
 __device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) {
     if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
     return a / b;
+}
+
+// Steps of `step` keys that a head of a sequence has.
+__device__ __forceinline__ int steps_of(const Tile &t, int step) {
+    return t.n > 0 ? static_cast<int>(quotient(static_cast<uint64_t>(t.total + step - 1), static_cast<uint64_t>(step))) : 0;
 }
 
 __device__ __forceinline__ int64_t uniform(int64_t v) {
@@ -318,15 +318,16 @@ struct Runs {
     int64_t behind;                     // steps of a head of the sequences before them
     Tile mine;
     uint32_t incl, own;  // steps of a head up to this lane's sequence, and its own
+    int step;            // keys of one
 
     __device__ __forceinline__ void hold(const AttendArgs &a, int64_t s) {
         const int lane = threadIdx.x & 63;
         base = s;
         mine = tile_of(a, s + lane < a.S ? s + lane : a.S - 1);
-        own = s + lane < a.S ? static_cast<uint32_t>(steps_of(mine)) : 0u;
+        own = s + lane < a.S ? static_cast<uint32_t>(steps_of(mine, step)) : 0u;
         incl = wave_incl_scan_u32(own, lane);
     }
-    __device__ __forceinline__ Runs(const AttendArgs &a, int64_t most) {
+    __device__ __forceinline__ Runs(const AttendArgs &a, int64_t most, int step_keys) : step(step_keys) {
         behind = 0;
         hold(a, 0);
         uint64_t sum = readlane_u32(incl, 63);
@@ -386,10 +387,10 @@ __device__ __forceinline__ Place place_of(int64_t tiles) {
 // into a part: f(tile, s, h, k0, end, part, part_ml) for one after the other of a
 // team's run.  `cols` columns a tile.
 template <int D, typename F>
-__device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, int64_t teams, int cols, float *part,
+__device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, int64_t teams, int step_keys, int cols, float *part,
                                           float *part_ml, F f) {
     const Place at = place_of(tiles);
-    Runs runs(a, teams);
+    Runs runs(a, teams, step_keys);
     if (static_cast<uint64_t>(at.team) >= runs.teams) return;
     int64_t pos = static_cast<int64_t>(runs.begin(at.team));
     const int64_t stop = static_cast<int64_t>(runs.begin(at.team + 1));
@@ -398,7 +399,7 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
     int64_t s = runs.base + l;
     const uint64_t off = static_cast<uint64_t>(pos) - runs.before(l) * heads;
     Tile t = runs.tile(l);
-    int steps = steps_of(t);
+    int steps = steps_of(t, step_keys);
     int h = static_cast<int>(quotient(off, static_cast<uint64_t>(steps)));
     int step = static_cast<int>(off - static_cast<uint64_t>(h) * static_cast<uint64_t>(steps));
     const int g = a.q_heads / a.kv_heads;
@@ -406,7 +407,7 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
         const int n = static_cast<int>(steps - step < stop - pos ? steps - step : stop - pos);
         const int c0 = static_cast<int>(at.ct) * cols, all = t.n * g;
         if (c0 < all) {
-            int64_t end = static_cast<int64_t>(step + n) * kStep;
+            int64_t end = static_cast<int64_t>(step + n) * step_keys;
             if (end > t.total) end = t.total;
             if (a.tree_mask == nullptr) {  // a chain: nothing sees what lies behind the tile's last row
                 const int last = (c0 + cols < all ? c0 + cols - 1 : all - 1) / g;
@@ -414,7 +415,7 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
             }
             const bool whole = n == steps;
             const int64_t slot = (at.team * tiles + at.ct) * 2 + (step == 0 ? 1 : 0);
-            f(t, s, h, static_cast<int64_t>(step) * kStep, end, whole ? nullptr : part + slot * cols * D,
+            f(t, s, h, static_cast<int64_t>(step) * step_keys, end, whole ? nullptr : part + slot * cols * D,
               whole ? nullptr : part_ml + slot * cols * 2);
         }
         pos += n;
@@ -426,7 +427,7 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
                 t = tile_of(a, ++s);
                 t.r0 = uniform(t.r0), t.length = uniform(t.length), t.total = uniform(t.total);
                 t.n = __builtin_amdgcn_readfirstlane(t.n);
-                steps = steps_of(t);
+                steps = steps_of(t, step_keys);
             } while (steps == 0);
         }
         __syncthreads();  // the stages are read: the next keys may overwrite them
@@ -434,7 +435,7 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
 }
 
 // The keys of a span, counted from its first one, k0 (a multiple
-// of kStep): where they lie, and how many rows there are to read.
+// of 64): where they lie, and how many rows there are to read.
 template <int D>
 struct Keys {
     const int32_t *table;  // of k0's page
@@ -565,11 +566,11 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
 }
 
 template <knn_dtype DT, int D, int NT>
-__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t teams, float *part,
+__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t teams, int step, float *part,
                                                            float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
     const int c0 = static_cast<int>(place_of(tiles).ct) * (16 * NT);
-    each_span<D>(a, tiles, teams, 16 * NT, part, part_ml,
+    each_span<D>(a, tiles, teams, step, 16 * NT, part, part_ml,
                  [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
                      span_few<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
                  });
@@ -656,11 +657,11 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
 }
 
 template <knn_dtype DT, int D, int NT>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t teams,
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t teams, int step,
                                                                       float *part, float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
     const int c0 = static_cast<int>(place_of(tiles).ct) * (64 * NT);
-    each_span<D>(a, tiles, teams, 64 * NT, part, part_ml,
+    each_span<D>(a, tiles, teams, step, 64 * NT, part, part_ml,
                  [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
                      span_many<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
                  });
@@ -670,14 +671,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArg
 // wave each: the references of up to 64 parts at once, a lane each, then the
 // parts' outputs.
 template <knn_dtype DT, int D>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles, int64_t teams, int cols,
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles, int64_t teams, int step, int cols,
                                                      const float *part, const float *part_ml) {
     constexpr int PER = D / 64;  // elements of a lane
     const int lane = threadIdx.x & 63;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // (row, query head)
     const int64_t heads = a.q_heads, row = static_cast<int64_t>(quotient(static_cast<uint64_t>(at), static_cast<uint64_t>(heads)));
     if (row >= a.rows || row >= a.row_offsets[a.S]) return;  // the whole wave
-    Runs runs(a, teams);
+    Runs runs(a, teams, step);
     int64_t s = 0;
     if (a.S > 64) s = set_of_query_wave(a.row_offsets, a.S, row);
     const int lane_of = a.S > 64 ? runs.find(a, [&](uint64_t, uint64_t) { return runs.base + lane == s; })
@@ -688,7 +689,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles
     if (row - t.r0 >= t.n) return;
     const int g = a.q_heads / a.kv_heads, head = static_cast<int>(at - row * heads), h = head / g;
     const int col = static_cast<int>(row - t.r0) * g + head - h * g, ct = col / cols, c = col - ct * cols;
-    const uint64_t steps = static_cast<uint64_t>(steps_of(t));
+    const uint64_t steps = static_cast<uint64_t>(steps_of(t, step));
     const uint64_t first = runs.before(lane_of) * static_cast<uint64_t>(a.kv_heads) + static_cast<uint64_t>(h) * steps;
     const int64_t w0 = runs.team_of(first), w1 = runs.team_of(first + steps - 1);
     if (w0 == w1) return;  // one team had all of it
@@ -738,12 +739,12 @@ hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *
     if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(blocks)), few(Shape<D>::W * 64);
     constexpr int N = D < 256 ? D : 64;  // (the wider kinds are not taken at 256)
-    if (p.cols == 16) k_attend<DT, D, 1><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
-    else if (p.cols == 32) k_attend<DT, N, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
-    else if (p.cols == 64) k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
-    else k_attend_many<DT, N, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, part, part_ml);
+    if (p.cols == 16) k_attend<DT, D, 1><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
+    else if (p.cols == 32) k_attend<DT, N, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
+    else if (p.cols == 64) k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
+    else k_attend_many<DT, N, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
     if (p.total > 0)
-        k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.tiles, p.teams, p.cols, part, part_ml);
+        k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.tiles, p.teams, p.step, p.cols, part, part_ml);
     return hipGetLastError();
 }
 
@@ -765,12 +766,16 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
     // (At head_dim 256 the wider kind of either kernel does not fit the registers.)
     p.cols = cols <= 16 ? 16 : cols <= 32 && head_dim < 256 ? 32 : cols <= 64 || head_dim == 256 ? 64 : 128;
     p.tiles = (cols + p.cols - 1) / p.cols;
-    // As many workgroups as the CUs hold at once, each with 256 keys or more; a multiple of 8 teams (the XCDs). 
+    // As many workgroups as the CUs hold at once, each with 256 keys or more; a multiple of 8 teams (the XCDs).  Heads
+    // of up to kWhole keys are not parted: nothing to join (of 1,001 keys, one token and 32 heads: 15.8 us, in four parts 14.5).
     const int64_t slots = head_dim == 256 || (p.cols <= 32 && head_dim == 128) ? 256 : 512;
-    const int64_t units = S * kv_heads, steps = (max_keys + kStep - 1) / kStep;
-    int64_t teams = slots / p.tiles, most = units * ((steps + 3) / 4);
+    const bool whole = max_keys <= kWhole;
+    p.step = whole ? static_cast<int>((max_keys + 63) / 64 * 64) : 64;
+    int64_t teams = slots / p.tiles, most = S * kv_heads * (whole ? 1 : (max_keys + 255) / 256);
     if (teams > most) teams = most;
     p.teams = (teams + 7) / 8 * 8;
+    if (p.teams < 8) p.teams = 8;
+    if (whole) return p;
     const size_t cells = static_cast<size_t>(p.teams * p.tiles) * 2 * static_cast<size_t>(p.cols);
     p.off_ml = cells * static_cast<size_t>(head_dim) * sizeof(float);
     p.total = p.off_ml + cells * 2 * sizeof(float);

@@ -58,8 +58,9 @@ struct AttendArgs {
 // joined by a second launch.
 struct AttendPlan {
     int cols;
+    int step;  // keys of the steps that runs are counted in; a head of one step is not parted
     int64_t tiles, teams;
-    size_t off_ml, total;  // workspace: the parts, then (maximum, sum); two parts a workgroup
+    size_t off_ml, total;  // workspace: the parts, then (maximum, sum); two parts a workgroup, or 0
 };
 
 AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_rows,

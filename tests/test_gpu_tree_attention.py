@@ -208,6 +208,29 @@ def test_entries_that_are_no_page():
     assert (out == 0).all()
 
 
+@pytest.mark.parametrize("S", [63, 64, 65, 130, 200])
+@pytest.mark.parametrize("most", [60, 1500])
+def test_many_sequences(S, most):
+    rng = np.random.RandomState(S + most)
+    lens = [int(x) for x in rng.randint(0, most, S)]
+    rows = [int(x) for x in rng.choice([0, 1, 1, 2, 5], S)]
+    rows[0] = rows[-1] = 0
+    lens[S // 2] = most * 3
+    x, mask, sees = batch("bf16", rows, lens, (4, 2), 64, 32, seed=S, tree=True)
+    check(x, mask, sees)
+
+
+def test_bounds_on_either_side_of_parting():
+    # a head of up to 256 keys has one workgroup, a longer one parts of several; the bound decides, not the lengths
+    x, mask, sees = batch("f16", [9, 2], [247, 100], (8, 2), 128, 32, seed=40, tree=True, width=40)
+    a = check(x, mask, sees, max_keys=256)
+    b = check(x, mask, sees, max_keys=288)
+    assert (a - b).abs().max() < 0.02
+    for keys in (255, 256, 257, 1023, 1024, 1025, 2047, 2048, 2049):
+        x, mask, sees = batch("bf16", [1, 3], [keys - 1, 5], (4, 4), 64, 64, seed=keys)
+        check(x)
+
+
 def test_strides_of_queries():
     x, _, _ = batch("bf16", [3, 2], [40, 100], (8, 2), 128, 16, seed=14)
     want = check(x)
