@@ -280,10 +280,10 @@ struct Shape {
     static constexpr int PER = 64 / LANES;      // keys of one load
     // Few columns: each wave on keys of its own.
     static constexpr int W = D == 256 ? 2 : 4;
-    static constexpr int STAGES = 2;
-    static constexpr size_t LDS = static_cast<size_t>(W) * STAGES * 2 * HALF;
+    static constexpr size_t few_lds(int stages) { return static_cast<size_t>(W) * static_cast<size_t>(stages) * 2 * HALF; }
     // Many columns: four waves on the same keys.
-    static constexpr int RING = D == 64 ? 8 : D == 128 ? 5 : 4;
+    static constexpr int U = D == 256 ? 1 : 2;  // 32-key tiles between two barriers
+    static constexpr int RING = D == 64 ? 8 : D == 128 ? 5 : 2;
     static constexpr size_t RING_LDS = static_cast<size_t>(RING) * 2 * HALF;
 };
 
@@ -463,10 +463,11 @@ struct Keys {
 // Few columns (NT x 16): the W waves share them and wave w takes the 32-key
 // tiles w, w + W, ... of a span with a reference and sums of its own, joined at
 // the end.  Each wave fills its own two stages by loads straight to LDS, one
-// tile ahead, and waits only for its own loads: no barrier in the loop.
+// tile ahead, and waits only for its own loads: no barrier in the loop.  Where
+// no wave gets a second tile it has one stage (NT = 1), and a CU two workgroups.
 template <knn_dtype DT, int D, int NT>
 __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int64_t s, int h, int c0, int64_t k0,
-                                         int64_t end, u32x4_t *lds, float *part, float *part_ml) {
+                                         int64_t end, int stages, u32x4_t *lds, float *part, float *part_ml) {
     using Sh = Shape<D>;
     constexpr int W = Sh::W, DB = D / 16, COLS = 16 * NT;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -476,10 +477,10 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
     Columns<DT, D, NT> c;
     c.load(a, t, h, g, c0, cols, col, quad);
     const uint32_t mine =
-        __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * static_cast<uint32_t>(Sh::STAGES * 2 * Sh::HALF);
+        __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * static_cast<uint32_t>(stages * 2 * Sh::HALF);
     const int n_tiles = end > k0 ? static_cast<int>((end - k0 + 31) / 32) : 0;
     const int own = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // this wave's tiles
-    const int64_t whole = (t.length < end ? t.length : end) - k0;       // keys that every column sees
+    const int whole = static_cast<int>((t.length < end ? t.length : end) - k0);  // keys that every column sees
     const Keys<D> keys(a, s, h, k0, end);
     // Lane l keeps the page of half l & 1 of this wave's tile l / 2 from tile `held` on.
     int32_t page_reg = 0;
@@ -533,7 +534,7 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
     constexpr int PITCH = D + 4;
     float *stat = reinterpret_cast<float *>(lds);    // [2][W][COLS]: reference, sum
     float *acc = stat + 2 * W * COLS;                // [W][COLS][PITCH]
-    static_assert((2 * W * COLS + W * COLS * PITCH) * sizeof(float) <= Sh::LDS, "the join fits the stages");
+    static_assert((2 * W * COLS + W * COLS * PITCH) * sizeof(float) <= Sh::few_lds(NT == 1 ? 1 : 2), "the join fits the stages");
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (quad == 0) {
@@ -566,26 +567,26 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
 }
 
 template <knn_dtype DT, int D, int NT>
-__global__ __launch_bounds__(Shape<D>::W * 64) void k_attend(AttendArgs a, int64_t tiles, int64_t teams, int step, float *part,
-                                                           float *part_ml) {
+__global__ __launch_bounds__(Shape<D>::W * 64, NT == 1 && D < 256 ? 2 : 1) void k_attend(AttendArgs a, int64_t tiles, int64_t teams, int step,
+                                                                int stages, float *part, float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
     const int c0 = static_cast<int>(place_of(tiles).ct) * (16 * NT);
     each_span<D>(a, tiles, teams, step, 16 * NT, part, part_ml,
                  [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
-                     span_few<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
+                     span_few<DT, D, NT>(a, t, s, h, c0, k0, end, stages, lds, to, to_ml);
                  });
 }
 
-// Many columns: four waves of NT x 16 each on the same keys, 64 at a time, which
-// all of them read out of a ring of 32-key stages.  Each wave fetches a quarter
-// of a tile.  One barrier every two tiles: behind it every wave's loads of them
-// have landed and every wave has read the two before, whose stages are filled
-// next.
+// Many columns: four waves of NT x 16 each on the same keys, 64 at a time (32 at
+// head_dim 256), which all of them read out of a ring of 32-key stages.  Each
+// wave fetches a quarter of a tile.  One barrier every U tiles: behind it every
+// wave's loads of them have landed and every wave has read the U before, whose
+// stages are filled next.
 template <knn_dtype DT, int D, int NT>
 __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, int64_t s, int h, int c0, int64_t k0,
                                           int64_t end, u32x4_t *lds, float *part, float *part_ml) {
     using Sh = Shape<D>;
-    constexpr int DB = D / 16, RING = Sh::RING, MINE = Sh::LOADS / 2;  // loads of a wave and tile
+    constexpr int DB = D / 16, U = Sh::U, RING = Sh::RING, MINE = Sh::LOADS / 2;  // loads of a wave and tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
     const int g = a.q_heads / a.kv_heads;
@@ -594,7 +595,7 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
     c.load(a, t, h, g, c0 + 16 * NT * wave, cols, col, quad);
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_offset(lds));
     const int n = end > k0 ? static_cast<int>((end - k0 + 31) / 32) : 0;
-    const int64_t whole = (t.length < end ? t.length : end) - k0;  // keys that every column sees
+    const int whole = static_cast<int>((t.length < end ? t.length : end) - k0);  // keys that every column sees
     const Keys<D> keys(a, s, h, k0, end);
     // Lane l keeps the page of half l & 1 of tile l / 2 from tile `held` on, and of the 32 tiles before.
     int32_t page_reg = 0, page_old = 0;
@@ -619,30 +620,33 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
     };
 
 #pragma unroll
-    for (int i = 0; i < RING - 2; ++i)
+    for (int i = 0; i < RING - U; ++i)
         if (i < n) fill(i);
     uint32_t stage = base;
-    for (int i = 0; i < n; i += 2) {
-        // This wave's loads of tiles i and i + 1 have landed when only the later tiles' are on their way.
-        if (i + RING - 3 < n) __builtin_amdgcn_s_waitcnt(vmcnt_encoding<(RING - 4) * MINE>());
+    for (int i = 0; i < n; i += U) {
+        // This wave's loads of tiles i .. i + U - 1 have landed when only the later tiles' are on their way.
+        if (i + RING - U - 1 < n) __builtin_amdgcn_s_waitcnt(vmcnt_encoding<(RING - 2 * U) * MINE>());
         else __builtin_amdgcn_s_waitcnt(kVmcntZero);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (i + RING - 2 < n) fill(i + RING - 2);
-        if (i + RING - 1 < n) fill(i + RING - 1);
-        // the pages of tiles i and i + 1 (i is even): held since they were filled
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + RING - U + u < n) fill(i + RING - U + u);
+        // the pages of tiles i .. i + U - 1 (of one 32): held since they were filled
         const int filled = i + RING - 1 < n ? i + RING - 1 : n - 1;
         const int32_t pages = (filled >> 5) != (i >> 5) ? page_old : page_reg;
-        uint32_t real = 0;
+        uint32_t real = 0, kt[U];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) real |= keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31) + u)) ? 1u << u : 0u;
-        uint32_t kt[2] = {stage, stage + 2 * Sh::HALF};
-        if (kt[1] == base + RING * 2 * Sh::HALF) kt[1] = base;
-        stage = kt[1] + 2 * Sh::HALF;
-        if (stage == base + RING * 2 * Sh::HALF) stage = base;
-        const bool all = 32 * i + 64 <= whole && real == 15u;
-        c.template tile<2>(a, t, kt, k0 + 32 * i, all, end, real, col, quad);
+        for (int u = 0; u < 2 * U; ++u) real |= keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31) + u)) ? 1u << u : 0u;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            kt[u] = stage;
+            stage += 2 * Sh::HALF;
+            if (stage == base + RING * 2 * Sh::HALF) stage = base;
+        }
+        const bool all = 32 * i + 32 * U <= whole && real == (1u << 2 * U) - 1u;
+        c.template tile<U>(a, t, kt, k0 + 32 * i, all, end, real, col, quad);
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -657,7 +661,7 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
 }
 
 template <knn_dtype DT, int D, int NT>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t teams, int step,
+__global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t teams, int step,
                                                                       float *part, float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
     const int c0 = static_cast<int>(place_of(tiles).ct) * (64 * NT);
@@ -739,8 +743,8 @@ hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *
     if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(blocks)), few(Shape<D>::W * 64);
     constexpr int N = D < 256 ? D : 64;  // (the wider kinds are not taken at 256)
-    if (p.cols == 16) k_attend<DT, D, 1><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
-    else if (p.cols == 32) k_attend<DT, N, 2><<<grid, few, Shape<D>::LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
+    if (p.cols == 16) k_attend<DT, D, 1><<<grid, few, Shape<D>::few_lds(p.stages), stream>>>(a, p.tiles, p.teams, p.step, p.stages, part, part_ml);
+    else if (p.cols == 32) k_attend<DT, N, 2><<<grid, few, Shape<D>::few_lds(p.stages), stream>>>(a, p.tiles, p.teams, p.step, p.stages, part, part_ml);
     else if (p.cols == 64) k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
     else k_attend_many<DT, N, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
     if (p.total > 0)
@@ -766,14 +770,17 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
     // (At head_dim 256 the wider kind of either kernel does not fit the registers.)
     p.cols = cols <= 16 ? 16 : cols <= 32 && head_dim < 256 ? 32 : cols <= 64 || head_dim == 256 ? 64 : 128;
     p.tiles = (cols + p.cols - 1) / p.cols;
-    // As many workgroups as the CUs hold at once, each with 256 keys or more; a multiple of 8 teams (the XCDs).  Heads
-    // of up to kWhole keys are not parted: nothing to join (of 1,001 keys, one token and 32 heads: 15.8 us, in four parts 14.5).
-    const int64_t slots = head_dim == 256 || (p.cols <= 32 && head_dim == 128) ? 256 : 512;
-    const bool whole = max_keys <= kWhole;
+    // As many workgroups as the CUs hold at once, each with 256 keys or more (many columns: 128); teams a multiple of 8
+    // (the XCDs).  Heads of up to kWhole keys are not parted: nothing to join (of 1,001 keys, one token and 32 heads:
+    // 15.8 us, in four parts 14.5).
+    const bool many = p.cols > 32, whole = max_keys <= kWhole;
     p.step = whole ? static_cast<int>((max_keys + 63) / 64 * 64) : 64;
-    int64_t teams = slots / p.tiles, most = S * kv_heads * (whole ? 1 : (max_keys + 255) / 256);
-    if (teams > most) teams = most;
-    p.teams = (teams + 7) / 8 * 8;
+    p.stages = p.cols == 16 && max_keys <= 32 * (head_dim == 256 ? 2 : 4) ? 1 : 2;
+    int64_t slots = 512;
+    if (!many && head_dim >= 128 && p.stages == 2) slots = 256;
+    const int64_t least = many ? 128 : 256, most = S * kv_heads * (whole ? 1 : (max_keys + least - 1) / least);
+    p.teams = (most + 7) / 8 * 8;
+    if (p.teams * p.tiles > slots) p.teams = slots / p.tiles / 8 * 8;  // one workgroup too many takes a second round
     if (p.teams < 8) p.teams = 8;
     if (whole) return p;
     const size_t cells = static_cast<size_t>(p.teams * p.tiles) * 2 * static_cast<size_t>(p.cols);

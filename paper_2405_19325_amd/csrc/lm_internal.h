@@ -58,7 +58,8 @@ struct AttendArgs {
 // joined by a second launch.
 struct AttendPlan {
     int cols;
-    int step;  // keys of the steps that runs are counted in; a head of one step is not parted
+    int step;    // keys of the steps that runs are counted in; a head of one step is not parted
+    int stages;  // few columns: stages of a wave
     int64_t tiles, teams;
     size_t off_ml, total;  // workspace: the parts, then (maximum, sum); two parts a workgroup, or 0
 };
