@@ -36,16 +36,20 @@ def _flat(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple
 
 
 class _Call:
-    """A call that is made again and again on one GPU; `_own`: the tensors that it allocated."""
+    """A call that is made again and again on one GPU, with the same buffers where they are."""
 
-    def _keep(self, index: int, *own: torch.Tensor):
-        self._index = index
-        self._own = own
-        self._home = _stream(None)
-        self._known = {self._home}
+    def _keep(self, index: int, name: str, args: Sequence, tensors: Sequence, own: Sequence[torch.Tensor]):
+        """`name`: the library's function; `args`: its arguments but the stream, converted once; `tensors`: what they
+        point to; `own`: those of them that this object allocated."""
+        fn = getattr(load(), name)
+        self._name, self._fn = name, fn
+        self._args = tuple(a if a is None else kind(a) for kind, a in zip(fn.argtypes, args))
+        self._index, self._tensors, self._own = index, tuple(tensors), tuple(own)
+        self._known = {_stream(None)}
 
-    def _handle(self, stream):
-        _need(torch.cuda.current_device() == self._index, f"made for cuda:{self._index}, which is not the current device")
+    def _call(self, stream):
+        if torch.cuda.current_device() != self._index:
+            raise ValueError(f"made for cuda:{self._index}, which is not the current device")
         h = _stream(stream)
         if h not in self._known:  # the allocator has to know who else uses what this object allocated
             if not torch.cuda.is_current_stream_capturing():
@@ -53,7 +57,9 @@ class _Call:
                 for t in self._own:
                     t.record_stream(s)
                 self._known.add(h)
-        return h
+        st = self._fn(*self._args, h)
+        if st != _lib.KNN_OK:
+            _lib.check(self._name, st)
 
 
 def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, row_offsets: torch.Tensor,
@@ -113,19 +119,15 @@ class KVAppend(_Call):
             half = inv_freq.numel()
             _flat("inv_freq", inv_freq, torch.float32, (half,))
         self.q_out = q_out
-        self._tensors = (q, k, v, row_offsets, cache_lens, pages, positions, inv_freq, source_rows)
-        self._caches = (k_cache, v_cache)
+        tensors = (q, k, v, row_offsets, cache_lens, pages, positions, inv_freq, source_rows)
         strides = [t.stride(i) if t is not None else 0 for t in (q, k, v) for i in (0, 1)]
-        self._sizes = (rows, source, S, q_heads, kv_heads, d, 2 * half, int(bool(interleaved)), *strides, n_pages,
-                       page_size, pages.shape[1], _dtype_code(k))
-        self._keep(index, *own)
+        args = (*map(_ptr, tensors), rows, source, S, q_heads, kv_heads, d, 2 * half, int(bool(interleaved)), *strides,
+                n_pages, page_size, pages.shape[1], _dtype_code(k), *map(_ptr, (q_out, k_cache, v_cache)))
+        self._keep(index, "knn_kv_append", args, (*tensors, q_out, k_cache, v_cache), own)
 
     def run(self, stream=None) -> Optional[torch.Tensor]:
         """One call; returns q_out (the rotated queries), valid after stream sync."""
-        h = self._handle(stream)
-        st = load().knn_kv_append(*map(_ptr, self._tensors), *self._sizes, _ptr(self.q_out),
-                                  *map(_ptr, self._caches), h)
-        _lib.check("knn_kv_append", st)
+        self._call(stream)
         return self.q_out
 
 
@@ -194,18 +196,16 @@ class TreeAttention(_Call):
         need = load().knn_tree_attention_workspace_size(rows, S, q_heads, kv_heads, d, int(max_rows), int(max_keys))
         self.workspace = torch.empty(max(int(need), 256), dtype=torch.uint8, device=q.device)
         own.append(self.workspace)
-        self._tensors = (q, k_cache, v_cache, pages, row_offsets, cache_lens, tree_mask)
-        self._sizes = (rows, S, q_heads, kv_heads, d, q.stride(0), q.stride(1), n_pages, page_size, pages.shape[1],
-                       words, int(max_rows), int(max_keys), _dtype_code(q),
-                       float(1.0 / math.sqrt(d) if scale is None else scale))
-        self._keep(index, *own)
+        tensors = (q, k_cache, v_cache, pages, row_offsets, cache_lens, tree_mask)
+        args = (*map(_ptr, tensors), rows, S, q_heads, kv_heads, d, q.stride(0), q.stride(1), n_pages, page_size,
+                pages.shape[1], words, int(max_rows), int(max_keys), _dtype_code(q),
+                float(1.0 / math.sqrt(d) if scale is None else scale), _ptr(out), _ptr(lse), _ptr(self.workspace),
+                self.workspace.numel())
+        self._keep(index, "knn_tree_attention", args, (*tensors, out, lse), own)
 
     def run(self, stream=None) -> torch.Tensor:
         """One call; returns out (and fills lse, where there is one), valid after stream sync."""
-        h = self._handle(stream)
-        st = load().knn_tree_attention(*map(_ptr, self._tensors), *self._sizes, _ptr(self.out), _ptr(self.lse),
-                                       _ptr(self.workspace), self.workspace.numel(), h)
-        _lib.check("knn_tree_attention", st)
+        self._call(stream)
         return self.out
 
 
@@ -242,16 +242,15 @@ class Sampler(_Call):
         code = _dtype_code(scores)
         need = load().knn_sample_workspace_size(rows, V, code)
         self.workspace = torch.empty(max(int(need), 256), dtype=torch.uint8, device=dev)
-        self._tensors = (scores, uniforms, temperature, top_k, top_p, min_p)
-        self._sizes = (rows, V, scores.stride(0), int(bool(probabilities)), code)
-        self._keep(index, self.token, self.prob, self.kept, self.workspace)
+        tensors = (scores, uniforms, temperature, top_k, top_p, min_p)
+        own = (self.token, self.prob, self.kept, self.workspace)
+        args = (*map(_ptr, tensors), rows, V, scores.stride(0), int(bool(probabilities)), code, *map(_ptr, own),
+                self.workspace.numel())
+        self._keep(index, "knn_sample", args, tensors, own)
 
     def run(self, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
         """One call; returns (token, its probability among those kept, how many were kept), valid after stream sync."""
-        h = self._handle(stream)
-        st = load().knn_sample(*map(_ptr, self._tensors), *self._sizes, _ptr(self.token), _ptr(self.prob),
-                               _ptr(self.kept), _ptr(self.workspace), self.workspace.numel(), h)
-        _lib.check("knn_sample", st)
+        self._call(stream)
         return self.token, self.prob, self.kept
 
 
