@@ -18,10 +18,22 @@
 // comparing it with all others.  Where they are more than the list holds (a
 // value that hundreds of tokens share, a row far from any logarithmic
 // spread), the cut is found on the keys that order like the values, eleven
-// bits a pass.
+// bits a pass.  A small k needs neither bins nor a weight for each element:
+// the k-th largest of the threads' own largest values bounds it from below,
+// and what is not under that bound is listed at once (32,000 logits, k = 50,
+// p = 0.9: 17 us, 32 by bins).  Min-p alone lists what is above its value
+// likewise (12 us, 18 by a pass that weighs).
 //
 // One workgroup takes a row.  A row of up to 128 KiB stays in LDS from the first
 // pass on; a longer one is read three times, from the caches after the first.
+//
+// Measured, with the call: 32,000 bfloat16 logits, one row: largest element
+// alone 6.7 us, drawn from all 18, top-p 24; 256 rows of 131,072 float logits
+// with top-p 122 us, of which 19 would read them once.  What bounds it is the
+// issue of 64-bit operations: 13 of a weight's 20 instructions are such, a
+// weight of 64 elements takes a SIMD about 160 clocks, and top-p takes two for
+// each element that it keeps.  (Weights in 32 bits would draw another token in
+// one row of 50.)  An atomic of 64 lanes on the bins takes 40 clocks of the CU.
 #include "knnlm_device.h"
 #include "lm_internal.h"
 
@@ -34,7 +46,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
 
 constexpr size_t kHeldBytes = 128 * 1024;
-constexpr int kList = 512;  // elements of a cut's bin that are compared with each other
+constexpr int kList = 512;  // elements that are compared with each other
+constexpr int kFew = 256;   // the largest k whose elements are listed at once
 
 template <knn_dtype DT>
 __device__ __forceinline__ float element(const void *row, int i) {
@@ -62,9 +75,11 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 
 // 2^(y / 64) 2^e for y <= 0, to 2^-51 relative: a table of the 64th roots of
 // two, and the power series of exp(f ln(2) / 64), |f| <= 1/2, whose 6th term is
-// 4e-17.  What is under 2^-200 counts as that.
-__device__ __forceinline__ double power2(double y, int e, const double *roots) {
+// 4e-17.  What is under 2^-200 counts as that; what is not `in` is under 2^-500.
+__device__ __forceinline__ double power2(double y, bool in, int e, const double *roots) {
     y = fmax(y, -12800.0);
+    // Not `in`: about -32768, by the high word alone.
+    y = __hiloint2double(in ? __double2hiint(y) : static_cast<int>(0xc0e00000), __double2loint(y));
     const double moved = y + 6755399441055744.0;  // 1.5 2^52: the nearest whole number in the low bits
     const double f = y - (moved - 6755399441055744.0);
     const int n = static_cast<int>(__double_as_longlong(moved));
@@ -74,7 +89,8 @@ __device__ __forceinline__ double power2(double y, int e, const double *roots) {
     r = fma(r, f, 2.1173137155464774e-07);       // c^3 / 3!
     r = fma(r, f, 5.864904955056169e-05);       // c^2 / 2
     r = fma(r, f, 0.010830424696249145);       // c
-    return ldexp(fma(root, r * f, root), (n >> 6) + e);
+    const double v = fma(root, r * f, root);  // its exponent and the others' sum stay within those of normal numbers
+    return __hiloint2double(__double2hiint(v) + ((n >> 6) + e) * (1 << 20), __double2loint(v));
 }
 
 // log2 of a positive finite x, to 2^-50: x = 2^e m, and with c one of 64 values
@@ -103,37 +119,46 @@ struct Weights {
     double top;    // the largest value, or its log2 where the values are probabilities
     double rate;   // 64 log2(e) / T, or 64 / T of probabilities
     double unit;   // 2^s
-    double least;  // min-p, as a weight
     int log2_unit;
     bool plain;
+    bool even;     // the largest value is infinite, and only such values stay
     const double *roots;
     const double2 *logs;
 
-    // An infinite value is as far from the largest as that from itself.
-    __device__ __forceinline__ static float finite(float x) { return fminf(x, 3.402823466e38f); }
+    // Of those `in`; of the others something that no whole number is left of.
     template <int N>
-    __device__ __forceinline__ void of(const float (&x)[N], double (&v)[N]) const {
-        if (PROBS && plain) {
+    __device__ __forceinline__ void of(const float (&x)[N], const bool (&in)[N], double (&v)[N]) const {
+        if (even) {
 #pragma unroll
-            for (int c = 0; c < N; ++c) v[c] = static_cast<double>(x[c]) * unit;
+            for (int c = 0; c < N; ++c) v[c] = in[c] ? unit : 0.0;
+        } else if (PROBS && plain) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) v[c] = static_cast<double>(in[c] ? x[c] : 0.0f) * unit;
         } else {
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                const double far = (PROBS ? log2_of(finite(x[c]), logs) : static_cast<double>(finite(x[c]))) - top;
-                v[c] = power2(far * rate, log2_unit, roots);
+                const double far = (PROBS ? log2_of(x[c], logs) : static_cast<double>(x[c])) - top;
+                v[c] = power2(far * rate, in[c], log2_unit, roots);
             }
         }
     }
     __device__ __forceinline__ double of(float x) const {
         const float y[1] = {x};
+        const bool in[1] = {true};
         double v[1];
-        of(y, v);
+        of(y, in, v);
         return v[0];
     }
     // To the nearest whole number: w < 2^52, so the sum's low bits are it.
     __device__ __forceinline__ static uint64_t whole(double w) {
         return static_cast<uint64_t>(__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ll);
     }
+};
+
+// What a row asks for; read before the row, since each is a wait for memory of its own.
+struct Wish {
+    float u, t, p, min_p;
+    int k;
 };
 
 struct Shared {
@@ -144,8 +169,8 @@ struct Shared {
     uint64_t weight[kList];
     uint64_t part[kWaves];
     uint32_t part32[kWaves];
-    uint64_t before, cut;
-    uint32_t bin, listed, kept;
+    uint64_t before, cut, total;
+    uint32_t bin, listed, kept, key;
     int index;
 };
 
@@ -182,23 +207,29 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t v, int lane) {
     return v + (row == 0 ? 0 : row == 1 ? r0 : row == 2 ? r1 : r2);
 }
 
+// What the waves before this one have in sh.part, and what all have.
+__device__ __forceinline__ uint64_t before_wave(const Shared &sh, int wave, int lane, uint64_t &all) {
+    static_assert(kWaves == 16, "one row of 16 lanes scans them");
+    uint64_t v = sh.part[lane & 15];
+    v += dpp_u64<0x111>(v);  // row_shr:1
+    v += dpp_u64<0x112>(v);  // row_shr:2
+    v += dpp_u64<0x114>(v);  // row_shr:4
+    v += dpp_u64<0x118>(v);  // row_shr:8
+    all = readlane_u64(v, 15);
+    return wave == 0 ? 0 : readlane_u64(v, wave - 1);
+}
+
 // The sum of sh.mass; with hit(before, own) true for one entry, its number and
 // what lies before it in sh.bin and sh.before.
 template <typename Goal, typename Hit>
 __device__ __forceinline__ uint64_t scan_bins(Shared &sh, Goal goal_of, Hit hit) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint64_t a = sh.mass[2 * threadIdx.x], b = sh.mass[2 * threadIdx.x + 1];
     const uint64_t incl = wave_scan64(a + b, lane);
     if (lane == 63) sh.part[wave] = incl;
     __syncthreads();
-    uint64_t before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const uint64_t v = sh.part[w];
-        before += w < wave ? v : 0;
-        total += v;
-    }
-    before += incl - a - b;
+    uint64_t total;
+    const uint64_t before = before_wave(sh, wave, lane, total) + incl - a - b;
     const auto goal = goal_of(total);
     if (hit(before, a, goal)) sh.bin = 2 * threadIdx.x, sh.before = before;
     if (hit(before + a, b, goal)) sh.bin = 2 * threadIdx.x + 1, sh.before = before + a;
@@ -206,7 +237,7 @@ __device__ __forceinline__ uint64_t scan_bins(Shared &sh, Goal goal_of, Hit hit)
     return total;
 }
 
-constexpr int kPieceLog2 = 9;  // elements of a row's pieces (more where a row would have over kBins of them)
+constexpr int kUnit = 512;  // places that a wave reads at a time
 
 // A row of scores: in LDS from the first reading on (HELD), or in memory.  Its
 // places start at the 4-element boundary in memory at or before the first
@@ -217,7 +248,19 @@ struct Row {
     const char *row;  // place 0
     char *held;
     int lead, end;  // the elements' places
-    int pieces, piece_log2;
+    // Units of kUnit places; a wave has `each` of them, one after another, in `per` pieces of 2^group units (the last one
+    // may be shorter): what the row's weights are summed by.
+    int each, per, group;
+
+    __device__ __forceinline__ int pieces() const { return kWaves * per; }
+    __device__ __forceinline__ int units() const { return (end + kUnit - 1) / kUnit; }
+    __device__ __forceinline__ int piece_of(int place) const {
+        const int unit = place / kUnit, of = unit / each;
+        return of * per + ((unit - of * each) >> group);
+    }
+    __device__ __forceinline__ int first_unit(int piece) const {
+        return piece / per * each + ((piece % per) << group);
+    }
 
     __device__ __forceinline__ static void widen4(const void *p, float (&x)[4]) {
         if constexpr (DT == KNN_F32) {
@@ -234,37 +277,40 @@ struct Row {
     __device__ __forceinline__ float at(int i) const {
         return i >= lead && i < end ? present(element<DT>(row, i), PROBS) : -INFINITY;
     }
-    // Places i .. i + 3 (i a multiple of four).
-    __device__ __forceinline__ void read4(int i, float (&x)[4]) const {
-        if (i >= lead && i + 3 < end) {
-            widen4(row + static_cast<int64_t>(i) * SIZE, x);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = present(x[c], PROBS);
+    // Places i + 4 lane .. i + 4 lane + 3 (i the wave's, a multiple of 256).  Whether all of the wave's are in the row is
+    // one scalar branch, so that no load is waited for before it is used.
+    __device__ __forceinline__ void read4(int i, int lane, float (&x)[4]) const {
+        if (i >= lead && i + 255 < end) {
+            widen4(row + static_cast<int64_t>(i + 4 * lane) * SIZE, x);
         } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) x[c] = at(i + c);
+            for (int c = 0; c < 4; ++c) x[c] = at(i + 4 * lane + c);
         }
     }
-    __device__ __forceinline__ void load4(int i, float (&x)[4]) const {
-        if constexpr (HELD) widen4(held + i * SIZE, x); else read4(i, x);
+    __device__ __forceinline__ void load4(int i, int lane, float (&x)[4]) const {
+        if constexpr (HELD) widen4(held + (i + 4 * lane) * SIZE, x); else read4(i, lane, x);
     }
-    __device__ __forceinline__ void load8(int i, float (&x)[8]) const {
+    __device__ __forceinline__ void load8(int i, int lane, float (&x)[8]) const {
         float u[4], v[4];
-        load4(i, u);
-        load4(i + 256, v);
+        load4(i, lane, u);
+        load4(i + 256, lane, v);
 #pragma unroll
         for (int c = 0; c < 4; ++c) x[c] = u[c], x[c + 4] = v[c];
     }
     // f(place, value) over this wave's pieces, one place a lane: where there is little code to spare.
     template <typename F, typename Done>
     __device__ __forceinline__ void slow_pass(int wave, int lane, F f, Done done) const {
-        const int each = (pieces + kWaves - 1) / kWaves;
-        const int last = min(pieces, (wave + 1) * each);
-        for (int piece = wave * each; piece < last; ++piece) {
+        const int stop = min(units(), (wave + 1) * each);
+        for (int unit = wave * each; unit < stop; ++unit) {
 #pragma unroll 1
-            for (int i = piece << piece_log2; i < (piece + 1) << piece_log2; i += kWave) f(i + lane, at(i + lane));
-            done(piece);
+            for (int i = unit * kUnit; i < (unit + 1) * kUnit; i += kWave) f(i + lane, at(i + lane));
+            ended(wave, unit, stop, done);
         }
+    }
+    template <typename Done>
+    __device__ __forceinline__ void ended(int wave, int unit, int stop, Done done) const {
+        const int n = unit - wave * each;
+        if (((n + 1) & ((1 << group) - 1)) == 0 || unit + 1 == stop) done(wave * per + (n >> group));
     }
     __device__ __forceinline__ void keep4(int i, const float (&x)[4]) const {
         if constexpr (DT == KNN_F32) {
@@ -282,18 +328,19 @@ struct Row {
     // places a lane; done(piece) after each piece.  FIRST: the first reading.
     template <bool FIRST = false, typename F, typename Done>
     __device__ __forceinline__ void pass(int wave, int lane, F f, Done done) const {
-        const int each = (pieces + kWaves - 1) / kWaves;
-        const int last = min(pieces, (wave + 1) * each);
+        const int first = wave * each, last = min(units(), first + each);
         if constexpr (FIRST) {  // eight loads a lane in flight
-            const int stop = last << piece_log2;
-            for (int i = (wave * each) << piece_log2; i < stop; i += 2048) {
+            const int stop = last * kUnit;
+            for (int i = first * kUnit; i < stop; i += 2048) {
                 float x[8][4];
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (i + 256 * j < stop) read4(i + 256 * j + 4 * lane, x[j]);
+                    if (i + 256 * j < stop) read4(i + 256 * j, lane, x[j]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     if (i + 256 * j < stop) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) x[j][c] = present(x[j][c], PROBS);
                         if constexpr (HELD) keep4(i + 256 * j + 4 * lane, x[j]);
                         f(i + 256 * j + 4 * lane, x[j]);
                     }
@@ -301,15 +348,17 @@ struct Row {
             }
         } else {
             // x[c] is at place i + 4 lane + c + (c < 4 ? 0 : 252); the next eight are on their way meanwhile
-            const int stop = last << piece_log2, mask = (1 << piece_log2) - 1;
-            int i = (wave * each) << piece_log2;
-            if (i >= stop) return;
+            if (first >= last) return;
             float x[8], next[8];
-            load8(i + 4 * lane, x);
-            for (; i < stop; i += 512) {
-                if (i + 512 < stop) load8(i + 512 + 4 * lane, next);
-                f(i + 4 * lane, x);
-                if (((i + 512) & mask) == 0) done(i >> piece_log2);
+            load8(first * kUnit, lane, x);
+            for (int unit = first; unit < last; ++unit) {
+                if (unit + 1 < last) load8((unit + 1) * kUnit, lane, next);
+                if constexpr (!HELD) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) x[c] = present(x[c], PROBS);
+                }
+                f(unit * kUnit + 4 * lane, x);
+                ended(wave, unit, last, done);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) x[c] = next[c];
             }
@@ -320,55 +369,88 @@ struct Row {
 __device__ __forceinline__ int place(int i, int c) { return i + c + (c < 4 ? 0 : 252); }
 
 // The filters and the draw of a row whose largest present value is `top` and
-// smallest `low`, at a temperature t > 0 and top-p p > 0.
+// smallest `low`, `mine` the largest that this thread read, at a temperature
+// and a top-p above 0.
 template <bool PROBS, typename R>
-__device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &sh, int64_t r, float top, float low, float t,
-                                     float p, int log2_unit) {
+__device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &sh, int64_t r, float top, float low, float mine,
+                                     const Wish &wish, int log2_unit) {
+    const float t = wish.t, p = wish.p, min_p = wish.min_p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int V = rw.end - rw.lead, pieces = rw.pieces, piece_log2 = rw.piece_log2;
+    const int V = rw.end - rw.lead;
     auto pass = [&](auto f, auto done) { rw.pass(wave, lane, f, done); };
     auto nothing = [](int) {};
     Weights<PROBS> w;
-    w.plain = PROBS && t == 1.0f && top < INFINITY;
+    w.plain = PROBS && t == 1.0f;
+    w.even = top == INFINITY;
     w.roots = sh.roots;
     w.logs = sh.logs;
-    w.top = PROBS ? log2_of(w.finite(top), sh.logs) : static_cast<double>(w.finite(top));
+    w.top = PROBS ? log2_of(top, sh.logs) : static_cast<double>(top);
     w.rate = (PROBS ? 64.0 : 92.332482616893656874) / static_cast<double>(t);
-    w.log2_unit = log2_unit - (w.plain ? ilogb(static_cast<double>(top)) + 1 : 0);
+    w.log2_unit = log2_unit - (w.plain && !w.even ? ilogb(static_cast<double>(top)) + 1 : 0);
     w.unit = ldexp(1.0, w.log2_unit);
-    const float min_p = a.min_p != nullptr ? a.min_p[r] : 0.0f;
-    w.least = (min_p > 0.0f ? fmin(static_cast<double>(min_p), 1.0) : 0.0) *
-              (w.plain ? static_cast<double>(top) * w.unit : w.unit);
+    // What min-p leaves is not below `least`, the first value of enough weight: between one a thousandth of an octave
+    // under it (log2f is right to 2^-20) and the largest, in 64ths.
+    float least = -INFINITY;
+    if (min_p > 0.0f && !w.even) {
+        const double enough = w.of(top) * fmin(static_cast<double>(min_p), 1.0);
+        const float far = t * (log2f(fminf(min_p, 1.0f)) - 0.001f);
+        const float under = PROBS ? top * exp2f(far) * 0.999f
+                                  : __double2float_rd(static_cast<double>(top) + 0.69314718 * static_cast<double>(far));
+        uint32_t lo = key_of(under), hi = key_of(top);
+        while (hi - lo > 1) {
+            const uint32_t each = (hi - lo) / 64 + 1, key = min(lo + (lane + 1) * each, hi);
+            const uint64_t above = __ballot(key == hi || w.of(value_of(key)) >= enough);
+            const uint32_t n = __ffsll(static_cast<unsigned long long>(above)) - 1;
+            hi = min(hi, lo + (n + 1) * each);
+            lo += n * each;
+        }
+        least = value_of(hi);
+    }
 
     // Bins that follow the order; what is past the last one's start is in it.
     // Logits: steps of the distance from the largest, over 32 T or the row's
     // range.  Probabilities: steps of the bits, which grow like a logarithm.
-    const float span = fminf(top - low, 32.0f * t);
-    const float step = span > 0.0f ? kBins / span : 0.0f;
+    // (Places do not depend on T: for them it is at least 1.)
     const uint32_t top_bits = __float_as_uint(top);
+    float step = 0.0f;
     int shift = 0;
-    if (PROBS) {
-        const float octaves = fminf(46.0f * t, 255.0f);  // 2^-46 = e^-32
-        uint32_t bits = min(top_bits - __float_as_uint(fminf(low, top)), static_cast<uint32_t>(octaves * 8388608.0f));
-        while (bits >> shift >= kBins) ++shift;
-    }
-    auto bin_of = [&](float x) -> uint32_t {
-        if (PROBS) return min((top_bits - __float_as_uint(x)) >> shift, static_cast<uint32_t>(kBins - 1));
-        return static_cast<uint32_t>(fminf((top - x) * step, static_cast<float>(kBins - 1)));
+    auto bins_for = [&](float warm) {
+        const float span = fminf(top - low, 32.0f * warm);
+        step = span > 0.0f ? kBins / span : 0.0f;
+        shift = 0;
+        if (PROBS) {
+            const float octaves = fminf(46.0f * warm, 255.0f);  // 2^-46 = e^-32
+            uint32_t bits = min(top_bits - __float_as_uint(fminf(low, top)), static_cast<uint32_t>(octaves * 8388608.0f));
+            while (bits >> shift >= kBins) ++shift;
+        }
     };
+    auto spot = [&](float x) {  // the bin, and of logits where in it
+        if constexpr (PROBS) return min((top_bits - __float_as_uint(x)) >> shift, static_cast<uint32_t>(kBins - 1));
+        else return fminf((top - x) * step, static_cast<float>(kBins - 1));
+    };
+    auto bin_of = [&](float x) { return static_cast<uint32_t>(spot(x)); };
 
     // What stays: x above `cut_x`, or equal to it with an index up to `cut_i`.
     float cut_x = top == INFINITY ? 3.402823466e38f : -INFINITY;
     int cut_i = -1;
     auto stays = [&](int i, float x) { return x > cut_x || (x == cut_x && i <= cut_i); };
+    auto stay8 = [&](int i, const float (&x)[8], bool (&in)[8]) {
+        bool equal = false;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) in[c] = x[c] > cut_x, equal |= x[c] == cut_x;
+        if (__any(equal)) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) in[c] = stays(place(i, c), x[c]);
+        }
+    };
     auto clear = [&]() {
         __syncthreads();
         sh.mass[2 * threadIdx.x] = 0;
         sh.mass[2 * threadIdx.x + 1] = 0;
-        if (threadIdx.x == 0) sh.listed = 0, sh.cut = ~0ull;
+        if (threadIdx.x == 0) sh.listed = 0, sh.cut = ~0ull, sh.total = 0, sh.key = ~0u;
         __syncthreads();
     };
-    uint32_t kept = 0;
+    uint32_t kept = 0;  // by this wave
     bool summed = false;
     uint64_t run = 0;  // this wave's weights of the piece at hand
     auto end_piece = [&](int piece) {
@@ -383,36 +465,139 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
         for (int c = 0; c < 8; ++c) any |= in[c];
         if (!__any(any)) return;
         double v[8];
-        w.of(x, v);
+        w.of(x, in, v);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) f(c, v[c]);
+        for (int c = 0; c < 8; ++c) f(c, Weights<PROBS>::whole(v[c]));
     };
     auto add = [&](const float (&x)[8], const bool (&in)[8]) {
-        weigh(x, in, [&](int c, double v) {
-            const bool keep = in[c] && v >= w.least;
-            run += keep ? Weights<PROBS>::whole(v) : 0;
-            kept += keep ? 1u : 0u;
-        });
+        bool keep[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            keep[c] = in[c] && x[c] >= least;
+            kept += static_cast<uint32_t>(__popcll(__ballot(keep[c])));
+        }
+        weigh(x, keep, [&](int, uint64_t v) { run += v; });
     };
     auto count = [&](uint64_t v, uint32_t bin) {
         atomicAdd(reinterpret_cast<unsigned long long *>(&sh.mass[bin]), static_cast<unsigned long long>(v));
     };
+    auto crosses = [](uint64_t at, uint64_t v, double to) {
+        return static_cast<double>(at) < to && static_cast<double>(at + v) >= to;
+    };
+    auto list = [&](int i, float x) {
+        const uint32_t at = atomicAdd(&sh.listed, 1u);
+        if (at < kList) sh.list[at] = static_cast<uint64_t>(key_of(x)) << 32 | ~static_cast<uint32_t>(i);
+    };
+    auto weigh_list = [&](int n) {
+        if (static_cast<int>(threadIdx.x) < n)
+            sh.weight[threadIdx.x] =
+                Weights<PROBS>::whole(w.of(value_of(static_cast<uint32_t>(sh.list[threadIdx.x] >> 32))));
+        __syncthreads();
+    };
+    // The last of the n listed, `from` and earlier in the order, before which less than the goal lies, in sh.cut: eight
+    // lanes an entry, each over an eighth of the others.  `take`: their weights are the row's.
+    auto cut_list = [&](int n, uint64_t from, uint64_t before, double goal, bool by_weight, bool take) {
+        for (int first = 0; first < n; first += kThreads / 8) {
+            const int me = first + static_cast<int>(threadIdx.x >> 3);
+            const uint64_t own = me < n ? sh.list[me] : ~0ull;
+            uint64_t ahead = 0;
+            for (int j = threadIdx.x & 7; j < n; j += 8) ahead += sh.list[j] > own ? (by_weight ? sh.weight[j] : 1) : 0;
+            ahead += dpp_u64<0xB1>(ahead);
+            ahead += dpp_u64<0x4E>(ahead);
+            ahead += dpp_u64<0x141>(ahead);
+            const bool ours = me < n && (threadIdx.x & 7) == 0 && own >= from && static_cast<double>(before + ahead) < goal;
+            if (ours) atomicMin(reinterpret_cast<unsigned long long *>(&sh.cut), static_cast<unsigned long long>(own));
+            const bool keep = ours && take && value_of(static_cast<uint32_t>(own >> 32)) >= least;
+            if (keep) count(sh.weight[me], rw.piece_of(static_cast<int>(~static_cast<uint32_t>(own))));
+            kept += static_cast<uint32_t>(__popcll(__ballot(keep)));
+        }
+        __syncthreads();
+    };
+    // Lists what is not below `from`; returns how many they are.
+    auto list_from = [&](float from) {
+        pass(
+            [&](int i, const float (&x)[8]) {
+                bool in[8], any = false;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) any |= in[c] = x[c] >= from;
+                if (!__any(any)) return;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (in[c]) list(place(i, c), x[c]);
+            },
+            nothing);
+        __syncthreads();
+        return static_cast<int>(sh.listed);
+    };
     // The cuts: by count (top-k), then by weight (top-p).
-    const int k = a.top_k != nullptr ? a.top_k[r] : 0;
-    const bool stages[2] = {k > 0 && k < V, p < 1.0f};
+    const int k = wish.k;
+    bool stages[2] = {k > 0 && k < V, p < 1.0f};
+
+    // Min-p alone: where few are left, only they are weighed.  (A pass that lists too many is lost: 6 us of 50,000 float
+    // elements.  400 threads out of 1024 have an element of 512 that lie anywhere.)
+    if (least > -INFINITY && !stages[0] && !stages[1] && __syncthreads_count(mine >= least) <= 384) {
+        clear();
+        const int n = list_from(least);
+        if (n <= kList) {
+            weigh_list(n);
+            cut_list(n, 0, 0, INFINITY, false, true);
+            cut_x = value_of(static_cast<uint32_t>(sh.cut >> 32));
+            cut_i = static_cast<int>(~static_cast<uint32_t>(sh.cut));
+            summed = true;
+        }
+    }
+
+    // A small k: what is not below the k-th largest of the threads' own largest
+    // values is k elements or more, and in an order that is not of the row's
+    // making few more.  All of them listed, both cuts are among them, and
+    // nothing else of the row is weighed.
+    if (stages[0] && k <= kFew) {
+        bins_for(fmaxf(t, 1.0f));
+        clear();
+        const bool in = mine > cut_x;
+        if (in) count(1, bin_of(mine));
+        __syncthreads();
+        auto goal_of = [&](uint64_t) { return static_cast<double>(k); };
+        if (scan_bins(sh, goal_of, crosses) >= static_cast<uint64_t>(k)) {
+            const uint32_t bin = sh.bin;
+            clear();
+            if (in && bin_of(mine) <= bin) atomicMin(&sh.key, key_of(mine));
+            __syncthreads();
+            const int n = list_from(value_of(sh.key));
+            if (n <= kList) {
+                weigh_list(n);
+                cut_list(n, 0, 0, k, false, !stages[1]);
+                if (stages[1]) {
+                    const uint64_t from = sh.cut;
+                    const bool stay = static_cast<int>(threadIdx.x) < n && sh.list[threadIdx.x] >= from;
+                    const uint64_t sum = wave_sum64(stay ? sh.weight[threadIdx.x] : 0);
+                    if (lane == 0 && sum != 0)
+                        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.total), static_cast<unsigned long long>(sum));
+                    __syncthreads();
+                    if (threadIdx.x == 0) sh.cut = ~0ull;
+                    __syncthreads();
+                    cut_list(n, from, 0, p * static_cast<double>(sh.total), true, true);
+                }
+                cut_x = value_of(static_cast<uint32_t>(sh.cut >> 32));
+                cut_i = static_cast<int>(~static_cast<uint32_t>(sh.cut));
+                summed = true;
+                stages[0] = stages[1] = false;
+            }
+        }
+    }
 #pragma unroll 1
     for (int stage = 0; stage < 2; ++stage) {
         if (stage == 0 ? !stages[0] : !stages[1]) continue;
         const bool by_weight = stage == 1, last = by_weight || !stages[1];  // last: sums the row's pieces too
+        bins_for(by_weight ? t : fmaxf(t, 1.0f));
         clear();
         pass(
             [&](int i, const float (&x)[8]) {
                 bool in[8];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) in[c] = stays(place(i, c), x[c]);
+                stay8(i, x, in);
                 if (by_weight) {
-                    weigh(x, in, [&](int c, double v) {
-                        if (in[c]) count(Weights<PROBS>::whole(v), bin_of(x[c]));
+                    weigh(x, in, [&](int c, uint64_t v) {
+                        if (v != 0) count(v, bin_of(x[c]));
                     });
                 } else {
 #pragma unroll
@@ -424,27 +609,28 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
         __syncthreads();
         const double share = p;
         auto goal_of = [&](uint64_t all) { return by_weight ? share * static_cast<double>(all) : static_cast<double>(k); };
-        auto crosses = [](uint64_t at, uint64_t v, double to) {
-            return static_cast<double>(at) < to && static_cast<double>(at + v) >= to;
-        };
         const uint64_t all = scan_bins(sh, goal_of, crosses);
         if (!by_weight && static_cast<uint64_t>(k) >= all) continue;  // all that is present stays
         const double goal = goal_of(all);
         const uint32_t bin = sh.bin;
         const uint64_t before = sh.before;
+        const auto bin_first = static_cast<decltype(spot(0.0f))>(bin), bin_end = bin_first + 1;
+        clear();  // for the pieces' weights
         pass(
             [&](int i, const float (&x)[8]) {
-                bool under[8];
+                bool in[8], under[8], at[8], any = false;
+                stay8(i, x, in);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
-                    const bool in = stays(place(i, c), x[c]);
-                    const uint32_t b = bin_of(x[c]);
-                    if (in && b == bin) {
-                        const uint32_t at = atomicAdd(&sh.listed, 1u);
-                        if (at < kList)
-                            sh.list[at] = static_cast<uint64_t>(key_of(x[c])) << 32 | ~static_cast<uint32_t>(place(i, c));
-                    }
-                    under[c] = in && b < bin;
+                    const auto b = spot(x[c]);
+                    under[c] = in[c] && b < bin_first;
+                    at[c] = in[c] && b >= bin_first && b < bin_end;
+                    any |= at[c];
+                }
+                if (__any(any)) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        if (at[c]) list(place(i, c), x[c]);
                 }
                 if (last) add(x, under);
             },
@@ -454,31 +640,8 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
         __syncthreads();
         const int n = static_cast<int>(sh.listed);
         if (n <= kList) {
-            if (static_cast<int>(threadIdx.x) < n) {
-                const double v = w.of(value_of(static_cast<uint32_t>(sh.list[threadIdx.x] >> 32)));
-                sh.weight[threadIdx.x] = Weights<PROBS>::whole(v);
-            }
-            __syncthreads();
-            // What lies before each entry: eight lanes an entry, each over an eighth of the others.
-            for (int first = 0; first < n; first += kThreads / 8) {
-                const int me = first + static_cast<int>(threadIdx.x >> 3);
-                const uint64_t mine = me < n ? sh.list[me] : ~0ull;
-                uint64_t ahead = 0;
-                for (int j = threadIdx.x & 7; j < n; j += 8)
-                    ahead += sh.list[j] > mine ? (by_weight ? sh.weight[j] : 1) : 0;
-                ahead += dpp_u64<0xB1>(ahead);
-                ahead += dpp_u64<0x4E>(ahead);
-                ahead += dpp_u64<0x141>(ahead);
-                if (me < n && (threadIdx.x & 7) == 0 && static_cast<double>(before + ahead) < goal) {
-                    atomicMin(reinterpret_cast<unsigned long long *>(&sh.cut), static_cast<unsigned long long>(mine));
-                    const double v = w.of(value_of(static_cast<uint32_t>(mine >> 32)));
-                    if (last && v >= w.least) {
-                        count(sh.weight[me], ~static_cast<uint32_t>(mine) >> piece_log2);
-                        ++kept;
-                    }
-                }
-            }
-            __syncthreads();
+            weigh_list(n);
+            cut_list(n, 0, before, goal, by_weight, last);
             cut_x = value_of(static_cast<uint32_t>(sh.cut >> 32));
             cut_i = static_cast<int>(~static_cast<uint32_t>(sh.cut));
             summed = last;
@@ -529,7 +692,7 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
         if (wave == 0) {
             uint64_t seen = sh.before;
             bool found = false;
-            for (int i = static_cast<int>(sh.bin) << piece_log2; !found; i += kWave) {
+            for (int i = rw.first_unit(static_cast<int>(sh.bin)) * kUnit; !found; i += kWave) {
                 const int at = i + lane;
                 const float x = rw.at(at);
                 const uint64_t eq = __ballot(x == x_at && stays(at, x));
@@ -548,65 +711,63 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
         pass(
             [&](int i, const float (&x)[8]) {
                 bool in[8];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) in[c] = stays(place(i, c), x[c]);
+                stay8(i, x, in);
                 add(x, in);
             },
             end_piece);
     } else {
         __syncthreads();
     }
-    kept = wave_sum32(kept);
     if (lane == 0) atomicAdd(&sh.kept, kept);
-    // Entries past the last piece hold no weight.
-    for (int i = pieces + threadIdx.x; i < kBins; i += kThreads) sh.mass[i] = 0;
     __syncthreads();
-    const float u = a.uniforms[r];
-    const double at = u > 0.0f ? fmin(static_cast<double>(u), 1.0) : 0.0;
+    const double at = wish.u > 0.0f ? fmin(static_cast<double>(wish.u), 1.0) : 0.0;
     auto aim = [&](uint64_t all) {  // the token is the first whose running weight exceeds it
         const uint64_t goal = static_cast<uint64_t>(at * static_cast<double>(all));
         return goal < all ? goal : all - 1;
     };
     const uint64_t total =
         scan_bins(sh, aim, [](uint64_t before, uint64_t v, uint64_t to) { return before <= to && to < before + v; });
-    if (wave != 0) return;
     const uint64_t goal = aim(total);
     uint64_t before = sh.before;
-    for (int i = static_cast<int>(sh.bin) << piece_log2;; i += 256) {
+    for (int i = rw.first_unit(static_cast<int>(sh.bin)) * kUnit; i < rw.end; i += kWaves * 256) {  // 256 places a wave
+        const int own = i + 256 * wave;
         float x[4];
-        rw.load4(i + 4 * lane, x);
         uint64_t q[4], sum = 0;
+        if (own < rw.end) {
+            rw.load4(own, lane, x);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const double v = stays(i + 4 * lane + c, x[c]) ? w.of(x[c]) : 0.0;
-            q[c] = v >= w.least ? Weights<PROBS>::whole(v) : 0;
-            sum += q[c];
+            for (int c = 0; c < 4; ++c) {
+                x[c] = present(x[c], PROBS);
+                const bool in = x[c] >= least && stays(own + 4 * lane + c, x[c]);
+                q[c] = in ? Weights<PROBS>::whole(w.of(x[c])) : 0;
+                sum += q[c];
+            }
         }
         const uint64_t incl = wave_scan64(sum, lane);
-        const uint64_t hit = __ballot(before + incl > goal);
-        if (hit != 0) {
-            if (lane == __ffsll(static_cast<unsigned long long>(hit)) - 1) {
-                uint64_t here = before + incl - sum;
-                int c = 0;
+        __syncthreads();
+        if (lane == 63) sh.part[wave] = incl;
+        __syncthreads();
+        uint64_t all;
+        uint64_t here = before + before_wave(sh, wave, lane, all) + incl - sum;
+        if (here <= goal && goal < here + sum) {
+            int c = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    here += q[j];
-                    c += here <= goal ? 1 : 0;
-                }
-                const float v = c == 0 ? x[0] : c == 1 ? x[1] : c == 2 ? x[2] : x[3];
-                a.token[r] = i + 4 * lane + c - rw.lead;
-                if (a.prob != nullptr) a.prob[r] = static_cast<float>(w.of(v) / static_cast<double>(total));
-                if (a.kept != nullptr) a.kept[r] = static_cast<int32_t>(sh.kept);
+            for (int j = 0; j < 4; ++j) {
+                here += q[j];
+                c += here <= goal ? 1 : 0;
             }
-            return;
+            const float v = c == 0 ? x[0] : c == 1 ? x[1] : c == 2 ? x[2] : x[3];
+            a.token[r] = own + 4 * lane + c - rw.lead;
+            if (a.prob != nullptr) a.prob[r] = static_cast<float>(w.of(v) / static_cast<double>(total));
+            if (a.kept != nullptr) a.kept[r] = static_cast<int32_t>(sh.kept);
         }
-        before += __shfl(incl, 63);
-        if (i + 256 >= rw.end) return;  // not reached: the piece holds the goal
+        before += all;
+        if (before > goal) return;
     }
 }
 
 template <knn_dtype DT, bool HELD, bool PROBS>
-__global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit, int piece_log2) {
+__global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit, int group) {
     __shared__ Shared sh;
     extern __shared__ __align__(16) char held[];
     const int64_t r = blockIdx.x;
@@ -614,9 +775,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit
     using R = Row<DT, HELD, PROBS>;
     const char *first_of_row = static_cast<const char *>(a.scores) + r * a.stride * R::SIZE;
     const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(first_of_row) % (4 * R::SIZE)) / R::SIZE;
-    const R rw{first_of_row - lead * R::SIZE, held, lead, lead + a.V, (lead + a.V + (1 << piece_log2) - 1) >> piece_log2,
-               piece_log2};
+    const int each = ((lead + a.V + kUnit - 1) / kUnit + kWaves - 1) / kWaves;
+    const R rw{first_of_row - lead * R::SIZE, held, lead, lead + a.V, each, ((each - 1) >> group) + 1, group};
 
+    Wish wish;
+    wish.u = a.uniforms[r];
+    wish.t = a.temperature != nullptr ? a.temperature[r] : 1.0f;
+    wish.p = a.top_p != nullptr ? a.top_p[r] : 1.0f;
+    wish.min_p = a.min_p != nullptr ? a.min_p[r] : 0.0f;
+    wish.k = a.top_k != nullptr ? a.top_k[r] : 0;
     if (threadIdx.x < 64) {
         sh.roots[threadIdx.x] = exp2(threadIdx.x * (1.0 / 64.0));
         if constexpr (PROBS) {
@@ -632,16 +799,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit
             for (int c = 0; c < 4; ++c) top = fmaxf(top, x[c]), low = fminf(low, x[c] > -INFINITY ? x[c] : INFINITY);
         },
         [](int) {});
+    const float mine = top;
     top = wave_allmax(top);
     low = wave_allmin(low);
     if (lane == 0) sh.part32[wave] = __float_as_uint(top), sh.part[wave] = __float_as_uint(low);
     if (threadIdx.x == 0) sh.kept = 0, sh.index = 0x7fffffff;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        top = fmaxf(top, __uint_as_float(sh.part32[w]));
-        low = fminf(low, __uint_as_float(static_cast<uint32_t>(sh.part[w])));
-    }
+    top = wave_allmax(__uint_as_float(sh.part32[lane & 15]));
+    low = wave_allmin(__uint_as_float(static_cast<uint32_t>(sh.part[lane & 15])));
     if (!(top > -INFINITY)) {
         if (threadIdx.x == 0) {
             a.token[r] = -1;
@@ -650,9 +815,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit
         }
         return;
     }
-    const float t = a.temperature != nullptr ? a.temperature[r] : 1.0f;
-    const float p = a.top_p != nullptr ? a.top_p[r] : 1.0f;
-    if (!(t > 0.0f) || p <= 0.0f) {  // the first element of the order
+    if (!(wish.t > 0.0f) || wish.p <= 0.0f) {  // the first element of the order
         int first = 0x7fffffff;
         rw.pass(
             wave, lane,
@@ -671,16 +834,16 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit
         }
         return;
     }
-    draw<PROBS>(a, rw, sh, r, top, low, t, p, log2_unit);
+    draw<PROBS>(a, rw, sh, r, top, low, mine, wish, log2_unit);
 }
 
 template <knn_dtype DT, bool PROBS>
-void launch(const SampleArgs &a, int log2_unit, int piece_log2, hipStream_t stream) {
+void launch(const SampleArgs &a, int log2_unit, int group, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(a.rows));
     // Whole pieces, with up to three places before the first element.
     const size_t bytes = ((static_cast<size_t>(a.V) + 3 + 511) & ~size_t{511}) * (DT == KNN_F32 ? 4 : 2);
-    if (bytes <= kHeldBytes) k_sample<DT, true, PROBS><<<grid, kThreads, bytes, stream>>>(a, log2_unit, piece_log2);
-    else k_sample<DT, false, PROBS><<<grid, kThreads, 0, stream>>>(a, log2_unit, piece_log2);
+    if (bytes <= kHeldBytes) k_sample<DT, true, PROBS><<<grid, kThreads, bytes, stream>>>(a, log2_unit, group);
+    else k_sample<DT, false, PROBS><<<grid, kThreads, 0, stream>>>(a, log2_unit, group);
 }
 
 template <knn_dtype DT>
@@ -688,9 +851,9 @@ hipError_t launch(const SampleArgs &a, hipStream_t stream) {
     int bits = 0;
     while ((int64_t{1} << bits) < a.V + 3) ++bits;
     const int unit = bits < 11 ? 51 : 62 - bits;  // 2^51 is what a sum with 2^52 can round to a whole number
-    const int piece = bits - 11 > kPieceLog2 ? bits - 11 : kPieceLog2;  // at most kBins pieces
-    if (a.probabilities) launch<DT, true>(a, unit, piece, stream);
-    else launch<DT, false>(a, unit, piece, stream);
+    const int group = bits > 22 ? bits - 20 : 2;  // at most kBins pieces
+    if (a.probabilities) launch<DT, true>(a, unit, group, stream);
+    else launch<DT, false>(a, unit, group, stream);
     return hipGetLastError();
 }
 

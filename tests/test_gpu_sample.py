@@ -222,3 +222,41 @@ def test_refusals():
                 dict(scores=x.double())):
         with pytest.raises((ValueError, TypeError)):
             knn.sample(**dict(dict(scores=x, uniforms=u), **bad))
+
+
+def test_small_k_and_min_p_of_ordered_rows():
+    V = 20000
+    down = -torch.arange(V).float() * 0.001
+    x = torch.stack([down, down.flip(0), (torch.arange(V) % 7).float(), torch.full((V,), -1e30), down, down]).cuda()
+    x[3, ::97] = 0.5 + torch.arange(len(range(0, V, 97))).float().cuda() * 0.01  # few that are not masked
+    x[4, 1:] = float("-inf")
+    x[5, 300:] = float("nan")
+    u = [0.0, 0.3, 0.5, 0.77, 0.9, 0.999]
+    for k in (1, 2, 255, 256, 257, 1023):
+        check(x, u, top_k=[k] * 6)
+        check(x, u, temperature=[1e-3, 0.1, 1.0, 2.0, 50.0, 1e4], top_k=[k] * 6, top_p=[0.9, 0.5, 0.99, 0.8, 0.3, 0.7])
+        check(x, u, top_k=[k] * 6, top_p=[0.9] * 6, min_p=[0.5, 0.1, 0.9, 0.97, 0.01, 1.0])
+    check(x, u, min_p=[0.9, 0.5, 1.0, 0.97, 0.01, 0.999])
+    check(x, u, temperature=[1e-3, 0.1, 1.0, 2.0, 50.0, 1e4], min_p=[0.9, 0.5, 1.0, 0.97, 0.01, 0.999])
+
+
+def test_infinite_elements_under_every_filter():
+    x = torch.randn(4, 5000, generator=torch.Generator().manual_seed(9)).cuda()
+    x[0, 77] = x[1, 5] = x[1, 4999] = float("inf")
+    x[2, :400] = float("inf")
+    x[3, 10:] = float("-inf")
+    u = [0.5, 0.6, 0.4, 0.9]
+    for form in (False, True):
+        for f in ({}, dict(top_k=[3] * 4), dict(top_p=[0.6] * 4), dict(min_p=[0.2] * 4),
+                  dict(top_k=[300] * 4, top_p=[0.7] * 4, min_p=[0.1] * 4, temperature=[0.5] * 4)):
+            check(x, u, form, **f)
+
+
+def test_a_row_of_millions():
+    V = (1 << 22) + 4321
+    # Weights in units of 2^-39 of the largest, their sum above 1000 of it, and errors of either sign: 2^11 2^-40 / 1000
+    # = 2e-12 is what to expect of the sum, far within check()'s 1e-9.
+    x = torch.randn(2, V, generator=torch.Generator().manual_seed(11)).mul_(2).half().cuda()
+    check(x, [0.3, 0.98], temperature=[0.9, 1.2])
+    check(x, [0.3, 0.98], top_p=[0.7, 0.4], top_k=[0, 100000])
+    check(x, [0.7, 0.1], min_p=[0.3, 0.001], top_k=[40, 0])
