@@ -25,7 +25,7 @@ namespace knnlm {
 
 namespace {
 
-constexpr float kFloor = -1.0e30f;  // reference before the first key
+constexpr float kFloor = -3.0e38f;  // reference before the first key
 constexpr float kSlack = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -115,6 +115,9 @@ __device__ __forceinline__ uint32_t seen(const AttendArgs &a, const Tile &t, int
     return (first_bits(-draft) | bits) & first_bits(limit - at);
 }
 
+// From q.k (with the scale's sign) to the exponent of two.
+__device__ __forceinline__ float c2_of(const AttendArgs &a) { return a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e; }
+
 // The columns of a wave: NT x 16 (row, query head) pairs of one key head.
 template <knn_dtype DT, int D, int NT>
 struct Columns {
@@ -122,13 +125,14 @@ struct Columns {
     u32x4_t q[NT][KK];  // right operand of the scores: lane = (column, 8 elements a quad)
     f32x4_t o[NT][DB];  // lane = (column, 4 elements a quad)
     f32x4_t sum[NT];    // the same sum four times
-    float m[NT];        // reference, of the scores times log2(e)
+    float m[NT];        // reference: of q.k, whatever the scale, so that a key at it weighs 1 however large it is
     int row_of[NT];     // row within the sequence
-    float c2;           // scale log2(e), not negative: its sign is in q
+    float c2, slack;    // scale log2(e), positive: its sign is in q; kSlack over it
 
     __device__ __forceinline__ void load(const AttendArgs &a, const Tile &t, int h, int g, int c0, int cols, int col,
                                          int quad) {
-        c2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
+        c2 = c2_of(a);
+        slack = kSlack / c2;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int c = c0 + 16 * n + col;
@@ -187,12 +191,11 @@ struct Columns {
             for (int u = 0; u < 2 * U; ++u)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top = __builtin_amdgcn_fmed3f(top, x[u][n][j], INFINITY);
-            top *= c2;
-            if (__any(top > m[n] + kSlack)) {
+            if (__any(top > m[n] + slack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 const float to = fmaxf(m[n], top);
-                const float by = exp2f(m[n] - to);
+                const float by = exp2f((m[n] - to) * c2);
                 m[n] = to;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sum[n][j] *= by;
@@ -205,7 +208,7 @@ struct Columns {
             for (int u = 0; u < U; ++u) {
                 float e[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(x[2 * u + (j >> 2)][n][j & 3], c2, -m[n]));
+                for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f((x[2 * u + (j >> 2)][n][j & 3] - m[n]) * c2);
                 p[u][n] = u32x4_t{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7])};
             }
         }
@@ -267,7 +270,7 @@ __device__ __forceinline__ void store(const AttendArgs &a, int64_t at, int col, 
         const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // no key: 0; NaN stays
         *reinterpret_cast<u32x2_t *>(static_cast<uint16_t *>(a.out) + at * D + d) =
             u32x2_t{pack2<DT>(r[0] * by, r[1] * by), pack2<DT>(r[2] * by, r[3] * by)};
-        if (d == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+        if (d == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top * c2_of(a) + log2f(l)) * kLn2;
     }
 }
 
@@ -556,7 +559,7 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
         f32x4_t r{0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float by = exp2f(stat[w * COLS + cc] - top);
+            const float by = exp2f((stat[w * COLS + cc] - top) * c.c2);
             l += by * stat[W * COLS + w * COLS + cc];
             r += by * *reinterpret_cast<const f32x4_t *>(acc + (w * COLS + cc) * PITCH + d);
         }
@@ -698,12 +701,13 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles
     const int64_t w0 = runs.team_of(first), w1 = runs.team_of(first + steps - 1);
     if (w0 == w1) return;  // one team had all of it
     auto slot = [&](int64_t w) { return ((w * tiles + ct) * 2 + (w == w0 ? 1 : 0)) * cols + c; };
+    const float c2 = c2_of(a);
     float top = kFloor, l = 0.0f, r[PER] = {};
     for (int64_t base = w0; base <= w1; base += 64) {
         const int n = static_cast<int>(w1 - base + 1 < 64 ? w1 - base + 1 : 64);
         const float2 ml = lane < n ? *reinterpret_cast<const float2 *>(part_ml + 2 * slot(base + lane)) : make_float2(kFloor, 0.0f);
         const float to = fmaxf(top, wave_allmax(ml.x));
-        const float old = exp2f(top - to), mine = exp2f(ml.x - to);
+        const float old = exp2f((top - to) * c2), mine = exp2f((ml.x - to) * c2);
         top = to;
         l *= old;
 #pragma unroll
@@ -734,7 +738,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles
 #pragma unroll
         for (int j = 0; j < PER; j += 2) *reinterpret_cast<uint32_t *>(out + j) = pack2<DT>(r[j] * by, r[j + 1] * by);
     }
-    if (lane == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top + log2f(l)) * kLn2;
+    if (lane == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top * c2_of(a) + log2f(l)) * kLn2;
 }
 
 template <knn_dtype DT, int D>

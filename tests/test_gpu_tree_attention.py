@@ -316,3 +316,16 @@ def test_refusals():
     odd = torch.zeros(4, 4, 136, dtype=torch.bfloat16, device="cuda")[:, :, 4:132]
     with pytest.raises(knn.KnnError):
         knn.tree_attention(**dict(args, q=odd))
+
+
+@pytest.mark.parametrize("length", [3, 300])
+def test_scores_far_below_zero(length):
+    """Equal scores of -64 * 1e32 / 8: the weights are equal however low they are, and the mean is exact (of ones)."""
+    x, _, _ = batch("bf16", [1], [length], (2, 1), 64, 16, seed=3)
+    x["q"].fill_(1e16)
+    x["k_cache"].fill_(-1e16)
+    x["v_cache"].fill_(1.0)
+    out, lse = knn.tree_attention(*[x[n] for n in NAMES], want_lse=True)
+    assert (out == 1.0).all()
+    score = -64 * float(torch.tensor(1e16).bfloat16()) ** 2 / 8
+    assert (lse.double() / score - 1).abs().max() < 70 * 2.0 ** -23  # a 32-bit sum of 64 products
