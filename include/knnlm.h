@@ -406,7 +406,8 @@ knn_status knn_mix_rrc(const int32_t *nbr_ids, const float *nbr_dists, const int
  * Element types are KNN_BF16 and KNN_F16; KNN_F32 is KNN_ERR_UNSUPPORTED
  * except for knn_sample.  None of these calls copies to the host or depends on
  * values that the host reads, so a captured graph replays on new lengths,
- * tables and parameters.
+ * tables and parameters.  Calls that may run at the same time need workspaces
+ * and outputs of their own.
  */
 
 /* Largest number of query or key heads. */
@@ -428,7 +429,8 @@ knn_status knn_mix_rrc(const int32_t *nbr_ids, const float *nbr_dists, const int
  *   source_count   rows that q, k and v hold (>= rows without source_rows).
  *   rot_dim        even, 0..head_dim: the first rot_dim elements of a head are rotated, in pairs (i, i + rot_dim / 2),
  *                  or (2 i, 2 i + 1) with interleaved != 0; the others are copied.
- *   q_out          [rows, q_heads, head_dim] dense; may be q itself where q is dense and source_rows NULL.
+ *   q_out          [rows, q_heads, head_dim] dense; may be q itself where q is dense and source_rows NULL, and lies
+ *                  apart from it otherwise.
  *   k_cache, v_cache   written at the rows' indices; nothing else of them is touched.  Where two rows name one slot
  *                  (two sequences that share a page), its elements are of either.
  * head_dim up to 1024 (KNN_ERR_UNSUPPORTED above).
@@ -459,10 +461,11 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
  *   tree_mask      [rows, mask_words] uint32 or NULL: bit (j & 31) of word j >> 5 of row i set means that it sees its
  *                  sequence's row j (itself only where its own bit is set); NULL: the rows up to itself.
  *   max_rows       host hint: the most rows of a sequence (1 .. 65535, at most `rows`; 32 mask_words with a mask).
- *   max_keys       host hint: at least cache_lens[s] + its rows, for every sequence; at most table_width * page_size.
- *                  It decides how the work is split: a bound near the longest sequence is the fastest.
+ *   max_keys       host hint: at least cache_lens[s] + its rows, for every sequence; at most table_width * page_size,
+ *                  and 2^31 - 1.  It decides how the work is split: a bound near the longest sequence is the fastest.
+ *                  Rows and keys past a hint that is too low are left out.
  *   scale          finite; 1 / sqrt(head_dim) as a rule.
- *   out            [rows, q_heads, head_dim] dtype, dense.  A row that sees no key gets 0.
+ *   out            [rows, q_heads, head_dim] dtype, dense, apart from q.  A row that sees no key gets 0.
  *   lse            [rows, q_heads] fp32 or NULL: the natural logarithm of the weights' sum (-inf for such a row).
  *   workspace      knn_tree_attention_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
  *

@@ -41,6 +41,7 @@ knn_status check_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_hea
     if (rows < 1 || S < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads != 0) return KNN_ERR_INVALID_ARG;
     if (max_rows < 1 || max_rows > rows || max_keys < 1) return KNN_ERR_INVALID_ARG;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return KNN_ERR_UNSUPPORTED;
+    // (the kernels count the steps of 64 keys of 64 sequences in 32 bits)
     if (rows > 0x7fffffff || max_rows > 65535 || max_keys > 0x7fffffff || q_heads > KNNLM_MAX_HEADS || S > 0x7fffffff)
         return KNN_ERR_UNSUPPORTED;
     return KNN_OK;
@@ -49,6 +50,17 @@ knn_status check_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_hea
 knn_status check_sample(int64_t rows, int64_t V, knn_dtype dtype) {
     if (rows < 1 || V < 1 || (dtype != KNN_F32 && dtype != KNN_BF16 && dtype != KNN_F16)) return KNN_ERR_INVALID_ARG;
     return rows > 0x7fffffff || V > kSampleMaxV ? KNN_ERR_UNSUPPORTED : KNN_OK;
+}
+
+// Whether an input of [rows, heads, head_dim] 16-bit elements with these strides and a dense output of `out_rows` rows
+// lie on common bytes.
+bool overlaps(const void *in, int64_t rows, int64_t heads, int64_t head_dim, int64_t row, int64_t head, const void *out,
+              int64_t out_rows) {
+    const double in_bytes = 2.0 * (static_cast<double>(rows - 1) * row + static_cast<double>(heads - 1) * head + head_dim);
+    const double out_bytes = 2.0 * out_rows * heads * head_dim;  // doubles: no sum of strides can pass them
+    const double apart = static_cast<double>(reinterpret_cast<uintptr_t>(out)) -
+                         static_cast<double>(reinterpret_cast<uintptr_t>(in));
+    return apart < in_bytes && -apart < out_bytes;
 }
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -85,6 +97,7 @@ knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_
     if (!workspace || !aligned(workspace, 256) ||
         workspace_bytes < knn_tree_attention_workspace_size(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys))
         return KNN_ERR_WORKSPACE;
+    if (overlaps(q, rows, q_heads, head_dim, q_row_stride, q_head_stride, out, rows)) return KNN_ERR_INVALID_ARG;
     AttendArgs a{};
     a.q = q, a.k_cache = k_cache, a.v_cache = v_cache;
     a.row_offsets = row_offsets, a.cache_lens = cache_lens, a.tree_mask = tree_mask;
@@ -121,6 +134,11 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
         return KNN_ERR_INVALID_ARG;
     if (head_dim > 1024 || q_heads > KNNLM_MAX_HEADS || rows > 0x7fffffff || source_count > 0x7fffffff)
         return KNN_ERR_UNSUPPORTED;
+    const bool in_place = q == q_out && source_rows == nullptr && q_head_stride == head_dim &&
+                          q_row_stride == q_heads * head_dim;
+    if (q != nullptr && !in_place &&
+        overlaps(q, source_count, q_heads, head_dim, q_row_stride, q_head_stride, q_out, rows))
+        return KNN_ERR_INVALID_ARG;
     AppendArgs a{};
     a.q = q, a.k = k, a.v = v;
     a.row_offsets = row_offsets, a.cache_lens = cache_lens, a.positions = positions;
@@ -149,6 +167,7 @@ knn_status knn_sample(const void *scores, const float *uniforms, const float *te
     const knn_status st = check_sample(rows, V, dtype);
     if (st != KNN_OK) return st;
     if (row_stride < 0) return KNN_ERR_INVALID_ARG;
+    if (!aligned(scores, dtype == KNN_F32 ? 4 : 2)) return KNN_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < knn_sample_workspace_size(rows, V, dtype))
         return KNN_ERR_WORKSPACE;
     SampleArgs a{};

@@ -36,7 +36,9 @@ def _flat(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple
 
 
 class _Call:
-    """A call that is made again and again on one GPU, with the same buffers where they are."""
+    """A call that is made again and again on one GPU, with the same buffers where they are.  Its runs share their
+    outputs and workspace, so they follow each other on one stream or wait for each other.  A graph that captured one
+    replays on its buffers: keep the object as long as the graph."""
 
     def _keep(self, index: int, name: str, args: Sequence, tensors: Sequence, own: Sequence[torch.Tensor]):
         """`name`: the library's function; `args`: its arguments but the stream, converted once; `tensors`: what they
@@ -65,7 +67,8 @@ class _Call:
 def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, row_offsets: torch.Tensor,
            cache_lens: torch.Tensor) -> Tuple[int, int, int, int, int]:
     """Checks the cache's tensors: (S, n_pages, kv_heads, page_size, head_dim)."""
-    _need(k_cache.dim() == 4 and k_cache.is_contiguous(), "k_cache: contiguous [n_pages, kv_heads, page_size, head_dim]")
+    _need(k_cache.dim() == 4 and k_cache.is_contiguous(),
+          "k_cache: contiguous [n_pages, kv_heads, page_size, head_dim]")
     _flat("v_cache", v_cache, k_cache.dtype, tuple(k_cache.shape))
     _need(pages.dim() == 2, "pages: [S, table_width]")
     _flat("pages", pages, torch.int32, tuple(pages.shape))
@@ -84,7 +87,7 @@ class KVAppend(_Call):
     [S, width] int32, row_offsets [S+1] int64, cache_lens [S] int32 as the header says.  positions [rows] int32
     (default: the cache index); inv_freq [rotated elements / 2] fp32 (None: no rotation); interleaved: pairs
     (2i, 2i+1); source_rows [rows] int32: the row that each row is read from.  q_out [rows, q_heads, d] is
-    allocated where it is not given (it may be q).
+    allocated where it is not given (it may be q where q is dense and there are no source_rows).
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -229,7 +232,8 @@ class Sampler(_Call):
                  temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
                  top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None):
         index = _on_device(scores, uniforms=uniforms, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
-        _need(scores.dim() == 2 and (scores.stride(1) == 1 or scores.shape[1] == 1), "scores: [rows, V] with dense rows")
+        _need(scores.dim() == 2 and (scores.stride(1) == 1 or scores.shape[1] == 1),
+              "scores: [rows, V] with dense rows")
         rows, V = scores.shape
         for name, t, dtype in (("uniforms", uniforms, torch.float32), ("temperature", temperature, torch.float32),
                                ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),

@@ -102,3 +102,21 @@ def test_oracle_sample_by_hand():
     assert lm.sample([0.25] * 4, 0.5, True, top_k=3)[::2] == (1, 3)  # running 1/3, 2/3: the first over a half
     assert lm.sample([0.0, -1.0], 0.5, True) == (-1, 0.0, 0)
     assert lm.sample(x, 0.9, False, temperature=0.0) == (1, 1.0, 1)
+
+
+def test_outputs_apart_from_their_inputs(lib):
+    """A call whose output would overwrite what it still reads is refused (q ends 4 * 1024 and 32 * 1024 elements on)."""
+    for q_out in (FAKE + 16, FAKE + 8 * 1024 - 2, FAKE - 8 * 1024 + 16):
+        assert lib.knn_kv_append(*dict(APPEND, q_out=q_out).values()) == INVALID
+    assert lib.knn_kv_append(*dict(APPEND, source_rows=FAKE).values()) == INVALID  # q_out is q, and rows change places
+    assert lib.knn_kv_append(*dict(APPEND, q_row=1032).values()) == INVALID        # q_out is q, with other strides
+    for out in (FAKE, FAKE + 64 * 1024 - 16, FAKE - 64 * 1024 + 16):
+        assert lib.knn_tree_attention(*dict(ATTEND, out=out).values()) == INVALID
+
+
+def test_limits_of_lengths_and_alignment(lib):
+    longest = dict(out=FAKE * 64, max_keys=1 << 31, table_width=1 << 20, page_size=65536)
+    assert lib.knn_tree_attention(*dict(ATTEND, **longest).values()) == UNSUPPORTED
+    assert lib.knn_tree_attention_workspace_size(32, 2, 8, 2, 128, 16, (1 << 31) - 1) > 0
+    assert lib.knn_tree_attention_workspace_size(32, 2, 8, 2, 128, 16, 1 << 31) == 0
+    assert lib.knn_sample(*dict(SAMPLE, scores=FAKE + 1).values()) == UNSUPPORTED
