@@ -141,3 +141,76 @@ def test_a_tree_is_drafted_verified_kept_and_decoded_on():
     most = float(np.nan_to_num(np.abs(host(seq.v))).max())
     want = host(fed[[41, 134]])
     assert (np.abs(host(after) - want) <= 2 * (2.0 ** -8 * (2 * np.abs(want) + most) + 1e-4 * most) + 1e-6).all()
+
+
+def test_two_calls_at_once_and_a_graph_of_all():
+    """Objects of their own on two streams at the same time, and one graph of append, attention and draw, replayed on
+    new lengths: the bits of the same calls one after the other."""
+    S, n, heads, kv_heads, d, page, V = 3, 4, 8, 2, 128, 32, 4001
+    shape = (64, kv_heads, page, d)
+    off = torch.arange(0, S * n + 1, n, dtype=torch.int64).cuda()
+    inv_freq = (10000.0 ** (-torch.arange(0, d, 2).float() / d)).cuda()
+
+    class Program:
+        def __init__(self, seed):
+            r = torch.Generator().manual_seed(seed)
+            self.q, self.k, self.v = (torch.randn(S * n, h, d, generator=r).bfloat16().cuda()
+                                      for h in (heads, kv_heads, kv_heads))
+            self.cache = [torch.randn(shape, generator=r).bfloat16().cuda() for _ in range(2)]
+            self.first = [c.clone() for c in self.cache]
+            self.pages = torch.randperm(64, generator=r)[:60].view(S, 20).int().cuda()
+            self.lens = torch.zeros(S, dtype=torch.int32, device="cuda")
+            rows = (*self.cache, self.pages, off, self.lens)
+            self.append = knn.KVAppend(self.k, self.v, *rows, q=self.q, inv_freq=inv_freq)
+            self.attend = knn.TreeAttention(self.append.q_out, *rows, max_rows=n, max_keys=640, want_lse=True)
+            logits = (torch.randn(S * n, V, generator=r) * 3).bfloat16().cuda()
+            self.draw = knn.Sampler(logits, torch.rand(S * n, generator=r).cuda(),
+                                    top_p=torch.full((S * n,), 0.9, device="cuda"))
+
+        def reset(self, lens):
+            self.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+            for c, f in zip(self.cache, self.first):
+                c.copy_(f)
+
+        def run(self):
+            self.append.run()
+            self.attend.run()
+            self.draw.run()
+
+        def results(self):
+            return [t.clone() for t in (*self.cache, self.append.q_out, self.attend.out, self.attend.lse,
+                                        self.draw.token, self.draw.prob, self.draw.kept)]
+
+    both = [Program(1), Program(2)]
+    lengths = [[600, 17, 0], [1, 636, 300], [255, 256, 257]]
+    want = {}
+    for i, lens in enumerate(lengths):
+        for j, p in enumerate(both):
+            p.reset(lens)
+            p.run()
+            want[i, j] = p.results()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in both]
+    for i, lens in enumerate(lengths):
+        for p in both:
+            p.reset(lens)
+        torch.cuda.synchronize()
+        for _ in range(3):  # the same rows at the same indices again
+            for p, s in zip(both, streams):
+                with torch.cuda.stream(s):
+                    p.run()
+        torch.cuda.synchronize()
+        for j, p in enumerate(both):
+            assert all(torch.equal(a, b) for a, b in zip(p.results(), want[i, j])), (i, j)
+    p = both[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.run()
+    for i, lens in enumerate(lengths * 2):
+        p.reset(lens)
+        graph.replay()
+        got = p.results()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[i % 3, 0])), i
+        p.run()  # the program's own work between the replays
+        torch.cuda.synchronize()
