@@ -329,3 +329,19 @@ def test_scores_far_below_zero(length):
     assert (out == 1.0).all()
     score = -64 * float(torch.tensor(1e16).bfloat16()) ** 2 / 8
     assert (lse.double() / score - 1).abs().max() < 70 * 2.0 ** -23  # a 32-bit sum of 64 products
+
+
+@pytest.mark.parametrize("heads", [(4, 2), (32, 2)])
+def test_hints_that_are_too_low_leave_out(heads):
+    """Sequence 0 has more rows and keys than the hints say: its first rows see the first keys, its others stay."""
+    x, _, _ = batch("f16", [5, 3], [100, 40], heads, 64, 16, seed=12)
+    out = torch.full((x["q"].shape[0], heads[0], 64), 7.0, dtype=torch.float16, device="cuda")
+    knn.tree_attention(*[x[n] for n in NAMES], max_rows=4, max_keys=64, out=out)
+    short = dict(x, cache_lens=torch.tensor([64, 40], dtype=torch.int32, device="cuda"))
+    none = torch.zeros(8, 1, dtype=torch.int32, device="cuda")  # of sequence 0 no draft is seen, so 64 keys are
+    none[5:] = knn.tree_words([-1, 0, 1], "cuda")
+    want = knn.tree_attention(*[short[n] for n in NAMES], tree_mask=none)
+    live = [0, 1, 2, 3, 5, 6, 7]
+    # the same sums in another order: half a step for each result and its weights, twice
+    assert ((out - want).float()[live].abs() <= 4 * 2.0 ** -11 * (1 + want.float()[live].abs().max())).all()
+    assert (out[4] == 7.0).all()
