@@ -506,7 +506,8 @@ size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_head
  * ordered by x, the larger first, the lower token first among equals, and
  *   1. top_k in [1, present): the first top_k stay;
  *   2. top_p < 1: of these, those before which less than top_p of their weight lies (always the first);
- *   3. min_p > 0: of these, those of weight min_p (of the largest's) and more (always the first).
+ *   3. min_p > 0: of these, those of weight min_p (of the largest's) and more (always the first, which of min_p > 1
+ *      is the only one, whatever equals it).
  * The token is the first one that stays, by token id, at which the running
  * weight of those that stay exceeds uniform times their sum.  T <= 0 or NaN
  * takes the first element of the order.  NaN filters are off.

@@ -370,7 +370,7 @@ __device__ __forceinline__ int place(int i, int c) { return i + c + (c < 4 ? 0 :
 
 // The filters and the draw of a row whose largest present value is `top` and
 // smallest `low`, `mine` the largest that this thread read, at a temperature
-// and a top-p above 0.
+// and a top-p above 0 and a min-p of up to 1.
 template <bool PROBS, typename R>
 __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &sh, int64_t r, float top, float low, float mine,
                                      const Wish &wish, int log2_unit) {
@@ -392,8 +392,8 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
     // under it (log2f is right to 2^-20) and the largest, in 64ths.
     float least = -INFINITY;
     if (min_p > 0.0f && !w.even) {
-        const double enough = w.of(top) * fmin(static_cast<double>(min_p), 1.0);
-        const float far = t * (log2f(fminf(min_p, 1.0f)) - 0.001f);
+        const double enough = w.of(top) * static_cast<double>(min_p);
+        const float far = t * (log2f(min_p) - 0.001f);
         const float under = PROBS ? top * exp2f(far) * 0.999f
                                   : __double2float_rd(static_cast<double>(top) + 0.69314718 * static_cast<double>(far));
         uint32_t lo = key_of(under), hi = key_of(top);
@@ -815,7 +815,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int log2_unit
         }
         return;
     }
-    if (!(wish.t > 0.0f) || wish.p <= 0.0f) {  // the first element of the order
+    // The first element of the order.  A min-p above 1 leaves only that one too: no weight reaches it, not even an equal one's.
+    if (!(wish.t > 0.0f) || wish.p <= 0.0f || wish.min_p > 1.0f) {
         int first = 0x7fffffff;
         rw.pass(
             wave, lane,

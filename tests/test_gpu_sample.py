@@ -260,3 +260,26 @@ def test_a_row_of_millions():
     check(x, [0.3, 0.98], temperature=[0.9, 1.2])
     check(x, [0.3, 0.98], top_p=[0.7, 0.4], top_k=[0, 100000])
     check(x, [0.7, 0.1], min_p=[0.3, 0.001], top_k=[40, 0])
+
+
+def test_min_p_above_one_keeps_the_first_alone():
+    """No weight reaches it, those of elements equal to the largest neither."""
+    x = torch.randn(8, 3000, generator=torch.Generator().manual_seed(12)).cuda()
+    x[0, :3] = torch.tensor([9.0, 9.0, 8.0])
+    x[1, 5::7] = 9.0                   # hundreds of equal ones
+    x[2, 3:] = 9.0
+    x[3, 40] = x[3, 2999] = INF
+    x[4, 1:] = INF
+    x[5, 700] = 9.0                    # alone
+    x[6, 100:] = -INF
+    x[6, 50] = x[6, 60] = 9.0
+    x[7, 10] = x[7, 20] = 9.0          # min-p of 1 itself: the equal ones stay
+    u = [0.9, 0.999, 0.5, 0.9, 0.99, 0.0, 0.99, 0.6]
+    m = [2.0, 1.0 + 2.0 ** -23, 1e30, 2.0, INF, 3.0, 1.5, 1.0]
+    for probs in (False, True):
+        _, prob, kept = check(x, u, probs, min_p=m)
+        assert (kept[:7] == 1).all() and kept[7] == 2 and (prob[:7] == 1.0).all()
+        check(x, u, probs, min_p=m, top_p=[0.9] * 8)
+        check(x, u, probs, min_p=m, top_k=[100] * 8)
+        check(x, u, probs, min_p=m, top_k=[1000] * 8, top_p=[0.7] * 8, temperature=[0.5] * 8)
+    check(torch.tensor([[1.0, 1.0, 0.0]], device="cuda"), [0.9], min_p=[2.0])
