@@ -473,7 +473,9 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
  * element type for the product with v, and summed as rounded.  Results do not
  * depend on the order in which workgroups run.  Keys and values that a row
  * does not see may hold anything, infinities and NaN too; a value that is not
- * finite makes NaN what sees it.  head_dim is 64, 128 or 256, q and the caches
+ * finite makes NaN that element of what sees it, whatever its key's weight (and
+ * so do finite ones whose weighted sums pass the range of fp32, as of bf16 values
+ * over 2^100 they may).  head_dim is 64, 128 or 256, q and the caches
  * and out lie on 16 bytes and the strides are multiples of 8 elements
  * (KNN_ERR_UNSUPPORTED otherwise).
  */

@@ -24,7 +24,7 @@
 // sequences of 2,000 to 16,000 tokens, 8 key heads: 402 us for 2.36 GB, 5.9 TB/s
 // with the join (a plain read: 7.0).  64 and more columns: the issue of a
 // weight's vector instructions beside its two matrix products, at 128 columns
-// of head_dim 128 with a full register file (256, four of them spilled).  Trees
+// of head_dim 128 with nearly a full register file (241 of 256).  Trees
 // of 64 rows on 4 x 131,072 tokens, 64 query heads on 8: 1.32 ms, 834 TFLOP/s
 // (a large library product: 1,166).  One token on 1,000 keys: 14.6 us, of which
 // 5.2 are the join's launch, and 9.2 two waits for memory, the barriers and the
@@ -129,6 +129,32 @@ __device__ __forceinline__ uint32_t seen(const AttendArgs &a, const Tile &t, int
 // From q.k (with the scale's sign) to the exponent of two.
 __device__ __forceinline__ float c2_of(const AttendArgs &a) { return a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e; }
 
+// The keys of a span, counted from its first one, k0 (a multiple
+// of 64): where they lie, and how many rows there are to read.
+template <int D>
+struct Keys {
+    const int32_t *table;  // of k0's page
+    int page_log2, slot0;  // slot0: k0's in its page
+    int64_t n_pages, head_bytes, page_bytes;
+    int last;  // the last key
+
+    __device__ __forceinline__ Keys(const AttendArgs &a, int64_t s, int h, int64_t k0, int64_t end)
+        : table(a.cache.pages + s * a.cache.table_width + (k0 >> a.cache.page_log2)), page_log2(a.cache.page_log2),
+          slot0(static_cast<int>(k0 & ((int64_t{1} << a.cache.page_log2) - 1))), n_pages(a.cache.n_pages),
+          head_bytes(static_cast<int64_t>(h) * 2 * D << a.cache.page_log2),
+          page_bytes(static_cast<int64_t>(a.kv_heads) * 2 * D << a.cache.page_log2), last(static_cast<int>(end - 1 - k0)) {}
+    // The page of a key (keys past the last one are read as the last one).
+    __device__ __forceinline__ int32_t entry(int key) const { return table[(slot0 + min(key, last)) >> page_log2]; }
+    __device__ __forceinline__ bool real(int32_t page) const { return page >= 0 && page < n_pages; }
+    // Byte offset of 16 keys from `key` on in either cache; `rows`: the last of them that there is.
+    __device__ __forceinline__ int64_t at(int key, int32_t page, int &rows) const {
+        if (!real(page)) page = 0;
+        key = key > last ? last & ~15 : key;
+        rows = min(last - key, 15);
+        return page * page_bytes + head_bytes + ((slot0 + key) & ((1 << page_log2) - 1)) * (2 * D);
+    }
+};
+
 // The columns of a wave: NT x 16 (row, query head) pairs of one key head.
 template <knn_dtype DT, int D, int NT>
 struct Columns {
@@ -170,7 +196,7 @@ struct Columns {
     // is cached or named by the row's mask.
     template <int U>
     __device__ __forceinline__ void tile(const AttendArgs &a, const Tile &t, const uint32_t (&kt)[U], int64_t key, bool all,
-                                         int64_t end, uint32_t real, int col, int quad) {
+                                         int64_t end, uint32_t real, int col, int quad, bool &left_out) {
         f32x4_t x[2 * U][NT];
 #pragma unroll
         for (int u = 0; u < 2 * U; ++u) {
@@ -246,8 +272,8 @@ struct Columns {
                 }
             return;
         }
-        // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such elements are
-        // left out of the product, and make NaN what sees them.
+        // A column must not take an infinity or NaN from a key that it does not see (0 * NaN is NaN): such elements are left
+        // out of the product, and poison() gives them to those who see them.
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -256,18 +282,60 @@ struct Columns {
                 const u32x4_t bad = {not_finite<DT>(v.x), not_finite<DT>(v.y), not_finite<DT>(v.z), not_finite<DT>(v.w)};
                 if (__any((bad.x | bad.y | bad.z | bad.w) != 0u)) {
                     v &= ~bad;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const f32x4_t sees = mfma16<DT>(bad & kOne, p[u][n], f32x4_t{0, 0, 0, 0});
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) o[n][d][j] = sees[j] > 0.0f ? __builtin_nanf("") : o[n][d][j];
-                    }
+                    left_out = true;
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[u][n], o[n][d]);
             }
     }
+
+    // Where a tile left values out: makes infinite, whatever the key's weight, the sums of the columns that see them (for
+    // mean() to make NaN), by a product of 2^127 and 2^127 in bf16 for either type.  32-key tiles first, first + step, ...
+    // of a span of n; the values come from memory once more, since their stage is long filled anew.  Behind the loop over the
+    // tiles and not in it, where the masks that it needs would hold registers (2% of the time of trees, 7% of a prompt's).
+    __device__ __forceinline__ void poison(const AttendArgs &a, const Tile &t, const Keys<D> &keys, int64_t k0, int64_t end,
+                                           int first, int step, int n_tiles, int col, int quad) {
+        constexpr uint32_t kFar = 0x7f00u;
+#pragma unroll 1
+        for (int i = first; i < n_tiles; i += step) {
+            u32x4_t far[NT];
+            const uint16_t *from[8];  // the values of element `col` of this lane's keys
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int key = 32 * i + 16 * half;
+                const int32_t page = keys.entry(key);
+                int rows;
+                const char *at = static_cast<const char *>(a.v_cache) + keys.at(key, page, rows);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    from[4 * half + j] = reinterpret_cast<const uint16_t *>(at) + min(4 * quad + j, rows) * D + col;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint32_t bits = keys.real(page) ? seen(a, t, row_of[n], k0 + key + 4 * quad, end) : 0u;
+                    far[n][2 * half] = ((bits & 1u) | (bits & 2u) << 15) * kFar;
+                    far[n][2 * half + 1] = ((bits >> 2 & 1u) | (bits >> 2 & 2u) << 15) * kFar;
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                u32x4_t bad;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    bad[j] = not_finite<DT>(from[2 * j][16 * d] | static_cast<uint32_t>(from[2 * j + 1][16 * d]) << 16) &
+                             (kFar | kFar << 16);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) o[n][d] = mfma16<KNN_BF16>(bad, far[n], o[n][d]);
+            }
+        }
+    }
 };
+
+// An element of the result: NaN where a value that is not finite was seen.  A tile that all columns see has them in its
+// product, which leaves an infinity or (of a weight of 0, or two signs) NaN.
+__device__ __forceinline__ float mean(float sum, float by) {
+    const float v = sum * by;
+    return fabsf(v) < INFINITY ? v : __builtin_nanf("");
+}
 
 // Four elements of a finished column, or of a part of one (`part` not null: its
 // columns [cols][D]), and with d == 0 its reference and sum.
@@ -280,7 +348,7 @@ __device__ __forceinline__ void store(const AttendArgs &a, int64_t at, int col, 
     } else {
         const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // no key: 0; NaN stays
         *reinterpret_cast<u32x2_t *>(static_cast<uint16_t *>(a.out) + at * D + d) =
-            u32x2_t{pack2<DT>(r[0] * by, r[1] * by), pack2<DT>(r[2] * by, r[3] * by)};
+            u32x2_t{pack2<DT>(mean(r[0], by), mean(r[1], by)), pack2<DT>(mean(r[2], by), mean(r[3], by))};
         if (d == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top * c2_of(a) + log2f(l)) * kLn2;
     }
 }
@@ -448,32 +516,6 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
     }
 }
 
-// The keys of a span, counted from its first one, k0 (a multiple
-// of 64): where they lie, and how many rows there are to read.
-template <int D>
-struct Keys {
-    const int32_t *table;  // of k0's page
-    int page_log2, slot0;  // slot0: k0's in its page
-    int64_t n_pages, head_bytes, page_bytes;
-    int last;  // the last key
-
-    __device__ __forceinline__ Keys(const AttendArgs &a, int64_t s, int h, int64_t k0, int64_t end)
-        : table(a.cache.pages + s * a.cache.table_width + (k0 >> a.cache.page_log2)), page_log2(a.cache.page_log2),
-          slot0(static_cast<int>(k0 & ((int64_t{1} << a.cache.page_log2) - 1))), n_pages(a.cache.n_pages),
-          head_bytes(static_cast<int64_t>(h) * 2 * D << a.cache.page_log2),
-          page_bytes(static_cast<int64_t>(a.kv_heads) * 2 * D << a.cache.page_log2), last(static_cast<int>(end - 1 - k0)) {}
-    // The page of a key (keys past the last one are read as the last one).
-    __device__ __forceinline__ int32_t entry(int key) const { return table[(slot0 + min(key, last)) >> page_log2]; }
-    __device__ __forceinline__ bool real(int32_t page) const { return page >= 0 && page < n_pages; }
-    // Byte offset of 16 keys from `key` on in either cache; `rows`: the last of them that there is.
-    __device__ __forceinline__ int64_t at(int key, int32_t page, int &rows) const {
-        if (!real(page)) page = 0;
-        key = key > last ? last & ~15 : key;
-        rows = min(last - key, 15);
-        return page * page_bytes + head_bytes + ((slot0 + key) & ((1 << page_log2) - 1)) * (2 * D);
-    }
-};
-
 // Few columns (NT x 16): the W waves share them and wave w takes the 32-key
 // tiles w, w + W, ... of a span with a reference and sums of its own, joined at
 // the end.  Each wave fills its own two stages by loads straight to LDS, one
@@ -521,6 +563,7 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
         }
     };
 
+    bool left_out = false;
     if (own > 0) {
         hold_pages(0);
         fill(0);
@@ -538,10 +581,12 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
         const uint32_t kt[1] = {mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF)};
         const int key = 32 * (wave + W * i);
         const bool all = key + 32 <= whole && real_a && real_b;
-        c.template tile<1>(a, t, kt, k0 + key, all, end, (real_a ? 1u : 0u) | (real_b ? 2u : 0u), col, quad);
+        c.template tile<1>(a, t, kt, k0 + key, all, end, (real_a ? 1u : 0u) | (real_b ? 2u : 0u), col, quad, left_out);
         // the stage is read: the next round's loads may overwrite it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+
+    if (left_out) c.poison(a, t, keys, k0, end, wave, W, n_tiles, col, quad);
 
     // Join the waves: references first, then each one's sums relative to the common reference.
     __syncthreads();  // every wave is done with its stages (its loads have landed)
@@ -636,9 +681,11 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
 #pragma unroll
     for (int i = 0; i < RING - U; ++i)
         if (i < n) fill(i);
-    uint32_t stage = base;
-    for (int i = 0; i < n; i += U) {
-        // This wave's loads of tiles i .. i + U - 1 have landed when only the later tiles' are on their way.
+    uint32_t stage = base, real = 0, kt[U];
+    bool left_out = false;
+    // Makes ready the tiles i .. i + U - 1; whether every column sees all of their keys.
+    auto ready = [&](int i) {
+        // This wave's loads of them have landed when only the later tiles' are on their way.
         if (i + RING - U - 1 < n) __builtin_amdgcn_s_waitcnt(vmcnt_encoding<(RING - 2 * U) * MINE>());
         else __builtin_amdgcn_s_waitcnt(kVmcntZero);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -650,7 +697,7 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
         // the pages of tiles i .. i + U - 1 (of one 32): held since they were filled
         const int filled = i + RING - 1 < n ? i + RING - 1 : n - 1;
         const int32_t pages = (filled >> 5) != (i >> 5) ? page_old : page_reg;
-        uint32_t real = 0, kt[U];
+        real = 0;
 #pragma unroll
         for (int u = 0; u < 2 * U; ++u) real |= keys.real(__builtin_amdgcn_readlane(pages, 2 * (i & 31) + u)) ? 1u << u : 0u;
 #pragma unroll
@@ -659,9 +706,20 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
             stage += 2 * Sh::HALF;
             if (stage == base + RING * 2 * Sh::HALF) stage = base;
         }
-        const bool all = 32 * i + 32 * U <= whole && real == (1u << 2 * U) - 1u;
-        c.template tile<U>(a, t, kt, k0 + 32 * i, all, end, real, col, quad);
+        return 32 * i + 32 * U <= whole && real == (1u << 2 * U) - 1u;
+    };
+    // (Two loops in one another: one for both kinds of tile moves half of the sums from register to register every time.)
+    for (int i = 0; i < n; i += U) {
+        bool all = ready(i);
+        while (all) {
+            c.template tile<U>(a, t, kt, k0 + 32 * i, true, end, real, col, quad, left_out);
+            i += U;
+            if (i >= n) break;
+            all = ready(i);
+        }
+        if (!all) c.template tile<U>(a, t, kt, k0 + 32 * i, false, end, real, col, quad, left_out);
     }
+    if (left_out) c.poison(a, t, keys, k0, end, 0, 1, n, col, quad);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
         const int cc = 16 * NT * wave + 16 * i + col;
@@ -744,10 +802,10 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles
     const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
     uint16_t *out = static_cast<uint16_t *>(a.out) + at * D + lane * PER;
     if constexpr (PER == 1) {
-        out[0] = static_cast<uint16_t>(pack2<DT>(r[0] * by, 0.0f));
+        out[0] = static_cast<uint16_t>(pack2<DT>(mean(r[0], by), 0.0f));
     } else {
 #pragma unroll
-        for (int j = 0; j < PER; j += 2) *reinterpret_cast<uint32_t *>(out + j) = pack2<DT>(r[j] * by, r[j + 1] * by);
+        for (int j = 0; j < PER; j += 2) *reinterpret_cast<uint32_t *>(out + j) = pack2<DT>(mean(r[j], by), mean(r[j + 1], by));
     }
     if (lane == 0 && a.lse != nullptr) a.lse[at] = l == 0.0f ? -INFINITY : (top * c2_of(a) + log2f(l)) * kLn2;
 }

@@ -345,3 +345,34 @@ def test_hints_that_are_too_low_leave_out(heads):
     # the same sums in another order: half a step for each result and its weights, twice
     assert ((out - want).float()[live].abs() <= 4 * 2.0 ** -11 * (1 + want.float()[live].abs().max())).all()
     assert (out[4] == 7.0).all()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("length", [200, 3001])
+@pytest.mark.parametrize("heads,rows,d", [((2, 1), 3, 64), ((16, 2), 3, 128), ((32, 2), 3, 128), ((32, 1), 4, 64),
+                                          ((8, 2), 3, 256), ((32, 2), 5, 256)])
+def test_values_that_are_not_finite_make_nan_what_sees_them(bad, dtype, length, heads, rows, d):
+    """Of heavy keys and of such as weigh nothing, in tiles that every row sees and in the last ones, and of a draft that
+    only the last row sees; every other element is what it was."""
+    x, _, _ = batch(dtype, [rows], [length], heads, d, 16, seed=21)
+    pages = x["pages"].cpu()
+
+    def slot(c):
+        return int(pages[0, c // 16]), slice(None), c % 16
+
+    x["q"] = x["q"].abs()
+    light = [37, length - 2]
+    for c in light:
+        x["k_cache"][slot(c)] = -200.0  # scores under -200 for positive q of this size: weights of 0
+    cells = {40: 5, length - 3: 6, light[0]: 7, light[1]: 40, length + rows - 1: 60}  # key: the element of its value
+    clean, lse0 = knn.tree_attention(*[x[n] for n in NAMES], want_lse=True)
+    for c, e in cells.items():
+        x["v_cache"][slot(c) + (e,)] = bad
+    out, lse = knn.tree_attention(*[x[n] for n in NAMES], want_lse=True)
+    torch.cuda.synchronize()
+    want = torch.zeros_like(out, dtype=torch.bool)
+    for c, e in cells.items():
+        want[max(0, c - length):, :, e] = True
+    assert torch.equal(torch.isnan(out), want)
+    assert torch.equal(out[~want], clean[~want]) and torch.equal(lse, lse0)
