@@ -38,6 +38,7 @@ namespace {
 
 constexpr float kFloor = -3.0e38f;  // reference before the first key
 constexpr float kSlack = 8.0f;
+constexpr float kBelow = 7.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int64_t kWhole = 256;  // keys of a head that is not parted
@@ -162,14 +163,16 @@ struct Columns {
     u32x4_t q[NT][KK];  // right operand of the scores: lane = (column, 8 elements a quad)
     f32x4_t o[NT][DB];  // lane = (column, 4 elements a quad)
     f32x4_t sum[NT];    // the same sum four times
-    float m[NT];        // reference: of q.k, whatever the scale, so that a key at it weighs 1 however large it is
+    float m[NT];        // reference: of q.k, whatever the scale, so that keys of one score weigh the same however large it is
     int row_of[NT];     // row within the sequence
-    float c2, slack;    // scale log2(e), positive: its sign is in q; kSlack over it
+    float c2;           // scale log2(e), positive: its sign is in q
+    float slack, below; // how far a score may lie over the reference, and the reference under the score that sets it
 
     __device__ __forceinline__ void load(const AttendArgs &a, const Tile &t, int h, int g, int c0, int cols, int col,
                                          int quad) {
         c2 = c2_of(a);
-        slack = kSlack / c2;
+        below = DT == KNN_F16 ? kBelow / c2 : 0.0f;
+        slack = (DT == KNN_F16 ? kSlack + kBelow : kSlack) / c2;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int c = c0 + 16 * n + col;
@@ -228,10 +231,10 @@ struct Columns {
             for (int u = 0; u < 2 * U; ++u)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top = __builtin_amdgcn_fmed3f(top, x[u][n][j], INFINITY);
-            if (__any(top > m[n] + slack)) {
+            if (__any(top - m[n] > slack)) {  // (their difference is right where m + slack may round to twice the slack)
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float to = fmaxf(m[n], top);
+                const float to = fmaxf(m[n], DT == KNN_F16 ? top - below : top);
                 const float by = exp2f((m[n] - to) * c2);
                 m[n] = to;
 #pragma unroll

@@ -376,3 +376,31 @@ def test_values_that_are_not_finite_make_nan_what_sees_them(bad, dtype, length, 
         want[max(0, c - length):, :, e] = True
     assert torch.equal(torch.isnan(out), want)
     assert torch.equal(out[~want], clean[~want]) and torch.equal(lse, lse0)
+
+
+@pytest.mark.parametrize("rows,heads", [(1, (8, 8)), (5, (64, 8))])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_long_flat_tail_behind_one_heavy_key(rows, heads, dtype):
+    """The first key's score is 17, those of the 32,767 behind it are 0: each weighs 2^-24.5 of the first.  f16 holds them
+    to 2^-32 of the largest, so that all together are off by 2^-17; half a step of the type for each weight and the result
+    and the 32-bit sums (2^-23 a term, of a mass of 2^-9) come on top.
+
+    The weights' own sum lies between 1 and 2, where a step of fp32 is 2^-23, and grows by 32 keys at a time, a wave's
+    quarter of the keys at one row and all of them at 40 columns: 256 and 1,024 sums that are each off by up to a step,
+    which the logarithm of a number over 1 takes on as they are."""
+    S, n, d, page = 64, 32768, 64, 128
+    k = torch.zeros(2, heads[1], page, d, dtype=TYPES[dtype], device="cuda")
+    v = torch.ones_like(k)
+    k[0, :, 0], v[0, :, 0] = 2.125, 0.0
+    q = torch.ones(S * rows, heads[0], d, dtype=k.dtype, device="cuda")
+    pages = torch.ones(S, n // page + 1, dtype=torch.int32, device="cuda")
+    pages[:, 0] = 0                                    # a page of ones and zeros is all the others
+    off = torch.arange(S + 1, device="cuda") * rows
+    lens = torch.full((S,), n, dtype=torch.int32, device="cuda")
+    none = torch.zeros(S * rows, 1, dtype=torch.int32, device="cuda")
+    out, lse = knn.tree_attention(q, k, v, pages, off, lens, tree_mask=none, want_lse=True)
+    mass = (n - 1) * np.exp(-17.0)
+    want, e = mass / (1 + mass), torch.finfo(k.dtype).eps / 2
+    assert (out.double() - want).abs().max() <= 3 * e * want + 2.0 ** -16
+    sums = n // 32 // (4 if rows == 1 else 1)
+    assert (lse.double() - 17.0 - np.log1p(mass)).abs().max() <= e * mass + 2.0 ** -16 + 18 * 2.0 ** -22 + sums * 2.0 ** -23
