@@ -158,10 +158,10 @@ class TreeAttention(_Call):
     """knn_tree_attention on these buffers: rows of drafts over the paged cache.
 
     q [rows, q_heads, d] (bf16 or f16; any row and head stride that is a multiple of 8), the cache's tensors as in
-    KVAppend.  max_rows and max_keys bound the rows of a sequence and its tokens with them; where they are not given
-    they come from the tensors' present contents, copied to the host once.  tree_mask [rows, words] int32 (see
-    tree_words) or None for chains.  out and lse ([rows, q_heads] fp32; only with want_lse) are allocated where they
-    are not given.
+    KVAppend.  max_rows and max_keys bound the rows of a sequence and its tokens with them, in every run; where they are
+    not given they are what can be at all: all rows (and bits of a mask's row) and the table's room.  Bounds near the
+    truth are faster, since they decide how the work is split.  tree_mask [rows, words] int32 (see tree_words) or None
+    for chains.  out and lse ([rows, q_heads] fp32; only with want_lse) are allocated where they are not given.
     """
 
     def __init__(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor,
@@ -175,17 +175,16 @@ class TreeAttention(_Call):
         _need(q.dim() == 3 and q.dtype == k_cache.dtype and q.shape[2] == d and q.stride(2) == 1,
               f"q: [rows, q_heads, {d}] {k_cache.dtype} with dense heads")
         rows, q_heads = q.shape[0], q.shape[1]
-        if max_rows is None or max_keys is None:
-            count = row_offsets.diff()
-            if max_rows is None:
-                max_rows = max(1, int(count.max()))
-            if max_keys is None:
-                max_keys = max(1, int((cache_lens + count).max()))
         words = 0
         if tree_mask is not None:
             _need(tree_mask.dim() == 2, "tree_mask: [rows, words]")
             words = tree_mask.shape[1]
             _flat("tree_mask", tree_mask, torch.int32, (rows, words))
+        if max_rows is None:
+            max_rows = rows if tree_mask is None else min(rows, 32 * words)
+            _need(max_rows <= 65535, "max_rows: to be given for more than 65535 rows (a sequence has that many at most)")
+        if max_keys is None:
+            max_keys = min(pages.shape[1] * page_size, 2 ** 31 - 1)
         own = []
         if out is None:
             out = torch.empty((rows, q_heads, d), dtype=q.dtype, device=q.device)
@@ -214,7 +213,16 @@ class TreeAttention(_Call):
 
 def tree_attention(q, k_cache, v_cache, pages, row_offsets, cache_lens, max_rows=None, max_keys=None, tree_mask=None,
                    scale=None, out=None, lse=None, want_lse=False, stream=None):
-    """One-shot knn_tree_attention: out, or (out, lse) with an lse."""
+    """One-shot knn_tree_attention: out, or (out, lse) with an lse.  max_rows and max_keys that are not given come from the
+    tensors' present contents, which are copied to the host for that."""
+    if max_rows is None or max_keys is None:
+        _flat("row_offsets", row_offsets, torch.int64, (pages.shape[0] + 1,))
+        _flat("cache_lens", cache_lens, torch.int32, (pages.shape[0],))
+        count = row_offsets.diff()
+        if max_rows is None:
+            max_rows = max(1, int(count.max()))
+        if max_keys is None:
+            max_keys = max(1, int((cache_lens + count).max()))
     call = TreeAttention(q, k_cache, v_cache, pages, row_offsets, cache_lens, max_rows, max_keys, tree_mask, scale, out,
                          lse, want_lse)
     call.run(stream)

@@ -404,3 +404,21 @@ def test_a_long_flat_tail_behind_one_heavy_key(rows, heads, dtype):
     assert (out.double() - want).abs().max() <= 3 * e * want + 2.0 ** -16
     sums = n // 32 // (4 if rows == 1 else 1)
     assert (lse.double() - 17.0 - np.log1p(mass)).abs().max() <= e * mass + 2.0 ** -16 + 18 * 2.0 ** -22 + sums * 2.0 ** -23
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_calls_without_hints_follow_lengths_and_rows(tree):
+    """One object, made when the sequences were short, on the tensors' contents of later steps: longer caches, and rows that
+    went from one sequence to the other."""
+    x, mask, sees = batch("bf16", [2, 2], [30, 40], (4, 2), 64, 16, seed=22, width=8, tree=tree)
+    g = torch.Generator().manual_seed(1)
+    x["k_cache"], x["v_cache"] = (torch.randn(16, 2, 16, 64, generator=g).bfloat16().cuda() for _ in range(2))
+    x["pages"] = torch.randperm(16, generator=g).view(2, 8).int().cuda()
+    call = knn.TreeAttention(*[x[n] for n in NAMES], tree_mask=mask, want_lse=True)
+    for lens, off in (([30, 40], [0, 2, 4]), ([31, 41], [0, 2, 4]), ([126, 3], [0, 2, 4]), ([5, 125], [0, 1, 4]),
+                      ([70, 80], [0, 4, 4]), ([124, 0], [0, 4, 4]), ([0, 0], [0, 0, 4])):
+        x["cache_lens"].copy_(torch.tensor(lens, dtype=torch.int32))
+        x["row_offsets"].copy_(torch.tensor(off))
+        call.run()
+        torch.cuda.synchronize()
+        compare(x, call.out, call.lse, sees, 1 / 8)
