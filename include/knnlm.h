@@ -429,8 +429,8 @@ knn_status knn_mix_rrc(const int32_t *nbr_ids, const float *nbr_dists, const int
  *   source_count   rows that q, k and v hold (>= rows without source_rows).
  *   rot_dim        even, 0..head_dim: the first rot_dim elements of a head are rotated, in pairs (i, i + rot_dim / 2),
  *                  or (2 i, 2 i + 1) with interleaved != 0; the others are copied.
- *   q_out          [rows, q_heads, head_dim] dense; may be q itself where q is dense and source_rows NULL, and lies
- *                  apart from it otherwise.
+ *   q_out          [rows, q_heads, head_dim] dense; may be q itself where q is dense (of a single row or head its stride
+ *                  says nothing) and source_rows NULL, and lies apart from it otherwise.
  *   k_cache, v_cache   written at the rows' indices; nothing else of them is touched.  Where two rows name one slot
  *                  (two sequences that share a page), its elements are of either.
  * head_dim up to 1024 (KNN_ERR_UNSUPPORTED above).

@@ -134,8 +134,9 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
         return KNN_ERR_INVALID_ARG;
     if (head_dim > 1024 || q_heads > KNNLM_MAX_HEADS || rows > 0x7fffffff || source_count > 0x7fffffff)
         return KNN_ERR_UNSUPPORTED;
-    const bool in_place = q == q_out && source_rows == nullptr && q_head_stride == head_dim &&
-                          q_row_stride == q_heads * head_dim;
+    // (the stride of a single row or head says nothing)
+    const bool in_place = q == q_out && source_rows == nullptr && (q_heads == 1 || q_head_stride == head_dim) &&
+                          (rows == 1 || q_row_stride == q_heads * head_dim);
     if (q != nullptr && !in_place &&
         overlaps(q, source_count, q_heads, head_dim, q_row_stride, q_head_stride, q_out, rows))
         return KNN_ERR_INVALID_ARG;

@@ -214,3 +214,20 @@ def test_another_stream_and_refusals():
     f = [t.float() if t.is_floating_point() else t for t in args]
     with pytest.raises(knn.KnnError):
         knn.kv_append(*f)
+
+
+def test_one_row_or_head_in_place():
+    """Dense to torch, whatever the stride of a dimension of one: a decoding token's part of a projection, a single head."""
+    x = batch("bf16", [1], [10], (4, 2), 128, 16, 128, seed=17)
+    want = check(dict(x, q_out=torch.zeros_like(x["q"])))[0]
+    qkv = torch.cat([x["q"], x["k"], x["v"]], dim=1)
+    q = qkv[:, :4]
+    names = ("k_cache", "v_cache", "pages", "row_offsets", "cache_lens")
+    got = knn.kv_append(qkv[:, 4:6], qkv[:, 6:], *[x[n] for n in names], q=q, q_out=q, inv_freq=x["inv_freq"])
+    assert got is q and (np.abs(host(got) - want) <= 2.0 ** -8 * np.abs(want) + 4e-6).all()
+    assert torch.equal(qkv[:, 4:6], x["k"]) and torch.equal(qkv[:, 6:], x["v"])
+    x = batch("f16", [3], [10], (1, 1), 64, 16, 64, seed=18)
+    want = check(dict(x, q_out=torch.zeros_like(x["q"])))[0]
+    q = x["q"].as_strided((3, 1, 64), (64, 999, 1))
+    got = knn.kv_append(x["k"], x["v"], *[x[n] for n in names], q=q, q_out=q, inv_freq=x["inv_freq"])
+    assert got is q and (np.abs(host(got) - want) <= 2.0 ** -11 * np.abs(want) + 4e-6 + 2.0 ** -25).all()
