@@ -476,8 +476,8 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
  * finite makes NaN that element of what sees it, whatever its key's weight (and
  * so do finite ones whose weighted sums pass the range of fp32, as of bf16 values
  * over 2^100 they may).  head_dim is 64, 128 or 256, q and the caches
- * and out lie on 16 bytes and the strides are multiples of 8 elements
- * (KNN_ERR_UNSUPPORTED otherwise).
+ * and out lie on 16 bytes and the strides (of more than one row or head) are
+ * multiples of 8 elements (KNN_ERR_UNSUPPORTED otherwise).
  */
 knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_cache, const int32_t *pages,
                               const int64_t *row_offsets, const int32_t *cache_lens, const uint32_t *tree_mask,

@@ -91,8 +91,9 @@ knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_
     if (max_keys > table_width * page_size || !isfinite(scale) || q_row_stride < 0 || q_head_stride < 0)
         return KNN_ERR_INVALID_ARG;
     if (tree_mask != nullptr && mask_words * 32 < max_rows) return KNN_ERR_INVALID_ARG;
-    if ((q_row_stride | q_head_stride) % 8 != 0 || !aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) ||
-        !aligned(out, 16))
+    // (the stride of a single row or head says nothing)
+    if (((rows > 1 ? q_row_stride : 0) | (q_heads > 1 ? q_head_stride : 0)) % 8 != 0 ||
+        !aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16))
         return KNN_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 256) ||
         workspace_bytes < knn_tree_attention_workspace_size(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys))

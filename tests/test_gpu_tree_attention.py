@@ -422,3 +422,12 @@ def test_calls_without_hints_follow_lengths_and_rows(tree):
         call.run()
         torch.cuda.synchronize()
         compare(x, call.out, call.lse, sees, 1 / 8)
+
+
+@pytest.mark.parametrize("rows,heads,strides", [(1, (4, 2), (333, 64)), (3, (1, 1), (64, 77)), (1, (1, 1), (13, 7))])
+def test_strides_of_a_single_row_or_head_say_nothing(rows, heads, strides):
+    x, _, _ = batch("bf16", [rows], [90], heads, 64, 16, seed=23)
+    want = check(x)
+    q = torch.zeros(2000, dtype=torch.bfloat16, device="cuda").as_strided((rows, heads[0], 64), (*strides, 1))
+    q.copy_(x["q"])
+    assert torch.equal(check(dict(x, q=q)), want)
