@@ -430,8 +430,10 @@ knn_status knn_mix_rrc(const int32_t *nbr_ids, const float *nbr_dists, const int
  *   rot_dim        even, 0..head_dim: the first rot_dim elements of a head are rotated, in pairs (i, i + rot_dim / 2),
  *                  or (2 i, 2 i + 1) with interleaved != 0; the others are copied.
  *   q_out          [rows, q_heads, head_dim] dense; may be q itself where q is dense (of a single row or head its stride
- *                  says nothing) and source_rows NULL, and lies apart from it otherwise.
- *   k_cache, v_cache   written at the rows' indices; nothing else of them is touched.  Where two rows name one slot
+ *                  says nothing) and source_rows NULL, and lies apart from it otherwise, and from all else.
+ *   k_cache, v_cache   written at the rows' indices; nothing else of them is touched.  All that is read lies apart from
+ *                  them (KNN_ERR_INVALID_ARG: rows that move within a cache would be read after others have been
+ *                  written there).  Where two rows name one slot
  *                  (two sequences that share a page), its elements are of either.
  * head_dim up to 1024 (KNN_ERR_UNSUPPORTED above).
  */
@@ -465,7 +467,8 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
  *                  and 2^31 - 1.  It decides how the work is split: a bound near the longest sequence is the fastest.
  *                  Rows and keys past a hint that is too low are left out.
  *   scale          finite; 1 / sqrt(head_dim) as a rule.
- *   out            [rows, q_heads, head_dim] dtype, dense, apart from q.  A row that sees no key gets 0.
+ *   out            [rows, q_heads, head_dim] dtype, dense.  A row that sees no key gets 0.  out, lse and workspace lie
+ *                  apart from all that is read and from each other (KNN_ERR_INVALID_ARG).
  *   lse            [rows, q_heads] fp32 or NULL: the natural logarithm of the weights' sum (-inf for such a row).
  *   workspace      knn_tree_attention_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
  *
@@ -514,7 +517,8 @@ size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_head
  * weight of those that stay exceeds uniform times their sum.  T <= 0 or NaN
  * takes the first element of the order.  NaN filters are off.
  *
- *   token          [rows] int32 out; -1 where nothing is present.
+ *   token          [rows] int32 out; -1 where nothing is present.  The three outputs lie apart from the scores and from
+ *                  each other (KNN_ERR_INVALID_ARG).
  *   prob           [rows] fp32 out or NULL: its share of the weight that stays (0 for token -1).
  *   kept           [rows] int32 out or NULL: how many stay.
  *   workspace      knn_sample_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.

@@ -52,15 +52,35 @@ knn_status check_sample(int64_t rows, int64_t V, knn_dtype dtype) {
     return rows > 0x7fffffff || V > kSampleMaxV ? KNN_ERR_UNSUPPORTED : KNN_OK;
 }
 
-// Whether an input of [rows, heads, head_dim] 16-bit elements with these strides and a dense output of `out_rows` rows
-// lie on common bytes.
-bool overlaps(const void *in, int64_t rows, int64_t heads, int64_t head_dim, int64_t row, int64_t head, const void *out,
-              int64_t out_rows) {
-    const double in_bytes = 2.0 * (static_cast<double>(rows - 1) * row + static_cast<double>(heads - 1) * head + head_dim);
-    const double out_bytes = 2.0 * out_rows * heads * head_dim;  // doubles: no sum of strides can pass them
-    const double apart = static_cast<double>(reinterpret_cast<uintptr_t>(out)) -
-                         static_cast<double>(reinterpret_cast<uintptr_t>(in));
-    return apart < in_bytes && -apart < out_bytes;
+// The bytes from the first to the last of a buffer (null: none), in doubles: no sum of strides can pass them.
+struct Extent {
+    const void *at;
+    double bytes;
+};
+
+// Of [rows, heads, head_dim] 16-bit elements with these strides; of n elements of `size` bytes.
+Extent strided(const void *at, int64_t rows, int64_t heads, int64_t head_dim, int64_t row, int64_t head) {
+    return Extent{at, 2.0 * (static_cast<double>(rows - 1) * row + static_cast<double>(heads - 1) * head + head_dim)};
+}
+Extent dense(const void *at, double n, int size) { return Extent{at, n * size}; }
+
+bool meet(const Extent &a, const Extent &b) {
+    if (a.at == nullptr || b.at == nullptr) return false;
+    const double apart = static_cast<double>(reinterpret_cast<uintptr_t>(b.at)) -
+                         static_cast<double>(reinterpret_cast<uintptr_t>(a.at));
+    return apart < a.bytes && -apart < b.bytes;
+}
+
+// Whether an output lies on an input or on another output.
+template <size_t N, size_t M>
+bool any_meet(const Extent (&outputs)[N], const Extent (&inputs)[M]) {
+    for (size_t i = 0; i < N; ++i) {
+        for (const Extent &in : inputs)
+            if (meet(outputs[i], in)) return true;
+        for (size_t j = 0; j < i; ++j)
+            if (meet(outputs[i], outputs[j])) return true;
+    }
+    return false;
 }
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -95,10 +115,21 @@ knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_
     if (((rows > 1 ? q_row_stride : 0) | (q_heads > 1 ? q_head_stride : 0)) % 8 != 0 ||
         !aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16))
         return KNN_ERR_UNSUPPORTED;
-    if (!workspace || !aligned(workspace, 256) ||
-        workspace_bytes < knn_tree_attention_workspace_size(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys))
-        return KNN_ERR_WORKSPACE;
-    if (overlaps(q, rows, q_heads, head_dim, q_row_stride, q_head_stride, out, rows)) return KNN_ERR_INVALID_ARG;
+    const size_t need =
+        knn_tree_attention_workspace_size(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return KNN_ERR_WORKSPACE;
+    const double cells = static_cast<double>(n_pages) * kv_heads * page_size * head_dim;
+    const Extent outputs[] = {dense(out, static_cast<double>(rows) * q_heads * head_dim, 2),
+                              dense(lse, static_cast<double>(rows) * q_heads, 4),
+                              dense(workspace, static_cast<double>(need), 1)};
+    const Extent inputs[] = {strided(q, rows, q_heads, head_dim, q_row_stride, q_head_stride),
+                             dense(k_cache, cells, 2),
+                             dense(v_cache, cells, 2),
+                             dense(pages, static_cast<double>(S) * table_width, 4),
+                             dense(row_offsets, static_cast<double>(S) + 1, 8),
+                             dense(cache_lens, static_cast<double>(S), 4),
+                             dense(tree_mask, static_cast<double>(rows) * mask_words, 4)};
+    if (any_meet(outputs, inputs)) return KNN_ERR_INVALID_ARG;
     AttendArgs a{};
     a.q = q, a.k_cache = k_cache, a.v_cache = v_cache;
     a.row_offsets = row_offsets, a.cache_lens = cache_lens, a.tree_mask = tree_mask;
@@ -138,9 +169,26 @@ knn_status knn_kv_append(const void *q, const void *k, const void *v, const int6
     // (the stride of a single row or head says nothing)
     const bool in_place = q == q_out && source_rows == nullptr && (q_heads == 1 || q_head_stride == head_dim) &&
                           (rows == 1 || q_row_stride == q_heads * head_dim);
-    if (q != nullptr && !in_place &&
-        overlaps(q, source_count, q_heads, head_dim, q_row_stride, q_head_stride, q_out, rows))
+    // (The two caches may be one: what is written to them is the caller's.)
+    const double cells = static_cast<double>(n_pages) * kv_heads * page_size * head_dim;
+    const Extent caches[] = {dense(k_cache, cells, 2), dense(v_cache, cells, 2)};
+    const Extent turned[] = {dense(q_out, static_cast<double>(rows) * q_heads * head_dim, 2)};
+    const Extent queries = strided(q, source_count, q_heads, head_dim, q_row_stride, q_head_stride);
+    const Extent inputs[] = {strided(k, source_count, kv_heads, head_dim, k_row_stride, k_head_stride),
+                             strided(v, source_count, kv_heads, head_dim, v_row_stride, v_head_stride),
+                             dense(pages, static_cast<double>(S) * table_width, 4),
+                             dense(row_offsets, static_cast<double>(S) + 1, 8),
+                             dense(cache_lens, static_cast<double>(S), 4),
+                             dense(positions, static_cast<double>(rows), 4),
+                             dense(inv_freq, static_cast<double>(rot_dim) / 2, 4),
+                             dense(source_rows, static_cast<double>(rows), 4)};
+    if ((!in_place && meet(turned[0], queries)) || any_meet(turned, inputs) || any_meet(turned, caches))
         return KNN_ERR_INVALID_ARG;
+    for (const Extent &c : caches) {
+        if (meet(c, queries)) return KNN_ERR_INVALID_ARG;
+        for (const Extent &in : inputs)
+            if (meet(c, in)) return KNN_ERR_INVALID_ARG;
+    }
     AppendArgs a{};
     a.q = q, a.k = k, a.v = v;
     a.row_offsets = row_offsets, a.cache_lens = cache_lens, a.positions = positions;
@@ -172,6 +220,11 @@ knn_status knn_sample(const void *scores, const float *uniforms, const float *te
     if (!aligned(scores, dtype == KNN_F32 ? 4 : 2)) return KNN_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < knn_sample_workspace_size(rows, V, dtype))
         return KNN_ERR_WORKSPACE;
+    const double elements = static_cast<double>(rows - 1) * row_stride + V;
+    const Extent outputs[] = {dense(token, static_cast<double>(rows), 4), dense(prob, static_cast<double>(rows), 4),
+                              dense(kept, static_cast<double>(rows), 4)};
+    const Extent inputs[] = {dense(scores, elements, dtype == KNN_F32 ? 4 : 2)};
+    if (any_meet(outputs, inputs)) return KNN_ERR_INVALID_ARG;
     SampleArgs a{};
     a.scores = scores, a.uniforms = uniforms;
     a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p;

@@ -120,3 +120,32 @@ def test_limits_of_lengths_and_alignment(lib):
     assert lib.knn_tree_attention_workspace_size(32, 2, 8, 2, 128, 16, (1 << 31) - 1) > 0
     assert lib.knn_tree_attention_workspace_size(32, 2, 8, 2, 128, 16, 1 << 31) == 0
     assert lib.knn_sample(*dict(SAMPLE, scores=FAKE + 1).values()) == UNSUPPORTED
+
+
+MB = 1 << 20
+# the buffers of each call a megabyte and more apart
+APART = {"append": dict(APPEND, **{n: (2 + i) * MB for i, n in enumerate((
+             "q", "k", "v", "row_offsets", "cache_lens", "pages", "positions", "inv_freq", "source_rows", "q_out",
+             "k_cache", "v_cache"))}),
+         "attend": dict(ATTEND, **{n: (2 + 2 * i) * MB for i, n in enumerate((
+             "q", "k_cache", "v_cache", "pages", "row_offsets", "cache_lens", "tree_mask", "out", "lse", "workspace"))}),
+         "sample": dict(SAMPLE, **{n: (2 + i) * MB for i, n in enumerate((
+             "scores", "uniforms", "temperature", "top_k", "top_p", "min_p", "token", "prob", "kept", "workspace"))})}
+NAMES = {"append": "knn_kv_append", "attend": "knn_tree_attention", "sample": "knn_sample"}
+
+
+@pytest.mark.parametrize("call,output,other,off", [
+    ("append", "q_out", n, 0) for n in ("q", "k", "v", "row_offsets", "cache_lens", "pages", "positions", "inv_freq",
+                                        "source_rows", "k_cache", "v_cache")] + [
+    ("append", c, n, 0) for c in ("k_cache", "v_cache") for n in ("q", "k", "v", "row_offsets", "cache_lens", "pages",
+                                                                  "positions", "inv_freq", "source_rows")] + [
+    ("append", "k_cache", "k", 3 * 256 * 2 + 254), ("append", "k_cache", "v", -10 * 2 * 16 * 128 * 2 + 2)] + [
+    ("attend", o, n, 0) for o in ("out", "lse", "workspace") for n in (
+        "q", "k_cache", "v_cache", "pages", "row_offsets", "cache_lens", "tree_mask")] + [
+    ("attend", "out", "lse", 0), ("attend", "lse", "workspace", 0), ("attend", "workspace", "out", 256)] + [
+    ("sample", o, "scores", (4 * 1000 - 1) * 4) for o in ("token", "prob", "kept")] + [
+    ("sample", "token", "prob", 12), ("sample", "prob", "kept", -12), ("sample", "kept", "token", 0)])
+def test_outputs_apart_from_all_that_is_read(lib, call, output, other, off):
+    """An output that lies on an input, at its first byte or on the last, or on another output, is refused."""
+    args = APART[call]
+    assert getattr(lib, NAMES[call])(*dict(args, **{output: args[other] + off}).values()) == INVALID
