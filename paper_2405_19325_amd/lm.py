@@ -37,8 +37,10 @@ def _flat(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple
 
 class _Call:
     """A call that is made again and again on one GPU, with the same buffers where they are.  Its runs share their
-    outputs and workspace, so they follow each other on one stream or wait for each other.  A graph that captured one
-    replays on its buffers: keep the object as long as the graph."""
+    outputs and workspace, so they follow each other on one stream or wait for each other.  A stream that it runs on for
+    the first time waits for the one that was current when it was made: what that one still does may be with the memory
+    that the outputs and the workspace were given.  A graph that captured one replays on its buffers: keep the object as
+    long as the graph."""
 
     def _keep(self, index: int, name: str, args: Sequence, tensors: Sequence, own: Sequence[torch.Tensor]):
         """`name`: the library's function; `args`: its arguments but the stream, converted once; `tensors`: what they
@@ -47,7 +49,8 @@ class _Call:
         self._name, self._fn = name, fn
         self._args = tuple(a if a is None else kind(a) for kind, a in zip(fn.argtypes, args))
         self._index, self._tensors, self._own = index, tuple(tensors), tuple(own)
-        self._known = {_stream(None)}
+        self._home = _stream(None)
+        self._known = {self._home}
 
     def _call(self, stream):
         if torch.cuda.current_device() != self._index:
@@ -55,7 +58,9 @@ class _Call:
         h = _stream(stream)
         if h not in self._known:  # the allocator has to know who else uses what this object allocated
             if not torch.cuda.is_current_stream_capturing():
-                s = torch.cuda.ExternalStream(h) if h else torch.cuda.default_stream()
+                s, home = (torch.cuda.ExternalStream(i) if i else torch.cuda.default_stream() for i in (h, self._home))
+                if self._own:
+                    s.wait_stream(home)
                 for t in self._own:
                     t.record_stream(s)
                 self._known.add(h)

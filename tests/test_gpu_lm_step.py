@@ -214,3 +214,31 @@ def test_two_calls_at_once_and_a_graph_of_all():
         assert all(torch.equal(a, b) for a, b in zip(got, want[i % 3, 0])), i
         p.run()  # the program's own work between the replays
         torch.cuda.synchronize()
+
+
+def test_outputs_on_another_stream_wait_for_the_memory_they_took():
+    """A block that the current stream still reads is freed; the next outputs get it, and are written on another stream."""
+    S, heads, d, page = 2048, 64, 128, 16
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn(64, 8, page, d, generator=g).bfloat16().cuda() for _ in range(2))
+    q = torch.randn(S, heads, d, generator=g).bfloat16().cuda()  # 32 MiB, as the outputs: a block of its own
+    pages = (torch.arange(S, dtype=torch.int32) % 64).view(S, 1).cuda()
+    off, lens = torch.arange(S + 1).cuda(), torch.full((S,), 7, dtype=torch.int32, device="cuda")
+    rows = dict(max_rows=1, max_keys=8)
+    want = knn.tree_attention(q, k, v, pages, off, lens, **rows)
+    x = torch.randn(4096, 4096, generator=g).bfloat16().cuda()
+    side = torch.cuda.Stream()
+    y = x @ x
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()  # no other free block of that size
+    first = torch.full_like(q, 3.0)
+    for _ in range(40):
+        y = x @ x
+    second = first.clone()  # behind the products
+    at = first.data_ptr()
+    del first
+    out = knn.tree_attention(q, k, v, pages, off, lens, stream=side, **rows)
+    torch.cuda.synchronize()
+    if out.data_ptr() != at:
+        pytest.skip("the allocator gave the outputs another block")
+    assert (second == 3.0).all() and torch.equal(out, want)

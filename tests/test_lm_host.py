@@ -149,3 +149,44 @@ def test_outputs_apart_from_all_that_is_read(lib, call, output, other, off):
     """An output that lies on an input, at its first byte or on the last, or on another output, is refused."""
     args = APART[call]
     assert getattr(lib, NAMES[call])(*dict(args, **{output: args[other] + off}).values()) == INVALID
+
+
+@pytest.mark.parametrize("home,stream", [(0, 7), (5, 7), (5, 0)])
+def test_another_stream_waits_once_for_where_the_buffers_came_from(monkeypatch, home, stream):
+    """The order of things on streams that only write down what they are asked for."""
+    from paper_2405_19325_amd import lm
+
+    log = []
+
+    class Stream:
+        def __init__(self, handle=0):
+            self.cuda_stream = handle
+
+        def wait_stream(self, other):
+            log.append(("wait", self.cuda_stream, other.cuda_stream))
+
+    class Buffer:
+        def record_stream(self, s):
+            log.append(("record", s.cuda_stream))
+
+    for name, fake in (("current_device", lambda: 0), ("is_current_stream_capturing", lambda: False),
+                       ("ExternalStream", Stream), ("default_stream", Stream)):
+        monkeypatch.setattr(lm.torch.cuda, name, fake)
+    monkeypatch.setattr(lm, "_stream", lambda s=None: home if s is None else s)
+
+    class Library:
+        @staticmethod
+        def call(*args):
+            log.append(("run", args[-1]))
+            return OK
+
+    Library.call.argtypes = []
+    monkeypatch.setattr(lm, "load", lambda: Library)
+    c = lm._Call()
+    c._keep(0, "call", (), (), (Buffer(),))
+    c._call(None)
+    assert log == [("run", home)]
+    del log[:]
+    c._call(stream)
+    c._call(stream)
+    assert log == [("wait", stream, home), ("record", stream), ("run", stream), ("run", stream)]
