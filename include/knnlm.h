@@ -490,7 +490,7 @@ knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_
                               knn_dtype dtype, float scale, void *out, float *lse, void *workspace,
                               size_t workspace_bytes, void *stream);
 
-/* Bytes of workspace knn_tree_attention needs for these sizes (0 if they are invalid). */
+/* Bytes of workspace knn_tree_attention needs for these sizes: at most 512 MiB (0 if they are invalid). */
 size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                                          int64_t max_rows, int64_t max_keys);
 

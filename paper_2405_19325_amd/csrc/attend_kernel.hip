@@ -41,7 +41,8 @@ constexpr float kSlack = 8.0f;
 constexpr float kBelow = 7.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int64_t kWhole = 256;  // keys of a head that is not parted
+constexpr int64_t kWhole = 256;   // keys of a head that is not parted
+constexpr int64_t kWide = 16384;  // workgroups of a wide call
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -490,7 +491,7 @@ __device__ __forceinline__ void each_span(const AttendArgs &a, int64_t tiles, in
     const int g = a.q_heads / a.kv_heads;
     while (true) {
         const int n = static_cast<int>(steps - step < stop - pos ? steps - step : stop - pos);
-        const int c0 = static_cast<int>(at.ct) * cols, all = t.n * g;
+        const int c0 = static_cast<int>(a.first_tile + at.ct) * cols, all = t.n * g;
         if (c0 < all) {
             int64_t end = static_cast<int64_t>(step + n) * step_keys;
             if (end > t.total) end = t.total;
@@ -632,7 +633,7 @@ template <knn_dtype DT, int D, int NT>
 __global__ __launch_bounds__(Shape<D>::W * 64, NT == 1 && D < 256 ? 2 : 1) void k_attend(AttendArgs a, int64_t tiles, int64_t teams, int step,
                                                                 int stages, float *part, float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
-    const int c0 = static_cast<int>(place_of(tiles).ct) * (16 * NT);
+    const int c0 = static_cast<int>(a.first_tile + place_of(tiles).ct) * (16 * NT);
     each_span<D>(a, tiles, teams, step, 16 * NT, part, part_ml,
                  [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
                      span_few<DT, D, NT>(a, t, s, h, c0, k0, end, stages, lds, to, to_ml);
@@ -739,7 +740,7 @@ template <knn_dtype DT, int D, int NT>
 __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a, int64_t tiles, int64_t teams, int step,
                                                                       float *part, float *part_ml) {
     extern __shared__ __align__(16) u32x4_t lds[];
-    const int c0 = static_cast<int>(place_of(tiles).ct) * (64 * NT);
+    const int c0 = static_cast<int>(a.first_tile + place_of(tiles).ct) * (64 * NT);
     each_span<D>(a, tiles, teams, step, 64 * NT, part, part_ml,
                  [&](const Tile &t, int64_t s, int h, int64_t k0, int64_t end, float *to, float *to_ml) {
                      span_many<DT, D, NT>(a, t, s, h, c0, k0, end, lds, to, to_ml);
@@ -750,12 +751,17 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a, int64_t ti
 // wave each: the references of up to 64 parts at once, a lane each, then the
 // parts' outputs.
 template <knn_dtype DT, int D>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles, int64_t teams, int step, int cols,
-                                                     const float *part, const float *part_ml) {
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles, int64_t all_tiles, int64_t teams, int step,
+                                                     int cols, const float *part, const float *part_ml) {
     constexpr int PER = D / 64;  // elements of a lane
     const int lane = threadIdx.x & 63;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // (row, query head)
-    const int64_t heads = a.q_heads, row = static_cast<int64_t>(quotient(static_cast<uint64_t>(at), static_cast<uint64_t>(heads)));
+    const int64_t heads = a.q_heads;
+    int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // (row, query head)
+    if (tiles < all_tiles) {  // of sequence blockIdx.y, from the first row that has columns in these tiles
+        at += (a.row_offsets[blockIdx.y] + a.first_tile * cols / (heads / a.kv_heads)) * heads;
+        if (at >= a.row_offsets[blockIdx.y + 1] * heads) return;
+    }
+    const int64_t row = static_cast<int64_t>(quotient(static_cast<uint64_t>(at), static_cast<uint64_t>(heads)));
     if (row >= a.rows || row >= a.row_offsets[a.S]) return;  // the whole wave
     Runs runs(a, teams, step);
     int64_t s = 0;
@@ -767,7 +773,9 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles
     const Tile t = runs.tile(lane_of);
     if (row - t.r0 >= t.n) return;
     const int g = a.q_heads / a.kv_heads, head = static_cast<int>(at - row * heads), h = head / g;
-    const int col = static_cast<int>(row - t.r0) * g + head - h * g, ct = col / cols, c = col - ct * cols;
+    const int col = static_cast<int>(row - t.r0) * g + head - h * g, c = col % cols;
+    const int64_t ct = col / cols - a.first_tile;
+    if (ct < 0 || ct >= tiles) return;  // of another launch
     const uint64_t steps = static_cast<uint64_t>(steps_of(t, step));
     const uint64_t first = runs.before(lane_of) * static_cast<uint64_t>(a.kv_heads) + static_cast<uint64_t>(h) * steps;
     const int64_t w0 = runs.team_of(first), w1 = runs.team_of(first + steps - 1);
@@ -814,17 +822,25 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles
 }
 
 template <knn_dtype DT, int D>
-hipError_t launch(const AttendArgs &a, const AttendPlan &p, float *part, float *part_ml, hipStream_t stream) {
-    const int64_t blocks = p.teams * p.tiles, joins = (a.rows * a.q_heads + 3) / 4;
-    if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<unsigned>(blocks)), few(Shape<D>::W * 64);
+hipError_t launch(AttendArgs a, const AttendPlan &p, float *part, float *part_ml, hipStream_t stream) {
+    if (p.teams * p.tiles > 0x7fffffffLL || (a.rows * a.q_heads + 3) / 4 > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const dim3 few(Shape<D>::W * 64);
     constexpr int N = D < 256 ? D : 64;  // (the wider kinds are not taken at 256)
-    if (p.cols == 16) k_attend<DT, D, 1><<<grid, few, Shape<D>::few_lds(p.stages), stream>>>(a, p.tiles, p.teams, p.step, p.stages, part, part_ml);
-    else if (p.cols == 32) k_attend<DT, N, 2><<<grid, few, Shape<D>::few_lds(p.stages), stream>>>(a, p.tiles, p.teams, p.step, p.stages, part, part_ml);
-    else if (p.cols == 64) k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
-    else k_attend_many<DT, N, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, p.tiles, p.teams, p.step, part, part_ml);
-    if (p.total > 0)
-        k_attend_join<DT, D><<<static_cast<unsigned>(joins), 256, 0, stream>>>(a, p.tiles, p.teams, p.step, p.cols, part, part_ml);
+    const int64_t g = a.q_heads / a.kv_heads;
+    for (int64_t first = 0; first < p.all_tiles; first += p.tiles) {
+        const int64_t tiles = p.all_tiles - first < p.tiles ? p.all_tiles - first : p.tiles;
+        const dim3 grid(static_cast<unsigned>(p.teams * tiles));
+        a.first_tile = first;
+        if (p.cols == 16) k_attend<DT, D, 1><<<grid, few, Shape<D>::few_lds(p.stages), stream>>>(a, tiles, p.teams, p.step, p.stages, part, part_ml);
+        else if (p.cols == 32) k_attend<DT, N, 2><<<grid, few, Shape<D>::few_lds(p.stages), stream>>>(a, tiles, p.teams, p.step, p.stages, part, part_ml);
+        else if (p.cols == 64) k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, tiles, p.teams, p.step, part, part_ml);
+        else k_attend_many<DT, N, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, tiles, p.teams, p.step, part, part_ml);
+        if (p.total == 0) continue;
+        // All rows, or of each sequence as many as may have columns in these tiles.
+        const int64_t rows = tiles == p.all_tiles ? a.rows : (tiles * p.cols + g - 1) / g + 1;
+        const dim3 joins(static_cast<unsigned>((rows * a.q_heads + 3) / 4), tiles == p.all_tiles ? 1u : static_cast<unsigned>(a.S));
+        k_attend_join<DT, D><<<joins, 256, 0, stream>>>(a, tiles, p.all_tiles, p.teams, p.step, p.cols, part, part_ml);
+    }
     return hipGetLastError();
 }
 
@@ -845,20 +861,31 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
     const int64_t cols = max_rows * (q_heads / kv_heads);
     // (At head_dim 256 the wider kind of either kernel does not fit the registers.)
     p.cols = cols <= 16 ? 16 : cols <= 32 && head_dim < 256 ? 32 : cols <= 64 || head_dim == 256 ? 64 : 128;
-    p.tiles = (cols + p.cols - 1) / p.cols;
+    p.all_tiles = p.tiles = (cols + p.cols - 1) / p.cols;
     // As many workgroups as the CUs hold at once, each with 256 keys or more (many columns: 128); teams a multiple of 8
     // (the XCDs).  Heads of up to kWhole keys are not parted: nothing to join (of 1,001 keys, one token and 32 heads:
-    // 15.8 us, in four parts 14.5).
-    const bool many = p.cols > 32, whole = max_keys <= kWhole;
+    // 15.8 us, in four parts 14.5).  Nor are those of wide calls, whose column tiles alone leave room for fewer than 8
+    // teams, where there are 8 heads or more: a workgroup each for a head and a tile (up to kWide of them, since most have
+    // no column where one sequence of many is long) fill the CUs as they get free, whatever a chain's tiles see.  @@
+    const int64_t heads = S * kv_heads;
+    const bool many = p.cols > 32, wide = p.tiles > 64 && heads >= 8 && max_keys <= (int64_t{1} << 30);
+    const bool whole = max_keys <= kWhole || wide;
     p.step = whole ? static_cast<int>((max_keys + 63) / 64 * 64) : 64;
     p.stages = p.cols == 16 && max_keys <= 32 * (head_dim == 256 ? 2 : 4) ? 1 : 2;
-    int64_t slots = 512;
+    int64_t slots = wide ? kWide : 512;
     if (!many && head_dim >= 128 && p.stages == 2) slots = 256;
-    const int64_t least = many ? 128 : 256, most = S * kv_heads * (whole ? 1 : (max_keys + least - 1) / least);
+    const int64_t least = many ? 128 : 256, most = heads * (whole ? 1 : (max_keys + least - 1) / least);
     p.teams = (most + 7) / 8 * 8;
     if (p.teams * p.tiles > slots) p.teams = slots / p.tiles / 8 * 8;  // one workgroup too many takes a second round
     if (p.teams < 8) p.teams = 8;
-    if (whole) return p;
+    // (The heads of one sequence in as many runs, or in a divisor of their number, are not parted either.)
+    if (whole || (S == 1 && kv_heads % p.teams == 0)) return p;
+    // Under 8 heads and over 64 column tiles there are 8 teams all the same, and parts of 16 times a head's queries in
+    // fp32: 4 GiB for 8,000 rows with 64 heads on one.  In eight launches that share 512 MiB these take 5.75 ms, in one
+    // 5.57.
+    const size_t tile = static_cast<size_t>(p.teams) * 2 * static_cast<size_t>(p.cols) * (static_cast<size_t>(head_dim) + 2) * sizeof(float);
+    const int64_t at_once = static_cast<int64_t>(kAttendParts / tile), launches = (p.tiles + at_once - 1) / at_once;
+    p.tiles = (p.tiles + launches - 1) / launches;
     const size_t cells = static_cast<size_t>(p.teams * p.tiles) * 2 * static_cast<size_t>(p.cols);
     p.off_ml = cells * static_cast<size_t>(head_dim) * sizeof(float);
     p.total = p.off_ml + cells * 2 * sizeof(float);

@@ -48,6 +48,7 @@ struct AttendArgs {
     float scale;
     void *out;   // [rows, q_heads, head_dim]
     float *lse;  // [rows, q_heads] or null
+    int64_t first_tile;  // of this launch, where there are several
 };
 
 // How an attention call is cut: column tiles of `cols` (row, query head) pairs
@@ -55,14 +56,16 @@ struct AttendArgs {
 // a workgroup a column tile.  The keys of all sequences and heads lie one
 // behind the other for that, so that every team gets as many, whatever the
 // sequences' lengths; what a team has of a head that others have parts of is
-// joined by a second launch.
+// joined by a second launch.  Where the parts of all column tiles would take
+// more than kAttendParts bytes, the tiles are worked off `tiles` at a time.
 struct AttendPlan {
     int cols;
     int step;    // keys of the steps that runs are counted in; a head of one step is not parted
     int stages;  // few columns: stages of a wave
-    int64_t tiles, teams;
+    int64_t all_tiles, tiles, teams;
     size_t off_ml, total;  // workspace: the parts, then (maximum, sum); two parts a workgroup, or 0
 };
+constexpr size_t kAttendParts = size_t{512} << 20;
 
 AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_rows,
                        int64_t max_keys);

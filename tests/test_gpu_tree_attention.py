@@ -431,3 +431,36 @@ def test_strides_of_a_single_row_or_head_say_nothing(rows, heads, strides):
     q = torch.zeros(2000, dtype=torch.bfloat16, device="cuda").as_strided((rows, heads[0], 64), (*strides, 1))
     q.copy_(x["q"])
     assert torch.equal(check(dict(x, q=q)), want)
+
+
+def some_rows(x, out, lse, rows, scale):
+    """Chains: these rows alone against the oracle, each as a sequence of its own on the tokens before it."""
+    off, lens = x["row_offsets"].cpu(), x["cache_lens"].cpu()
+    seq = torch.searchsorted(off, torch.tensor(rows), right=True) - 1
+    at = torch.tensor(rows)
+    y = dict(x, q=x["q"][rows], pages=x["pages"][seq.cuda()], row_offsets=torch.arange(len(rows) + 1),
+             cache_lens=(lens[seq] + at - off[seq]).int())
+    compare(y, out[rows], lse[rows], None, scale)
+
+
+@pytest.mark.parametrize("dtype,rows,lens,heads,d", [
+    ("bf16", [1100], [0], (64, 1), 128),            # 550 column tiles on one key head: parts in two launches
+    ("f16", [1030, 40, 0], [10, 700, 3], (64, 1), 128),
+    ("bf16", [600], [301], (64, 1), 128),           # parts in one
+    ("f16", [2100], [0], (16, 1), 256),             # the same at 64 columns
+    ("bf16", [1100, 7], [0, 40], (64, 2), 64),
+    ("bf16", [3, 520, 1, 0, 270, 1, 1, 2], [900, 0, 64, 5, 300, 0, 7, 3000], (64, 1), 128),  # eight heads: none parted
+    ("bf16", [1] * 40 + [505] + [2] * 30, [77] * 71, (64, 1), 128),
+    ("bf16", [2000], [0], (8, 8), 128),
+    ("f16", [1500, 700], [0, 1000], (8, 2), 128),
+    ("bf16", [1030], [1000], (64, 8), 64),
+    ("f16", [1030, 1], [0, 200], (64, 4), 256)])
+def test_prompts(dtype, rows, lens, heads, d):
+    x, _, _ = batch(dtype, rows, lens, heads, d, 64, seed=sum(rows))
+    out, lse = torch.full_like(x["q"], 7.0), torch.full((sum(rows), heads[0]), 5.0, device="cuda")
+    knn.tree_attention(*[x[n] for n in NAMES], out=out, lse=lse)
+    torch.cuda.synchronize()
+    T = sum(rows)
+    some_rows(x, out, lse, sorted({int(i) for i in np.linspace(0, T - 1, 17)} | {T // 2 - 1, T // 2 + 1}), d ** -0.5)
+    # every row was written: its largest weighted value is none of the constants
+    assert torch.isfinite(lse).all() and not (out == 7.0).all(2).any() and not (lse == 5.0).any()

@@ -190,3 +190,17 @@ def test_another_stream_waits_once_for_where_the_buffers_came_from(monkeypatch, 
     c._call(stream)
     c._call(stream)
     assert log == [("wait", stream, home), ("record", stream), ("run", stream), ("run", stream)]
+
+
+def test_attention_workspace_is_bounded(lib):
+    """Two parts a workgroup, of column tiles that are worked off so many at a time that 512 MiB hold them; none where no
+    head is parted."""
+    size = lib.knn_tree_attention_workspace_size
+    for rows in (1, 64, 1000, 8000, 32000, 65535):
+        for S in (1, 4, 64):
+            for heads, kv in ((8, 1), (64, 1), (1024, 1), (64, 8), (32, 32), (1024, 16)):
+                for d in (64, 128, 256):
+                    for keys in (rows, 4 * rows, 1 << 20):
+                        assert 0 < size(rows * S, S, heads, kv, d, rows, keys) <= 512 << 20
+    assert size(8000, 1, 64, 8, 128, 8000, 9000) == 256   # eight heads in eight runs
+    assert size(64, 4, 64, 8, 128, 64, 131136) > 1 << 20  # parts all the same where heads lie in several runs
