@@ -523,9 +523,12 @@ size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_head
  *   kept           [rows] int32 out or NULL: how many stay.
  *   workspace      knn_sample_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
  *
- * Weights are in 64 bits and are summed as whole numbers of 2^-s of the
- * largest, s = 62 - ceil(log2(V + 3)) and at most 51, so the outcome is the same bits every time
- * and that of exact arithmetic but for borders that lie that near.
+ * Weights are in 64 bits, right to 2^-50 (1 - ln w) of a weight w, and of
+ * probabilities at another T than 1 to 2^-51 / T more.  They are summed as whole
+ * numbers of 2^-s of the largest, s = 62 - ceil(log2(V + 3)) and at most 51 (of
+ * probabilities at T = 1: of the power of two over the largest), so the outcome
+ * is the same bits every time, and that of exact arithmetic but for borders that
+ * lie that near.
  * V <= 2^24 (KNN_ERR_UNSUPPORTED above).
  */
 knn_status knn_sample(const void *scores, const float *uniforms, const float *temperature, const int32_t *top_k,

@@ -93,10 +93,17 @@ __device__ __forceinline__ double power2(double y, bool in, int e, const double 
     return __hiloint2double(__double2hiint(v) + ((n >> 6) + e) * (1 << 20), __double2loint(v));
 }
 
-// log2 of a positive finite x, to 2^-50: x = 2^e m, and with c one of 64 values
-// near 1 / m, log2 m = -log2 c + log2(1 + r), r = m c - 1, |r| < 2^-6.9, by
-// the series of the logarithm, whose 8th term is 2^-58.
-__device__ __forceinline__ double log2_of(float x, const double2 *logs) {
+// log2 of a positive finite x, its whole part apart from the rest, which is in
+// [0, 1) and right to 2^-52: in one number the rest of a small probability
+// would lose up to 7 bits to the whole part, and 1 / T as much more.  x = 2^e m,
+// and with c one of 64 values near 1 / m, log2 m = -log2 c + log2(1 + r),
+// r = m c - 1, |r| < 2^-6.9, by the series of the logarithm, whose 8th term is
+// 2^-58.
+struct Log2 {
+    double rest;
+    int whole;
+};
+__device__ __forceinline__ Log2 log2_of(float x, const double2 *logs) {
     const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(static_cast<double>(x)));
     const double m = __longlong_as_double(static_cast<long long>((bits & 0x000fffffffffffffull) | 0x3ff0000000000000ull));
     const double2 at = logs[(bits >> 46) & 63];
@@ -108,7 +115,7 @@ __device__ __forceinline__ double log2_of(float x, const double2 *logs) {
     q = fma(q, r, 1.0 / 3.0);
     q = fma(q, r, -1.0 / 2.0);
     q = fma(q, r, 1.0);
-    return fma(r * q, 1.4426950408889634074, at.y) + static_cast<double>(static_cast<int>(bits >> 52) - 1023);
+    return Log2{fma(r * q, 1.4426950408889634074, at.y), static_cast<int>(bits >> 52) - 1023};
 }
 
 // The weights of a row, as a function of the value; the largest one's is 2^s.
@@ -116,7 +123,8 @@ __device__ __forceinline__ double log2_of(float x, const double2 *logs) {
 // a power of two.
 template <bool PROBS>
 struct Weights {
-    double top;    // the largest value, or its log2 where the values are probabilities
+    double top;    // the largest value, or where the values are probabilities its log2: the rest, and
+    int top_whole; // the whole part
     double rate;   // 64 log2(e) / T, or 64 / T of probabilities
     double unit;   // 2^s
     int log2_unit;
@@ -137,7 +145,13 @@ struct Weights {
         } else {
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                const double far = (PROBS ? log2_of(x[c], logs) : static_cast<double>(x[c])) - top;
+                double far;
+                if constexpr (PROBS) {
+                    const Log2 l = log2_of(x[c], logs);
+                    far = (l.rest - top) + static_cast<double>(l.whole - top_whole);
+                } else {
+                    far = static_cast<double>(x[c]) - top;
+                }
                 v[c] = power2(far * rate, in[c], log2_unit, roots);
             }
         }
@@ -384,7 +398,9 @@ __device__ __forceinline__ void draw(const SampleArgs &a, const R &rw, Shared &s
     w.even = top == INFINITY;
     w.roots = sh.roots;
     w.logs = sh.logs;
-    w.top = PROBS ? log2_of(top, sh.logs) : static_cast<double>(top);
+    const Log2 top_log = PROBS ? log2_of(top, sh.logs) : Log2{static_cast<double>(top), 0};
+    w.top = top_log.rest;
+    w.top_whole = top_log.whole;
     w.rate = (PROBS ? 64.0 : 92.332482616893656874) / static_cast<double>(t);
     w.log2_unit = log2_unit - (w.plain && !w.even ? ilogb(static_cast<double>(top)) + 1 : 0);
     w.unit = ldexp(1.0, w.log2_unit);

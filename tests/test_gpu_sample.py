@@ -1,6 +1,7 @@
 """Drawing tokens on the GPU against the fp64 oracle: every filter, ties, borders, absent elements, odd sizes, streams
 and graphs.  Tokens and counts have to be equal."""
 import itertools
+from decimal import Decimal, localcontext
 
 import numpy as np
 import pytest
@@ -283,3 +284,32 @@ def test_min_p_above_one_keeps_the_first_alone():
         check(x, u, probs, min_p=m, top_k=[100] * 8)
         check(x, u, probs, min_p=m, top_k=[1000] * 8, top_p=[0.7] * 8, temperature=[0.5] * 8)
     check(torch.tensor([[1.0, 1.0, 0.0]], device="cuda"), [0.9], min_p=[2.0])
+
+
+@pytest.mark.parametrize("first,second,t,u", [
+    (2.0335712280772356e-10, 2.0255402910507314e-10, 0.013835875317454338, 0.42898452281951904),
+    (2.6456388191320457e-09, 2.6005610997970052e-09, 0.020649559795856476, 0.3031722903251648)])
+def test_small_probabilities_at_a_low_temperature(first, second, t, u):
+    """The share w / (1 + w) of the second, w = (x / max)^(1 / T), lies 2^-45.3 or 2^-46.6 from the uniform.  w is right to
+    2^-51 / T of itself, which moves the share by w / (1 + w)^2 < 1 / 4 of that: 2^-46.8 and 2^-47.6.  A logarithm in one
+    number, of -32 and -28, is off by up to 2^-48 in either, 8 times as much."""
+    with localcontext() as c:
+        c.prec = 60
+        w = ((Decimal(second) / Decimal(first)).ln() / Decimal(t)).exp()
+        share = w / (1 + w)
+        assert 2.0 ** -47 < abs(share - Decimal(u)) < 2.0 ** -45
+        want = 0 if share > Decimal(u) else 1
+    x = torch.tensor([[second, first]], device="cuda")
+    token, _, kept = knn.sample(x, torch.tensor([u], device="cuda"), probabilities=True,
+                                temperature=torch.tensor([t], device="cuda"))
+    assert (int(token[0]), int(kept[0])) == (want, 2)
+
+
+def test_small_probabilities_with_every_filter():
+    x, u = rows_of(8, 4097, "f32", "probs", 13)
+    x *= 1e-6 / x.max(1, keepdim=True).values
+    t = [0.01, 0.02, 0.05, 0.1, 0.3, 1.0, 1.5, 0.015]
+    check(x, u, True, temperature=t)
+    check(x, u, True, temperature=t, top_p=[0.9, 0.5, 0.99, 0.7, 0.9, 0.3, 0.9, 0.999])
+    check(x, u, True, temperature=t, top_k=[3, 50, 300, 7, 1000, 2, 64, 9], min_p=[0.0, 1e-4, 0.01, 0.5, 0.001, 0.2, 0.05, 1e-6])
+    check(x * 1e-30, u, True, temperature=t, top_p=[0.9] * 8)  # into the numbers below fp32's normal range
