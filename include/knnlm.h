@@ -394,7 +394,8 @@ knn_status knn_mix_rrc(const int32_t *nbr_ids, const float *nbr_dists, const int
  * read nor written.  A sequence may own no row.
  *
  * Cache.  k_cache and v_cache are [n_pages, kv_heads, page_size, head_dim];
- * page_size is a power of two from 16 to 65536.  pages [S, table_width] int32
+ * page_size is a power of two from 16 to 65536, and a cache has up to 2^62
+ * elements (KNN_ERR_UNSUPPORTED above).  pages [S, table_width] int32
  * (device) names each sequence's pages: its cache index c lies in page
  * pages[s, c / page_size], slot c % page_size.  cache_lens [S] int32 (device)
  * is the number of tokens of each sequence that are in the cache before the

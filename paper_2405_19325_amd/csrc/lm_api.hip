@@ -24,8 +24,10 @@ knn_status check_cache(int64_t S, int64_t kv_heads, int64_t head_dim, int64_t n_
     if (page_size < 1 || (page_size & (page_size - 1)) != 0) return KNN_ERR_INVALID_ARG;
     if (dtype == KNN_F32 || page_size < 16 || page_size > kMaxPage || kv_heads > KNNLM_MAX_HEADS)
         return KNN_ERR_UNSUPPORTED;
-    // every page starts at an element offset of fewer than 2^62
-    if (n_pages > (int64_t{1} << 31) || S > 0x7fffffff || table_width > 0x7fffffff) return KNN_ERR_UNSUPPORTED;
+    // (every offset in bytes fits 64 bits)
+    if (n_pages > (int64_t{1} << 31) || S > 0x7fffffff || table_width > 0x7fffffff ||
+        static_cast<double>(n_pages) * kv_heads * page_size * head_dim > 4611686018427387904.0)  // 2^62
+        return KNN_ERR_UNSUPPORTED;
     return KNN_OK;
 }
 

@@ -204,3 +204,11 @@ def test_attention_workspace_is_bounded(lib):
                         assert 0 < size(rows * S, S, heads, kv, d, rows, keys) <= 512 << 20
     assert size(8000, 1, 64, 8, 128, 8000, 9000) == 256   # eight heads in eight runs
     assert size(64, 4, 64, 8, 128, 64, 131136) > 1 << 20  # parts all the same where heads lie in several runs
+
+
+def test_caches_whose_offsets_pass_64_bits(lib):
+    """2^62 elements are 2^63 bytes; the limits of each size alone allow 2^67."""
+    for over in (dict(n_pages=1 << 31, kv_heads=1024, q_heads=1024, page_size=65536),
+                 dict(n_pages=1 << 31, kv_heads=512, q_heads=512, page_size=65536)):
+        assert lib.knn_kv_append(*dict(APART["append"], **over).values()) == UNSUPPORTED
+        assert lib.knn_tree_attention(*dict(APART["attend"], **over).values()) == UNSUPPORTED
