@@ -145,8 +145,10 @@ struct Keys {
           slot0(static_cast<int>(k0 & ((int64_t{1} << a.cache.page_log2) - 1))), n_pages(a.cache.n_pages),
           head_bytes(static_cast<int64_t>(h) * 2 * D << a.cache.page_log2),
           page_bytes(static_cast<int64_t>(a.kv_heads) * 2 * D << a.cache.page_log2), last(static_cast<int>(end - 1 - k0)) {}
-    // The page of a key (keys past the last one are read as the last one).
-    __device__ __forceinline__ int32_t entry(int key) const { return table[(slot0 + min(key, last)) >> page_log2]; }
+    // The page of a key (keys past the last one are read as the last one; 32 tiles ahead they may pass 2^31).
+    __device__ __forceinline__ int32_t entry(int64_t key) const {
+        return table[(slot0 + (key < last ? static_cast<int>(key) : last)) >> page_log2];
+    }
     __device__ __forceinline__ bool real(int32_t page) const { return page >= 0 && page < n_pages; }
     // Byte offset of 16 keys from `key` on in either cache; `rows`: the last of them that there is.
     __device__ __forceinline__ int64_t at(int key, int32_t page, int &rows) const {
@@ -545,7 +547,7 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
     // Lane l keeps the page of half l & 1 of this wave's tile l / 2 from tile `held` on.
     int32_t page_reg = 0;
     auto hold_pages = [&](int held) {
-        page_reg = keys.entry(32 * (wave + W * (held + (lane >> 1))) + 16 * (lane & 1));
+        page_reg = keys.entry(int64_t{32} * (wave + W * (held + (lane >> 1))) + 16 * (lane & 1));
     };
     auto page_of = [&](int tile, int half) { return __builtin_amdgcn_readlane(page_reg, 2 * (tile & 31) + half); };
     auto fill = [&](int i) {  // tile i of this wave into stage i & 1
@@ -584,7 +586,7 @@ __device__ __forceinline__ void span_few(const AttendArgs &a, const Tile &t, int
         asm volatile("" ::: "memory");
         const uint32_t kt[1] = {mine + static_cast<uint32_t>(i & 1) * (2 * Sh::HALF)};
         const int key = 32 * (wave + W * i);
-        const bool all = key + 32 <= whole && real_a && real_b;
+        const bool all = key <= whole - 32 && real_a && real_b;
         c.template tile<1>(a, t, kt, k0 + key, all, end, (real_a ? 1u : 0u) | (real_b ? 2u : 0u), col, quad, left_out);
         // the stage is read: the next round's loads may overwrite it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -664,7 +666,7 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
     int32_t page_reg = 0, page_old = 0;
     auto hold_pages = [&](int held) {
         page_old = page_reg;
-        page_reg = keys.entry(32 * (held + (lane >> 1)) + 16 * (lane & 1));
+        page_reg = keys.entry(int64_t{32} * (held + (lane >> 1)) + 16 * (lane & 1));
     };
     const int half = wave >> 1;  // of a tile's 32 keys: which 16 this wave fetches half of
     auto fill = [&](int i) {     // this wave's quarter of tile i into its stage
@@ -710,7 +712,7 @@ __device__ __forceinline__ void span_many(const AttendArgs &a, const Tile &t, in
             stage += 2 * Sh::HALF;
             if (stage == base + RING * 2 * Sh::HALF) stage = base;
         }
-        return 32 * i + 32 * U <= whole && real == (1u << 2 * U) - 1u;
+        return 32 * i <= whole - 32 * U && real == (1u << 2 * U) - 1u;
     };
     // (Two loops in one another: one for both kinds of tile moves half of the sums from register to register every time.)
     for (int i = 0; i < n; i += U) {
