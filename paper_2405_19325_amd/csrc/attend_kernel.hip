@@ -753,13 +753,13 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a, int64_t ti
 // wave each: the references of up to 64 parts at once, a lane each, then the
 // parts' outputs.
 template <knn_dtype DT, int D>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles, int64_t all_tiles, int64_t teams, int step,
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int64_t tiles, bool by_sequence, int64_t teams, int step,
                                                      int cols, const float *part, const float *part_ml) {
     constexpr int PER = D / 64;  // elements of a lane
     const int lane = threadIdx.x & 63;
     const int64_t heads = a.q_heads;
     int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // (row, query head)
-    if (tiles < all_tiles) {  // of sequence blockIdx.y, from the first row that has columns in these tiles
+    if (by_sequence) {  // of sequence blockIdx.y, from the first row that has columns in these tiles
         at += (a.row_offsets[blockIdx.y] + a.first_tile * cols / (heads / a.kv_heads)) * heads;
         if (at >= a.row_offsets[blockIdx.y + 1] * heads) return;
     }
@@ -838,10 +838,12 @@ hipError_t launch(AttendArgs a, const AttendPlan &p, float *part, float *part_ml
         else if (p.cols == 64) k_attend_many<DT, D, 1><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, tiles, p.teams, p.step, part, part_ml);
         else k_attend_many<DT, N, 2><<<grid, 256, Shape<D>::RING_LDS, stream>>>(a, tiles, p.teams, p.step, part, part_ml);
         if (p.total == 0) continue;
-        // All rows, or of each sequence as many as may have columns in these tiles.
-        const int64_t rows = tiles == p.all_tiles ? a.rows : (tiles * p.cols + g - 1) / g + 1;
-        const dim3 joins(static_cast<unsigned>((rows * a.q_heads + 3) / 4), tiles == p.all_tiles ? 1u : static_cast<unsigned>(a.S));
-        k_attend_join<DT, D><<<joins, 256, 0, stream>>>(a, tiles, p.all_tiles, p.teams, p.step, p.cols, part, part_ml);
+        // All rows, or where those are fewer as many of each sequence as may have columns in these tiles.
+        const int64_t some = (tiles * p.cols + g - 1) / g + 1;
+        const bool by_sequence = tiles < p.all_tiles && a.S <= 65535 && a.S * some < a.rows;
+        const dim3 joins(static_cast<unsigned>(((by_sequence ? some : a.rows) * a.q_heads + 3) / 4),
+                         by_sequence ? static_cast<unsigned>(a.S) : 1u);
+        k_attend_join<DT, D><<<joins, 256, 0, stream>>>(a, tiles, by_sequence, p.teams, p.step, p.cols, part, part_ml);
     }
     return hipGetLastError();
 }
@@ -866,11 +868,18 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
     p.all_tiles = p.tiles = (cols + p.cols - 1) / p.cols;
     // As many workgroups as the CUs hold at once, each with 256 keys or more (many columns: 128); teams a multiple of 8
     // (the XCDs).  Heads of up to kWhole keys are not parted: nothing to join (of 1,001 keys, one token and 32 heads:
-    // 15.8 us, in four parts 14.5).  Nor are those of wide calls, whose column tiles alone leave room for fewer than 8
-    // teams, where there are 8 heads or more: a workgroup each for a head and a tile (up to kWide of them, since most have
-    // no column where one sequence of many is long) fill the CUs as they get free, whatever a chain's tiles see.  @@
-    const int64_t heads = S * kv_heads;
-    const bool many = p.cols > 32, wide = p.tiles > 64 && heads >= 8 && max_keys <= (int64_t{1} << 30);
+    // 15.8 us, in four parts 14.5).  Nor are those of wide calls, whose column tiles leave room for fewer than 8 teams
+    // where there are 8 heads or more: a workgroup each for a head and a tile (up to kWide of them) fill the CUs as they
+    // get free, whatever a chain's tiles see.  (Under 8 key heads a sequence 8 teams share its keys among more; where it
+    // may be much longer than the rows it is parted.)  Four prompts of 4,000 to 8,000 rows with 64 heads on 8 take 6.05 ms, 9.5 in
+    // 8 teams, and a prompt's 1,040 rows beside 63 decoding sequences of 100 to 8,000 tokens 0.97 ms, 7.95.  As wide are
+    // those whose rows cannot fill half of the tiles that max_rows asks for (a sequence has rows g / cols / S + 1 of them at
+    // most, on average), with four and more heads for each team that there would be room for: 512 rows of as many
+    // sequences with 64 heads on 8, of which max_rows says nothing, take 1.29 ms, 6.97 in 16 teams (0.31 where it is 1).
+    const int64_t g = q_heads / kv_heads, heads = S * kv_heads, room = 512 / p.tiles / 8 * 8;
+    const bool loose = p.tiles * p.cols * S >= 2 * (rows * g + p.cols * S) && heads >= 4 * room;
+    const bool many = p.cols > 32, short_ones = heads >= 8 && max_keys <= 8 * max_rows;
+    const bool wide = max_keys <= (int64_t{1} << 30) && (room < 8 ? kv_heads >= 8 || short_ones : loose);
     const bool whole = max_keys <= kWhole || wide;
     p.step = whole ? static_cast<int>((max_keys + 63) / 64 * 64) : 64;
     p.stages = p.cols == 16 && max_keys <= 32 * (head_dim == 256 ? 2 : 4) ? 1 : 2;

@@ -446,6 +446,7 @@ def some_rows(x, out, lse, rows, scale):
 @pytest.mark.parametrize("dtype,rows,lens,heads,d", [
     ("bf16", [1100], [0], (64, 1), 128),            # 550 column tiles on one key head: parts in two launches
     ("f16", [1030, 40, 0], [10, 700, 3], (64, 1), 128),
+    ("bf16", [1, 1, 1020, 2, 1, 1, 1, 1, 1], [9000, 7, 100, 30, 0, 63, 64, 65, 900], (64, 1), 128),
     ("bf16", [600], [301], (64, 1), 128),           # parts in one
     ("f16", [2100], [0], (16, 1), 256),             # the same at 64 columns
     ("bf16", [1100, 7], [0, 40], (64, 2), 64),
@@ -464,3 +465,19 @@ def test_prompts(dtype, rows, lens, heads, d):
     some_rows(x, out, lse, sorted({int(i) for i in np.linspace(0, T - 1, 17)} | {T // 2 - 1, T // 2 + 1}), d ** -0.5)
     # every row was written: its largest weighted value is none of the constants
     assert torch.isfinite(lse).all() and not (out == 7.0).all(2).any() and not (lse == 5.0).any()
+
+
+@pytest.mark.parametrize("most", [60, 700])
+def test_rows_that_cannot_fill_what_max_rows_asks_for(most):
+    """Many sequences of few rows and no bound on them: a head is not parted then, whatever its keys."""
+    S = 200
+    rng = np.random.RandomState(most)
+    lens = [int(n) for n in rng.randint(0, most, S)]
+    rows = [int(n) for n in rng.choice([0, 1, 1, 2, 3], S)]
+    lens[S // 2], rows[7] = most * 3, 150
+    x, mask, sees = batch("bf16", rows, lens, (8, 4), 64, 32, seed=S + most, tree=True)
+    call = knn.TreeAttention(*[x[n] for n in NAMES], tree_mask=mask, want_lse=True)
+    assert call.workspace.numel() == 256
+    call.run()
+    torch.cuda.synchronize()
+    compare(x, call.out, call.lse, sees, 1 / 8)
