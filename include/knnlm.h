@@ -522,7 +522,7 @@ size_t knn_tree_attention_workspace_size(int64_t rows, int64_t S, int64_t q_head
  *                  each other (KNN_ERR_INVALID_ARG).
  *   prob           [rows] fp32 out or NULL: its share of the weight that stays (0 for token -1).
  *   kept           [rows] int32 out or NULL: how many stay.
- *   workspace      knn_sample_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
+ *   workspace      knn_sample_workspace_size() bytes, 256-byte aligned: asked for, but neither read nor written yet.
  *
  * Weights are in 64 bits, right to 2^-50 (1 - ln w) of a weight w, and of
  * probabilities at another T than 1 to 2^-51 / T more.  They are summed as whole

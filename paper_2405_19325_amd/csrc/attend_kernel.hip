@@ -16,18 +16,22 @@
 // column, which is what the second product O^T = V^T P^T wants of its right
 // operand, in an order of the keys that the left operand follows: the weights
 // never leave the registers.  V^T comes out of LDS by the transposing read.
-// The row of ones in front of V sums the weights as they were rounded for the
-// product, so that they sum to one.
+// The matrix instruction takes both operands in one type, so the weights are
+// rounded to 16 bits for it: errors of 0.0023 of the largest output in bf16 and
+// 0.00029 in f16, 0.0017 and 0.00021 of these the output's own rounding.  (A third
+// product, of what the rounding leaves, would cost where the matrix cores are the
+// bound what it does.)  The row of ones in front of V sums the weights as they
+// were rounded, in 32 bits, so that they sum to one.
 //
 // What bounds it.  Up to 16 columns a key head (decoding, spans without shared
 // heads): the bytes of the keys, each of which is read once.  64 ragged
-// sequences of 2,000 to 16,000 tokens, 8 key heads: 402 us for 2.36 GB, 5.9 TB/s
+// sequences of 2,000 to 16,000 tokens, 8 key heads: 408 us for 2.36 GB, 5.8 TB/s
 // with the join (a plain read: 7.0).  64 and more columns: the issue of a
 // weight's vector instructions beside its two matrix products, at 128 columns
 // of head_dim 128 with nearly a full register file (241 of 256).  Trees
-// of 64 rows on 4 x 131,072 tokens, 64 query heads on 8: 1.32 ms, 834 TFLOP/s
-// (a large library product: 1,166).  One token on 1,000 keys: 14.6 us, of which
-// 5.2 are the join's launch, and 9.2 two waits for memory, the barriers and the
+// of 64 rows on 4 x 131,072 tokens, 64 query heads on 8: 1.28 ms, 857 TFLOP/s
+// (a large library product: 1,166).  One token on 1,000 keys: 13.9 us, of which
+// 5.2 are the join's launch, and 8.7 two waits for memory, the barriers and the
 // launch of the first.
 #include "lm_internal.h"
 #include "mfma_device.h"

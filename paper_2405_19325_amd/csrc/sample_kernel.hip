@@ -6,7 +6,7 @@
 // largest one (2^s <= 2^62 / V, so no sum overflows).  Whole numbers add up to
 // the same sum in any order, so the outcome depends neither on how a row is
 // cut nor on the order of atomics; what a weight loses is under 2^-(s+1) of
-// the largest, 2^-46 for 131,072 tokens, which moves the drawn token for one
+// the largest, 2^-45 for 131,072 tokens, which moves the drawn token for one
 // row in 10^7.  (In 32 bits it would for one row in 50.)
 //
 // Every filter keeps a first part of one order: larger x first, the lower
@@ -29,11 +29,12 @@
 //
 // Measured, with the call: 32,000 bfloat16 logits, one row: largest element
 // alone 6.7 us, drawn from all 18, top-p 24; 256 rows of 131,072 float logits
-// with top-p 122 us, of which 19 would read them once.  What bounds it is the
-// issue of 64-bit operations: 13 of a weight's 20 instructions are such, a
-// weight of 64 elements takes a SIMD about 160 clocks, and top-p takes two for
-// each element that it keeps.  (Weights in 32 bits would draw another token in
-// one row of 50.)  An atomic of 64 lanes on the bins takes 40 clocks of the CU.
+// with top-p 122 us, of which 19 would read them once.  The time is that of the
+// issue of 64-bit operations: 13 of a weight's 20 instructions are such, a weight
+// of 64 elements takes a SIMD about 160 clocks.  (Weights in 32 bits would draw
+// another token in one row of 50.)  The pass after a cut weighs all 512 places of a
+// wave where one of them stays; of a nucleus of one element in 25 that is next to
+// all.  An atomic of 64 lanes on the bins takes 40 clocks of the CU.
 #include "knnlm_device.h"
 #include "lm_internal.h"
 
