@@ -18,17 +18,17 @@
 // never leave the registers.  V^T comes out of LDS by the transposing read.
 // The matrix instruction takes both operands in one type, so the weights are
 // rounded to 16 bits for it: errors of 0.0023 of the largest output in bf16 and
-// 0.00029 in f16, 0.0017 and 0.00021 of these the output's own rounding.  (A third
-// product, of what the rounding leaves, would cost where the matrix cores are the
-// bound what it does.)  The row of ones in front of V sums the weights as they
-// were rounded, in 32 bits, so that they sum to one.
+// 0.00029 in f16, 0.0017 and 0.00021 of these the output's own rounding.  (A product
+// of what the rounding leaves would be half as many matrix instructions again.)
+// The row of ones in front of V sums the weights as they were rounded, in 32 bits,
+// so that they sum to one.
 //
 // What bounds it.  Up to 16 columns a key head (decoding, spans without shared
 // heads): the bytes of the keys, each of which is read once.  64 ragged
 // sequences of 2,000 to 16,000 tokens, 8 key heads: 408 us for 2.36 GB, 5.8 TB/s
 // with the join (a plain read: 7.0).  64 and more columns: the issue of a
 // weight's vector instructions beside its two matrix products, at 128 columns
-// of head_dim 128 with nearly a full register file (241 of 256).  Trees
+// of head_dim 128 with nearly a full register file (239 of 256).  Trees
 // of 64 rows on 4 x 131,072 tokens, 64 query heads on 8: 1.28 ms, 857 TFLOP/s
 // (a large library product: 1,166).  One token on 1,000 keys: 13.9 us, of which
 // 5.2 are the join's launch, and 8.7 two waits for memory, the barriers and the
@@ -292,7 +292,7 @@ struct Columns {
                 const u32x4_t bad = {not_finite<DT>(v.x), not_finite<DT>(v.y), not_finite<DT>(v.z), not_finite<DT>(v.w)};
                 if (__any((bad.x | bad.y | bad.z | bad.w) != 0u)) {
                     v &= ~bad;
-                    left_out = true;
+                    left_out = left_out || key + 32 * u < end;  // (a tile behind the end was not filled: it holds anything)
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) o[n][d] = mfma16<DT>(v, p[u][n], o[n][d]);
@@ -874,12 +874,13 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
     // (the XCDs).  Heads of up to kWhole keys are not parted: nothing to join (of 1,001 keys, one token and 32 heads:
     // 15.8 us, in four parts 14.5).  Nor are those of wide calls, whose column tiles leave room for fewer than 8 teams
     // where there are 8 heads or more: a workgroup each for a head and a tile (up to kWide of them) fill the CUs as they
-    // get free, whatever a chain's tiles see.  (Under 8 key heads a sequence 8 teams share its keys among more; where it
-    // may be much longer than the rows it is parted.)  Four prompts of 4,000 to 8,000 rows with 64 heads on 8 take 6.05 ms, 9.5 in
-    // 8 teams, and a prompt's 1,040 rows beside 63 decoding sequences of 100 to 8,000 tokens 0.97 ms, 7.95.  As wide are
-    // those whose rows cannot fill half of the tiles that max_rows asks for (a sequence has rows g / cols / S + 1 of them at
-    // most, on average), with four and more heads for each team that there would be room for: 512 rows of as many
-    // sequences with 64 heads on 8, of which max_rows says nothing, take 1.29 ms, 6.97 in 16 teams (0.31 where it is 1).
+    // get free, whatever a chain's tiles see.  (A sequence of fewer than 8 key heads would have fewer workgroups a tile than
+    // 8 teams: it is parted where it may be over 8 times as long as the rows.)  Four prompts of 4,000 to 8,000 rows with 64
+    // heads on 8 take 6.05 ms, 9.5 in 8 teams, and a prompt's 1,040 rows beside 63 decoding sequences of 100 to 8,000 tokens
+    // 0.97 ms, 7.95.  As wide are those whose rows cannot fill half of the tiles that max_rows asks for (a sequence has
+    // rows g / cols / S + 1 of them at most, on average), with four and more heads for each team that there would be room
+    // for: 512 rows of as many sequences with 64 heads on 8, of which max_rows says nothing, take 1.29 ms, 6.97 in 16 teams
+    // (0.31 where it is 1).
     const int64_t g = q_heads / kv_heads, heads = S * kv_heads, room = 512 / p.tiles / 8 * 8;
     const bool loose = p.tiles * p.cols * S >= 2 * (rows * g + p.cols * S) && heads >= 4 * room;
     const bool many = p.cols > 32, short_ones = heads >= 8 && max_keys <= 8 * max_rows;

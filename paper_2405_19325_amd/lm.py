@@ -92,7 +92,8 @@ class KVAppend(_Call):
     [S, width] int32, row_offsets [S+1] int64, cache_lens [S] int32 as the header says.  positions [rows] int32
     (default: the cache index); inv_freq [rotated elements / 2] fp32 (None: no rotation); interleaved: pairs
     (2i, 2i+1); source_rows [rows] int32: the row that each row is read from.  q_out [rows, q_heads, d] is
-    allocated where it is not given (it may be q where q is dense and there are no source_rows).
+    allocated where it is not given (it may be q where q is dense and there are no source_rows).  What is read lies
+    apart from the caches.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
