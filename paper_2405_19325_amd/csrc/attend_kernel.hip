@@ -867,7 +867,12 @@ AttendPlan plan_attend(int64_t rows, int64_t S, int64_t q_heads, int64_t kv_head
                        int64_t max_keys) {
     AttendPlan p{};
     const int64_t cols = max_rows * (q_heads / kv_heads);
-    // (At head_dim 256 the wider kind of either kernel does not fit the registers.)
+    // As few columns a workgroup as hold a sequence's, so that its keys are read once a head; measured on 32 sequences of
+    // 2,000 to 8,000 tokens, 8 heads of 128: 16 columns 133 us, 137 in the kind of 32; 20 columns 138 in that of 32, 143
+    // in two tiles of 16; 64 columns 158, 163 in the kind of 128 and 186 in two tiles of 32; 68 columns 166 in that of
+    // 128, 193 in two tiles of 64.  (Heads of 64 on 4 sequences of 16,000 to 32,000 tokens would be the faster in two
+    // narrow tiles up to 64 columns: 41 us for 48 at 20, 50 for 53 at 64.)  At head_dim 256 the wider kind of either
+    // kernel does not fit the registers.
     p.cols = cols <= 16 ? 16 : cols <= 32 && head_dim < 256 ? 32 : cols <= 64 || head_dim == 256 ? 64 : 128;
     p.all_tiles = p.tiles = (cols + p.cols - 1) / p.cols;
     // As many workgroups as the CUs hold at once, each with 256 keys or more (many columns: 128); teams a multiple of 8
