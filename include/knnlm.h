@@ -541,6 +541,127 @@ knn_status knn_sample(const void *scores, const float *uniforms, const float *te
 size_t knn_sample_workspace_size(int64_t rows, int64_t V, knn_dtype dtype);
 
 /*
+ * knn_key_weights -- the weight that the rows put on each cached key, per key
+ * head, added up over the steps of a run: what knn_cache_evict goes by.  With
+ * the rows' sums as knn_tree_attention gave them (lse), for key j of a sequence
+ *
+ *   w_j = sum exp(scale q.k_j - lse)   over the rows that see j and their query heads of the key head,
+ *   mass_j = decay mass_j + w_j   of a token that was cached before (j < cache_lens[s]),
+ *   mass_j = w_j                  of the rows' own keys.
+ *
+ *   q, source_rows, source_count
+ *                  as knn_kv_append reads them: row t is row source_rows[t] of q and lse (an accepted path out of a
+ *                  draft's rows, once knn_kv_append has put it over the tree's drafts), or row t itself (NULL).  A row
+ *                  whose source lies outside [0, source_count) adds nothing.
+ *   lse            [source_count, q_heads] fp32.  Where it is not finite (a row that saw no key) the row adds nothing.
+ *   tree_mask, max_rows, max_keys, scale
+ *                  as in knn_tree_attention.
+ *   decay          finite, >= 0.  0 starts anew: what mass held is not read.
+ *   mass           [n_pages, kv_heads, page_size] fp32, beside the cache: read and written.
+ *   key_positions  [n_pages, kv_heads, page_size] int32 or NULL: the rows' own places get positions[t].
+ *   positions      [rows] int32 or NULL: the cache index.  Only with key_positions.
+ *
+ * A sequence without rows keeps its masses.  Places past a sequence's tokens are left as they are.  mass and
+ * key_positions lie apart from all that is read and from each other.  Sums are in fp32, in an order that does not
+ * depend on how workgroups run.  Sizes, alignment and strides as knn_tree_attention serves them.
+ */
+knn_status knn_key_weights(const void *q, const float *lse, const void *k_cache, const int32_t *pages,
+                           const int64_t *row_offsets, const int32_t *cache_lens, const int32_t *positions,
+                           const int32_t *source_rows, const uint32_t *tree_mask, int64_t rows, int64_t source_count,
+                           int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t q_row_stride,
+                           int64_t q_head_stride, int64_t n_pages, int64_t page_size, int64_t table_width,
+                           int64_t mask_words, int64_t max_rows, int64_t max_keys, knn_dtype dtype, float scale,
+                           float decay, float *mass, int32_t *key_positions, void *stream);
+
+/*
+ * knn_cache_evict -- the tokens of little weight leave the cache, whose places
+ * are closed up.  Each key head of a sequence keeps its own tokens: of the
+ * cache_lens[s] ones, budgets[s] stay, the first of this order:
+ *
+ *   tokens at positions below `sinks`, and from next_positions[s] - recent on, before all others;
+ *   of two such, or of two others, the one of more mass (NaN is the least);
+ *   of equal ones, the one of the lower cache index.
+ *
+ * They take the indices 0 .. budgets[s] - 1: those that lie there already stay
+ * where they are, and the others, in the order of their indices, take the
+ * places of those that leave.  So no more is moved than has to be, and the
+ * cache's tokens are in no order of positions any more: keys carry their
+ * rotation with them, and later rows are appended with positions of their own.
+ *
+ *   k_cache, v_cache   moved in place, apart from each other.  The pages of a sequence must be no other's.
+ *   mass           as knn_key_weights keeps it.
+ *   key_positions  [n_pages, kv_heads, page_size] int32 or NULL: the position of each place's token is its index.
+ *   budgets        [S] int32; a negative one leaves the sequence as it is, like one of cache_lens[s] or more.
+ *   next_positions [S] int32, the position of each sequence's next token, or NULL: cache_lens[s].
+ *   sinks, recent  >= 0.  Where more tokens than the budget are at such positions, those of the most mass stay.
+ *   max_keys       host hint: at least every cache_lens[s]; at most table_width * page_size, and 2^31 - 1.
+ *   mass_out, positions_out
+ *                  as mass and key_positions, the ledger of afterwards: written at the indices that stay (places past
+ *                  them are left as they are).  mass and key_positions themselves are written where they are given, or
+ *                  NULL (the latter with key_positions NULL); apart from all else otherwise.
+ *   new_lens       [S] int32 out: min(cache_lens[s], budgets[s]), or cache_lens[s] of a sequence left as it is.
+ *   workspace      knn_cache_evict_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
+ *
+ * A sequence that is longer than max_keys or its table, or one of whose pages is none, is left as it is; so are the
+ * places from new_lens[s] on, of every buffer.  All else that is read lies apart from what is written.  head_dim up to
+ * 1024; KNN_BF16 or KNN_F16.
+ */
+knn_status knn_cache_evict(void *k_cache, void *v_cache, float *mass, int32_t *key_positions, const int32_t *pages,
+                           const int32_t *cache_lens, const int32_t *budgets, const int32_t *next_positions, int64_t S,
+                           int64_t kv_heads, int64_t head_dim, int64_t n_pages, int64_t page_size, int64_t table_width,
+                           int64_t max_keys, int32_t sinks, int32_t recent, knn_dtype dtype, float *mass_out,
+                           int32_t *positions_out, int32_t *new_lens, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
+/* Bytes of workspace knn_cache_evict needs for these sizes (0 if they are invalid). */
+size_t knn_cache_evict_workspace_size(int64_t S, int64_t kv_heads, int64_t max_keys);
+
+/*
+ * knn_adjust_scores -- penalties for repeated tokens, biases and the tokens
+ * that a grammar allows, on logits or on a distribution such as knn_nest_step's
+ * p_m, before knn_sample draws from them.  For row t of sequence s, token v
+ * with c occurrences in what counts as output, and x the logit:
+ *
+ *   1. x / repetition[t] where x > 0, x repetition[t] elsewhere, if v occurs at all (in the prompt or the output);
+ *   2. x - presence[t] if c > 0, and - frequency[t] c;
+ *   3. x + the bias of v;
+ *   4. -inf if the row's `allowed` has no bit for v.
+ *
+ * Probabilities (probabilities != 0) go through the same steps as ln p, and
+ * come back as exp of the outcome (they need not add up to 1); one that is not
+ * above 0 stays as it is, and one that is not allowed is 0.
+ *
+ *   scores         [rows, V] fp32, bf16 or f16, rows row_stride elements apart.
+ *   history        [S, history_width] int32 or NULL: the tokens of each sequence so far, of which the first
+ *                  history_lens[s] ([S] int32) count, the first prompt_lens[s] of these ([S] int32, or NULL: none) as
+ *                  its prompt and the others as output.  Tokens outside [0, V) are passed over.
+ *   row_offsets    [S+1] int64: the sequences' rows, as above; or NULL: each row is a sequence (S = rows).
+ *   row_tokens     [rows] int32 or NULL: the token that each row was run on.  Those of the rows that a row sees count as
+ *                  output as well: by tree_mask ([rows, mask_words] as in knn_tree_attention), or without one the rows
+ *                  of its sequence up to itself.
+ *   repetition, presence, frequency
+ *                  [rows] fp32, each or NULL; off where not finite, the first one also where not above 0.  They need
+ *                  history or row_tokens.
+ *   bias_tokens, bias_values
+ *                  [S, bias_width] int32 and fp32, or NULL: added to those tokens' scores.  Of a token that is named more
+ *                  than once the last value counts; tokens outside [0, V) are passed over.
+ *   allowed        [rows, ceil(V / 32)] uint32 or NULL: bit (v & 31) of word v >> 5 set means that v may be drawn.
+ *   out            [rows, V] dtype, rows out_stride (>= V) apart: scores itself with its stride, and then only what
+ *                  changes is written; else apart from all that is read.
+ *
+ * Logits are worked out in fp32, probabilities in 64 bits and rounded to fp32, before they are rounded to dtype; what no
+ * step reaches keeps its bits.
+ * V <= 2^24, history_width and bias_width <= 2^30 (KNN_ERR_UNSUPPORTED above).
+ */
+knn_status knn_adjust_scores(const void *scores, const int32_t *history, const int32_t *history_lens,
+                             const int32_t *prompt_lens, const int64_t *row_offsets, const int32_t *row_tokens,
+                             const uint32_t *tree_mask, const float *repetition, const float *presence,
+                             const float *frequency, const int32_t *bias_tokens, const float *bias_values,
+                             const uint32_t *allowed, int64_t rows, int64_t V, int64_t S, int64_t row_stride,
+                             int64_t history_width, int64_t mask_words, int64_t bias_width, int64_t out_stride,
+                             int32_t probabilities, knn_dtype dtype, void *out, void *stream);
+
+/*
  * knn_stream_read -- a measurement aid, not a step of the method: one plain
  * read of `bytes` bytes of device memory at `buf` (16-byte aligned, a multiple
  * of 16 bytes) with the same 16-byte non-temporal loads the distance stage

@@ -21,7 +21,8 @@ from ._lib import DTYPES, KEYS_PACKED, PARTS, KnnError, load, status_string  # n
 __all__ = ["MixtureProblem", "mixture", "mixture_noalloc", "distances", "key_sqnorms", "pack_keys",
            "packed_keys_bytes", "mix", "mix_rrc", "spec_verify", "mask_words", "stream_read", "workspace_size",
            "preferred_workspace_size", "KVAppend", "kv_append", "TreeAttention", "tree_attention",
-           "tree_words", "Sampler", "sample", "KnnError", "load", "status_string", "abi_version"]
+           "tree_words", "KeyWeights", "key_weights", "CacheEvict", "cache_evict", "ScoreAdjuster", "adjust_scores",
+           "Sampler", "sample", "KnnError", "load", "status_string", "abi_version"]
 
 _TORCH_DTYPES = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
 
@@ -352,4 +353,5 @@ def spec_verify(p_max, p_draft, next_token, draft_offsets, gamma, uniforms=None)
     return n_acc, tok
 
 
-from .lm import KVAppend, Sampler, TreeAttention, kv_append, sample, tree_attention, tree_words  # noqa: E402  (uses the helpers above)
+from .lm import (CacheEvict, KeyWeights, KVAppend, Sampler, ScoreAdjuster, TreeAttention, adjust_scores,  # noqa: E402
+                 cache_evict, key_weights, kv_append, sample, tree_attention, tree_words)  # (uses the helpers above)

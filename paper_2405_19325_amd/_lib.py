@@ -53,6 +53,10 @@ SIGNATURES: Dict[str, tuple] = {
     "knn_tree_attention_workspace_size": (SZ, [I64] * 7),
     "knn_sample": (I, [P] * 6 + [I64] * 3 + [I32, I, P, P, P, P, SZ, P]),
     "knn_sample_workspace_size": (SZ, [I64, I64, I]),
+    "knn_key_weights": (I, [P] * 9 + [I64] * 14 + [I, F, F, P, P, P]),
+    "knn_cache_evict": (I, [P] * 8 + [I64] * 7 + [I32, I32, I, P, P, P, P, SZ, P]),
+    "knn_cache_evict_workspace_size": (SZ, [I64] * 3),
+    "knn_adjust_scores": (I, [P] * 13 + [I64] * 8 + [I32, I, P, P]),
     "knn_stream_read": (I, [P, SZ, P, P]),
     "knn_status_string": (ctypes.c_char_p, [I]),
     "knn_abi_version": (I, []),

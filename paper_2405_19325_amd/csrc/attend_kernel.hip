@@ -33,7 +33,7 @@
 // (a large library product: 1,166).  One token on 1,000 keys: 13.9 us, of which
 // 5.2 are the join's launch, and 8.7 two waits for memory, the barriers and the
 // launch of the first.
-#include "lm_internal.h"
+#include "lm_device.h"
 #include "mfma_device.h"
 
 namespace knnlm {
@@ -50,30 +50,6 @@ constexpr int64_t kWide = 16384;  // workgroups of a wide call
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
-
-// What a workgroup works on.
-struct Tile {
-    int64_t r0;      // first row of the sequence
-    int n;           // its rows
-    int64_t length;  // cached tokens
-    int64_t total;   // keys
-};
-
-__device__ __forceinline__ Tile tile_of(const AttendArgs &a, int64_t s) {
-    Tile t;
-    t.r0 = a.row_offsets[s];
-    int64_t r1 = a.row_offsets[s + 1];
-    if (r1 > a.rows) r1 = a.rows;
-    const int64_t n = r1 - t.r0;
-    t.n = static_cast<int>(n < 0 ? 0 : n > a.max_rows ? a.max_rows : n);
-    const int64_t len = a.cache_lens[s];
-    t.length = len < 0 ? 0 : len;
-    t.total = t.length + t.n;
-    if (t.total > a.max_keys) t.total = a.max_keys;
-    const int64_t room = a.cache.table_width << a.cache.page_log2;
-    if (t.total > room) t.total = room;
-    return t;
-}
 
 template <knn_dtype DT>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {  // to nearest, ties to even

@@ -1,6 +1,6 @@
 // C ABI of the language model's own step around the mixture: cache append,
-// attention of drafts, sampling.  Host-side validation and the launches on
-// the caller's stream.
+// attention of drafts, weights of cached keys, eviction, adjusted scores,
+// sampling.  Host-side validation and the launches on the caller's stream.
 #include <math.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -53,6 +53,14 @@ knn_status check_sample(int64_t rows, int64_t V, knn_dtype dtype) {
     if (rows < 1 || V < 1 || (dtype != KNN_F32 && dtype != KNN_BF16 && dtype != KNN_F16)) return KNN_ERR_INVALID_ARG;
     return rows > 0x7fffffff || V > kSampleMaxV ? KNN_ERR_UNSUPPORTED : KNN_OK;
 }
+
+knn_status check_evict(int64_t S, int64_t kv_heads, int64_t max_keys) {
+    if (S < 1 || kv_heads < 1 || max_keys < 1) return KNN_ERR_INVALID_ARG;
+    if (kv_heads > KNNLM_MAX_HEADS || S > 0x7fffffff / kv_heads || max_keys > 0x7fffffff) return KNN_ERR_UNSUPPORTED;
+    return KNN_OK;
+}
+
+constexpr int64_t kAdjustMaxWidth = int64_t{1} << 30;
 
 // The bytes from the first to the last of a buffer (null: none), in doubles: no sum of strides can pass them.
 struct Extent {
@@ -234,6 +242,163 @@ knn_status knn_sample(const void *scores, const float *uniforms, const float *te
     a.probabilities = probabilities != 0;
     a.token = token, a.prob = prob, a.kept = kept;
     return status_of(launch_sample(a, dtype, workspace, static_cast<hipStream_t>(stream)));
+}
+
+knn_status knn_key_weights(const void *q, const float *lse, const void *k_cache, const int32_t *pages,
+                           const int64_t *row_offsets, const int32_t *cache_lens, const int32_t *positions,
+                           const int32_t *source_rows, const uint32_t *tree_mask, int64_t rows, int64_t source_count,
+                           int64_t S, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t q_row_stride,
+                           int64_t q_head_stride, int64_t n_pages, int64_t page_size, int64_t table_width,
+                           int64_t mask_words, int64_t max_rows, int64_t max_keys, knn_dtype dtype, float scale,
+                           float decay, float *mass, int32_t *key_positions, void *stream) {
+    if (!q || !lse || !k_cache || !pages || !row_offsets || !cache_lens || !mass) return KNN_ERR_INVALID_ARG;
+    if (positions != nullptr && key_positions == nullptr) return KNN_ERR_INVALID_ARG;
+    if (source_count < 1 || (source_rows == nullptr && source_count < rows)) return KNN_ERR_INVALID_ARG;
+    knn_status st = check_cache(S, kv_heads, head_dim, n_pages, page_size, table_width, dtype);
+    if (st != KNN_OK) return st;
+    st = check_attend(rows, S, q_heads, kv_heads, head_dim, max_rows, max_keys);
+    if (st != KNN_OK) return st;
+    if (max_keys > table_width * page_size || !isfinite(scale) || !isfinite(decay) || decay < 0.0f ||
+        q_row_stride < 0 || q_head_stride < 0)
+        return KNN_ERR_INVALID_ARG;
+    if (tree_mask != nullptr && mask_words * 32 < max_rows) return KNN_ERR_INVALID_ARG;
+    // (the stride of a single row or head says nothing)
+    if (((source_count > 1 ? q_row_stride : 0) | (q_heads > 1 ? q_head_stride : 0)) % 8 != 0 || !aligned(q, 16) ||
+        !aligned(k_cache, 16) || source_count > 0x7fffffff)
+        return KNN_ERR_UNSUPPORTED;
+    const double places = static_cast<double>(n_pages) * kv_heads * page_size;
+    const Extent outputs[] = {dense(mass, places, 4), dense(key_positions, places, 4)};
+    const Extent inputs[] = {strided(q, source_count, q_heads, head_dim, q_row_stride, q_head_stride),
+                             dense(lse, static_cast<double>(source_count) * q_heads, 4),
+                             dense(k_cache, places * head_dim, 2),
+                             dense(pages, static_cast<double>(S) * table_width, 4),
+                             dense(row_offsets, static_cast<double>(S) + 1, 8),
+                             dense(cache_lens, static_cast<double>(S), 4),
+                             dense(positions, static_cast<double>(rows), 4),
+                             dense(source_rows, static_cast<double>(rows), 4),
+                             dense(tree_mask, static_cast<double>(rows) * mask_words, 4)};
+    if (any_meet(outputs, inputs)) return KNN_ERR_INVALID_ARG;
+    WeighArgs a{};
+    a.q = q, a.lse = lse, a.k_cache = k_cache;
+    a.row_offsets = row_offsets, a.cache_lens = cache_lens, a.positions = positions;
+    a.source_rows = source_rows, a.tree_mask = tree_mask;
+    a.rows = rows, a.source_count = source_count, a.S = S;
+    a.q_heads = static_cast<int>(q_heads), a.kv_heads = static_cast<int>(kv_heads);
+    a.head_dim = static_cast<int>(head_dim);
+    a.q_row = q_row_stride, a.q_head = q_head_stride;
+    a.cache = paged(pages, n_pages, page_size, table_width);
+    a.mask_words = mask_words, a.max_rows = max_rows, a.max_keys = max_keys;
+    a.scale = scale, a.decay = decay;
+    a.mass = mass, a.key_positions = key_positions;
+    return status_of(launch_key_weights(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+size_t knn_cache_evict_workspace_size(int64_t S, int64_t kv_heads, int64_t max_keys) {
+    if (check_evict(S, kv_heads, max_keys) != KNN_OK) return 0;
+    const size_t need = evict_workspace(S, kv_heads, max_keys);
+    return need < 256 ? 256 : (need + 255) / 256 * 256;
+}
+
+knn_status knn_cache_evict(void *k_cache, void *v_cache, float *mass, int32_t *key_positions, const int32_t *pages,
+                           const int32_t *cache_lens, const int32_t *budgets, const int32_t *next_positions, int64_t S,
+                           int64_t kv_heads, int64_t head_dim, int64_t n_pages, int64_t page_size, int64_t table_width,
+                           int64_t max_keys, int32_t sinks, int32_t recent, knn_dtype dtype, float *mass_out,
+                           int32_t *positions_out, int32_t *new_lens, void *workspace, size_t workspace_bytes,
+                           void *stream) {
+    if (!k_cache || !v_cache || !mass || !pages || !cache_lens || !budgets || !mass_out || !new_lens ||
+        (key_positions != nullptr) != (positions_out != nullptr))
+        return KNN_ERR_INVALID_ARG;
+    knn_status st = check_cache(S, kv_heads, head_dim, n_pages, page_size, table_width, dtype);
+    if (st != KNN_OK) return st;
+    st = check_evict(S, kv_heads, max_keys);
+    if (st != KNN_OK) return st;
+    if (max_keys > table_width * page_size || sinks < 0 || recent < 0) return KNN_ERR_INVALID_ARG;
+    if (head_dim > 1024) return KNN_ERR_UNSUPPORTED;
+    const size_t need = knn_cache_evict_workspace_size(S, kv_heads, max_keys);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return KNN_ERR_WORKSPACE;
+    const double places = static_cast<double>(n_pages) * kv_heads * page_size;
+    // (A ledger that is written in place is no input beside itself.)
+    const bool same_mass = mass_out == mass, same_positions = positions_out == key_positions;
+    const Extent outputs[] = {dense(k_cache, places * head_dim, 2),
+                              dense(v_cache, places * head_dim, 2),
+                              dense(mass_out, places, 4),
+                              dense(positions_out, places, 4),
+                              dense(new_lens, static_cast<double>(S), 4),
+                              dense(workspace, static_cast<double>(need), 1)};
+    const Extent inputs[] = {dense(same_mass ? nullptr : mass, places, 4),
+                             dense(same_positions ? nullptr : key_positions, places, 4),
+                             dense(pages, static_cast<double>(S) * table_width, 4),
+                             dense(cache_lens, static_cast<double>(S), 4),
+                             dense(budgets, static_cast<double>(S), 4),
+                             dense(next_positions, static_cast<double>(S), 4)};
+    if (any_meet(outputs, inputs)) return KNN_ERR_INVALID_ARG;
+    EvictArgs a{};
+    a.k_cache = k_cache, a.v_cache = v_cache;
+    a.mass = mass, a.key_positions = key_positions;
+    a.cache_lens = cache_lens, a.budgets = budgets, a.next_positions = next_positions;
+    a.S = S, a.kv_heads = static_cast<int>(kv_heads), a.head_dim = static_cast<int>(head_dim);
+    a.cache = paged(pages, n_pages, page_size, table_width);
+    a.max_keys = max_keys;
+    a.sinks = sinks, a.recent = recent;
+    a.mass_out = mass_out, a.positions_out = positions_out, a.new_lens = new_lens;
+    return status_of(launch_cache_evict(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+knn_status knn_adjust_scores(const void *scores, const int32_t *history, const int32_t *history_lens,
+                             const int32_t *prompt_lens, const int64_t *row_offsets, const int32_t *row_tokens,
+                             const uint32_t *tree_mask, const float *repetition, const float *presence,
+                             const float *frequency, const int32_t *bias_tokens, const float *bias_values,
+                             const uint32_t *allowed, int64_t rows, int64_t V, int64_t S, int64_t row_stride,
+                             int64_t history_width, int64_t mask_words, int64_t bias_width, int64_t out_stride,
+                             int32_t probabilities, knn_dtype dtype, void *out, void *stream) {
+    if (!scores || !out) return KNN_ERR_INVALID_ARG;
+    const knn_status st = check_sample(rows, V, dtype);
+    if (st != KNN_OK) return st;
+    if (S < 1 || (row_offsets == nullptr && S != rows) || row_stride < 0 || (rows > 1 && out_stride < V))
+        return KNN_ERR_INVALID_ARG;
+    if ((history != nullptr) != (history_lens != nullptr) || (history != nullptr && history_width < 1) ||
+        (prompt_lens != nullptr && history == nullptr))
+        return KNN_ERR_INVALID_ARG;
+    if (tree_mask != nullptr && (row_tokens == nullptr || mask_words < 1)) return KNN_ERR_INVALID_ARG;
+    if ((repetition != nullptr || presence != nullptr || frequency != nullptr) && history == nullptr &&
+        row_tokens == nullptr)
+        return KNN_ERR_INVALID_ARG;
+    if ((bias_tokens != nullptr) != (bias_values != nullptr) || (bias_tokens != nullptr && bias_width < 1))
+        return KNN_ERR_INVALID_ARG;
+    const int size = dtype == KNN_F32 ? 4 : 2;
+    if (S > 0x7fffffff || (history != nullptr && history_width > kAdjustMaxWidth) ||
+        (bias_tokens != nullptr && bias_width > kAdjustMaxWidth) || (tree_mask != nullptr && mask_words > kAdjustMaxWidth) ||
+        !aligned(scores, size) || !aligned(out, size))
+        return KNN_ERR_UNSUPPORTED;
+    const bool in_place = out == scores && (rows == 1 || out_stride == row_stride);
+    const Extent outputs[] = {dense(out, static_cast<double>(rows - 1) * out_stride + V, size)};
+    const double words = static_cast<double>((V + 31) / 32);
+    const Extent inputs[] = {
+        dense(in_place ? nullptr : scores, static_cast<double>(rows - 1) * row_stride + V, size),
+        dense(history, static_cast<double>(S) * history_width, 4),
+        dense(history_lens, static_cast<double>(S), 4),
+        dense(prompt_lens, static_cast<double>(S), 4),
+        dense(row_offsets, static_cast<double>(S) + 1, 8),
+        dense(row_tokens, static_cast<double>(rows), 4),
+        dense(tree_mask, static_cast<double>(rows) * mask_words, 4),
+        dense(repetition, static_cast<double>(rows), 4),
+        dense(presence, static_cast<double>(rows), 4),
+        dense(frequency, static_cast<double>(rows), 4),
+        dense(bias_tokens, static_cast<double>(S) * bias_width, 4),
+        dense(bias_values, static_cast<double>(S) * bias_width, 4),
+        dense(allowed, static_cast<double>(rows) * words, 4)};
+    if (any_meet(outputs, inputs)) return KNN_ERR_INVALID_ARG;
+    AdjustArgs a{};
+    a.scores = scores, a.out = out;
+    a.history = history, a.history_lens = history_lens, a.prompt_lens = prompt_lens;
+    a.row_offsets = row_offsets, a.row_tokens = row_tokens, a.tree_mask = tree_mask;
+    a.repetition = repetition, a.presence = presence, a.frequency = frequency;
+    a.bias_tokens = bias_tokens, a.bias_values = bias_values, a.allowed = allowed;
+    a.rows = rows, a.S = S, a.V = static_cast<int>(V);
+    a.stride = row_stride, a.out_stride = out_stride;
+    a.history_width = history_width, a.mask_words = mask_words, a.bias_width = bias_width;
+    a.probabilities = probabilities != 0;
+    return status_of(launch_adjust_scores(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

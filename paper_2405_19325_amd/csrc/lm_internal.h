@@ -1,5 +1,6 @@
 // Internal interfaces between the C ABI of the language model's own step
-// (lm_api.hip) and its kernels: cache append, attention of drafts, sampling.
+// (lm_api.hip) and its kernels: cache append, attention of drafts, weights of
+// cached keys, eviction, adjusted scores, sampling.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -90,6 +91,68 @@ struct SampleArgs {
 constexpr int64_t kSampleMaxV = int64_t{1} << 24;
 
 hipError_t launch_sample(const SampleArgs &args, knn_dtype dtype, void *workspace, hipStream_t stream);
+
+struct WeighArgs {
+    const void *q;     // [source_count, q_heads, head_dim], rows q_row elements apart, heads q_head
+    const float *lse;  // [source_count, q_heads]
+    const void *k_cache;
+    const int64_t *row_offsets;
+    const int32_t *cache_lens;
+    const int32_t *positions;    // or null: the cache index
+    const int32_t *source_rows;  // or null: row t itself
+    const uint32_t *tree_mask;   // [rows, mask_words] or null: a chain
+    int64_t rows, source_count, S;
+    int q_heads, kv_heads, head_dim;
+    int64_t q_row, q_head;
+    PagedCache cache;
+    int64_t mask_words;
+    int64_t max_rows, max_keys;
+    float scale, decay;
+    float *mass;
+    int32_t *key_positions;  // or null
+};
+
+hipError_t launch_key_weights(const WeighArgs &args, knn_dtype dtype, hipStream_t stream);
+
+struct EvictArgs {
+    void *k_cache, *v_cache;
+    const float *mass;
+    const int32_t *key_positions;  // or null: the cache index
+    const int32_t *cache_lens;
+    const int32_t *budgets;
+    const int32_t *next_positions;  // or null: cache_lens
+    int64_t S;
+    int kv_heads, head_dim;
+    PagedCache cache;
+    int64_t max_keys;
+    int sinks, recent;
+    float *mass_out;         // mass itself, or apart from it
+    int32_t *positions_out;  // key_positions itself (also null), or apart from it
+    int32_t *new_lens;
+};
+
+size_t evict_workspace(int64_t S, int64_t kv_heads, int64_t max_keys);
+hipError_t launch_cache_evict(const EvictArgs &args, void *workspace, hipStream_t stream);
+
+struct AdjustArgs {
+    const void *scores;                                // [rows, V], rows `stride` elements apart
+    const int32_t *history;                            // [S, history_width] or null
+    const int32_t *history_lens, *prompt_lens;         // prompt_lens: or null, 0
+    const int64_t *row_offsets;                        // or null: row t is sequence t
+    const int32_t *row_tokens;                         // or null
+    const uint32_t *tree_mask;                         // [rows, mask_words] or null: a chain
+    const float *repetition, *presence, *frequency;    // each [rows], or null: 1, 0, 0
+    const int32_t *bias_tokens;                        // [S, bias_width] or null
+    const float *bias_values;
+    const uint32_t *allowed;  // [rows, ceil(V / 32)] or null
+    int64_t rows, S;
+    int V;
+    int64_t stride, history_width, mask_words, bias_width, out_stride;
+    bool probabilities;
+    void *out;  // scores itself, or apart from it
+};
+
+hipError_t launch_adjust_scores(const AdjustArgs &args, knn_dtype dtype, hipStream_t stream);
 
 hipError_t launch_kv_append(const AppendArgs &args, knn_dtype dtype, hipStream_t stream);
 

@@ -1,4 +1,5 @@
-"""The language model's own step around the mixture: cache append, attention of drafts, sampling.
+"""The language model's own step around the mixture: cache append, attention of drafts, the weights of cached keys and
+eviction by them, adjusted scores, sampling.
 
 Like the rest of the package this only marshals arguments; the HIP kernels
 behind include/knnlm.h do the work.  Each class keeps the buffers, the planning
@@ -69,7 +70,7 @@ class _Call:
             _lib.check(self._name, st)
 
 
-def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, row_offsets: torch.Tensor,
+def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, row_offsets: Optional[torch.Tensor],
            cache_lens: torch.Tensor) -> Tuple[int, int, int, int, int]:
     """Checks the cache's tensors: (S, n_pages, kv_heads, page_size, head_dim)."""
     _need(k_cache.dim() == 4 and k_cache.is_contiguous(),
@@ -78,7 +79,7 @@ def _paged(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, ro
     _need(pages.dim() == 2, "pages: [S, table_width]")
     _flat("pages", pages, torch.int32, tuple(pages.shape))
     S = pages.shape[0]
-    _flat("row_offsets", row_offsets, torch.int64, (S + 1,))
+    _flat("row_offsets", row_offsets, torch.int64, (S + 1,))  # (None for calls without rows)
     _flat("cache_lens", cache_lens, torch.int32, (S,))
     n_pages, kv_heads, page_size, d = k_cache.shape
     return S, n_pages, kv_heads, page_size, d
@@ -160,6 +161,26 @@ def tree_words(parents: Sequence[int], device) -> torch.Tensor:
     return (words - ((words >> 31) << 32)).to(torch.int32).to(device)
 
 
+def _drawn(q: torch.Tensor, k_cache: torch.Tensor, pages: torch.Tensor, tree_mask: Optional[torch.Tensor], rows: int,
+           max_rows: Optional[int], max_keys: Optional[int]) -> Tuple[int, int, int]:
+    """Checks q and the mask of rows over a paged cache: (mask words, max_rows, max_keys), the latter what can be at all
+    where they are not given."""
+    d = k_cache.shape[3]
+    _need(q.dim() == 3 and q.dtype == k_cache.dtype and q.shape[2] == d and q.stride(2) == 1,
+          f"q: [rows, q_heads, {d}] {k_cache.dtype} with dense heads")
+    words = 0
+    if tree_mask is not None:
+        _need(tree_mask.dim() == 2, "tree_mask: [rows, words]")
+        words = tree_mask.shape[1]
+        _flat("tree_mask", tree_mask, torch.int32, (rows, words))
+    if max_rows is None:
+        max_rows = rows if tree_mask is None else min(rows, 32 * words)
+        _need(max_rows <= 65535, "max_rows: to be given for more than 65535 rows (a sequence has that many at most)")
+    if max_keys is None:
+        max_keys = min(pages.shape[1] * k_cache.shape[2], 2 ** 31 - 1)
+    return words, int(max_rows), int(max_keys)
+
+
 class TreeAttention(_Call):
     """knn_tree_attention on these buffers: rows of drafts over the paged cache.
 
@@ -178,19 +199,8 @@ class TreeAttention(_Call):
         index = _on_device(q, k_cache=k_cache, v_cache=v_cache, pages=pages, row_offsets=row_offsets,
                            cache_lens=cache_lens, tree_mask=tree_mask, out=out, lse=lse)
         S, n_pages, kv_heads, page_size, d = _paged(k_cache, v_cache, pages, row_offsets, cache_lens)
-        _need(q.dim() == 3 and q.dtype == k_cache.dtype and q.shape[2] == d and q.stride(2) == 1,
-              f"q: [rows, q_heads, {d}] {k_cache.dtype} with dense heads")
+        words, max_rows, max_keys = _drawn(q, k_cache, pages, tree_mask, q.shape[0], max_rows, max_keys)
         rows, q_heads = q.shape[0], q.shape[1]
-        words = 0
-        if tree_mask is not None:
-            _need(tree_mask.dim() == 2, "tree_mask: [rows, words]")
-            words = tree_mask.shape[1]
-            _flat("tree_mask", tree_mask, torch.int32, (rows, words))
-        if max_rows is None:
-            max_rows = rows if tree_mask is None else min(rows, 32 * words)
-            _need(max_rows <= 65535, "max_rows: to be given for more than 65535 rows (a sequence has that many at most)")
-        if max_keys is None:
-            max_keys = min(pages.shape[1] * page_size, 2 ** 31 - 1)
         own = []
         if out is None:
             out = torch.empty((rows, q_heads, d), dtype=q.dtype, device=q.device)
@@ -233,6 +243,188 @@ def tree_attention(q, k_cache, v_cache, pages, row_offsets, cache_lens, max_rows
                          lse, want_lse)
     call.run(stream)
     return call.out if call.lse is None else (call.out, call.lse)
+
+
+class KeyWeights(_Call):
+    """knn_key_weights on these buffers: what the rows' attention put on each cached key, added to mass.
+
+    q [source rows, q_heads, d] and the cache's tensors as in TreeAttention, with lse [source rows, q_heads] fp32 as it
+    gave it; mass [n_pages, kv_heads, page_size] fp32 (zeros to begin with).  decay: the share that earlier weights keep.
+    source_rows [rows] int32 as in KVAppend: an accepted path out of a draft's rows.  key_positions [n_pages, kv_heads,
+    page_size] int32 gets positions [rows] int32 (default: the cache index) at the rows' own places.  max_rows, max_keys
+    and tree_mask as in TreeAttention.
+    """
+
+    def __init__(self, q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, pages: torch.Tensor,
+                 row_offsets: torch.Tensor, cache_lens: torch.Tensor, mass: torch.Tensor,
+                 max_rows: Optional[int] = None, max_keys: Optional[int] = None,
+                 key_positions: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                 source_rows: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, decay: float = 1.0):
+        index = _on_device(q, lse=lse, k_cache=k_cache, pages=pages, row_offsets=row_offsets, cache_lens=cache_lens,
+                           mass=mass, key_positions=key_positions, positions=positions, source_rows=source_rows,
+                           tree_mask=tree_mask)
+        S, n_pages, kv_heads, page_size, d = _paged(k_cache, k_cache, pages, row_offsets, cache_lens)
+        source = q.shape[0]
+        rows = source if source_rows is None else source_rows.numel()
+        words, max_rows, max_keys = _drawn(q, k_cache, pages, tree_mask, rows, max_rows, max_keys)
+        q_heads = q.shape[1]
+        _flat("lse", lse, torch.float32, (source, q_heads))
+        _flat("mass", mass, torch.float32, (n_pages, kv_heads, page_size))
+        _flat("key_positions", key_positions, torch.int32, (n_pages, kv_heads, page_size))
+        _flat("source_rows", source_rows, torch.int32, (rows,))
+        _flat("positions", positions, torch.int32, (rows,))
+        _need(positions is None or key_positions is not None, "positions without key_positions")
+        self.mass, self.key_positions = mass, key_positions
+        tensors = (q, lse, k_cache, pages, row_offsets, cache_lens, positions, source_rows, tree_mask)
+        args = (*map(_ptr, tensors), rows, source, S, q_heads, kv_heads, d, q.stride(0), q.stride(1), n_pages, page_size,
+                pages.shape[1], words, max_rows, max_keys, _dtype_code(q),
+                float(1.0 / math.sqrt(d) if scale is None else scale), float(decay), _ptr(mass), _ptr(key_positions))
+        self._keep(index, "knn_key_weights", args, (*tensors, mass, key_positions), ())
+
+    def run(self, stream=None) -> torch.Tensor:
+        """One call; returns mass, valid after stream sync."""
+        self._call(stream)
+        return self.mass
+
+
+def key_weights(q, lse, k_cache, pages, row_offsets, cache_lens, mass, max_rows=None, max_keys=None, key_positions=None,
+                positions=None, source_rows=None, tree_mask=None, scale=None, decay=1.0, stream=None):
+    """One-shot knn_key_weights: adds to mass and returns it."""
+    return KeyWeights(q, lse, k_cache, pages, row_offsets, cache_lens, mass, max_rows, max_keys, key_positions, positions,
+                      source_rows, tree_mask, scale, decay).run(stream)
+
+
+class CacheEvict(_Call):
+    """knn_cache_evict on these buffers: of each sequence's cached tokens the budgets[s] of most mass stay, in each key
+    head its own; the caches and the ledger (mass, key_positions) are closed up.
+
+    k_cache, v_cache, pages and cache_lens as in KVAppend, mass and key_positions as in KeyWeights (key_positions None:
+    a token's position is its cache index); budgets [S] int32 (negative: the sequence is left as it is); next_positions
+    [S] int32, the position of each sequence's next token (None: cache_lens).  Tokens at positions below `sinks`, or among
+    the last `recent` ones, stay before all others.  max_keys bounds cache_lens in every run (None: the table's room).
+    mass_out and positions_out take the ledger of afterwards; without them mass and key_positions are written.  run()
+    returns new_lens [S] int32, which is apart from cache_lens: copy it there for the next step.
+    """
+
+    def __init__(self, k_cache: torch.Tensor, v_cache: torch.Tensor, mass: torch.Tensor, pages: torch.Tensor,
+                 cache_lens: torch.Tensor, budgets: torch.Tensor, max_keys: Optional[int] = None,
+                 key_positions: Optional[torch.Tensor] = None, next_positions: Optional[torch.Tensor] = None,
+                 sinks: int = 0, recent: int = 0, mass_out: Optional[torch.Tensor] = None,
+                 positions_out: Optional[torch.Tensor] = None):
+        index = _on_device(k_cache, v_cache=v_cache, mass=mass, pages=pages, cache_lens=cache_lens, budgets=budgets,
+                           key_positions=key_positions, next_positions=next_positions, mass_out=mass_out,
+                           positions_out=positions_out)
+        S, n_pages, kv_heads, page_size, d = _paged(k_cache, v_cache, pages, None, cache_lens)
+        ledger = (n_pages, kv_heads, page_size)
+        mass_out = mass if mass_out is None else mass_out
+        positions_out = key_positions if positions_out is None else positions_out
+        for name, t, dtype, shape in (("mass", mass, torch.float32, ledger), ("mass_out", mass_out, torch.float32, ledger),
+                                      ("key_positions", key_positions, torch.int32, ledger),
+                                      ("positions_out", positions_out, torch.int32, ledger),
+                                      ("budgets", budgets, torch.int32, (S,)),
+                                      ("next_positions", next_positions, torch.int32, (S,))):
+            _flat(name, t, dtype, shape)
+        _need(key_positions is not None or positions_out is None, "positions_out without key_positions")
+        if max_keys is None:
+            max_keys = min(pages.shape[1] * page_size, 2 ** 31 - 1)
+        self.new_lens = torch.empty(S, dtype=torch.int32, device=k_cache.device)
+        need = load().knn_cache_evict_workspace_size(S, kv_heads, int(max_keys))
+        self.workspace = torch.empty(max(int(need), 256), dtype=torch.uint8, device=k_cache.device)
+        self.mass, self.key_positions = mass_out, positions_out
+        tensors = (k_cache, v_cache, mass, key_positions, pages, cache_lens, budgets, next_positions)
+        args = (*map(_ptr, tensors), S, kv_heads, d, n_pages, page_size, pages.shape[1], int(max_keys), int(sinks),
+                int(recent), _dtype_code(k_cache), _ptr(mass_out), _ptr(positions_out), _ptr(self.new_lens),
+                _ptr(self.workspace), self.workspace.numel())
+        self._keep(index, "knn_cache_evict", args, (*tensors, mass_out, positions_out), (self.new_lens, self.workspace))
+
+    def run(self, stream=None) -> torch.Tensor:
+        """One call; returns new_lens, valid after stream sync."""
+        self._call(stream)
+        return self.new_lens
+
+
+def cache_evict(k_cache, v_cache, mass, pages, cache_lens, budgets, max_keys=None, key_positions=None, next_positions=None,
+                sinks=0, recent=0, mass_out=None, positions_out=None, stream=None):
+    """One-shot knn_cache_evict: closes up the caches and the ledger and returns the new lengths [S].  max_keys that is not
+    given comes from cache_lens' present contents, which are copied to the host for that."""
+    if max_keys is None:
+        max_keys = max(1, min(int(cache_lens.max()), pages.shape[1] * k_cache.shape[2]))
+    return CacheEvict(k_cache, v_cache, mass, pages, cache_lens, budgets, max_keys, key_positions, next_positions, sinks,
+                      recent, mass_out, positions_out).run(stream)
+
+
+class ScoreAdjuster(_Call):
+    """knn_adjust_scores on these buffers: penalties, biases and a grammar's mask on scores [rows, V] (f32, bf16 or f16,
+    dense rows), before a Sampler draws from them.
+
+    scores are logits, or a distribution with probabilities=True.  history [S, width] int32 with history_lens [S] int32,
+    of which the first prompt_lens [S] are the prompt; row_offsets [S+1] int64 gives the sequences' rows (None: each row
+    is a sequence); row_tokens [rows] int32, the tokens that the rows were run on, count for the rows that see them
+    (tree_mask [rows, words] int32, see tree_words; None: a chain).  repetition, presence, frequency [rows] fp32 or None:
+    1, 0 and 0 (off).  bias_tokens [S, n] int32 with bias_values [S, n] fp32.  allowed [rows, (V + 31) // 32] int32, bit
+    v & 31 of word v >> 5 for each token that may be drawn.  out (allocated where it is not given) may be scores itself.
+    """
+
+    def __init__(self, scores: torch.Tensor, history: Optional[torch.Tensor] = None,
+                 history_lens: Optional[torch.Tensor] = None, prompt_lens: Optional[torch.Tensor] = None,
+                 row_offsets: Optional[torch.Tensor] = None, row_tokens: Optional[torch.Tensor] = None,
+                 tree_mask: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                 presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                 bias_tokens: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                 allowed: Optional[torch.Tensor] = None, probabilities: bool = False,
+                 out: Optional[torch.Tensor] = None):
+        index = _on_device(scores, history=history, history_lens=history_lens, prompt_lens=prompt_lens,
+                           row_offsets=row_offsets, row_tokens=row_tokens, tree_mask=tree_mask, repetition=repetition,
+                           presence=presence, frequency=frequency, bias_tokens=bias_tokens, bias_values=bias_values,
+                           allowed=allowed, out=out)
+        _need(scores.dim() == 2 and (scores.stride(1) == 1 or scores.shape[1] == 1),
+              "scores: [rows, V] with dense rows")
+        rows, V = scores.shape
+        S = rows if row_offsets is None else row_offsets.numel() - 1
+        width = words = n_bias = 0
+        for name, t in (("history", history), ("tree_mask", tree_mask), ("bias_tokens", bias_tokens)):
+            _need(t is None or t.dim() == 2, f"{name}: two dimensions")
+        if history is not None:
+            width = history.shape[1]
+        if tree_mask is not None:
+            words = tree_mask.shape[1]
+        if bias_tokens is not None:
+            n_bias = bias_tokens.shape[1]
+        i32, f32 = torch.int32, torch.float32
+        for name, t, dtype, shape in (
+                ("row_offsets", row_offsets, torch.int64, (S + 1,)), ("history", history, i32, (S, width)),
+                ("history_lens", history_lens, i32, (S,)), ("prompt_lens", prompt_lens, i32, (S,)),
+                ("row_tokens", row_tokens, i32, (rows,)), ("tree_mask", tree_mask, i32, (rows, words)),
+                ("repetition", repetition, f32, (rows,)), ("presence", presence, f32, (rows,)),
+                ("frequency", frequency, f32, (rows,)), ("bias_tokens", bias_tokens, i32, (S, n_bias)),
+                ("bias_values", bias_values, f32, (S, n_bias)), ("allowed", allowed, i32, (rows, (V + 31) // 32))):
+            _flat(name, t, dtype, shape)
+        own = ()
+        if out is None:
+            out = torch.empty((rows, V), dtype=scores.dtype, device=scores.device)
+            own = (out,)
+        _need(out.dtype == scores.dtype and tuple(out.shape) == (rows, V) and (out.stride(1) == 1 or V == 1),
+              f"out: [{rows}, {V}] {scores.dtype} with dense rows")
+        self.out = out
+        tensors = (scores, history, history_lens, prompt_lens, row_offsets, row_tokens, tree_mask, repetition, presence,
+                   frequency, bias_tokens, bias_values, allowed)
+        args = (*map(_ptr, tensors), rows, V, S, scores.stride(0), width, words, n_bias, out.stride(0),
+                int(bool(probabilities)), _dtype_code(scores), _ptr(out))
+        self._keep(index, "knn_adjust_scores", args, (*tensors, out), own)
+
+    def run(self, stream=None) -> torch.Tensor:
+        """One call; returns out, valid after stream sync."""
+        self._call(stream)
+        return self.out
+
+
+def adjust_scores(scores, history=None, history_lens=None, prompt_lens=None, row_offsets=None, row_tokens=None,
+                  tree_mask=None, repetition=None, presence=None, frequency=None, bias_tokens=None, bias_values=None,
+                  allowed=None, probabilities=False, out=None, stream=None):
+    """One-shot knn_adjust_scores: the adjusted scores."""
+    return ScoreAdjuster(scores, history, history_lens, prompt_lens, row_offsets, row_tokens, tree_mask, repetition,
+                         presence, frequency, bias_tokens, bias_values, allowed, probabilities, out).run(stream)
 
 
 class Sampler(_Call):

@@ -1,0 +1,215 @@
+"""Eviction on the GPU against the oracle, every place of the caches and the ledger equal: budgets, lengths from zero on,
+ties, protected tokens, masses that are no numbers, pages, and what has to stay as it was."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2405_19325_amd as knn
+from oracle import lm
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def batch(lens, Hk=2, d=64, page=16, dtype="bf16", seed=0, width=None, masses="spread"):
+    g = torch.Generator().manual_seed(seed)
+    need = [max(1, -(-n // page)) for n in lens]
+    width = width or max(need)
+    n_pages = sum(need) + 2
+    order = torch.randperm(n_pages, generator=g)
+    pages = torch.full((len(lens), width), -7, dtype=torch.int32)
+    at = 0
+    for s, n in enumerate(need):
+        pages[s, :n] = order[at:at + n].int()
+        at += n
+    shape = (n_pages, Hk, page)
+    # every place has elements of its own: whole numbers that the type holds
+    k = torch.randint(0, 256, (*shape, d), generator=g).to(TYPES[dtype])
+    mass = torch.randn(shape, generator=g).exp() if masses == "spread" else torch.randint(0, 3, shape, generator=g).float()
+    return {"k_cache": k.cuda(), "v_cache": (255 - k).flip(3).cuda(), "mass": mass.cuda(), "pages": pages.cuda(),
+            "key_positions": torch.randint(0, 10 * max(1, max(lens)), shape, generator=g, dtype=torch.int32).cuda(),
+            "cache_lens": torch.tensor(lens, dtype=torch.int32).cuda()}
+
+
+def ints(t):
+    return None if t is None else t.cpu().numpy()
+
+
+def bits(t):
+    return None if t is None else t.cpu().view({2: torch.int16, 4: torch.int32}[t.element_size()]).numpy()
+
+
+def check(x, budgets, next_positions=None, sinks=0, recent=0, max_keys=None, out=False, positions=True):
+    """Runs the eviction and compares all that it writes with the oracle, bit by bit."""
+    x = dict(x)
+    if not positions:
+        x["key_positions"] = None
+    budgets = torch.tensor(budgets, dtype=torch.int32).cuda()
+    nxt = None if next_positions is None else torch.tensor(next_positions, dtype=torch.int32).cuda()
+    outs = {}
+    if out:
+        outs["mass_out"] = torch.full_like(x["mass"], -3.0)
+        if positions:
+            outs["positions_out"] = torch.full_like(x["key_positions"], -4)
+    limit = max_keys if max_keys is not None else max(1, min(int(x["cache_lens"].max()), x["pages"].numel()
+                                                             // len(x["pages"]) * x["k_cache"].shape[2]))
+    # the caches as bit patterns, the masses as the numbers that order like them
+    want = lm.evict(bits(x["k_cache"]), bits(x["v_cache"]), x["mass"].cpu().numpy(), ints(x["key_positions"]),
+                    ints(x["pages"]), ints(x["cache_lens"]), ints(budgets), ints(nxt), sinks, recent, limit,
+                    *(ints(outs.get(n)) for n in ("mass_out", "positions_out")))
+    before = {n: t.clone() for n, t in x.items() if t is not None}
+    got = knn.cache_evict(x["k_cache"], x["v_cache"], x["mass"], x["pages"], x["cache_lens"], budgets, max_keys,
+                          key_positions=x["key_positions"], next_positions=nxt, sinks=sinks, recent=recent, **outs)
+    torch.cuda.synchronize()
+    assert np.array_equal(ints(got), want[4])
+    assert np.array_equal(bits(x["k_cache"]), want[0]) and np.array_equal(bits(x["v_cache"]), want[1])
+    assert np.array_equal(bits(outs.get("mass_out", x["mass"])), want[2].view(np.int32))
+    if positions:
+        assert np.array_equal(ints(outs.get("positions_out", x["key_positions"])), want[3])
+    for n in ("pages", "cache_lens") + (("mass", "key_positions") if out and positions else ()):
+        assert torch.equal(before[n], x[n])
+    return got
+
+
+@pytest.mark.parametrize("out", [False, True])
+@pytest.mark.parametrize("positions", [False, True])
+@pytest.mark.parametrize("masses", ["spread", "even"])
+def test_lengths_and_budgets(out, positions, masses):
+    lens = [0, 1, 2, 15, 16, 17, 64, 65, 200, 333]
+    budgets = [0, 0, 1, 7, 15, 17, 1, 64, 100, 0]
+    x = batch(lens, masses=masses, seed=len(masses))
+    check(x, budgets, next_positions=[3000] * 10, sinks=30, recent=300, out=out, positions=positions)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("page", [16, 64, 256])
+@pytest.mark.parametrize("Hk,d", [(1, 64), (5, 128), (2, 256), (3, 80), (2, 33), (1, 1), (2, 1024)])
+def test_heads_pages_and_sizes(dtype, page, Hk, d):
+    check(batch([100, 300, 5], Hk, d, page, dtype, seed=d), [50, 290, 4], recent=3, positions=False)
+
+
+@pytest.mark.parametrize("n,budget", [(1025, 1024), (1024, 1023), (4105, 4096), (5000, 100), (20000, 19999), (20000, 7000),
+                                      (40000, 3), (70001, 65536), (140000, 30000)])
+def test_long_lengths(n, budget):
+    for masses in ("spread", "even"):
+        check(batch([n, n // 3 + 1], 2, 64, 64, seed=n, masses=masses), [budget, budget], [10 * n, 10 * n], sinks=5,
+              recent=n // 2, out=masses == "even")
+
+
+def test_more_protected_tokens_than_the_budget():
+    x = batch([300, 300, 300], seed=1)
+    for budgets in ([100, 1, 299], [0, 200, 150]):
+        check({n: t.clone() for n, t in x.items()}, budgets, sinks=120, recent=110, positions=False)
+        check({n: t.clone() for n, t in x.items()}, budgets, [3000] * 3, sinks=1000, recent=1500)
+
+
+def test_protected_positions_at_the_ends_of_32_bits():
+    x = batch([100, 60, 50], seed=2)
+    top = 2 ** 31 - 1
+    x["key_positions"][::2] = top
+    x["key_positions"][1::3] = -(2 ** 31)
+    for sinks, recent, nxt in ((top, 5, top), (3, top, -(2 ** 31)), (0, 0, top), (0, 1, top), (0, top, top)):
+        check({n: t.clone() for n, t in x.items()}, [50, 10, 49], [nxt] * 3, sinks, recent)
+
+
+def test_masses_that_are_no_numbers():
+    x = batch([200, 200, 90], seed=3)
+    m = x["mass"].flatten()
+    for i, v in enumerate((float("nan"), float("inf"), -float("inf"), 0.0, -0.0, -1.0, 1e-45, -1e-45, 3.4e38)):
+        m[i::23] = v
+    for budgets in ([100, 30, 89], [180, 3, 1], [1, 199, 45]):
+        check({n: t.clone() for n, t in x.items()}, budgets)
+        check({n: t.clone() for n, t in x.items()}, budgets, sinks=40, recent=30, positions=False)
+    for v in (float("nan"), 0.0, float("-inf")):
+        x["mass"][:] = v
+        check({n: t.clone() for n, t in x.items()}, [100, 30, 89], sinks=4, recent=10, positions=False)
+    x["mass"][:] = torch.where(torch.rand_like(x["mass"]) < 0.5, 0.0, -0.0)  # equal, whatever their sign
+    check(x, [100, 30, 89])
+
+
+def test_sequences_that_are_left_as_they_are():
+    x = batch([100, 100, 100, 100, 100], width=8, seed=4)
+    x["pages"][1, 3] = -1
+    x["pages"][2, 6] = x["k_cache"].shape[0]
+    x["cache_lens"][3] = 8 * 16 + 1  # longer than its table
+    x["cache_lens"][4] = -5
+    for out in (False, True):
+        check({n: t.clone() for n, t in x.items()}, [100, 50, 50, 50, 50], out=out, max_keys=128)
+        check({n: t.clone() for n, t in x.items()}, [-1, -(2 ** 31), 99, 4, 0], out=out, max_keys=128)
+    x = batch([100, 90, 20], seed=5)
+    check(x, [10, 20, 10], max_keys=95, out=True)  # longer than the hint
+
+
+def test_far_pages_of_a_large_cache():
+    """Offsets past 2^32 bytes of keys, and past 2^31 elements."""
+    x = batch([300, 700], 2, 128, 256, seed=6)
+    n = 40000
+    move = n - x["k_cache"].shape[0]
+    big = {name: torch.zeros((n, *x[name].shape[1:]), dtype=x[name].dtype, device="cuda")
+           for name in ("k_cache", "v_cache", "mass", "key_positions")}
+    for name, t in big.items():
+        t[move:] = x[name]
+    pages = torch.where(x["pages"] >= 0, x["pages"] + move, x["pages"])
+    knn.cache_evict(big["k_cache"], big["v_cache"], big["mass"], pages, x["cache_lens"],
+                    torch.tensor([100, 650], dtype=torch.int32).cuda(), key_positions=big["key_positions"])
+    check(x, [100, 650])
+    for name, t in big.items():
+        assert torch.equal(t[move:], x[name]) and float(t[:move].abs().max()) == 0
+
+
+def test_step_after_step_in_a_graph():
+    """One token more each step, and one evicted; the graph is replayed on the lengths that it wrote."""
+    x = batch([80, 80], Hk=2, width=8, seed=7)  # pages for more than the 64 tokens that are there
+    x["cache_lens"][:] = 64
+    budgets = torch.tensor([64, 40], dtype=torch.int32).cuda()
+    nxt = torch.tensor([640, 640], dtype=torch.int32).cuda()
+    call = knn.CacheEvict(x["k_cache"], x["v_cache"], x["mass"], x["pages"], x["cache_lens"], budgets, 80,
+                          key_positions=x["key_positions"], next_positions=nxt, sinks=3, recent=10)
+
+    def step():
+        x["cache_lens"].add_(1)
+        nxt.add_(1)
+        call.run()
+        x["cache_lens"].copy_(call.new_lens)
+
+    kept = {n: t.clone() for n, t in dict(x, nxt=nxt).items()}
+
+    def back():
+        for n, t in kept.items():
+            (nxt if n == "nxt" else x[n]).copy_(t)
+
+    want = []
+    for _ in range(4):
+        step()
+        want.append({n: x[n].clone() for n in ("k_cache", "v_cache", "mass", "key_positions", "cache_lens")})
+    back()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    back()
+    for w in want:
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, t in w.items():
+            assert torch.equal(x[n], t), n
+    assert x["cache_lens"].tolist() == [64, 40]
+
+
+def test_argument_checks():
+    x = batch([100])
+    args = dict(k_cache=x["k_cache"], v_cache=x["v_cache"], mass=x["mass"], pages=x["pages"], cache_lens=x["cache_lens"],
+                budgets=torch.tensor([50], dtype=torch.int32).cuda())
+    for over in (dict(mass=x["mass"].half()), dict(mass=x["mass"][:1]), dict(key_positions=x["mass"]),
+                 dict(positions_out=x["key_positions"]), dict(budgets=args["budgets"].long()),
+                 dict(mass_out=x["mass"].cpu()), dict(v_cache=x["v_cache"][:, :1]), dict(next_positions=x["pages"])):
+        with pytest.raises(ValueError):
+            knn.cache_evict(**dict(args, **over))
+    for over in (dict(sinks=-1), dict(v_cache=x["k_cache"]), dict(max_keys=1 << 20), dict(max_keys=0)):
+        with pytest.raises(knn.KnnError):
+            knn.cache_evict(**dict(args, **over))
