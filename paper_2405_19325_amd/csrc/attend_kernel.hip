@@ -62,17 +62,6 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {  // to nearest, ti
     }
 }
 
-// 16-byte chunk c of row r of a tile in LDS lies at chunk c ^ spread(r).  LDS
-// has 64 banks, 16 chunks wide: the 16 rows x 1 chunk that 16 lanes of a
-// product's operand read take at once, and the 8 rows x 2 neighbouring chunks
-// of 32 lanes of a transposing read, then fall on 16 different ones.  (Rows of
-// 8 chunks lie two in 16.)
-template <int D>
-__device__ __forceinline__ int spread(int r) {
-    if constexpr (D == 64) return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
-    return ((r & 7) << 1) | ((r >> 3) & 1);
-}
-
 // Four 16-bit elements of one column: lane l of each 16 gets column l of the 4
 // rows whose 8-byte pieces the 16 lanes point at.
 __device__ __forceinline__ u32x2_t read_transposed(uint32_t lds) {

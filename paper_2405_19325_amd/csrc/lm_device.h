@@ -32,6 +32,17 @@ __device__ __forceinline__ Tile tile_of(const Args &a, int64_t s) {
     return t;
 }
 
+// 16-byte chunk c of row r of a tile in LDS lies at chunk c ^ spread(r).  LDS
+// has 64 banks, 16 chunks wide: the 16 rows x 1 chunk that 16 lanes of a
+// product's operand read take at once, and the 8 rows x 2 neighbouring chunks
+// of 32 lanes of a transposing read, then fall on 16 different ones.  (Rows of
+// 8 chunks lie two in 16.)
+template <int D>
+__device__ __forceinline__ int spread(int r) {
+    if constexpr (D == 64) return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
+    return ((r & 7) << 1) | ((r >> 3) & 1);
+}
+
 // Where cache index c of sequence s and key head h lies: its place in [n_pages,
 // kv_heads, page_size], or -1 where its page is none.  c is within the table.
 __device__ __forceinline__ int64_t place_of(const PagedCache &cache, int kv_heads, int64_t s, int h, int64_t c) {
