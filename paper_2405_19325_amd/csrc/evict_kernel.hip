@@ -8,10 +8,18 @@
 // The order as one number: the bits of a float, with the sign turned so that
 // they order like the values, lie in 1 .. 0xff800000 (0x007fffff is -infinity, 1
 // NaN).  With no more protected tokens than the budget these are 0xffffffff,
-// and all stay; with more, all others are 0 and none does.  The budget-th
-// largest number is found bit by bit.
+// and all stay; with more, all others are 0 and none does.  The border is the
+// budget-th largest number; of those equal to it the first ones stay.
 //
-// A workgroup takes a head of a sequence.
+// Heads of up to 8,192 tokens: a workgroup has them in registers and finds the
+// border two bits a round, by counting.  Longer ones are cut into segments,
+// a workgroup each, which ends at the budget so that a segment holds sources or
+// targets only.  All of a head's workgroups look at the same 4,096 tokens,
+// whose order gives two numbers that the border lies between but for one head
+// in thousands; each counts its segment's numbers above, at and below these and
+// lists those between.  A second launch finds the border in the few that are
+// listed (or, where it lies elsewhere, in all), and with it each segment's
+// share of the moves, which a last one makes.
 #include "lm_device.h"
 
 namespace knnlm {
@@ -20,6 +28,11 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
+constexpr int kHeld = 8;                    // tokens of a thread
+constexpr int kChunk = kHeld * kThreads;
+constexpr int kSegments = 64;               // of a head, about
+constexpr int kSamples = 4;                 // of a thread
+constexpr int64_t kGrid = int64_t{1} << 20;  // heads at once
 
 // A number that orders like x, NaN first.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -28,156 +41,652 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return b ^ ((b >> 31) != 0 ? 0xffffffffu : 0x80000000u);
 }
 
-// The sum over the workgroup, for every thread.  `part`: kWaves words.
-__device__ __forceinline__ uint32_t block_sum(uint32_t v, uint32_t *part) {
-    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
-    v = wave_incl_scan_u32(v, lane);
-    __syncthreads();
-    if (lane == kWave - 1) part[threadIdx.x / kWave] = v;
-    __syncthreads();
-    uint32_t sum = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += part[w];
-    return sum;
-}
+// LDS of the collective steps.  Their words alternate, so that a step may be
+// called again without a barrier.
+struct Shared {
+    uint32_t part[2][4 * kWaves];
+};
 
-// How many threads before this one have `flag`, and how many there are.
-__device__ __forceinline__ uint32_t block_rank(bool flag, uint32_t &total, uint32_t *part) {
+// The sums over the workgroup of N numbers that each wave has (the same in all
+// of its lanes).
+template <int N>
+__device__ __forceinline__ void block_sums(uint32_t (&v)[N], Shared &sh, int &turn) {
+    static_assert(N <= 4, "a row of 16 lanes each");
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = static_cast<int>(threadIdx.x) / kWave;
-    const uint64_t set = __ballot(flag);
-    __syncthreads();
-    if (lane == 0) part[wave] = static_cast<uint32_t>(__popcll(set));
-    __syncthreads();
-    uint32_t before = 0;
-    total = 0;
+    turn ^= 1;
+    uint32_t mine = v[0];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) before = total;
-        total += part[w];
-    }
-    return before + static_cast<uint32_t>(__popcll(set & ((uint64_t{1} << lane) - 1)));
+    for (int i = 1; i < N; ++i) mine = lane == i ? v[i] : mine;
+    if (lane < N) sh.part[turn][lane * kWaves + wave] = mine;
+    __syncthreads();
+    uint32_t x = lane < N * kWaves ? sh.part[turn][lane] : 0u;  // 16 waves: a row of lanes a number
+    x += dpp_u32<0xB1>(0u, x);
+    x += dpp_u32<0x4E>(0u, x);
+    x += dpp_u32<0x141>(0u, x);
+    x += dpp_u32<0x140>(0u, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = readlane_u32(x, 16 * i);
 }
 
-struct Ledger {
-    const EvictArgs &a;
+__device__ __forceinline__ uint32_t votes(bool flag) { return static_cast<uint32_t>(__popcll(__ballot(flag))); }
+
+// The rank-th largest (from 1) of what `count` counts: count(a, b, c, v) sets v
+// to how many numbers of this wave are at least a, b and c (a < b < c).  Where
+// a count is the rank itself, its bound serves as well as the number.
+template <class Count>
+__device__ __forceinline__ uint32_t border_of(uint32_t rank, Count count, Shared &sh, int &turn, bool exact) {
+    uint32_t border = 0;
+    for (int bit = 30; bit >= 0; bit -= 2) {
+        uint32_t v[3];
+        count(border | 1u << bit, border | 2u << bit, border | 3u << bit, v);
+        block_sums(v, sh, turn);
+        const uint32_t digit = v[2] >= rank ? 3u : v[1] >= rank ? 2u : v[0] >= rank ? 1u : 0u;
+        border |= digit << bit;
+        if (!exact && digit != 0 && v[digit - 1] == rank) break;
+    }
+    return border;
+}
+
+// A head of a sequence and what becomes of it.
+struct Head {
     int64_t s;
     int h;
+    int64_t n, keep;  // tokens; those that stay
     int64_t recent_from;
-    int mode;  // 0: protected ones are above all; 1: others are below all
+    bool leave;       // left as it is
 
-    __device__ __forceinline__ int64_t place(int64_t j) const { return place_of(a.cache, a.kv_heads, s, h, j); }
-    __device__ __forceinline__ bool fixed(int64_t j, int64_t at) const {
+    __device__ __forceinline__ int64_t place(const EvictArgs &a, int64_t j) const {
+        return place_of(a.cache, a.kv_heads, s, h, j);
+    }
+    __device__ __forceinline__ bool fixed(const EvictArgs &a, int64_t j, int64_t at) const {
         const int64_t p = a.key_positions != nullptr ? a.key_positions[at] : j;
         return p < a.sinks || p >= recent_from;
     }
-    __device__ __forceinline__ uint32_t order(int64_t j) const {
-        const int64_t at = place(j);
-        const bool f = fixed(j, at);
-        if (mode == 0) return f ? 0xffffffffu : order_of(a.mass[at]);
-        return f ? order_of(a.mass[at]) : 0u;
+};
+
+// For all threads of a workgroup together.
+__device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
+    Head x;
+    x.s = pair / a.kv_heads;
+    x.h = static_cast<int>(pair - x.s * a.kv_heads);
+    const int64_t len = a.cache_lens[x.s], budget = a.budgets[x.s];
+    const int64_t room = a.cache.table_width << a.cache.page_log2, limit = a.max_keys < room ? a.max_keys : room;
+    const int64_t n = len < 0 ? 0 : len;
+    x.recent_from = (a.next_positions != nullptr ? a.next_positions[x.s] : len) - a.recent;
+    x.leave = budget < 0 || budget >= n || n > limit;
+    if (!x.leave) {
+        bool whole = true;
+        const int64_t entries = (n + (int64_t{1} << a.cache.page_log2) - 1) >> a.cache.page_log2;
+        for (int64_t e = threadIdx.x; e < entries; e += kThreads) {
+            const int64_t page = a.cache.pages[x.s * a.cache.table_width + e];
+            whole = whole && page >= 0 && page < a.cache.n_pages;
+        }
+        x.leave = __syncthreads_or(!whole) != 0;
+    }
+    x.n = n < limit ? n : limit;
+    x.keep = x.leave ? x.n : budget;
+    return x;
+}
+
+__device__ __forceinline__ void put_len(const EvictArgs &a, const Head &x) {
+    a.new_lens[x.s] = x.leave ? a.cache_lens[x.s] : static_cast<int32_t>(x.keep);
+}
+
+// The ledger's entry of a token that stays where it is, where the ledger of
+// afterwards is another.
+__device__ __forceinline__ void carry(const EvictArgs &a, int64_t at) {
+    if (a.mass_out != a.mass) a.mass_out[at] = a.mass[at];
+    if (a.positions_out != a.key_positions) a.positions_out[at] = a.key_positions[at];
+}
+
+__device__ __forceinline__ void carry_all(const EvictArgs &a, const Head &x, int64_t from, int64_t to) {
+    if (a.mass_out == a.mass && a.positions_out == a.key_positions) return;
+    for (int64_t j = from + threadIdx.x; j < to; j += kThreads) {
+        const int64_t at = x.place(a, j);
+        if (at >= 0) carry(a, at);
+    }
+}
+
+// Up to 64 moves by a wave, one a lane: keys, values and the ledger's entries.
+template <int CHUNKS>  // of 16 bytes in a head; 0: any number of elements
+__device__ __forceinline__ void move(const EvictArgs &a, int64_t from, int64_t to, int count) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
+    if (lane < count) {
+        a.mass_out[to] = a.mass[from];
+        if (a.key_positions != nullptr) a.positions_out[to] = a.key_positions[from];
+    }
+    const int from_lo = static_cast<int>(from), from_hi = static_cast<int>(from >> 32);
+    const int to_lo = static_cast<int>(to), to_hi = static_cast<int>(to >> 32);
+    auto of = [](int lo, int hi, int m) {
+        return static_cast<int64_t>(static_cast<uint32_t>(__shfl(lo, m))) | static_cast<int64_t>(__shfl(hi, m)) << 32;
+    };
+    if constexpr (CHUNKS > 0) {
+        constexpr int AT_ONCE = kWave / CHUNKS, UNROLL = 4;
+        const int mine = lane / CHUNKS, chunk = lane % CHUNKS;
+        u32x4_t *k = static_cast<u32x4_t *>(a.k_cache), *v = static_cast<u32x4_t *>(a.v_cache);
+        for (int m = 0; m < count; m += AT_ONCE * UNROLL) {
+            u32x4_t kr[UNROLL], vr[UNROLL];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const int i = m + u * AT_ONCE + mine;
+                const int64_t src = of(from_lo, from_hi, i < count ? i : 0) * CHUNKS + chunk;
+                kr[u] = k[src], vr[u] = v[src];
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const int i = m + u * AT_ONCE + mine;
+                const int64_t dst = of(to_lo, to_hi, i < count ? i : 0) * CHUNKS + chunk;
+                if (i < count) k[dst] = kr[u], v[dst] = vr[u];
+            }
+        }
+    } else {
+        uint16_t *k = static_cast<uint16_t *>(a.k_cache), *v = static_cast<uint16_t *>(a.v_cache);
+        for (int m = 0; m < count; ++m) {
+            const int64_t src = of(from_lo, from_hi, m) * a.head_dim, dst = of(to_lo, to_hi, m) * a.head_dim;
+            for (int e = lane; e < a.head_dim; e += kWave) k[dst + e] = k[src + e], v[dst + e] = v[src + e];
+        }
+    }
+}
+
+// The moves that a head's workgroups found.
+struct Moves {
+    int32_t *count;  // [heads]
+    int32_t *from;   // [heads][most] cache indices, then where to
+    int64_t most;
+};
+
+// A head in a workgroup's registers.  `CHUNKS` as in move; MOVE: made here,
+// else left to another launch.
+template <bool MOVE, int CHUNKS>
+__global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves moves) {
+    __shared__ Shared sh;
+    __shared__ uint32_t ranks[kHeld * kWaves];
+    __shared__ uint16_t lists[MOVE ? 2 : 1][MOVE ? kChunk / 2 : 1];  // sources, targets
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
+    int turn = 0;
+    for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
+        const Head x = head_of(a, pair);
+        if (x.h == 0 && tid == 0) put_len(a, x);
+        if (x.leave) {
+            carry_all(a, x, 0, x.n);
+            if (!MOVE && tid == 0) moves.count[pair] = 0;
+            continue;
+        }
+        const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep);
+        uint32_t order[kHeld];  // 0 behind the last token
+        uint32_t fixed = 0;     // as bits
+        uint32_t protects[1] = {0};
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) {
+            order[r] = 0;
+            const int j = r * kThreads + tid;
+            if (r * kThreads >= n) continue;
+            bool f = false;
+            if (j < n) {
+                const int64_t at = x.place(a, j);
+                order[r] = order_of(a.mass[at]);
+                f = x.fixed(a, j, at);
+            }
+            fixed |= f ? 1u << r : 0u;
+            protects[0] += votes(f);
+        }
+        block_sums(protects, sh, turn);
+        const bool few = protects[0] <= static_cast<uint32_t>(keep);
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) {
+            const bool f = (fixed >> r & 1u) != 0u;
+            order[r] = few ? (f ? 0xffffffffu : order[r]) : (f ? order[r] : 0u);
+        }
+        uint32_t border = 0xffffffffu, all[2] = {0, 0};  // at the border and above, above
+        if (keep > 0) {
+            border = border_of(
+                keep,
+                [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
+                    v[0] = v[1] = v[2] = 0;
+#pragma unroll
+                    for (int r = 0; r < kHeld; ++r) {
+                        if (r * kThreads >= n) break;
+                        v[0] += votes(order[r] >= b0);
+                        v[1] += votes(order[r] >= b1);
+                        v[2] += votes(order[r] >= b2);
+                    }
+                },
+                sh, turn, false);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                all[0] += votes(order[r] >= border);
+                all[1] += votes(order[r] > border);
+            }
+            block_sums(all, sh, turn);
+        }
+        // The count of each (row of threads, wave) that come before this wave's: rows first.
+        auto before = [&](uint32_t(&mine)[kHeld], uint32_t(&sum)[kHeld]) {
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r)
+                if (lane == 0) ranks[r * kWaves + wave] = mine[r];
+            __syncthreads();
+            const uint32_t lo = ranks[2 * lane], hi = ranks[2 * lane + 1];
+            const uint32_t upto = wave_incl_scan_u32(lo + hi, lane);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                const int i = r * kWaves + wave;
+                const uint32_t pair_end = readlane_u32(upto, i >> 1);
+                sum[r] = pair_end - ((i & 1) != 0 ? readlane_u32(hi, i >> 1) : readlane_u32(lo + hi, i >> 1));
+            }
+        };
+        const uint64_t under = (uint64_t{1} << lane) - 1;
+        uint32_t kept = 0;  // as bits
+        if (keep > 0 && all[0] != static_cast<uint32_t>(keep)) {
+            const uint32_t even = keep - all[1];  // of those at the border
+            uint32_t mine[kHeld], sum[kHeld];
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) mine[r] = votes(order[r] == border);
+            before(mine, sum);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                const uint32_t rank = sum[r] + static_cast<uint32_t>(__popcll(__ballot(order[r] == border) & under));
+                kept |= order[r] > border || (order[r] == border && rank < even) ? 1u << r : 0u;
+            }
+        } else if (keep > 0) {
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) kept |= order[r] >= border ? 1u << r : 0u;
+        }
+        uint32_t mine[kHeld], sum[kHeld];
+        uint64_t sources[kHeld], targets[kHeld];
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) {
+            const int j = r * kThreads + tid;
+            const bool k = (kept >> r & 1u) != 0u;
+            sources[r] = __ballot(k && j >= keep);
+            targets[r] = __ballot(!k && j < keep);
+            mine[r] = static_cast<uint32_t>(__popcll(sources[r])) | static_cast<uint32_t>(__popcll(targets[r])) << 16;
+            if (k && j < keep && (a.mass_out != a.mass || a.positions_out != a.key_positions)) carry(a, x.place(a, j));
+        }
+        before(mine, sum);
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) {
+            const int j = r * kThreads + tid;
+            const bool source = (sources[r] >> lane & 1u) != 0u, target = (targets[r] >> lane & 1u) != 0u;
+            const uint32_t rs = (sum[r] & 0xffffu) + static_cast<uint32_t>(__popcll(sources[r] & under));
+            const uint32_t rt = (sum[r] >> 16) + static_cast<uint32_t>(__popcll(targets[r] & under));
+            if constexpr (MOVE) {
+                if (source) lists[0][rs] = static_cast<uint16_t>(j);
+                if (target) lists[1][rt] = static_cast<uint16_t>(j);
+            } else {
+                if (source) moves.from[pair * 2 * moves.most + rs] = j;
+                if (target) moves.from[(pair * 2 + 1) * moves.most + rt] = j;
+            }
+        }
+        const uint32_t each = (ranks[2 * lane] & 0xffffu) + (ranks[2 * lane + 1] & 0xffffu);
+        const uint32_t total = readlane_u32(wave_incl_scan_u32(each, lane), kWave - 1);
+        if constexpr (MOVE) __syncthreads();
+        if constexpr (MOVE) {
+            for (uint32_t m = wave * kWave; m < total; m += kWaves * kWave) {
+                const uint32_t i = m + lane < total ? m + lane : m;
+                move<CHUNKS>(a, x.place(a, lists[0][i]), x.place(a, lists[1][i]),
+                             static_cast<int>(total - m < kWave ? total - m : kWave));
+            }
+            __syncthreads();
+        } else if (tid == 0) {
+            moves.count[pair] = static_cast<int32_t>(total);
+        }
+    }
+}
+
+template <int CHUNKS>
+__global__ __launch_bounds__(256) void k_evict_move(EvictArgs a, Moves moves) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
+    for (int64_t pair = blockIdx.y; pair < a.S * a.kv_heads; pair += gridDim.y) {
+        const int64_t s = pair / a.kv_heads;
+        const int h = static_cast<int>(pair - s * a.kv_heads);
+        const int64_t count = moves.count[pair];
+        const int32_t *from = moves.from + pair * 2 * moves.most, *to = from + moves.most;
+        for (int64_t m = (static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave) * kWave; m < count;
+             m += static_cast<int64_t>(gridDim.x) * 4 * kWave) {
+            const int64_t i = m + lane < count ? m + lane : m;
+            move<CHUNKS>(a, place_of(a.cache, a.kv_heads, s, h, from[i]), place_of(a.cache, a.kv_heads, s, h, to[i]),
+                         static_cast<int>(count - m < kWave ? count - m : kWave));
+        }
+    }
+}
+
+// What a segment's workgroup counted in the first launch.
+struct Counts {
+    uint32_t low, high;               // the two numbers, the same for all segments of a head
+    uint32_t above, at_high, between, at_low;  // how many of the segment's are over `high`, at it, ...
+    uint32_t fixed;
+    uint32_t pad;
+};
+
+// The segments of a head: [0, keep) and [keep, n) in pieces of `size`.
+struct Segments {
+    int64_t size;
+    int below, all;  // how many lie below the budget; all
+
+    __device__ __forceinline__ Segments(const Head &x, int64_t size_) : size(size_) {
+        below = static_cast<int>((x.keep + size - 1) / size);
+        all = below + static_cast<int>((x.n - x.keep + size - 1) / size);
+    }
+    __device__ __forceinline__ int64_t begin(const Head &x, int w) const {
+        return w < below ? w * size : x.keep + (w - below) * size;
+    }
+    __device__ __forceinline__ int64_t end(const Head &x, int w) const {
+        const int64_t e = begin(x, w) + size, most = w < below ? x.keep : x.n;
+        return e < most ? e : most;
+    }
+    __device__ __forceinline__ int of(const Head &x, int64_t j) const {
+        return j < x.keep ? static_cast<int>(j / size) : below + static_cast<int>((j - x.keep) / size);
     }
 };
 
-__global__ __launch_bounds__(kThreads) void k_cache_evict(EvictArgs a, int32_t *lists, int64_t most) {
-    __shared__ uint32_t part[kWaves];
-    const int64_t pair = blockIdx.x;
-    const int64_t s = pair / a.kv_heads;
-    const int h = static_cast<int>(pair % a.kv_heads);
-    const int64_t len = a.cache_lens[s], budget = a.budgets[s];
-    const int64_t room = a.cache.table_width << a.cache.page_log2;
-    const int64_t limit = a.max_keys < room ? a.max_keys : room;
-    const int64_t n = len < 0 ? 0 : len;
-    // Left as it is: within the budget, too long, or with a page that is none.
-    bool whole = n <= limit;
-    const int64_t entries = ((n < limit ? n : limit) + (int64_t{1} << a.cache.page_log2) - 1) >> a.cache.page_log2;
-    for (int64_t e = threadIdx.x; e < entries; e += kThreads) {
-        const int64_t page = a.cache.pages[s * a.cache.table_width + e];
-        if (page < 0 || page >= a.cache.n_pages) whole = false;
-    }
-    const bool leave = __syncthreads_or(!whole) != 0 || budget < 0 || budget >= n;
-    const int64_t K = leave ? n : budget;
-    if (h == 0 && threadIdx.x == 0) a.new_lens[s] = static_cast<int32_t>(leave ? len : budget);
-    const bool copies = a.mass_out != a.mass, turns = a.positions_out != a.key_positions;
-    if (copies || turns) {
-        const int64_t upto = K < limit ? K : limit;
-        for (int64_t j = threadIdx.x; j < upto; j += kThreads) {
-            const int64_t at = place_of(a.cache, a.kv_heads, s, h, j);
-            if (at < 0) continue;
-            if (copies) a.mass_out[at] = a.mass[at];
-            if (turns) a.positions_out[at] = a.key_positions[at];
-        }
-    }
-    if (leave) return;
+constexpr int kMostSegments = kSegments + 2;
 
-    const int64_t next = a.next_positions != nullptr ? a.next_positions[s] : len;
-    Ledger ledger{a, s, h, next - a.recent, 0};
-    uint32_t count = 0;
-    for (int64_t j = threadIdx.x; j < n; j += kThreads) count += ledger.fixed(j, ledger.place(j)) ? 1u : 0u;
-    ledger.mode = block_sum(count, part) > static_cast<uint64_t>(K) ? 1 : 0;
-    uint32_t border = 0;  // the K-th largest number, the largest of which K are as large
-    uint32_t above = 0;   // how many are larger
-    if (K > 0) {
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t to = border | 1u << bit;
-            count = 0;
-            for (int64_t j = threadIdx.x; j < n; j += kThreads) count += ledger.order(j) >= to ? 1u : 0u;
-            count = block_sum(count, part);
-            if (count >= static_cast<uint64_t>(K)) border = to;
+// The number of token j, where there are no more protected ones than the budget
+// (few), or more.
+__device__ __forceinline__ uint32_t number_of(const EvictArgs &a, const Head &x, int64_t j, bool few, bool *fixed = nullptr) {
+    const int64_t at = x.place(a, j);
+    const bool f = x.fixed(a, j, at);
+    if (fixed != nullptr) *fixed = f;
+    return few ? (f ? 0xffffffffu : order_of(a.mass[at])) : (f ? order_of(a.mass[at]) : 0u);
+}
+
+// The first launch over long heads: counts, and the numbers between, listed in
+// the segment's part of `lists` [heads][max_keys].
+__global__ __launch_bounds__(kThreads) void k_evict_count(EvictArgs a, Counts *counts, uint32_t *lists, int64_t size) {
+    __shared__ Shared sh;
+    __shared__ uint32_t listed;
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
+    int turn = 0;
+    for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
+        const Head x = head_of(a, pair);
+        const Segments seg(x, size);
+        const int w = static_cast<int>(blockIdx.y);
+        if (x.leave || w >= seg.all || x.keep == 0) continue;
+        // One token of each of 4,096 equal pieces, at no regular distance.
+        uint32_t sample[kSamples];
+        constexpr int kAll = kSamples * kThreads;
+        const int64_t some = x.n < kAll ? x.n : kAll;
+#pragma unroll
+        for (int r = 0; r < kSamples; ++r) {
+            const int64_t i = r * kThreads + tid;
+            sample[r] = 0;
+            if (i < some) {
+                const int64_t j0 = i * x.n / some, j1 = (i + 1) * x.n / some;
+                uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
+                mix ^= mix >> 15;
+                sample[r] = number_of(a, x, j0 + mix % static_cast<uint32_t>(j1 - j0), true);
+            }
         }
+        auto count = [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
+            v[0] = v[1] = v[2] = 0;
+#pragma unroll
+            for (int r = 0; r < kSamples; ++r) {
+                v[0] += votes(sample[r] >= b0);
+                v[1] += votes(sample[r] >= b1);
+                v[2] += votes(sample[r] >= b2);
+            }
+        };
+        // Four standard deviations of the sample's count to either side.
+        const float share = static_cast<float>(x.keep) / static_cast<float>(x.n), rank = share * static_cast<float>(some);
+        const float off = some < kAll ? 1.0f : 4.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
+        const int first = static_cast<int>(rank - off), last = static_cast<int>(rank + off) + 1;
+        const uint32_t high = first < 1 ? 0xffffffffu : border_of(first, count, sh, turn, true);
+        const uint32_t low = last > some ? 0u : border_of(last, count, sh, turn, true);
+        if (tid == 0) listed = 0;
+        __syncthreads();
+        uint32_t v[4] = {0, 0, 0, 0}, fixed[1] = {0};
+        const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
+        uint32_t *list = lists + pair * a.max_keys + begin;
+        for (int64_t j0 = begin; j0 < end; j0 += kThreads) {
+            const int64_t j = j0 + tid;
+            bool f = false;
+            const uint32_t o = j < end ? number_of(a, x, j, true, &f) : 0u;
+            const bool in = j < end, between = in && o > low && o < high;
+            v[0] += votes(in && o > high);
+            v[1] += votes(in && o == high);
+            v[3] += votes(in && o == low && o != high);
+            fixed[0] += votes(f);
+            const uint64_t set = __ballot(between);
+            const uint32_t n = static_cast<uint32_t>(__popcll(set));
+            v[2] += n;
+            uint32_t at = 0;
+            if (lane == 0 && n != 0) at = atomicAdd(&listed, n);
+            at = readlane_u32(at, 0);
+            if (between) list[at + __popcll(set & ((uint64_t{1} << lane) - 1))] = o;
+        }
+        block_sums(v, sh, turn);
+        block_sums(fixed, sh, turn);
+        if (tid == 0)
+            counts[pair * kMostSegments + w] = Counts{low, high, v[0], v[1], v[2], v[3], fixed[0], 0};
+        __syncthreads();
+    }
+}
+
+// The second one: the border, and each segment's sources or targets.
+__global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Counts *counts, const uint32_t *lists, int64_t size,
+                                                         Moves moves) {
+    __shared__ Shared sh;
+    __shared__ Counts held[kMostSegments];
+    __shared__ uint32_t over[kMostSegments], even[kMostSegments];  // over and at the border, of each segment
+    __shared__ uint32_t starts[kMostSegments + 1];                 // of the listed numbers
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
+    int turn = 0;
+    for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
+        const Head x = head_of(a, pair);
+        const Segments seg(x, size);
+        const int w = static_cast<int>(blockIdx.y);
+        if (x.h == 0 && w == 0 && tid == 0) put_len(a, x);
+        if (w == 0 && tid == 0 && (x.leave || x.keep == 0)) moves.count[pair] = 0;
+        if (w >= seg.all) continue;
+        const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
+        if (x.leave || x.keep == 0) {
+            if (x.leave) carry_all(a, x, begin, end);
+            continue;
+        }
+        __syncthreads();
+        if (tid < seg.all) held[tid] = counts[pair * kMostSegments + tid], over[tid] = even[tid] = 0;
+        __syncthreads();
+        uint32_t above = 0, at_high = 0, between = 0, at_low = 0, fixed = 0;
+        for (int i = 0; i < seg.all; ++i) {
+            if (tid == 0) starts[i] = between;
+            above += held[i].above, at_high += held[i].at_high, between += held[i].between, at_low += held[i].at_low;
+            fixed += held[i].fixed;
+        }
+        if (tid == 0) starts[seg.all] = between;
+        __syncthreads();
+        const uint32_t keep = static_cast<uint32_t>(x.keep), low = held[0].low, high = held[0].high;
+        const bool few = fixed <= keep;
+        uint32_t border;
+        auto listed = [&](uint32_t e, int &of) {  // the e-th listed number, and its segment
+            int lo = 0, hi = seg.all;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (starts[mid] <= e) lo = mid; else hi = mid;
+            }
+            of = lo;
+            return lists[pair * a.max_keys + seg.begin(x, lo) + (e - starts[lo])];
+        };
+        if (few && keep > above && keep <= above + at_high) {
+            border = high;
+            if (tid < seg.all) over[tid] = held[tid].above, even[tid] = held[tid].at_high;
+        } else if (few && keep > above + at_high && keep <= above + at_high + between) {
+            const uint32_t rank = keep - above - at_high;
+            uint32_t o[kHeld];
+            const bool fits = between <= static_cast<uint32_t>(kChunk);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                const uint32_t e = r * kThreads + tid;
+                int of;
+                o[r] = fits && e < between ? listed(e, of) : 0u;
+            }
+            border = border_of(
+                rank,
+                [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
+                    v[0] = v[1] = v[2] = 0;
+                    if (fits) {
+#pragma unroll
+                        for (int r = 0; r < kHeld; ++r) {
+                            if (static_cast<uint32_t>(r * kThreads) >= between) break;
+                            v[0] += votes(o[r] >= b0);
+                            v[1] += votes(o[r] >= b1);
+                            v[2] += votes(o[r] >= b2);
+                        }
+                    } else {
+                        for (uint32_t e0 = 0; e0 < between; e0 += kThreads) {
+                            int of;
+                            const uint32_t n = e0 + tid < between ? listed(e0 + tid, of) : 0u;
+                            v[0] += votes(n >= b0);
+                            v[1] += votes(n >= b1);
+                            v[2] += votes(n >= b2);
+                        }
+                    }
+                },
+                sh, turn, true);
+            if (tid < seg.all) over[tid] = held[tid].above + held[tid].at_high;
+            __syncthreads();
+            for (uint32_t e = tid; e < between; e += kThreads) {
+                int of;
+                const uint32_t n = listed(e, of);
+                if (n > border) atomicAdd(&over[of], 1u);
+                if (n == border) atomicAdd(&even[of], 1u);
+            }
+        } else if (few && keep > above + at_high + between && keep <= above + at_high + between + at_low) {
+            border = low;
+            if (tid < seg.all) {
+                over[tid] = held[tid].above + held[tid].at_high + held[tid].between;
+                even[tid] = held[tid].at_low;
+            }
+        } else {  // the two numbers do not hold it, or more tokens are protected than stay
+            border = border_of(
+                keep,
+                [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
+                    v[0] = v[1] = v[2] = 0;
+                    for (int64_t j0 = 0; j0 < x.n; j0 += kThreads) {
+                        const uint32_t n = j0 + tid < x.n ? number_of(a, x, j0 + tid, few) : 0u;
+                        v[0] += votes(n >= b0);
+                        v[1] += votes(n >= b1);
+                        v[2] += votes(n >= b2);
+                    }
+                },
+                sh, turn, true);
+            for (int64_t j = tid; j < x.n; j += kThreads) {
+                const uint32_t n = number_of(a, x, j, few);
+                if (n > border) atomicAdd(&over[seg.of(x, j)], 1u);
+                if (n == border) atomicAdd(&even[seg.of(x, j)], 1u);
+            }
+        }
+        __syncthreads();
+        // Of those at the border the first ones stay; and what comes before this segment.
+        uint32_t left = keep, first_even = 0, stays = 0, first = 0, all = 0;
+        for (int i = 0; i < seg.all; ++i) left -= over[i];
+        for (int i = 0; i < seg.all; ++i) {
+            const uint32_t take = even[i] < left ? even[i] : left;
+            const uint32_t kept = over[i] + take;
+            left -= take;
+            const uint32_t mine = i < seg.below ? static_cast<uint32_t>(seg.end(x, i) - seg.begin(x, i)) - kept : kept;
+            if (i == w) stays = take;
+            if (i < w && (i < seg.below) == (w < seg.below)) first += mine;
+            if (i >= seg.below) all += mine;
+        }
+        if (w == 0 && tid == 0) moves.count[pair] = static_cast<int32_t>(all);
+        int32_t *out = moves.from + (pair * 2 + (w < seg.below ? 1 : 0)) * moves.most;
+        for (int64_t j0 = begin; j0 < end; j0 += kThreads) {
+            const int64_t j = j0 + tid;
+            const uint32_t n = j < end ? number_of(a, x, j, few) : 0u;
+            const bool at_border = j < end && n == border;
+            bool kept = j < end && n > border;
+            // Ranks among the threads: at the border, then what is listed.
+            auto rank = [&](bool flag, uint32_t &sum) {
+                const uint64_t set = __ballot(flag);
+                turn ^= 1;
+                if (lane == 0) sh.part[turn][tid / kWave] = static_cast<uint32_t>(__popcll(set));
+                __syncthreads();
+                const uint32_t of = lane < kWaves ? sh.part[turn][lane] : 0u;
+                const uint32_t upto = wave_incl_scan_u32(of, lane);
+                sum = readlane_u32(upto, kWaves - 1);
+                return readlane_u32(upto - of, tid / kWave) + static_cast<uint32_t>(__popcll(set & ((uint64_t{1} << lane) - 1)));
+            };
+            uint32_t sum;
+            const uint32_t r = first_even + rank(at_border, sum);
+            first_even += sum;
+            kept = kept || (at_border && r < stays);
+            const bool moved = j < end && (w < seg.below ? !kept : kept);
+            const uint32_t to = first + rank(moved, sum);
+            first += sum;
+            if (moved) out[to] = static_cast<int32_t>(j);
+            else if (j < end && w < seg.below && (a.mass_out != a.mass || a.positions_out != a.key_positions)) carry(a, x.place(a, j));
+        }
+        __syncthreads();
+    }
+}
+
+struct Plan {
+    int64_t size, segments;  // of long heads
+    size_t off_counts, off_lists, off_from, total;
+    int64_t most;
+};
+
+Plan plan_evict(int64_t heads, int64_t max_keys) {
+    Plan p{};
+    const size_t n = static_cast<size_t>(heads), keys = static_cast<size_t>(max_keys);
+    auto take = [&](size_t bytes) {
+        const size_t at = p.total;
+        p.total += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    take(n * sizeof(int32_t));  // how many moves
+    p.most = max_keys / 2 + 1;  // no more than half of a head's tokens move
+    p.off_from = take(n * 2 * static_cast<size_t>(p.most) * sizeof(int32_t));
+    if (max_keys > kChunk) {
+        p.size = ((max_keys + kSegments - 1) / kSegments + kChunk - 1) / kChunk * kChunk;
+        p.segments = (max_keys + p.size - 1) / p.size + 1;
+        p.off_counts = take(n * kMostSegments * sizeof(Counts));
+        p.off_lists = take(n * keys * sizeof(uint32_t));
+    }
+    return p;
+}
+
+template <int CHUNKS>
+hipError_t launch(const EvictArgs &a, char *workspace, hipStream_t stream) {
+    const int64_t heads = a.S * a.kv_heads;
+    const Plan p = plan_evict(heads, a.max_keys);
+    const Moves moves{reinterpret_cast<int32_t *>(workspace), reinterpret_cast<int32_t *>(workspace + p.off_from), p.most};
+    const unsigned grid = static_cast<unsigned>(heads < kGrid ? heads : kGrid);
+    if (a.max_keys <= kChunk) {
+        if (heads >= 256 || a.max_keys <= 2048) {
+            k_evict_held<true, CHUNKS><<<dim3(grid), kThreads, 0, stream>>>(a, moves);
+            return hipGetLastError();
+        }
+        k_evict_held<false, CHUNKS><<<dim3(grid), kThreads, 0, stream>>>(a, moves);
     } else {
-        border = 0xffffffffu;
+        Counts *counts = reinterpret_cast<Counts *>(workspace + p.off_counts);
+        uint32_t *lists = reinterpret_cast<uint32_t *>(workspace + p.off_lists);
+        const dim3 segments(grid, static_cast<unsigned>(p.segments));
+        k_evict_count<<<segments, kThreads, 0, stream>>>(a, counts, lists, p.size);
+        k_evict_list<<<segments, kThreads, 0, stream>>>(a, counts, lists, p.size, moves);
     }
-    count = 0;
-    for (int64_t j = threadIdx.x; j < n; j += kThreads) count += ledger.order(j) > border ? 1u : 0u;
-    above = block_sum(count, part);
-    // Of those at the border the first ones stay.
-    const int64_t even = K - above;
-    int32_t *from = lists + pair * 2 * most, *to = from + most;
-    int64_t evens = 0, froms = 0, tos = 0;
-    for (int64_t j0 = 0; j0 < n; j0 += kThreads) {
-        const int64_t j = j0 + threadIdx.x;
-        const uint32_t o = j < n ? ledger.order(j) : 0u;
-        uint32_t total;
-        const bool at_border = j < n && o == border && K > 0;
-        const int64_t rank = evens + block_rank(at_border, total, part);
-        evens += total;
-        const bool kept = j < n && K > 0 && (o > border || (at_border && rank < even));
-        const bool source = kept && j >= K, target = j < K && !kept;
-        int64_t r = froms + block_rank(source, total, part);
-        froms += total;
-        if (source) from[r] = static_cast<int32_t>(j);
-        r = tos + block_rank(target, total, part);
-        tos += total;
-        if (target) to[r] = static_cast<int32_t>(j);
-    }
-    __syncthreads();
-    for (int64_t m = threadIdx.x / kWave; m < froms; m += kWaves) {
-        const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
-        const int64_t src = ledger.place(from[m]), dst = ledger.place(to[m]);
-        for (int e = lane; e < a.head_dim; e += kWave) {
-            uint16_t *k = static_cast<uint16_t *>(a.k_cache), *v = static_cast<uint16_t *>(a.v_cache);
-            k[dst * a.head_dim + e] = k[src * a.head_dim + e];
-            v[dst * a.head_dim + e] = v[src * a.head_dim + e];
-        }
-        if (lane == 0) {
-            a.mass_out[dst] = a.mass[src];
-            if (a.key_positions != nullptr) a.positions_out[dst] = a.key_positions[src];
-        }
-    }
-    if (a.key_positions == nullptr) return;
+    // Enough workgroups for 256 CUs; no more than a head can have moves for.
+    const int64_t batches = (p.most + 4 * kWave - 1) / (4 * kWave), wanted = (2048 + heads - 1) / heads;
+    const dim3 movers(static_cast<unsigned>(batches < wanted ? batches : wanted),
+                      static_cast<unsigned>(heads < 65535 ? heads : 65535));
+    k_evict_move<CHUNKS><<<movers, 256, 0, stream>>>(a, moves);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-// The indices that move and where to: no more than half of a head's tokens do.
-size_t evict_workspace(int64_t S, int64_t kv_heads, int64_t max_keys) {
-    return sizeof(int32_t) * 2 * static_cast<size_t>(S * kv_heads) * static_cast<size_t>(max_keys / 2 + 1);
-}
+size_t evict_workspace(int64_t S, int64_t kv_heads, int64_t max_keys) { return plan_evict(S * kv_heads, max_keys).total; }
 
 hipError_t launch_cache_evict(const EvictArgs &a, void *workspace, hipStream_t stream) {
-    k_cache_evict<<<dim3(static_cast<unsigned>(a.S * a.kv_heads)), kThreads, 0, stream>>>(
-        a, static_cast<int32_t *>(workspace), a.max_keys / 2 + 1);
-    return hipGetLastError();
+    char *ws = static_cast<char *>(workspace);
+    const bool aligned = reinterpret_cast<uintptr_t>(a.k_cache) % 16 == 0 && reinterpret_cast<uintptr_t>(a.v_cache) % 16 == 0;
+    switch (aligned ? a.head_dim : 0) {
+    case 64: return launch<8>(a, ws, stream);
+    case 128: return launch<16>(a, ws, stream);
+    case 256: return launch<32>(a, ws, stream);
+    default: return launch<0>(a, ws, stream);
+    }
 }
 
 }  // namespace knnlm
