@@ -82,9 +82,29 @@ __device__ __forceinline__ uint32_t border_of(uint32_t rank, Count count, Shared
         block_sums(v, sh, turn);
         const uint32_t digit = v[2] >= rank ? 3u : v[1] >= rank ? 2u : v[0] >= rank ? 1u : 0u;
         border |= digit << bit;
-        if (!exact && digit != 0 && v[digit - 1] == rank) break;
+        if (!exact && (v[0] == rank || v[1] == rank || v[2] == rank)) break;
     }
     return border;
+}
+
+// What comes before this wave's counts of each row of threads, rows first and
+// waves within them, and all of them.  `ranks`: kHeld x kWaves words.
+__device__ __forceinline__ void before(uint32_t *ranks, const uint32_t (&mine)[kHeld], uint32_t (&sum)[kHeld], uint32_t &total) {
+    static_assert(kHeld * kWaves == 2 * kWave, "two a lane");
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    __syncthreads();
+    uint32_t v = mine[0];
+#pragma unroll
+    for (int r = 1; r < kHeld; ++r) v = lane == r ? mine[r] : v;
+    if (lane < kHeld) ranks[lane * kWaves + wave] = v;
+    __syncthreads();
+    const uint32_t lo = ranks[2 * lane], hi = ranks[2 * lane + 1];
+    const uint32_t upto = wave_incl_scan_u32(lo + hi, lane);
+    const uint32_t mine_first = upto - lo - hi + ((wave & 1) != 0 ? lo : 0u);
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) sum[r] = readlane_u32(mine_first, (r * kWaves + wave) >> 1);
+    total = readlane_u32(upto, kWave - 1);
 }
 
 // A head of a sequence and what becomes of it.
@@ -98,9 +118,40 @@ struct Head {
     __device__ __forceinline__ int64_t place(const EvictArgs &a, int64_t j) const {
         return place_of(a.cache, a.kv_heads, s, h, j);
     }
-    __device__ __forceinline__ bool fixed(const EvictArgs &a, int64_t j, int64_t at) const {
-        const int64_t p = a.key_positions != nullptr ? a.key_positions[at] : j;
-        return p < a.sinks || p >= recent_from;
+    // Tokens j[0], j[1], ... (all of them there): their numbers by mass alone, and as bits which are protected.  The
+    // loads of all are on their way together.
+    template <int N>
+    __device__ __forceinline__ void orders(const EvictArgs &a, const int (&j)[N], uint32_t (&o)[N], uint32_t &fixed) const {
+        const int32_t *table = a.cache.pages + s * a.cache.table_width;
+        const int in_page = (1 << a.cache.page_log2) - 1;
+        int64_t at[N];
+        float m[N];
+        int32_t p[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            at[i] = ((static_cast<int64_t>(table[j[i] >> a.cache.page_log2]) * a.kv_heads + h) << a.cache.page_log2) + (j[i] & in_page);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            m[i] = a.mass[at[i]];
+            p[i] = a.key_positions != nullptr ? a.key_positions[at[i]] : j[i];
+        }
+        fixed = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            o[i] = order_of(m[i]);
+            fixed |= p[i] < a.sinks || p[i] >= recent_from ? 1u << i : 0u;
+        }
+    }
+    // The numbers themselves, where there are no more protected ones than the budget (few), or more.
+    template <int N>
+    __device__ __forceinline__ void numbers(const EvictArgs &a, const int (&j)[N], bool few, uint32_t (&o)[N]) const {
+        uint32_t fixed;
+        orders(a, j, o, fixed);
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = number(o[i], (fixed >> i & 1u) != 0u, few);
+    }
+    __device__ static __forceinline__ uint32_t number(uint32_t order, bool fixed, bool few) {
+        return few ? (fixed ? 0xffffffffu : order) : (fixed ? order : 0u);
     }
 };
 
@@ -117,9 +168,13 @@ __device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
     if (!x.leave) {
         bool whole = true;
         const int64_t entries = (n + (int64_t{1} << a.cache.page_log2) - 1) >> a.cache.page_log2;
-        for (int64_t e = threadIdx.x; e < entries; e += kThreads) {
-            const int64_t page = a.cache.pages[x.s * a.cache.table_width + e];
-            whole = whole && page >= 0 && page < a.cache.n_pages;
+        const int32_t *table = a.cache.pages + x.s * a.cache.table_width;
+        for (int64_t e = threadIdx.x; e < entries; e += 4 * kThreads) {
+            int32_t page[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) page[u] = table[e + u * kThreads < entries ? e + u * kThreads : e];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) whole = whole && page[u] >= 0 && page[u] < a.cache.n_pages;
         }
         x.leave = __syncthreads_or(!whole) != 0;
     }
@@ -146,6 +201,9 @@ __device__ __forceinline__ void carry_all(const EvictArgs &a, const Head &x, int
         if (at >= 0) carry(a, at);
     }
 }
+
+// Moves that a wave makes at once: four loads of 16 bytes a lane of either cache.
+constexpr int batch_of(int chunks) { return chunks > 0 ? 4 * kWave / chunks : 16; }
 
 // Up to 64 moves by a wave, one a lane: keys, values and the ledger's entries.
 template <int CHUNKS>  // of 16 bytes in a head; 0: any number of elements
@@ -203,6 +261,7 @@ __global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves move
     __shared__ uint32_t ranks[kHeld * kWaves];
     __shared__ uint16_t lists[MOVE ? 2 : 1][MOVE ? kChunk / 2 : 1];  // sources, targets
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
+    const uint64_t under = (uint64_t{1} << lane) - 1;
     int turn = 0;
     for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
         const Head x = head_of(a, pair);
@@ -213,30 +272,18 @@ __global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves move
             continue;
         }
         const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep);
-        uint32_t order[kHeld];  // 0 behind the last token
-        uint32_t fixed = 0;     // as bits
-        uint32_t protects[1] = {0};
+        uint32_t order[kHeld], fixed, protects[1] = {0};
+        int j[kHeld];
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) {
-            order[r] = 0;
-            const int j = r * kThreads + tid;
-            if (r * kThreads >= n) continue;
-            bool f = false;
-            if (j < n) {
-                const int64_t at = x.place(a, j);
-                order[r] = order_of(a.mass[at]);
-                f = x.fixed(a, j, at);
-            }
-            fixed |= f ? 1u << r : 0u;
-            protects[0] += votes(f);
-        }
+        for (int r = 0; r < kHeld; ++r) j[r] = r * kThreads + tid < n ? r * kThreads + tid : n - 1;
+        x.orders(a, j, order, fixed);
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) protects[0] += votes(r * kThreads + tid < n && (fixed >> r & 1u) != 0u);
         block_sums(protects, sh, turn);
         const bool few = protects[0] <= static_cast<uint32_t>(keep);
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) {
-            const bool f = (fixed >> r & 1u) != 0u;
-            order[r] = few ? (f ? 0xffffffffu : order[r]) : (f ? order[r] : 0u);
-        }
+        for (int r = 0; r < kHeld; ++r)  // 0 behind the last token
+            order[r] = r * kThreads + tid < n ? Head::number(order[r], (fixed >> r & 1u) != 0u, few) : 0u;
         uint32_t border = 0xffffffffu, all[2] = {0, 0};  // at the border and above, above
         if (keep > 0) {
             border = border_of(
@@ -259,30 +306,13 @@ __global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves move
             }
             block_sums(all, sh, turn);
         }
-        // The count of each (row of threads, wave) that come before this wave's: rows first.
-        auto before = [&](uint32_t(&mine)[kHeld], uint32_t(&sum)[kHeld]) {
-            __syncthreads();
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r)
-                if (lane == 0) ranks[r * kWaves + wave] = mine[r];
-            __syncthreads();
-            const uint32_t lo = ranks[2 * lane], hi = ranks[2 * lane + 1];
-            const uint32_t upto = wave_incl_scan_u32(lo + hi, lane);
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                const int i = r * kWaves + wave;
-                const uint32_t pair_end = readlane_u32(upto, i >> 1);
-                sum[r] = pair_end - ((i & 1) != 0 ? readlane_u32(hi, i >> 1) : readlane_u32(lo + hi, i >> 1));
-            }
-        };
-        const uint64_t under = (uint64_t{1} << lane) - 1;
         uint32_t kept = 0;  // as bits
         if (keep > 0 && all[0] != static_cast<uint32_t>(keep)) {
             const uint32_t even = keep - all[1];  // of those at the border
-            uint32_t mine[kHeld], sum[kHeld];
+            uint32_t mine[kHeld], sum[kHeld], total;
 #pragma unroll
             for (int r = 0; r < kHeld; ++r) mine[r] = votes(order[r] == border);
-            before(mine, sum);
+            before(ranks, mine, sum, total);
 #pragma unroll
             for (int r = 0; r < kHeld; ++r) {
                 const uint32_t rank = sum[r] + static_cast<uint32_t>(__popcll(__ballot(order[r] == border) & under));
@@ -292,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves move
 #pragma unroll
             for (int r = 0; r < kHeld; ++r) kept |= order[r] >= border ? 1u << r : 0u;
         }
-        uint32_t mine[kHeld], sum[kHeld];
+        uint32_t mine[kHeld], sum[kHeld], total;
         uint64_t sources[kHeld], targets[kHeld];
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) {
@@ -303,7 +333,8 @@ __global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves move
             mine[r] = static_cast<uint32_t>(__popcll(sources[r])) | static_cast<uint32_t>(__popcll(targets[r])) << 16;
             if (k && j < keep && (a.mass_out != a.mass || a.positions_out != a.key_positions)) carry(a, x.place(a, j));
         }
-        before(mine, sum);
+        before(ranks, mine, sum, total);
+        total &= 0xffffu;
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) {
             const int j = r * kThreads + tid;
@@ -318,14 +349,13 @@ __global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves move
                 if (target) moves.from[(pair * 2 + 1) * moves.most + rt] = j;
             }
         }
-        const uint32_t each = (ranks[2 * lane] & 0xffffu) + (ranks[2 * lane + 1] & 0xffffu);
-        const uint32_t total = readlane_u32(wave_incl_scan_u32(each, lane), kWave - 1);
         if constexpr (MOVE) __syncthreads();
         if constexpr (MOVE) {
-            for (uint32_t m = wave * kWave; m < total; m += kWaves * kWave) {
-                const uint32_t i = m + lane < total ? m + lane : m;
+            constexpr int BATCH = batch_of(CHUNKS);
+            for (uint32_t m = wave * BATCH; m < total; m += kWaves * BATCH) {
+                const uint32_t i = lane < BATCH && m + lane < total ? m + lane : m;
                 move<CHUNKS>(a, x.place(a, lists[0][i]), x.place(a, lists[1][i]),
-                             static_cast<int>(total - m < kWave ? total - m : kWave));
+                             static_cast<int>(total - m < BATCH ? total - m : BATCH));
             }
             __syncthreads();
         } else if (tid == 0) {
@@ -342,11 +372,12 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictArgs a, Moves moves) {
         const int h = static_cast<int>(pair - s * a.kv_heads);
         const int64_t count = moves.count[pair];
         const int32_t *from = moves.from + pair * 2 * moves.most, *to = from + moves.most;
-        for (int64_t m = (static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave) * kWave; m < count;
-             m += static_cast<int64_t>(gridDim.x) * 4 * kWave) {
-            const int64_t i = m + lane < count ? m + lane : m;
+        constexpr int BATCH = batch_of(CHUNKS);
+        for (int64_t m = (static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave) * BATCH; m < count;
+             m += static_cast<int64_t>(gridDim.x) * 4 * BATCH) {
+            const int64_t i = lane < BATCH && m + lane < count ? m + lane : m;
             move<CHUNKS>(a, place_of(a.cache, a.kv_heads, s, h, from[i]), place_of(a.cache, a.kv_heads, s, h, to[i]),
-                         static_cast<int>(count - m < kWave ? count - m : kWave));
+                         static_cast<int>(count - m < BATCH ? count - m : BATCH));
         }
     }
 }
@@ -382,15 +413,6 @@ struct Segments {
 
 constexpr int kMostSegments = kSegments + 2;
 
-// The number of token j, where there are no more protected ones than the budget
-// (few), or more.
-__device__ __forceinline__ uint32_t number_of(const EvictArgs &a, const Head &x, int64_t j, bool few, bool *fixed = nullptr) {
-    const int64_t at = x.place(a, j);
-    const bool f = x.fixed(a, j, at);
-    if (fixed != nullptr) *fixed = f;
-    return few ? (f ? 0xffffffffu : order_of(a.mass[at])) : (f ? order_of(a.mass[at]) : 0u);
-}
-
 // The first launch over long heads: counts, and the numbers between, listed in
 // the segment's part of `lists` [heads][max_keys].
 __global__ __launch_bounds__(kThreads) void k_evict_count(EvictArgs a, Counts *counts, uint32_t *lists, int64_t size) {
@@ -407,17 +429,18 @@ __global__ __launch_bounds__(kThreads) void k_evict_count(EvictArgs a, Counts *c
         uint32_t sample[kSamples];
         constexpr int kAll = kSamples * kThreads;
         const int64_t some = x.n < kAll ? x.n : kAll;
+        int which[kSamples];
 #pragma unroll
         for (int r = 0; r < kSamples; ++r) {
-            const int64_t i = r * kThreads + tid;
-            sample[r] = 0;
-            if (i < some) {
-                const int64_t j0 = i * x.n / some, j1 = (i + 1) * x.n / some;
-                uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
-                mix ^= mix >> 15;
-                sample[r] = number_of(a, x, j0 + mix % static_cast<uint32_t>(j1 - j0), true);
-            }
+            const int64_t i = r * kThreads + tid < some ? r * kThreads + tid : some - 1;
+            const int64_t j0 = i * x.n / some, j1 = (i + 1) * x.n / some;
+            uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
+            mix ^= mix >> 15;
+            which[r] = static_cast<int>(j0 + mix % static_cast<uint32_t>(j1 - j0));
         }
+        x.numbers(a, which, true, sample);
+#pragma unroll
+        for (int r = 0; r < kSamples; ++r) sample[r] = r * kThreads + tid < some ? sample[r] : 0u;
         auto count = [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
             v[0] = v[1] = v[2] = 0;
 #pragma unroll
@@ -438,22 +461,32 @@ __global__ __launch_bounds__(kThreads) void k_evict_count(EvictArgs a, Counts *c
         uint32_t v[4] = {0, 0, 0, 0}, fixed[1] = {0};
         const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
         uint32_t *list = lists + pair * a.max_keys + begin;
-        for (int64_t j0 = begin; j0 < end; j0 += kThreads) {
-            const int64_t j = j0 + tid;
-            bool f = false;
-            const uint32_t o = j < end ? number_of(a, x, j, true, &f) : 0u;
-            const bool in = j < end, between = in && o > low && o < high;
-            v[0] += votes(in && o > high);
-            v[1] += votes(in && o == high);
-            v[3] += votes(in && o == low && o != high);
-            fixed[0] += votes(f);
-            const uint64_t set = __ballot(between);
-            const uint32_t n = static_cast<uint32_t>(__popcll(set));
-            v[2] += n;
+        for (int64_t j0 = begin; j0 < end; j0 += kChunk) {
+            int j[kHeld];
+            uint32_t o[kHeld], protects;
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) j[r] = static_cast<int>(j0 + r * kThreads + tid < end ? j0 + r * kThreads + tid : end - 1);
+            x.orders(a, j, o, protects);
+            // How many this thread lists, and where.
+            uint32_t set = 0;
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                const bool in = j0 + r * kThreads + tid < end, f = in && (protects >> r & 1u) != 0u;
+                o[r] = f ? 0xffffffffu : o[r];
+                v[0] += votes(in && o[r] > high);
+                v[1] += votes(in && o[r] == high);
+                v[3] += votes(in && o[r] == low && o[r] != high);
+                fixed[0] += votes(f);
+                set |= in && o[r] > low && o[r] < high ? 1u << r : 0u;
+            }
+            const uint32_t mine = __popc(set), upto = wave_incl_scan_u32(mine, lane), sum = readlane_u32(upto, kWave - 1);
+            v[2] += sum;
             uint32_t at = 0;
-            if (lane == 0 && n != 0) at = atomicAdd(&listed, n);
-            at = readlane_u32(at, 0);
-            if (between) list[at + __popcll(set & ((uint64_t{1} << lane) - 1))] = o;
+            if (lane == 0 && sum != 0) at = atomicAdd(&listed, sum);
+            at = readlane_u32(at, 0) + upto - mine;
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r)
+                if (set >> r & 1u) list[at++] = o[r];
         }
         block_sums(v, sh, turn);
         block_sums(fixed, sh, turn);
@@ -470,7 +503,9 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
     __shared__ Counts held[kMostSegments];
     __shared__ uint32_t over[kMostSegments], even[kMostSegments];  // over and at the border, of each segment
     __shared__ uint32_t starts[kMostSegments + 1];                 // of the listed numbers
+    __shared__ uint32_t ranks[kHeld * kWaves];
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
+    const uint64_t under = (uint64_t{1} << lane) - 1;
     int turn = 0;
     for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
         const Head x = head_of(a, pair);
@@ -497,7 +532,16 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
         __syncthreads();
         const uint32_t keep = static_cast<uint32_t>(x.keep), low = held[0].low, high = held[0].high;
         const bool few = fixed <= keep;
-        uint32_t border;
+        uint32_t border;  // (1 and more)
+        // The numbers of tokens j0 .. j0 + kChunk - 1 before `stop`, 0 of the others.
+        auto some = [&](int64_t j0, int64_t stop, uint32_t(&o)[kHeld]) {
+            int j[kHeld];
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) j[r] = static_cast<int>(j0 + r * kThreads + tid < stop ? j0 + r * kThreads + tid : stop - 1);
+            x.numbers(a, j, few, o);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) o[r] = j0 + r * kThreads + tid < stop ? o[r] : 0u;
+        };
         auto listed = [&](uint32_t e, int &of) {  // the e-th listed number, and its segment
             int lo = 0, hi = seg.all;
             while (hi - lo > 1) {
@@ -562,18 +606,27 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
                 keep,
                 [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
                     v[0] = v[1] = v[2] = 0;
-                    for (int64_t j0 = 0; j0 < x.n; j0 += kThreads) {
-                        const uint32_t n = j0 + tid < x.n ? number_of(a, x, j0 + tid, few) : 0u;
-                        v[0] += votes(n >= b0);
-                        v[1] += votes(n >= b1);
-                        v[2] += votes(n >= b2);
+                    for (int64_t j0 = 0; j0 < x.n; j0 += kChunk) {
+                        uint32_t o[kHeld];
+                        some(j0, x.n, o);
+#pragma unroll
+                        for (int r = 0; r < kHeld; ++r) {
+                            v[0] += votes(o[r] >= b0);
+                            v[1] += votes(o[r] >= b1);
+                            v[2] += votes(o[r] >= b2);
+                        }
                     }
                 },
                 sh, turn, true);
-            for (int64_t j = tid; j < x.n; j += kThreads) {
-                const uint32_t n = number_of(a, x, j, few);
-                if (n > border) atomicAdd(&over[seg.of(x, j)], 1u);
-                if (n == border) atomicAdd(&even[seg.of(x, j)], 1u);
+            for (int64_t j0 = 0; j0 < x.n; j0 += kChunk) {
+                uint32_t o[kHeld];
+                some(j0, x.n, o);
+#pragma unroll
+                for (int r = 0; r < kHeld; ++r) {
+                    const int64_t j = j0 + r * kThreads + tid;
+                    if (o[r] > border) atomicAdd(&over[seg.of(x, j)], 1u);
+                    if (o[r] == border) atomicAdd(&even[seg.of(x, j)], 1u);
+                }
             }
         }
         __syncthreads();
@@ -591,31 +644,36 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
         }
         if (w == 0 && tid == 0) moves.count[pair] = static_cast<int32_t>(all);
         int32_t *out = moves.from + (pair * 2 + (w < seg.below ? 1 : 0)) * moves.most;
-        for (int64_t j0 = begin; j0 < end; j0 += kThreads) {
-            const int64_t j = j0 + tid;
-            const uint32_t n = j < end ? number_of(a, x, j, few) : 0u;
-            const bool at_border = j < end && n == border;
-            bool kept = j < end && n > border;
-            // Ranks among the threads: at the border, then what is listed.
-            auto rank = [&](bool flag, uint32_t &sum) {
-                const uint64_t set = __ballot(flag);
-                turn ^= 1;
-                if (lane == 0) sh.part[turn][tid / kWave] = static_cast<uint32_t>(__popcll(set));
-                __syncthreads();
-                const uint32_t of = lane < kWaves ? sh.part[turn][lane] : 0u;
-                const uint32_t upto = wave_incl_scan_u32(of, lane);
-                sum = readlane_u32(upto, kWaves - 1);
-                return readlane_u32(upto - of, tid / kWave) + static_cast<uint32_t>(__popcll(set & ((uint64_t{1} << lane) - 1)));
-            };
-            uint32_t sum;
-            const uint32_t r = first_even + rank(at_border, sum);
-            first_even += sum;
-            kept = kept || (at_border && r < stays);
-            const bool moved = j < end && (w < seg.below ? !kept : kept);
-            const uint32_t to = first + rank(moved, sum);
-            first += sum;
-            if (moved) out[to] = static_cast<int32_t>(j);
-            else if (j < end && w < seg.below && (a.mass_out != a.mass || a.positions_out != a.key_positions)) carry(a, x.place(a, j));
+        const bool below = w < seg.below, carries = below && (a.mass_out != a.mass || a.positions_out != a.key_positions);
+        for (int64_t j0 = begin; j0 < end; j0 += kChunk) {
+            uint32_t o[kHeld], mine[kHeld], sum[kHeld], kept = 0, total;
+            some(j0, end, o);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                kept |= o[r] > border ? 1u << r : 0u;
+                mine[r] = votes(o[r] == border);
+            }
+            before(ranks, mine, sum, total);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                const uint32_t rank = first_even + sum[r] + static_cast<uint32_t>(__popcll(__ballot(o[r] == border) & under));
+                kept |= o[r] == border && rank < stays ? 1u << r : 0u;
+            }
+            first_even += total;
+            uint64_t set[kHeld];
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) {
+                const bool in = j0 + r * kThreads + tid < end, k = (kept >> r & 1u) != 0u;
+                set[r] = __ballot(in && k != below);
+                mine[r] = static_cast<uint32_t>(__popcll(set[r]));
+                if (carries && in && k) carry(a, x.place(a, j0 + r * kThreads + tid));
+            }
+            before(ranks, mine, sum, total);
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r)
+                if (set[r] >> lane & 1u)
+                    out[first + sum[r] + static_cast<uint32_t>(__popcll(set[r] & under))] = static_cast<int32_t>(j0 + r * kThreads + tid);
+            first += total;
         }
         __syncthreads();
     }
@@ -667,7 +725,8 @@ hipError_t launch(const EvictArgs &a, char *workspace, hipStream_t stream) {
         k_evict_list<<<segments, kThreads, 0, stream>>>(a, counts, lists, p.size, moves);
     }
     // Enough workgroups for 256 CUs; no more than a head can have moves for.
-    const int64_t batches = (p.most + 4 * kWave - 1) / (4 * kWave), wanted = (2048 + heads - 1) / heads;
+    constexpr int64_t BATCH = batch_of(CHUNKS);
+    const int64_t batches = (p.most + 4 * BATCH - 1) / (4 * BATCH), wanted = (8192 + heads - 1) / heads;
     const dim3 movers(static_cast<unsigned>(batches < wanted ? batches : wanted),
                       static_cast<unsigned>(heads < 65535 ? heads : 65535));
     k_evict_move<CHUNKS><<<movers, 256, 0, stream>>>(a, moves);
