@@ -11,8 +11,9 @@
 // and all stay; with more, all others are 0 and none does.  The border is the
 // budget-th largest number; of those equal to it the first ones stay.
 //
-// Heads of up to 8,192 tokens: a workgroup has them in registers and finds the
-// border two bits a round, by counting.  Longer ones are cut into segments,
+// Heads of up to 8,192 tokens: a workgroup has them in registers, 16 places a
+// thread, and finds the border eleven bits at a time by counting into bins.
+// Longer ones are cut into segments,
 // a workgroup each, which ends at the budget so that a segment holds sources or
 // targets only.  All of a head's workgroups look at the same 4,096 tokens,
 // whose order gives two numbers that the border lies between but for one head
@@ -26,12 +27,13 @@ namespace knnlm {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kHeld = 8;                    // tokens of a thread
+constexpr int kHeld = 16;                    // tokens of a thread, one behind the other: they lie within a page
 constexpr int kChunk = kHeld * kThreads;
-constexpr int kSegments = 64;               // of a head, about
-constexpr int kSamples = 4;                 // of a thread
+constexpr int kSegments = 64;                // of a head, about
+constexpr int kSamples = 8;                  // of a thread
+constexpr int kBits = 11, kBins = 1 << kBits;
 constexpr int64_t kGrid = int64_t{1} << 20;  // heads at once
 
 // A number that orders like x, NaN first.
@@ -41,70 +43,77 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return b ^ ((b >> 31) != 0 ? 0xffffffffu : 0x80000000u);
 }
 
-// LDS of the collective steps.  Their words alternate, so that a step may be
-// called again without a barrier.
+// LDS of the collective steps.
 struct Shared {
-    uint32_t part[2][4 * kWaves];
+    uint32_t bins[kBins];     // all 0 between them
+    uint32_t part[2][kWaves]; // these alternate, so that a sum may follow another without a barrier between
+    uint32_t bin, rank, count;
 };
 
-// The sums over the workgroup of N numbers that each wave has (the same in all
-// of its lanes).
-template <int N>
-__device__ __forceinline__ void block_sums(uint32_t (&v)[N], Shared &sh, int &turn) {
-    static_assert(N <= 4, "a row of 16 lanes each");
+__device__ __forceinline__ void clear(Shared &sh) {
+    static_assert(kBins == 4 * kThreads, "four bins a thread");
+    reinterpret_cast<uint4 *>(sh.bins)[threadIdx.x] = make_uint4(0, 0, 0, 0);
+}
+
+// What the threads before this one have of v together, and all (up to 2^32).
+__device__ __forceinline__ uint32_t before(uint32_t v, uint32_t &all, Shared &sh, int &turn) {
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = static_cast<int>(threadIdx.x) / kWave;
+    const uint32_t upto = wave_incl_scan_u32(v, lane);
     turn ^= 1;
-    uint32_t mine = v[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) mine = lane == i ? v[i] : mine;
-    if (lane < N) sh.part[turn][lane * kWaves + wave] = mine;
+    if (lane == kWave - 1) sh.part[turn][wave] = upto;
     __syncthreads();
-    uint32_t x = lane < N * kWaves ? sh.part[turn][lane] : 0u;  // 16 waves: a row of lanes a number
-    x += dpp_u32<0xB1>(0u, x);
-    x += dpp_u32<0x4E>(0u, x);
-    x += dpp_u32<0x141>(0u, x);
-    x += dpp_u32<0x140>(0u, x);
+    uint32_t first = upto - v;
+    all = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = readlane_u32(x, 16 * i);
-}
-
-__device__ __forceinline__ uint32_t votes(bool flag) { return static_cast<uint32_t>(__popcll(__ballot(flag))); }
-
-// The rank-th largest (from 1) of what `count` counts: count(a, b, c, v) sets v
-// to how many numbers of this wave are at least a, b and c (a < b < c).  Where
-// a count is the rank itself, its bound serves as well as the number.
-template <class Count>
-__device__ __forceinline__ uint32_t border_of(uint32_t rank, Count count, Shared &sh, int &turn, bool exact) {
-    uint32_t border = 0;
-    for (int bit = 30; bit >= 0; bit -= 2) {
-        uint32_t v[3];
-        count(border | 1u << bit, border | 2u << bit, border | 3u << bit, v);
-        block_sums(v, sh, turn);
-        const uint32_t digit = v[2] >= rank ? 3u : v[1] >= rank ? 2u : v[0] >= rank ? 1u : 0u;
-        border |= digit << bit;
-        if (!exact && (v[0] == rank || v[1] == rank || v[2] == rank)) break;
+    for (int w = 0; w < kWaves; ++w) {
+        const uint32_t x = sh.part[turn][w];
+        first += w < wave ? x : 0u;
+        all += x;
     }
-    return border;
+    return first;
 }
 
-// What comes before this wave's counts of each row of threads, rows first and
-// waves within them, and all of them.  `ranks`: kHeld x kWaves words.
-__device__ __forceinline__ void before(uint32_t *ranks, const uint32_t (&mine)[kHeld], uint32_t (&sum)[kHeld], uint32_t &total) {
-    static_assert(kHeld * kWaves == 2 * kWave, "two a lane");
-    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
-    __syncthreads();
-    uint32_t v = mine[0];
-#pragma unroll
-    for (int r = 1; r < kHeld; ++r) v = lane == r ? mine[r] : v;
-    if (lane < kHeld) ranks[lane * kWaves + wave] = v;
-    __syncthreads();
-    const uint32_t lo = ranks[2 * lane], hi = ranks[2 * lane + 1];
-    const uint32_t upto = wave_incl_scan_u32(lo + hi, lane);
-    const uint32_t mine_first = upto - lo - hi + ((wave & 1) != 0 ? lo : 0u);
-#pragma unroll
-    for (int r = 0; r < kHeld; ++r) sum[r] = readlane_u32(mine_first, (r * kWaves + wave) >> 1);
-    total = readlane_u32(upto, kWave - 1);
+// The border of the `rank` largest numbers: those over `over` are among them,
+// and of those equal to it the first `even`.
+struct Border {
+    uint32_t over, even;
+};
+
+// By eleven bits at a time, counted into bins.  each(f) calls f with all of
+// this thread's numbers (0: none), the same ones every time; rank is at least
+// 1 and at most as many as there are.
+template <class Each>
+__device__ __forceinline__ Border border_of(uint32_t rank, Each each, Shared &sh, int &turn) {
+    uint32_t prefix = 0;
+#pragma unroll 1
+    for (int shift = 32 - kBits;; shift = shift > kBits ? shift - kBits : 0) {
+        // (the last digit has the ten bits that are left)
+        const int bits = shift == 0 ? 32 - 2 * kBits : kBits;
+        const bool top = shift == 32 - kBits;
+        each([&](uint32_t o) {
+            if (o != 0u && (top || o >> (shift + bits) == prefix)) atomicAdd(&sh.bins[o >> shift & ((1u << bits) - 1u)], 1u);
+        });
+        __syncthreads();
+        // Four bins a thread, the highest ones first.
+        uint4 *mine = reinterpret_cast<uint4 *>(sh.bins) + (kThreads - 1 - threadIdx.x);
+        const uint4 c = *mine;
+        *mine = make_uint4(0, 0, 0, 0);
+        uint32_t all;
+        const uint32_t first = before(c.x + c.y + c.z + c.w, all, sh, turn);
+        if (rank > first && rank <= first + c.x + c.y + c.z + c.w) {
+            uint32_t left = rank - first, bin = 4 * (kThreads - 1 - threadIdx.x) + 3, count = c.w;
+            if (left > count) left -= count, --bin, count = c.z;
+            if (left > count) left -= count, --bin, count = c.y;
+            if (left > count) left -= count, --bin, count = c.x;
+            sh.bin = bin, sh.rank = left, sh.count = count;
+        }
+        __syncthreads();
+        prefix = prefix << bits | sh.bin;
+        rank = sh.rank;
+        const bool whole = sh.count == rank;  // all of the bin: no need to look into it
+        if (whole) return Border{prefix == 0 ? 0u : (prefix << shift) - 1u, 0u};
+        if (shift == 0) return Border{prefix, rank};
+    }
 }
 
 // A head of a sequence and what becomes of it.
@@ -114,44 +123,31 @@ struct Head {
     int64_t n, keep;  // tokens; those that stay
     int64_t recent_from;
     bool leave;       // left as it is
+    bool vec;         // the ledgers lie on 16 bytes
 
     __device__ __forceinline__ int64_t place(const EvictArgs &a, int64_t j) const {
         return place_of(a.cache, a.kv_heads, s, h, j);
     }
-    // Tokens j[0], j[1], ... (all of them there): their numbers by mass alone, and as bits which are protected.  The
-    // loads of all are on their way together.
+    // The number of a token, where there are no more protected ones than the budget (few), or more.
+    __device__ static __forceinline__ uint32_t number(uint32_t order, bool fixed, bool few) {
+        return few ? (fixed ? 0xffffffffu : order) : (fixed ? order : 0u);
+    }
+    __device__ __forceinline__ bool fixed(const EvictArgs &a, int32_t p) const { return p < a.sinks || p >= recent_from; }
+    // N tokens, wherever they lie: their numbers.  All loads are on their way together.
     template <int N>
-    __device__ __forceinline__ void orders(const EvictArgs &a, const int (&j)[N], uint32_t (&o)[N], uint32_t &fixed) const {
-        const int32_t *table = a.cache.pages + s * a.cache.table_width;
-        const int in_page = (1 << a.cache.page_log2) - 1;
+    __device__ __forceinline__ void numbers(const EvictArgs &a, const int (&j)[N], uint32_t (&o)[N]) const {
         int64_t at[N];
         float m[N];
         int32_t p[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            at[i] = ((static_cast<int64_t>(table[j[i] >> a.cache.page_log2]) * a.kv_heads + h) << a.cache.page_log2) + (j[i] & in_page);
+        for (int i = 0; i < N; ++i) at[i] = place(a, j[i]);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             m[i] = a.mass[at[i]];
             p[i] = a.key_positions != nullptr ? a.key_positions[at[i]] : j[i];
         }
-        fixed = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            o[i] = order_of(m[i]);
-            fixed |= p[i] < a.sinks || p[i] >= recent_from ? 1u << i : 0u;
-        }
-    }
-    // The numbers themselves, where there are no more protected ones than the budget (few), or more.
-    template <int N>
-    __device__ __forceinline__ void numbers(const EvictArgs &a, const int (&j)[N], bool few, uint32_t (&o)[N]) const {
-        uint32_t fixed;
-        orders(a, j, o, fixed);
-#pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = number(o[i], (fixed >> i & 1u) != 0u, few);
-    }
-    __device__ static __forceinline__ uint32_t number(uint32_t order, bool fixed, bool few) {
-        return few ? (fixed ? 0xffffffffu : order) : (fixed ? order : 0u);
+        for (int i = 0; i < N; ++i) o[i] = number(order_of(m[i]), fixed(a, p[i]), true);
     }
 };
 
@@ -180,6 +176,8 @@ __device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
     }
     x.n = n < limit ? n : limit;
     x.keep = x.leave ? x.n : budget;
+    x.vec = ((reinterpret_cast<uintptr_t>(a.mass) | reinterpret_cast<uintptr_t>(a.key_positions) |
+              reinterpret_cast<uintptr_t>(a.mass_out) | reinterpret_cast<uintptr_t>(a.positions_out)) % 16) == 0;
     return x;
 }
 
@@ -187,18 +185,86 @@ __device__ __forceinline__ void put_len(const EvictArgs &a, const Head &x) {
     a.new_lens[x.s] = x.leave ? a.cache_lens[x.s] : static_cast<int32_t>(x.keep);
 }
 
-// The ledger's entry of a token that stays where it is, where the ledger of
-// afterwards is another.
-__device__ __forceinline__ void carry(const EvictArgs &a, int64_t at) {
-    if (a.mass_out != a.mass) a.mass_out[at] = a.mass[at];
-    if (a.positions_out != a.key_positions) a.positions_out[at] = a.key_positions[at];
+// kHeld tokens from j0 on, a multiple of kHeld: what the ledger has of those in [from, to).
+struct Held {
+    int64_t at;      // place of the first
+    uint32_t in;     // as bits: those in the range
+    uint32_t fixed;  // and of these the protected ones
+    union {
+        float m[kHeld];
+        float4 m4[kHeld / 4];
+    };
+    union {
+        int32_t p[kHeld];
+        int4 p4[kHeld / 4];
+    };
+
+    __device__ __forceinline__ void load(const EvictArgs &a, const Head &x, int64_t j0, int64_t from, int64_t to) {
+        in = fixed = 0;
+        if (j0 >= to || j0 + kHeld <= from) return;
+        in = (1u << kHeld) - 1u;
+        if (j0 < from) in &= ~0u << (from - j0);
+        if (j0 + kHeld > to) in &= (1u << (to - j0)) - 1u;
+        at = x.place(a, j0);
+        if (x.vec) {
+#pragma unroll
+            for (int i = 0; i < kHeld / 4; ++i) {
+                m4[i] = reinterpret_cast<const float4 *>(a.mass + at)[i];
+                if (a.key_positions != nullptr) p4[i] = reinterpret_cast<const int4 *>(a.key_positions + at)[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                m[i] = a.mass[at + i];
+                if (a.key_positions != nullptr) p[i] = a.key_positions[at + i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            if (a.key_positions == nullptr) p[i] = static_cast<int32_t>(j0) + i;
+            fixed |= x.fixed(a, p[i]) ? 1u << i : 0u;
+        }
+        fixed &= in;
+    }
+    // 0 of those out of the range.
+    __device__ __forceinline__ void numbers(bool few, uint32_t (&o)[kHeld]) const {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            o[i] = (in >> i & 1u) != 0u ? Head::number(order_of(m[i]), (fixed >> i & 1u) != 0u, few) : 0u;
+    }
+    // The entries in the range go into a ledger of afterwards that is another.  (Those of places that are given up are
+    // written over by what moves there, later.)
+    __device__ __forceinline__ void carry(const EvictArgs &a, const Head &x) const {
+        const bool masses = a.mass_out != a.mass, positions = a.positions_out != a.key_positions;
+        if (in == (1u << kHeld) - 1u && x.vec) {
+#pragma unroll
+            for (int i = 0; i < kHeld / 4; ++i) {
+                if (masses) reinterpret_cast<float4 *>(a.mass_out + at)[i] = m4[i];
+                if (positions) reinterpret_cast<int4 *>(a.positions_out + at)[i] = p4[i];
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            if ((in >> i & 1u) == 0u) continue;
+            if (masses) a.mass_out[at + i] = m[i];
+            if (positions) a.positions_out[at + i] = p[i];
+        }
+    }
+};
+
+__device__ __forceinline__ bool carries(const EvictArgs &a) {
+    return a.mass_out != a.mass || a.positions_out != a.key_positions;
 }
 
+// The ledger's entries [from, to) of a head that is left as it is, as far as it has pages.
 __device__ __forceinline__ void carry_all(const EvictArgs &a, const Head &x, int64_t from, int64_t to) {
-    if (a.mass_out == a.mass && a.positions_out == a.key_positions) return;
+    if (!carries(a)) return;
     for (int64_t j = from + threadIdx.x; j < to; j += kThreads) {
         const int64_t at = x.place(a, j);
-        if (at >= 0) carry(a, at);
+        if (at < 0) continue;
+        if (a.mass_out != a.mass) a.mass_out[at] = a.mass[at];
+        if (a.positions_out != a.key_positions) a.positions_out[at] = a.key_positions[at];
     }
 }
 
@@ -253,16 +319,15 @@ struct Moves {
     int64_t most;
 };
 
-// A head in a workgroup's registers.  `CHUNKS` as in move; MOVE: made here,
-// else left to another launch.
+// A head in a workgroup's registers.  `CHUNKS` as in move; MOVE: the moves are
+// made here, else left to another launch.
 template <bool MOVE, int CHUNKS>
-__global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves moves) {
+__global__ __launch_bounds__(kThreads, 4) void k_evict_held(EvictArgs a, Moves moves) {
     __shared__ Shared sh;
-    __shared__ uint32_t ranks[kHeld * kWaves];
     __shared__ uint16_t lists[MOVE ? 2 : 1][MOVE ? kChunk / 2 : 1];  // sources, targets
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
-    const uint64_t under = (uint64_t{1} << lane) - 1;
     int turn = 0;
+    clear(sh);
     for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
         const Head x = head_of(a, pair);
         if (x.h == 0 && tid == 0) put_len(a, x);
@@ -271,86 +336,59 @@ __global__ __launch_bounds__(kThreads) void k_evict_held(EvictArgs a, Moves move
             if (!MOVE && tid == 0) moves.count[pair] = 0;
             continue;
         }
-        const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep);
-        uint32_t order[kHeld], fixed, protects[1] = {0};
-        int j[kHeld];
-#pragma unroll
-        for (int r = 0; r < kHeld; ++r) j[r] = r * kThreads + tid < n ? r * kThreads + tid : n - 1;
-        x.orders(a, j, order, fixed);
-#pragma unroll
-        for (int r = 0; r < kHeld; ++r) protects[0] += votes(r * kThreads + tid < n && (fixed >> r & 1u) != 0u);
-        block_sums(protects, sh, turn);
-        const bool few = protects[0] <= static_cast<uint32_t>(keep);
-#pragma unroll
-        for (int r = 0; r < kHeld; ++r)  // 0 behind the last token
-            order[r] = r * kThreads + tid < n ? Head::number(order[r], (fixed >> r & 1u) != 0u, few) : 0u;
-        uint32_t border = 0xffffffffu, all[2] = {0, 0};  // at the border and above, above
-        if (keep > 0) {
+        const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep), j0 = tid * kHeld;
+        Held t;
+        t.load(a, x, j0, 0, n);
+        uint32_t protects, o[kHeld];
+        before(__popc(t.fixed), protects, sh, turn);
+        const bool few = protects <= static_cast<uint32_t>(keep);
+        t.numbers(few, o);
+        const uint32_t rank = few ? keep - protects : keep;  // among those that are not protected, or among these alone
+        Border border{few ? 0xfffffffeu : 0xffffffffu, 0u};
+        if (rank > 0)
             border = border_of(
-                keep,
-                [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
-                    v[0] = v[1] = v[2] = 0;
+                rank,
+                [&](auto count) {
 #pragma unroll
-                    for (int r = 0; r < kHeld; ++r) {
-                        if (r * kThreads >= n) break;
-                        v[0] += votes(order[r] >= b0);
-                        v[1] += votes(order[r] >= b1);
-                        v[2] += votes(order[r] >= b2);
-                    }
+                    for (int i = 0; i < kHeld; ++i)
+                        if (o[i] != 0xffffffffu) count(o[i]);
                 },
-                sh, turn, false);
+                sh, turn);
+        uint32_t over = 0, at_it = 0;  // as bits
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                all[0] += votes(order[r] >= border);
-                all[1] += votes(order[r] > border);
+        for (int i = 0; i < kHeld; ++i) {
+            over |= o[i] > border.over ? 1u << i : 0u;
+            at_it |= o[i] == border.over ? 1u << i : 0u;
+        }
+        uint32_t all;
+        if (border.even != 0) {
+            uint32_t rank = before(__popc(at_it), all, sh, turn);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (at_it >> i & 1u) over |= rank++ < border.even ? 1u << i : 0u;
+        }
+        const uint32_t low = keep <= j0 ? 0u : keep >= j0 + kHeld ? (1u << kHeld) - 1u : (1u << (keep - j0)) - 1u;
+        const uint32_t sources = over & ~low, targets = t.in & low & ~over;
+        const uint32_t first = before(__popc(sources) | __popc(targets) << 16, all, sh, turn);
+        const uint32_t total = all & 0xffffu;
+        uint32_t rs = first & 0xffffu, rt = first >> 16;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            if (sources >> i & 1u) {
+                if constexpr (MOVE) lists[0][rs++] = static_cast<uint16_t>(j0 + i);
+                else moves.from[pair * 2 * moves.most + rs++] = j0 + i;
             }
-            block_sums(all, sh, turn);
-        }
-        uint32_t kept = 0;  // as bits
-        if (keep > 0 && all[0] != static_cast<uint32_t>(keep)) {
-            const uint32_t even = keep - all[1];  // of those at the border
-            uint32_t mine[kHeld], sum[kHeld], total;
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) mine[r] = votes(order[r] == border);
-            before(ranks, mine, sum, total);
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                const uint32_t rank = sum[r] + static_cast<uint32_t>(__popcll(__ballot(order[r] == border) & under));
-                kept |= order[r] > border || (order[r] == border && rank < even) ? 1u << r : 0u;
-            }
-        } else if (keep > 0) {
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) kept |= order[r] >= border ? 1u << r : 0u;
-        }
-        uint32_t mine[kHeld], sum[kHeld], total;
-        uint64_t sources[kHeld], targets[kHeld];
-#pragma unroll
-        for (int r = 0; r < kHeld; ++r) {
-            const int j = r * kThreads + tid;
-            const bool k = (kept >> r & 1u) != 0u;
-            sources[r] = __ballot(k && j >= keep);
-            targets[r] = __ballot(!k && j < keep);
-            mine[r] = static_cast<uint32_t>(__popcll(sources[r])) | static_cast<uint32_t>(__popcll(targets[r])) << 16;
-            if (k && j < keep && (a.mass_out != a.mass || a.positions_out != a.key_positions)) carry(a, x.place(a, j));
-        }
-        before(ranks, mine, sum, total);
-        total &= 0xffffu;
-#pragma unroll
-        for (int r = 0; r < kHeld; ++r) {
-            const int j = r * kThreads + tid;
-            const bool source = (sources[r] >> lane & 1u) != 0u, target = (targets[r] >> lane & 1u) != 0u;
-            const uint32_t rs = (sum[r] & 0xffffu) + static_cast<uint32_t>(__popcll(sources[r] & under));
-            const uint32_t rt = (sum[r] >> 16) + static_cast<uint32_t>(__popcll(targets[r] & under));
-            if constexpr (MOVE) {
-                if (source) lists[0][rs] = static_cast<uint16_t>(j);
-                if (target) lists[1][rt] = static_cast<uint16_t>(j);
-            } else {
-                if (source) moves.from[pair * 2 * moves.most + rs] = j;
-                if (target) moves.from[(pair * 2 + 1) * moves.most + rt] = j;
+            if (targets >> i & 1u) {
+                if constexpr (MOVE) lists[1][rt++] = static_cast<uint16_t>(j0 + i);
+                else moves.from[(pair * 2 + 1) * moves.most + rt++] = j0 + i;
             }
         }
-        if constexpr (MOVE) __syncthreads();
+        if (carries(a)) {
+            t.in &= low;
+            if (t.in != 0u) t.carry(a, x);
+        }
         if constexpr (MOVE) {
+            __syncthreads();
             constexpr int BATCH = batch_of(CHUNKS);
             for (uint32_t m = wave * BATCH; m < total; m += kWaves * BATCH) {
                 const uint32_t i = lane < BATCH && m + lane < total ? m + lane : m;
@@ -384,30 +422,33 @@ __global__ __launch_bounds__(256) void k_evict_move(EvictArgs a, Moves moves) {
 
 // What a segment's workgroup counted in the first launch.
 struct Counts {
-    uint32_t low, high;               // the two numbers, the same for all segments of a head
+    uint32_t low, high;                        // the two numbers, the same for all segments of a head
     uint32_t above, at_high, between, at_low;  // how many of the segment's are over `high`, at it, ...
     uint32_t fixed;
     uint32_t pad;
 };
 
-// The segments of a head: [0, keep) and [keep, n) in pieces of `size`.
+// The segments of a head: [0, keep) and [keep, n) in pieces of `size`, a
+// multiple of kChunk; those behind the budget count from its multiple of kHeld.
 struct Segments {
-    int64_t size;
+    int64_t size, behind;
     int below, all;  // how many lie below the budget; all
 
-    __device__ __forceinline__ Segments(const Head &x, int64_t size_) : size(size_) {
+    __device__ __forceinline__ Segments(const Head &x, int64_t size_) : size(size_), behind(x.keep / kHeld * kHeld) {
         below = static_cast<int>((x.keep + size - 1) / size);
-        all = below + static_cast<int>((x.n - x.keep + size - 1) / size);
+        all = below + static_cast<int>((x.n - (x.keep < x.n ? behind : x.n) + size - 1) / size);
     }
+    __device__ __forceinline__ int64_t start(int w) const { return w < below ? w * size : behind + (w - below) * size; }
     __device__ __forceinline__ int64_t begin(const Head &x, int w) const {
-        return w < below ? w * size : x.keep + (w - below) * size;
+        const int64_t b = start(w);
+        return w < below || b > x.keep ? b : x.keep;
     }
     __device__ __forceinline__ int64_t end(const Head &x, int w) const {
-        const int64_t e = begin(x, w) + size, most = w < below ? x.keep : x.n;
+        const int64_t e = start(w) + size, most = w < below ? x.keep : x.n;
         return e < most ? e : most;
     }
     __device__ __forceinline__ int of(const Head &x, int64_t j) const {
-        return j < x.keep ? static_cast<int>(j / size) : below + static_cast<int>((j - x.keep) / size);
+        return j < x.keep ? static_cast<int>(j / size) : below + static_cast<int>((j - behind) / size);
     }
 };
 
@@ -415,21 +456,21 @@ constexpr int kMostSegments = kSegments + 2;
 
 // The first launch over long heads: counts, and the numbers between, listed in
 // the segment's part of `lists` [heads][max_keys].
-__global__ __launch_bounds__(kThreads) void k_evict_count(EvictArgs a, Counts *counts, uint32_t *lists, int64_t size) {
+__global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts *counts, uint32_t *lists, int64_t size) {
     __shared__ Shared sh;
-    __shared__ uint32_t listed;
-    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
+    const int tid = static_cast<int>(threadIdx.x);
     int turn = 0;
+    clear(sh);
     for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
         const Head x = head_of(a, pair);
         const Segments seg(x, size);
         const int w = static_cast<int>(blockIdx.y);
         if (x.leave || w >= seg.all || x.keep == 0) continue;
         // One token of each of 4,096 equal pieces, at no regular distance.
-        uint32_t sample[kSamples];
         constexpr int kAll = kSamples * kThreads;
         const int64_t some = x.n < kAll ? x.n : kAll;
         int which[kSamples];
+        uint32_t sample[kSamples];
 #pragma unroll
         for (int r = 0; r < kSamples; ++r) {
             const int64_t i = r * kThreads + tid < some ? r * kThreads + tid : some - 1;
@@ -438,75 +479,61 @@ __global__ __launch_bounds__(kThreads) void k_evict_count(EvictArgs a, Counts *c
             mix ^= mix >> 15;
             which[r] = static_cast<int>(j0 + mix % static_cast<uint32_t>(j1 - j0));
         }
-        x.numbers(a, which, true, sample);
+        x.numbers(a, which, sample);
+        auto each = [&](auto count) {
 #pragma unroll
-        for (int r = 0; r < kSamples; ++r) sample[r] = r * kThreads + tid < some ? sample[r] : 0u;
-        auto count = [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
-            v[0] = v[1] = v[2] = 0;
-#pragma unroll
-            for (int r = 0; r < kSamples; ++r) {
-                v[0] += votes(sample[r] >= b0);
-                v[1] += votes(sample[r] >= b1);
-                v[2] += votes(sample[r] >= b2);
-            }
+            for (int r = 0; r < kSamples; ++r)
+                if (r * kThreads + tid < some) count(sample[r]);
         };
         // Four standard deviations of the sample's count to either side.
         const float share = static_cast<float>(x.keep) / static_cast<float>(x.n), rank = share * static_cast<float>(some);
         const float off = some < kAll ? 1.0f : 4.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
         const int first = static_cast<int>(rank - off), last = static_cast<int>(rank + off) + 1;
-        const uint32_t high = first < 1 ? 0xffffffffu : border_of(first, count, sh, turn, true);
-        const uint32_t low = last > some ? 0u : border_of(last, count, sh, turn, true);
-        if (tid == 0) listed = 0;
-        __syncthreads();
-        uint32_t v[4] = {0, 0, 0, 0}, fixed[1] = {0};
+        // (A border that ends a bin is one less than the numbers over it.)
+        const uint32_t high = first < 1 ? 0xffffffffu : border_of(first, each, sh, turn).over;
+        const uint32_t low = last > some ? 0u : border_of(last, each, sh, turn).over;
+        uint32_t above = 0, at_high = 0, at_low = 0, fixed = 0, listed = 0;
         const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
         uint32_t *list = lists + pair * a.max_keys + begin;
-        for (int64_t j0 = begin; j0 < end; j0 += kChunk) {
-            int j[kHeld];
-            uint32_t o[kHeld], protects;
+        for (int64_t at = seg.start(w); at < end; at += kChunk) {
+            Held t;
+            t.load(a, x, at + tid * kHeld, begin, end);
+            uint32_t o[kHeld], set = 0, all;
+            t.numbers(true, o);
+            fixed += __popc(t.fixed);
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) j[r] = static_cast<int>(j0 + r * kThreads + tid < end ? j0 + r * kThreads + tid : end - 1);
-            x.orders(a, j, o, protects);
-            // How many this thread lists, and where.
-            uint32_t set = 0;
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                const bool in = j0 + r * kThreads + tid < end, f = in && (protects >> r & 1u) != 0u;
-                o[r] = f ? 0xffffffffu : o[r];
-                v[0] += votes(in && o[r] > high);
-                v[1] += votes(in && o[r] == high);
-                v[3] += votes(in && o[r] == low && o[r] != high);
-                fixed[0] += votes(f);
-                set |= in && o[r] > low && o[r] < high ? 1u << r : 0u;
+            for (int i = 0; i < kHeld; ++i) {
+                const bool in = (t.in >> i & 1u) != 0u;
+                above += in && o[i] > high ? 1u : 0u;
+                at_high += in && o[i] == high ? 1u : 0u;
+                at_low += in && o[i] == low && o[i] != high ? 1u : 0u;
+                set |= in && o[i] > low && o[i] < high ? 1u << i : 0u;
             }
-            const uint32_t mine = __popc(set), upto = wave_incl_scan_u32(mine, lane), sum = readlane_u32(upto, kWave - 1);
-            v[2] += sum;
-            uint32_t at = 0;
-            if (lane == 0 && sum != 0) at = atomicAdd(&listed, sum);
-            at = readlane_u32(at, 0) + upto - mine;
+            uint32_t to = listed + before(__popc(set), all, sh, turn);
+            listed += all;
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r)
-                if (set >> r & 1u) list[at++] = o[r];
+            for (int i = 0; i < kHeld; ++i)
+                if (set >> i & 1u) list[to++] = o[i];
         }
-        block_sums(v, sh, turn);
-        block_sums(fixed, sh, turn);
-        if (tid == 0)
-            counts[pair * kMostSegments + w] = Counts{low, high, v[0], v[1], v[2], v[3], fixed[0], 0};
-        __syncthreads();
+        Counts c{low, high, 0, 0, listed, 0, 0, 0};
+        before(above, c.above, sh, turn);
+        before(at_high, c.at_high, sh, turn);
+        before(at_low, c.at_low, sh, turn);
+        before(fixed, c.fixed, sh, turn);
+        if (tid == 0) counts[pair * kMostSegments + w] = c;
     }
 }
 
 // The second one: the border, and each segment's sources or targets.
-__global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Counts *counts, const uint32_t *lists, int64_t size,
+__global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const Counts *counts, const uint32_t *lists, int64_t size,
                                                          Moves moves) {
     __shared__ Shared sh;
     __shared__ Counts held[kMostSegments];
     __shared__ uint32_t over[kMostSegments], even[kMostSegments];  // over and at the border, of each segment
     __shared__ uint32_t starts[kMostSegments + 1];                 // of the listed numbers
-    __shared__ uint32_t ranks[kHeld * kWaves];
-    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
-    const uint64_t under = (uint64_t{1} << lane) - 1;
+    const int tid = static_cast<int>(threadIdx.x);
     int turn = 0;
+    clear(sh);
     for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
         const Head x = head_of(a, pair);
         const Segments seg(x, size);
@@ -532,16 +559,7 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
         __syncthreads();
         const uint32_t keep = static_cast<uint32_t>(x.keep), low = held[0].low, high = held[0].high;
         const bool few = fixed <= keep;
-        uint32_t border;  // (1 and more)
-        // The numbers of tokens j0 .. j0 + kChunk - 1 before `stop`, 0 of the others.
-        auto some = [&](int64_t j0, int64_t stop, uint32_t(&o)[kHeld]) {
-            int j[kHeld];
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) j[r] = static_cast<int>(j0 + r * kThreads + tid < stop ? j0 + r * kThreads + tid : stop - 1);
-            x.numbers(a, j, few, o);
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) o[r] = j0 + r * kThreads + tid < stop ? o[r] : 0u;
-        };
+        Border border;
         auto listed = [&](uint32_t e, int &of) {  // the e-th listed number, and its segment
             int lo = 0, hi = seg.all;
             while (hi - lo > 1) {
@@ -552,51 +570,45 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
             return lists[pair * a.max_keys + seg.begin(x, lo) + (e - starts[lo])];
         };
         if (few && keep > above && keep <= above + at_high) {
-            border = high;
+            border = Border{high, keep - above};
             if (tid < seg.all) over[tid] = held[tid].above, even[tid] = held[tid].at_high;
         } else if (few && keep > above + at_high && keep <= above + at_high + between) {
-            const uint32_t rank = keep - above - at_high;
+            // As many as the registers hold are read once, the others again and again.
             uint32_t o[kHeld];
-            const bool fits = between <= static_cast<uint32_t>(kChunk);
+            int of[kHeld];
 #pragma unroll
             for (int r = 0; r < kHeld; ++r) {
                 const uint32_t e = r * kThreads + tid;
-                int of;
-                o[r] = fits && e < between ? listed(e, of) : 0u;
+                o[r] = listed(e < between ? e : between - 1, of[r]);
             }
-            border = border_of(
-                rank,
-                [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
-                    v[0] = v[1] = v[2] = 0;
-                    if (fits) {
 #pragma unroll
-                        for (int r = 0; r < kHeld; ++r) {
-                            if (static_cast<uint32_t>(r * kThreads) >= between) break;
-                            v[0] += votes(o[r] >= b0);
-                            v[1] += votes(o[r] >= b1);
-                            v[2] += votes(o[r] >= b2);
-                        }
-                    } else {
-                        for (uint32_t e0 = 0; e0 < between; e0 += kThreads) {
-                            int of;
-                            const uint32_t n = e0 + tid < between ? listed(e0 + tid, of) : 0u;
-                            v[0] += votes(n >= b0);
-                            v[1] += votes(n >= b1);
-                            v[2] += votes(n >= b2);
-                        }
-                    }
+            for (int r = 0; r < kHeld; ++r) o[r] = static_cast<uint32_t>(r * kThreads + tid) < between ? o[r] : 0u;
+            auto rest = [&](auto f) {
+                for (uint32_t e = kChunk + tid; e < between; e += kThreads) {
+                    int seg_of;
+                    const uint32_t n = listed(e, seg_of);
+                    f(n, seg_of);
+                }
+            };
+            border = border_of(
+                keep - above - at_high,
+                [&](auto count) {
+#pragma unroll
+                    for (int r = 0; r < kHeld; ++r) count(o[r]);
+                    rest([&](uint32_t n, int) { count(n); });
                 },
-                sh, turn, true);
+                sh, turn);
             if (tid < seg.all) over[tid] = held[tid].above + held[tid].at_high;
             __syncthreads();
-            for (uint32_t e = tid; e < between; e += kThreads) {
-                int of;
-                const uint32_t n = listed(e, of);
-                if (n > border) atomicAdd(&over[of], 1u);
-                if (n == border) atomicAdd(&even[of], 1u);
-            }
+            auto sort = [&](uint32_t n, int seg_of) {
+                if (n > border.over) atomicAdd(&over[seg_of], 1u);
+                if (n == border.over && n != 0u) atomicAdd(&even[seg_of], 1u);
+            };
+#pragma unroll
+            for (int r = 0; r < kHeld; ++r) sort(o[r], of[r]);
+            rest(sort);
         } else if (few && keep > above + at_high + between && keep <= above + at_high + between + at_low) {
-            border = low;
+            border = Border{low, keep - above - at_high - between};
             if (tid < seg.all) {
                 over[tid] = held[tid].above + held[tid].at_high + held[tid].between;
                 even[tid] = held[tid].at_low;
@@ -604,35 +616,33 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
         } else {  // the two numbers do not hold it, or more tokens are protected than stay
             border = border_of(
                 keep,
-                [&](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t(&v)[3]) {
-                    v[0] = v[1] = v[2] = 0;
-                    for (int64_t j0 = 0; j0 < x.n; j0 += kChunk) {
+                [&](auto count) {
+                    for (int64_t at = 0; at < x.n; at += kChunk) {
+                        Held t;
+                        t.load(a, x, at + tid * kHeld, 0, x.n);
                         uint32_t o[kHeld];
-                        some(j0, x.n, o);
+                        t.numbers(few, o);
 #pragma unroll
-                        for (int r = 0; r < kHeld; ++r) {
-                            v[0] += votes(o[r] >= b0);
-                            v[1] += votes(o[r] >= b1);
-                            v[2] += votes(o[r] >= b2);
-                        }
+                        for (int i = 0; i < kHeld; ++i) count(o[i]);
                     }
                 },
-                sh, turn, true);
-            for (int64_t j0 = 0; j0 < x.n; j0 += kChunk) {
+                sh, turn);
+            for (int64_t at = 0; at < x.n; at += kChunk) {
+                Held t;
+                t.load(a, x, at + tid * kHeld, 0, x.n);
                 uint32_t o[kHeld];
-                some(j0, x.n, o);
+                t.numbers(few, o);
 #pragma unroll
-                for (int r = 0; r < kHeld; ++r) {
-                    const int64_t j = j0 + r * kThreads + tid;
-                    if (o[r] > border) atomicAdd(&over[seg.of(x, j)], 1u);
-                    if (o[r] == border) atomicAdd(&even[seg.of(x, j)], 1u);
+                for (int i = 0; i < kHeld; ++i) {
+                    const int64_t j = at + tid * kHeld + i;
+                    if (o[i] > border.over) atomicAdd(&over[seg.of(x, j)], 1u);
+                    if (o[i] == border.over && o[i] != 0u) atomicAdd(&even[seg.of(x, j)], 1u);
                 }
             }
         }
         __syncthreads();
         // Of those at the border the first ones stay; and what comes before this segment.
-        uint32_t left = keep, first_even = 0, stays = 0, first = 0, all = 0;
-        for (int i = 0; i < seg.all; ++i) left -= over[i];
+        uint32_t left = border.even, stays = 0, first = 0, all = 0;
         for (int i = 0; i < seg.all; ++i) {
             const uint32_t take = even[i] < left ? even[i] : left;
             const uint32_t kept = over[i] + take;
@@ -643,37 +653,33 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a, const Coun
             if (i >= seg.below) all += mine;
         }
         if (w == 0 && tid == 0) moves.count[pair] = static_cast<int32_t>(all);
-        int32_t *out = moves.from + (pair * 2 + (w < seg.below ? 1 : 0)) * moves.most;
-        const bool below = w < seg.below, carries = below && (a.mass_out != a.mass || a.positions_out != a.key_positions);
-        for (int64_t j0 = begin; j0 < end; j0 += kChunk) {
-            uint32_t o[kHeld], mine[kHeld], sum[kHeld], kept = 0, total;
-            some(j0, end, o);
+        const bool below = w < seg.below;
+        int32_t *out = moves.from + (pair * 2 + (below ? 1 : 0)) * moves.most;
+        uint32_t first_even = 0;
+        for (int64_t at = seg.start(w); at < end; at += kChunk) {
+            const int64_t j0 = at + tid * kHeld;
+            Held t;
+            t.load(a, x, j0, begin, end);
+            uint32_t o[kHeld], kept = 0, at_it = 0, total;
+            t.numbers(few, o);
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                kept |= o[r] > border ? 1u << r : 0u;
-                mine[r] = votes(o[r] == border);
+            for (int i = 0; i < kHeld; ++i) {
+                kept |= o[i] > border.over ? 1u << i : 0u;
+                at_it |= o[i] == border.over ? 1u << i : 0u;
             }
-            before(ranks, mine, sum, total);
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                const uint32_t rank = first_even + sum[r] + static_cast<uint32_t>(__popcll(__ballot(o[r] == border) & under));
-                kept |= o[r] == border && rank < stays ? 1u << r : 0u;
-            }
+            at_it &= t.in;
+            uint32_t rank = first_even + before(__popc(at_it), total, sh, turn);
             first_even += total;
-            uint64_t set[kHeld];
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                const bool in = j0 + r * kThreads + tid < end, k = (kept >> r & 1u) != 0u;
-                set[r] = __ballot(in && k != below);
-                mine[r] = static_cast<uint32_t>(__popcll(set[r]));
-                if (carries && in && k) carry(a, x.place(a, j0 + r * kThreads + tid));
-            }
-            before(ranks, mine, sum, total);
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r)
-                if (set[r] >> lane & 1u)
-                    out[first + sum[r] + static_cast<uint32_t>(__popcll(set[r] & under))] = static_cast<int32_t>(j0 + r * kThreads + tid);
+            for (int i = 0; i < kHeld; ++i)
+                if (at_it >> i & 1u) kept |= rank++ < stays ? 1u << i : 0u;
+            const uint32_t set = below ? t.in & ~kept : kept;
+            uint32_t to = first + before(__popc(set), total, sh, turn);
             first += total;
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (set >> i & 1u) out[to++] = static_cast<int32_t>(j0 + i);
+            if (below && carries(a) && t.in != 0u) t.carry(a, x);
         }
         __syncthreads();
     }
