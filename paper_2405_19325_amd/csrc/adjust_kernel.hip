@@ -18,6 +18,7 @@ namespace knnlm {
 
 namespace {
 
+constexpr int64_t kGrid = 1 << 20;      // rows of a row of the grid
 constexpr int kPer = 8;                 // tokens of a thread
 constexpr uint32_t kPrompt = 1u << 31;  // beside a token's count: it is in the prompt
 
@@ -83,151 +84,150 @@ __global__ __launch_bounds__(THREADS) void k_adjust(AdjustArgs a) {
     const int tid = static_cast<int>(threadIdx.x);
     const bool counts = a.history != nullptr || a.row_tokens != nullptr, biased = a.bias_tokens != nullptr;
     const uint32_t off = PROBS ? 0u : Ty::narrow(-INFINITY);
-    for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
-        int64_t s = t, first = t;
-        if (a.row_offsets != nullptr) {
-            if (t >= a.row_offsets[a.S]) break;
-            s = set_of_query(a.row_offsets, a.S, t);
-            first = a.row_offsets[s];
-        }
-        const char *in = static_cast<const char *>(a.scores) + t * a.stride * Ty::SIZE;
-        char *out = static_cast<char *>(a.out) + t * a.out_stride * Ty::SIZE;
-        // Places are counted from the 16 bytes that hold the first score; place p is token p - lead.
-        const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16) / Ty::SIZE;
-        const int p0 = static_cast<int>(blockIdx.y) * SLICE, v0 = p0 - lead;
-        if (v0 >= a.V) continue;
-        const bool even = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(in)) % 16 == 0;
-        u32x4_t x[GROUPS];
-        uint32_t may[GROUPS];  // a bit a token: it is allowed
-        auto group = [&](int g) { return (g * THREADS + tid) * VEC; };  // place in the slice
-        auto fetch = [&](int g) {
-            const int v = v0 + group(g);
-            if (v >= 0 && v + VEC <= a.V) {
-                x[g] = *reinterpret_cast<const u32x4_t *>(in + static_cast<int64_t>(v) * Ty::SIZE);
-            } else {
-                x[g] = u32x4_t{0, 0, 0, 0};
+    const int64_t t = static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.x;
+    if (t >= a.rows) return;
+    int64_t s = t, first = t;
+    if (a.row_offsets != nullptr) {
+        if (t >= a.row_offsets[a.S]) return;
+        s = set_of_query(a.row_offsets, a.S, t);
+        first = a.row_offsets[s];
+    }
+    const char *in = static_cast<const char *>(a.scores) + t * a.stride * Ty::SIZE;
+    char *out = static_cast<char *>(a.out) + t * a.out_stride * Ty::SIZE;
+    // Places are counted from the 16 bytes that hold the first score; place p is token p - lead.
+    const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16) / Ty::SIZE;
+    const int p0 = static_cast<int>(blockIdx.y) * SLICE, v0 = p0 - lead;
+    if (v0 >= a.V) return;
+    const bool even = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(in)) % 16 == 0;
+    u32x4_t x[GROUPS];
+    uint32_t may[GROUPS];  // a bit a token: it is allowed
+    auto group = [&](int g) { return (g * THREADS + tid) * VEC; };  // place in the slice
+    auto fetch = [&](int g) {
+        const int v = v0 + group(g);
+        if (v >= 0 && v + VEC <= a.V) {
+            x[g] = *reinterpret_cast<const u32x4_t *>(in + static_cast<int64_t>(v) * Ty::SIZE);
+        } else {
+            x[g] = u32x4_t{0, 0, 0, 0};
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (v + e >= 0 && v + e < a.V) {
-                        if constexpr (DT == KNN_F32) x[g][e] = Ty::raw(in, v + e);
-                        else x[g][e / 2] |= Ty::raw(in, v + e) << (e % 2 * 16);
-                    }
+            for (int e = 0; e < VEC; ++e)
+                if (v + e >= 0 && v + e < a.V) {
+                    if constexpr (DT == KNN_F32) x[g][e] = Ty::raw(in, v + e);
+                    else x[g][e / 2] |= Ty::raw(in, v + e) << (e % 2 * 16);
+                }
+        }
+    };
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        if constexpr (!LAZY) fetch(g);
+        may[g] = ~0u;
+        if (!LAZY && a.allowed != nullptr) {
+            const int words = (a.V + 31) / 32, v = v0 + group(g);
+            const uint32_t *row = a.allowed + t * words;
+            const int w = v < 0 ? 0 : v >> 5, lo = w < words ? w : words - 1, hi = w + 1 < words ? w + 1 : words - 1;
+            const uint64_t both = static_cast<uint64_t>(row[lo]) | static_cast<uint64_t>(row[hi]) << 32;
+            may[g] = static_cast<uint32_t>(v < 0 ? both << -v : both >> (v & 31));
+        }
+    }
+    for (int i = tid; i < SLICE; i += THREADS) {
+        if (counts) seen[i] = 0u;
+        if (biased) last[i] = -1;
+    }
+    if (tid == 0) n_touched = 0;
+    __syncthreads();
+    auto at = [&](int64_t v) {  // the place of a token in this slice; -1: in another, or none
+        const int64_t p = v - v0;
+        return v >= 0 && v < a.V && p >= 0 && p < SLICE ? static_cast<int>(p) : -1;
+    };
+    if (a.history != nullptr) {
+        const int64_t len = a.history_lens[s] < a.history_width ? a.history_lens[s] : a.history_width;
+        const int64_t prompt = a.prompt_lens != nullptr ? a.prompt_lens[s] : 0;
+        const int32_t *history = a.history + s * a.history_width;
+        for (int64_t i0 = tid; i0 < len; i0 += kPer * THREADS) {
+            int32_t v[kPer];
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) v[u] = history[i0 + u * THREADS < len ? i0 + u * THREADS : i0];
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+                const int64_t i = i0 + u * THREADS;
+                const int p = i < len ? at(v[u]) : -1;
+                if (p >= 0 && i < prompt) atomicOr(&seen[p], kPrompt);
+                if (p >= 0 && i >= prompt) atomicAdd(&seen[p], 1u);
             }
-        };
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            if constexpr (!LAZY) fetch(g);
-            may[g] = ~0u;
-            if (!LAZY && a.allowed != nullptr) {
-                const int words = (a.V + 31) / 32, v = v0 + group(g);
-                const uint32_t *row = a.allowed + t * words;
-                const int w = v < 0 ? 0 : v >> 5, lo = w < words ? w : words - 1, hi = w + 1 < words ? w + 1 : words - 1;
-                const uint64_t both = static_cast<uint64_t>(row[lo]) | static_cast<uint64_t>(row[hi]) << 32;
-                may[g] = static_cast<uint32_t>(v < 0 ? both << -v : both >> (v & 31));
-            }
         }
-        for (int i = tid; i < SLICE; i += THREADS) {
-            if (counts) seen[i] = 0u;
-            if (biased) last[i] = -1;
+    }
+    if (a.row_tokens != nullptr) {
+        int64_t rows = a.row_offsets != nullptr ? a.row_offsets[s + 1] : t + 1;
+        rows = (rows < a.rows ? rows : a.rows) - first;
+        if (a.tree_mask == nullptr) rows = t - first + 1;
+        else if (rows > 32 * a.mask_words) rows = 32 * a.mask_words;
+        for (int64_t i = tid; i < rows; i += THREADS) {
+            const bool sees = a.tree_mask == nullptr || (a.tree_mask[t * a.mask_words + (i >> 5)] >> (i & 31) & 1u) != 0u;
+            const int p = at(a.row_tokens[first + i]);
+            if (sees && p >= 0) atomicAdd(&seen[p], 1u);
         }
-        if (tid == 0) n_touched = 0;
-        __syncthreads();
-        auto at = [&](int64_t v) {  // the place of a token in this slice; -1: in another, or none
-            const int64_t p = v - v0;
-            return v >= 0 && v < a.V && p >= 0 && p < SLICE ? static_cast<int>(p) : -1;
-        };
-        if (a.history != nullptr) {
-            const int64_t len = a.history_lens[s] < a.history_width ? a.history_lens[s] : a.history_width;
-            const int64_t prompt = a.prompt_lens != nullptr ? a.prompt_lens[s] : 0;
-            const int32_t *history = a.history + s * a.history_width;
-            for (int64_t i0 = tid; i0 < len; i0 += kPer * THREADS) {
-                int32_t v[kPer];
+    }
+    if (biased)
+        for (int64_t i = tid; i < a.bias_width; i += THREADS) {
+            const int p = at(a.bias_tokens[s * a.bias_width + i]);
+            if (p >= 0) atomicMax(&last[p], static_cast<int32_t>(i));
+        }
+    Rule rule{parameter(a.repetition, t, 1.0f), parameter(a.presence, t, 0.0f), parameter(a.frequency, t, 0.0f)};
+    if (!(rule.repetition > 0.0f)) rule.repetition = 1.0f;
+    __syncthreads();
+    const float *biases = a.bias_values + s * a.bias_width;
 #pragma unroll
-                for (int u = 0; u < kPer; ++u) v[u] = history[i0 + u * THREADS < len ? i0 + u * THREADS : i0];
+    for (int g = 0; g < GROUPS; ++g) {
+        const int v = v0 + group(g);
+        uint32_t c[VEC];
+        int32_t b[VEC];
+        uint32_t any = 0;
 #pragma unroll
-                for (int u = 0; u < kPer; ++u) {
-                    const int64_t i = i0 + u * THREADS;
-                    const int p = i < len ? at(v[u]) : -1;
-                    if (p >= 0 && i < prompt) atomicOr(&seen[p], kPrompt);
-                    if (p >= 0 && i >= prompt) atomicAdd(&seen[p], 1u);
+        for (int e = 0; e < VEC; ++e) {
+            c[e] = counts ? seen[group(g) + e] : 0u;
+            b[e] = biased ? last[group(g) + e] : -1;
+            any |= c[e] != 0u || b[e] >= 0 ? 1u << e : 0u;
+        }
+        if constexpr (LAZY) {
+            if (any == 0u) continue;
+            if constexpr (!PROBS) fetch(g);
+        }
+        uint32_t change = ~may[g] & ((1u << VEC) - 1u);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            if (change >> e & 1u) {
+                if constexpr (DT == KNN_F32) x[g][e] = off;
+                else x[g][e / 2] = e % 2 != 0 ? (x[g][e / 2] & 0xffffu) | off << 16 : (x[g][e / 2] & 0xffff0000u) | off;
+            } else if (any >> e & 1u) {
+                if constexpr (PROBS) {
+                    touched[atomicAdd(&n_touched, 1u)] = static_cast<uint16_t>(group(g) + e);
+                } else {
+                    Ty::put(x[g], e, rule.of(Ty::widen(x[g], e), c[e], b[e] >= 0, b[e] >= 0 ? biases[b[e]] : 0.0f));
+                    change |= 1u << e;
                 }
             }
         }
-        if (a.row_tokens != nullptr) {
-            int64_t rows = a.row_offsets != nullptr ? a.row_offsets[s + 1] : t + 1;
-            rows = (rows < a.rows ? rows : a.rows) - first;
-            if (a.tree_mask == nullptr) rows = t - first + 1;
-            else if (rows > 32 * a.mask_words) rows = 32 * a.mask_words;
-            for (int64_t i = tid; i < rows; i += THREADS) {
-                const bool sees = a.tree_mask == nullptr || (a.tree_mask[t * a.mask_words + (i >> 5)] >> (i & 31) & 1u) != 0u;
-                const int p = at(a.row_tokens[first + i]);
-                if (sees && p >= 0) atomicAdd(&seen[p], 1u);
-            }
-        }
-        if (biased)
-            for (int64_t i = tid; i < a.bias_width; i += THREADS) {
-                const int p = at(a.bias_tokens[s * a.bias_width + i]);
-                if (p >= 0) atomicMax(&last[p], static_cast<int32_t>(i));
-            }
-        Rule rule{parameter(a.repetition, t, 1.0f), parameter(a.presence, t, 0.0f), parameter(a.frequency, t, 0.0f)};
-        if (!(rule.repetition > 0.0f)) rule.repetition = 1.0f;
-        __syncthreads();
-        const float *biases = a.bias_values + s * a.bias_width;
+        if (a.out == a.scores && change == 0u) continue;
+        if (even && v >= 0 && v + VEC <= a.V) {
+            *reinterpret_cast<u32x4_t *>(out + static_cast<int64_t>(v) * Ty::SIZE) = x[g];
+        } else {
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            const int v = v0 + group(g);
-            uint32_t c[VEC];
-            int32_t b[VEC];
-            uint32_t any = 0;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                c[e] = counts ? seen[group(g) + e] : 0u;
-                b[e] = biased ? last[group(g) + e] : -1;
-                any |= c[e] != 0u || b[e] >= 0 ? 1u << e : 0u;
-            }
-            if constexpr (LAZY) {
-                if (any == 0u) continue;
-                if constexpr (!PROBS) fetch(g);
-            }
-            uint32_t change = ~may[g] & ((1u << VEC) - 1u);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                if (change >> e & 1u) {
-                    if constexpr (DT == KNN_F32) x[g][e] = off;
-                    else x[g][e / 2] = e % 2 != 0 ? (x[g][e / 2] & 0xffffu) | off << 16 : (x[g][e / 2] & 0xffff0000u) | off;
-                } else if (any >> e & 1u) {
-                    if constexpr (PROBS) {
-                        touched[atomicAdd(&n_touched, 1u)] = static_cast<uint16_t>(group(g) + e);
-                    } else {
-                        Ty::put(x[g], e, rule.of(Ty::widen(x[g], e), c[e], b[e] >= 0, b[e] >= 0 ? biases[b[e]] : 0.0f));
-                        change |= 1u << e;
-                    }
+            for (int e = 0; e < VEC; ++e)
+                if (v + e >= 0 && v + e < a.V) {
+                    if constexpr (DT == KNN_F32) Ty::set(out, v + e, x[g][e]);
+                    else Ty::set(out, v + e, x[g][e / 2] >> (e % 2 * 16) & 0xffffu);
                 }
-            }
-            if (a.out == a.scores && change == 0u) continue;
-            if (even && v >= 0 && v + VEC <= a.V) {
-                *reinterpret_cast<u32x4_t *>(out + static_cast<int64_t>(v) * Ty::SIZE) = x[g];
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (v + e >= 0 && v + e < a.V) {
-                        if constexpr (DT == KNN_F32) Ty::set(out, v + e, x[g][e]);
-                        else Ty::set(out, v + e, x[g][e / 2] >> (e % 2 * 16) & 0xffffu);
-                    }
-            }
         }
+    }
+    if constexpr (PROBS) {
         __syncthreads();
-        if constexpr (PROBS) {
-            for (uint32_t i = tid; i < n_touched; i += THREADS) {
-                const int p = touched[i], v = v0 + p;
-                const uint32_t raw = Ty::raw(in, v);
-                const float from = Ty::widen(u32x4_t{raw, 0, 0, 0}, 0);
-                if (!(from > 0.0f)) continue;  // (it was written as it is)
-                const int32_t b = biased ? last[p] : -1;
-                const double y = rule.of(log(static_cast<double>(from)), counts ? seen[p] : 0u, b >= 0, b >= 0 ? biases[b] : 0.0f);
-                Ty::set(out, v, Ty::narrow(static_cast<float>(exp(y))));
-            }
-            __syncthreads();
+        for (uint32_t i = tid; i < n_touched; i += THREADS) {
+            const int p = touched[i], v = v0 + p;
+            const uint32_t raw = Ty::raw(in, v);
+            const float from = Ty::widen(u32x4_t{raw, 0, 0, 0}, 0);
+            if (!(from > 0.0f)) continue;  // (it was written as it is)
+            const int32_t b = biased ? last[p] : -1;
+            const double y = rule.of(log(static_cast<double>(from)), counts ? seen[p] : 0u, b >= 0, b >= 0 ? biases[b] : 0.0f);
+            Ty::set(out, v, Ty::narrow(static_cast<float>(exp(y))));
         }
     }
 }
@@ -236,7 +236,8 @@ template <knn_dtype DT, bool PROBS, bool LAZY, int THREADS>
 hipError_t launch(const AdjustArgs &a, hipStream_t stream) {
     constexpr int SLICE = kPer * THREADS;
     const int64_t slices = (a.V + Type<DT>::VEC - 1 + SLICE - 1) / SLICE;
-    const dim3 grid(static_cast<unsigned>(a.rows < (1 << 20) ? a.rows : 1 << 20), static_cast<unsigned>(slices));
+    const dim3 grid(static_cast<unsigned>(a.rows < kGrid ? a.rows : kGrid), static_cast<unsigned>(slices),
+                    static_cast<unsigned>((a.rows + kGrid - 1) / kGrid));
     k_adjust<DT, PROBS, LAZY, THREADS><<<grid, THREADS, sizeof(uint32_t) * SLICE * (a.bias_tokens != nullptr ? 2 : 1), stream>>>(a);
     return hipGetLastError();
 }

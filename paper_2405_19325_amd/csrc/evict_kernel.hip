@@ -34,7 +34,7 @@ constexpr int kChunk = kHeld * kThreads;
 constexpr int kSegments = 64;                // of a head, about
 constexpr int kSamples = 8;                  // of a thread
 constexpr int kBits = 11, kBins = 1 << kBits;
-constexpr int64_t kGrid = int64_t{1} << 20;  // heads at once
+constexpr int64_t kGrid = int64_t{1} << 20;  // heads of a row of the grid
 
 // A number that orders like x, NaN first.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -121,7 +121,7 @@ struct Head {
     int64_t s;
     int h;
     int64_t n, keep;  // tokens; those that stay
-    int64_t recent_from;
+    int32_t recent_from;
     bool leave;       // left as it is
     bool vec;         // the ledgers lie on 16 bytes
 
@@ -151,6 +151,8 @@ struct Head {
     }
 };
 
+__device__ __forceinline__ int64_t pair_of() { return static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.x; }
+
 // For all threads of a workgroup together.
 __device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
     Head x;
@@ -159,7 +161,8 @@ __device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
     const int64_t len = a.cache_lens[x.s], budget = a.budgets[x.s];
     const int64_t room = a.cache.table_width << a.cache.page_log2, limit = a.max_keys < room ? a.max_keys : room;
     const int64_t n = len < 0 ? 0 : len;
-    x.recent_from = (a.next_positions != nullptr ? a.next_positions[x.s] : len) - a.recent;
+    const int64_t recent_from = (a.next_positions != nullptr ? a.next_positions[x.s] : len) - a.recent;
+    x.recent_from = static_cast<int32_t>(recent_from > -0x80000000LL ? recent_from : -0x80000000LL);
     x.leave = budget < 0 || budget >= n || n > limit;
     if (!x.leave) {
         bool whole = true;
@@ -185,68 +188,69 @@ __device__ __forceinline__ void put_len(const EvictArgs &a, const Head &x) {
     a.new_lens[x.s] = x.leave ? a.cache_lens[x.s] : static_cast<int32_t>(x.keep);
 }
 
-// kHeld tokens from j0 on, a multiple of kHeld: what the ledger has of those in [from, to).
+// N tokens from j0 on, a multiple of N: what the ledger has of those in [from, to).
+template <int N = kHeld>
 struct Held {
     int64_t at;      // place of the first
     uint32_t in;     // as bits: those in the range
     uint32_t fixed;  // and of these the protected ones
     union {
-        float m[kHeld];
-        float4 m4[kHeld / 4];
+        float m[N];
+        float4 m4[N / 4];
     };
     union {
-        int32_t p[kHeld];
-        int4 p4[kHeld / 4];
+        int32_t p[N];
+        int4 p4[N / 4];
     };
 
     __device__ __forceinline__ void load(const EvictArgs &a, const Head &x, int64_t j0, int64_t from, int64_t to) {
         in = fixed = 0;
-        if (j0 >= to || j0 + kHeld <= from) return;
-        in = (1u << kHeld) - 1u;
+        if (j0 >= to || j0 + N <= from) return;
+        in = (1u << N) - 1u;
         if (j0 < from) in &= ~0u << (from - j0);
-        if (j0 + kHeld > to) in &= (1u << (to - j0)) - 1u;
+        if (j0 + N > to) in &= (1u << (to - j0)) - 1u;
         at = x.place(a, j0);
         if (x.vec) {
 #pragma unroll
-            for (int i = 0; i < kHeld / 4; ++i) {
+            for (int i = 0; i < N / 4; ++i) {
                 m4[i] = reinterpret_cast<const float4 *>(a.mass + at)[i];
                 if (a.key_positions != nullptr) p4[i] = reinterpret_cast<const int4 *>(a.key_positions + at)[i];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i) {
+            for (int i = 0; i < N; ++i) {
                 m[i] = a.mass[at + i];
                 if (a.key_positions != nullptr) p[i] = a.key_positions[at + i];
             }
         }
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
+        for (int i = 0; i < N; ++i) {
             if (a.key_positions == nullptr) p[i] = static_cast<int32_t>(j0) + i;
             fixed |= x.fixed(a, p[i]) ? 1u << i : 0u;
         }
         fixed &= in;
     }
     // 0 of those out of the range.
-    __device__ __forceinline__ void numbers(bool few, uint32_t (&o)[kHeld]) const {
+    __device__ __forceinline__ void numbers(bool few, uint32_t (&o)[N]) const {
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i)
+        for (int i = 0; i < N; ++i)
             o[i] = (in >> i & 1u) != 0u ? Head::number(order_of(m[i]), (fixed >> i & 1u) != 0u, few) : 0u;
     }
-    // The entries in the range go into a ledger of afterwards that is another.  (Those of places that are given up are
-    // written over by what moves there, later.)
-    __device__ __forceinline__ void carry(const EvictArgs &a, const Head &x) const {
+    // The entries of `some` go into a ledger of afterwards that is another.  (Those of places that are given up are written
+    // over by what moves there, later.)
+    __device__ __forceinline__ void carry(const EvictArgs &a, const Head &x, uint32_t some) const {
         const bool masses = a.mass_out != a.mass, positions = a.positions_out != a.key_positions;
-        if (in == (1u << kHeld) - 1u && x.vec) {
+        if (some == (1u << N) - 1u && x.vec) {
 #pragma unroll
-            for (int i = 0; i < kHeld / 4; ++i) {
+            for (int i = 0; i < N / 4; ++i) {
                 if (masses) reinterpret_cast<float4 *>(a.mass_out + at)[i] = m4[i];
                 if (positions) reinterpret_cast<int4 *>(a.positions_out + at)[i] = p4[i];
             }
             return;
         }
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            if ((in >> i & 1u) == 0u) continue;
+        for (int i = 0; i < N; ++i) {
+            if ((some >> i & 1u) == 0u) continue;
             if (masses) a.mass_out[at + i] = m[i];
             if (positions) a.positions_out[at + i] = p[i];
         }
@@ -328,77 +332,73 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_held(EvictArgs a, Moves m
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1), wave = tid / kWave;
     int turn = 0;
     clear(sh);
-    for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
-        const Head x = head_of(a, pair);
-        if (x.h == 0 && tid == 0) put_len(a, x);
-        if (x.leave) {
-            carry_all(a, x, 0, x.n);
-            if (!MOVE && tid == 0) moves.count[pair] = 0;
-            continue;
-        }
-        const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep), j0 = tid * kHeld;
-        Held t;
-        t.load(a, x, j0, 0, n);
-        uint32_t protects, o[kHeld];
-        before(__popc(t.fixed), protects, sh, turn);
-        const bool few = protects <= static_cast<uint32_t>(keep);
-        t.numbers(few, o);
-        const uint32_t rank = few ? keep - protects : keep;  // among those that are not protected, or among these alone
-        Border border{few ? 0xfffffffeu : 0xffffffffu, 0u};
-        if (rank > 0)
-            border = border_of(
-                rank,
-                [&](auto count) {
+    const int64_t pair = pair_of();
+    if (pair >= a.S * a.kv_heads) return;
+    const Head x = head_of(a, pair);
+    if (x.h == 0 && tid == 0) put_len(a, x);
+    if (x.leave) {
+        carry_all(a, x, 0, x.n);
+        if (!MOVE && tid == 0) moves.count[pair] = 0;
+        return;
+    }
+    const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep), j0 = tid * kHeld;
+    Held<> t;
+    t.load(a, x, j0, 0, n);
+    const uint32_t low = keep <= j0 ? 0u : keep >= j0 + kHeld ? (1u << kHeld) - 1u : (1u << (keep - j0)) - 1u;
+    if (carries(a) && (t.in & low) != 0u) t.carry(a, x, t.in & low);
+    uint32_t protects, o[kHeld];
+    before(__popc(t.fixed), protects, sh, turn);
+    const bool few = protects <= static_cast<uint32_t>(keep);
+    t.numbers(few, o);
+    const uint32_t rank = few ? keep - protects : keep;  // among those that are not protected, or among these alone
+    Border border{few ? 0xfffffffeu : 0xffffffffu, 0u};
+    if (rank > 0)
+        border = border_of(
+            rank,
+            [&](auto count) {
 #pragma unroll
-                    for (int i = 0; i < kHeld; ++i)
-                        if (o[i] != 0xffffffffu) count(o[i]);
-                },
-                sh, turn);
-        uint32_t over = 0, at_it = 0;  // as bits
+                for (int i = 0; i < kHeld; ++i)
+                    if (o[i] != 0xffffffffu) count(o[i]);
+            },
+            sh, turn);
+    uint32_t over = 0, at_it = 0;  // as bits
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            over |= o[i] > border.over ? 1u << i : 0u;
-            at_it |= o[i] == border.over ? 1u << i : 0u;
-        }
-        uint32_t all;
-        if (border.even != 0) {
-            uint32_t rank = before(__popc(at_it), all, sh, turn);
+    for (int i = 0; i < kHeld; ++i) {
+        over |= o[i] > border.over ? 1u << i : 0u;
+        at_it |= o[i] == border.over ? 1u << i : 0u;
+    }
+    uint32_t all;
+    if (border.even != 0) {
+        uint32_t rank = before(__popc(at_it), all, sh, turn);
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (at_it >> i & 1u) over |= rank++ < border.even ? 1u << i : 0u;
-        }
-        const uint32_t low = keep <= j0 ? 0u : keep >= j0 + kHeld ? (1u << kHeld) - 1u : (1u << (keep - j0)) - 1u;
-        const uint32_t sources = over & ~low, targets = t.in & low & ~over;
-        const uint32_t first = before(__popc(sources) | __popc(targets) << 16, all, sh, turn);
-        const uint32_t total = all & 0xffffu;
-        uint32_t rs = first & 0xffffu, rt = first >> 16;
+        for (int i = 0; i < kHeld; ++i)
+            if (at_it >> i & 1u) over |= rank++ < border.even ? 1u << i : 0u;
+    }
+    const uint32_t sources = over & ~low, targets = t.in & low & ~over;
+    const uint32_t first = before(__popc(sources) | __popc(targets) << 16, all, sh, turn);
+    const uint32_t total = all & 0xffffu;
+    uint32_t rs = first & 0xffffu, rt = first >> 16;
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            if (sources >> i & 1u) {
-                if constexpr (MOVE) lists[0][rs++] = static_cast<uint16_t>(j0 + i);
-                else moves.from[pair * 2 * moves.most + rs++] = j0 + i;
-            }
-            if (targets >> i & 1u) {
-                if constexpr (MOVE) lists[1][rt++] = static_cast<uint16_t>(j0 + i);
-                else moves.from[(pair * 2 + 1) * moves.most + rt++] = j0 + i;
-            }
+    for (int i = 0; i < kHeld; ++i) {
+        if (sources >> i & 1u) {
+            if constexpr (MOVE) lists[0][rs++] = static_cast<uint16_t>(j0 + i);
+            else moves.from[pair * 2 * moves.most + rs++] = j0 + i;
         }
-        if (carries(a)) {
-            t.in &= low;
-            if (t.in != 0u) t.carry(a, x);
+        if (targets >> i & 1u) {
+            if constexpr (MOVE) lists[1][rt++] = static_cast<uint16_t>(j0 + i);
+            else moves.from[(pair * 2 + 1) * moves.most + rt++] = j0 + i;
         }
-        if constexpr (MOVE) {
-            __syncthreads();
-            constexpr int BATCH = batch_of(CHUNKS);
-            for (uint32_t m = wave * BATCH; m < total; m += kWaves * BATCH) {
-                const uint32_t i = lane < BATCH && m + lane < total ? m + lane : m;
-                move<CHUNKS>(a, x.place(a, lists[0][i]), x.place(a, lists[1][i]),
-                             static_cast<int>(total - m < BATCH ? total - m : BATCH));
-            }
-            __syncthreads();
-        } else if (tid == 0) {
-            moves.count[pair] = static_cast<int32_t>(total);
+    }
+    if constexpr (MOVE) {
+        __syncthreads();
+        constexpr int BATCH = batch_of(CHUNKS);
+        for (uint32_t m = wave * BATCH; m < total; m += kWaves * BATCH) {
+            const uint32_t i = lane < BATCH && m + lane < total ? m + lane : m;
+            move<CHUNKS>(a, x.place(a, lists[0][i]), x.place(a, lists[1][i]),
+                         static_cast<int>(total - m < BATCH ? total - m : BATCH));
         }
+    } else if (tid == 0) {
+        moves.count[pair] = static_cast<int32_t>(total);
     }
 }
 
@@ -461,67 +461,67 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
     const int tid = static_cast<int>(threadIdx.x);
     int turn = 0;
     clear(sh);
-    for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
-        const Head x = head_of(a, pair);
-        const Segments seg(x, size);
-        const int w = static_cast<int>(blockIdx.y);
-        if (x.leave || w >= seg.all || x.keep == 0) continue;
-        // One token of each of 4,096 equal pieces, at no regular distance.
-        constexpr int kAll = kSamples * kThreads;
-        const int64_t some = x.n < kAll ? x.n : kAll;
-        int which[kSamples];
-        uint32_t sample[kSamples];
+    const int64_t pair = pair_of();
+    if (pair >= a.S * a.kv_heads) return;
+    const Head x = head_of(a, pair);
+    const Segments seg(x, size);
+    const int w = static_cast<int>(blockIdx.y);
+    if (x.leave || w >= seg.all || x.keep == 0) return;
+    // One token of each of 4,096 equal pieces, at no regular distance.
+    constexpr int kAll = kSamples * kThreads;
+    const int64_t some = x.n < kAll ? x.n : kAll;
+    int which[kSamples];
+    uint32_t sample[kSamples];
 #pragma unroll
-        for (int r = 0; r < kSamples; ++r) {
-            const int64_t i = r * kThreads + tid < some ? r * kThreads + tid : some - 1;
-            const int64_t j0 = i * x.n / some, j1 = (i + 1) * x.n / some;
-            uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
-            mix ^= mix >> 15;
-            which[r] = static_cast<int>(j0 + mix % static_cast<uint32_t>(j1 - j0));
-        }
-        x.numbers(a, which, sample);
-        auto each = [&](auto count) {
-#pragma unroll
-            for (int r = 0; r < kSamples; ++r)
-                if (r * kThreads + tid < some) count(sample[r]);
-        };
-        // Four standard deviations of the sample's count to either side.
-        const float share = static_cast<float>(x.keep) / static_cast<float>(x.n), rank = share * static_cast<float>(some);
-        const float off = some < kAll ? 1.0f : 4.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
-        const int first = static_cast<int>(rank - off), last = static_cast<int>(rank + off) + 1;
-        // (A border that ends a bin is one less than the numbers over it.)
-        const uint32_t high = first < 1 ? 0xffffffffu : border_of(first, each, sh, turn).over;
-        const uint32_t low = last > some ? 0u : border_of(last, each, sh, turn).over;
-        uint32_t above = 0, at_high = 0, at_low = 0, fixed = 0, listed = 0;
-        const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
-        uint32_t *list = lists + pair * a.max_keys + begin;
-        for (int64_t at = seg.start(w); at < end; at += kChunk) {
-            Held t;
-            t.load(a, x, at + tid * kHeld, begin, end);
-            uint32_t o[kHeld], set = 0, all;
-            t.numbers(true, o);
-            fixed += __popc(t.fixed);
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i) {
-                const bool in = (t.in >> i & 1u) != 0u;
-                above += in && o[i] > high ? 1u : 0u;
-                at_high += in && o[i] == high ? 1u : 0u;
-                at_low += in && o[i] == low && o[i] != high ? 1u : 0u;
-                set |= in && o[i] > low && o[i] < high ? 1u << i : 0u;
-            }
-            uint32_t to = listed + before(__popc(set), all, sh, turn);
-            listed += all;
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (set >> i & 1u) list[to++] = o[i];
-        }
-        Counts c{low, high, 0, 0, listed, 0, 0, 0};
-        before(above, c.above, sh, turn);
-        before(at_high, c.at_high, sh, turn);
-        before(at_low, c.at_low, sh, turn);
-        before(fixed, c.fixed, sh, turn);
-        if (tid == 0) counts[pair * kMostSegments + w] = c;
+    for (int r = 0; r < kSamples; ++r) {
+        const int64_t i = r * kThreads + tid < some ? r * kThreads + tid : some - 1;
+        const int64_t j0 = i * x.n / some, j1 = (i + 1) * x.n / some;
+        uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
+        mix ^= mix >> 15;
+        which[r] = static_cast<int>(j0 + mix % static_cast<uint32_t>(j1 - j0));
     }
+    x.numbers(a, which, sample);
+    auto each = [&](auto count) {
+#pragma unroll
+        for (int r = 0; r < kSamples; ++r)
+            if (r * kThreads + tid < some) count(sample[r]);
+    };
+    // Four standard deviations of the sample's count to either side.
+    const float share = static_cast<float>(x.keep) / static_cast<float>(x.n), rank = share * static_cast<float>(some);
+    const float off = some < kAll ? 1.0f : 4.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
+    const int first = static_cast<int>(rank - off), last = static_cast<int>(rank + off) + 1;
+    // (A border that ends a bin is one less than the numbers over it.)
+    const uint32_t high = first < 1 ? 0xffffffffu : border_of(first, each, sh, turn).over;
+    const uint32_t low = last > some ? 0u : border_of(last, each, sh, turn).over;
+    uint32_t above = 0, at_high = 0, at_low = 0, fixed = 0, listed = 0;
+    const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
+    uint32_t *list = lists + pair * a.max_keys + begin;
+    for (int64_t at = seg.start(w); at < end; at += kChunk) {
+        Held<> t;
+        t.load(a, x, at + tid * kHeld, begin, end);
+        uint32_t o[kHeld], set = 0, all;
+        t.numbers(true, o);
+        fixed += __popc(t.fixed);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const bool in = (t.in >> i & 1u) != 0u;
+            above += in && o[i] > high ? 1u : 0u;
+            at_high += in && o[i] == high ? 1u : 0u;
+            at_low += in && o[i] == low && o[i] != high ? 1u : 0u;
+            set |= in && o[i] > low && o[i] < high ? 1u << i : 0u;
+        }
+        uint32_t to = listed + before(__popc(set), all, sh, turn);
+        listed += all;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (set >> i & 1u) list[to++] = o[i];
+    }
+    Counts c{low, high, 0, 0, listed, 0, 0, 0};
+    before(above, c.above, sh, turn);
+    before(at_high, c.at_high, sh, turn);
+    before(at_low, c.at_low, sh, turn);
+    before(fixed, c.fixed, sh, turn);
+    if (tid == 0) counts[pair * kMostSegments + w] = c;
 }
 
 // The second one: the border, and each segment's sources or targets.
@@ -534,155 +534,143 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     const int tid = static_cast<int>(threadIdx.x);
     int turn = 0;
     clear(sh);
-    for (int64_t pair = blockIdx.x; pair < a.S * a.kv_heads; pair += gridDim.x) {
-        const Head x = head_of(a, pair);
-        const Segments seg(x, size);
-        const int w = static_cast<int>(blockIdx.y);
-        if (x.h == 0 && w == 0 && tid == 0) put_len(a, x);
-        if (w == 0 && tid == 0 && (x.leave || x.keep == 0)) moves.count[pair] = 0;
-        if (w >= seg.all) continue;
-        const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
-        if (x.leave || x.keep == 0) {
-            if (x.leave) carry_all(a, x, begin, end);
-            continue;
+    const int64_t pair = pair_of();
+    if (pair >= a.S * a.kv_heads) return;
+    const Head x = head_of(a, pair);
+    const Segments seg(x, size);
+    const int w = static_cast<int>(blockIdx.y);
+    if (x.h == 0 && w == 0 && tid == 0) put_len(a, x);
+    if (w == 0 && tid == 0 && (x.leave || x.keep == 0)) moves.count[pair] = 0;
+    if (w >= seg.all) return;
+    const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
+    if (x.leave || x.keep == 0) {
+        if (x.leave) carry_all(a, x, begin, end);
+        return;
+    }
+    __syncthreads();
+    if (tid < seg.all) held[tid] = counts[pair * kMostSegments + tid], over[tid] = even[tid] = 0;
+    __syncthreads();
+    uint32_t above = 0, at_high = 0, between = 0, at_low = 0, fixed = 0;
+    for (int i = 0; i < seg.all; ++i) {
+        if (tid == 0) starts[i] = between;
+        above += held[i].above, at_high += held[i].at_high, between += held[i].between, at_low += held[i].at_low;
+        fixed += held[i].fixed;
+    }
+    if (tid == 0) starts[seg.all] = between;
+    __syncthreads();
+    const uint32_t keep = static_cast<uint32_t>(x.keep), low = held[0].low, high = held[0].high;
+    const bool few = fixed <= keep;
+    Border border;
+    auto segment_of = [&](uint32_t e) {  // of the e-th listed number
+        int lo = 0, hi = seg.all;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (starts[mid] <= e) lo = mid; else hi = mid;
         }
-        __syncthreads();
-        if (tid < seg.all) held[tid] = counts[pair * kMostSegments + tid], over[tid] = even[tid] = 0;
-        __syncthreads();
-        uint32_t above = 0, at_high = 0, between = 0, at_low = 0, fixed = 0;
-        for (int i = 0; i < seg.all; ++i) {
-            if (tid == 0) starts[i] = between;
-            above += held[i].above, at_high += held[i].at_high, between += held[i].between, at_low += held[i].at_low;
-            fixed += held[i].fixed;
+        return lo;
+    };
+    auto listed = [&](uint32_t e) {
+        const int i = segment_of(e);
+        return lists[pair * a.max_keys + seg.begin(x, i) + (e - starts[i])];
+    };
+    if (few && keep > above && keep <= above + at_high) {
+        border = Border{high, keep - above};
+        if (tid < seg.all) over[tid] = held[tid].above, even[tid] = held[tid].at_high;
+    } else if (few && keep > above + at_high && keep <= above + at_high + between) {
+        // As many as the registers hold are read once, the others again and again.
+        uint32_t o[kHeld];
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) {
+            const uint32_t e = r * kThreads + tid;
+            o[r] = 0u;
+            if (static_cast<uint32_t>(r * kThreads) < between) o[r] = listed(e < between ? e : between - 1);
+            o[r] = e < between ? o[r] : 0u;
         }
-        if (tid == 0) starts[seg.all] = between;
-        __syncthreads();
-        const uint32_t keep = static_cast<uint32_t>(x.keep), low = held[0].low, high = held[0].high;
-        const bool few = fixed <= keep;
-        Border border;
-        auto listed = [&](uint32_t e, int &of) {  // the e-th listed number, and its segment
-            int lo = 0, hi = seg.all;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (starts[mid] <= e) lo = mid; else hi = mid;
-            }
-            of = lo;
-            return lists[pair * a.max_keys + seg.begin(x, lo) + (e - starts[lo])];
+        auto rest = [&](auto f) {
+            for (uint32_t e = kChunk + tid; e < between; e += kThreads) f(listed(e), e);
         };
-        if (few && keep > above && keep <= above + at_high) {
-            border = Border{high, keep - above};
-            if (tid < seg.all) over[tid] = held[tid].above, even[tid] = held[tid].at_high;
-        } else if (few && keep > above + at_high && keep <= above + at_high + between) {
-            // As many as the registers hold are read once, the others again and again.
-            uint32_t o[kHeld];
-            int of[kHeld];
+        border = border_of(
+            keep - above - at_high,
+            [&](auto count) {
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) {
-                const uint32_t e = r * kThreads + tid;
-                o[r] = listed(e < between ? e : between - 1, of[r]);
-            }
+                for (int r = 0; r < kHeld; ++r) count(o[r]);
+                rest([&](uint32_t n, uint32_t) { count(n); });
+            },
+            sh, turn);
+        if (tid < seg.all) over[tid] = held[tid].above + held[tid].at_high;
+        __syncthreads();
+        auto sort = [&](uint32_t n, uint32_t e) {
+            if (n > border.over) atomicAdd(&over[segment_of(e)], 1u);
+            if (n == border.over && n != 0u) atomicAdd(&even[segment_of(e)], 1u);
+        };
 #pragma unroll
-            for (int r = 0; r < kHeld; ++r) o[r] = static_cast<uint32_t>(r * kThreads + tid) < between ? o[r] : 0u;
-            auto rest = [&](auto f) {
-                for (uint32_t e = kChunk + tid; e < between; e += kThreads) {
-                    int seg_of;
-                    const uint32_t n = listed(e, seg_of);
-                    f(n, seg_of);
-                }
-            };
-            border = border_of(
-                keep - above - at_high,
-                [&](auto count) {
-#pragma unroll
-                    for (int r = 0; r < kHeld; ++r) count(o[r]);
-                    rest([&](uint32_t n, int) { count(n); });
-                },
-                sh, turn);
-            if (tid < seg.all) over[tid] = held[tid].above + held[tid].at_high;
-            __syncthreads();
-            auto sort = [&](uint32_t n, int seg_of) {
-                if (n > border.over) atomicAdd(&over[seg_of], 1u);
-                if (n == border.over && n != 0u) atomicAdd(&even[seg_of], 1u);
-            };
-#pragma unroll
-            for (int r = 0; r < kHeld; ++r) sort(o[r], of[r]);
-            rest(sort);
-        } else if (few && keep > above + at_high + between && keep <= above + at_high + between + at_low) {
-            border = Border{low, keep - above - at_high - between};
-            if (tid < seg.all) {
-                over[tid] = held[tid].above + held[tid].at_high + held[tid].between;
-                even[tid] = held[tid].at_low;
-            }
-        } else {  // the two numbers do not hold it, or more tokens are protected than stay
-            border = border_of(
-                keep,
-                [&](auto count) {
-                    for (int64_t at = 0; at < x.n; at += kChunk) {
-                        Held t;
-                        t.load(a, x, at + tid * kHeld, 0, x.n);
-                        uint32_t o[kHeld];
-                        t.numbers(few, o);
-#pragma unroll
-                        for (int i = 0; i < kHeld; ++i) count(o[i]);
-                    }
-                },
-                sh, turn);
-            for (int64_t at = 0; at < x.n; at += kChunk) {
-                Held t;
-                t.load(a, x, at + tid * kHeld, 0, x.n);
-                uint32_t o[kHeld];
+        for (int r = 0; r < kHeld; ++r) sort(o[r], r * kThreads + tid);
+        rest(sort);
+    } else if (few && keep > above + at_high + between && keep <= above + at_high + between + at_low) {
+        border = Border{low, keep - above - at_high - between};
+        if (tid < seg.all) {
+            over[tid] = held[tid].above + held[tid].at_high + held[tid].between;
+            even[tid] = held[tid].at_low;
+        }
+    } else {  // the two numbers do not hold it, or more tokens are protected than stay
+        auto all_of_them = [&](auto f) {
+            for (int64_t j = 4 * tid; j < x.n; j += 4 * kThreads) {
+                Held<4> t;
+                t.load(a, x, j, 0, x.n);
+                uint32_t o[4];
                 t.numbers(few, o);
 #pragma unroll
-                for (int i = 0; i < kHeld; ++i) {
-                    const int64_t j = at + tid * kHeld + i;
-                    if (o[i] > border.over) atomicAdd(&over[seg.of(x, j)], 1u);
-                    if (o[i] == border.over && o[i] != 0u) atomicAdd(&even[seg.of(x, j)], 1u);
-                }
+                for (int i = 0; i < 4; ++i) f(o[i], j + i);
             }
-        }
-        __syncthreads();
-        // Of those at the border the first ones stay; and what comes before this segment.
-        uint32_t left = border.even, stays = 0, first = 0, all = 0;
-        for (int i = 0; i < seg.all; ++i) {
-            const uint32_t take = even[i] < left ? even[i] : left;
-            const uint32_t kept = over[i] + take;
-            left -= take;
-            const uint32_t mine = i < seg.below ? static_cast<uint32_t>(seg.end(x, i) - seg.begin(x, i)) - kept : kept;
-            if (i == w) stays = take;
-            if (i < w && (i < seg.below) == (w < seg.below)) first += mine;
-            if (i >= seg.below) all += mine;
-        }
-        if (w == 0 && tid == 0) moves.count[pair] = static_cast<int32_t>(all);
-        const bool below = w < seg.below;
-        int32_t *out = moves.from + (pair * 2 + (below ? 1 : 0)) * moves.most;
-        uint32_t first_even = 0;
-        for (int64_t at = seg.start(w); at < end; at += kChunk) {
-            const int64_t j0 = at + tid * kHeld;
-            Held t;
-            t.load(a, x, j0, begin, end);
-            uint32_t o[kHeld], kept = 0, at_it = 0, total;
-            t.numbers(few, o);
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i) {
-                kept |= o[i] > border.over ? 1u << i : 0u;
-                at_it |= o[i] == border.over ? 1u << i : 0u;
-            }
-            at_it &= t.in;
-            uint32_t rank = first_even + before(__popc(at_it), total, sh, turn);
-            first_even += total;
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (at_it >> i & 1u) kept |= rank++ < stays ? 1u << i : 0u;
-            const uint32_t set = below ? t.in & ~kept : kept;
-            uint32_t to = first + before(__popc(set), total, sh, turn);
-            first += total;
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (set >> i & 1u) out[to++] = static_cast<int32_t>(j0 + i);
-            if (below && carries(a) && t.in != 0u) t.carry(a, x);
-        }
-        __syncthreads();
+        };
+        border = border_of(keep, [&](auto count) { all_of_them([&](uint32_t o, int64_t) { count(o); }); }, sh, turn);
+        all_of_them([&](uint32_t o, int64_t j) {
+            if (o > border.over) atomicAdd(&over[seg.of(x, j)], 1u);
+            if (o == border.over && o != 0u) atomicAdd(&even[seg.of(x, j)], 1u);
+        });
     }
+    __syncthreads();
+    // Of those at the border the first ones stay; and what comes before this segment.
+    uint32_t left = border.even, stays = 0, first = 0, all = 0;
+    for (int i = 0; i < seg.all; ++i) {
+        const uint32_t take = even[i] < left ? even[i] : left;
+        const uint32_t kept = over[i] + take;
+        left -= take;
+        const uint32_t mine = i < seg.below ? static_cast<uint32_t>(seg.end(x, i) - seg.begin(x, i)) - kept : kept;
+        if (i == w) stays = take;
+        if (i < w && (i < seg.below) == (w < seg.below)) first += mine;
+        if (i >= seg.below) all += mine;
+    }
+    if (w == 0 && tid == 0) moves.count[pair] = static_cast<int32_t>(all);
+    const bool below = w < seg.below;
+    int32_t *out = moves.from + (pair * 2 + (below ? 1 : 0)) * moves.most;
+    uint32_t first_even = 0;
+    for (int64_t at = seg.start(w); at < end; at += kChunk) {
+        const int64_t j0 = at + tid * kHeld;
+        Held<> t;
+        t.load(a, x, j0, begin, end);
+        if (below && carries(a) && t.in != 0u) t.carry(a, x, t.in);
+        uint32_t o[kHeld], kept = 0, at_it = 0, total;
+        t.numbers(few, o);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            kept |= o[i] > border.over ? 1u << i : 0u;
+            at_it |= o[i] == border.over ? 1u << i : 0u;
+        }
+        at_it &= t.in;
+        uint32_t rank = first_even + before(__popc(at_it), total, sh, turn);
+        first_even += total;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (at_it >> i & 1u) kept |= rank++ < stays ? 1u << i : 0u;
+        const uint32_t set = below ? t.in & ~kept : kept;
+        uint32_t to = first + before(__popc(set), total, sh, turn);
+        first += total;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (set >> i & 1u) out[to++] = static_cast<int32_t>(j0 + i);
+    }
+    __syncthreads();
 }
 
 struct Plan {
@@ -716,17 +704,17 @@ hipError_t launch(const EvictArgs &a, char *workspace, hipStream_t stream) {
     const int64_t heads = a.S * a.kv_heads;
     const Plan p = plan_evict(heads, a.max_keys);
     const Moves moves{reinterpret_cast<int32_t *>(workspace), reinterpret_cast<int32_t *>(workspace + p.off_from), p.most};
-    const unsigned grid = static_cast<unsigned>(heads < kGrid ? heads : kGrid);
+    const dim3 grid(static_cast<unsigned>(heads < kGrid ? heads : kGrid), 1, static_cast<unsigned>((heads + kGrid - 1) / kGrid));
     if (a.max_keys <= kChunk) {
         if (heads >= 256 || a.max_keys <= 2048) {
-            k_evict_held<true, CHUNKS><<<dim3(grid), kThreads, 0, stream>>>(a, moves);
+            k_evict_held<true, CHUNKS><<<grid, kThreads, 0, stream>>>(a, moves);
             return hipGetLastError();
         }
-        k_evict_held<false, CHUNKS><<<dim3(grid), kThreads, 0, stream>>>(a, moves);
+        k_evict_held<false, CHUNKS><<<grid, kThreads, 0, stream>>>(a, moves);
     } else {
         Counts *counts = reinterpret_cast<Counts *>(workspace + p.off_counts);
         uint32_t *lists = reinterpret_cast<uint32_t *>(workspace + p.off_lists);
-        const dim3 segments(grid, static_cast<unsigned>(p.segments));
+        const dim3 segments(grid.x, static_cast<unsigned>(p.segments), grid.z);
         k_evict_count<<<segments, kThreads, 0, stream>>>(a, counts, lists, p.size);
         k_evict_list<<<segments, kThreads, 0, stream>>>(a, counts, lists, p.size, moves);
     }
