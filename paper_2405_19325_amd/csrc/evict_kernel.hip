@@ -45,32 +45,53 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 
 // LDS of the collective steps.
 struct Shared {
-    uint32_t bins[kBins];     // all 0 between them
-    uint32_t part[2][kWaves]; // these alternate, so that a sum may follow another without a barrier between
-    uint32_t bin, rank, count;
+    uint32_t bins[kBins];      // all 0 between them
+    uint32_t part[2][3][kWaves]; // these alternate, so that a sum may follow another without a barrier between
+    uint32_t bin[2], rank[2], count[2];
+    uint32_t n, few[kWave];    // the numbers of a bin with few
 };
 
 __device__ __forceinline__ void clear(Shared &sh) {
     static_assert(kBins == 4 * kThreads, "four bins a thread");
     reinterpret_cast<uint4 *>(sh.bins)[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 0) sh.n = 0;
 }
+
+__device__ __forceinline__ uint32_t votes(bool flag) { return static_cast<uint32_t>(__popcll(__ballot(flag))); }
 
 // What the threads before this one have of v together, and all (up to 2^32).
 __device__ __forceinline__ uint32_t before(uint32_t v, uint32_t &all, Shared &sh, int &turn) {
     const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = static_cast<int>(threadIdx.x) / kWave;
     const uint32_t upto = wave_incl_scan_u32(v, lane);
     turn ^= 1;
-    if (lane == kWave - 1) sh.part[turn][wave] = upto;
+    if (lane == kWave - 1) sh.part[turn][0][wave] = upto;
     __syncthreads();
     uint32_t first = upto - v;
     all = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        const uint32_t x = sh.part[turn][w];
+        const uint32_t x = sh.part[turn][0][w];
         first += w < wave ? x : 0u;
         all += x;
     }
     return first;
+}
+
+// The workgroup's sum, least and largest.
+__device__ __forceinline__ void reduce(uint32_t &sum, uint32_t &least, uint32_t &largest, Shared &sh, int &turn) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = static_cast<int>(threadIdx.x) / kWave;
+    turn ^= 1;
+    const uint32_t s = readlane_u32(wave_incl_scan_u32(sum, lane), kWave - 1);
+    const uint32_t lo = wave_allmin_u32(least), hi = wave_allmax_u32(largest);
+    if (lane == 0) sh.part[turn][0][wave] = s, sh.part[turn][1][wave] = lo, sh.part[turn][2][wave] = hi;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        sum += sh.part[turn][0][w];
+        least = min(least, sh.part[turn][1][w]);
+        largest = max(largest, sh.part[turn][2][w]);
+    }
 }
 
 // The border of the `rank` largest numbers: those over `over` are among them,
@@ -79,41 +100,75 @@ struct Border {
     uint32_t over, even;
 };
 
-// By eleven bits at a time, counted into bins.  each(f) calls f with all of
-// this thread's numbers (0: none), the same ones every time; rank is at least
-// 1 and at most as many as there are.
-template <class Each>
-__device__ __forceinline__ Border border_of(uint32_t rank, Each each, Shared &sh, int &turn) {
-    uint32_t prefix = 0;
-#pragma unroll 1
-    for (int shift = 32 - kBits;; shift = shift > kBits ? shift - kBits : 0) {
-        // (the last digit has the ten bits that are left)
-        const int bits = shift == 0 ? 32 - 2 * kBits : kBits;
-        const bool top = shift == 32 - kBits;
-        each([&](uint32_t o) {
-            if (o != 0u && (top || o >> (shift + bits) == prefix)) atomicAdd(&sh.bins[o >> shift & ((1u << bits) - 1u)], 1u);
-        });
-        __syncthreads();
-        // Four bins a thread, the highest ones first.
-        uint4 *mine = reinterpret_cast<uint4 *>(sh.bins) + (kThreads - 1 - threadIdx.x);
-        const uint4 c = *mine;
-        *mine = make_uint4(0, 0, 0, 0);
-        uint32_t all;
-        const uint32_t first = before(c.x + c.y + c.z + c.w, all, sh, turn);
-        if (rank > first && rank <= first + c.x + c.y + c.z + c.w) {
-            uint32_t left = rank - first, bin = 4 * (kThreads - 1 - threadIdx.x) + 3, count = c.w;
+// Numbers base .. base + 2^bits - 1, the rank-th largest of which is looked for.
+struct Range {
+    uint32_t base;
+    int bits;
+    uint32_t rank, count;
+    __device__ __forceinline__ bool has(uint32_t o) const { return bits >= 32 || (o >= base && (o - base) >> bits == 0u); }
+};
+
+__device__ __forceinline__ Range range_of(uint32_t least, uint32_t largest, uint32_t rank) {
+    return Range{least, 32 - __clz(static_cast<int>(largest - least)), rank, 0xffffffffu};
+}
+
+// Cuts a range down to one of its 2,048 bins (several, for as many ranks in it).
+// each(f) calls f with all of this thread's numbers (0: none), the same ones
+// every time; a rank is at least 1 and at most as many as the range has.
+template <int N, class Each>
+__device__ __forceinline__ void narrow(Range (&r)[N], Each each, Shared &sh, int &turn) {
+    const uint32_t base = r[0].base;
+    const int shift = r[0].bits > kBits ? r[0].bits - kBits : 0;
+    const Range in = r[0];
+    each([&](uint32_t o) {
+        if (o != 0u && in.has(o)) atomicAdd(&sh.bins[(o - base) >> shift], 1u);
+    });
+    __syncthreads();
+    // Four bins a thread, the highest ones first.
+    uint4 *mine = reinterpret_cast<uint4 *>(sh.bins) + (kThreads - 1 - threadIdx.x);
+    const uint4 c = *mine;
+    *mine = make_uint4(0, 0, 0, 0);
+    uint32_t all;
+    const uint32_t first = before(c.x + c.y + c.z + c.w, all, sh, turn);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (r[i].rank > first && r[i].rank <= first + c.x + c.y + c.z + c.w) {
+            uint32_t left = r[i].rank - first, bin = 4 * (kThreads - 1 - threadIdx.x) + 3, count = c.w;
             if (left > count) left -= count, --bin, count = c.z;
             if (left > count) left -= count, --bin, count = c.y;
             if (left > count) left -= count, --bin, count = c.x;
-            sh.bin = bin, sh.rank = left, sh.count = count;
+            sh.bin[i] = bin, sh.rank[i] = left, sh.count[i] = count;
         }
-        __syncthreads();
-        prefix = prefix << bits | sh.bin;
-        rank = sh.rank;
-        const bool whole = sh.count == rank;  // all of the bin: no need to look into it
-        if (whole) return Border{prefix == 0 ? 0u : (prefix << shift) - 1u, 0u};
-        if (shift == 0) return Border{prefix, rank};
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = Range{base + (sh.bin[i] << shift), shift, sh.rank[i], sh.count[i]};
+}
+
+// The border, all numbers being in [least, largest].
+template <class Each>
+__device__ __forceinline__ Border border_of(uint32_t rank, uint32_t least, uint32_t largest, Each each, Shared &sh, int &turn) {
+    Range r[1] = {range_of(least, largest, rank)};
+    do {
+        narrow(r, each, sh, turn);
+        if (r[0].count == r[0].rank) return Border{r[0].base - 1u, 0u};  // all of the bin (no number is 0)
+    } while (r[0].bits > 0 && r[0].count > kWave);
+    if (r[0].bits == 0) return Border{r[0].base, r[0].rank};
+    // The few that are left, a lane each in every wave.
+    each([&](uint32_t o) {
+        if (o != 0u && r[0].has(o)) sh.few[atomicAdd(&sh.n, 1u)] = o;
+    });
+    __syncthreads();
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), n = static_cast<int>(r[0].count);
+    const uint32_t x = lane < n ? sh.few[lane] : 0u;
+    uint32_t over = 0, upto = 0;
+    for (int i = 0; i < n; ++i) {
+        const uint32_t y = readlane_u32(x, i);
+        over += y > x ? 1u : 0u;
+        upto += y >= x ? 1u : 0u;
     }
+    const uint64_t at = __ballot(lane < n && over < r[0].rank && r[0].rank <= upto);
+    const int which = __ffsll(static_cast<unsigned long long>(at)) - 1;
+    return Border{readlane_u32(x, which), r[0].rank - readlane_u32(over, which)};
 }
 
 // A head of a sequence and what becomes of it.
@@ -153,8 +208,8 @@ struct Head {
 
 __device__ __forceinline__ int64_t pair_of() { return static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.x; }
 
-// For all threads of a workgroup together.
-__device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
+// Without a look at its pages.
+__device__ __forceinline__ Head head_at(const EvictArgs &a, int64_t pair) {
     Head x;
     x.s = pair / a.kv_heads;
     x.h = static_cast<int>(pair - x.s * a.kv_heads);
@@ -164,23 +219,28 @@ __device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
     const int64_t recent_from = (a.next_positions != nullptr ? a.next_positions[x.s] : len) - a.recent;
     x.recent_from = static_cast<int32_t>(recent_from > -0x80000000LL ? recent_from : -0x80000000LL);
     x.leave = budget < 0 || budget >= n || n > limit;
-    if (!x.leave) {
-        bool whole = true;
-        const int64_t entries = (n + (int64_t{1} << a.cache.page_log2) - 1) >> a.cache.page_log2;
-        const int32_t *table = a.cache.pages + x.s * a.cache.table_width;
-        for (int64_t e = threadIdx.x; e < entries; e += 4 * kThreads) {
-            int32_t page[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) page[u] = table[e + u * kThreads < entries ? e + u * kThreads : e];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) whole = whole && page[u] >= 0 && page[u] < a.cache.n_pages;
-        }
-        x.leave = __syncthreads_or(!whole) != 0;
-    }
     x.n = n < limit ? n : limit;
     x.keep = x.leave ? x.n : budget;
     x.vec = ((reinterpret_cast<uintptr_t>(a.mass) | reinterpret_cast<uintptr_t>(a.key_positions) |
               reinterpret_cast<uintptr_t>(a.mass_out) | reinterpret_cast<uintptr_t>(a.positions_out)) % 16) == 0;
+    return x;
+}
+
+// For all threads of a workgroup together.
+__device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
+    Head x = head_at(a, pair);
+    if (x.leave) return x;
+    bool whole = true;
+    const int64_t entries = (x.n + (int64_t{1} << a.cache.page_log2) - 1) >> a.cache.page_log2;
+    const int32_t *table = a.cache.pages + x.s * a.cache.table_width;
+    for (int64_t e = threadIdx.x; e < entries; e += 4 * kThreads) {
+        int32_t page[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) page[u] = table[e + u * kThreads < entries ? e + u * kThreads : e];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) whole = whole && page[u] >= 0 && page[u] < a.cache.n_pages;
+    }
+    if (__syncthreads_or(!whole) != 0) x.leave = true, x.keep = x.n;
     return x;
 }
 
@@ -194,6 +254,7 @@ struct Held {
     int64_t at;      // place of the first
     uint32_t in;     // as bits: those in the range
     uint32_t fixed;  // and of these the protected ones
+    bool missing;    // there are some, and their page is none
     union {
         float m[N];
         float4 m4[N / 4];
@@ -205,11 +266,14 @@ struct Held {
 
     __device__ __forceinline__ void load(const EvictArgs &a, const Head &x, int64_t j0, int64_t from, int64_t to) {
         in = fixed = 0;
+        missing = false;
         if (j0 >= to || j0 + N <= from) return;
+        at = x.place(a, j0);
+        missing = at < 0;
+        if (missing) return;
         in = (1u << N) - 1u;
         if (j0 < from) in &= ~0u << (from - j0);
         if (j0 + N > to) in &= (1u << (to - j0)) - 1u;
-        at = x.place(a, j0);
         if (x.vec) {
 #pragma unroll
             for (int i = 0; i < N / 4; ++i) {
@@ -334,27 +398,37 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_held(EvictArgs a, Moves m
     clear(sh);
     const int64_t pair = pair_of();
     if (pair >= a.S * a.kv_heads) return;
-    const Head x = head_of(a, pair);
+    Head x = head_at(a, pair);
+    const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep), j0 = tid * kHeld;
+    Held<> t;
+    t.load(a, x, j0, 0, x.leave ? 0 : n);  // every page is some thread's
+    const uint32_t low = keep <= j0 ? 0u : keep >= j0 + kHeld ? (1u << kHeld) - 1u : (1u << (keep - j0)) - 1u;
+    if (carries(a) && (t.in & low) != 0u) t.carry(a, x, t.in & low);
+    uint32_t o[kHeld], least = 0xffffffffu, largest = 0u;
+    t.numbers(true, o);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        if (o[i] == 0u || o[i] == 0xffffffffu) continue;
+        least = min(least, o[i]), largest = max(largest, o[i]);
+    }
+    uint32_t protects = t.missing ? 1u << 16 : __popc(t.fixed);  // 8,192 at most are protected
+    if (!x.leave) {
+        reduce(protects, least, largest, sh, turn);
+        x.leave = protects >> 16 != 0u;
+    }
     if (x.h == 0 && tid == 0) put_len(a, x);
     if (x.leave) {
         carry_all(a, x, 0, x.n);
         if (!MOVE && tid == 0) moves.count[pair] = 0;
         return;
     }
-    const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep), j0 = tid * kHeld;
-    Held<> t;
-    t.load(a, x, j0, 0, n);
-    const uint32_t low = keep <= j0 ? 0u : keep >= j0 + kHeld ? (1u << kHeld) - 1u : (1u << (keep - j0)) - 1u;
-    if (carries(a) && (t.in & low) != 0u) t.carry(a, x, t.in & low);
-    uint32_t protects, o[kHeld];
-    before(__popc(t.fixed), protects, sh, turn);
     const bool few = protects <= static_cast<uint32_t>(keep);
-    t.numbers(few, o);
+    if (!few) t.numbers(false, o), least = 1u, largest = 0xff800000u;
     const uint32_t rank = few ? keep - protects : keep;  // among those that are not protected, or among these alone
     Border border{few ? 0xfffffffeu : 0xffffffffu, 0u};
     if (rank > 0)
         border = border_of(
-            rank,
+            rank, least, largest,
             [&](auto count) {
 #pragma unroll
                 for (int i = 0; i < kHeld; ++i)
@@ -467,32 +541,55 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
     const Segments seg(x, size);
     const int w = static_cast<int>(blockIdx.y);
     if (x.leave || w >= seg.all || x.keep == 0) return;
-    // One token of each of 4,096 equal pieces, at no regular distance.
-    constexpr int kAll = kSamples * kThreads;
-    const int64_t some = x.n < kAll ? x.n : kAll;
+    // One token of each of 4,096 equal pieces, at no regular distance; all of fewer.
+    constexpr int kAll = kSamples * kThreads, kLog2 = 12;
+    static_assert(kAll == 1 << kLog2, "pieces by shifts");
+    const bool whole = x.n <= kAll;
+    const int some = whole ? static_cast<int>(x.n) : kAll;
     int which[kSamples];
-    uint32_t sample[kSamples];
+    uint32_t sample[kSamples], least = 0xffffffffu, largest = 0u, held = 0;
 #pragma unroll
     for (int r = 0; r < kSamples; ++r) {
-        const int64_t i = r * kThreads + tid < some ? r * kThreads + tid : some - 1;
-        const int64_t j0 = i * x.n / some, j1 = (i + 1) * x.n / some;
-        uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
-        mix ^= mix >> 15;
-        which[r] = static_cast<int>(j0 + mix % static_cast<uint32_t>(j1 - j0));
+        const int i = r * kThreads + tid < some ? r * kThreads + tid : some - 1;
+        const int j0 = static_cast<int>(i * x.n >> kLog2), j1 = static_cast<int>((i + 1) * x.n >> kLog2);
+        const uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
+        which[r] = whole ? i : j0 + static_cast<int>(__umulhi(mix ^ mix >> 15, static_cast<uint32_t>(j1 - j0)));
     }
     x.numbers(a, which, sample);
-    auto each = [&](auto count) {
 #pragma unroll
-        for (int r = 0; r < kSamples; ++r)
-            if (r * kThreads + tid < some) count(sample[r]);
-    };
+    for (int r = 0; r < kSamples; ++r) {
+        if (r * kThreads + tid >= some) sample[r] = 0u;
+        if (sample[r] == 0u || sample[r] == 0xffffffffu) continue;
+        least = min(least, sample[r]), largest = max(largest, sample[r]);
+        ++held;
+    }
+    reduce(held, least, largest, sh, turn);
+    const int fixed_ones = some - static_cast<int>(held);
     // Four standard deviations of the sample's count to either side.
     const float share = static_cast<float>(x.keep) / static_cast<float>(x.n), rank = share * static_cast<float>(some);
-    const float off = some < kAll ? 1.0f : 4.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
-    const int first = static_cast<int>(rank - off), last = static_cast<int>(rank + off) + 1;
-    // (A border that ends a bin is one less than the numbers over it.)
-    const uint32_t high = first < 1 ? 0xffffffffu : border_of(first, each, sh, turn).over;
-    const uint32_t low = last > some ? 0u : border_of(last, each, sh, turn).over;
+    const float off = whole ? 1.0f : 4.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
+    const int first = static_cast<int>(rank - off) - fixed_ones, last = static_cast<int>(rank + off) + 1 - fixed_ones;
+    uint32_t high = 0xfffffffeu, low = 0u;  // protected tokens are above, and no number is 0
+    if (held > 0) {
+        auto each = [&](auto count) {
+#pragma unroll
+            for (int r = 0; r < kSamples; ++r)
+                if (sample[r] != 0xffffffffu) count(sample[r]);
+        };
+        // The bins of both ranks; one that holds many is cut further (they may all be equal).
+        auto clamp = [&](int i) { return static_cast<uint32_t>(i < 1 ? 1 : i > static_cast<int>(held) ? static_cast<int>(held) : i); };
+        Range r[2] = {range_of(least, largest, clamp(first)), range_of(least, largest, clamp(last))};
+        narrow(r, each, sh, turn);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            Range one[1] = {r[i]};
+            while (one[0].bits > 0 && one[0].count > kWave) narrow(one, each, sh, turn);
+            r[i] = one[0];
+        }
+        // A bin's numbers lie between; one number is a border itself.
+        if (first >= 1) high = r[0].bits > 0 ? r[0].base + (1u << r[0].bits) : r[0].base;
+        if (last <= static_cast<int>(held)) low = r[1].bits > 0 ? r[1].base - 1u : r[1].base;
+    }
     uint32_t above = 0, at_high = 0, at_low = 0, fixed = 0, listed = 0;
     const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
     uint32_t *list = lists + pair * a.max_keys + begin;
@@ -524,6 +621,13 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
     if (tid == 0) counts[pair * kMostSegments + w] = c;
 }
 
+// How many of the ascending starts[0 .. n - 1] are at most e, for a wave together.
+__device__ __forceinline__ int votes_upto(const uint32_t *starts, int n, uint32_t e, int lane) {
+    static_assert(kMostSegments <= 2 * kWave, "two a lane");
+    return static_cast<int>(votes(lane < n && starts[lane < n ? lane : 0] <= e) +
+                            votes(lane + kWave < n && starts[lane + kWave < n ? lane + kWave : 0] <= e));
+}
+
 // The second one: the border, and each segment's sources or targets.
 __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const Counts *counts, const uint32_t *lists, int64_t size,
                                                          Moves moves) {
@@ -531,7 +635,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     __shared__ Counts held[kMostSegments];
     __shared__ uint32_t over[kMostSegments], even[kMostSegments];  // over and at the border, of each segment
     __shared__ uint32_t starts[kMostSegments + 1];                 // of the listed numbers
-    const int tid = static_cast<int>(threadIdx.x);
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     int turn = 0;
     clear(sh);
     const int64_t pair = pair_of();
@@ -561,17 +666,16 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     const uint32_t keep = static_cast<uint32_t>(x.keep), low = held[0].low, high = held[0].high;
     const bool few = fixed <= keep;
     Border border;
-    auto segment_of = [&](uint32_t e) {  // of the e-th listed number
-        int lo = 0, hi = seg.all;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (starts[mid] <= e) lo = mid; else hi = mid;
-        }
-        return lo;
+    // The segments of the 64 listed numbers from e0 on, a lane each (all lanes of the wave together).
+    auto segment_of = [&](uint32_t e0) {
+        const uint32_t end = e0 + kWave - 1 < between ? e0 + kWave - 1 : between - 1;
+        int of = votes_upto(starts, seg.all, e0, lane) - 1, next = of + 1;
+        for (; next < seg.all && starts[next] <= end; ++next) of = starts[next] <= e0 + lane ? next : of;
+        return of;
     };
-    auto listed = [&](uint32_t e) {
-        const int i = segment_of(e);
-        return lists[pair * a.max_keys + seg.begin(x, i) + (e - starts[i])];
+    auto listed = [&](uint32_t e0, int of) {
+        const uint32_t e = e0 + lane < between ? e0 + lane : between - 1;
+        return lists[pair * a.max_keys + seg.begin(x, of) + (e - starts[of])];
     };
     if (few && keep > above && keep <= above + at_high) {
         border = Border{high, keep - above};
@@ -579,32 +683,51 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     } else if (few && keep > above + at_high && keep <= above + at_high + between) {
         // As many as the registers hold are read once, the others again and again.
         uint32_t o[kHeld];
+        auto at = [&](int r) { return static_cast<uint32_t>((r * kWaves + wave) * kWave); };
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) {
-            const uint32_t e = r * kThreads + tid;
             o[r] = 0u;
-            if (static_cast<uint32_t>(r * kThreads) < between) o[r] = listed(e < between ? e : between - 1);
-            o[r] = e < between ? o[r] : 0u;
+            if (at(r) < between) o[r] = listed(at(r), segment_of(at(r)));
+        }
+        uint32_t least = 0xffffffffu, largest = 0u, sum = 0;
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) {
+            if (at(r) + lane >= between) o[r] = 0u;
+            if (o[r] != 0u) least = min(least, o[r]), largest = max(largest, o[r]);
         }
         auto rest = [&](auto f) {
-            for (uint32_t e = kChunk + tid; e < between; e += kThreads) f(listed(e), e);
+            for (uint32_t e = at(kHeld); e < between; e += kThreads) {
+                const int of = segment_of(e);
+                const uint32_t n = listed(e, of);
+                f(e + lane < between ? n : 0u, of);
+            }
         };
+        if (between > static_cast<uint32_t>(kChunk)) least = low + 1u, largest = high;
+        reduce(sum, least, largest, sh, turn);
         border = border_of(
-            keep - above - at_high,
+            keep - above - at_high, least, largest,
             [&](auto count) {
 #pragma unroll
                 for (int r = 0; r < kHeld; ++r) count(o[r]);
-                rest([&](uint32_t n, uint32_t) { count(n); });
+                rest([&](uint32_t n, int) { count(n); });
             },
             sh, turn);
         if (tid < seg.all) over[tid] = held[tid].above + held[tid].at_high;
         __syncthreads();
-        auto sort = [&](uint32_t n, uint32_t e) {
-            if (n > border.over) atomicAdd(&over[segment_of(e)], 1u);
-            if (n == border.over && n != 0u) atomicAdd(&even[segment_of(e)], 1u);
+        auto sort = [&](uint32_t n, int of) {  // by segments: most often the wave's are all of one
+            const int one = __builtin_amdgcn_readfirstlane(of);
+            if (__all(of == one)) {
+                const uint32_t more = votes(n > border.over), same = votes(n == border.over && n != 0u);
+                if (lane == 0 && more != 0u) atomicAdd(&over[one], more);
+                if (lane == 0 && same != 0u) atomicAdd(&even[one], same);
+            } else {
+                if (n > border.over) atomicAdd(&over[of], 1u);
+                if (n == border.over && n != 0u) atomicAdd(&even[of], 1u);
+            }
         };
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) sort(o[r], r * kThreads + tid);
+        for (int r = 0; r < kHeld; ++r)
+            if (at(r) < between) sort(o[r], segment_of(at(r)));
         rest(sort);
     } else if (few && keep > above + at_high + between && keep <= above + at_high + between + at_low) {
         border = Border{low, keep - above - at_high - between};
@@ -623,7 +746,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
                 for (int i = 0; i < 4; ++i) f(o[i], j + i);
             }
         };
-        border = border_of(keep, [&](auto count) { all_of_them([&](uint32_t o, int64_t) { count(o); }); }, sh, turn);
+        border = border_of(keep, 1u, 0xffffffffu, [&](auto count) { all_of_them([&](uint32_t o, int64_t) { count(o); }); }, sh, turn);
         all_of_them([&](uint32_t o, int64_t j) {
             if (o > border.over) atomicAdd(&over[seg.of(x, j)], 1u);
             if (o == border.over && o != 0u) atomicAdd(&even[seg.of(x, j)], 1u);
