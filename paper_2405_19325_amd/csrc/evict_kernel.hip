@@ -29,10 +29,11 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kHeld = 16;                    // tokens of a thread, one behind the other: they lie within a page
+constexpr int kGroups = 4;                   // of four tokens of a thread, which lie within a page
+constexpr int kHeld = 4 * kGroups;
+constexpr int kRow = 4 * kThreads;           // tokens from a thread's group to its next one
 constexpr int kChunk = kHeld * kThreads;
 constexpr int kSegments = 64;                // of a head, about
-constexpr int kSamples = 8;                  // of a thread
 constexpr int kBits = 11, kBins = 1 << kBits;
 constexpr int64_t kGrid = int64_t{1} << 20;  // heads of a row of the grid
 
@@ -75,6 +76,53 @@ __device__ __forceinline__ uint32_t before(uint32_t v, uint32_t &all, Shared &sh
         all += x;
     }
     return first;
+}
+
+// For tokens held as Held has them: how many of `set` (bits) come before each of
+// this thread's groups, and all; the workgroup's sum of `more`.
+__device__ __forceinline__ void before_groups(uint32_t set, uint32_t (&first)[kGroups], uint32_t &all, uint32_t &more, Shared &sh,
+                                              int &turn) {
+    static_assert(kGroups == 4 && kRow < 1 << 16, "two rows' counts in a word");
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = static_cast<int>(threadIdx.x) / kWave;
+    uint32_t v[2], upto[2], rows[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[i] = __popc(set >> (8 * i) & 15u) | __popc(set >> (8 * i + 4) & 15u) << 16;
+        upto[i] = wave_incl_scan_u32(v[i], lane);
+    }
+    const uint32_t sum = wave_incl_scan_u32(more, lane);
+    turn ^= 1;
+    if (lane == kWave - 1) sh.part[turn][0][wave] = upto[0], sh.part[turn][1][wave] = upto[1], sh.part[turn][2][wave] = sum;
+    __syncthreads();
+    more = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) more += sh.part[turn][2][w];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        upto[i] -= v[i];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t x = sh.part[turn][i][w];
+            upto[i] += w < wave ? x : 0u;
+            rows[i] += x;
+        }
+    }
+    all = 0;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const int at = 16 * (g & 1);
+        first[g] = all + (upto[g / 2] >> at & 0xffffu);
+        all += rows[g / 2] >> at & 0xffffu;
+    }
+}
+
+// f(bit) for each bit that is set.
+template <class F>
+__device__ __forceinline__ void each_bit(uint32_t set, F f) {
+    while (set != 0u) {
+        f(__ffs(static_cast<int>(set)) - 1);
+        set &= set - 1u;
+    }
 }
 
 // The workgroup's sum, least and largest.
@@ -188,28 +236,12 @@ struct Head {
         return few ? (fixed ? 0xffffffffu : order) : (fixed ? order : 0u);
     }
     __device__ __forceinline__ bool fixed(const EvictArgs &a, int32_t p) const { return p < a.sinks || p >= recent_from; }
-    // N tokens, wherever they lie: their numbers.  All loads are on their way together.
-    template <int N>
-    __device__ __forceinline__ void numbers(const EvictArgs &a, const int (&j)[N], uint32_t (&o)[N]) const {
-        int64_t at[N];
-        float m[N];
-        int32_t p[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) at[i] = place(a, j[i]);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            m[i] = a.mass[at[i]];
-            p[i] = a.key_positions != nullptr ? a.key_positions[at[i]] : j[i];
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = number(order_of(m[i]), fixed(a, p[i]), true);
-    }
 };
 
 __device__ __forceinline__ int64_t pair_of() { return static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.x; }
 
-// Without a look at its pages.
-__device__ __forceinline__ Head head_at(const EvictArgs &a, int64_t pair) {
+// (Without a look at its pages.)
+__device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
     Head x;
     x.s = pair / a.kv_heads;
     x.h = static_cast<int>(pair - x.s * a.kv_heads);
@@ -226,97 +258,95 @@ __device__ __forceinline__ Head head_at(const EvictArgs &a, int64_t pair) {
     return x;
 }
 
-// For all threads of a workgroup together.
-__device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
-    Head x = head_at(a, pair);
-    if (x.leave) return x;
-    bool whole = true;
-    const int64_t entries = (x.n + (int64_t{1} << a.cache.page_log2) - 1) >> a.cache.page_log2;
-    const int32_t *table = a.cache.pages + x.s * a.cache.table_width;
-    for (int64_t e = threadIdx.x; e < entries; e += 4 * kThreads) {
-        int32_t page[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) page[u] = table[e + u * kThreads < entries ? e + u * kThreads : e];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) whole = whole && page[u] >= 0 && page[u] < a.cache.n_pages;
-    }
-    if (__syncthreads_or(!whole) != 0) x.leave = true, x.keep = x.n;
-    return x;
-}
-
 __device__ __forceinline__ void put_len(const EvictArgs &a, const Head &x) {
     a.new_lens[x.s] = x.leave ? a.cache_lens[x.s] : static_cast<int32_t>(x.keep);
 }
 
-// N tokens from j0 on, a multiple of N: what the ledger has of those in [from, to).
-template <int N = kHeld>
+// Groups of four tokens, from j[0], j[1], ... on (multiples of four): what the ledger has of those in [from, to).
+template <int G = kGroups>
 struct Held {
-    int64_t at;      // place of the first
+    int64_t at[G];   // place of a group's first
     uint32_t in;     // as bits: those in the range
     uint32_t fixed;  // and of these the protected ones
-    bool missing;    // there are some, and their page is none
+    bool missing;    // there are some whose page is none
     union {
-        float m[N];
-        float4 m4[N / 4];
+        float m[4 * G];
+        float4 m4[G];
     };
     union {
-        int32_t p[N];
-        int4 p4[N / 4];
+        int32_t p[4 * G];
+        int4 p4[G];
     };
 
-    __device__ __forceinline__ void load(const EvictArgs &a, const Head &x, int64_t j0, int64_t from, int64_t to) {
+    __device__ __forceinline__ void load(const EvictArgs &a, const Head &x, const int64_t (&j)[G], int64_t from, int64_t to) {
         in = fixed = 0;
         missing = false;
-        if (j0 >= to || j0 + N <= from) return;
-        at = x.place(a, j0);
-        missing = at < 0;
-        if (missing) return;
-        in = (1u << N) - 1u;
-        if (j0 < from) in &= ~0u << (from - j0);
-        if (j0 + N > to) in &= (1u << (to - j0)) - 1u;
-        if (x.vec) {
+        bool some[G];
 #pragma unroll
-            for (int i = 0; i < N / 4; ++i) {
-                m4[i] = reinterpret_cast<const float4 *>(a.mass + at)[i];
-                if (a.key_positions != nullptr) p4[i] = reinterpret_cast<const int4 *>(a.key_positions + at)[i];
-            }
-        } else {
+        for (int g = 0; g < G; ++g) {
+            some[g] = j[g] < to && j[g] + 4 > from;
+            at[g] = some[g] ? x.place(a, j[g]) : 0;
+            if (at[g] < 0) missing = true, some[g] = false;
+        }
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                m[i] = a.mass[at + i];
-                if (a.key_positions != nullptr) p[i] = a.key_positions[at + i];
+        for (int g = 0; g < G; ++g) {
+            if (!some[g]) continue;
+            uint32_t bits = 15u;
+            if (j[g] < from) bits &= 15u << (from - j[g]);
+            if (j[g] + 4 > to) bits &= (1u << (to - j[g])) - 1u;
+            in |= bits << 4 * g;
+            if (x.vec) {
+                m4[g] = *reinterpret_cast<const float4 *>(a.mass + at[g]);
+                if (a.key_positions != nullptr) p4[g] = *reinterpret_cast<const int4 *>(a.key_positions + at[g]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    m[4 * g + e] = a.mass[at[g] + e];
+                    if (a.key_positions != nullptr) p[4 * g + e] = a.key_positions[at[g] + e];
+                }
             }
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (a.key_positions == nullptr) p[i] = static_cast<int32_t>(j0) + i;
+        for (int i = 0; i < 4 * G; ++i) {
+            if (a.key_positions == nullptr) p[i] = static_cast<int32_t>(j[i / 4]) + i % 4;
             fixed |= x.fixed(a, p[i]) ? 1u << i : 0u;
         }
         fixed &= in;
     }
-    // 0 of those out of the range.
-    __device__ __forceinline__ void numbers(bool few, uint32_t (&o)[N]) const {
+    // This thread's part of kChunk tokens from j0 on.
+    __device__ __forceinline__ void load_chunk(const EvictArgs &a, const Head &x, int64_t j0, int64_t from, int64_t to) {
+        int64_t j[G];
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int g = 0; g < G; ++g) j[g] = token(j0, 4 * g);
+        load(a, x, j, from, to);
+    }
+    __device__ static __forceinline__ int64_t token(int64_t j0, int bit) {
+        return j0 + static_cast<int64_t>(bit / 4) * kRow + 4 * static_cast<int>(threadIdx.x) + bit % 4;
+    }
+    // 0 of those out of the range.
+    __device__ __forceinline__ void numbers(bool few, uint32_t (&o)[4 * G]) const {
+#pragma unroll
+        for (int i = 0; i < 4 * G; ++i)
             o[i] = (in >> i & 1u) != 0u ? Head::number(order_of(m[i]), (fixed >> i & 1u) != 0u, few) : 0u;
     }
     // The entries of `some` go into a ledger of afterwards that is another.  (Those of places that are given up are written
     // over by what moves there, later.)
     __device__ __forceinline__ void carry(const EvictArgs &a, const Head &x, uint32_t some) const {
         const bool masses = a.mass_out != a.mass, positions = a.positions_out != a.key_positions;
-        if (some == (1u << N) - 1u && x.vec) {
 #pragma unroll
-            for (int i = 0; i < N / 4; ++i) {
-                if (masses) reinterpret_cast<float4 *>(a.mass_out + at)[i] = m4[i];
-                if (positions) reinterpret_cast<int4 *>(a.positions_out + at)[i] = p4[i];
+        for (int g = 0; g < G; ++g) {
+            const uint32_t bits = some >> 4 * g & 15u;
+            if (bits == 15u && x.vec) {
+                if (masses) *reinterpret_cast<float4 *>(a.mass_out + at[g]) = m4[g];
+                if (positions) *reinterpret_cast<int4 *>(a.positions_out + at[g]) = p4[g];
+                continue;
             }
-            return;
-        }
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if ((some >> i & 1u) == 0u) continue;
-            if (masses) a.mass_out[at + i] = m[i];
-            if (positions) a.positions_out[at + i] = p[i];
+            for (int e = 0; e < 4; ++e) {
+                if ((bits >> e & 1u) == 0u) continue;
+                if (masses) a.mass_out[at[g] + e] = m[4 * g + e];
+                if (positions) a.positions_out[at[g] + e] = p[4 * g + e];
+            }
         }
     }
 };
@@ -387,6 +417,24 @@ struct Moves {
     int64_t most;
 };
 
+// Of the tokens that a thread holds of kChunk from j0 on, those below `keep`, as bits.
+__device__ __forceinline__ uint32_t below_of(int64_t j0, int64_t keep) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const int64_t left = keep - Held<>::token(j0, 4 * g);
+        bits |= (left <= 0 ? 0u : left >= 4 ? 15u : (1u << left) - 1u) << 4 * g;
+    }
+    return bits;
+}
+
+// How many are kept before the token of bit i, `first` those before its group.
+__device__ __forceinline__ uint32_t kept_before(uint32_t kept, const uint32_t (&first)[kGroups], int i) {
+    const int g = i / 4;
+    const uint32_t at = g == 0 ? first[0] : g == 1 ? first[1] : g == 2 ? first[2] : first[3];
+    return at + __popc((kept >> 4 * g & 15u) & ((1u << (i & 3)) - 1u));
+}
+
 // A head in a workgroup's registers.  `CHUNKS` as in move; MOVE: the moves are
 // made here, else left to another launch.
 template <bool MOVE, int CHUNKS>
@@ -398,11 +446,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_held(EvictArgs a, Moves m
     clear(sh);
     const int64_t pair = pair_of();
     if (pair >= a.S * a.kv_heads) return;
-    Head x = head_at(a, pair);
-    const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep), j0 = tid * kHeld;
+    Head x = head_of(a, pair);
+    const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep);
     Held<> t;
-    t.load(a, x, j0, 0, x.leave ? 0 : n);  // every page is some thread's
-    const uint32_t low = keep <= j0 ? 0u : keep >= j0 + kHeld ? (1u << kHeld) - 1u : (1u << (keep - j0)) - 1u;
+    t.load_chunk(a, x, 0, 0, x.leave ? 0 : n);  // every page is some thread's
+    const uint32_t low = below_of(0, keep);
     if (carries(a) && (t.in & low) != 0u) t.carry(a, x, t.in & low);
     uint32_t o[kHeld], least = 0xffffffffu, largest = 0u;
     t.numbers(true, o);
@@ -435,34 +483,31 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_held(EvictArgs a, Moves m
                     if (o[i] != 0xffffffffu) count(o[i]);
             },
             sh, turn);
-    uint32_t over = 0, at_it = 0;  // as bits
+    uint32_t kept = 0, at_it = 0;  // as bits
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-        over |= o[i] > border.over ? 1u << i : 0u;
+        kept |= o[i] > border.over ? 1u << i : 0u;
         at_it |= o[i] == border.over ? 1u << i : 0u;
     }
-    uint32_t all;
+    uint32_t first[kGroups], all, kept_low = 0;
     if (border.even != 0) {
-        uint32_t rank = before(__popc(at_it), all, sh, turn);
+        before_groups(at_it, first, all, kept_low, sh, turn);
 #pragma unroll
         for (int i = 0; i < kHeld; ++i)
-            if (at_it >> i & 1u) over |= rank++ < border.even ? 1u << i : 0u;
+            if (at_it >> i & 1u) kept |= first[i / 4]++ < border.even ? 1u << i : 0u;
     }
-    const uint32_t sources = over & ~low, targets = t.in & low & ~over;
-    const uint32_t first = before(__popc(sources) | __popc(targets) << 16, all, sh, turn);
-    const uint32_t total = all & 0xffffu;
-    uint32_t rs = first & 0xffffu, rt = first >> 16;
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-        if (sources >> i & 1u) {
-            if constexpr (MOVE) lists[0][rs++] = static_cast<uint16_t>(j0 + i);
-            else moves.from[pair * 2 * moves.most + rs++] = j0 + i;
-        }
-        if (targets >> i & 1u) {
-            if constexpr (MOVE) lists[1][rt++] = static_cast<uint16_t>(j0 + i);
-            else moves.from[(pair * 2 + 1) * moves.most + rt++] = j0 + i;
-        }
-    }
+    // With as many kept before it, a target is what lies before it less these, and a source these less those below the budget.
+    kept_low = __popc(kept & low);
+    before_groups(kept, first, all, kept_low, sh, turn);
+    const uint32_t total = keep - kept_low;
+    int32_t *out = MOVE ? nullptr : moves.from + pair * 2 * moves.most;
+    each_bit((kept & ~low) | (t.in & low & ~kept), [&](int i) {
+        const uint32_t j = static_cast<uint32_t>(Held<>::token(0, i)), before_it = kept_before(kept, first, i);
+        const bool target = (low >> i & 1u) != 0u;
+        const uint32_t to = target ? j - before_it : before_it - kept_low;
+        if constexpr (MOVE) lists[target ? 1 : 0][to] = static_cast<uint16_t>(j);
+        else out[(target ? moves.most : 0) + to] = static_cast<int32_t>(j);
+    });
     if constexpr (MOVE) {
         __syncthreads();
         constexpr int BATCH = batch_of(CHUNKS);
@@ -499,7 +544,7 @@ struct Counts {
     uint32_t low, high;                        // the two numbers, the same for all segments of a head
     uint32_t above, at_high, between, at_low;  // how many of the segment's are over `high`, at it, ...
     uint32_t fixed;
-    uint32_t pad;
+    uint32_t missing;                          // threads that met a page that is none
 };
 
 // The segments of a head: [0, keep) and [keep, n) in pieces of `size`, a
@@ -540,44 +585,48 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
     const Head x = head_of(a, pair);
     const Segments seg(x, size);
     const int w = static_cast<int>(blockIdx.y);
-    if (x.leave || w >= seg.all || x.keep == 0) return;
-    // One token of each of 4,096 equal pieces, at no regular distance; all of fewer.
-    constexpr int kAll = kSamples * kThreads, kLog2 = 12;
-    static_assert(kAll == 1 << kLog2, "pieces by shifts");
-    const bool whole = x.n <= kAll;
-    const int some = whole ? static_cast<int>(x.n) : kAll;
-    int which[kSamples];
-    uint32_t sample[kSamples], least = 0xffffffffu, largest = 0u, held = 0;
+    if (x.leave || w >= seg.all) return;
+    // Four tokens of each of 2,048 equal pieces, at no regular distance; all of as many.  (Neighbours may be alike: what
+    // they say is worth that of 2,048 tokens at least.)
+    constexpr int kLog2 = 11;
+    static_assert(kGroups * kThreads == 1 << kLog2, "pieces by shifts");
+    const bool whole = x.n <= kChunk;
+    int64_t which[kGroups];
 #pragma unroll
-    for (int r = 0; r < kSamples; ++r) {
-        const int i = r * kThreads + tid < some ? r * kThreads + tid : some - 1;
-        const int j0 = static_cast<int>(i * x.n >> kLog2), j1 = static_cast<int>((i + 1) * x.n >> kLog2);
-        const uint32_t mix = static_cast<uint32_t>(i) * 2654435761u;
-        which[r] = whole ? i : j0 + static_cast<int>(__umulhi(mix ^ mix >> 15, static_cast<uint32_t>(j1 - j0)));
+    for (int g = 0; g < kGroups; ++g) {
+        const uint32_t i = g * kThreads + tid, mix = i * 2654435761u;
+        const int64_t j0 = i * x.n >> kLog2, j1 = (i + 1) * x.n >> kLog2;
+        const int64_t j = j0 + __umulhi(mix ^ mix >> 15, static_cast<uint32_t>(j1 - j0));
+        which[g] = whole ? Held<>::token(0, 4 * g) : j & ~int64_t{3};
     }
-    x.numbers(a, which, sample);
+    uint32_t sample[kHeld], least = 0xffffffffu, largest = 0u, held = 0;  // held: with those protected ones << 16
+    {
+        Held<> t;
+        t.load(a, x, which, 0, x.n);
+        t.numbers(true, sample);
+        held = __popc(t.in & ~t.fixed) | __popc(t.fixed) << 16;
+    }
 #pragma unroll
-    for (int r = 0; r < kSamples; ++r) {
-        if (r * kThreads + tid >= some) sample[r] = 0u;
-        if (sample[r] == 0u || sample[r] == 0xffffffffu) continue;
-        least = min(least, sample[r]), largest = max(largest, sample[r]);
-        ++held;
+    for (int i = 0; i < kHeld; ++i) {
+        if (sample[i] == 0u || sample[i] == 0xffffffffu) continue;
+        least = min(least, sample[i]), largest = max(largest, sample[i]);
     }
     reduce(held, least, largest, sh, turn);
-    const int fixed_ones = some - static_cast<int>(held);
-    // Four standard deviations of the sample's count to either side.
-    const float share = static_cast<float>(x.keep) / static_cast<float>(x.n), rank = share * static_cast<float>(some);
-    const float off = whole ? 1.0f : 4.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
+    const int others = static_cast<int>(held & 0xffffu), fixed_ones = static_cast<int>(held >> 16);
+    // Six standard deviations of the sample's count to either side: three where neighbours are alike.
+    const float share = static_cast<float>(x.keep) / static_cast<float>(x.n);
+    const float rank = share * static_cast<float>(others + fixed_ones);
+    const float off = whole ? 1.0f : 6.0f * sqrtf(rank * (1.0f - share)) + 2.0f;
     const int first = static_cast<int>(rank - off) - fixed_ones, last = static_cast<int>(rank + off) + 1 - fixed_ones;
     uint32_t high = 0xfffffffeu, low = 0u;  // protected tokens are above, and no number is 0
-    if (held > 0) {
+    if (others > 0) {
         auto each = [&](auto count) {
 #pragma unroll
-            for (int r = 0; r < kSamples; ++r)
-                if (sample[r] != 0xffffffffu) count(sample[r]);
+            for (int i = 0; i < kHeld; ++i)
+                if (sample[i] != 0xffffffffu) count(sample[i]);
         };
         // The bins of both ranks; one that holds many is cut further (they may all be equal).
-        auto clamp = [&](int i) { return static_cast<uint32_t>(i < 1 ? 1 : i > static_cast<int>(held) ? static_cast<int>(held) : i); };
+        auto clamp = [&](int i) { return static_cast<uint32_t>(i < 1 ? 1 : i > others ? others : i); };
         Range r[2] = {range_of(least, largest, clamp(first)), range_of(least, largest, clamp(last))};
         narrow(r, each, sh, turn);
 #pragma unroll
@@ -588,24 +637,24 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
         }
         // A bin's numbers lie between; one number is a border itself.
         if (first >= 1) high = r[0].bits > 0 ? r[0].base + (1u << r[0].bits) : r[0].base;
-        if (last <= static_cast<int>(held)) low = r[1].bits > 0 ? r[1].base - 1u : r[1].base;
+        if (last <= others) low = r[1].bits > 0 ? r[1].base - 1u : r[1].base;
     }
-    uint32_t above = 0, at_high = 0, at_low = 0, fixed = 0, listed = 0;
+    uint32_t above = 0, at_high = 0, at_low = 0, fixed = 0, missing = 0, listed = 0;
     const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
     uint32_t *list = lists + pair * a.max_keys + begin;
     for (int64_t at = seg.start(w); at < end; at += kChunk) {
         Held<> t;
-        t.load(a, x, at + tid * kHeld, begin, end);
+        t.load_chunk(a, x, at, begin, end);
         uint32_t o[kHeld], set = 0, all;
         t.numbers(true, o);
         fixed += __popc(t.fixed);
+        missing |= t.missing ? 1u : 0u;
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            const bool in = (t.in >> i & 1u) != 0u;
-            above += in && o[i] > high ? 1u : 0u;
-            at_high += in && o[i] == high ? 1u : 0u;
-            at_low += in && o[i] == low && o[i] != high ? 1u : 0u;
-            set |= in && o[i] > low && o[i] < high ? 1u << i : 0u;
+        for (int i = 0; i < kHeld; ++i) {  // (0 is none)
+            above += o[i] > high ? 1u : 0u;
+            at_high += o[i] == high ? 1u : 0u;
+            at_low += o[i] == low && o[i] != high && o[i] != 0u ? 1u : 0u;
+            set |= o[i] > low && o[i] < high ? 1u << i : 0u;
         }
         uint32_t to = listed + before(__popc(set), all, sh, turn);
         listed += all;
@@ -618,6 +667,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
     before(at_high, c.at_high, sh, turn);
     before(at_low, c.at_low, sh, turn);
     before(fixed, c.fixed, sh, turn);
+    before(missing, c.missing, sh, turn);
     if (tid == 0) counts[pair * kMostSegments + w] = c;
 }
 
@@ -641,25 +691,29 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     clear(sh);
     const int64_t pair = pair_of();
     if (pair >= a.S * a.kv_heads) return;
-    const Head x = head_of(a, pair);
+    Head x = head_of(a, pair);
     const Segments seg(x, size);
     const int w = static_cast<int>(blockIdx.y);
-    if (x.h == 0 && w == 0 && tid == 0) put_len(a, x);
-    if (w == 0 && tid == 0 && (x.leave || x.keep == 0)) moves.count[pair] = 0;
-    if (w >= seg.all) return;
     const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
+    uint32_t above = 0, at_high = 0, between = 0, at_low = 0, fixed = 0, missing = 0;
+    if (!x.leave) {
+        if (tid < seg.all) held[tid] = counts[pair * kMostSegments + tid], over[tid] = even[tid] = 0;
+        __syncthreads();
+        for (int i = 0; i < seg.all; ++i) {
+            if (tid == 0) starts[i] = between;
+            above += held[i].above, at_high += held[i].at_high, between += held[i].between, at_low += held[i].at_low;
+            fixed += held[i].fixed, missing += held[i].missing;
+        }
+        x.leave = missing != 0u;
+    }
+    if (w == 0 && tid == 0) {
+        if (x.h == 0) put_len(a, x);
+        if (x.leave || x.keep == 0) moves.count[pair] = 0;
+    }
+    if (w >= seg.all) return;
     if (x.leave || x.keep == 0) {
         if (x.leave) carry_all(a, x, begin, end);
         return;
-    }
-    __syncthreads();
-    if (tid < seg.all) held[tid] = counts[pair * kMostSegments + tid], over[tid] = even[tid] = 0;
-    __syncthreads();
-    uint32_t above = 0, at_high = 0, between = 0, at_low = 0, fixed = 0;
-    for (int i = 0; i < seg.all; ++i) {
-        if (tid == 0) starts[i] = between;
-        above += held[i].above, at_high += held[i].at_high, between += held[i].between, at_low += held[i].at_low;
-        fixed += held[i].fixed;
     }
     if (tid == 0) starts[seg.all] = between;
     __syncthreads();
@@ -683,11 +737,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     } else if (few && keep > above + at_high && keep <= above + at_high + between) {
         // As many as the registers hold are read once, the others again and again.
         uint32_t o[kHeld];
+        int segment[kHeld];
         auto at = [&](int r) { return static_cast<uint32_t>((r * kWaves + wave) * kWave); };
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) segment[r] = at(r) < between ? segment_of(at(r)) : 0;
 #pragma unroll
         for (int r = 0; r < kHeld; ++r) {
             o[r] = 0u;
-            if (at(r) < between) o[r] = listed(at(r), segment_of(at(r)));
+            if (at(r) < between) o[r] = listed(at(r), segment[r]);
         }
         uint32_t least = 0xffffffffu, largest = 0u, sum = 0;
 #pragma unroll
@@ -727,7 +784,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
         };
 #pragma unroll
         for (int r = 0; r < kHeld; ++r)
-            if (at(r) < between) sort(o[r], segment_of(at(r)));
+            if (at(r) < between) sort(o[r], segment[r]);
         rest(sort);
     } else if (few && keep > above + at_high + between && keep <= above + at_high + between + at_low) {
         border = Border{low, keep - above - at_high - between};
@@ -737,13 +794,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
         }
     } else {  // the two numbers do not hold it, or more tokens are protected than stay
         auto all_of_them = [&](auto f) {
-            for (int64_t j = 4 * tid; j < x.n; j += 4 * kThreads) {
-                Held<4> t;
+            for (int64_t at = 4 * tid; at < x.n; at += kRow) {
+                Held<1> t;
+                const int64_t j[1] = {at};
                 t.load(a, x, j, 0, x.n);
                 uint32_t o[4];
                 t.numbers(few, o);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f(o[i], j + i);
+                for (int i = 0; i < 4; ++i) f(o[i], at + i);
             }
         };
         border = border_of(keep, 1u, 0xffffffffu, [&](auto count) { all_of_them([&](uint32_t o, int64_t) { count(o); }); }, sh, turn);
@@ -769,11 +827,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     int32_t *out = moves.from + (pair * 2 + (below ? 1 : 0)) * moves.most;
     uint32_t first_even = 0;
     for (int64_t at = seg.start(w); at < end; at += kChunk) {
-        const int64_t j0 = at + tid * kHeld;
         Held<> t;
-        t.load(a, x, j0, begin, end);
+        t.load_chunk(a, x, at, begin, end);
         if (below && carries(a) && t.in != 0u) t.carry(a, x, t.in);
-        uint32_t o[kHeld], kept = 0, at_it = 0, total;
+        uint32_t o[kHeld], kept = 0, at_it = 0, before_it[kGroups], total, none = 0;
         t.numbers(few, o);
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
@@ -781,19 +838,22 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
             at_it |= o[i] == border.over ? 1u << i : 0u;
         }
         at_it &= t.in;
-        uint32_t rank = first_even + before(__popc(at_it), total, sh, turn);
-        first_even += total;
+        if (border.even != 0) {
+            before_groups(at_it, before_it, total, none, sh, turn);
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (at_it >> i & 1u) kept |= rank++ < stays ? 1u << i : 0u;
-        const uint32_t set = below ? t.in & ~kept : kept;
-        uint32_t to = first + before(__popc(set), total, sh, turn);
-        first += total;
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (set >> i & 1u) out[to++] = static_cast<int32_t>(j0 + i);
+            for (int i = 0; i < kHeld; ++i)
+                if (at_it >> i & 1u) kept |= first_even + before_it[i / 4]++ < stays ? 1u << i : 0u;
+            first_even += total;
+        }
+        before_groups(kept, before_it, total, none, sh, turn);
+        // Below the budget, whose segments begin with a token of theirs, a target has before it what is not kept.
+        each_bit(below ? t.in & ~kept : kept, [&](int i) {
+            const int64_t j = Held<>::token(at, i);
+            const uint32_t k = kept_before(kept, before_it, i);
+            out[first + (below ? static_cast<uint32_t>(j - at) - k : k)] = static_cast<int32_t>(j);
+        });
+        first += below ? static_cast<uint32_t>((end - at < kChunk ? end - at : kChunk)) - total : total;
     }
-    __syncthreads();
 }
 
 struct Plan {
