@@ -60,7 +60,7 @@ knn_status check_evict(int64_t S, int64_t kv_heads, int64_t max_keys) {
     return KNN_OK;
 }
 
-constexpr int64_t kAdjustMaxWidth = int64_t{1} << 30;
+constexpr int64_t kAdjustMaxWidth = int64_t{1} << 28;  // (occurrences are counted in 30 bits)
 
 // The bytes from the first to the last of a buffer (null: none), in doubles: no sum of strides can pass them.
 struct Extent {
@@ -366,9 +366,10 @@ knn_status knn_adjust_scores(const void *scores, const int32_t *history, const i
     if ((bias_tokens != nullptr) != (bias_values != nullptr) || (bias_tokens != nullptr && bias_width < 1))
         return KNN_ERR_INVALID_ARG;
     const int size = dtype == KNN_F32 ? 4 : 2;
-    if (S > 0x7fffffff || (history != nullptr && history_width > kAdjustMaxWidth) ||
-        (bias_tokens != nullptr && bias_width > kAdjustMaxWidth) || (tree_mask != nullptr && mask_words > kAdjustMaxWidth) ||
-        !aligned(scores, size) || !aligned(out, size))
+    const int64_t most = kAdjustMaxWidth;
+    if (S > 0x7fffffff || (history != nullptr && history_width > most) || (bias_tokens != nullptr && bias_width > most) ||
+        (row_tokens != nullptr && rows > most) || (tree_mask != nullptr && mask_words > most) || !aligned(scores, size) ||
+        !aligned(out, size))
         return KNN_ERR_UNSUPPORTED;
     const bool in_place = out == scores && (rows == 1 || out_stride == row_stride);
     const Extent outputs[] = {dense(out, static_cast<double>(rows - 1) * out_stride + V, size)};
