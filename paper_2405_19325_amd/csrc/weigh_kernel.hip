@@ -165,20 +165,32 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                     __syncthreads();
                     stage<D, THREADS>(a, t, st, h, g, c0, n, padded);
                     __syncthreads();
-                    for (int tile = round + wave; tile < stop; tile += WAVES) {
-                        // The page of each 16 keys: block b's in lane b.
-                        const int block0 = tile * B;
-                        int32_t page = table[min(block0 + (lane & (B - 1)), last_block) << 4 >> a.cache.page_log2];
-                        const bool real = page >= 0 && page < a.cache.n_pages;
-                        page = real ? page : 0;
+                    // The pages of this wave's next tiles: block b of the i-th in lane i B + b, or -1.
+                    constexpr int AHEAD = kWave / B;
+                    int32_t pages = 0;
+                    for (int tile = round + wave, i = 0; tile < stop; tile += WAVES, ++i) {
+                        const int block0 = tile * B, first = i % AHEAD * B;
+                        if (first == 0) {
+                            const int block = (tile + lane / B * WAVES) * B + lane % B;
+                            pages = table[min(block, last_block) << 4 >> a.cache.page_log2];
+                            pages = pages >= 0 && pages < a.cache.n_pages ? pages : -1;
+                        }
+                        // Each quarter of the wave has a block's masses.
+                        const int j0 = tile * Sh::KEYS, j = j0 + 16 * (quad & (B - 1)) + col;
+                        const int32_t p = __shfl(pages, first + (quad & (B - 1)));
+                        const bool mine = quad < B && j < total_keys && p >= 0;
+                        const int64_t place = ((static_cast<int64_t>(p) * a.kv_heads + h) << a.cache.page_log2) + (j & in_page);
+                        float mass = 0.0f;
+                        if (mine && j < length && a.decay != 0.0f && c0 + most >= cols) mass = a.mass[place];
                         u32x4_t k[B][KK];
 #pragma unroll
                         for (int b = 0; b < B; ++b) {
-                            const int64_t p = static_cast<int64_t>(__builtin_amdgcn_readlane(page, b)) * a.kv_heads + h;
+                            const int32_t page = __builtin_amdgcn_readlane(pages, first + b);
+                            const int64_t at_page = static_cast<int64_t>(page < 0 ? 0 : page) * a.kv_heads + h;
                             const int slot = (min(block0 + b, last_block) << 4) & in_page;
                             // (of the last block, the places behind the last key are read as well, whatever they hold)
                             const u32x4_t *kp = reinterpret_cast<const u32x4_t *>(static_cast<const uint16_t *>(a.k_cache) +
-                                                                                  ((p << a.cache.page_log2) + slot) * D);
+                                                                                  ((at_page << a.cache.page_log2) + slot) * D);
 #pragma unroll
                             for (int kk = 0; kk < KK; ++kk) k[b][kk] = kp[col * (D / 8) + quad + 4 * kk];
                         }
@@ -195,7 +207,6 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                                 for (int b = 0; b < B; ++b) x[b] = mfma16<DT>(q[kk], k[b][kk], x[b]);
                         };
                         float w[B] = {};
-                        const int j0 = tile * Sh::KEYS;
                         bool plain = j0 + Sh::KEYS <= length;
                         if (plain) {
 #pragma unroll 1
@@ -242,17 +253,11 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                             sum[b] += __shfl_xor(sum[b], 16);
                             sum[b] += __shfl_xor(sum[b], 32);
                         }
-                        // Each quarter of the wave writes a block.
-                        const int32_t p = __shfl(page, quad & (B - 1));
-                        const bool there = __shfl(static_cast<int>(real), quad & (B - 1)) != 0;
-                        float mass = sum[0];
+                        float drawn = sum[0];
 #pragma unroll
-                        for (int b = 1; b < B; ++b) mass = quad == b ? sum[b] : mass;
-                        const int j = j0 + 16 * quad + col;
-                        if (quad >= B || j >= total_keys || !there) continue;
-                        const int64_t place = ((static_cast<int64_t>(p) * a.kv_heads + h) << a.cache.page_log2) + (j & in_page);
-                        if (j < length && a.decay != 0.0f) mass += a.decay * a.mass[place];
-                        a.mass[place] = mass;
+                        for (int b = 1; b < B; ++b) drawn = quad == b ? sum[b] : drawn;
+                        if (!mine) continue;
+                        a.mass[place] = drawn + a.decay * mass;
                         if (j >= length && a.key_positions != nullptr)
                             a.key_positions[place] = a.positions != nullptr ? a.positions[t.r0 + (j - length)] : j;
                     }
