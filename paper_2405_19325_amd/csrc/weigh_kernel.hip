@@ -267,6 +267,233 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
     }
 }
 
+// Four bytes a lane into LDS, lane l's at lds + 4 l (as load_to_lds_16).
+__device__ __forceinline__ void load_to_lds_4(const void *src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds));
+}
+
+constexpr int kRing = 4;          // stages of a wave
+constexpr int kStageBytes = 8192;  // of keys
+constexpr int kStageOps = 9;       // loads of a stage: 8 of keys, 1 of masses
+
+// Few columns, NT x 16 at most: the bytes of the keys are the bound.  Each wave
+// has a run of stages of its own, and their keys on the way to its ring in LDS
+// up to three stages ahead, a row's bytes by lanes side by side and past the
+// caches (a plain read of 4 KiB pieces in that order: 6.8 TB/s; in the order of
+// the instructions' registers 5.9).  The columns' queries stay in registers.
+template <knn_dtype DT, int D, int NT>
+__global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
+    constexpr int KK = D / 32, ROW = 2 * D, KEYS = kStageBytes / ROW, B = KEYS / 16;
+    constexpr int LANES = D / 8, PER = kWave / LANES;  // lanes of a row, rows of a load
+    __shared__ __align__(16) u32x4_t ring[4][kRing][kStageBytes / 16];
+    __shared__ float masses[4][kRing][kWave];
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int col = lane & 15, quad = lane >> 4;
+    const int g = a.q_heads / a.kv_heads;
+    const float c2 = a.scale * kLog2e;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_offset(ring[wave][0]));
+    const uint32_t masses_at = __builtin_amdgcn_readfirstlane(
+        static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) float *)masses[wave][0])));
+
+    // The stages of all sequences and heads lie one behind the other; this wave
+    // takes those that begin in its share.
+    const int64_t per = (a.S + kWave - 1) / kWave, s_lo = lane * per < a.S ? lane * per : a.S;
+    const int64_t s_hi = s_lo + per < a.S ? s_lo + per : a.S;
+    auto stages_of = [&](int64_t s) {
+        const Tile t = tile_of(a, s);
+        return t.n == 0 ? 0 : tiles_of(t.total, KEYS) * a.kv_heads;
+    };
+    int64_t mine = 0;
+    for (int64_t s = s_lo; s < s_hi; ++s) mine += stages_of(s);
+    int64_t upto = mine;
+#pragma unroll
+    for (int off = 1; off < kWave; off *= 2) {
+        const int64_t o = __shfl_up(upto, off);
+        if (lane >= off) upto += o;
+    }
+    // (the same in all lanes: kept in scalar registers)
+    auto uniform = [](int64_t x) {
+        return static_cast<int64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(x)))) |
+               static_cast<int64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32))) << 32;
+    };
+    const int64_t all = uniform(__shfl(upto, kWave - 1));
+    const int64_t waves = static_cast<int64_t>(gridDim.x) * 4, self = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    const int64_t from = all / waves * self + all % waves * self / waves;
+    const int64_t to = all / waves * (self + 1) + all % waves * (self + 1) / waves;
+    if (from >= to) return;
+    int64_t s = s_lo, base = upto - mine;
+    const bool has = from >= base && from < upto;  // (one lane)
+    if (has)
+        for (; s < s_hi; ++s) {
+            const int64_t n = stages_of(s);
+            if (from < base + n) break;
+            base += n;
+        }
+    const int owner = __ffsll(static_cast<unsigned long long>(__ballot(has))) - 1;
+    s = uniform(__shfl(s, owner)), base = uniform(__shfl(base, owner));
+
+    for (; s < a.S && base < to; ++s) {
+        const Tile t = tile_of(a, s);
+        if (t.n == 0) continue;
+        const int64_t stages = uniform(tiles_of(t.total, KEYS)), each = stages * a.kv_heads;
+        const int64_t first = from > base ? from - base : 0, last = to - base < each ? to - base : each;
+        base += each;
+        const int cols = t.n * g, total_keys = static_cast<int>(t.total), last_block = (total_keys - 1) >> 4;
+        const int length = static_cast<int>(t.length < t.total ? t.length : t.total);
+        const int in_page = (1 << a.cache.page_log2) - 1;
+        const int32_t *table = a.cache.pages + s * a.cache.table_width;
+        for (int64_t at = first; at < last;) {
+            const int h = static_cast<int>(uniform(at / stages));
+            const int st0 = static_cast<int>(at - h * stages);
+            const int n = static_cast<int>((last - h * stages < stages ? last - h * stages : stages) - st0);
+            at += n;
+            auto page_of = [&](int block) {
+                const int32_t page = load_scalar_i32(table + ((min(block, last_block) << 4) >> a.cache.page_log2));
+                return page >= 0 && page < a.cache.n_pages ? page : -1;
+            };
+            // Stage i of the run into its place of the ring.
+            auto fill = [&](int i) {
+                const uint32_t lds = ring_at + static_cast<uint32_t>(i % kRing) * kStageBytes;
+                int64_t mass_at = 0;
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    const int block = (st0 + i) * B + b, page = page_of(block);
+                    const int64_t at_page = static_cast<int64_t>(page < 0 ? 0 : page) * a.kv_heads + h;
+                    // (of the last block, the places behind the last key are read as well, whatever they hold)
+                    const int64_t place = (at_page << a.cache.page_log2) + ((min(block, last_block) << 4) & in_page);
+                    const char *from_block = static_cast<const char *>(a.k_cache) + place * ROW;
+#pragma unroll
+                    for (int j = 0; j < 16 / PER; ++j) {
+                        const int r = j * PER + lane / LANES;
+                        load_to_lds_16_nt(from_block, r * ROW + 16 * ((lane % LANES) ^ spread<D>(r)),
+                                          lds + b * 16 * ROW + j * 1024);
+                    }
+                    if (b == 0 || quad == b) mass_at = place;
+                }
+                load_to_lds_4(a.mass + mass_at + col, masses_at + static_cast<uint32_t>(i % kRing) * (4 * kWave));
+            };
+#pragma unroll
+            for (int i = 0; i < kRing - 1; ++i)
+                if (i < n) fill(i);
+            // The columns: lane = (column, 8 elements a quad) of the queries, four columns of the sums.
+            u32x4_t q[NT][KK];
+            f32x4_t lse2[NT];
+            auto source_of = [&](int c) -> int64_t {
+                if (c >= cols) return -1;
+                const int64_t row = t.r0 + c / g, source = a.source_rows != nullptr ? a.source_rows[row] : row;
+                return source < a.source_count ? source : -1;
+            };
+#pragma unroll
+            for (int m = 0; m < NT; ++m) {
+                if (16 * m >= cols) break;
+                const int c = 16 * m + col;
+                const int64_t source = source_of(c);
+                const uint16_t *from_q = static_cast<const uint16_t *>(a.q) + (source < 0 ? 0 : source) * a.q_row +
+                                         (h * g + (c < cols ? c % g : 0)) * a.q_head;
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    q[m][kk] = *reinterpret_cast<const u32x4_t *>(from_q + 32 * kk + 8 * quad);
+                    if (source < 0) q[m][kk] = u32x4_t{0, 0, 0, 0};
+                }
+                const float l = source < 0 ? INFINITY : a.lse[source * a.q_heads + h * g + c % g];
+                const float l2 = isfinite(l) ? l * kLog2e : INFINITY;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) lse2[m][r] = __shfl(l2, 4 * quad + r);
+            }
+
+            for (int i = 0; i < n; ++i) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage that is filled next has been read
+                if (i + kRing - 1 < n) {
+                    fill(i + kRing - 1);
+                    // This stage's loads are done when no more are under way than those of the later ones.
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kRing - 1) * kStageOps) : "memory");
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                }
+                const uint32_t lds = ring_at + static_cast<uint32_t>(i % kRing) * kStageBytes;
+                const int j0 = (st0 + i) * KEYS;
+                float w[B];
+                auto key = [&](int b, int kk) {
+                    return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t *>(
+                        static_cast<uintptr_t>(lds + (16 * b + col) * ROW + 16 * ((4 * kk + quad) ^ spread<D>(col))));
+                };
+                bool plain = j0 + KEYS <= length;
+                if (plain) {
+                    bool odd = false;
+#pragma unroll
+                    for (int b = 0; b < B; ++b) {
+                        u32x4_t k[KK];
+#pragma unroll
+                        for (int kk = 0; kk < KK; ++kk) k[kk] = key(b, kk);
+                        w[b] = 0.0f;
+#pragma unroll
+                        for (int m = 0; m < NT; ++m) {
+                            if (16 * m >= cols) break;
+                            f32x4_t x{0, 0, 0, 0};
+#pragma unroll
+                            for (int kk = 0; kk < KK; ++kk) x = mfma16<DT>(q[m][kk], k[kk], x);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) w[b] += __builtin_amdgcn_exp2f(fmaf(x[r], c2, -lse2[m][r]));
+                        }
+                        odd = odd || w[b] != w[b];
+                    }
+                    // Keys that are not finite: whose they are is looked at column by column.
+                    plain = !__any(odd);
+                }
+                if (!plain) {
+#pragma unroll
+                    for (int b = 0; b < B; ++b) {
+                        const int draft = j0 + 16 * b + col - length;
+                        w[b] = 0.0f;
+#pragma unroll
+                        for (int m = 0; m < NT; ++m) {
+                            if (16 * m >= cols) break;
+                            f32x4_t x{0, 0, 0, 0};
+#pragma unroll
+                            for (int kk = 0; kk < KK; ++kk) x = mfma16<DT>(q[m][kk], key(b, kk), x);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int row = lse2[m][r] < INFINITY ? (16 * m + 4 * quad + r) / g : kNobody;
+                                const float e = __builtin_amdgcn_exp2f(fmaf(x[r], c2, -lse2[m][r]));
+                                w[b] += sees(a, t, row, draft) ? e : 0.0f;
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    w[b] += __shfl_xor(w[b], 16);
+                    w[b] += __shfl_xor(w[b], 32);
+                }
+                // Each quarter of the wave writes a block.
+                float drawn = w[0];
+                int page = page_of((st0 + i) * B);
+#pragma unroll
+                for (int b = 1; b < B; ++b) {
+                    const int other = page_of((st0 + i) * B + b);
+                    drawn = quad == b ? w[b] : drawn, page = quad == b ? other : page;
+                }
+                const float mass = masses[wave][i % kRing][lane];
+                const int j = j0 + 16 * quad + col;
+                if (quad < B && j < total_keys && page >= 0) {
+                    const int64_t place = ((static_cast<int64_t>(page) * a.kv_heads + h) << a.cache.page_log2) + (j & in_page);
+                    a.mass[place] = drawn + (j < length && a.decay != 0.0f ? a.decay * mass : 0.0f);
+                    if (j >= length && a.key_positions != nullptr)
+                        a.key_positions[place] = a.positions != nullptr ? a.positions[t.r0 + (j - length)] : j;
+                }
+            }
+        }
+    }
+}
+
+template <knn_dtype DT, int D, int NT>
+void launch_few(const WeighArgs &a, hipStream_t stream) {
+    const int64_t stages = a.S * a.kv_heads * tiles_of(a.max_keys, kStageBytes / (2 * D));
+    const int64_t blocks = (stages + 3) / 4 < kCus ? (stages + 3) / 4 : kCus;
+    k_key_weights_few<DT, D, NT><<<dim3(static_cast<unsigned>(blocks)), 4 * kWave, 0, stream>>>(a);
+}
+
 template <knn_dtype DT, int D, int WAVES>
 void launch(const WeighArgs &a, int most, hipStream_t stream) {
     using Sh = Shape<D>;
@@ -284,7 +511,10 @@ template <knn_dtype DT, int D>
 hipError_t launch(const WeighArgs &a, hipStream_t stream) {
     const int64_t cols = (a.max_rows * (a.q_heads / a.kv_heads) + 15) / 16 * 16;
     const int most = static_cast<int>(cols < Shape<D>::MOST ? cols : Shape<D>::MOST);
-    if (most * 4 <= Shape<D>::MOST) launch<DT, D, 4>(a, most, stream);
+    if (most <= 16) launch_few<DT, D, 1>(a, stream);
+    else if (most <= 32) launch_few<DT, D, 2>(a, stream);
+    else if (most <= 80) launch_few<DT, D, 5>(a, stream);
+    else if (most * 4 <= Shape<D>::MOST) launch<DT, D, 4>(a, most, stream);
     else if (most * 2 <= Shape<D>::MOST) launch<DT, D, 8>(a, most, stream);
     else launch<DT, D, 16>(a, most, stream);
     return hipGetLastError();
