@@ -8,11 +8,19 @@
 // The rows and query heads of a key head are the columns of S = Q K^T on the
 // matrix cores: 16 columns x 16 keys an instruction, with the keys as its right
 // operand, so that a lane holds 4 columns of one key and the sum over columns
-// stays within it until the end of a tile.  A wave holds 64 keys (32 of
-// head_dim 256) in the registers that the instructions read, straight from
-// memory; the queries of the sequence's rows lie in LDS, read by all waves of
-// the workgroup.  So keys are read once, by a wave each, and waves wait for
-// each other only where a workgroup goes on to another head.
+// stays within it until the end of a tile.  Weights are worked out as 2^(x c -
+// lse c'), whose rounding is that of lse itself, and summed in 32 bits.
+//
+// What bounds it.  Up to 96 columns a key head (decoding, accepted paths): the
+// bytes of the keys.  Each wave has a run of keys of its own, which come through
+// LDS; 64 ragged sequences of 2,000 to 16,000 tokens, 8 key heads: 228 us for 1.22
+// GB, 5.3 TB/s (189 without the masses, whose scattered writes of 64 bytes cost
+// more than their share).  More columns: the exponential's 16 clocks and the 8 of
+// a multiplication and a sum for 64 weights, beside 16 of the matrix cores.  A
+// wave holds 64 keys in the registers that the instructions read, straight from
+// memory, and the queries lie in LDS, read by all waves of the workgroup; 64 rows
+// of 64 heads on 8 on 4 x 131,008 tokens: 575 us, 970 TFLOP/s (a large library
+// product: 1,190).
 #include "lm_device.h"
 #include "mfma_device.h"
 
@@ -386,7 +394,7 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
             };
 #pragma unroll
             for (int m = 0; m < NT; ++m) {
-                if (16 * m >= cols) break;
+                if (NT > 1 && 32 * (m / 2) >= cols) break;  // (in pairs: zeros where the second one has no column)
                 const int c = 16 * m + col;
                 const int64_t source = source_of(c);
                 const uint16_t *from_q = static_cast<const uint16_t *>(a.q) + (source < 0 ? 0 : source) * a.q_row +
@@ -420,24 +428,42 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
                 };
                 bool plain = j0 + KEYS <= length;
                 if (plain) {
+                    // Two column tiles and all blocks at a time: as many chains of matrix instructions beside each other.
+                    constexpr int M = NT > 1 ? 2 : 1;
+                    u32x4_t k[B][KK];
                     bool odd = false;
 #pragma unroll
                     for (int b = 0; b < B; ++b) {
-                        u32x4_t k[KK];
-#pragma unroll
-                        for (int kk = 0; kk < KK; ++kk) k[kk] = key(b, kk);
                         w[b] = 0.0f;
 #pragma unroll
-                        for (int m = 0; m < NT; ++m) {
-                            if (16 * m >= cols) break;
-                            f32x4_t x{0, 0, 0, 0};
-#pragma unroll
-                            for (int kk = 0; kk < KK; ++kk) x = mfma16<DT>(q[m][kk], k[kk], x);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) w[b] += __builtin_amdgcn_exp2f(fmaf(x[r], c2, -lse2[m][r]));
-                        }
-                        odd = odd || w[b] != w[b];
+                        for (int kk = 0; kk < KK; ++kk) k[b][kk] = key(b, kk);
                     }
+#pragma unroll
+                    for (int m0 = 0; m0 < NT; m0 += M) {
+                        if (16 * m0 >= cols) break;
+                        f32x4_t x[M][B];
+#pragma unroll
+                        for (int m = 0; m < M; ++m)
+#pragma unroll
+                            for (int b = 0; b < B; ++b) x[m][b] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+                        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+                            for (int m = 0; m < M; ++m)
+#pragma unroll
+                                for (int b = 0; b < B; ++b) x[m][b] = mfma16<DT>(q[m0 + m][kk], k[b][kk], x[m][b]);
+#pragma unroll
+                        for (int m = 0; m < M; ++m)
+#pragma unroll
+                            for (int b = 0; b < B; ++b) {
+                                float e[4];
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(x[m][b][r], c2, -lse2[m0 + m][r]));
+                                w[b] += (e[0] + e[1]) + (e[2] + e[3]);
+                            }
+                    }
+#pragma unroll
+                    for (int b = 0; b < B; ++b) odd = odd || w[b] != w[b];
                     // Keys that are not finite: whose they are is looked at column by column.
                     plain = !__any(odd);
                 }
@@ -478,7 +504,9 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
                 const int j = j0 + 16 * quad + col;
                 if (quad < B && j < total_keys && page >= 0) {
                     const int64_t place = ((static_cast<int64_t>(page) * a.kv_heads + h) << a.cache.page_log2) + (j & in_page);
-                    a.mass[place] = drawn + (j < length && a.decay != 0.0f ? a.decay * mass : 0.0f);
+                    // (written through, as an agent's: paths over 8 x 100,000 tokens 334 us, 346 by way of the caches' write-back)
+                    __hip_atomic_store(a.mass + place, drawn + (j < length && a.decay != 0.0f ? a.decay * mass : 0.0f),
+                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                     if (j >= length && a.key_positions != nullptr)
                         a.key_positions[place] = a.positions != nullptr ? a.positions[t.r0 + (j - length)] : j;
                 }
@@ -500,7 +528,6 @@ void launch(const WeighArgs &a, int most, hipStream_t stream) {
     const size_t lds = static_cast<size_t>(most) * (Sh::ROW + 8);
     const size_t fit = (size_t{156} << 10) / (lds + 1024);
     const int64_t room = fit * WAVES > 16 ? 16 / WAVES : fit < 1 ? 1 : static_cast<int64_t>(fit);  // workgroups of a CU
-    // (a sequence has max_rows rows at most, and there are `rows`)
     const int64_t tiles = a.S * a.kv_heads * tiles_of(a.max_keys, Sh::KEYS);
     int64_t blocks = (tiles + WAVES - 1) / WAVES;
     if (blocks > kCus * room) blocks = kCus * room;
@@ -511,9 +538,13 @@ template <knn_dtype DT, int D>
 hipError_t launch(const WeighArgs &a, hipStream_t stream) {
     const int64_t cols = (a.max_rows * (a.q_heads / a.kv_heads) + 15) / 16 * 16;
     const int most = static_cast<int>(cols < Shape<D>::MOST ? cols : Shape<D>::MOST);
+    // Waves of their own while the columns' queries fit the registers; measured on 4 x 65,536 tokens, 64 heads on 8: 8
+    // columns 96 us, 117 the other way; 96 columns 117 and 128; at head_dim 256 183 and 210, 195 and 221; at 64, where a
+    // column tile does half the work for the same exponentials, 55 and 62, but 75 and 65 at 48 columns.
     if (most <= 16) launch_few<DT, D, 1>(a, stream);
     else if (most <= 32) launch_few<DT, D, 2>(a, stream);
-    else if (most <= 80) launch_few<DT, D, 5>(a, stream);
+    else if (D > 64 && most <= 96) launch_few<DT, (D > 64 ? D : 128), 6>(a, stream);
+    // Four waves a workgroup while four of these fit a CU's LDS with their queries; else eight, or all sixteen.
     else if (most * 4 <= Shape<D>::MOST) launch<DT, D, 4>(a, most, stream);
     else if (most * 2 <= Shape<D>::MOST) launch<DT, D, 8>(a, most, stream);
     else launch<DT, D, 16>(a, most, stream);

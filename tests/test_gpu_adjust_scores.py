@@ -283,3 +283,35 @@ def test_argument_checks():
         knn.adjust_scores(c["scores"], repetition=c["repetition"])
     with pytest.raises(knn.KnnError):
         knn.adjust_scores(c["scores"], out=c["scores"].view(-1).as_strided((4, 100), (50, 1)))
+
+
+@pytest.mark.parametrize("V,rows", [(2048, 2), (2047, 1), (8192, 200), (8190, 200)])
+@pytest.mark.parametrize("probs", [False, True])
+def test_every_token_is_touched(V, rows, probs):
+    """A whole slice's tokens in the history, of either kind of workgroup, and with biases besides."""
+    c = batch(rows, V, probs=probs, seed=13, width=V + 5, bias=4)
+    c["history"][:, :V] = torch.arange(V, dtype=torch.int32).flip(0)
+    c["history_lens"][:] = V
+    c["bias_tokens"][:, 0] = V - 1
+    check(c)
+
+
+def test_histories_longer_than_a_pass_and_many_drafts():
+    c = batch(1200, 300, "bf16", drafts=[1000, 200], seed=14, width=9000)
+    c["history_lens"][:] = torch.tensor([9000, 8193], dtype=torch.int32)
+    c["prompt_lens"][:] = torch.tensor([8500, 8192], dtype=torch.int32)
+    c["frequency"][:] = 2.0 ** -10
+    want, got = want_of(c), host(knn.adjust_scores(**c))
+    # half a step of bf16, and before it the fp32 steps' roundings of numbers under 64
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -16).all()
+
+
+def test_on_another_stream():
+    c = batch(20, 5000, "bf16", seed=15, bias=6, grammar=True)
+    want = knn.adjust_scores(**c)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    call = knn.ScoreAdjuster(**c)
+    call.run(side)
+    side.synchronize()
+    assert torch.equal(call.out, want)

@@ -68,7 +68,7 @@ def check(x, budgets, next_positions=None, sinks=0, recent=0, max_keys=None, out
     if positions:
         assert np.array_equal(ints(outs.get("positions_out", x["key_positions"])), want[3])
     for n in ("pages", "cache_lens") + (("mass", "key_positions") if out and positions else ()):
-        assert torch.equal(before[n], x[n])
+        assert np.array_equal(bits(before[n]), bits(x[n]))
     return got
 
 
@@ -213,3 +213,99 @@ def test_argument_checks():
     for over in (dict(sinks=-1), dict(v_cache=x["k_cache"]), dict(max_keys=1 << 20), dict(max_keys=0)):
         with pytest.raises(knn.KnnError):
             knn.cache_evict(**dict(args, **over))
+
+
+LONG = [20000, 9000, 5, 0, 8193, 12345]
+
+
+def shaped(x, kind, n):
+    """Masses of all places in some shape that samples may misjudge."""
+    g = torch.Generator().manual_seed(n)
+    m = x["mass"].cpu()
+    if kind == "equal":
+        m[:] = 0.3
+    elif kind == "zero but few":
+        m[:] = torch.where(torch.rand(m.shape, generator=g) < 0.01, torch.rand(m.shape, generator=g), torch.zeros(1))
+    elif kind == "by pages":  # neighbours are alike
+        m[:] = torch.rand((m.shape[0], 1, 1), generator=g)
+    elif kind == "two":
+        m[:] = torch.where(torch.rand(m.shape, generator=g) < 0.3, 1.0, 1.0 + 2.0 ** -23)
+    elif kind == "narrow":
+        m[:] = 1.0 + torch.rand(m.shape, generator=g) * 2.0 ** -12
+    elif kind == "wide":
+        m[:] = torch.exp(torch.randn(m.shape, generator=g) * 25)
+    elif kind == "signed":
+        m[:] = torch.randn(m.shape, generator=g) * 10.0 ** torch.randint(-30, 30, m.shape, generator=g)
+    elif kind == "one outlier":
+        m[:] = 1e-3 * torch.rand(m.shape, generator=g)
+        m[0] = 3e38
+    elif kind == "nan":
+        m[:] = torch.where(torch.rand(m.shape, generator=g) < 0.6, float("nan"), 1.0)
+    x["mass"] = m.cuda()
+    return x
+
+
+@pytest.mark.parametrize("kind", ["equal", "zero but few", "by pages", "two", "narrow", "wide", "signed", "one outlier", "nan",
+                                  "spread"])
+def test_long_heads_of_any_shape(kind):
+    for budgets in ([2500, 8000, 4, 0, 8192, 12344], [19999, 1, 0, 0, 1, 6000]):
+        check(shaped(batch(LONG, 1, 64, 64, seed=8), kind, budgets[0]), budgets, [10 * n for n in LONG], sinks=4, recent=64,
+              out=budgets[1] == 1)
+    check(shaped(batch([8192, 100, 4097, 33], 2, 64, 16, seed=9), kind, 5), [4096, 50, 4096, 32], sinks=3, recent=9,
+          positions=False)
+
+
+def test_long_heads_with_more_protected_tokens_than_the_budget():
+    x = batch(LONG, 1, 64, 64, seed=10)
+    check({n: t.clone() for n, t in x.items()}, [2500, 800, 4, 0, 100, 12344], sinks=1500, recent=1200, positions=False)
+    check(x, [2500, 800, 4, 0, 100, 12344], [10 * n for n in LONG], sinks=30000, recent=40000, out=True)
+
+
+def test_long_heads_that_are_left_as_they_are():
+    x = batch(LONG, 2, 64, 16, width=1300, seed=11)
+    x["pages"][0, 700] = -1
+    x["pages"][1, 3] = x["k_cache"].shape[0]
+    x["cache_lens"][5] = 1300 * 16 + 1
+    for out in (False, True):
+        for budgets in ([100, 0, -1, 0, 100, 7], [0, 8999, 5, 3, 8193, 0]):
+            check({n: t.clone() for n, t in x.items()}, budgets, out=out, max_keys=20800)
+
+
+def test_ledgers_off_16_bytes_and_caches_off_them():
+    for lens, budgets in (([100, 333, 16], [50, 332, 1]), ([9000, 50], [3000, 20])):
+        x = batch(lens, 2, 64, 16, seed=12)
+        for n in ("mass", "key_positions"):
+            wide = torch.zeros(x[n].numel() + 1, dtype=x[n].dtype, device="cuda")
+            wide[1:] = x[n].flatten()
+            x[n] = wide[1:].view(x[n].shape)
+        for n in ("k_cache", "v_cache"):
+            wide = torch.zeros(x[n].numel() + 1, dtype=x[n].dtype, device="cuda")
+            wide[1:] = x[n].flatten()
+            x[n] = wide[1:].view(x[n].shape)
+        check({n: t.clone() if t.data_ptr() % 16 == 0 else t for n, t in x.items()}, budgets, sinks=2, recent=5)
+
+
+def test_many_short_heads():
+    n = np.random.RandomState(5).randint(0, 60, 300).tolist()
+    check(batch(n, 3, 64, 16, seed=13), [max(0, v - 3) for v in n], sinks=1, recent=2, positions=False)
+
+
+def test_on_another_stream_and_two_calls_at_once():
+    a, b = (batch([9000, 700], 2, 64, 64, seed=s) for s in (14, 15))
+    want = []
+    for x in (a, b):
+        y = {n: t.clone() for n, t in x.items()}
+        check(y, [4000, 600])
+        want.append(y)
+    budgets = torch.tensor([4000, 600], dtype=torch.int32).cuda()
+    calls = [knn.CacheEvict(x["k_cache"], x["v_cache"], x["mass"], x["pages"], x["cache_lens"], budgets, 9000,
+                            key_positions=x["key_positions"]) for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in calls]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for c, s in zip(calls, streams):
+        c.run(s)
+    torch.cuda.synchronize()
+    for x, y in zip((a, b), want):
+        for n in ("k_cache", "v_cache", "mass", "key_positions"):
+            assert torch.equal(x[n], y[n])

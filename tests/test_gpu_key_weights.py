@@ -284,3 +284,57 @@ def test_argument_checks():
             knn.key_weights(**dict(args, **over))
     with pytest.raises(knn.KnnError):
         knn.key_weights(**dict(args, decay=-1.0))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_column_counts_of_every_kernel(dtype, d):
+    """1 to 16, 32, 96 columns by waves of their own, then four, eight and sixteen waves a workgroup; more columns than LDS
+    holds in rounds."""
+    for rows, heads in (([2, 5], (8, 2)), ([4, 1], (16, 2)), ([12, 7], (16, 2)), ([13], (16, 2)), ([31, 2], (8, 2)),
+                        ([50, 9], (16, 2)), ([70, 3], (16, 2)), ([150], (16, 2))):
+        check(batch(dtype, rows, [300, 77][:len(rows)], heads, d, 32, seed=d + rows[0]), decay=0.5)
+
+
+def test_many_sequences():
+    """More than a wave's lanes and than a workgroup's threads, some without rows or tokens."""
+    g = np.random.RandomState(3)
+    for n, rows in ((150, 2), (700, 1), (300, 20)):
+        lens = g.randint(0, 40, n).tolist()
+        rows_of = g.randint(0, rows + 1, n).tolist()
+        rows_of[-1] = rows
+        check(batch("bf16", rows_of, lens, (8, 2), 64, 16, seed=n))
+
+
+def test_keys_that_are_not_finite_and_seen():
+    """An infinite element of a cached key: its own mass is no number, every other key's is as it would be."""
+    for rows, heads in (([1, 2], (4, 2)), ([40, 3], (16, 2))):
+        x = batch("bf16", rows, [100, 60], heads, 64, 16, seed=20)
+        want, _, tol = want_of(x)
+        at = (int(x["pages"][0, 3]), 1, 5)  # cache index 53 of the first sequence
+        x["k_cache"][at] = float("nan")
+        knn.key_weights(x["q"], x["lse"], x["k_cache"], x["pages"], x["row_offsets"], x["cache_lens"], x["mass"])
+        got = host(x["mass"])
+        assert np.isnan(got[at])
+        want[at] = got[at] = 0.0
+        assert (np.abs(got - want) <= tol).all()
+
+
+def test_nobody_adds_to_keys_that_are_not_finite():
+    """Rows whose sums are not finite add nothing, also to keys that are not."""
+    for rows, heads in (([1, 2], (4, 2)), ([40, 3], (16, 2))):
+        x = batch("f16", rows, [100, 60], heads, 64, 16, seed=21)
+        x["lse"][:] = float("-inf")
+        x["k_cache"][:] = float("inf")
+        check(x, decay=0.5)
+
+
+def test_on_another_stream():
+    x = batch("bf16", [2, 5], [400, 100], (8, 2), 128, 16, seed=22)
+    want, _, tol = want_of(x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call = knn.KeyWeights(x["q"], x["lse"], x["k_cache"], x["pages"], x["row_offsets"], x["cache_lens"], x["mass"])
+    call.run(side)
+    side.synchronize()
+    assert (np.abs(host(x["mass"]) - want) <= tol).all()
