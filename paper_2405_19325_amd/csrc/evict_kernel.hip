@@ -78,6 +78,18 @@ __device__ __forceinline__ uint32_t before(uint32_t v, uint32_t &all, Shared &sh
     return first;
 }
 
+// The workgroup's sums of three.
+__device__ __forceinline__ void sums(uint32_t &a, uint32_t &b, uint32_t &c, Shared &sh, int &turn) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1), wave = static_cast<int>(threadIdx.x) / kWave;
+    a = wave_incl_scan_u32(a, lane), b = wave_incl_scan_u32(b, lane), c = wave_incl_scan_u32(c, lane);
+    turn ^= 1;
+    if (lane == kWave - 1) sh.part[turn][0][wave] = a, sh.part[turn][1][wave] = b, sh.part[turn][2][wave] = c;
+    __syncthreads();
+    a = b = c = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) a += sh.part[turn][0][w], b += sh.part[turn][1][w], c += sh.part[turn][2][w];
+}
+
 // For tokens held as Held has them: how many of `set` (bits) come before each of
 // this thread's groups, and all; the workgroup's sum of `more`.
 __device__ __forceinline__ void before_groups(uint32_t set, uint32_t (&first)[kGroups], uint32_t &all, uint32_t &more, Shared &sh,
@@ -287,7 +299,7 @@ struct Held {
     };
 
     __device__ __forceinline__ void load(const EvictArgs &a, const Head &x, const int64_t (&j)[G], int64_t from, int64_t to) {
-        in = fixed = 0;
+        in = 0;
         missing = false;
         bool some[G];
 #pragma unroll
@@ -314,11 +326,15 @@ struct Held {
                 }
             }
         }
+        if (a.key_positions != nullptr) return;
 #pragma unroll
-        for (int i = 0; i < 4 * G; ++i) {
-            if (a.key_positions == nullptr) p[i] = static_cast<int32_t>(j[i / 4]) + i % 4;
-            fixed |= x.fixed(a, p[i]) ? 1u << i : 0u;
-        }
+        for (int i = 0; i < 4 * G; ++i) p[i] = static_cast<int32_t>(j[i / 4]) + i % 4;
+    }
+    // What was loaded is looked at: apart, so that other loads may follow before it has come.
+    __device__ __forceinline__ void look(const EvictArgs &a, const Head &x) {
+        fixed = 0;
+#pragma unroll
+        for (int i = 0; i < 4 * G; ++i) fixed |= x.fixed(a, p[i]) ? 1u << i : 0u;
         fixed &= in;
     }
     // This thread's part of kChunk tokens from j0 on.
@@ -458,6 +474,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_held(EvictArgs a, Moves m
     const int n = static_cast<int>(x.n), keep = static_cast<int>(x.keep);
     Held<> t;
     t.load_chunk(a, x, 0, 0, x.leave ? 0 : n);  // every page is some thread's
+    t.look(a, x);
     const uint32_t low = below_of(0, keep);
     if (carries(a) && (t.in & low) != 0u) t.carry(a, x, t.in & low);
     uint32_t o[kHeld], least = 0xffffffffu, largest = 0u;
@@ -607,12 +624,16 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
         const int64_t j = j0 + __umulhi(mix ^ mix >> 15, static_cast<uint32_t>(j1 - j0));
         which[g] = whole ? Held<>::token(0, 4 * g) : j & ~int64_t{3};
     }
+    const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
+    Held<> t;  // the segment's own tokens, on their way together with the sample
+    t.load_chunk(a, x, seg.start(w), begin, end);
     uint32_t sample[kHeld], least = 0xffffffffu, largest = 0u, held = 0;  // held: with those protected ones << 16
     {
-        Held<> t;
-        t.load(a, x, which, 0, x.n);
-        t.numbers(true, sample);
-        held = __popc(t.in & ~t.fixed) | __popc(t.fixed) << 16;
+        Held<> some;
+        some.load(a, x, which, 0, x.n);
+        some.look(a, x);
+        some.numbers(true, sample);
+        held = __popc(some.in & ~some.fixed) | __popc(some.fixed) << 16;
     }
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
@@ -648,11 +669,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
         if (last <= others) low = r[1].bits > 0 ? r[1].base - 1u : r[1].base;
     }
     uint32_t above = 0, at_high = 0, at_low = 0, fixed = 0, missing = 0, listed = 0;
-    const int64_t begin = seg.begin(x, w), end = seg.end(x, w);
     uint32_t *list = lists + pair * a.max_keys + begin;
     for (int64_t at = seg.start(w); at < end; at += kChunk) {
-        Held<> t;
-        t.load_chunk(a, x, at, begin, end);
+        if (at != seg.start(w)) t.load_chunk(a, x, at, begin, end);
+        t.look(a, x);
         uint32_t o[kHeld], set = 0, all;
         t.numbers(true, o);
         fixed += __popc(t.fixed);
@@ -670,12 +690,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_count(EvictArgs a, Counts
         for (int i = 0; i < kHeld; ++i)
             if (set >> i & 1u) list[to++] = o[i];
     }
-    Counts c{low, high, 0, 0, listed, 0, 0, 0};
-    before(above, c.above, sh, turn);
-    before(at_high, c.at_high, sh, turn);
-    before(at_low, c.at_low, sh, turn);
-    before(fixed, c.fixed, sh, turn);
-    before(missing, c.missing, sh, turn);
+    Counts c{low, high, 0, 0, listed, 0, 0, 0};  // (all threads have the same `listed`)
+    sums(above, at_high, at_low, sh, turn);
+    sums(fixed, missing, listed, sh, turn);
+    c.above = above, c.at_high = at_high, c.at_low = at_low, c.fixed = fixed, c.missing = missing;
     if (tid == 0) counts[pair * kMostSegments + w] = c;
 }
 
@@ -724,6 +742,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
         return;
     }
     if (tid == 0) starts[seg.all] = between;
+    Held<> t;  // the segment's own tokens, on their way while the border is looked for
+    t.load_chunk(a, x, seg.start(w), begin, end);
     __syncthreads();
     const uint32_t keep = static_cast<uint32_t>(x.keep), low = held[0].low, high = held[0].high;
     const bool few = fixed <= keep;
@@ -803,11 +823,12 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     } else {  // the two numbers do not hold it, or more tokens are protected than stay
         auto all_of_them = [&](auto f) {
             for (int64_t at = 4 * tid; at < x.n; at += kRow) {
-                Held<1> t;
+                Held<1> four;
                 const int64_t j[1] = {at};
-                t.load(a, x, j, 0, x.n);
+                four.load(a, x, j, 0, x.n);
+                four.look(a, x);
                 uint32_t o[4];
-                t.numbers(few, o);
+                four.numbers(few, o);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) f(o[i], at + i);
             }
@@ -835,8 +856,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
     int32_t *out = moves.from + (pair * 2 + (below ? 1 : 0)) * moves.most;
     uint32_t first_even = 0;
     for (int64_t at = seg.start(w); at < end; at += kChunk) {
-        Held<> t;
-        t.load_chunk(a, x, at, begin, end);
+        if (at != seg.start(w)) t.load_chunk(a, x, at, begin, end);
+        t.look(a, x);
         if (below && carries(a) && t.in != 0u) t.carry(a, x, t.in);
         uint32_t o[kHeld], kept = 0, at_it = 0, before_it[kGroups], total, none = 0;
         t.numbers(few, o);
