@@ -7,7 +7,11 @@
 // (integer atomics: the same counts in any order), and finds the last bias of
 // each (the largest entry).  A history has far fewer tokens than the vocabulary:
 // those that are touched are listed by the first thread that comes to each, and
-// the list is worked off by all.
+// the list is worked off by all.  Of logits the outcome is put among the copied
+// scores on their way (256 rows of 131,072: 84 us, 87 where it is written over
+// them); of probabilities it is written over them, since the scores would be
+// held beside the 64-bit functions' registers (19 us for 128 rows of 50,257, 22
+// to 33 the other way).
 //
 // Logits are worked out in 32 bits; probabilities as logarithms in 64, since the
 // logarithm of a small one times a penalty, in 32 bits, would be off by 2^-18 of
@@ -50,6 +54,8 @@ struct Type {
     }
 };
 
+typedef uint32_t u32x4_at4_t __attribute__((ext_vector_type(4), aligned(4)));
+
 // What a row's parameters make of a score.
 struct Rule {
     float repetition, presence, frequency;  // 1, 0, 0: off
@@ -76,13 +82,13 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
     constexpr int SLICE = kPer * THREADS, VEC = Ty::VEC, GROUPS = Ty::GROUPS;
     extern __shared__ __align__(16) uint32_t lds[];
     const bool biased = a.bias_tokens != nullptr;
-    uint32_t *seen = lds;
+    uint32_t *seen = lds;  // a touched token's count, later its score
     int32_t *last = reinterpret_cast<int32_t *>(lds + SLICE);
-    // The tokens that are touched, by first come; two workgroups of the larger kind just fit a CU, so the count is the
-    // list's last word, and a slice where all but the last two are touched is gone through without it.
-    uint32_t *listed = lds + (biased ? 2 : 1) * SLICE + SLICE / 2 - 1;
-    uint16_t *list = reinterpret_cast<uint16_t *>(lds + (biased ? 2 : 1) * SLICE);
-    constexpr uint32_t LIST = SLICE - 2;
+    // A bit a token: it is touched.  Then those that are, by first come.  Two workgroups of the larger kind just fit a CU, so
+    // the list is that much shorter than a slice, and a slice that is touched nearly whole is gone through without it.
+    uint32_t *bits = lds + (biased ? 2 : 1) * SLICE, *listed = bits + SLICE / 32;
+    uint16_t *list = reinterpret_cast<uint16_t *>(listed + 1);
+    constexpr uint32_t LIST = SLICE - SLICE / 16 - 2;
     const int tid = static_cast<int>(threadIdx.x);
     const uint32_t off = PROBS ? 0u : Ty::narrow(-INFINITY);
     const int64_t t = static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.x;
@@ -138,31 +144,53 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
         words4[i * THREADS + tid] = make_uint4(0, 0, 0, 0);
         if (biased) words4[(kPer / 4 + i) * THREADS + tid] = make_uint4(~0u, ~0u, ~0u, ~0u);
     }
-    if (tid == 0) *listed = 0;
+    if (tid <= SLICE / 32) bits[tid] = 0;  // and the count of the list
     __syncthreads();
 
     // Tokens are counted from the slice's first one; q is none of its where it is not under `count`.
     const int vmin = v0 < 0 ? 0 : v0;
     const uint32_t count = static_cast<uint32_t>((v0 + SLICE < a.V ? v0 + SLICE : a.V) - vmin);
     auto place = [&](int32_t v) { return static_cast<uint32_t>(v) - static_cast<uint32_t>(vmin); };
-    auto touch = [&](uint32_t q, uint32_t old) {
+    const int shift = vmin - v0;  // from there to the place in the slice
+    auto touch = [&](uint32_t p, uint32_t old) {
         if (old != 0u) return;  // another thread was the first
+        if (!PROBS && copies) atomicOr(&bits[p >> 5], 1u << (p & 31));
         const uint32_t i = atomicAdd(listed, 1u);
-        if (i < LIST) list[i] = static_cast<uint16_t>(q);
+        if (i < LIST) list[i] = static_cast<uint16_t>(p);
     };
     if (a.history != nullptr) {
-        const int64_t all = a.history_lens[s], len = all < a.history_width ? all : a.history_width;
-        const int64_t prompt = a.prompt_lens != nullptr ? a.prompt_lens[s] : 0;
+        const int64_t all = a.history_lens[s];
+        const int len = static_cast<int>(all < a.history_width ? all : a.history_width);
+        const int64_t all_prompt = a.prompt_lens != nullptr ? a.prompt_lens[s] : 0;
+        const int prompt = static_cast<int>(all_prompt < len ? all_prompt : len);
         const int32_t *history = a.history + s * a.history_width;
-        for (int64_t i0 = tid; i0 < len; i0 += kPer * THREADS) {
-            uint32_t q[kPer];
+        auto note = [&](uint32_t q, bool before) {
+            if (q >= count) return;
+            const uint32_t p = q + shift;
+            touch(p, before ? atomicOr(&seen[p], kPrompt) : atomicAdd(&seen[p], 1u));
+        };
+        // Four tokens a load, two loads a thread; what is left at the end one by one.
+        constexpr int STEP = kPer * THREADS;
+        int i0 = 0;
+        for (; i0 + STEP <= len; i0 += STEP) {
+            u32x4_at4_t v[kPer / 4];
 #pragma unroll
-            for (int u = 0; u < kPer; ++u) q[u] = place(history[i0 + u * THREADS < len ? i0 + u * THREADS : i0]);
+            for (int u = 0; u < kPer / 4; ++u)
+                v[u] = *reinterpret_cast<const u32x4_at4_t *>(history + i0 + (u * THREADS + tid) * 4);
+#pragma unroll
+            for (int u = 0; u < kPer / 4; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    note(place(static_cast<int32_t>(v[u][e])), i0 + (u * THREADS + tid) * 4 + e < prompt);
+        }
+        if (i0 < len) {
+            int32_t v[kPer];
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) v[u] = history[i0 + u * THREADS + tid < len ? i0 + u * THREADS + tid : i0];
 #pragma unroll
             for (int u = 0; u < kPer; ++u) {
-                const int64_t i = i0 + u * THREADS;
-                if (q[u] >= count || i >= len) continue;
-                touch(q[u], i < prompt ? atomicOr(&seen[q[u]], kPrompt) : atomicAdd(&seen[q[u]], 1u));
+                if (i0 + u * THREADS >= len) break;
+                if (i0 + u * THREADS + tid < len) note(place(v[u]), i0 + u * THREADS + tid < prompt);
             }
         }
     }
@@ -173,30 +201,32 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
         for (int64_t i = tid; i < drafts; i += THREADS) {
             const bool sees = a.tree_mask == nullptr || (a.tree_mask[t * a.mask_words + (i >> 5)] >> (i & 31) & 1u) != 0u;
             const uint32_t q = place(a.row_tokens[first + i]);
-            if (sees && q < count) touch(q, atomicAdd(&seen[q], 1u));
+            if (sees && q < count) touch(q + shift, atomicAdd(&seen[q + shift], 1u));
         }
     }
     if (biased) {
         for (int64_t i = tid; i < a.bias_width; i += THREADS) {
             const uint32_t q = place(a.bias_tokens[s * a.bias_width + i]);
             if (q >= count) continue;
-            atomicMax(&last[q], static_cast<int32_t>(i));
-            touch(q, atomicOr(&seen[q], kBiased));
+            atomicMax(&last[q + shift], static_cast<int32_t>(i));
+            touch(q + shift, atomicOr(&seen[q + shift], kBiased));
         }
     }
-    // The scores as they are, but for those that are not allowed.
-    if (copies) {
+    // The scores as they are, but for those that are not allowed and (of logits) those that are touched.
+    auto copy = [&]() {
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
             const int v = v0 + group(g);
-            const uint32_t change = ~may[g] & ((1u << VEC) - 1u);
-            if (in_place && change == 0u) continue;
-            if (allowed != nullptr) {
+            constexpr uint32_t ALL = (1u << VEC) - 1u;
+            const uint32_t never = ~may[g] & ALL, other = PROBS ? 0u : bits[group(g) >> 5] >> (group(g) & 31) & ALL;
+            if (in_place && (never | other) == 0u) continue;
+            if ((never | other) != 0u) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    if ((change >> e & 1u) == 0u) continue;
-                    if constexpr (DT == KNN_F32) x[g][e] = off;
-                    else x[g][e / 2] = e % 2 != 0 ? (x[g][e / 2] & 0xffffu) | off << 16 : (x[g][e / 2] & 0xffff0000u) | off;
+                    if (((never | other) >> e & 1u) == 0u) continue;
+                    const uint32_t to = (never >> e & 1u) != 0u ? off : seen[group(g) + e];
+                    if constexpr (DT == KNN_F32) x[g][e] = to;
+                    else x[g][e / 2] = e % 2 != 0 ? (x[g][e / 2] & 0xffffu) | to << 16 : (x[g][e / 2] & 0xffff0000u) | to;
                 }
             }
             if (even && v >= 0 && v + VEC <= a.V) {
@@ -210,34 +240,39 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
                     }
             }
         }
-    }
+    };
+    if (PROBS && copies) copy();
     __syncthreads();
 
     Rule rule{parameter(a.repetition, t, 1.0f), parameter(a.presence, t, 0.0f), parameter(a.frequency, t, 0.0f)};
     if (!(rule.repetition > 0.0f)) rule.repetition = 1.0f;
-    auto adjust = [&](uint32_t q) {
-        const int v = vmin + static_cast<int>(q);
-        const float from = Ty::widen(u32x4_t{Ty::raw(in, v), 0, 0, 0}, 0);
-        if (allowed != nullptr && (allowed[v >> 5] >> (v & 31) & 1u) == 0u) return;
-        const uint32_t c = seen[q] & ~kBiased;
-        const int32_t b = biased ? last[q] : -1;
+    auto adjust = [&](uint32_t p) {
+        const int v = v0 + static_cast<int>(p);
+        const uint32_t raw = Ty::raw(in, v);
+        const float from = Ty::widen(u32x4_t{raw, 0, 0, 0}, 0);
+        const uint32_t c = seen[p] & ~kBiased;
+        const int32_t b = biased ? last[p] : -1;
         const float bias = b >= 0 ? a.bias_values[s * a.bias_width + b] : 0.0f;
-        float to;
+        uint32_t to = raw;
         if constexpr (PROBS) {
-            if (!(from > 0.0f)) return;
-            to = static_cast<float>(exp(rule.of(log(static_cast<double>(from)), c, b >= 0, bias)));
+            if (from > 0.0f)
+                to = Ty::narrow(static_cast<float>(exp(rule.of(log(static_cast<double>(from)), c, b >= 0, bias))));
         } else {
-            to = rule.of(from, c, b >= 0, bias);
+            to = Ty::narrow(rule.of(from, c, b >= 0, bias));
         }
-        Ty::set(out, v, Ty::narrow(to));
+        if (!PROBS && copies) seen[p] = to;
+        else if (allowed == nullptr || (allowed[v >> 5] >> (v & 31) & 1u) != 0u) Ty::set(out, v, to);
     };
     const uint32_t n = *listed;
     if (n <= LIST) {
         for (uint32_t i = tid; i < n; i += THREADS) adjust(list[i]);
     } else {
-        for (uint32_t q = tid; q < count; q += THREADS)
-            if (seen[q] != 0u) adjust(q);
+        for (uint32_t p = shift + tid; p < shift + count; p += THREADS)
+            if (seen[p] != 0u) adjust(p);
     }
+    if (PROBS || !copies) return;
+    __syncthreads();
+    copy();
 }
 
 template <knn_dtype DT, bool PROBS, int THREADS>
