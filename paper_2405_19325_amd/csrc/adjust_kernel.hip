@@ -1,7 +1,7 @@
 // Penalties for repeated tokens, biases and the tokens that a grammar allows,
 // on rows of logits or probabilities.
 //
-// A workgroup takes a slice of a row's tokens, 8 of them a thread, copies its
+// A workgroup takes a slice of 8,192 of a row's tokens, 8 a thread, copies its
 // scores but for those that are not allowed, and meanwhile counts in LDS how
 // often each token is in the row's history and in the drafts that the row sees
 // (integer atomics: the same counts in any order), and finds the last bias of
@@ -24,7 +24,9 @@ namespace knnlm {
 namespace {
 
 constexpr int64_t kGrid = 1 << 20;      // rows of a row of the grid
+constexpr int kThreads = 1024;
 constexpr int kPer = 8;                 // tokens of a thread
+constexpr int kSlice = kPer * kThreads;
 // Beside a token's count: it is in the prompt; it has a bias.
 constexpr uint32_t kPrompt = 1u << 31, kBiased = 1u << 30;
 
@@ -76,19 +78,19 @@ __device__ __forceinline__ float parameter(const float *p, int64_t t, float off)
 }
 
 // A slice of a row's scores.  LDS: words [slice], where there are biases the last of each [slice], and the list.
-template <knn_dtype DT, bool PROBS, int THREADS>
-__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(AdjustArgs a) {
+template <knn_dtype DT, bool PROBS>
+__global__ __launch_bounds__(kThreads, 8) void k_adjust(AdjustArgs a) {
     using Ty = Type<DT>;
-    constexpr int SLICE = kPer * THREADS, VEC = Ty::VEC, GROUPS = Ty::GROUPS;
+    constexpr int VEC = Ty::VEC, GROUPS = Ty::GROUPS;
     extern __shared__ __align__(16) uint32_t lds[];
     const bool biased = a.bias_tokens != nullptr;
     uint32_t *seen = lds;  // a touched token's count, later its score
-    int32_t *last = reinterpret_cast<int32_t *>(lds + SLICE);
-    // A bit a token: it is touched.  Then those that are, by first come.  Two workgroups of the larger kind just fit a CU, so
+    int32_t *last = reinterpret_cast<int32_t *>(lds + kSlice);
+    // A bit a token: it is touched.  Then those that are, by first come.  Two workgroups just fit a CU, so
     // the list is that much shorter than a slice, and a slice that is touched nearly whole is gone through without it.
-    uint32_t *bits = lds + (biased ? 2 : 1) * SLICE, *listed = bits + SLICE / 32;
+    uint32_t *bits = lds + (biased ? 2 : 1) * kSlice, *listed = bits + kSlice / 32;
     uint16_t *list = reinterpret_cast<uint16_t *>(listed + 1);
-    constexpr uint32_t LIST = SLICE - SLICE / 16 - 2;
+    constexpr uint32_t LIST = kSlice - kSlice / 16 - 2;
     const int tid = static_cast<int>(threadIdx.x);
     const uint32_t off = PROBS ? 0u : Ty::narrow(-INFINITY);
     const int64_t t = static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.x;
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
     char *out = static_cast<char *>(a.out) + t * a.out_stride * Ty::SIZE;
     // Places are counted from the 16 bytes that hold the first score; place p is token p - lead.
     const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16) / Ty::SIZE;
-    const int v0 = static_cast<int>(blockIdx.y) * SLICE - lead;
+    const int v0 = static_cast<int>(blockIdx.y) * kSlice - lead;
     if (v0 >= a.V) return;
     const bool even = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(in)) % 16 == 0;
     const bool in_place = a.out == a.scores, copies = !in_place || a.allowed != nullptr;
@@ -113,7 +115,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
     // The slice's scores, and a bit a token: it is allowed.
     u32x4_t x[GROUPS];
     uint32_t may[GROUPS];
-    auto group = [&](int g) { return (g * THREADS + tid) * VEC; };  // place in the slice
+    auto group = [&](int g) { return (g * kThreads + tid) * VEC; };  // place in the slice
     if (copies) {
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
@@ -141,15 +143,15 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
     uint4 *words4 = reinterpret_cast<uint4 *>(lds);
 #pragma unroll
     for (int i = 0; i < kPer / 4; ++i) {
-        words4[i * THREADS + tid] = make_uint4(0, 0, 0, 0);
-        if (biased) words4[(kPer / 4 + i) * THREADS + tid] = make_uint4(~0u, ~0u, ~0u, ~0u);
+        words4[i * kThreads + tid] = make_uint4(0, 0, 0, 0);
+        if (biased) words4[(kPer / 4 + i) * kThreads + tid] = make_uint4(~0u, ~0u, ~0u, ~0u);
     }
-    if (tid <= SLICE / 32) bits[tid] = 0;  // and the count of the list
+    if (tid <= kSlice / 32) bits[tid] = 0;  // and the count of the list
     __syncthreads();
 
     // Tokens are counted from the slice's first one; q is none of its where it is not under `count`.
     const int vmin = v0 < 0 ? 0 : v0;
-    const uint32_t count = static_cast<uint32_t>((v0 + SLICE < a.V ? v0 + SLICE : a.V) - vmin);
+    const uint32_t count = static_cast<uint32_t>((v0 + kSlice < a.V ? v0 + kSlice : a.V) - vmin);
     auto place = [&](int32_t v) { return static_cast<uint32_t>(v) - static_cast<uint32_t>(vmin); };
     const int shift = vmin - v0;  // from there to the place in the slice
     auto touch = [&](uint32_t p, uint32_t old) {
@@ -170,27 +172,27 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
             touch(p, before ? atomicOr(&seen[p], kPrompt) : atomicAdd(&seen[p], 1u));
         };
         // Four tokens a load, two loads a thread; what is left at the end one by one.
-        constexpr int STEP = kPer * THREADS;
+        constexpr int STEP = kPer * kThreads;
         int i0 = 0;
         for (; i0 + STEP <= len; i0 += STEP) {
             u32x4_at4_t v[kPer / 4];
 #pragma unroll
             for (int u = 0; u < kPer / 4; ++u)
-                v[u] = *reinterpret_cast<const u32x4_at4_t *>(history + i0 + (u * THREADS + tid) * 4);
+                v[u] = *reinterpret_cast<const u32x4_at4_t *>(history + i0 + (u * kThreads + tid) * 4);
 #pragma unroll
             for (int u = 0; u < kPer / 4; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    note(place(static_cast<int32_t>(v[u][e])), i0 + (u * THREADS + tid) * 4 + e < prompt);
+                    note(place(static_cast<int32_t>(v[u][e])), i0 + (u * kThreads + tid) * 4 + e < prompt);
         }
         if (i0 < len) {
             int32_t v[kPer];
 #pragma unroll
-            for (int u = 0; u < kPer; ++u) v[u] = history[i0 + u * THREADS + tid < len ? i0 + u * THREADS + tid : i0];
+            for (int u = 0; u < kPer; ++u) v[u] = history[i0 + u * kThreads + tid < len ? i0 + u * kThreads + tid : i0];
 #pragma unroll
             for (int u = 0; u < kPer; ++u) {
-                if (i0 + u * THREADS >= len) break;
-                if (i0 + u * THREADS + tid < len) note(place(v[u]), i0 + u * THREADS + tid < prompt);
+                if (i0 + u * kThreads >= len) break;
+                if (i0 + u * kThreads + tid < len) note(place(v[u]), i0 + u * kThreads + tid < prompt);
             }
         }
     }
@@ -198,14 +200,14 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
         int64_t rows = a.row_offsets != nullptr ? a.row_offsets[s + 1] : t + 1;
         rows = (rows < a.rows ? rows : a.rows) - first;
         const int64_t drafts = a.tree_mask == nullptr ? t - first + 1 : rows < 32 * a.mask_words ? rows : 32 * a.mask_words;
-        for (int64_t i = tid; i < drafts; i += THREADS) {
+        for (int64_t i = tid; i < drafts; i += kThreads) {
             const bool sees = a.tree_mask == nullptr || (a.tree_mask[t * a.mask_words + (i >> 5)] >> (i & 31) & 1u) != 0u;
             const uint32_t q = place(a.row_tokens[first + i]);
             if (sees && q < count) touch(q + shift, atomicAdd(&seen[q + shift], 1u));
         }
     }
     if (biased) {
-        for (int64_t i = tid; i < a.bias_width; i += THREADS) {
+        for (int64_t i = tid; i < a.bias_width; i += kThreads) {
             const uint32_t q = place(a.bias_tokens[s * a.bias_width + i]);
             if (q >= count) continue;
             atomicMax(&last[q + shift], static_cast<int32_t>(i));
@@ -265,9 +267,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
     };
     const uint32_t n = *listed;
     if (n <= LIST) {
-        for (uint32_t i = tid; i < n; i += THREADS) adjust(list[i]);
+        for (uint32_t i = tid; i < n; i += kThreads) adjust(list[i]);
     } else {
-        for (uint32_t p = shift + tid; p < shift + count; p += THREADS)
+        for (uint32_t p = shift + tid; p < shift + count; p += kThreads)
             if (seen[p] != 0u) adjust(p);
     }
     if (PROBS || !copies) return;
@@ -275,20 +277,14 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 4) void k_adjust(Adj
     copy();
 }
 
-template <knn_dtype DT, bool PROBS, int THREADS>
-hipError_t launch(const AdjustArgs &a, hipStream_t stream) {
-    constexpr int SLICE = kPer * THREADS;
-    const int64_t slices = (a.V + Type<DT>::VEC - 1 + SLICE - 1) / SLICE;
-    const dim3 grid(static_cast<unsigned>(a.rows < kGrid ? a.rows : kGrid), static_cast<unsigned>(slices),
-                    static_cast<unsigned>((a.rows + kGrid - 1) / kGrid));
-    k_adjust<DT, PROBS, THREADS><<<grid, THREADS, sizeof(uint32_t) * (SLICE * (a.bias_tokens != nullptr ? 2 : 1) + SLICE / 2), stream>>>(a);
-    return hipGetLastError();
-}
-
 template <knn_dtype DT, bool PROBS>
 hipError_t launch(const AdjustArgs &a, hipStream_t stream) {
-    if (a.rows * ((a.V + 2047) / 2048) <= 1024) return launch<DT, PROBS, 256>(a, stream);
-    return launch<DT, PROBS, 1024>(a, stream);
+    const int64_t slices = (a.V + Type<DT>::VEC - 1 + kSlice - 1) / kSlice;
+    const dim3 grid(static_cast<unsigned>(a.rows < kGrid ? a.rows : kGrid), static_cast<unsigned>(slices),
+                    static_cast<unsigned>((a.rows + kGrid - 1) / kGrid));
+    const size_t words = kSlice * (a.bias_tokens != nullptr ? 2 : 1) + kSlice / 2;
+    k_adjust<DT, PROBS><<<grid, kThreads, sizeof(uint32_t) * words, stream>>>(a);
+    return hipGetLastError();
 }
 
 template <knn_dtype DT>

@@ -918,7 +918,10 @@ hipError_t launch(const EvictArgs &a, char *workspace, hipStream_t stream) {
     const Moves moves{reinterpret_cast<int32_t *>(workspace), reinterpret_cast<int32_t *>(workspace + p.off_from), p.most};
     const dim3 grid(static_cast<unsigned>(heads < kGrid ? heads : kGrid), 1, static_cast<unsigned>((heads + kGrid - 1) / kGrid));
     if (a.max_keys <= kChunk) {
-        if (heads >= 256 || a.max_keys <= 2048) {
+        // Moves by the head's own workgroup where there are heads enough to fill the CUs with them, or few tokens. (8 heads, a
+        // step over 4,000 tokens 9.8 us, 12.3 in two launches; to half of them 25.0 and 15.1; of 2,000 16.0 and 13.2, a step of
+        // 1,025 7.4 and 9.8.  128 heads of 4,000 48.7 and 51.0, of 8,000 to a quarter 72.8 and 64.5; 256 104 and 108.)
+        if (a.max_keys <= 2048 || a.max_keys <= 32 * heads) {
             k_evict_held<true, CHUNKS><<<grid, kThreads, 0, stream>>>(a, moves);
             return hipGetLastError();
         }
