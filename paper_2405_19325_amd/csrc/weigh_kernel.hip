@@ -74,21 +74,46 @@ __device__ __forceinline__ void stage(const WeighArgs &a, const Tile &t, const S
         st.lse2[c] = isfinite(lse) ? lse * kLog2e : INFINITY;
         st.row[c] = isfinite(lse) ? i : kNobody;
     }
-    for (int e = static_cast<int>(threadIdx.x); e < padded * CHUNKS; e += THREADS) {
-        const int c = e / CHUNKS, chunk = e % CHUNKS, i = (c0 + c) / g;
-        const int64_t source = c < n ? source_of(i) : -1;
-        u32x4_t v{0, 0, 0, 0};
-        if (source >= 0)
-            v = *reinterpret_cast<const u32x4_t *>(static_cast<const uint16_t *>(a.q) + source * a.q_row +
-                                                   (h * g + (c0 + c - i * g)) * a.q_head + chunk * 8);
-        st.q[c * CHUNKS + (chunk ^ spread<D>(c))] = v;
+    constexpr int AHEAD = 4;  // loads of a thread on their way
+    for (int e0 = static_cast<int>(threadIdx.x); e0 < padded * CHUNKS; e0 += AHEAD * THREADS) {
+        u32x4_t v[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int e = e0 + u * THREADS, c = e / CHUNKS, chunk = e % CHUNKS, i = (c0 + c) / g;
+            const int64_t source = c < n ? source_of(i) : -1;
+            v[u] = u32x4_t{0, 0, 0, 0};
+            if (source >= 0)
+                v[u] = *reinterpret_cast<const u32x4_t *>(static_cast<const uint16_t *>(a.q) + source * a.q_row +
+                                                          (h * g + (c0 + c - i * g)) * a.q_head + chunk * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int e = e0 + u * THREADS, c = e / CHUNKS;
+            if (c < padded) st.q[c * CHUNKS + (e % CHUNKS ^ spread<D>(c))] = v[u];
+        }
     }
 }
 
-// Whether a column of this row sees a key: all see the cached ones (draft < 0).
-__device__ __forceinline__ bool sees(const WeighArgs &a, const Tile &t, int row, int draft) {
-    if (a.tree_mask == nullptr || draft < 0 || row == kNobody) return draft <= row;
-    return draft < 32 * a.mask_words && (a.tree_mask[(t.r0 + row) * a.mask_words + (draft >> 5)] >> (draft & 31) & 1u) != 0u;
+// Which of 64 keys a column of this row sees, as bits: the first of them is the
+// sequence's draft d0 (a cached one where negative).
+__device__ __forceinline__ uint64_t seen_of(const WeighArgs &a, const Tile &t, int row, int d0) {
+    auto first_bits = [](int n) { return n <= 0 ? uint64_t{0} : n >= 64 ? ~uint64_t{0} : (uint64_t{1} << n) - 1; };
+    if (row == kNobody) return 0;
+    if (a.tree_mask == nullptr) return first_bits(row - d0 + 1);
+    const uint32_t *words = a.tree_mask + (t.r0 + row) * a.mask_words;
+    const int from = d0 < 0 ? 0 : d0, last = static_cast<int>(a.mask_words) - 1;  // (a mask has at most 2^31 bits)
+    uint32_t w[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const int at = (from >> 5) + i;
+        w[i] = words[at < last ? at : last];
+        w[i] = at <= last ? w[i] : 0u;
+    }
+    const int off = from & 31;
+    uint64_t bits = (w[0] | static_cast<uint64_t>(w[1]) << 32) >> off;
+    if (off != 0) bits |= static_cast<uint64_t>(w[2]) << (64 - off);
+    if (d0 >= 0) return bits;
+    return d0 <= -64 ? ~uint64_t{0} : bits << -d0 | first_bits(-d0);
 }
 
 template <knn_dtype DT, int D, int WAVES>
@@ -234,21 +259,26 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                             plain = !__any(odd);
                         }
                         if (!plain) {
-                            const int draft0 = j0 + col - length;  // of block 0's key
 #pragma unroll
-                            for (int b = 0; b < B; ++b) {  // (a block at a time, to spare registers)
-                                w[b] = 0.0f;
+                            for (int b = 0; b < B; ++b) w[b] = 0.0f;
 #pragma unroll 1
-                                for (int c = 0; c < padded; c += 16) {
+                            for (int c = 0; c < padded; c += 16) {
+                                uint64_t seen[4];
+                                u32x4_t q[KK];
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) seen[r] = seen_of(a, t, st.row[c + 4 * quad + r], j0 - length) >> col;
+#pragma unroll
+                                for (int kk = 0; kk < KK; ++kk)
+                                    q[kk] = st.q[(c + col) * (D / 8) + ((4 * kk + quad) ^ spread<D>(col))];
+#pragma unroll
+                                for (int b = 0; b < B; ++b) {  // (a block at a time, to spare registers)
                                     f32x4_t x{0, 0, 0, 0};
 #pragma unroll
-                                    for (int kk = 0; kk < KK; ++kk)
-                                        x = mfma16<DT>(st.q[(c + col) * (D / 8) + ((4 * kk + quad) ^ spread<D>(col))], k[b][kk], x);
+                                    for (int kk = 0; kk < KK; ++kk) x = mfma16<DT>(q[kk], k[b][kk], x);
 #pragma unroll
                                     for (int r = 0; r < 4; ++r) {
-                                        const int row = st.row[c + 4 * quad + r];
                                         const float e = __builtin_amdgcn_exp2f(fmaf(x[r], c2, -st.lse2[c + 4 * quad + r]));
-                                        w[b] += sees(a, t, row, draft0 + 16 * b) ? e : 0.0f;
+                                        w[b] += (seen[r] >> 16 * b & 1u) != 0u ? e : 0.0f;
                                     }
                                 }
                             }
@@ -469,20 +499,25 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
                 }
                 if (!plain) {
 #pragma unroll
-                    for (int b = 0; b < B; ++b) {
-                        const int draft = j0 + 16 * b + col - length;
-                        w[b] = 0.0f;
+                    for (int b = 0; b < B; ++b) w[b] = 0.0f;
 #pragma unroll
-                        for (int m = 0; m < NT; ++m) {
-                            if (16 * m >= cols) break;
+                    for (int m = 0; m < NT; ++m) {
+                        if (16 * m >= cols) break;
+                        uint64_t seen[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int row = lse2[m][r] < INFINITY ? (16 * m + 4 * quad + r) / g : kNobody;
+                            seen[r] = seen_of(a, t, row, j0 - length) >> col;
+                        }
+#pragma unroll
+                        for (int b = 0; b < B; ++b) {
                             f32x4_t x{0, 0, 0, 0};
 #pragma unroll
                             for (int kk = 0; kk < KK; ++kk) x = mfma16<DT>(q[m][kk], key(b, kk), x);
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                const int row = lse2[m][r] < INFINITY ? (16 * m + 4 * quad + r) / g : kNobody;
                                 const float e = __builtin_amdgcn_exp2f(fmaf(x[r], c2, -lse2[m][r]));
-                                w[b] += sees(a, t, row, draft) ? e : 0.0f;
+                                w[b] += (seen[r] >> 16 * b & 1u) != 0u ? e : 0.0f;
                             }
                         }
                     }
@@ -529,8 +564,8 @@ void launch(const WeighArgs &a, int most, hipStream_t stream) {
     const size_t fit = (size_t{156} << 10) / (lds + 1024);
     const int64_t room = fit * WAVES > 16 ? 16 / WAVES : fit < 1 ? 1 : static_cast<int64_t>(fit);  // workgroups of a CU
     const int64_t tiles = a.S * a.kv_heads * tiles_of(a.max_keys, Sh::KEYS);
-    int64_t blocks = (tiles + WAVES - 1) / WAVES;
-    if (blocks > kCus * room) blocks = kCus * room;
+    // (A workgroup a tile where there are so few: another head's queries are another wait.)
+    const int64_t blocks = tiles < kCus * room ? tiles : kCus * room;
     k_key_weights<DT, D, WAVES><<<dim3(static_cast<unsigned>(blocks)), WAVES * kWave, lds, stream>>>(a, most);
 }
 
