@@ -95,7 +95,7 @@ __device__ __forceinline__ void stage(const WeighArgs &a, const Tile &t, const S
 }
 
 // Which of 64 keys a column of this row sees, as bits: the first of them is the
-// sequence's draft d0 (a cached one where negative).
+// sequence's draft d0 (a cached one where negative, and no less than -64).
 __device__ __forceinline__ uint64_t seen_of(const WeighArgs &a, const Tile &t, int row, int d0) {
     auto first_bits = [](int n) { return n <= 0 ? uint64_t{0} : n >= 64 ? ~uint64_t{0} : (uint64_t{1} << n) - 1; };
     if (row == kNobody) return 0;
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                                 for (int b = 0; b < B; ++b) x[b] = mfma16<DT>(q[kk], k[b][kk], x[b]);
                         };
                         float w[B] = {};
-                        bool plain = j0 + Sh::KEYS <= length;
+                        bool plain = length - j0 >= Sh::KEYS;  // (a length may be all that 31 bits hold)
                         if (plain) {
 #pragma unroll 1
                             for (int c = 0; c < padded; c += 16) {
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                                 uint64_t seen[4];
                                 u32x4_t q[KK];
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) seen[r] = seen_of(a, t, st.row[c + 4 * quad + r], j0 - length) >> col;
+                                for (int r = 0; r < 4; ++r) seen[r] = seen_of(a, t, st.row[c + 4 * quad + r], max(j0 - length, -64)) >> col;
 #pragma unroll
                                 for (int kk = 0; kk < KK; ++kk)
                                     q[kk] = st.q[(c + col) * (D / 8) + ((4 * kk + quad) ^ spread<D>(col))];
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
                     return *reinterpret_cast<const __attribute__((address_space(3))) u32x4_t *>(
                         static_cast<uintptr_t>(lds + (16 * b + col) * ROW + 16 * ((4 * kk + quad) ^ spread<D>(col))));
                 };
-                bool plain = j0 + KEYS <= length;
+                bool plain = length - j0 >= KEYS;  // (a length may be all that 31 bits hold)
                 if (plain) {
                     // Two column tiles and all blocks at a time: as many chains of matrix instructions beside each other.
                     constexpr int M = NT > 1 ? 2 : 1;
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const int row = lse2[m][r] < INFINITY ? (16 * m + 4 * quad + r) / g : kNobody;
-                            seen[r] = seen_of(a, t, row, j0 - length) >> col;
+                            seen[r] = seen_of(a, t, row, max(j0 - length, -64)) >> col;
                         }
 #pragma unroll
                         for (int b = 0; b < B; ++b) {
@@ -552,8 +552,8 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
 
 template <knn_dtype DT, int D, int NT>
 void launch_few(const WeighArgs &a, hipStream_t stream) {
-    const int64_t stages = a.S * a.kv_heads * tiles_of(a.max_keys, kStageBytes / (2 * D));
-    const int64_t blocks = (stages + 3) / 4 < kCus ? (stages + 3) / 4 : kCus;
+    const double stages = static_cast<double>(a.S) * a.kv_heads * static_cast<double>(tiles_of(a.max_keys, kStageBytes / (2 * D)));
+    const int64_t blocks = stages < 4 * kCus ? (static_cast<int64_t>(stages) + 3) / 4 : kCus;
     k_key_weights_few<DT, D, NT><<<dim3(static_cast<unsigned>(blocks)), 4 * kWave, 0, stream>>>(a);
 }
 
@@ -563,9 +563,9 @@ void launch(const WeighArgs &a, int most, hipStream_t stream) {
     const size_t lds = static_cast<size_t>(most) * (Sh::ROW + 8);
     const size_t fit = (size_t{156} << 10) / (lds + 1024);
     const int64_t room = fit * WAVES > 16 ? 16 / WAVES : fit < 1 ? 1 : static_cast<int64_t>(fit);  // workgroups of a CU
-    const int64_t tiles = a.S * a.kv_heads * tiles_of(a.max_keys, Sh::KEYS);
+    const double tiles = static_cast<double>(a.S) * a.kv_heads * static_cast<double>(tiles_of(a.max_keys, Sh::KEYS));
     // (A workgroup a tile where there are so few: another head's queries are another wait.)
-    const int64_t blocks = tiles < kCus * room ? tiles : kCus * room;
+    const int64_t most_blocks = kCus * room, blocks = tiles < most_blocks ? static_cast<int64_t>(tiles) : most_blocks;
     k_key_weights<DT, D, WAVES><<<dim3(static_cast<unsigned>(blocks)), WAVES * kWave, lds, stream>>>(a, most);
 }
 
