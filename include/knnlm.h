@@ -561,7 +561,8 @@ size_t knn_sample_workspace_size(int64_t rows, int64_t V, knn_dtype dtype);
  *   key_positions  [n_pages, kv_heads, page_size] int32 or NULL: the rows' own places get positions[t].
  *   positions      [rows] int32 or NULL: the cache index.  Only with key_positions.
  *
- * A sequence without rows keeps its masses.  Places past a sequence's tokens are left as they are.  mass and
+ * A sequence without rows keeps its masses.  Places past a sequence's tokens are left as they are; those of a page that
+ * two sequences share get the weight of either.  mass and
  * key_positions lie apart from all that is read and from each other.  Sums are in fp32, in an order that does not
  * depend on how workgroups run.  Sizes, alignment and strides as knn_tree_attention serves them.
  */
@@ -613,7 +614,9 @@ knn_status knn_cache_evict(void *k_cache, void *v_cache, float *mass, int32_t *k
                            int32_t *positions_out, int32_t *new_lens, void *workspace, size_t workspace_bytes,
                            void *stream);
 
-/* Bytes of workspace knn_cache_evict needs for these sizes (0 if they are invalid). */
+/* Bytes of workspace knn_cache_evict needs for these sizes (0 if they are invalid): about 4 a token of max_keys in each
+ * head, 8 where max_keys is over 8,192.  S kv_heads is under 2^31 and S kv_heads max_keys up to 2^56
+ * (KNN_ERR_UNSUPPORTED above). */
 size_t knn_cache_evict_workspace_size(int64_t S, int64_t kv_heads, int64_t max_keys);
 
 /*

@@ -56,7 +56,10 @@ knn_status check_sample(int64_t rows, int64_t V, knn_dtype dtype) {
 
 knn_status check_evict(int64_t S, int64_t kv_heads, int64_t max_keys) {
     if (S < 1 || kv_heads < 1 || max_keys < 1) return KNN_ERR_INVALID_ARG;
-    if (kv_heads > KNNLM_MAX_HEADS || S > 0x7fffffff / kv_heads || max_keys > 0x7fffffff) return KNN_ERR_UNSUPPORTED;
+    // (heads are counted in 31 bits, and a workspace of up to 12 bytes a token fits 64)
+    if (kv_heads > KNNLM_MAX_HEADS || S > 0x7fffffff / kv_heads || max_keys > 0x7fffffff ||
+        static_cast<double>(S) * kv_heads * max_keys > 72057594037927936.0)  // 2^56
+        return KNN_ERR_UNSUPPORTED;
     return KNN_OK;
 }
 

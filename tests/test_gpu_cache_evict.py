@@ -285,6 +285,26 @@ def test_ledgers_off_16_bytes_and_caches_off_them():
         check({n: t.clone() if t.data_ptr() % 16 == 0 else t for n, t in x.items()}, budgets, sinks=2, recent=5)
 
 
+def test_one_ledger_in_place_and_one_apart():
+    for lens, budget in (([200, 33], [150, 10]), ([9000, 33], [4000, 10])):
+        x = batch(lens, 2, 64, 32, seed=16)
+        want = lm.evict(bits(x["k_cache"]), bits(x["v_cache"]), x["mass"].cpu().numpy(), ints(x["key_positions"]),
+                        ints(x["pages"]), lens, budget, recent=5)
+        apart = {n: torch.zeros_like(x[n]) for n in ("mass", "key_positions")}
+        for n, other in (("mass", "key_positions"), ("key_positions", "mass")):
+            y = {m: t.clone() for m, t in x.items()}
+            out = {"mass_out" if n == "mass" else "positions_out": apart[n]}
+            knn.cache_evict(y["k_cache"], y["v_cache"], y["mass"], y["pages"], y["cache_lens"],
+                            torch.tensor(budget, dtype=torch.int32).cuda(), key_positions=y["key_positions"], recent=5, **out)
+            assert np.array_equal(bits(y["k_cache"]), want[0]) and torch.equal(y[n], x[n])
+            assert np.array_equal(ints(y[other]), want[3] if other == "key_positions" else want[2])
+            for s in range(2):
+                for c in range(budget[s]):
+                    page, slot = lm.place(ints(x["pages"]), s, c, len(x["mass"]), 32)
+                    ledger = want[2] if n == "mass" else want[3]
+                    assert np.array_equal(ints(apart[n])[page, :, slot], ledger[page, :, slot])
+
+
 def test_many_short_heads():
     n = np.random.RandomState(5).randint(0, 60, 300).tolist()
     check(batch(n, 3, 64, 16, seed=13), [max(0, v - 3) for v in n], sinks=1, recent=2, positions=False)

@@ -76,6 +76,8 @@ def test_evict_workspace_size(lib):
     size = lib.knn_cache_evict_workspace_size
     for keys in (1, 2, 31, 4096, 131072, 0x7fffffff):
         assert size(2, 8, keys) > 0 and size(2, 8, keys) % 256 == 0
+    assert size((1 << 31) - 1, 1, (1 << 31) - 1) == 0  # 2^64 bytes
+    assert size(1 << 20, 32, (1 << 31) - 1) > 1 << 57
     assert size(0, 8, 100) == 0 and size(2, 0, 100) == 0 and size(2, 8, 0) == 0 and size(2, 8, 1 << 31) == 0
 
 
