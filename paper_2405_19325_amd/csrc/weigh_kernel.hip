@@ -209,9 +209,10 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                             pages = pages >= 0 && pages < a.cache.n_pages ? pages : -1;
                         }
                         // Each quarter of the wave has a block's masses.
-                        const int j0 = tile * Sh::KEYS, j = j0 + 16 * (quad & (B - 1)) + col;
+                        const int j0 = tile * Sh::KEYS, part = 16 * (quad & (B - 1)) + col;
+                        const int j = static_cast<int>(static_cast<uint32_t>(j0) + part);
                         const int32_t p = __shfl(pages, first + (quad & (B - 1)));
-                        const bool mine = quad < B && j < total_keys && p >= 0;
+                        const bool mine = quad < B && part < total_keys - j0 && p >= 0;
                         const int64_t place = ((static_cast<int64_t>(p) * a.kv_heads + h) << a.cache.page_log2) + (j & in_page);
                         float mass = 0.0f;
                         if (mine && j < length && a.decay != 0.0f && c0 + most >= cols) mass = a.mass[place];
@@ -536,8 +537,8 @@ __global__ __launch_bounds__(4 * kWave, 1) void k_key_weights_few(WeighArgs a) {
                     drawn = quad == b ? w[b] : drawn, page = quad == b ? other : page;
                 }
                 const float mass = masses[wave][i % kRing][lane];
-                const int j = j0 + 16 * quad + col;
-                if (quad < B && j < total_keys && page >= 0) {
+                const int part = 16 * quad + col, j = static_cast<int>(static_cast<uint32_t>(j0) + part);
+                if (quad < B && part < total_keys - j0 && page >= 0) {
                     const int64_t place = ((static_cast<int64_t>(page) * a.kv_heads + h) << a.cache.page_log2) + (j & in_page);
                     // (written through, as an agent's: paths over 8 x 100,000 tokens 334 us, 346 by way of the caches' write-back)
                     __hip_atomic_store(a.mass + place, drawn + (j < length && a.decay != 0.0f ? a.decay * mass : 0.0f),

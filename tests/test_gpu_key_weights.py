@@ -338,3 +338,31 @@ def test_on_another_stream():
     call.run(side)
     side.synchronize()
     assert (np.abs(host(x["mass"]) - want) <= tol).all()
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (112, 1)])
+def test_the_longest_length(heads):
+    """2^31 - 1 keys, all but the last page's of two pages that the table names again and again."""
+    page, total, H = 1024, 2 ** 31 - 1, heads[0]
+    g = torch.Generator().manual_seed(21)
+    k = torch.randn(3, 1, page, 64, generator=g).bfloat16().cuda()
+    q = torch.randn(1, H, 64, generator=g).bfloat16().cuda()
+    lse = (torch.rand(1, H, generator=g) + 3.0).cuda()
+    pages = torch.zeros(1, total // page + 1, dtype=torch.int32).cuda()
+    pages[:, 1::2] = 1
+    pages[:, -1] = 2
+    mass = torch.rand(3, 1, page, generator=g).cuda()
+    before = mass.clone()
+    positions = torch.full((3, 1, page), -5, dtype=torch.int32).cuda()
+    knn.key_weights(q, lse, k, pages, offsets([1]), torch.tensor([total - 1], dtype=torch.int32).cuda(), mass, max_rows=1,
+                    max_keys=total, key_positions=positions, decay=0.0)
+    x, size = host(k)[:, 0] @ host(q)[0].T / 8.0, np.abs(host(k)[:, 0]) @ np.abs(host(q)[0]).T / 8.0  # [pages, page, heads]
+    weights = np.exp(x - host(lse)[0])
+    want = weights.sum(-1)
+    # (as in want_of)
+    off = (weights * (64 * 2.0 ** -23 * size + 2.0 ** -22 * (np.abs(x) + np.abs(host(lse)[0]) + 1))).sum(-1)
+    off += (H + 4) * 2.0 ** -24 * want
+    assert np.all(np.abs(host(mass)[:2, 0] - want[:2]) <= off[:2])
+    assert np.all(np.abs(host(mass)[2, 0, :-1] - want[2, :-1]) <= off[2, :-1])
+    assert float(mass[2, 0, -1]) == float(before[2, 0, -1])
+    assert int(positions[2, 0, -2]) == total - 1 and int((positions == -5).sum()) == 3 * page - 1
