@@ -329,3 +329,46 @@ def test_on_another_stream_and_two_calls_at_once():
     for x, y in zip((a, b), want):
         for n in ("k_cache", "v_cache", "mass", "key_positions"):
             assert torch.equal(x[n], y[n])
+
+
+def test_the_longest_head():
+    """2^31 - 1 tokens, whose keys and values are their indices; weights of 24 bits in no order, many of them alike."""
+    n, page, piece = 2 ** 31 - 1, 65536, 2 ** 28
+    pages = torch.arange(2 ** 31 // page, dtype=torch.int32).cuda()[None]
+    shape = (pages.numel(), 1, page)
+    index = torch.empty(2 ** 31, dtype=torch.int32, device="cuda")
+    mass = torch.empty(2 ** 31, dtype=torch.float32, device="cuda")
+    for j in range(0, 2 ** 31, piece):
+        index[j:j + piece] = torch.arange(j, j + piece, dtype=torch.int64, device="cuda").int()
+        mass[j:j + piece] = ((torch.arange(j, j + piece, dtype=torch.int64, device="cuda") * 2654435761 >> 8) & 0xffffff).float()
+    border = float(7 << 20)
+    over = sum(int((mass[j:min(n, j + piece)] > border).sum()) for j in range(0, n, piece))
+    even = sum(int((mass[j:min(n, j + piece)] == border).sum()) for j in range(0, n, piece))
+    keep = over + even // 2
+    assert even > 3 and 2 ** 30 < keep < n
+    # who stays, and from where the places that are given up are filled
+    gone, come, left = [], [], even // 2
+    for j in range(0, n, piece):
+        m = mass[j:min(n, j + piece)]
+        equal = m == border
+        stays = (m > border) | (equal & (equal.long().cumsum(0) <= left))
+        left = max(0, left - int(equal.sum()))
+        here = max(0, min(keep - j, len(m)))
+        gone.append((~stays[:here]).nonzero()[:, 0].add_(j).int())
+        come.append(stays[here:].nonzero()[:, 0].add_(j + here).int())
+    del m, equal, stays
+    gone, come = torch.cat(gone), torch.cat(come)
+    assert gone.numel() == come.numel()
+    want = index.clone()
+    for i in range(0, gone.numel(), piece):
+        want[gone[i:i + piece].long()] = come[i:i + piece]
+    del gone, come
+    k, v = index.clone(), index.clone()
+    lens, budget = (torch.tensor([x], dtype=torch.int32).cuda() for x in (n, keep))
+    new = knn.cache_evict(k.view(torch.bfloat16).view(*shape, 2), v.view(torch.bfloat16).view(*shape, 2), mass.view(shape),
+                          pages, lens, budget, max_keys=n)
+    assert new.tolist() == [keep]
+    assert torch.equal(k, want) and torch.equal(v, want)
+    for j in range(0, keep, piece):  # and each weight went with its token
+        w = want[j:min(keep, j + piece)].long()
+        assert torch.equal(mass[j:j + len(w)], ((w * 2654435761 >> 8) & 0xffffff).float())
