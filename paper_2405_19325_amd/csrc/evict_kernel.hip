@@ -21,6 +21,15 @@
 // lists those between.  A second launch finds the border in the few that are
 // listed (or, where it lies elsewhere, in all), and with it each segment's
 // share of the moves, which a last one makes.
+//
+// What bounds it.  A step's few moves: waits, one behind the other; 512 heads of
+// 4,100 tokens in 19 us, 7 until their loads are on the way, 5 for these and the
+// ledger of afterwards, 2 for the border, 3 for the lists, 2 for the moves.  A
+// prompt's cut: the moves, at 5.2 to 5.6 TB/s read and written (keys of 128
+// heads 31 us of 58; two prompts of 131,072 tokens to an eighth 46 of 101, behind
+// 19 for the counts and 24 for the border and the lists).  The order is found
+// by counting, not by sorting: it reads each mass once, or twice where heads are
+// long.
 #include "lm_device.h"
 
 namespace knnlm {

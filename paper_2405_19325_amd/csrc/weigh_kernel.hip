@@ -19,8 +19,10 @@
 // a multiplication and a sum for 64 weights, beside 16 of the matrix cores.  A
 // wave holds 64 keys in the registers that the instructions read, straight from
 // memory, and the queries lie in LDS, read by all waves of the workgroup; 64 rows
-// of 64 heads on 8 on 4 x 131,008 tokens: 575 us, 970 TFLOP/s (a large library
-// product: 1,190).
+// of 64 heads on 8 on 4 x 131,008 tokens: 564 us, 970 TFLOP/s (a large library
+// product: 1,190); the matrix cores are busy half of the time.  Where a call has
+// few tiles, waits are what it takes: 40 rows of 64 heads on 8 over 30 tokens 28
+// us with a workgroup a tile, 167 with as many as the tiles' cost asks for.
 #include "lm_device.h"
 #include "mfma_device.h"
 
