@@ -8,10 +8,15 @@
 // each (the largest entry).  A history has far fewer tokens than the vocabulary:
 // those that are touched are listed by the first thread that comes to each, and
 // the list is worked off by all.  Of logits the outcome is put among the copied
-// scores on their way (256 rows of 131,072: 84 us, 87 where it is written over
-// them); of probabilities it is written over them, since the scores would be
-// held beside the 64-bit functions' registers (19 us for 128 rows of 50,257, 22
-// to 33 the other way).
+// scores on their way (256 rows of 131,072: 3 us less than where it is written
+// over them); of probabilities it is written over them, since the scores would be
+// held beside the 64-bit functions' registers (4 to 15 us more for 128 rows of
+// 50,257).
+//
+// What bounds it.  256 rows of 131,072 fp32 logits with all steps take 81 us:
+// the copy and its mask 55 (4.9 TB/s), the histories 17, biases and the touched
+// tokens the rest, waits during which little is on its way; of 128 rows of
+// 50,257 probabilities, 18 us, the 64-bit functions take 3 and the histories 5.
 //
 // Logits are worked out in 32 bits; probabilities as logarithms in 64, since the
 // logarithm of a small one times a penalty, in 32 bits, would be off by 2^-18 of
@@ -23,7 +28,7 @@ namespace knnlm {
 
 namespace {
 
-constexpr int64_t kGrid = 1 << 20;      // rows of a row of the grid
+constexpr int64_t kGrid = 1 << 15;      // groups of rows of a row of the grid
 constexpr int kThreads = 1024;
 constexpr int kPer = 8;                 // tokens of a thread
 constexpr int kSlice = kPer * kThreads;
@@ -77,9 +82,10 @@ __device__ __forceinline__ float parameter(const float *p, int64_t t, float off)
     return isfinite(x) ? x : off;
 }
 
-// A slice of a row's scores.  LDS: words [slice], where there are biases the last of each [slice], and the list.
+// A slice of a row's scores; the grid's x goes through 2^log2 rows and their
+// slices.  LDS: words [slice], where there are biases the last of each [slice], and the list.
 template <knn_dtype DT, bool PROBS>
-__global__ __launch_bounds__(kThreads, 8) void k_adjust(AdjustArgs a) {
+__global__ __launch_bounds__(kThreads, 8) void k_adjust(AdjustArgs a, int log2) {
     using Ty = Type<DT>;
     constexpr int VEC = Ty::VEC, GROUPS = Ty::GROUPS;
     extern __shared__ __align__(16) uint32_t lds[];
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(kThreads, 8) void k_adjust(AdjustArgs a) {
     constexpr uint32_t LIST = kSlice - kSlice / 16 - 2;
     const int tid = static_cast<int>(threadIdx.x);
     const uint32_t off = PROBS ? 0u : Ty::narrow(-INFINITY);
-    const int64_t t = static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.x;
+    const int64_t t = ((static_cast<int64_t>(blockIdx.z) * kGrid + blockIdx.y) << log2) + (blockIdx.x & ((1u << log2) - 1u));
     if (t >= a.rows) return;
     int64_t s = t, first = t;
     if (a.row_offsets != nullptr) {
@@ -105,7 +111,7 @@ __global__ __launch_bounds__(kThreads, 8) void k_adjust(AdjustArgs a) {
     char *out = static_cast<char *>(a.out) + t * a.out_stride * Ty::SIZE;
     // Places are counted from the 16 bytes that hold the first score; place p is token p - lead.
     const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(in) % 16) / Ty::SIZE;
-    const int v0 = static_cast<int>(blockIdx.y) * kSlice - lead;
+    const int v0 = static_cast<int>(blockIdx.x >> log2) * kSlice - lead;
     if (v0 >= a.V) return;
     const bool even = (reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(in)) % 16 == 0;
     const bool in_place = a.out == a.scores, copies = !in_place || a.allowed != nullptr;
@@ -280,10 +286,16 @@ __global__ __launch_bounds__(kThreads, 8) void k_adjust(AdjustArgs a) {
 template <knn_dtype DT, bool PROBS>
 hipError_t launch(const AdjustArgs &a, hipStream_t stream) {
     const int64_t slices = (a.V + Type<DT>::VEC - 1 + kSlice - 1) / kSlice;
-    const dim3 grid(static_cast<unsigned>(a.rows < kGrid ? a.rows : kGrid), static_cast<unsigned>(slices),
-                    static_cast<unsigned>((a.rows + kGrid - 1) / kGrid));
+    // Workgroups go to the eight dies in turn: with rows by eights the slices of one lie behind each other on one die, whose
+    // cache has the row's history after the first (256 rows of 131,072 logits: 158 MB read and 81 us, 253 and 84 with all
+    // rows' first slices before their second ones).  Probabilities, whose slices differ more in what they take: by 32 (128
+    // rows of 50,257 17.9 us, 18.6 that way, 19.7 by eights).
+    const int log2 = a.rows < 8 ? 0 : PROBS ? 5 : 3;
+    const int64_t groups = (a.rows + (1 << log2) - 1) >> log2;
+    const dim3 grid(static_cast<unsigned>(slices << log2), static_cast<unsigned>(groups < kGrid ? groups : kGrid),
+                    static_cast<unsigned>((groups + kGrid - 1) / kGrid));
     const size_t words = kSlice * (a.bias_tokens != nullptr ? 2 : 1) + kSlice / 2;
-    k_adjust<DT, PROBS><<<grid, kThreads, sizeof(uint32_t) * words, stream>>>(a);
+    k_adjust<DT, PROBS><<<grid, kThreads, sizeof(uint32_t) * words, stream>>>(a, log2);
     return hipGetLastError();
 }
 
