@@ -21,8 +21,8 @@
 // memory, and the queries lie in LDS, read by all waves of the workgroup; 64 rows
 // of 64 heads on 8 on 4 x 131,008 tokens: 564 us, 970 TFLOP/s (a large library
 // product: 1,190); the matrix cores are busy half of the time.  Where a call has
-// few tiles, waits are what it takes: 40 rows of 64 heads on 8 over 30 tokens 28
-// us with a workgroup a tile, 167 with as many as the tiles' cost asks for.
+// few tiles, waits are what it takes, and waves share a tile's columns: 40 rows of
+// 64 heads on 8 over 30 tokens 15 us (28 where a tile is one wave's).
 #include "lm_device.h"
 #include "mfma_device.h"
 
@@ -118,13 +118,16 @@ __device__ __forceinline__ uint64_t seen_of(const WeighArgs &a, const Tile &t, i
     return d0 <= -64 ? ~uint64_t{0} : bits << -d0 | first_bits(-d0);
 }
 
-template <knn_dtype DT, int D, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, int most) {
+// SHARED: where a workgroup has fewer tiles than waves, several of these share a
+// tile's columns; half as many waves, with the registers of two.
+template <knn_dtype DT, int D, int WAVES, bool SHARED>
+__global__ __launch_bounds__(WAVES * kWave, SHARED ? WAVES / 4 : 4) void k_key_weights(WeighArgs a, int most) {
     using Sh = Shape<D>;
     constexpr int KK = Sh::KK, B = Sh::B, THREADS = WAVES * kWave;
     extern __shared__ __align__(16) u32x4_t lds[];
     __shared__ int64_t sums[WAVES];
     __shared__ int64_t found[2];
+    __shared__ float parts_of[SHARED ? WAVES : 1][kWave];
     const Staged st{lds, reinterpret_cast<float *>(lds + static_cast<size_t>(most) * (D / 8)),
                     reinterpret_cast<int32_t *>(lds + static_cast<size_t>(most) * (D / 8)) + most};
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kWave - 1);
@@ -190,10 +193,19 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
             const int total_keys = static_cast<int>(t.total), last_block = (total_keys - 1) >> 4;
             const int length = static_cast<int>(t.length < t.total ? t.length : t.total);
             const int in_page = (1 << a.cache.page_log2) - 1;
+            auto put = [&](int64_t place, int j, float drawn, float mass) {
+                a.mass[place] = drawn + a.decay * mass;
+                if (j >= length && a.key_positions != nullptr)
+                    a.key_positions[place] = a.positions != nullptr ? a.positions[t.r0 + (j - length)] : j;
+            };
             // Rounds of one tile a wave, with the columns once more each; one round of all tiles where they fit LDS.
             const int step = cols > most ? WAVES : tile1 - tile0;
             for (int round = tile0; round < tile1; round += step) {
                 const int stop = step < tile1 - round ? round + step : tile1;
+                int share_log2 = 0;
+                if constexpr (SHARED)
+                    while (2 * (stop - round) << share_log2 <= WAVES) ++share_log2;
+                const int pace = WAVES >> share_log2, share = wave & ((1 << share_log2) - 1);
                 float sum[B] = {};
                 for (int c0 = 0; c0 < cols; c0 += most) {
                     const int n = cols - c0 < most ? cols - c0 : most, padded = (n + 15) & ~15;
@@ -203,10 +215,10 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                     // The pages of this wave's next tiles: block b of the i-th in lane i B + b, or -1.
                     constexpr int AHEAD = kWave / B;
                     int32_t pages = 0;
-                    for (int tile = round + wave, i = 0; tile < stop; tile += WAVES, ++i) {
+                    for (int tile = round + (wave >> share_log2), i = 0; tile < stop; tile += pace, ++i) {
                         const int block0 = tile * B, first = i % AHEAD * B;
                         if (first == 0) {
-                            const int block = (tile + lane / B * WAVES) * B + lane % B;
+                            const int block = (tile + lane / B * pace) * B + lane % B;
                             pages = table[min(block, last_block) << 4 >> a.cache.page_log2];
                             pages = pages >= 0 && pages < a.cache.n_pages ? pages : -1;
                         }
@@ -217,7 +229,7 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                         const bool mine = quad < B && part < total_keys - j0 && p >= 0;
                         const int64_t place = ((static_cast<int64_t>(p) * a.kv_heads + h) << a.cache.page_log2) + (j & in_page);
                         float mass = 0.0f;
-                        if (mine && j < length && a.decay != 0.0f && c0 + most >= cols) mass = a.mass[place];
+                        if (mine && j < length && a.decay != 0.0f && c0 + most >= cols && (!SHARED || share_log2 == 0)) mass = a.mass[place];
                         u32x4_t k[B][KK];
 #pragma unroll
                         for (int b = 0; b < B; ++b) {
@@ -246,7 +258,7 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                         bool plain = length - j0 >= Sh::KEYS;  // (a length may be all that 31 bits hold)
                         if (plain) {
 #pragma unroll 1
-                            for (int c = 0; c < padded; c += 16) {
+                            for (int c = 16 * share; c < padded; c += 16 << share_log2) {
                                 f32x4_t x[B];
                                 scores(c, x);
                                 const f32x4_t l = *reinterpret_cast<const f32x4_t *>(st.lse2 + c + 4 * quad);
@@ -265,7 +277,7 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
 #pragma unroll
                             for (int b = 0; b < B; ++b) w[b] = 0.0f;
 #pragma unroll 1
-                            for (int c = 0; c < padded; c += 16) {
+                            for (int c = 16 * share; c < padded; c += 16 << share_log2) {
                                 uint64_t seen[4];
                                 u32x4_t q[KK];
 #pragma unroll
@@ -297,11 +309,22 @@ __global__ __launch_bounds__(WAVES * kWave, 4) void k_key_weights(WeighArgs a, i
                         float drawn = sum[0];
 #pragma unroll
                         for (int b = 1; b < B; ++b) drawn = quad == b ? sum[b] : drawn;
-                        if (!mine) continue;
-                        a.mass[place] = drawn + a.decay * mass;
-                        if (j >= length && a.key_positions != nullptr)
-                            a.key_positions[place] = a.positions != nullptr ? a.positions[t.r0 + (j - length)] : j;
+                        if (SHARED && share_log2 > 0) {  // (one tile a wave: the parts are joined in a fixed order)
+                            parts_of[wave][lane] = drawn;
+                            continue;
+                        }
+                        if (mine) put(place, j, drawn, mass);
                     }
+                    if (!SHARED || share_log2 == 0 || c0 + most < cols) continue;
+                    __syncthreads();
+                    const int tile = round + (wave >> share_log2), j0 = tile * Sh::KEYS, part = 16 * quad + col;
+                    if (share > 0 || tile >= stop || quad >= B || part >= total_keys - j0) continue;
+                    const int j = static_cast<int>(static_cast<uint32_t>(j0) + part);
+                    const int64_t place = place_of(a.cache, a.kv_heads, s, h, j);
+                    if (place < 0) continue;
+                    float drawn = parts_of[wave][lane];
+                    for (int w = 1; w < 1 << share_log2; ++w) drawn += parts_of[wave + w][lane];
+                    put(place, j, drawn, j < length && a.decay != 0.0f ? a.mass[place] : 0.0f);
                 }
             }
         }
@@ -560,16 +583,14 @@ void launch_few(const WeighArgs &a, hipStream_t stream) {
     k_key_weights_few<DT, D, NT><<<dim3(static_cast<unsigned>(blocks)), 4 * kWave, 0, stream>>>(a);
 }
 
-template <knn_dtype DT, int D, int WAVES>
-void launch(const WeighArgs &a, int most, hipStream_t stream) {
-    using Sh = Shape<D>;
-    const size_t lds = static_cast<size_t>(most) * (Sh::ROW + 8);
+template <knn_dtype DT, int D, int WAVES, bool SHARED>
+void launch(const WeighArgs &a, int most, double tiles, hipStream_t stream) {
+    const size_t lds = static_cast<size_t>(most) * (Shape<D>::ROW + 8);
     const size_t fit = (size_t{156} << 10) / (lds + 1024);
     const int64_t room = fit * WAVES > 16 ? 16 / WAVES : fit < 1 ? 1 : static_cast<int64_t>(fit);  // workgroups of a CU
-    const double tiles = static_cast<double>(a.S) * a.kv_heads * static_cast<double>(tiles_of(a.max_keys, Sh::KEYS));
     // (A workgroup a tile where there are so few: another head's queries are another wait.)
     const int64_t most_blocks = kCus * room, blocks = tiles < most_blocks ? static_cast<int64_t>(tiles) : most_blocks;
-    k_key_weights<DT, D, WAVES><<<dim3(static_cast<unsigned>(blocks)), WAVES * kWave, lds, stream>>>(a, most);
+    k_key_weights<DT, D, WAVES, SHARED><<<dim3(static_cast<unsigned>(blocks)), WAVES * kWave, lds, stream>>>(a, most);
 }
 
 template <knn_dtype DT, int D>
@@ -582,10 +603,22 @@ hipError_t launch(const WeighArgs &a, hipStream_t stream) {
     if (most <= 16) launch_few<DT, D, 1>(a, stream);
     else if (most <= 32) launch_few<DT, D, 2>(a, stream);
     else if (D > 64 && most <= 96) launch_few<DT, (D > 64 ? D : 128), 6>(a, stream);
-    // Four waves a workgroup while four of these fit a CU's LDS with their queries; else eight, or all sixteen.
-    else if (most * 4 <= Shape<D>::MOST) launch<DT, D, 4>(a, most, stream);
-    else if (most * 2 <= Shape<D>::MOST) launch<DT, D, 8>(a, most, stream);
-    else launch<DT, D, 16>(a, most, stream);
+    else {
+        const double tiles =
+            static_cast<double>(a.S) * a.kv_heads * static_cast<double>(tiles_of(a.max_keys, Shape<D>::KEYS));
+        // Eight waves that share a tile's columns while there is at most a tile a CU, or so many that their columns' queries
+        // take over 40 KiB and each has several of its own: the waits of one tile behind the other weigh more than half as
+        // many waves.  Measured in turn, us, this way and the other: 64 rows of 64 heads on 8 over 2 x 300 tokens 18 and 38, as
+        // trees 22 and 59; 8 x 400 27 and 46; 8 x 900 34 and 48; 8 x 7,000 82 and 93, 4 x 130,000 556 and 548; at head_dim 64
+        // 8 x 900 35 and 40, 8 x 2,000 46 and 41; at 256 8 x 900 54 and 65, 8 x 2,000 99 and 89.  Of 160 columns, 8 x 1,500
+        // tokens on 2 key heads: 24 and 21.  1,024 columns on 2 x 30,000: 215 and 203.
+        const int several = most * Shape<D>::ROW <= 40960 ? 1 : D == 64 ? 6 : D == 256 || cols > Shape<D>::MOST ? 8 : 32;
+        if (tiles <= several * kCus) launch<DT, D, 8, true>(a, most, tiles, stream);
+        // Four waves a workgroup while four of these fit a CU's LDS with their queries; else eight, or all sixteen.
+        else if (most * 4 <= Shape<D>::MOST) launch<DT, D, 4, false>(a, most, tiles, stream);
+        else if (most * 2 <= Shape<D>::MOST) launch<DT, D, 8, false>(a, most, tiles, stream);
+        else launch<DT, D, 16, false>(a, most, tiles, stream);
+    }
     return hipGetLastError();
 }
 

@@ -296,6 +296,25 @@ def test_column_counts_of_every_kernel(dtype, d):
         check(batch(dtype, rows, [300, 77][:len(rows)], heads, d, 32, seed=d + rows[0]), decay=0.5)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("tree", [False, True])
+def test_column_counts_under_high_hints(d, tree):
+    """As many columns in calls that may have many tiles, which waves do not share."""
+    for rows, heads in (([13], (16, 2)), ([31, 2], (8, 2)), ([50, 9], (16, 2)), ([70, 3], (16, 2)), ([150], (16, 2))):
+        x = batch("bf16", rows, [300, 77][:len(rows)], heads, d, 32, seed=d + rows[0], width=30000, tree=tree)
+        check(x, decay=0.5, hints=False)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_tiles_whose_columns_waves_share(d):
+    """More tiles than workgroups, from one a workgroup to more than it has waves."""
+    check(batch("bf16", [40] * 9, [1300, 1700, 60, 1999, 1111, 900, 1500, 2, 1700], (32, 2), d, 16, seed=d), decay=0.5)
+    check(batch("f16", [64, 3], [4000, 0], (12, 1), d, 64, seed=d + 1, tree=True))
+    x = batch("bf16", [40] * 5, [700, 900, 1, 500, 300], (64, 8), d, 16, seed=d + 2, path=True)
+    x["pages"][1, 20] = x["pages"][3, 0] = -1
+    check(x)
+
+
 def test_many_sequences():
     """More than a wave's lanes and than a workgroup's threads, some without rows or tokens."""
     g = np.random.RandomState(3)
