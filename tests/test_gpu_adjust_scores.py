@@ -315,3 +315,20 @@ def test_on_another_stream():
     call.run(side)
     side.synchronize()
     assert torch.equal(call.out, want)
+
+
+@pytest.mark.parametrize("rows,probs", [((1 << 18) + 9, False), ((1 << 20) + 33, True)])
+def test_more_rows_than_a_row_of_the_grid(rows, probs):
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.rand(rows, 5, generator=g, device="cuda") + 0.1
+    history = torch.randint(0, 5, (rows, 1), generator=g, device="cuda", dtype=torch.int32)
+    allowed = torch.randint(0, 32, (rows, 1), generator=g, device="cuda", dtype=torch.int32)
+    presence = torch.rand(rows, generator=g, device="cuda")
+    got = knn.adjust_scores(x, history, torch.ones(rows, dtype=torch.int32, device="cuda"), presence=presence,
+                            allowed=allowed, probabilities=probs)
+    off = torch.zeros(rows, 5, dtype=torch.float64, device="cuda").scatter_(1, history.long(), presence.double()[:, None])
+    want = x.double() * torch.exp(-off) if probs else x.double() - off
+    seen = (allowed >> torch.arange(5, device="cuda", dtype=torch.int32) & 1) != 0
+    want = torch.where(seen, want, 0.0 if probs else float("-inf"))
+    # one rounding to 32 bits, of a value of at most 1.1
+    assert ((got - want).abs()[seen] <= 2.0 ** -24 * 1.1 + 1e-12).all() and torch.equal(got[~seen].double(), want[~seen])
