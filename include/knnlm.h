@@ -597,9 +597,10 @@ knn_status knn_key_weights(const void *q, const float *lse, const void *k_cache,
  *   sinks, recent  >= 0.  Where more tokens than the budget are at such positions, those of the most mass stay.
  *   max_keys       host hint: at least every cache_lens[s]; at most table_width * page_size, and 2^31 - 1.
  *   mass_out, positions_out
- *                  as mass and key_positions, the ledger of afterwards: written at the indices that stay (places past
- *                  them are left as they are).  mass and key_positions themselves are written where they are given, or
- *                  NULL (the latter with key_positions NULL); apart from all else otherwise.
+ *                  as mass and key_positions, the ledger of afterwards: written at the indices that stay, all of them of
+ *                  a sequence left as it is, as far as it has pages (places past them are left as they are).  mass and
+ *                  key_positions themselves are written where they are given, or NULL (the latter with key_positions
+ *                  NULL); apart from all else otherwise.
  *   new_lens       [S] int32 out: min(cache_lens[s], budgets[s]), or cache_lens[s] of a sequence left as it is.
  *   workspace      knn_cache_evict_workspace_size() bytes, 256-byte aligned; contents on entry are ignored.
  *

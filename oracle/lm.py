@@ -157,12 +157,13 @@ def evict(k_cache, v_cache, mass, key_positions, pages, cache_lens, budgets, nex
     mass_to = np.array(mass if mass_out is None else mass_out)
     positions_to = None if key_positions is None else np.array(key_positions if positions_out is None else positions_out)
     n_pages, kv_heads, page_size, _ = k.shape
-    room = min(pages.shape[1] * page_size, math.inf if max_keys is None else max_keys)
+    room = pages.shape[1] * page_size
+    most = room if max_keys is None else min(room, max_keys)
     new_lens = np.array(cache_lens)
     for s, n in enumerate(int(x) for x in cache_lens):
         where = [place(pages, s, c, n_pages, page_size) for c in range(max(0, min(n, room)))]
         stay = len(where)
-        if 0 <= budgets[s] < n <= room and None not in where:
+        if 0 <= budgets[s] < n <= most and None not in where:
             stay = new_lens[s] = int(budgets[s])
         nxt = n if next_positions is None else int(next_positions[s])
         for h in range(kv_heads):

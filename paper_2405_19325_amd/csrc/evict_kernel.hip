@@ -252,7 +252,7 @@ __device__ __forceinline__ Border border_of(uint32_t rank, uint32_t least, uint3
 struct Head {
     int64_t s;
     int h;
-    int64_t n, keep;  // tokens; those that stay
+    int64_t n, keep;  // tokens, and those that stay; of a head that is left as it is, those that its table has room for
     int32_t recent_from;
     bool leave;       // left as it is
     bool vec;         // the ledgers lie on 16 bytes
@@ -280,7 +280,7 @@ __device__ __forceinline__ Head head_of(const EvictArgs &a, int64_t pair) {
     const int64_t recent_from = (a.next_positions != nullptr ? a.next_positions[x.s] : len) - a.recent;
     x.recent_from = static_cast<int32_t>(recent_from > -0x80000000LL ? recent_from : -0x80000000LL);
     x.leave = budget < 0 || budget >= n || n > limit;
-    x.n = n < limit ? n : limit;
+    x.n = n < room ? n : room;
     x.keep = x.leave ? x.n : budget;
     x.vec = ((reinterpret_cast<uintptr_t>(a.mass) | reinterpret_cast<uintptr_t>(a.key_positions) |
               reinterpret_cast<uintptr_t>(a.mass_out) | reinterpret_cast<uintptr_t>(a.positions_out)) % 16) == 0;
@@ -745,11 +745,12 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
         if (x.h == 0) put_len(a, x);
         if (x.leave || x.keep == 0) moves.count[pair] = 0;
     }
-    if (w >= seg.all) return;
-    if (x.leave || x.keep == 0) {
-        if (x.leave) carry_all(a, x, begin, end);
+    if (x.leave) {  // (its length may be more than max_keys, which the grid is for)
+        for (int64_t from = w * size; from < x.n; from += gridDim.y * size)
+            carry_all(a, x, from, from + size < x.n ? from + size : x.n);
         return;
     }
+    if (w >= seg.all || x.keep == 0) return;
     if (tid == 0) starts[seg.all] = between;
     Held<> t;  // the segment's own tokens, on their way while the border is looked for
     t.load_chunk(a, x, seg.start(w), begin, end);

@@ -372,3 +372,18 @@ def test_the_longest_head():
     for j in range(0, keep, piece):  # and each weight went with its token
         w = want[j:min(keep, j + piece)].long()
         assert torch.equal(mass[j:j + len(w)], ((w * 2654435761 >> 8) & 0xffffff).float())
+
+
+def test_sequences_longer_than_the_hint_keep_their_whole_ledger():
+    """Left as they are, with a ledger apart up to their lengths (or as far as their tables go), not up to max_keys."""
+    for lens, width, budgets, max_keys in (([100, 90, 20, 95, 200], None, [10, 20, 10, 0, 199], 95),
+                                           ([5000, 30, 3000], None, [10, 20, 10], 2500),
+                                           ([20000, 9000, 5, 12345, 70001], 1100, [2500, 800, 4, 12344, 0], 9000)):
+        x = batch(lens, 2, 64, 64 if width else 16, width=width, seed=17)
+        if width:
+            x["pages"][0, 250] = -1  # behind the hint: passed over
+            x["cache_lens"][4] = 1100 * 64 + 7  # longer than its table, whose last entries are no pages
+        for positions in (False, True):
+            kept = {n: t.clone() for n, t in x.items()}
+            new = check(kept, budgets, out=True, positions=positions, max_keys=max_keys)
+            assert int(new[0]) == lens[0] and torch.equal(kept["mass"], x["mass"])
