@@ -555,7 +555,7 @@ size_t knn_sample_workspace_size(int64_t rows, int64_t V, knn_dtype dtype);
  *                  whose source lies outside [0, source_count) adds nothing.
  *   lse            [source_count, q_heads] fp32.  Where it is not finite (a row that saw no key) the row adds nothing.
  *   tree_mask, max_rows, max_keys, scale
- *                  as in knn_tree_attention.
+ *                  as in knn_tree_attention; mask_words <= 2^28 (KNN_ERR_UNSUPPORTED above).
  *   decay          finite, >= 0.  0 starts anew: what mass held is not read.
  *   mass           [n_pages, kv_heads, page_size] fp32, beside the cache: read and written.
  *   key_positions  [n_pages, kv_heads, page_size] int32 or NULL: the rows' own places get positions[t].
@@ -655,7 +655,8 @@ size_t knn_cache_evict_workspace_size(int64_t S, int64_t kv_heads, int64_t max_k
  *
  * Logits are worked out in fp32, probabilities in 64 bits and rounded to fp32, before they are rounded to dtype; what no
  * step reaches keeps its bits.
- * V <= 2^24; history_width, bias_width and the rows of a call with row_tokens <= 2^28 (KNN_ERR_UNSUPPORTED above).
+ * V <= 2^24; history_width, bias_width, mask_words and the rows of a call with row_tokens <= 2^28 (KNN_ERR_UNSUPPORTED
+ * above).
  */
 knn_status knn_adjust_scores(const void *scores, const int32_t *history, const int32_t *history_lens,
                              const int32_t *prompt_lens, const int64_t *row_offsets, const int32_t *row_tokens,

@@ -64,6 +64,7 @@ knn_status check_evict(int64_t S, int64_t kv_heads, int64_t max_keys) {
 }
 
 constexpr int64_t kAdjustMaxWidth = int64_t{1} << 28;  // (occurrences are counted in 30 bits)
+constexpr int64_t kMaxMaskWords = int64_t{1} << 28;    // (weights find a mask's words in 32 bits)
 
 // The bytes from the first to the last of a buffer (null: none), in doubles: no sum of strides can pass them.
 struct Extent {
@@ -123,7 +124,7 @@ knn_status knn_tree_attention(const void *q, const void *k_cache, const void *v_
     if (st != KNN_OK) return st;
     if (max_keys > table_width * page_size || !isfinite(scale) || q_row_stride < 0 || q_head_stride < 0)
         return KNN_ERR_INVALID_ARG;
-    if (tree_mask != nullptr && mask_words * 32 < max_rows) return KNN_ERR_INVALID_ARG;
+    if (tree_mask != nullptr && mask_words < (max_rows + 31) / 32) return KNN_ERR_INVALID_ARG;
     // (the stride of a single row or head says nothing)
     if (((rows > 1 ? q_row_stride : 0) | (q_heads > 1 ? q_head_stride : 0)) % 8 != 0 ||
         !aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16))
@@ -264,10 +265,10 @@ knn_status knn_key_weights(const void *q, const float *lse, const void *k_cache,
     if (max_keys > table_width * page_size || !isfinite(scale) || !isfinite(decay) || decay < 0.0f ||
         q_row_stride < 0 || q_head_stride < 0)
         return KNN_ERR_INVALID_ARG;
-    if (tree_mask != nullptr && mask_words * 32 < max_rows) return KNN_ERR_INVALID_ARG;
+    if (tree_mask != nullptr && mask_words < (max_rows + 31) / 32) return KNN_ERR_INVALID_ARG;
     // (the stride of a single row or head says nothing)
     if (((source_count > 1 ? q_row_stride : 0) | (q_heads > 1 ? q_head_stride : 0)) % 8 != 0 || !aligned(q, 16) ||
-        !aligned(k_cache, 16) || source_count > 0x7fffffff)
+        !aligned(k_cache, 16) || source_count > 0x7fffffff || (tree_mask != nullptr && mask_words > kMaxMaskWords))
         return KNN_ERR_UNSUPPORTED;
     const double places = static_cast<double>(n_pages) * kv_heads * page_size;
     const Extent outputs[] = {dense(mass, places, 4), dense(key_positions, places, 4)};
@@ -371,8 +372,8 @@ knn_status knn_adjust_scores(const void *scores, const int32_t *history, const i
     const int size = dtype == KNN_F32 ? 4 : 2;
     const int64_t most = kAdjustMaxWidth;
     if (S > 0x7fffffff || (history != nullptr && history_width > most) || (bias_tokens != nullptr && bias_width > most) ||
-        (row_tokens != nullptr && rows > most) || (tree_mask != nullptr && mask_words > most) || !aligned(scores, size) ||
-        !aligned(out, size))
+        (row_tokens != nullptr && rows > most) || (tree_mask != nullptr && mask_words > kMaxMaskWords) ||
+        !aligned(scores, size) || !aligned(out, size))
         return KNN_ERR_UNSUPPORTED;
     const bool in_place = out == scores && (rows == 1 || out_stride == row_stride);
     const Extent outputs[] = {dense(out, static_cast<double>(rows - 1) * out_stride + V, size)};

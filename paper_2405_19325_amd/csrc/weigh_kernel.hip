@@ -103,7 +103,7 @@ __device__ __forceinline__ uint64_t seen_of(const WeighArgs &a, const Tile &t, i
     if (row == kNobody) return 0;
     if (a.tree_mask == nullptr) return first_bits(row - d0 + 1);
     const uint32_t *words = a.tree_mask + (t.r0 + row) * a.mask_words;
-    const int from = d0 < 0 ? 0 : d0, last = static_cast<int>(a.mask_words) - 1;  // (a mask has at most 2^31 bits)
+    const int from = d0 < 0 ? 0 : d0, last = static_cast<int>(a.mask_words) - 1;  // (at most 2^28)
     uint32_t w[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {

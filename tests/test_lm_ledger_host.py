@@ -167,3 +167,15 @@ def test_oracle_adjust_by_hand():
     assert np.allclose(got, [0.25 ** 2 / 2, 0.0, 0.0, 1.0])
     assert lm.adjust(x, output=[0], repetition=math.nan, presence=math.inf, frequency=math.nan).tolist() == x
     assert lm.adjust(x, output=[0], repetition=-1.0).tolist() == x
+
+
+@pytest.mark.parametrize("words", [(1 << 28) + 1, 1 << 31, (1 << 31) + 100, 1 << 58, 1 << 59, (1 << 59) + 1, (1 << 63) - 1])
+def test_masks_that_are_too_wide(lib, words):
+    assert call(lib, "weigh", mask_words=words) == UNSUPPORTED
+    assert call(lib, "adjust", mask_words=words) == UNSUPPORTED
+
+
+def test_masks_of_fewer_bits_than_rows(lib):
+    for rows, words, expect in ((33, 1, INVALID), (33, 0, INVALID), (64, 1, INVALID), (33, -1, INVALID), (33, -(1 << 62), INVALID),
+                                (33, (1 << 28) + 1, UNSUPPORTED)):
+        assert call(lib, "weigh", rows=64, source_count=64, max_rows=rows, mask_words=words) == expect
