@@ -170,8 +170,8 @@ def _drawn(q: torch.Tensor, k_cache: torch.Tensor, pages: torch.Tensor, tree_mas
           f"q: [rows, q_heads, {d}] {k_cache.dtype} with dense heads")
     words = 0
     if tree_mask is not None:
-        _need(tree_mask.dim() == 2, "tree_mask: [rows, words]")
-        words = tree_mask.shape[1]
+        _need(tree_mask.dim() == 2 and tree_mask.shape[1] > 0, "tree_mask: [rows, words], a word at least")
+        words = tree_mask.shape[1]  # (one without elements has no address, and would say a chain)
         _flat("tree_mask", tree_mask, torch.int32, (rows, words))
     if max_rows is None:
         max_rows = rows if tree_mask is None else min(rows, 32 * words)
@@ -388,6 +388,7 @@ class ScoreAdjuster(_Call):
         if history is not None:
             width = history.shape[1]
         if tree_mask is not None:
+            _need(tree_mask.shape[1] > 0, "tree_mask: a word at least")  # (as in _drawn)
             words = tree_mask.shape[1]
         if bias_tokens is not None:
             n_bias = bias_tokens.shape[1]

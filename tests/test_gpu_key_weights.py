@@ -385,3 +385,21 @@ def test_the_longest_length(heads):
     assert np.all(np.abs(host(mass)[2, 0, :-1] - want[2, :-1]) <= off[2, :-1])
     assert float(mass[2, 0, -1]) == float(before[2, 0, -1])
     assert int(positions[2, 0, -2]) == total - 1 and int((positions == -5).sum()) == 3 * page - 1
+
+
+def test_masks_without_words_are_refused():
+    """A mask with no bit for any row is none, where the call without one would be a chain's."""
+    x = batch("bf16", [2, 1], [40, 5], (4, 2), 64, 16)
+    none = torch.empty(3, 0, dtype=torch.int32, device="cuda")
+    rows = dict(pages=x["pages"], row_offsets=x["row_offsets"], cache_lens=x["cache_lens"], tree_mask=none, max_rows=2,
+                max_keys=64)
+    before = x["mass"].clone()
+    with pytest.raises(ValueError):
+        knn.key_weights(x["q"], x["lse"], x["k_cache"], mass=x["mass"], **rows)
+    with pytest.raises(ValueError):
+        knn.tree_attention(x["q"], x["k_cache"], x["k_cache"].clone(), **rows)
+    with pytest.raises(ValueError):
+        knn.adjust_scores(torch.zeros(3, 10, device="cuda"), row_offsets=x["row_offsets"], tree_mask=none,
+                          row_tokens=torch.zeros(3, dtype=torch.int32, device="cuda"),
+                          presence=torch.ones(3, device="cuda"))
+    assert torch.equal(x["mass"], before)
