@@ -656,7 +656,7 @@ size_t knn_cache_evict_workspace_size(int64_t S, int64_t kv_heads, int64_t max_k
  * Logits are worked out in fp32, probabilities in 64 bits and rounded to fp32, before they are rounded to dtype; what no
  * step reaches keeps its bits.
  * V <= 2^24; history_width, bias_width, mask_words and the rows of a call with row_tokens <= 2^28 (KNN_ERR_UNSUPPORTED
- * above).
+ * above), the first three at least 1 where their buffers are given.
  */
 knn_status knn_adjust_scores(const void *scores, const int32_t *history, const int32_t *history_lens,
                              const int32_t *prompt_lens, const int64_t *row_offsets, const int32_t *row_tokens,

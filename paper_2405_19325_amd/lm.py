@@ -362,8 +362,9 @@ class ScoreAdjuster(_Call):
     of which the first prompt_lens [S] are the prompt; row_offsets [S+1] int64 gives the sequences' rows (None: each row
     is a sequence); row_tokens [rows] int32, the tokens that the rows were run on, count for the rows that see them
     (tree_mask [rows, words] int32, see tree_words; None: a chain).  repetition, presence, frequency [rows] fp32 or None:
-    1, 0 and 0 (off).  bias_tokens [S, n] int32 with bias_values [S, n] fp32.  allowed [rows, (V + 31) // 32] int32, bit
-    v & 31 of word v >> 5 for each token that may be drawn.  out (allocated where it is not given) may be scores itself.
+    1, 0 and 0 (off).  bias_tokens [S, n] int32 with bias_values [S, n] fp32.  Tables without
+    columns hold nothing.  allowed [rows, (V + 31) // 32] int32, bit v & 31 of word v >> 5 for each token that may be
+    drawn.  out (allocated where it is not given) may be scores itself.
     """
 
     def __init__(self, scores: torch.Tensor, history: Optional[torch.Tensor] = None,
@@ -401,6 +402,10 @@ class ScoreAdjuster(_Call):
                 ("frequency", frequency, f32, (rows,)), ("bias_tokens", bias_tokens, i32, (S, n_bias)),
                 ("bias_values", bias_values, f32, (S, n_bias)), ("allowed", allowed, i32, (rows, (V + 31) // 32))):
             _flat(name, t, dtype, shape)
+        if history is not None and history_lens is not None and width == 0:  # nothing has been drawn yet
+            history = history_lens = prompt_lens = None
+            if row_tokens is None:
+                repetition = presence = frequency = None  # (of occurrences, of which there are none)
         own = ()
         if out is None:
             out = torch.empty((rows, V), dtype=scores.dtype, device=scores.device)

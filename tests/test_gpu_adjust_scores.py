@@ -332,3 +332,20 @@ def test_more_rows_than_a_row_of_the_grid(rows, probs):
     want = torch.where(seen, want, 0.0 if probs else float("-inf"))
     # one rounding to 32 bits, of a value of at most 1.1
     assert ((got - want).abs()[seen] <= 2.0 ** -24 * 1.1 + 1e-12).all() and torch.equal(got[~seen].double(), want[~seen])
+
+
+@pytest.mark.parametrize("probs", [False, True])
+def test_histories_and_biases_of_no_entries(probs):
+    """Tables without columns are none at all, as a program has them that has drawn nothing yet."""
+    c = batch(6, 500, probs=probs, drafts=[4, 2], bias=3, grammar=True, seed=16)
+    none = dict(history=c["history"][:, :0], bias_tokens=c["bias_tokens"][:, :0], bias_values=c["bias_values"][:, :0])
+    for some in (("history",), ("bias_tokens", "bias_values"), tuple(none)):
+        check(dict(c, **{n: none[n] for n in some}))
+    no_drafts = {n: t for n, t in c.items() if n not in ("row_tokens", "tree_mask")}
+    check(dict(no_drafts, history=torch.empty(2, 0, dtype=torch.int32, device="cuda")))
+    got = knn.adjust_scores(**dict({n: t for n, t in no_drafts.items() if n != "allowed"}, **none))
+    assert torch.equal(got, c["scores"])
+    with pytest.raises(ValueError):
+        knn.adjust_scores(**dict(c, history=none["history"], history_lens=c["history_lens"][:1]))
+    with pytest.raises((ValueError, knn.KnnError)):
+        knn.adjust_scores(c["scores"], history=c["history"], row_offsets=c["row_offsets"])
