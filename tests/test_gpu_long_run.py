@@ -1,6 +1,8 @@
 """A long run of decoding on a cache with a budget, as the calls are made together: rows are appended at positions of their
 own, attend, give the keys they saw their weight, the keys of least weight leave; a token is drawn from scores with
 penalties.  Once step by step against the oracle, once with a tree of drafts, once captured and replayed."""
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -249,3 +251,45 @@ def test_steps_in_a_graph():
         for x, y in zip(a.state(), b.state()):
             assert torch.equal(x, y)
     assert a.lens.tolist() == [BUDGET, BUDGET]
+
+
+def test_the_example_of_the_readme():
+    """Its lines as they stand there, step after step: the first tokens and the last ones are never evicted."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        block = next(b for b in f.read().split("```")[1::2] if "knn.CacheEvict" in b)
+    setup, step = block.removeprefix("python\n").rstrip("\n").rsplit("\n", 1)
+    assert "evict.run()" in step
+    n, per, budget, page, width = 290, 8, 300, 64, 128
+    g = torch.Generator().manual_seed(5)
+    dev = dict(device="cuda")
+    shape = (S * width, HK, page, D)
+    x = {"knn": knn, "added": per, "table": torch.arange(S * width, dtype=torch.int32, **dev).view(S, width),
+         "lens": torch.full((S,), n, dtype=torch.int32, **dev), "budgets": torch.full((S,), budget, dtype=torch.int32, **dev),
+         "next_positions": torch.full((S,), n, dtype=torch.int32, **dev),
+         "depths": torch.zeros(S * per, dtype=torch.int32, **dev), "mass": torch.full(shape[:3], 5.0, **dev),
+         "where": torch.arange(width * page, dtype=torch.int32, **dev).view(1, width, 1, page).expand(
+             S, width, HK, page).reshape(shape[:3]).contiguous(),
+         "p_m": torch.softmax(torch.randn(S, V, generator=g), 1).cuda(),
+         "history": torch.randint(0, V, (S, 50), generator=g, dtype=torch.int32).cuda(),
+         "history_lens": torch.full((S,), 50, dtype=torch.int32, **dev), "prompt_lens": torch.full((S,), 9, dtype=torch.int32, **dev),
+         "penalty": torch.full((S,), 1.2, **dev), "grammar": torch.full((S, (V + 31) // 32), -1, dtype=torch.int32, **dev)}
+    x["where"].masked_fill_(x["where"] >= n, -1)
+    x["mass"].masked_fill_((x["where"] >= 0) & (x["where"] < 4), 0.0)  # the first tokens have drawn least
+    x["k_cache"], x["v_cache"] = (torch.randn(shape, generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    x["rows"] = dict(pages=x["table"], row_offsets=torch.arange(S + 1, dtype=torch.int64, **dev) * per, cache_lens=x["lens"])
+    q, k, v = (torch.randn(S * per, h, D, generator=g).to(torch.bfloat16).cuda() for h in (H, HK, HK))
+    x["append"] = knn.KVAppend(k, v, x["k_cache"], x["v_cache"], q=q, positions=x["depths"], **x["rows"])
+    x["attend"] = knn.TreeAttention(x["append"].q_out, x["k_cache"], x["v_cache"], max_rows=16, max_keys=8192, want_lse=True,
+                                    **x["rows"])
+    exec(setup, x)
+    at = n
+    for _ in range(12):
+        x["depths"].copy_(torch.arange(at, at + per, dtype=torch.int32, **dev).repeat(S))
+        x["append"].run()
+        x["attend"].run()
+        exec(step, x)
+        at += per
+        assert x["lens"].tolist() == [min(budget, at)] * S and x["scores"].shape == (S, V)
+        places = x["where"].view(S, width, HK, page).permute(0, 2, 1, 3).reshape(S, HK, -1)[:, :, :min(budget, at)]
+        for kept in places.reshape(S * HK, -1).tolist():
+            assert len(set(kept)) == len(kept) and {0, 1, 2, 3, *range(at - 256, at)} <= set(kept)
