@@ -561,8 +561,9 @@ size_t knn_sample_workspace_size(int64_t rows, int64_t V, knn_dtype dtype);
  *   key_positions  [n_pages, kv_heads, page_size] int32 or NULL: the rows' own places get positions[t].
  *   positions      [rows] int32 or NULL: the cache index.  Only with key_positions.
  *
- * A sequence without rows keeps its masses.  Places past a sequence's tokens are left as they are; those of a page that
- * two sequences share get the weight of either.  mass and
+ * A sequence without rows keeps its masses.  Places past a sequence's tokens are left as they are.  A page belongs to
+ * one sequence with rows: where two have the same page, both read and write its masses in no order, and what these
+ * are afterwards (and so what is evicted by them) is not defined; all other places get what is said here.  mass and
  * key_positions lie apart from all that is read and from each other.  Sums are in fp32, in an order that does not
  * depend on how workgroups run.  Sizes, alignment and strides as knn_tree_attention serves them.
  */

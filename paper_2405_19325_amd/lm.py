@@ -252,7 +252,7 @@ class KeyWeights(_Call):
     gave it; mass [n_pages, kv_heads, page_size] fp32 (zeros to begin with).  decay: the share that earlier weights keep.
     source_rows [rows] int32 as in KVAppend: an accepted path out of a draft's rows.  key_positions [n_pages, kv_heads,
     page_size] int32 gets positions [rows] int32 (default: the cache index) at the rows' own places.  max_rows, max_keys
-    and tree_mask as in TreeAttention.
+    and tree_mask as in TreeAttention.  Masses of a page that two sequences with rows share are not defined afterwards.
     """
 
     def __init__(self, q: torch.Tensor, lse: torch.Tensor, k_cache: torch.Tensor, pages: torch.Tensor,

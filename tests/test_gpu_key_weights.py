@@ -403,3 +403,16 @@ def test_masks_without_words_are_refused():
                           row_tokens=torch.zeros(3, dtype=torch.int32, device="cuda"),
                           presence=torch.ones(3, device="cuda"))
     assert torch.equal(x["mass"], before)
+
+
+@pytest.mark.parametrize("heads,rows", [((8, 2), [1, 2]), ((64, 1), [9, 3])])
+def test_a_page_that_two_sequences_share(heads, rows):
+    """What its places get is not said; all others have what the oracle says."""
+    x = batch("bf16", rows, [40, 500], heads, 64, 16, seed=17)
+    x["pages"][1, 0] = x["pages"][0, 0]
+    want, where, tol = want_of(x, decay=0.5)
+    knn.key_weights(x["q"], x["lse"], x["k_cache"], x["pages"], x["row_offsets"], x["cache_lens"], x["mass"],
+                    key_positions=x["key_positions"], positions=x["positions"], decay=0.5)
+    torch.cuda.synchronize()
+    err = np.abs(host(x["mass"]) - want) <= tol
+    assert np.delete(err, int(x["pages"][0, 0]), 0).all() and np.array_equal(ints(x["key_positions"]), where)
