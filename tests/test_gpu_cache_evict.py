@@ -387,3 +387,43 @@ def test_sequences_longer_than_the_hint_keep_their_whole_ledger():
             kept = {n: t.clone() for n, t in x.items()}
             new = check(kept, budgets, out=True, positions=positions, max_keys=max_keys)
             assert int(new[0]) == lens[0] and torch.equal(kept["mass"], x["mass"])
+
+
+WIDE = 1 << 20  # of a table: a segment is two chunks of 8,192 tokens
+
+
+@pytest.mark.parametrize("out", [False, True])
+@pytest.mark.parametrize("positions", [False, True])
+@pytest.mark.parametrize("kind", ["equal", "two", "by pages", "spread"])
+def test_segments_of_several_chunks(kind, positions, out):
+    lens = [40000, 20000, 9000, 5, 0, 16385, 16384]
+    x = shaped(batch(lens, 2, 64, 64, width=WIDE // 64, seed=18), kind, 18)
+    for budgets in ([20000, 16383, 100, 4, 0, 8193, 16383], [39999, 8192, 8999, 0, 0, 1, 8191]):
+        y = {n: t.clone() for n, t in x.items()}
+        check(y, budgets, [10 * n for n in lens] if positions else None, sinks=4, recent=64, max_keys=WIDE, out=out,
+              positions=positions)
+        if out:
+            assert torch.equal(y["mass"].view(torch.int32), x["mass"].view(torch.int32))
+
+
+@pytest.mark.parametrize("out", [False, True])
+def test_segments_of_several_chunks_with_many_protected_tokens_or_no_page(out):
+    lens = [40000, 20000, 16390]
+    x = batch(lens, 2, 64, 64, width=WIDE // 64, seed=19, masses="even")
+    for recent in (20000 - 30, 17000, 30000):  # just the budget of the first sequence; more than others'; more than all
+        check({n: t.clone() for n, t in x.items()}, [20000, 10000, 16389], sinks=30, recent=recent, max_keys=WIDE, out=out,
+              positions=False)
+    x["pages"][0, 500] = -1                      # in the last chunk
+    x["pages"][1, 128] = x["k_cache"].shape[0]   # the first one of the second chunk
+    for positions in (False, True):
+        check({n: t.clone() for n, t in x.items()}, [30000, 100, 16000], sinks=4, recent=64, max_keys=WIDE, out=out,
+              positions=positions)
+
+
+@pytest.mark.parametrize("max_keys", [None, 40000, WIDE])
+@pytest.mark.parametrize("n,budget", [(300, 100), (5000, 4000), (20000, 2500), (20000, 19999), (16385, 16384), (20000, 5)])
+def test_a_window_that_is_the_whole_budget(n, budget, max_keys):
+    """The first tokens and the last ones stay, whatever the masses; and one more, or one less, than these."""
+    for off in (0, 1, -1):
+        x = batch([n, n // 2, 30], 2, 64, 64, seed=20, masses="even", width=None if max_keys is None else max_keys // 64)
+        check(x, [budget, min(budget, n // 2 - 1), 29], sinks=4, recent=budget - 4 + off, max_keys=max_keys, positions=False)

@@ -179,3 +179,14 @@ def test_masks_of_fewer_bits_than_rows(lib):
     for rows, words, expect in ((33, 1, INVALID), (33, 0, INVALID), (64, 1, INVALID), (33, -1, INVALID), (33, -(1 << 62), INVALID),
                                 (33, (1 << 28) + 1, UNSUPPORTED)):
         assert call(lib, "weigh", rows=64, source_count=64, max_rows=rows, mask_words=words) == expect
+
+
+def test_adjust_refuses_more_than_its_counts_hold(lib):
+    """Occurrences have 30 bits beside two flags: of histories and of drafts 2^28 at most."""
+    over = (1 << 28) + 1
+    for name in ("history_width", "bias_width", "mask_words"):
+        assert call(lib, "adjust", **{name: over}) == UNSUPPORTED
+        assert call(lib, "adjust", **{name: over - 1}) == INVALID  # (such a buffer lies on the output here)
+    rows = dict(rows=over, V=10, row_stride=10, out_stride=10)
+    assert call(lib, "adjust", **rows) == UNSUPPORTED
+    assert call(lib, "adjust", row_tokens=None, tree_mask=None, **rows) == INVALID
