@@ -19,8 +19,11 @@
 // whose order gives two numbers that the border lies between but for one head
 // in thousands; each counts its segment's numbers above, at and below these and
 // lists those between.  A second launch finds the border in the few that are
-// listed (or, where it lies elsewhere, in all), and with it each segment's
-// share of the moves, which a last one makes.
+// listed, and with it each segment's share of the moves, which a last one makes.
+// Where the border lies elsewhere, or as many tokens are protected as stay or
+// more, each of the workgroups goes through the whole head for it: 16 heads of
+// 131,072 tokens to 16,384 in 201 us where 16,384 are protected, 281 where more
+// are, 89 where fewer.
 //
 // What bounds it.  A step's few moves: waits, one behind the other; 512 heads of
 // 4,100 tokens in 19 us, 7 until their loads are on the way, 5 for these and the
@@ -830,7 +833,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_evict_list(EvictArgs a, const C
             over[tid] = held[tid].above + held[tid].at_high + held[tid].between;
             even[tid] = held[tid].at_low;
         }
-    } else {  // the two numbers do not hold it, or more tokens are protected than stay
+    } else {  // the two numbers do not hold it, or as many tokens are protected as stay, or more
         auto all_of_them = [&](auto f) {
             for (int64_t at = 4 * tid; at < x.n; at += kRow) {
                 Held<1> four;
